@@ -37,7 +37,8 @@ typedef enum {
   PCTC_ERR_UNSUPPORTED = 3,         /* dtype/shape the kernels do not cover (see each function)  */
   PCTC_ERR_CUDA = 4,                /* a CUDA runtime or driver call failed (launch errors)      */
   PCTC_ERR_BAD_TARGET = 5,          /* reserved: bad targets are reported per utterance instead  */
-  PCTC_ERR_TIMEOUT = 6              /* a bounded device-side wait gave up (see pctc_workspace_status) */
+  PCTC_ERR_TIMEOUT = 6,             /* a bounded device-side wait gave up (see pctc_workspace_status) */
+  PCTC_ERR_HOST_MEMORY = 7          /* the host could not allocate a small table for its checks  */
 } pctc_status_t;
 
 typedef enum { PCTC_BF16 = 0, PCTC_FP32 = 1 } pctc_dtype_t;
@@ -281,6 +282,41 @@ pctc_status_t pctc_topk_decode(const pctc_problem_t* problem,
                                const int32_t* input_lengths, int32_t k,
                                int32_t* topk_classes, float* topk_logprobs,
                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Global gradient norm over many tensors, and clipping: what stands between the gradients of
+ * pruned_ctc_fwd_bwd (with those of the model below it) and the weight update.
+ *   S = sum over all tensors and values of g^2,  norm = sqrt(S),
+ *   f = min(1, max_norm / (norm + eps)),         out = f * g, rounded once to out's type.
+ * Values are squared in fp32 and summed in 64 bits in a fixed order (values that fp32 squares would
+ * lose are squared in 64 bits), so repeated calls agree bit for bit.  If the norm is not finite in fp32, f is 1:
+ * nothing is scaled, and the norm tells the caller.
+ *
+ * n tensors (any n >= 0; more than 1,024 take several launches), HOST arrays:
+ *   grads  [n] device pointers to contiguous values;  outs [n] likewise, or NULL: every tensor in place.
+ *          outs[i] == grads[i] is in place, too.  Any element-aligned address will do; 16-byte aligned ones
+ *          (grads[i] and outs[i] equally far from a 16-byte boundary) are read and written fastest.
+ *   numels [n] (0 allowed, its pointers are then not looked at), dtypes [n] pctc_dtype_t,
+ *   out_dtypes [n] or NULL (as dtypes): dtypes[i] or PCTC_FP32.
+ * No written buffer may overlap another buffer of the list (PCTC_ERR_INVALID_ARG); the same gradient
+ * may be read twice, and then counts twice.  max_norm > 0 (+inf: the norm only), eps >= 0.
+ *
+ * pctc_clip_grad_norm does it all; norm [1] fp32 (device).  For gradients that are sharded over ranks,
+ * pctc_grad_sqsum leaves S of this rank's values in sqsum [1] (device, fp64), the ranks add these up,
+ * and pctc_grad_scale does the rest (norm [1] or NULL).
+ * workspace: >= pctc_clip_workspace_bytes(n), 256-byte aligned; nothing in it outlives the call.
+ * These calls use `stream` only, may be captured into a CUDA graph and may be issued from several threads.
+ */
+pctc_status_t pctc_clip_workspace_bytes(int32_t n, size_t* bytes_out);
+pctc_status_t pctc_clip_grad_norm(int32_t n, const void* const* grads, void* const* outs,
+                                  const int64_t* numels, const int32_t* dtypes, const int32_t* out_dtypes,
+                                  float max_norm, float eps, float* norm,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+pctc_status_t pctc_grad_sqsum(int32_t n, const void* const* grads, const int64_t* numels, const int32_t* dtypes,
+                              double* sqsum, void* workspace, size_t workspace_bytes, void* stream);
+pctc_status_t pctc_grad_scale(int32_t n, const void* const* grads, void* const* outs,
+                              const int64_t* numels, const int32_t* dtypes, const int32_t* out_dtypes,
+                              const double* sqsum, float max_norm, float eps, float* norm, void* stream);
 
 /*
  * Contraction kernel on its own, for validation of the tensor-core path:

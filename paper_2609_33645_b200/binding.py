@@ -23,7 +23,8 @@ UTT_INFEASIBLE, UTT_NONFINITE, UTT_BAD_TARGET, UTT_SUBSET_OVERFLOW = 1, 2, 4, 8
 EXPORTS = ("pctc_workspace_bytes", "pctc_chunk_width", "pruned_ctc_fwd_bwd", "pruned_ctc_fwd_bwd_traced", "pctc_gemm_bf16",
            "pctc_workspace_status", "pctc_status_string", "pctc_host_call_scratch_bytes",
            "pruned_ctc_fwd_bwd_host", "pctc_subset_relabel_noalloc", "pctc_greedy_workspace_bytes",
-           "pctc_greedy_decode", "pctc_topk_workspace_bytes", "pctc_topk_decode")
+           "pctc_greedy_decode", "pctc_topk_workspace_bytes", "pctc_topk_decode",
+           "pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale")
 NOALLOC_MAX_V = 262144
 
 PHASES = ("prep", "lse", "subset_logp", "dp", "dlogits", "dh", "dw", "dbias", "finish")
@@ -131,6 +132,17 @@ def _configure(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.pctc_topk_decode.restype = ctypes.c_int
     lib.pctc_topk_decode.argtypes = [ctypes.POINTER(Problem), vp, vp, vp, i32p, ctypes.c_int32, vp, vp, vp,
                                      ctypes.c_size_t, vp]
+    i64p, vpp, size_p = ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(vp), ctypes.POINTER(ctypes.c_size_t)
+    lib.pctc_clip_workspace_bytes.restype = ctypes.c_int
+    lib.pctc_clip_workspace_bytes.argtypes = [ctypes.c_int32, size_p]
+    lib.pctc_clip_grad_norm.restype = ctypes.c_int
+    lib.pctc_clip_grad_norm.argtypes = [ctypes.c_int32, vpp, vpp, i64p, i32p, i32p, ctypes.c_float, ctypes.c_float,
+                                        vp, vp, ctypes.c_size_t, vp]
+    lib.pctc_grad_sqsum.restype = ctypes.c_int
+    lib.pctc_grad_sqsum.argtypes = [ctypes.c_int32, vpp, i64p, i32p, vp, vp, ctypes.c_size_t, vp]
+    lib.pctc_grad_scale.restype = ctypes.c_int
+    lib.pctc_grad_scale.argtypes = [ctypes.c_int32, vpp, vpp, i64p, i32p, i32p, vp, ctypes.c_float, ctypes.c_float,
+                                    vp, vp]
     lib.pctc_gemm_bf16.restype = ctypes.c_int
     lib.pctc_gemm_bf16.argtypes = [vp, vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                    ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp]
@@ -428,3 +440,117 @@ def topk_decode(hidden, W, bias, input_lengths, k, *, chunk=0, gemm_path=GEMM_AU
     if st != 0:
         raise PctcError(st, "pctc_topk_decode")
     return dict(classes=classes, logprobs=logprobs, workspace=workspace)
+
+
+def _run_on(dev, call, what, *args):
+    """`call(*args, stream)` on the current stream of `dev`, which is made the current device for the call."""
+    import torch
+
+    stream = ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+    if torch.cuda.current_device() == dev.index:
+        st = call(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            st = call(*args, stream)
+    if st != 0:
+        raise PctcError(st, what)
+
+
+def _grad_list(grads, what):
+    """(device, pointers, element counts, dtype codes) of a list of contiguous bf16 / fp32 CUDA tensors."""
+    import torch
+
+    if not grads:
+        raise ValueError(f"{what} must hold at least one tensor")
+    codes = {torch.bfloat16: PCTC_BF16, torch.float32: PCTC_FP32}
+    dev = grads[0].device
+    if dev.type != "cuda" or any(g.device != dev for g in grads):
+        raise ValueError(f"{what} must be CUDA tensors of one device")
+    try:
+        kinds = [codes[g.dtype] for g in grads]
+    except KeyError:
+        raise ValueError(f"{what} must be bf16 or fp32") from None
+    if not all([g.is_contiguous() for g in grads]):
+        raise ValueError(f"{what} must be contiguous")
+    n = len(grads)
+    return (dev, (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]), (ctypes.c_int64 * n)(*[g.numel() for g in grads]),
+            (ctypes.c_int32 * n)(*kinds))
+
+
+def _grad_outs(grads, out, dev):
+    """(pointers, dtype codes) of the tensors that the scaled gradients go to, or (None, None): in place."""
+    if out is None:
+        return None, None
+    if len(out) != len(grads) or any([o.shape != g.shape for o, g in zip(out, grads)]):
+        raise ValueError("out must hold one tensor of the same shape for every gradient")
+    odev, ptrs, _, kinds = _grad_list(out, "out")
+    if odev != dev:
+        raise ValueError("out must be on the gradients' device")
+    return ptrs, kinds
+
+
+def clip_workspace_bytes(n: int) -> int:
+    """Workspace of clip_grad_norm / grad_sqsum for n tensors."""
+    need = ctypes.c_size_t(0)
+    st = load().pctc_clip_workspace_bytes(int(n), ctypes.byref(need))
+    if st != 0:
+        raise PctcError(st, "pctc_clip_workspace_bytes")
+    return int(need.value)
+
+
+def _clip_workspace(n, dev, workspace):
+    import torch
+
+    need = clip_workspace_bytes(n)
+    if workspace is None or workspace.numel() < need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    return workspace
+
+
+def clip_grad_norm(grads, max_norm, *, out=None, eps=1e-6, workspace=None):
+    """Clip gradients by their global norm: every tensor times min(1, max_norm / (norm + eps)).
+
+    grads: contiguous CUDA tensors of one device, bf16 and fp32 in any mixture, scaled in place, or
+    into the tensors of `out` (same shapes; each of its gradient's type or fp32).  Returns a dict:
+    norm [1] fp32 on the device (nothing waits for it), grads (the scaled tensors) and the reusable
+    workspace.  If the norm is not finite nothing is scaled.  The same tensor may not be given twice.
+    """
+    import torch
+
+    grads = list(grads)
+    dev, ptrs, numels, kinds = _grad_list(grads, "grads")
+    outs, out_kinds = _grad_outs(grads, out, dev)
+    workspace = _clip_workspace(len(grads), dev, workspace)
+    norm = torch.empty(1, dtype=torch.float32, device=dev)
+    _run_on(dev, load().pctc_clip_grad_norm, "pctc_clip_grad_norm", len(grads), ptrs, outs, numels, kinds, out_kinds,
+            float(max_norm), float(eps), _dptr(norm), _dptr(workspace), ctypes.c_size_t(workspace.numel()))
+    return dict(norm=norm, grads=grads if out is None else list(out), workspace=workspace)
+
+
+def grad_sqsum(grads, *, workspace=None):
+    """Sum of the squares of all values of `grads` (as in clip_grad_norm): sqsum [1] fp64 on the device, and
+    the workspace.  Ranks that hold different shards add these up before grad_scale."""
+    import torch
+
+    grads = list(grads)
+    dev, ptrs, numels, kinds = _grad_list(grads, "grads")
+    workspace = _clip_workspace(len(grads), dev, workspace)
+    sqsum = torch.empty(1, dtype=torch.float64, device=dev)
+    _run_on(dev, load().pctc_grad_sqsum, "pctc_grad_sqsum", len(grads), ptrs, numels, kinds, _dptr(sqsum),
+            _dptr(workspace), ctypes.c_size_t(workspace.numel()))
+    return dict(sqsum=sqsum, workspace=workspace)
+
+
+def grad_scale(grads, sqsum, max_norm, *, out=None, eps=1e-6):
+    """The second half of clip_grad_norm, from a sum of squares [1] fp64 on the device."""
+    import torch
+
+    grads = list(grads)
+    dev, ptrs, numels, kinds = _grad_list(grads, "grads")
+    outs, out_kinds = _grad_outs(grads, out, dev)
+    if sqsum.dtype != torch.float64 or sqsum.numel() != 1 or sqsum.device != dev:
+        raise ValueError("sqsum must be one fp64 value on the gradients' device")
+    norm = torch.empty(1, dtype=torch.float32, device=dev)
+    _run_on(dev, load().pctc_grad_scale, "pctc_grad_scale", len(grads), ptrs, outs, numels, kinds, out_kinds,
+            _dptr(sqsum), float(max_norm), float(eps), _dptr(norm))
+    return dict(norm=norm, grads=grads if out is None else list(out))

@@ -216,6 +216,7 @@ const char* pctc_status_string(pctc_status_t s) {
     case PCTC_ERR_CUDA: return "CUDA error";
     case PCTC_ERR_BAD_TARGET: return "bad target";
     case PCTC_ERR_TIMEOUT: return "bounded device wait gave up";
+    case PCTC_ERR_HOST_MEMORY: return "out of host memory";
   }
   return "unknown status";
 }

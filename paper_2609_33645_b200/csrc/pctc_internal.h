@@ -5,7 +5,10 @@
 
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
+#include <stddef.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 namespace pctc {
 
@@ -30,6 +33,26 @@ __device__ __forceinline__ bool index_ok(long long idx, long long lo, long long 
   return false;
 }
 #endif
+
+// ---------------------------------------------------------------------------
+// Host checks of lists of buffers: a byte range that a call reads or writes.
+// ---------------------------------------------------------------------------
+struct Span {
+  size_t lo, hi;                // [lo, hi)
+  bool write;
+};
+// Whether a written range overlaps any other range of the list (sorts the list).
+inline bool spans_conflict(Span* s, size_t n) {
+  const auto before = [](const Span& a, const Span& b) { return a.lo < b.lo; };
+  if (!std::is_sorted(s, s + n, before)) std::sort(s, s + n, before);
+  size_t end_any = 0, end_write = 0;
+  for (size_t i = 0; i < n; ++i) {
+    if (s[i].lo < (s[i].write ? end_any : end_write)) return true;
+    end_any = std::max(end_any, s[i].hi);
+    if (s[i].write) end_write = std::max(end_write, s[i].hi);
+  }
+  return false;
+}
 
 // ---------------------------------------------------------------------------
 // Contractions:  acc(i,j) = sum_k A(i,k) * B(j,k),  then an epilogue.

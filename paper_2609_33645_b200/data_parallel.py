@@ -150,3 +150,21 @@ def pruned_ctc_fwd_bwd_data_parallel(hidden, W, bias, targets, input_lengths, ta
     elif res.get("dbias") is not None:
         dist.all_reduce(res["dbias"], group=group)
     return res
+
+
+def clip_grad_norm_data_parallel(grads, max_norm, *, group=None, sharded=False, out=None, eps=1e-6):
+    """Clip by the global gradient norm after the exchange step (`binding.clip_grad_norm` over ranks).
+
+    Replicated gradients (sharded=False, what `allreduce_rows` leaves): every rank holds the same values
+    and computes the same norm, bit for bit, so nothing is exchanged.  sharded=True: every value of the
+    gradient is held by one rank of `group`; the ranks add up their sums of squares (one fp64 number)
+    and each scales its own shard.  Returns norm [1] and grads.
+    """
+    import torch.distributed as dist
+
+    if not sharded or not dist.is_initialized():
+        r = binding.clip_grad_norm(grads, max_norm, out=out, eps=eps)
+        return dict(norm=r["norm"], grads=r["grads"])
+    sq = binding.grad_sqsum(grads)["sqsum"]
+    dist.all_reduce(sq, group=group)
+    return binding.grad_scale(grads, sq, max_norm, out=out, eps=eps)

@@ -1,0 +1,185 @@
+"""Gradient clipping on the GPU against 64-bit arithmetic on the same values.
+
+Tolerances: the norm is a sum of non-negative squares.  Up to eight values are squared and added in fp32
+(at most 8 roundings of 2^-24 relative), all else in 64 bits, so S is off by less than 8 * 2^-24 and the norm by
+half of that, and then rounded once: 5 * 2^-24.  A scaled value is g * f with f off by the norm's error and one
+rounding to fp32, times one fp32 rounding (7 * 2^-24), then rounded to its type (bf16: 2^-8)."""
+
+import math
+
+import pytest
+import torch
+
+from paper_2609_33645_b200 import binding, data_parallel
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NORM_TOL = 5 * 2.0 ** -24
+VALUE_TOL = {torch.float32: 8 * 2.0 ** -24, torch.bfloat16: 2.0 ** -8 + 8 * 2.0 ** -24}
+
+
+def reference(grads, max_norm, eps=1e-6):
+    norm = math.sqrt(sum(float((g.double() ** 2).sum()) for g in grads))
+    fits = math.isfinite(norm) and norm <= torch.finfo(torch.float32).max
+    f = min(1.0, max_norm / (norm + eps)) if fits else 1.0
+    return norm, [g.double() * f for g in grads]
+
+
+def close(got, want, dtype):
+    tiny = torch.finfo(dtype).tiny
+    assert bool(((got.double() - want).abs() <= VALUE_TOL[dtype] * want.abs() + tiny * 2.0 ** -7).all())
+
+
+def make(sizes, dtypes, scale, seed, offset=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    out = []
+    for i, s in enumerate(sizes):
+        dt = dtypes[i % len(dtypes)]
+        buf = torch.zeros(s + 16, device=DEV, dtype=dt)
+        v = buf[offset:offset + s]
+        v.normal_(std=scale * (1 + i % 3), generator=g)
+        out.append(v)
+    return out
+
+
+SIZES = [[1], [7], [8], [8191, 8192, 8193], [1000 * 64, 64, 1, 0, 3], [5] * 60, [300_001, 17, 65_536], [2, 3] * 700]
+
+
+@pytest.mark.parametrize("offset", [0, 1, 5])
+@pytest.mark.parametrize("dtypes", [(torch.float32,), (torch.bfloat16,), (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: f"{len(s)}x{max(s)}")
+def test_norm_and_values(sizes, dtypes, offset):
+    for over in (True, False):
+        grads = make(sizes, dtypes, 0.5, len(sizes), offset)
+        total = max(1, sum(sizes))
+        max_norm = (0.05 if over else 50.0) * math.sqrt(total)
+        before = [g.clone() for g in grads]
+        norm, want = reference(before, max_norm)
+        assert (norm > max_norm) == over
+        for mode in ("same", "fp32", "shifted", "place"):
+            if mode == "place":
+                r = binding.clip_grad_norm(grads, max_norm)
+                outs = grads
+            else:
+                outs = [torch.empty(g.numel() + 16, device=DEV, dtype=torch.float32 if mode == "fp32" else g.dtype)
+                        [3 if mode == "shifted" else 0:][:g.numel()] for g in grads]
+                r = binding.clip_grad_norm(grads, max_norm, out=outs)
+                for g, b in zip(grads, before):
+                    assert torch.equal(g, b)
+            assert float(r["norm"]) == pytest.approx(norm, rel=NORM_TOL)
+            for o, w, b in zip(outs, want, before):
+                close(o, w, o.dtype)
+                if not over:
+                    assert torch.equal(o.double(), b.double())
+
+
+def test_neighbours_of_the_gradients_are_left_alone():
+    for dt in (torch.bfloat16, torch.float32):
+        for off in range(8):
+            for n in (0, 1, 6, 7, 8, 9, 8200):
+                buf = torch.full((n + 32,), 7.0, device=DEV, dtype=dt)
+                buf[off:off + n] = 1.0
+                keep = buf.clone()
+                binding.clip_grad_norm([buf[off:off + n]], 1e-3)
+                assert torch.equal(buf[:off], keep[:off]) and torch.equal(buf[off + n:], keep[off + n:])
+                if n:
+                    assert float(buf[off:off + n].max()) < 1.0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("value", [0.0, 1e-30, 1e-38, 1e30, 3e38])
+def test_values_whose_squares_leave_fp32(dtype, value):
+    g = torch.full((1001,), value, device=DEV, dtype=dtype)
+    g[500:] = 0
+    norm, want = reference([g], 1.0)
+    r = binding.clip_grad_norm([g], 1.0)
+    if norm <= float(torch.finfo(torch.float32).max):
+        assert float(r["norm"]) == pytest.approx(norm, rel=NORM_TOL, abs=2.0 ** -149)
+    else:
+        assert float(r["norm"]) == math.inf          # beyond fp32: counts as not finite
+    close(g, want[0], dtype)
+
+
+def test_a_factor_below_the_normal_range():
+    g = torch.full((4,), 1.5e38, device=DEV)
+    norm, want = reference([g], 1e-3)
+    binding.clip_grad_norm([g], 1e-3)
+    close(g, want[0], torch.float32)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_a_norm_that_is_not_finite_scales_nothing(bad):
+    g = torch.randn(10_000, device=DEV)
+    g[1234] = bad
+    keep = g.clone()
+    r = binding.clip_grad_norm([g], 1e-3)
+    assert torch.equal(g.nan_to_num(1.5), keep.nan_to_num(1.5))
+    assert not math.isfinite(float(r["norm"]))
+    out = [torch.zeros_like(g)]
+    binding.clip_grad_norm([g], 1e-3, out=out)
+    assert torch.equal(out[0].nan_to_num(1.5), keep.nan_to_num(1.5))
+
+
+def test_two_halves_make_the_whole_and_repeats_agree_bitwise():
+    a = make([40_000, 999, 64], (torch.bfloat16, torch.float32), 0.3, 3)
+    b = [t.clone() for t in a]
+    c = [t.clone() for t in a]
+    ra = binding.clip_grad_norm(a, 2.0)
+    rb = binding.clip_grad_norm(b, 2.0)
+    sq = binding.grad_sqsum(c)["sqsum"]
+    rc = binding.grad_scale(c, sq, 2.0)
+    assert torch.equal(ra["norm"], rb["norm"]) and all(torch.equal(x, y) for x, y in zip(a, b))
+    # the partial sums are added in another order: 64 bits, then one rounding
+    assert float(rc["norm"]) == pytest.approx(float(ra["norm"]), rel=2.0 ** -23)
+    for x, y in zip(a, c):
+        close(y, x.double(), x.dtype)
+    # a norm without clipping
+    d = [t.clone() for t in c]
+    binding.clip_grad_norm(d, math.inf)
+    assert all(torch.equal(x, y) for x, y in zip(c, d))
+
+
+def test_data_parallel_form_without_a_group_is_the_plain_call():
+    a = make([1000, 64], (torch.float32,), 1.0, 5)
+    b = [t.clone() for t in a]
+    r = data_parallel.clip_grad_norm_data_parallel(a, 1.0, sharded=True)
+    s = binding.clip_grad_norm(b, 1.0)
+    assert torch.equal(r["norm"], s["norm"]) and all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_captured_into_a_graph_and_on_another_stream():
+    g = make([70_000, 33], (torch.bfloat16,), 0.2, 9)
+    out = [torch.zeros_like(t) for t in g]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        binding.clip_grad_norm(g, 1.0, out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    first = [t.clone() for t in out]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = binding.clip_grad_norm(g, 1.0, out=out)
+    for t in g:
+        t.mul_(2.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    norm, want = reference(g, 1.0)
+    assert float(r["norm"]) == pytest.approx(norm, rel=NORM_TOL)
+    for o, w, f in zip(out, want, first):
+        close(o, w, o.dtype)
+
+
+def test_gradients_of_the_head_are_clipped():
+    """The call as a training step makes it: gradients of the head, then clipping, then the update."""
+    g = torch.Generator(device=DEV).manual_seed(0)
+    hidden = torch.randn(2, 30, 64, device=DEV, generator=g)
+    W = torch.randn(500, 64, device=DEV, generator=g) / 8
+    bias = torch.zeros(500, device=DEV)
+    targets = torch.randint(1, 500, (2, 5), device=DEV, generator=g, dtype=torch.int32)
+    r = binding.pruned_ctc_fwd_bwd(hidden, W, bias, targets, [30, 20], [5, 3], 0)
+    grads = [r["dW"], r["dbias"], r["dH"]]
+    norm, want = reference(grads, 0.5)
+    c = binding.clip_grad_norm(grads, 0.5)
+    assert float(c["norm"]) == pytest.approx(norm, rel=NORM_TOL) and norm > 0.5
+    for x, w in zip(grads, want):
+        close(x, w, x.dtype)
