@@ -53,6 +53,7 @@ typedef enum { PCTC_GEMM_AUTO = 0, PCTC_GEMM_SIMT = 1 } pctc_gemm_path_t;
 #define PCTC_UTT_NONFINITE 2  /* loss not finite (NaN/Inf input, or empty retained lattice)  */
 #define PCTC_UTT_BAD_TARGET 4 /* a token equals blank_id or lies outside [0, V)              */
 #define PCTC_UTT_SUBSET_OVERFLOW 8 /* the batch has more selected classes than problem.max_K  */
+#define PCTC_UTT_STATE_FULL 16 /* prefix search: the state was not started for these sizes, or is full */
 
 /*
  * The problem of Section 3.1 / Algorithm 1, line 1.
@@ -262,8 +263,8 @@ pctc_status_t pctc_greedy_decode(const pctc_problem_t* problem,
 
 /*
  * The k best classes of every frame with their log-probabilities under the full-vocabulary
- * softmax: what a CTC prefix beam search (the paper's decoder, Section 5.1: beam 4; the search
- * itself is not part of this library) consumes per frame.  The head is applied in vocabulary
+ * softmax: what a CTC prefix beam search (the paper's decoder, Section 5.1: beam 4; here
+ * pctc_prefix_advance) consumes per frame.  The head is applied in vocabulary
  * chunks of problem->chunk columns (0: 4,096) as in the paper's recognition path (Appendix D);
  * a chunk's logits live in the workspace only until the frame's running k best and its running
  * log-sum-exp (Eq. "lognorm") have been updated, so no frames-by-vocabulary array exists.
@@ -282,6 +283,57 @@ pctc_status_t pctc_topk_decode(const pctc_problem_t* problem,
                                const int32_t* input_lengths, int32_t k,
                                int32_t* topk_classes, float* topk_logprobs,
                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * CTC prefix beam search (the paper's decoder, Section 5.1: beam 4) over the k best classes of every
+ * frame, as pctc_topk_decode gives them: the label sequences whose alignments -- all of them summed,
+ * as in the loss -- have the largest probability, `beams` of them at every frame.
+ *
+ * A prefix x carries pb (its alignments that end in blank) and pn (those that end in its last label).
+ * A frame with class probabilities p makes of it: x itself with pb' = (pb+pn) p[blank] and
+ * pn' = pn p[last(x)], and x c for every other class c of the frame with pn' = (c == last(x) ? pb : pb+pn) p[c];
+ * equal label sequences are added up.  The `beams` most probable go on; among equals stays come first, by
+ * slot, then (slot r, class number j) by r * k + j.  Classes that are not among a frame's k count as
+ * impossible, and so does a class under exp(-700) of the frame's best.  A class may stand at a frame once;
+ * again, it counts where it stands first.  Entries with class -1 or log-probability -inf are absent; NaN
+ * and +inf are absent and flag the utterance PCTC_UTT_NONFINITE.  Log-probabilities need not be normalised.
+ * If a frame leaves nothing possible, the utterance has no hypothesis from then on (PCTC_UTT_INFEASIBLE).
+ *
+ * The search lives in a caller-owned state buffer, so that frames can arrive in any portions (one at a
+ * time, too); the result does not depend on how they are cut.  Probabilities are carried in 64 bits.
+ */
+typedef struct {
+  int32_t N;             /* utterances                                                        */
+  int32_t T;             /* row count of classes[n] and logprobs[n] in this call              */
+  int32_t k;             /* classes per frame, 1 .. 32                                        */
+  int32_t beams;         /* prefixes kept, 1 .. 32                                            */
+  int32_t blank_id;
+  int32_t max_frames;    /* frames the state has room for, per utterance, over all its calls  */
+} pctc_prefix_t;
+
+/* Size of the state (T and k do not matter): per utterance 1.7 KB and 8 bytes per beam and frame. */
+pctc_status_t pctc_prefix_state_bytes(const pctc_prefix_t* problem, size_t* bytes_out);
+
+/*
+ * Takes lengths[n] frames (HOST, 0 <= lengths[n] <= T and max_frames) of every utterance.
+ *   classes [N,T,k] int32, logprobs [N,T,k] fp32 (device); frames from lengths[n] on are not read.
+ *   fresh 1: starts the state (whatever it held), 0: goes on.  A call that goes on with other sizes than the
+ *   state was started with, or beyond max_frames, leaves that utterance's hypotheses as they are and
+ *   flags it PCTC_UTT_STATE_FULL.
+ *   state: >= pctc_prefix_state_bytes(), 256-byte aligned, state_bytes its size.
+ */
+pctc_status_t pctc_prefix_advance(const pctc_prefix_t* problem, const int32_t* classes, const float* logprobs,
+                                  const int32_t* lengths, int32_t fresh, void* state, size_t state_bytes,
+                                  void* stream);
+/*
+ * The hypotheses so far, best first (the state is left as it is):
+ *   tokens [N, beams, token_stride] padded with -1 (labels from token_stride on are not written),
+ *   token_lengths [N, beams], scores [N, beams] fp32: the log-probability; -inf (and length 0) where there are
+ *   fewer hypotheses than beams; utt_flags [N] or NULL.
+ */
+pctc_status_t pctc_prefix_read(const pctc_prefix_t* problem, const void* state, size_t state_bytes,
+                               int32_t* tokens, int32_t token_stride, int32_t* token_lengths, float* scores,
+                               int32_t* utt_flags, void* stream);
 
 /*
  * Global gradient norm over many tensors, and clipping: what stands between the gradients of

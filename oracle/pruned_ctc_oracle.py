@@ -465,3 +465,94 @@ def discarded_mass(loss_beam, loss_exact):
     """Delta_n = L_beta,n - L_n and delta_n = 1 - exp(-Delta_n)  (Appendix B.3)."""
     delta_big = np.asarray(loss_beam, dtype=np.float64) - np.asarray(loss_exact, dtype=np.float64)
     return delta_big, -np.expm1(-delta_big)
+
+
+# ----------------------------------------------------------------------------
+# CTC prefix beam search over the k best classes of every frame
+# ----------------------------------------------------------------------------
+
+def frame_probabilities(classes, logprobs):
+    """One frame's (class, probability) pairs in the order given, and the frame's shift: probabilities are
+    exp(logprob - shift) to 24 significant bits with shift the largest logprob; absent entries (class -1,
+    a logprob that is not finite, a class's second place, under exp(-700) of the best) come out as (-2, 0).
+    Also whether an entry was NaN or +inf."""
+    seen, bad = set(), False
+    kept = []
+    for c, v in zip(classes, logprobs):
+        c, v = int(c), float(v)
+        if c >= 0 and (np.isnan(v) or v == np.inf):
+            bad = True
+        ok = c >= 0 and np.isfinite(v) and c not in seen
+        if ok:
+            seen.add(c)
+        kept.append((c, v) if ok else (-2, -np.inf))
+    shift = max((v for _, v in kept), default=-np.inf)
+    if shift == -np.inf:
+        return [(-2, 0.0)] * len(kept), 0.0, bad
+    out = []
+    for c, v in kept:
+        if c < 0 or v - shift < -700.0:
+            out.append((-2, 0.0))
+            continue
+        m, e = np.frexp(np.exp(np.float64(v) - np.float64(shift)))
+        # half up on the magnitude, 24 bits
+        out.append((c, float(np.ldexp(np.floor(m * 2.0 ** 24 + 0.5), int(e) - 24))))
+    return out, shift, bad
+
+
+def prefix_beam_search(classes, logprobs, n_frames, blank, beams):
+    """The `beams` label sequences with the largest summed alignment probability, frame by frame.
+
+    classes, logprobs [T, k].  Returns (hypotheses, bad): a list of (labels, log-probability), best first, and
+    whether some entry was NaN or +inf.  A prefix is a node of a tree of labels, so equal sequences are one
+    node; slots are ordered by pb + pn, equal ones with stays first by slot and then by r * k + j.
+    """
+    classes, logprobs = np.asarray(classes), np.asarray(logprobs)
+    child, label, parent = {}, {0: None}, {0: None}
+    slots = [(0, np.float64(1.0), np.float64(0.0))]
+    log_scale, bad = 0.0, False
+    for t in range(int(n_frames)):
+        pairs, shift, b = frame_probabilities(classes[t], logprobs[t])
+        bad = bad or b
+        p = dict((c, q) for c, q in pairs if c >= 0 and q > 0.0)
+        held = {node: i for i, (node, _, _) in enumerate(slots)}
+        stay = [[(pb + pn) * np.float64(p.get(blank, 0.0)), pn * np.float64(p.get(label[node], 0.0))] for node, pb, pn in slots]
+        grown = []
+        for r, (node, pb, pn) in enumerate(slots):
+            for j, (c, q) in enumerate(pairs):
+                if c < 0 or c == blank or q == 0.0:
+                    continue
+                v = (pb if c == label[node] else pb + pn) * np.float64(q)
+                to = child.get((node, c))
+                if to is not None and to in held:
+                    stay[held[to]][1] = stay[held[to]][1] + v
+                else:
+                    grown.append((v, r, j, c))
+        cand = [(pb + pn, 0, i, 0, None) for i, (pb, pn) in enumerate(stay)]
+        cand += [(v, 1, r, j, c) for v, r, j, c in grown]
+        cand = sorted([e for e in cand if e[0] > 0.0], key=lambda e: (-e[0],) + e[1:4])[:beams]
+        new = []
+        for v, kind, r, j, c in cand:
+            if kind == 0:
+                new.append((slots[r][0], stay[r][0], stay[r][1]))
+            else:
+                at = (slots[r][0], c)
+                if at not in child:
+                    child[at] = len(child) + 1
+                    label[child[at]], parent[child[at]] = c, slots[r][0]
+                new.append((child[at], np.float64(0.0), v))
+        slots = new
+        log_scale += shift
+        if t % 16 == 15 and slots:
+            e = int(np.frexp(slots[0][1] + slots[0][2])[1])
+            slots = [(node, np.ldexp(pb, -e), np.ldexp(pn, -e)) for node, pb, pn in slots]
+            log_scale += e * np.log(2.0)
+    out = []
+    for node, pb, pn in slots:
+        score = float(np.log(pb + pn) + log_scale)
+        labels = []
+        while node:
+            labels.append(label[node])
+            node = parent[node]
+        out.append((labels[::-1], score))
+    return out, bad

@@ -18,13 +18,14 @@ LIB_PATH = os.path.join(HERE, "libprunedctc.so")
 
 PCTC_BF16, PCTC_FP32 = 0, 1
 GEMM_AUTO, GEMM_SIMT = 0, 1
-UTT_INFEASIBLE, UTT_NONFINITE, UTT_BAD_TARGET, UTT_SUBSET_OVERFLOW = 1, 2, 4, 8
+UTT_INFEASIBLE, UTT_NONFINITE, UTT_BAD_TARGET, UTT_SUBSET_OVERFLOW, UTT_STATE_FULL = 1, 2, 4, 8, 16
 
 EXPORTS = ("pctc_workspace_bytes", "pctc_chunk_width", "pruned_ctc_fwd_bwd", "pruned_ctc_fwd_bwd_traced", "pctc_gemm_bf16",
            "pctc_workspace_status", "pctc_status_string", "pctc_host_call_scratch_bytes",
            "pruned_ctc_fwd_bwd_host", "pctc_subset_relabel_noalloc", "pctc_greedy_workspace_bytes",
            "pctc_greedy_decode", "pctc_topk_workspace_bytes", "pctc_topk_decode",
-           "pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale")
+           "pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
+           "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read")
 NOALLOC_MAX_V = 262144
 
 PHASES = ("prep", "lse", "subset_logp", "dp", "dlogits", "dh", "dw", "dbias", "finish")
@@ -41,6 +42,10 @@ class Problem(ctypes.Structure):
         ("max_K", ctypes.c_int32),
         ("utt_weights", ctypes.c_void_p),
     ]
+
+
+class PrefixProblem(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("N", "T", "k", "beams", "blank_id", "max_frames")]
 
 
 class TraceStruct(ctypes.Structure):
@@ -143,6 +148,13 @@ def _configure(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.pctc_grad_scale.restype = ctypes.c_int
     lib.pctc_grad_scale.argtypes = [ctypes.c_int32, vpp, vpp, i64p, i32p, i32p, vp, ctypes.c_float, ctypes.c_float,
                                     vp, vp]
+    prefix_p = ctypes.POINTER(PrefixProblem)
+    lib.pctc_prefix_state_bytes.restype = ctypes.c_int
+    lib.pctc_prefix_state_bytes.argtypes = [prefix_p, size_p]
+    lib.pctc_prefix_advance.restype = ctypes.c_int
+    lib.pctc_prefix_advance.argtypes = [prefix_p, vp, vp, i32p, ctypes.c_int32, vp, ctypes.c_size_t, vp]
+    lib.pctc_prefix_read.restype = ctypes.c_int
+    lib.pctc_prefix_read.argtypes = [prefix_p, vp, ctypes.c_size_t, vp, ctypes.c_int32, vp, vp, vp, vp]
     lib.pctc_gemm_bf16.restype = ctypes.c_int
     lib.pctc_gemm_bf16.argtypes = [vp, vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                    ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp]
@@ -554,3 +566,93 @@ def grad_scale(grads, sqsum, max_norm, *, out=None, eps=1e-6):
     _run_on(dev, load().pctc_grad_scale, "pctc_grad_scale", len(grads), ptrs, outs, numels, kinds, out_kinds,
             _dptr(sqsum), float(max_norm), float(eps), _dptr(norm))
     return dict(norm=norm, grads=grads if out is None else list(out))
+
+
+class PrefixBeam:
+    """A CTC prefix beam search in progress, for frames that arrive in portions.
+
+    `advance(classes, logprobs, lengths)` takes the next frames (classes [N,t,k] int32 and logprobs
+    [N,t,k] fp32 as topk_decode gives them, any t; lengths: host integers, how many of the t count
+    per utterance, None for all); `read()` returns the hypotheses so far.  The state lives in one device
+    buffer with room for max_frames frames an utterance.  Calls on one object belong on one stream.
+    """
+
+    def __init__(self, N, beams, max_frames, blank_id, device):
+        import torch
+
+        self.N, self.beams, self.max_frames, self.blank_id = int(N), int(beams), int(max_frames), int(blank_id)
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        need = ctypes.c_size_t(0)
+        st = load().pctc_prefix_state_bytes(ctypes.byref(self._problem(1, 1)), ctypes.byref(need))
+        if st != 0:
+            raise PctcError(st, "pctc_prefix_state_bytes")
+        self.frames = np.zeros(self.N, dtype=np.int64)
+        self.started = False
+        self.state = torch.empty(int(need.value), dtype=torch.uint8, device=self.device)
+
+    def _problem(self, T, k):
+        return PrefixProblem(self.N, int(T), int(k), self.beams, self.blank_id, self.max_frames)
+
+    def advance(self, classes, logprobs, lengths=None):
+        import torch
+
+        if classes.dtype != torch.int32 or logprobs.dtype != torch.float32:
+            raise ValueError("classes must be int32 and logprobs fp32")
+        if classes.dim() != 3 or classes.shape[0] != self.N or logprobs.shape != classes.shape:
+            raise ValueError("classes and logprobs must be [N, frames, k]")
+        if classes.device != self.device or logprobs.device != self.device:
+            raise ValueError("classes and logprobs must be on the state's device")
+        if not (classes.is_contiguous() and logprobs.is_contiguous()):
+            raise ValueError("classes and logprobs must be contiguous")
+        T, k = classes.shape[1:]
+        ln = np.full(self.N, T, dtype=np.int32) if lengths is None else _i32(lengths)
+        if ln.shape != (self.N,):
+            raise ValueError("one length per utterance is required")
+        if ((self.frames + ln) > self.max_frames).any():
+            raise ValueError("more frames than the state has room for")
+        _run_on(self.device, load().pctc_prefix_advance, "pctc_prefix_advance", ctypes.byref(self._problem(T, k)),
+                _dptr(classes), _dptr(logprobs), _ptr_i32(ln), 0 if self.started else 1, _dptr(self.state),
+                ctypes.c_size_t(self.state.numel()))
+        self.started = True
+        self.frames += ln
+
+    def read(self, max_tokens=None):
+        """Device tensors, best hypothesis first: tokens [N,beams,max_tokens] int32 (-1 behind the last; max_tokens
+        defaults to the frames taken so far), token_lengths [N,beams], scores [N,beams] fp32 (log-probabilities,
+        -inf where there are fewer hypotheses than beams), flags [N]."""
+        import torch
+
+        if not self.started:
+            raise ValueError("no frames yet")
+        width = max(1, int(self.frames.max()) if max_tokens is None else int(max_tokens))
+        o = dict(dtype=torch.int32, device=self.device)
+        res = dict(tokens=torch.empty((self.N, self.beams, width), **o),
+                   token_lengths=torch.empty((self.N, self.beams), **o),
+                   scores=torch.empty((self.N, self.beams), dtype=torch.float32, device=self.device),
+                   flags=torch.empty((self.N,), **o))
+        _run_on(self.device, load().pctc_prefix_read, "pctc_prefix_read", ctypes.byref(self._problem(1, 1)),
+                _dptr(self.state), ctypes.c_size_t(self.state.numel()), _dptr(res["tokens"]), width,
+                _dptr(res["token_lengths"]), _dptr(res["scores"]), _dptr(res["flags"]))
+        return res
+
+
+def prefix_beam_decode(classes, logprobs, input_lengths, blank_id, beams):
+    """CTC prefix beam search over whole utterances: classes [N,T,k] int32 and logprobs [N,T,k] fp32 as
+    topk_decode gives them, input_lengths host integers.  Returns the dict of PrefixBeam.read() with tokens
+    [N,beams,T], plus the PrefixBeam itself as "search"."""
+    search = PrefixBeam(classes.shape[0], beams, max(1, classes.shape[1]), blank_id, classes.device)
+    search.advance(classes, logprobs, input_lengths)
+    res = search.read(max_tokens=classes.shape[1])
+    res["search"] = search
+    return res
+
+
+def beam_decode(hidden, W, bias, input_lengths, blank_id, beams, *, k=8, chunk=0, gemm_path=GEMM_AUTO, workspace=None):
+    """CTC prefix beam search with the head: topk_decode's k best classes of every frame, then
+    prefix_beam_decode over them.  Returns the latter's dict plus the head's workspace."""
+    best = topk_decode(hidden, W, bias, input_lengths, k, chunk=chunk, gemm_path=gemm_path, workspace=workspace)
+    res = prefix_beam_decode(best["classes"], best["logprobs"], input_lengths, blank_id, beams)
+    res["workspace"] = best["workspace"]
+    return res
