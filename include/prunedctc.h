@@ -336,6 +336,40 @@ pctc_status_t pctc_prefix_read(const pctc_prefix_t* problem, const void* state, 
                                int32_t* utt_flags, void* stream);
 
 /*
+ * Beam search's selection over beams and vocabulary, for a decoder that works beside or behind the CTC head
+ * (rescoring, transcription with a language model's head): with logits x and lse_b = log sum_v exp x[b,v],
+ *   cand(b,v) = score_b + (x[b,v] - lse_b)
+ * and the K largest candidates of every utterance, best first; among equals the lowest b * V + v.  The
+ * comparisons are of 64-bit sums; the scores that come back are rounded once to fp32.
+ *
+ * A beam whose score is -inf is dead: its logits are not read and it gives no candidates (a first step with
+ * one hypothesis: all scores but one -inf).  An ended beam (finished[n,b] != 0) keeps its score in a single
+ * candidate, token eos_id.  Logits of -inf are excluded tokens; a row with nothing else gives no candidates.
+ * A row with a NaN or +inf, or a beam whose score is one, gives none either and flags its utterance
+ * PCTC_UTT_NONFINITE.  Slots for which there is no candidate get score -inf and parent and token -1.
+ */
+typedef struct {
+  int32_t N, B, K;       /* utterances; beams in and out, 1 .. 32 each (K > B is a first step's)   */
+  int64_t V;             /* vocabulary, up to 2,097,152                                       */
+  int64_t stride_n;      /* elements between utterances ...                                   */
+  int64_t stride_b;      /* ... and between beams of the logits (>= V); the V logits of a beam
+                            are contiguous.  Fastest where every row starts 16-byte aligned   */
+  int32_t dtype;         /* pctc_dtype_t of the logits                                        */
+  int32_t eos_id;        /* token that ends a hypothesis, or -1: there is none                */
+} pctc_beam_t;
+
+/*
+ * Device pointers: logits, scores [N,B] fp32, finished [N,B] bytes or NULL (needs eos_id >= 0).  Outputs:
+ * scores_out [N,K] fp32, parents [N,K] and tokens [N,K] int32, finished_out [N,K] bytes or NULL (1: the parent
+ * had ended, or the token is eos_id), utt_flags [N] or NULL.  scores_out and finished_out may be
+ * scores and finished themselves (K == B).  One launch, no workspace; may be captured into a CUDA graph and
+ * issued from several threads.
+ */
+pctc_status_t pctc_beam_select(const pctc_beam_t* problem, const void* logits, const float* scores,
+                               const uint8_t* finished, float* scores_out, int32_t* parents, int32_t* tokens,
+                               uint8_t* finished_out, int32_t* utt_flags, void* stream);
+
+/*
  * Global gradient norm over many tensors, and clipping: what stands between the gradients of
  * pruned_ctc_fwd_bwd (with those of the model below it) and the weight update.
  *   S = sum over all tensors and values of g^2,  norm = sqrt(S),

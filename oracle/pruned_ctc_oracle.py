@@ -556,3 +556,39 @@ def prefix_beam_search(classes, logprobs, n_frames, blank, beams):
             node = parent[node]
         out.append((labels[::-1], score))
     return out, bad
+
+
+# ----------------------------------------------------------------------------
+# Beam search's selection over beams and vocabulary
+# ----------------------------------------------------------------------------
+
+def beam_select(logits, scores, beams, finished=None, eos=None):
+    """One utterance: logits [B, V], scores [B].  The `beams` best (score, beam, token), best first, equal ones by
+    lowest beam and then lowest token; whether a beam held a NaN or +inf; and the smallest distance between
+    neighbours among them and to the first one left out (for near-tie checks)."""
+    logits = np.asarray(logits, dtype=np.float64)
+    B, V = logits.shape
+    cand, bad = [], False
+    for b in range(B):
+        s = float(scores[b])
+        if np.isnan(s) or s == np.inf:
+            bad = True
+            continue
+        if s == -np.inf:
+            continue
+        if finished is not None and finished[b]:
+            cand.append((s, b, eos))
+            continue
+        row = logits[b]
+        if np.isnan(row).any() or (row == np.inf).any():
+            bad = True
+            continue
+        if (row == -np.inf).all():
+            continue
+        values = s + (row - (row.max() + np.log(np.exp(row - row.max()).sum())))
+        order = np.lexsort((np.arange(V), -values))[: beams + 1]
+        cand += [(float(values[v]), b, int(v)) for v in order if values[v] > -np.inf]
+    cand.sort(key=lambda e: (-e[0], e[1], e[2]))
+    near = min((cand[i][0] - cand[i + 1][0] for i in range(min(beams, len(cand) - 1)) if cand[i][0] != cand[i + 1][0]),
+               default=np.inf)
+    return cand[:beams], bad, near

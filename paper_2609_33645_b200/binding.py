@@ -25,7 +25,7 @@ EXPORTS = ("pctc_workspace_bytes", "pctc_chunk_width", "pruned_ctc_fwd_bwd", "pr
            "pruned_ctc_fwd_bwd_host", "pctc_subset_relabel_noalloc", "pctc_greedy_workspace_bytes",
            "pctc_greedy_decode", "pctc_topk_workspace_bytes", "pctc_topk_decode",
            "pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
-           "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read")
+           "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read", "pctc_beam_select")
 NOALLOC_MAX_V = 262144
 
 PHASES = ("prep", "lse", "subset_logp", "dp", "dlogits", "dh", "dw", "dbias", "finish")
@@ -46,6 +46,12 @@ class Problem(ctypes.Structure):
 
 class PrefixProblem(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int32) for name in ("N", "T", "k", "beams", "blank_id", "max_frames")]
+
+
+class BeamProblem(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("B", ctypes.c_int32), ("K", ctypes.c_int32), ("V", ctypes.c_int64),
+                ("stride_n", ctypes.c_int64), ("stride_b", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("eos_id", ctypes.c_int32)]
 
 
 class TraceStruct(ctypes.Structure):
@@ -155,6 +161,8 @@ def _configure(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.pctc_prefix_advance.argtypes = [prefix_p, vp, vp, i32p, ctypes.c_int32, vp, ctypes.c_size_t, vp]
     lib.pctc_prefix_read.restype = ctypes.c_int
     lib.pctc_prefix_read.argtypes = [prefix_p, vp, ctypes.c_size_t, vp, ctypes.c_int32, vp, vp, vp, vp]
+    lib.pctc_beam_select.restype = ctypes.c_int
+    lib.pctc_beam_select.argtypes = [ctypes.POINTER(BeamProblem)] + [vp] * 9
     lib.pctc_gemm_bf16.restype = ctypes.c_int
     lib.pctc_gemm_bf16.argtypes = [vp, vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                    ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp]
@@ -655,4 +663,50 @@ def beam_decode(hidden, W, bias, input_lengths, blank_id, beams, *, k=8, chunk=0
     best = topk_decode(hidden, W, bias, input_lengths, k, chunk=chunk, gemm_path=gemm_path, workspace=workspace)
     res = prefix_beam_decode(best["classes"], best["logprobs"], input_lengths, blank_id, beams)
     res["workspace"] = best["workspace"]
+    return res
+
+
+def beam_select(logits, scores, beams, *, finished=None, eos_id=None):
+    """One step of beam search: the `beams` best continuations of every utterance over beams and vocabulary.
+
+    logits [N,B,V] bf16 or fp32 with contiguous rows (any strides between rows, e.g. a view of a padded
+    vocabulary), scores [N,B] fp32 (-inf: a dead beam), finished [N,B] bool or None (ended hypotheses, which
+    keep their score in one candidate with token eos_id), eos_id the token that ends a hypothesis or None.
+    Returns device tensors: scores [N,beams] fp32, parents and tokens [N,beams] int32 (-1 where there are
+    fewer candidates than beams), finished [N,beams] bool and flags [N] int32 (UTT_NONFINITE).  Best
+    first; among equals the lowest beam, then the lowest token.
+    """
+    import torch
+
+    if logits.dim() != 3 or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits must be [N, B, V], bf16 or fp32")
+    N, B, V = logits.shape
+    if not logits.is_cuda or (V > 1 and logits.stride(2) != 1):
+        raise ValueError("logits must be a CUDA tensor with contiguous rows")
+    dev = logits.device
+    if scores.dtype != torch.float32 or scores.shape != (N, B) or not scores.is_contiguous() or scores.device != dev:
+        raise ValueError("scores must be contiguous fp32 [N, B] on the device of the logits")
+    if finished is not None:
+        if finished.dtype != torch.bool or finished.shape != (N, B) or not finished.is_contiguous() or finished.device != dev:
+            raise ValueError("finished must be contiguous bool [N, B] on the device of the logits")
+        if eos_id is None:
+            raise ValueError("finished needs an eos_id")
+    if eos_id is not None and not 0 <= int(eos_id) < V:
+        raise ValueError("eos_id must be a token")
+    K = int(beams)
+    if K < 1:
+        raise ValueError("beams must be at least 1")
+    # a dimension of size 1 has no stride that counts
+    stride_b = max(logits.stride(1), V) if B > 1 else V
+    if B > 1 and logits.stride(1) < V:
+        raise ValueError("rows of logits overlap")
+    prob = BeamProblem(N, B, K, V, logits.stride(0) if N > 1 else 0, stride_b,
+                       PCTC_BF16 if logits.dtype == torch.bfloat16 else PCTC_FP32, -1 if eos_id is None else int(eos_id))
+    o = dict(dtype=torch.int32, device=dev)
+    res = dict(scores=torch.empty((N, K), dtype=torch.float32, device=dev), parents=torch.empty((N, K), **o),
+               tokens=torch.empty((N, K), **o), finished=torch.empty((N, K), dtype=torch.bool, device=dev),
+               flags=torch.empty((N,), **o))
+    _run_on(dev, load().pctc_beam_select, "pctc_beam_select", ctypes.byref(prob), _dptr(logits), _dptr(scores),
+            _dptr(finished), _dptr(res["scores"]), _dptr(res["parents"]), _dptr(res["tokens"]), _dptr(res["finished"]),
+            _dptr(res["flags"]))
     return res

@@ -1,0 +1,537 @@
+// Beam search's selection over beams and vocabulary, and the reordering of the states that go with it.
+//
+// Selection.  With lse_b the log-sum-exp of beam b's logits,
+//   cand(b, v) = score_b + (x_bv - lse_b),
+// and the K largest of an utterance's B * V candidates go on; among equals the lowest b * V + v.  Every logit
+// has to be read once for lse_b, and a candidate can be judged only after that: what is kept of the one
+// pass over HBM is the maximum of every 256 logits.  The K best candidates lie in the K blocks with the
+// best maxima (K better ones stand against any other), so a few blocks are read again, from L2, and only there
+// single logits are compared.
+//
+// One cluster of CTAs takes one utterance: every CTA streams its share of the columns of all rows, the
+// shares' (maximum, sum of exponentials) meet in distributed shared memory, every CTA finds the candidates in
+// its own blocks, and the first one ranks them all.  One launch, no workspace.  Bound by HBM when there are many rows,
+// by latency when there are few.
+//
+// Exponentials and their sums within a thread are fp32, of differences from a running maximum (so that
+// their errors are relative to the difference, not to the logit); everything after that, and every comparison
+// of candidates, is 64 bits: candidates of different beams are ordered by sums whose fp32 rounding
+// would be larger than their distance.
+#include "../../include/prunedctc.h"
+#include "pctc_internal.h"
+
+#include <cooperative_groups.h>
+#include <math_constants.h>
+
+namespace cg = cooperative_groups;
+
+namespace pctc {
+namespace {
+
+constexpr int SEL_MAX = 32;                       // beams in and out
+constexpr int SEL_THREADS = 512, SEL_WARPS = SEL_THREADS / 32;
+constexpr int SEL_BLOCK = 256;                    // logits per maximum: 8 a lane
+constexpr int SEL_BATCH = 4;                      // blocks a warp has in flight
+constexpr int SEL_MAX_BLOCKS = 512;               // blocks a CTA reads again
+constexpr int SEL_MAX_CAND = 1280;
+constexpr long long SEL_MAX_V = 1 << 21;
+constexpr int SEL_MAX_DYN = SEL_MAX * (int)(SEL_MAX_V / SEL_BLOCK) / 8 * 4;      // maxima, at 8 CTAs a cluster
+
+struct SelArgs {
+  const void* logits;
+  long long stride_n, stride_b;                   // elements
+  const float* scores;
+  const unsigned char* finished;                  // or null
+  int N, B, K, V, eos, nb;                        // nb: blocks a row
+  float* scores_out;
+  int *parents, *tokens;
+  unsigned char* finished_out;
+  int* flags;
+};
+
+struct Cand {
+  double score;
+  unsigned long long at;                          // b << 32 | v
+};
+__device__ __forceinline__ bool before(const Cand& a, const Cand& b) {
+  return a.score > b.score || (a.score == b.score && a.at < b.at);
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Eight logits of a lane: 16-byte loads where every row starts on a 16-byte boundary, else one by one.
+template <typename T, bool VEC>
+struct Octet;
+template <>
+struct Octet<__nv_bfloat16, true> {
+  uint4 r;
+  static __device__ __forceinline__ int index(int lane, int e) { return lane * 8 + e; }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, int lane) {
+    const int i = lane * 8;
+    if (i + 8 <= left) {
+      r = *(const uint4*)(p + i);
+    } else {
+      unsigned w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const unsigned lo = i + 2 * e < left ? ((const unsigned short*)p)[i + 2 * e] : 0xff80u;
+        const unsigned hi = i + 2 * e + 1 < left ? ((const unsigned short*)p)[i + 2 * e + 1] : 0xff80u;
+        w[e] = lo | hi << 16;
+      }
+      r = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    const unsigned w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Octet<float, true> {
+  float4 a, b;
+  static __device__ __forceinline__ int index(int lane, int e) { return (e < 4 ? 0 : 124) + lane * 4 + e; }
+  static __device__ __forceinline__ float4 quad(const float* p, int i, int left) {
+    if (i + 4 <= left) return *(const float4*)(p + i);
+    float4 v;
+    v.x = i < left ? p[i] : -CUDART_INF_F;
+    v.y = i + 1 < left ? p[i + 1] : -CUDART_INF_F;
+    v.z = i + 2 < left ? p[i + 2] : -CUDART_INF_F;
+    v.w = -CUDART_INF_F;
+    return v;
+  }
+  __device__ __forceinline__ void load(const float* p, int left, int lane) {
+    a = quad(p, lane * 4, left);
+    b = quad(p, 128 + lane * 4, left);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+};
+template <typename T>
+struct Octet<T, false> {
+  T v[8];
+  static __device__ __forceinline__ int index(int lane, int e) { return e * 32 + lane; }
+  __device__ __forceinline__ void load(const T* p, int left, int lane) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e * 32 + lane < left ? p[e * 32 + lane] : (T)(-CUDART_INF_F);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+  }
+};
+
+struct SelShared {
+  float score[SEL_MAX];
+  unsigned char kind[SEL_MAX];                    // 0 dead, 1 live, 2 ended
+  int rows[SEL_MAX];                              // the live rows, ascending
+  int nlive, bad;
+  float part_m[SEL_WARPS][SEL_MAX];               // per warp and live row
+  double part_s[SEL_WARPS][SEL_MAX];
+  float row_m[SEL_MAX];                           // of this CTA's columns
+  double row_s[SEL_MAX];
+  double lse[SEL_MAX];                            // by row; NaN: the row gives no candidates
+  double group[32];
+  double thr;
+  int warp_count[SEL_WARPS];
+  int nblocks, ncand, overflow;
+  int blocks[SEL_MAX_BLOCKS];
+  Cand cand[SEL_MAX_CAND];
+  Cand best[SEL_WARPS];
+};
+
+// (max, sum) pairs of the lanes of a warp joined: m the largest, s = sum_i s_i exp(m_i - m), in 64 bits.
+__device__ __forceinline__ void join(float& m, double& s) {
+  const float mine = m;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (mine != m && s != 0.0) s *= exp((double)mine - (double)m);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+}
+
+template <typename T>
+__device__ __forceinline__ Cand candidate(const SelShared& sh, const T* base, long long stride_b, int b, int v) {
+  Cand c;
+  c.score = (double)sh.score[b] + ((double)(float)base[b * stride_b + v] - sh.lse[b]);
+  c.at = (unsigned long long)b << 32 | (unsigned)v;
+  return c;
+}
+
+// The K best by K passes over all candidates, each for the best one behind the last: for inputs whose ties or
+// order leave more candidates than the lists hold.  Called by all threads of one CTA.
+template <typename T>
+__device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  Cand last{CUDART_INF, 0};
+  int found = 0;
+  for (int k = 0; k < a.K; ++k) {
+    Cand best{-CUDART_INF, ~0ull};
+    for (int i = 0; i < sh.nlive; ++i) {
+      const int b = sh.rows[i];
+      if (isnan(sh.lse[b])) continue;
+      for (int v = tid; v < a.V; v += SEL_THREADS) {
+        const Cand c = candidate(sh, base, a.stride_b, b, v);
+        if (c.score > -CUDART_INF && before(last, c) && before(c, best)) best = c;
+      }
+    }
+    if (tid < a.B && sh.kind[tid] == 2) {
+      const Cand c{(double)sh.score[tid], (unsigned long long)tid << 32 | (unsigned)a.eos};
+      if (before(last, c) && before(c, best)) best = c;
+    }
+    for (int o = 16; o; o >>= 1) {
+      const Cand c{__shfl_xor_sync(0xffffffffu, best.score, o), __shfl_xor_sync(0xffffffffu, best.at, o)};
+      if (before(c, best)) best = c;
+    }
+    __syncthreads();
+    if (lane == 0) sh.best[warp] = best;
+    __syncthreads();
+    best = sh.best[0];
+    for (int w = 1; w < SEL_WARPS; ++w)
+      if (before(sh.best[w], best)) best = sh.best[w];
+    if (best.score == -CUDART_INF) break;
+    if (tid == 0) sh.cand[k] = best;
+    last = best;
+    ++found;
+  }
+  __syncthreads();
+  if (tid == 0) sh.ncand = found;
+  __syncthreads();
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a) {
+  __shared__ SelShared sh;
+  extern __shared__ float bmax[];                 // [live rows][blocks of this CTA]
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
+  const int n = blockIdx.x / C;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const T* base = (const T*)a.logits + n * a.stride_n;
+  const int b0 = (int)((long long)a.nb * c / C), b1 = (int)((long long)a.nb * (c + 1) / C), nbl = b1 - b0;
+
+  if (warp == 0) {
+    const float s = lane < a.B ? a.scores[n * a.B + lane] : -CUDART_INF_F;
+    const bool done = lane < a.B && a.finished && a.finished[n * a.B + lane];
+    const int kind = !isfinite(s) ? 0 : done ? 2 : 1;
+    const unsigned live = __ballot_sync(0xffffffffu, kind == 1);
+    const unsigned bad = __ballot_sync(0xffffffffu, isnan(s) || s == CUDART_INF_F);
+    if (lane < a.B) {
+      sh.score[lane] = s;
+      sh.kind[lane] = (unsigned char)kind;
+    }
+    if (kind == 1) sh.rows[__popc(live & ((1u << lane) - 1))] = lane;
+    if (lane == 0) {
+      sh.nlive = __popc(live);
+      sh.bad = bad != 0;
+      sh.nblocks = sh.ncand = sh.overflow = 0;
+    }
+  }
+  for (int i = tid; i < SEL_WARPS * SEL_MAX; i += SEL_THREADS) {
+    (&sh.part_m[0][0])[i] = -CUDART_INF_F;
+    (&sh.part_s[0][0])[i] = 0.0;
+  }
+  __syncthreads();
+
+  // ---- one pass over this CTA's columns of all live rows ----
+  // A warp takes the same columns of every row, so that equal rows have equal sums, bit for bit, and their
+  // candidates tie.
+  const int items = sh.nlive * nbl;
+  {
+    const int w0 = nbl * warp / SEL_WARPS, w1 = nbl * (warp + 1) / SEL_WARPS;
+    const int end = sh.nlive * (w1 - w0);
+    int r = 0, blk = w0;
+    float ref = -CUDART_INF_F, sum = 0.f;
+    for (int it = 0; it < end; it += SEL_BATCH) {
+      Octet<T, VEC> raw[SEL_BATCH];
+      int lr = r, lb = blk;
+#pragma unroll
+      for (int u = 0; u < SEL_BATCH; ++u) {
+        if (it + u < end) {
+          const int v0 = (b0 + lb) * SEL_BLOCK;
+          raw[u].load(base + sh.rows[lr] * a.stride_b + v0, a.V - v0, lane);
+          if (++lb == w1) { lb = w0; ++lr; }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < SEL_BATCH; ++u) {
+        if (it + u < end) {
+          float x[8];
+          raw[u].get(x);
+          float m = x[0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) m = fmaxf(m, x[e]);
+          m = warp_max(m);
+          if (lane == 0) bmax[r * nbl + blk] = m;
+          if (m > ref) {
+            sum *= exp2_approx((ref - m) * 1.44269504f);
+            ref = m;
+          }
+          const float z = ref == -CUDART_INF_F ? 0.f : ref;     // all masked so far: exp(-inf) = 0, NaN stays NaN
+          float t = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) t += exp2_approx((x[e] - z) * 1.44269504f);
+          sum += t;
+          if (++blk == w1) {                      // the row ends for this warp
+            double s = sum;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (lane == 0) { sh.part_m[warp][r] = ref; sh.part_s[warp][r] = s; }
+            ref = -CUDART_INF_F;
+            sum = 0.f;
+            blk = w0;
+            ++r;
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+  for (int r = warp; r < sh.nlive; r += SEL_WARPS) {
+    float m = lane < SEL_WARPS ? sh.part_m[lane][r] : -CUDART_INF_F;
+    double s = lane < SEL_WARPS ? sh.part_s[lane][r] : 0.0;
+    join(m, s);
+    if (lane == 0) { sh.row_m[r] = m; sh.row_s[r] = s; }
+  }
+  cluster.sync();
+  for (int r = warp; r < sh.nlive; r += SEL_WARPS) {
+    float m = -CUDART_INF_F;
+    double s = 0.0;
+    if (lane < C) {
+      const SelShared* other = cluster.map_shared_rank(&sh, lane);
+      m = other->row_m[r];
+      s = other->row_s[r];
+    }
+    join(m, s);
+    // nothing allowed, or a NaN or +inf among the logits: no candidates
+    const double lse = (double)m + log(s);
+    const bool fine = isfinite(lse);
+    if (lane == 0) {
+      sh.lse[sh.rows[r]] = fine ? lse : CUDART_NAN;
+      if (!fine && !(s == 0.0)) atomicOr(&sh.bad, 1);
+    }
+  }
+  __syncthreads();
+
+  // ---- the blocks that can hold one of the K best: those from the K-th best of 32 groups' maxima on ----
+  auto block_score = [&](int e) {
+    const int r = e / nbl, b = sh.rows[r];
+    const double s = (double)sh.score[b] + ((double)bmax[e] - sh.lse[b]);
+    return isnan(s) ? -CUDART_INF : s;
+  };
+  double top = -CUDART_INF;                       // group g: the blocks e with e % 32 == g, sixteen threads each
+  for (int e = (tid & 15) * 32 + (tid >> 4); e < items; e += SEL_THREADS) top = fmax(top, block_score(e));
+#pragma unroll
+  for (int o = 8; o; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if ((lane & 15) == 0) sh.group[tid >> 4] = top;
+  __syncthreads();
+  if (warp == 0) {
+    const double mine = sh.group[lane];
+    int rank = 0;
+    for (int i = 0; i < 32; ++i) {
+      const double o = __shfl_sync(0xffffffffu, mine, i);
+      rank += o > mine || (o == mine && i < lane);
+    }
+    if (rank == a.K - 1) sh.thr = mine;
+  }
+  __syncthreads();
+  const double thr = sh.thr;
+  int equal = 0;                                  // blocks that tie with the threshold: the first K of them will do
+  for (int e0 = 0; e0 < items; e0 += SEL_THREADS) {
+    const int e = e0 + tid;
+    const double s = e < items ? block_score(e) : -CUDART_INF;
+    const bool some = s > -CUDART_INF;
+    const unsigned eq = __ballot_sync(0xffffffffu, some && s == thr);
+    if (lane == 0) sh.warp_count[warp] = __popc(eq);
+    __syncthreads();
+    int prior = equal, all = equal;
+    for (int w = 0; w < SEL_WARPS; ++w) {
+      if (w < warp) prior += sh.warp_count[w];
+      all += sh.warp_count[w];
+    }
+    equal = all;
+    if (some && (s > thr || (s == thr && prior + __popc(eq & ((1u << lane) - 1)) < a.K))) {
+      const int p = atomicAdd(&sh.nblocks, 1);
+      if (p < SEL_MAX_BLOCKS) sh.blocks[p] = e; else sh.overflow = 1;
+    }
+    __syncthreads();
+  }
+
+  // ---- single logits of those blocks ----
+  const int nblk = sh.nblocks < SEL_MAX_BLOCKS ? sh.nblocks : SEL_MAX_BLOCKS;
+  for (int i = warp; i < nblk; i += SEL_WARPS) {
+    const int e = sh.blocks[i], r = e / nbl, b = sh.rows[r], v0 = (b0 + e - r * nbl) * SEL_BLOCK;
+    Octet<T, VEC> raw;
+    raw.load(base + b * a.stride_b + v0, a.V - v0, lane);
+    float x[8];
+    raw.get(x);
+    double s[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s[q] = (double)sh.score[b] + ((double)x[q] - sh.lse[b]);
+    unsigned used = 0;
+    for (int k = 0; k < a.K; ++k) {               // at most K of a block, best first, down to the threshold
+      double best = -CUDART_INF;
+      int at = 0x7fffffff, q0 = 0;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int v = v0 + Octet<T, VEC>::index(lane, q);
+        if (!(used >> q & 1) && (s[q] > best || (s[q] == best && s[q] > -CUDART_INF && v < at))) {
+          best = s[q];
+          at = v;
+          q0 = q;
+        }
+      }
+      double all = best;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) all = fmax(all, __shfl_xor_sync(0xffffffffu, all, o));
+      if (!(all >= thr) || all == -CUDART_INF) break;
+      const int first = (int)__reduce_min_sync(0xffffffffu, best == all ? (unsigned)at : 0x7fffffffu);
+      if (best == all && at == first) {
+        used |= 1u << q0;
+        const int p = atomicAdd(&sh.ncand, 1);
+        if (p < SEL_MAX_CAND) sh.cand[p] = Cand{all, (unsigned long long)b << 32 | (unsigned)at}; else sh.overflow = 1;
+      }
+    }
+  }
+  cluster.sync();
+
+  // ---- the first CTA ranks what all have found ----
+  if (c == 0) {
+    double least = thr;                           // K candidates of one CTA reach its threshold, so the best one holds for all
+    bool over = false;
+    for (int o = 0; o < C; ++o) {
+      const SelShared* other = cluster.map_shared_rank(&sh, o);
+      least = fmax(least, other->thr);
+      over = over || other->overflow;
+    }
+    __syncthreads();
+    for (int o = 1; o < C; ++o) {
+      const SelShared* other = cluster.map_shared_rank(&sh, o);
+      const int m = other->ncand < SEL_MAX_CAND ? other->ncand : SEL_MAX_CAND;
+      for (int i = tid; i < m; i += SEL_THREADS) {
+        const Cand x = other->cand[i];
+        if (x.score < least) continue;
+        const int p = atomicAdd(&sh.ncand, 1);
+        if (p < SEL_MAX_CAND) sh.cand[p] = x;
+      }
+    }
+    if (tid < a.B && sh.kind[tid] == 2) {
+      const int p = atomicAdd(&sh.ncand, 1);
+      if (p < SEL_MAX_CAND) sh.cand[p] = Cand{(double)sh.score[tid], (unsigned long long)tid << 32 | (unsigned)a.eos};
+    }
+    __syncthreads();
+    if (over || sh.ncand > SEL_MAX_CAND) select_by_passes(sh, a, base);
+    const int nc = sh.ncand;
+    auto put = [&](int k, double score, int parent, int token) {
+      const int o = n * a.K + k;
+      a.scores_out[o] = (float)score;
+      a.parents[o] = parent;
+      a.tokens[o] = token;
+      if (a.finished_out) a.finished_out[o] = parent >= 0 && (sh.kind[parent] == 2 || token == a.eos);
+    };
+    for (int i = tid; i < nc; i += SEL_THREADS) {
+      const Cand x = sh.cand[i];
+      int rank = 0;
+      for (int j = 0; j < nc; ++j) rank += before(sh.cand[j], x);
+      if (rank < a.K) put(rank, x.score, (int)(x.at >> 32), (int)(unsigned)x.at);
+    }
+    for (int k = nc + tid; k < a.K; k += SEL_THREADS) put(k, -CUDART_INF, -1, -1);
+    if (tid == 0 && a.flags) a.flags[n] = sh.bad ? PCTC_UTT_NONFINITE : 0;
+  }
+  cluster.sync();                                 // nobody leaves while its shared memory is read
+}
+
+pctc_status_t check(const pctc_beam_t* p) {
+  if (!p) return PCTC_ERR_INVALID_ARG;
+  if (p->N <= 0 || p->B <= 0 || p->K <= 0 || p->V <= 0) return PCTC_ERR_INVALID_ARG;
+  if (p->dtype != PCTC_BF16 && p->dtype != PCTC_FP32) return PCTC_ERR_UNSUPPORTED;
+  if (p->B > SEL_MAX || p->K > SEL_MAX || p->V > SEL_MAX_V) return PCTC_ERR_UNSUPPORTED;
+  if (p->eos_id < -1 || (long long)p->eos_id >= p->V) return PCTC_ERR_INVALID_ARG;
+  if (p->stride_b < p->V || p->stride_n < 0) return PCTC_ERR_INVALID_ARG;
+  if ((long long)p->N * SEL_MAX > 0x3fffffffLL) return PCTC_ERR_UNSUPPORTED;
+  return PCTC_OK;
+}
+
+template <typename T, bool VEC>
+cudaError_t launch_select(const SelArgs& a, int C, cudaStream_t stream) {
+  const size_t dyn = (size_t)a.B * ((a.nb + C - 1) / C) * 4;
+  auto kern = k_beam_select<T, VEC>;
+  if (dyn + sizeof(SelShared) > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_MAX_DYN);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.N * C);
+  cfg.blockDim = dim3(SEL_THREADS);
+  cfg.dynamicSmemBytes = dyn;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
+// CTAs of a cluster: up to the portable 8, while every warp has a block of every row.
+int cluster_size(int nb) {
+  int C = 1;
+  while (C < 8 && nb >= C * 2 * SEL_WARPS) C *= 2;
+  return C;
+}
+
+}  // namespace
+}  // namespace pctc
+
+using namespace pctc;
+
+extern "C" {
+
+pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const float* scores, const uint8_t* finished,
+                               float* scores_out, int32_t* parents, int32_t* tokens, uint8_t* finished_out,
+                               int32_t* utt_flags, void* stream_v) {
+  const pctc_status_t st = check(p);
+  if (st != PCTC_OK) return st;
+  if (!logits || !scores || !scores_out || !parents || !tokens) return PCTC_ERR_INVALID_ARG;
+  if (finished && p->eos_id < 0) return PCTC_ERR_INVALID_ARG;
+  const size_t es = p->dtype == PCTC_BF16 ? 2 : 4;
+  if ((size_t)logits & (es - 1)) return PCTC_ERR_INVALID_ARG;
+  if (((size_t)scores | (size_t)scores_out | (size_t)parents | (size_t)tokens) & 3) return PCTC_ERR_INVALID_ARG;
+  SelArgs a;
+  a.logits = logits;
+  a.stride_n = p->stride_n;
+  a.stride_b = p->stride_b;
+  a.scores = scores;
+  a.finished = finished;
+  a.N = p->N; a.B = p->B; a.K = p->K; a.V = (int)p->V; a.eos = p->eos_id;
+  a.nb = (int)((p->V + SEL_BLOCK - 1) / SEL_BLOCK);
+  a.scores_out = scores_out;
+  a.parents = parents;
+  a.tokens = tokens;
+  a.finished_out = finished_out;
+  a.flags = utt_flags;
+  const int C = cluster_size(a.nb);
+  const bool vec = (((size_t)logits | (size_t)p->stride_n * es | (size_t)p->stride_b * es) & 15) == 0;
+  cudaStream_t stream = (cudaStream_t)stream_v;
+  const cudaError_t e = p->dtype == PCTC_BF16
+      ? (vec ? launch_select<__nv_bfloat16, true>(a, C, stream) : launch_select<__nv_bfloat16, false>(a, C, stream))
+      : (vec ? launch_select<float, true>(a, C, stream) : launch_select<float, false>(a, C, stream));
+  return e == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,67 @@
+"""Beam selection and reordering, without a GPU: the oracle on planted answers, and the refusals."""
+
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pruned_ctc_oracle as O
+from paper_2609_33645_b200 import binding
+
+AT = 1 << 20            # a made-up address: these calls return before they touch a device
+
+
+def test_oracle_selection():
+    x = np.log(np.array([[0.5, 0.25, 0.25], [0.1, 0.8, 0.1]]))
+    got, bad, _ = O.beam_select(x + 7.0, [-1.0, -1.0], 3)
+    assert not bad and [(b, v) for _, b, v in got] == [(1, 1), (0, 0), (0, 1)]
+    assert got[0][0] == pytest.approx(-1.0 + math.log(0.8))
+    got, _, _ = O.beam_select(x, [-1.0, -np.inf], 9)
+    assert [(b, v) for _, b, v in got] == [(0, 0), (0, 1), (0, 2)]
+    got, _, _ = O.beam_select(x, [-1.0, -1.1], 2, finished=[False, True], eos=2)
+    assert [(s, b, v) for s, b, v in got] == [(-1.1, 1, 2), (pytest.approx(-1 + math.log(0.5)), 0, 0)]
+    x[0, 1] = np.nan
+    assert O.beam_select(x, [-1.0, -1.0], 2)[1]
+
+
+def _problem(**kw):
+    d = dict(N=2, B=4, K=4, V=100, stride_n=400, stride_b=100, dtype=0, eos_id=-1)
+    d.update(kw)
+    return binding.BeamProblem(*[d[f] for f, _ in binding.BeamProblem._fields_])
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(N=0), 1), (dict(B=0), 1), (dict(K=0), 1), (dict(V=0), 1), (dict(B=33), 3), (dict(K=33), 3),
+    (dict(V=2 ** 21 + 1, stride_b=2 ** 22), 3), (dict(dtype=2), 3), (dict(eos_id=100), 1), (dict(eos_id=-2), 1),
+    (dict(stride_b=99), 1), (dict(stride_n=-1), 1), (dict(N=2 ** 30), 3),
+])
+def test_bad_selections_are_refused_before_any_launch(lib, kw, want):
+    p = _problem(**kw)
+    assert lib.load().pctc_beam_select(ctypes.byref(p), AT, AT, None, AT, AT, AT, None, None, None) == want
+
+
+def test_bad_pointers_are_refused_before_any_launch(lib):
+    p, f = _problem(), lib.load().pctc_beam_select
+    good = [AT, AT, None, AT, AT, AT, None, None, None]
+    for i in (0, 1, 3, 4, 5):
+        args = list(good)
+        args[i] = None
+        assert f(ctypes.byref(p), *args) == 1
+        args[i] = AT + 1
+        assert f(ctypes.byref(p), *args) == 1
+    args = list(good)
+    args[2] = AT                                            # ended beams without a token that ends
+    assert f(ctypes.byref(p), *args) == 1
+    assert f(None, *good) == 1
+
+
+def test_binding_refuses_what_it_cannot_hand_on():
+    x, s = torch.zeros(2, 4, 10), torch.zeros(2, 4)
+    with pytest.raises(ValueError, match="CUDA"):
+        binding.beam_select(x, s, 4)
+    with pytest.raises(ValueError, match="bf16 or fp32"):
+        binding.beam_select(x.double(), s, 4)
+    with pytest.raises(ValueError, match="bf16 or fp32"):
+        binding.beam_select(x[0], s, 4)

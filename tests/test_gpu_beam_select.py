@@ -1,0 +1,197 @@
+"""Beam selection on the GPU against the oracle in 64 bits on the same values.
+
+Parents and tokens have to be equal wherever neighbouring candidates are further apart than the error of a score;
+exact ties are ties on both sides.  That error: lse sums exponentials in fp32, each within about 2^-21 relative, and
+a thread adds a few hundred of them (2^-24 each, partly cancelling): 1e-6 bounds it with room.  Scores come back rounded
+to fp32: 2^-24 relative more."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pruned_ctc_oracle as O
+from paper_2609_33645_b200 import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+LSE_TOL = 1e-6
+
+
+def make(N, B, V, dtype, seed, scale=2.5, pad=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    full = (torch.randn(N, B, V + pad, generator=g, device=DEV) * scale).to(dtype)
+    full[:, :, V:] = 1e4 if pad else 0                      # what lies behind a row may not be read as its part
+    scores = -10 - 5 * torch.rand(N, B, generator=g, device=DEV)
+    return full[:, :, :V], scores
+
+
+def check(logits, scores, K, finished=None, eos=None):
+    r = binding.beam_select(logits, scores, K, finished=finished, eos_id=eos)
+    x, s = logits.float().cpu().numpy(), scores.cpu().numpy()
+    f = None if finished is None else finished.cpu().numpy()
+    out, parents, tokens, ended, flags = (r[q].cpu().numpy() for q in ("scores", "parents", "tokens", "finished", "flags"))
+    skipped = 0
+    for n in range(x.shape[0]):
+        want, bad, near = O.beam_select(x[n], s[n], K, None if f is None else f[n], eos)
+        assert flags[n] == (2 if bad else 0)
+        for k in range(K):
+            if k >= len(want):
+                assert out[n, k] == -math.inf and parents[n, k] == -1 and tokens[n, k] == -1 and not ended[n, k]
+                continue
+            score, b, v = want[k]
+            assert abs(float(out[n, k]) - score) <= LSE_TOL + 2.0 ** -23 * abs(score)
+            if near > 2 * LSE_TOL:
+                assert (parents[n, k], tokens[n, k]) == (b, v), (n, k)
+            assert ended[n, k] == ((f is not None and f[n, parents[n, k]]) or (eos is not None and tokens[n, k] == eos))
+        skipped += near <= 2 * LSE_TOL
+    assert skipped <= max(1, x.shape[0] // 8)
+    return r
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,B,K,V,pad", [
+    (1, 1, 1, 1, 0), (1, 1, 5, 1, 0), (2, 1, 4, 3, 0), (1, 4, 4, 255, 0), (3, 2, 7, 256, 0), (3, 4, 4, 257, 0),
+    (2, 3, 3, 1000, 0), (2, 8, 8, 1000, 24), (1, 32, 32, 1000, 0), (5, 5, 10, 4099, 0), (2, 16, 16, 5000, 3),
+    (1, 32, 32, 20001, 7), (9, 4, 4, 32768, 0), (1, 4, 4, 151936, 0), (4, 8, 8, 151936, 128), (2, 1, 32, 180000, 0),
+    (20, 2, 2, 65537, 0), (1, 2, 2, 2 ** 21, 0), (1, 31, 32, 70000, 1),
+])
+def test_against_the_oracle(N, B, K, V, pad, dtype):
+    logits, scores = make(N, B, V, dtype, V + B + K, pad=pad)
+    check(logits, scores, K)
+
+
+def test_the_widest_call():
+    logits, scores = make(1, 32, 2 ** 21, torch.bfloat16, 1)
+    r = binding.beam_select(logits, scores, 32)
+    lse = torch.logsumexp(logits.double(), -1)
+    cand = scores.double()[..., None] + (logits.double() - lse[..., None])
+    want, _ = torch.sort(cand.reshape(1, -1), descending=True, stable=True)
+    assert float((r["scores"].double() - want[:, :32]).abs().max()) <= LSE_TOL + 2.0 ** -23 * 40
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scale", [0.0, 0.01, 30.0])
+def test_ties_and_peaks(scale, dtype):
+    """Rows of equal logits, rows that repeat, and rows with one token that has it all."""
+    for B, K, V in [(4, 4, 1000), (3, 16, 3001), (8, 8, 40000), (32, 32, 9000)]:
+        logits, scores = make(2, B, V, dtype, 7, scale)
+        scores[:, 1:] = scores[:, :1]
+        logits[:, 1::2] = logits[:, :1]
+        check(logits, scores, K)
+
+
+def test_more_ties_than_the_lists_hold():
+    # blocks whose maxima all lie in one group of blocks: 33 blocks apart by 32, so that the candidates outgrow the lists
+    logits = torch.full((1, 32, 256 * 64), -50.0, device=DEV)
+    logits[:, :, 0:256] = 1.0
+    logits[:, :, 32 * 256:33 * 256] = 1.0
+    scores = torch.full((1, 32), -3.0, device=DEV)
+    check(logits, scores, 32)
+    scores = torch.arange(32, device=DEV).float()[None] * -1e-3
+    check(logits, scores, 32)
+
+
+def test_dead_ended_and_masked():
+    logits, scores = make(8, 4, 3000, torch.float32, 5)
+    finished = torch.zeros(8, 4, dtype=torch.bool, device=DEV)
+    scores[0, 1:] = -math.inf                               # a first step
+    scores[1] = -math.inf                                   # nothing is left
+    finished[2] = True                                      # all have ended
+    finished[3, 1] = True
+    scores[3, 1] = 0.0
+    finished[4, 0] = True
+    scores[4, 0] = -math.inf
+    logits[5, :, 5:] = -math.inf                            # few tokens allowed
+    logits[6] = -math.inf                                   # none
+    logits[6, 2, 77] = -3.0                                 # one
+    logits[7, 0] = -math.inf
+    for K in (1, 4, 16):
+        check(logits, scores, K, finished, 2)
+        check(logits.to(torch.bfloat16), scores, K, finished, 2999)
+    keep = logits[0, 1:].clone()
+    logits[0, 1:] = math.nan                                # a dead beam's logits do not count
+    logits[2] = math.nan                                    # nor an ended one's
+    check(logits, scores, 4, finished, 0)
+    logits[0, 1:] = keep
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_rows_that_are_not_finite_are_flagged(value):
+    logits, scores = make(3, 4, 30000, torch.bfloat16, 6)
+    logits[0, 2, 12345] = value
+    logits[1, 0, 29999] = value
+    logits[1, 1, 0] = value
+    scores[2, 3] = value
+    r = check(logits, scores, 4)
+    assert r["flags"].tolist() == [2, 2, 2] and not (r["parents"][0] == 2).any()
+    row = torch.full((1, 1, 600), -math.inf, device=DEV)
+    row[0, 0, 300] = value
+    check(row, torch.zeros(1, 1, device=DEV), 3)
+
+
+def test_lowest_value_masks():
+    """Masks of the type's lowest value instead of -inf."""
+    for dtype in (torch.float32, torch.bfloat16):
+        logits, scores = make(2, 4, 5000, dtype, 8)
+        logits[:, :, 100:] = torch.finfo(dtype).min
+        check(logits, scores, 4)
+        logits[1] = torch.finfo(dtype).min
+        check(logits, scores, 4)
+
+
+def test_strides():
+    logits, scores = make(3, 4, 1111, torch.bfloat16, 9, pad=9)
+    base = check(logits, scores, 4)
+    swapped = logits.transpose(0, 1).contiguous().transpose(0, 1)
+    a = binding.beam_select(swapped, scores, 4)
+    shared = logits[:1].expand(3, 4, 1111)                  # one utterance's logits for all: stride 0
+    b = binding.beam_select(shared, scores[:1].expand(3, 4).contiguous(), 4)
+    for q in ("parents", "tokens"):
+        assert torch.equal(a[q], base[q])
+        assert torch.equal(b[q], base[q][:1].expand(3, 4))
+    with pytest.raises(ValueError, match="contiguous rows"):
+        binding.beam_select(logits.transpose(1, 2), scores, 4)
+    with pytest.raises(ValueError, match="overlap"):
+        binding.beam_select(logits[:, :1].expand(3, 4, 1111), scores, 4)
+    with pytest.raises(ValueError, match="scores"):
+        binding.beam_select(logits, scores.double(), 4)
+    with pytest.raises(ValueError, match="finished"):
+        binding.beam_select(logits, scores, 4, finished=scores > 0)
+    with pytest.raises(ValueError, match="eos_id"):
+        binding.beam_select(logits, scores, 4, eos_id=1111)
+    with pytest.raises(binding.PctcError):
+        binding.beam_select(logits, scores, 33)
+
+
+def test_captured_into_a_graph_and_on_another_stream():
+    logits, scores = make(4, 4, 20000, torch.bfloat16, 10)
+    want = binding.beam_select(logits, scores, 4)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = binding.beam_select(logits, scores, 4)
+    torch.cuda.current_stream().wait_stream(side)
+    x = torch.zeros_like(logits)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = binding.beam_select(x, scores, 4)
+    x.copy_(logits)
+    graph.replay()
+    for q in ("scores", "parents", "tokens", "flags"):
+        assert torch.equal(r[q], want[q]) and torch.equal(other[q], want[q])
+
+
+def test_scores_may_be_written_over():
+    import ctypes
+    logits, scores = make(3, 4, 20000, torch.bfloat16, 12)
+    want = binding.beam_select(logits, scores, 4, finished=torch.zeros(3, 4, dtype=torch.bool, device=DEV), eos_id=0)
+    done = torch.zeros(3, 4, dtype=torch.bool, device=DEV)
+    p = binding.BeamProblem(3, 4, 4, 20000, logits.stride(0), logits.stride(1), 0, 0)
+    o = [torch.empty(3, 4, dtype=torch.int32, device=DEV) for _ in range(2)]
+    st = binding.load().pctc_beam_select(ctypes.byref(p), logits.data_ptr(), scores.data_ptr(), done.data_ptr(),
+                                         scores.data_ptr(), o[0].data_ptr(), o[1].data_ptr(), done.data_ptr(), None,
+                                         torch.cuda.current_stream().cuda_stream)
+    assert st == 0 and torch.equal(scores, want["scores"]) and torch.equal(o[0], want["parents"])
+    assert torch.equal(o[1], want["tokens"]) and torch.equal(done, want["finished"])
