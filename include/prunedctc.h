@@ -370,6 +370,35 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* problem, const void* logits, c
                                uint8_t* finished_out, int32_t* utt_flags, void* stream);
 
 /*
+ * Reordering of decoder states after a selection: dst[n,k] = src[n, parents[n,k]] for every state of a
+ * list (caches, token histories, recurrent states; any type), in one launch per 256 states.
+ * In place (dst == src, K == B, equal strides) needs no second buffer, and beams that stay in their slot
+ * cost nothing.  Slots whose parent lies outside [0, B) (-1: no candidate) are left as they are.
+ *
+ * A state's row of one beam is `segments` pieces, segment_stride bytes apart, of `units` units of
+ * unit_bytes each; with timed = 1 only the first lengths[n] units of every piece are moved and those behind
+ * are left as they are.  A cache [N,B,heads,L,D] is heads segments of L units of D values; a state [N,B,D]
+ * is one segment of one unit.  src and dst share that layout and may have other beam and utterance strides.
+ * What is written may overlap nothing else of the list: a state given twice, or rows into each other, is
+ * refused (PCTC_ERR_INVALID_ARG); views of one buffer that interleave row by row are told apart where
+ * their beam strides are equal.  16-byte aligned addresses, strides and units are moved fastest.
+ */
+typedef struct {
+  const void* src;
+  void* dst;
+  int64_t src_stride_n, src_stride_b, dst_stride_n, dst_stride_b;   /* bytes                    */
+  int64_t segments, segment_stride;                                 /* segment_stride in bytes  */
+  int64_t units, unit_bytes;
+  int32_t timed;
+  int32_t reserved;
+} pctc_beam_state_t;
+
+/* states HOST [n_states]; parents [N,K] int32 and lengths [N] int32 (NULL if no state is timed; a length
+ * is cut to 0 .. units) device.  May be captured into a CUDA graph and issued from several threads. */
+pctc_status_t pctc_beam_reorder(int32_t n_states, const pctc_beam_state_t* states, int32_t N, int32_t B, int32_t K,
+                                const int32_t* parents, const int32_t* lengths, void* stream);
+
+/*
  * Global gradient norm over many tensors, and clipping: what stands between the gradients of
  * pruned_ctc_fwd_bwd (with those of the model below it) and the weight update.
  *   S = sum over all tensors and values of g^2,  norm = sqrt(S),

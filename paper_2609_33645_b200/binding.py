@@ -25,7 +25,8 @@ EXPORTS = ("pctc_workspace_bytes", "pctc_chunk_width", "pruned_ctc_fwd_bwd", "pr
            "pruned_ctc_fwd_bwd_host", "pctc_subset_relabel_noalloc", "pctc_greedy_workspace_bytes",
            "pctc_greedy_decode", "pctc_topk_workspace_bytes", "pctc_topk_decode",
            "pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
-           "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read", "pctc_beam_select")
+           "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read", "pctc_beam_select",
+           "pctc_beam_reorder")
 NOALLOC_MAX_V = 262144
 
 PHASES = ("prep", "lse", "subset_logp", "dp", "dlogits", "dh", "dw", "dbias", "finish")
@@ -52,6 +53,15 @@ class BeamProblem(ctypes.Structure):
     _fields_ = [("N", ctypes.c_int32), ("B", ctypes.c_int32), ("K", ctypes.c_int32), ("V", ctypes.c_int64),
                 ("stride_n", ctypes.c_int64), ("stride_b", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("eos_id", ctypes.c_int32)]
+
+
+class BeamState(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p),
+                ("src_stride_n", ctypes.c_int64), ("src_stride_b", ctypes.c_int64),
+                ("dst_stride_n", ctypes.c_int64), ("dst_stride_b", ctypes.c_int64),
+                ("segments", ctypes.c_int64), ("segment_stride", ctypes.c_int64),
+                ("units", ctypes.c_int64), ("unit_bytes", ctypes.c_int64),
+                ("timed", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class TraceStruct(ctypes.Structure):
@@ -163,6 +173,9 @@ def _configure(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.pctc_prefix_read.argtypes = [prefix_p, vp, ctypes.c_size_t, vp, ctypes.c_int32, vp, vp, vp, vp]
     lib.pctc_beam_select.restype = ctypes.c_int
     lib.pctc_beam_select.argtypes = [ctypes.POINTER(BeamProblem)] + [vp] * 9
+    lib.pctc_beam_reorder.restype = ctypes.c_int
+    lib.pctc_beam_reorder.argtypes = [ctypes.c_int32, ctypes.POINTER(BeamState), ctypes.c_int32, ctypes.c_int32,
+                                      ctypes.c_int32, vp, vp, vp]
     lib.pctc_gemm_bf16.restype = ctypes.c_int
     lib.pctc_gemm_bf16.argtypes = [vp, vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                    ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp]
@@ -710,3 +723,74 @@ def beam_select(logits, scores, beams, *, finished=None, eos_id=None):
             _dptr(finished), _dptr(res["scores"]), _dptr(res["parents"]), _dptr(res["tokens"]), _dptr(res["finished"]),
             _dptr(res["flags"]))
     return res
+
+
+def _state_layout(x, axis, what):
+    """(utterance stride, beam stride, segments, segment stride, units, unit size) of a state [N, B, ...], in bytes."""
+    shape, strides, size = x.shape, x.stride(), x.element_size()
+    inner = 1
+    for d in range(x.dim() - 1, 1, -1):                     # contiguous behind the beam dimension
+        if shape[d] != 1 and strides[d] != inner:
+            raise ValueError(f"{what} must be contiguous behind the beam dimension")
+        inner *= shape[d]
+    if axis is None:
+        layout = (1, 0, 1, inner * size)
+    else:
+        if not 2 <= axis < x.dim():
+            raise ValueError("a time axis lies behind the beam dimension")
+        unit = size
+        for d in shape[axis + 1:]:
+            unit *= d
+        before = 1
+        for d in shape[2:axis]:
+            before *= d
+        layout = (before, shape[axis] * unit, shape[axis], unit)
+    return (strides[0] * size, strides[1] * size) + layout
+
+
+def beam_reorder(states, parents, *, lengths=None, time_axes=None, out=None):
+    """Move decoder states to the beams that were selected: state[n, k] = state[n, parents[n, k]] for every tensor
+    of `states` ([N, B, ...] of any type, contiguous behind the beam dimension), in one launch.
+
+    parents [N, K] int32 (beam_select's; entries outside [0, B) leave their slot as it is).  out: tensors
+    [N, K, ...] to write to; None: in place (K == B).  time_axes: for each state the dimension of which only
+    the first lengths[n] entries (lengths [N] int32 on the device) are moved, or None for whole rows; what lies
+    behind is left as it is.  Returns the list of written tensors.
+    """
+    import torch
+
+    states = list(states)
+    if not states:
+        raise ValueError("states must hold at least one tensor")
+    dev = states[0].device
+    if dev.type != "cuda":
+        raise ValueError("states must be CUDA tensors")
+    if parents.dtype != torch.int32 or parents.dim() != 2 or not parents.is_contiguous() or parents.device != dev:
+        raise ValueError("parents must be contiguous int32 [N, K] on the states' device")
+    N, K = parents.shape
+    outs = states if out is None else list(out)
+    axes = [None] * len(states) if time_axes is None else list(time_axes)
+    if len(outs) != len(states) or len(axes) != len(states):
+        raise ValueError("out and time_axes must have one entry for every state")
+    if lengths is None:
+        if any(a is not None for a in axes):
+            raise ValueError("a time axis needs lengths")
+    elif lengths.dtype != torch.int32 or lengths.shape != (N,) or not lengths.is_contiguous() or lengths.device != dev:
+        raise ValueError("lengths must be contiguous int32 [N] on the states' device")
+    B = states[0].shape[1] if states[0].dim() > 1 else 0
+    table = (BeamState * len(states))()
+    used = 0
+    for x, o, axis in zip(states, outs, axes):
+        if x.dim() < 2 or x.shape[0] != N or x.shape[1] != B or x.device != dev:
+            raise ValueError("states must be [N, B, ...] on one device")
+        if o.shape != x.shape[:1] + (K,) + x.shape[2:] or o.dtype != x.dtype or o.device != dev:
+            raise ValueError("out must be [N, K, ...] tensors of the states' types" if out is not None else
+                             "in place, parents must have as many columns as the states have beams")
+        if x.numel() == 0:
+            continue
+        sn, sb, *row = _state_layout(x, axis, "states")
+        on, ob = (sn, sb) if o is x else _state_layout(o, axis, "out")[:2]
+        table[used] = BeamState(x.data_ptr(), o.data_ptr(), sn, sb, on, ob, *row, 0 if axis is None else 1, 0)
+        used += 1
+    _run_on(dev, load().pctc_beam_reorder, "pctc_beam_reorder", used, table, N, B, K, _dptr(parents), _dptr(lengths))
+    return outs

@@ -23,6 +23,8 @@
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
+#include <new>
+
 namespace cg = cooperative_groups;
 
 namespace pctc {
@@ -532,6 +534,245 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const f
       ? (vec ? launch_select<__nv_bfloat16, true>(a, C, stream) : launch_select<__nv_bfloat16, false>(a, C, stream))
       : (vec ? launch_select<float, true>(a, C, stream) : launch_select<float, false>(a, C, stream));
   return e == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Reordering of states
+// ---------------------------------------------------------------------------
+//
+// out[n, k] = in[n, parents[n, k]] for a list of states.  A state's row of one beam is `segments` pieces of
+// `units` units each (the units of a time axis, of which only the first lengths[n] count).  A CTA owns a column:
+// the same bytes of all beams of an utterance; a thread loads its 1 to 16 bytes of every parent before it
+// stores any.  So a parent that several beams share is read once, and in place needs no second buffer: nobody
+// else touches the column.  In place a beam that stays where it is moves nothing.
+namespace pctc {
+namespace {
+
+constexpr int MOVE_THREADS = 256;
+constexpr int MOVE_ROWS = 2;                      // 16-byte columns a thread works on at a time
+constexpr int MOVE_CTAS_PER_SM = 4;
+
+struct MoveState {
+  const char* src;
+  char* dst;
+  long long src_n, src_b, dst_n, dst_b;           // byte strides of utterances and beams
+  long long seg;                                  // byte stride of segments
+  long long unit;                                 // bytes of a unit
+  int segments, units;                            // units: of the whole axis (lengths are cut to it)
+  int tiles;                                      // tiles of one segment
+  int timed;                                      // lengths apply
+  int width;                                      // bytes a thread moves at a time: 16, 8, 4, 2 or 1
+};
+template <int LIM>
+struct MoveTable {
+  MoveState s[LIM];
+  int tile0[LIM + 1];                             // tiles before state i
+  int n;
+};
+constexpr int MOVE_SMALL = 32, MOVE_LARGE = 256;
+static_assert(sizeof(MoveTable<MOVE_LARGE>) <= 32000, "kernel parameters");
+
+template <typename U, int KB>
+__device__ __forceinline__ void move_tile(const MoveState& s, const int* __restrict__ par, int K, long long bytes, int n,
+                                          int seg, int tile) {
+  const bool in_place = s.src == s.dst;
+  const char* src = s.src + n * s.src_n + seg * s.seg;
+  char* dst = s.dst + n * s.dst_n + seg * s.seg;
+  const long long first = ((long long)tile * MOVE_ROWS * MOVE_THREADS + threadIdx.x) * (int)sizeof(U);
+#pragma unroll(KB <= 4 ? MOVE_ROWS : 1)          // a column of 8 beams or more is enough in flight
+  for (int q = 0; q < MOVE_ROWS; ++q) {
+    const long long at = first + (long long)q * MOVE_THREADS * (int)sizeof(U);
+    if (at >= bytes) return;
+    U v[KB];
+#pragma unroll
+    for (int k = 0; k < KB; ++k)
+      if (k < K && par[k] >= 0 && !(in_place && par[k] == k)) v[k] = *(const U*)(src + par[k] * s.src_b + at);
+#pragma unroll
+    for (int k = 0; k < KB; ++k)
+      if (k < K && par[k] >= 0 && !(in_place && par[k] == k)) *(U*)(dst + k * s.dst_b + at) = v[k];
+  }
+}
+
+template <int LIM, int KB>
+__global__ void __launch_bounds__(MOVE_THREADS) k_beam_move(const __grid_constant__ MoveTable<LIM> tab,
+                                                            const int* __restrict__ parents,
+                                                            const int* __restrict__ lengths, int N, int B, int K) {
+  __shared__ int par[KB];
+  const int total = tab.tile0[tab.n];
+  for (int t = blockIdx.x; t < total; t += gridDim.x) {
+    int lo = 0, hi = tab.n - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (tab.tile0[mid] <= t) lo = mid; else hi = mid - 1;
+    }
+    const MoveState& s = tab.s[lo];
+    const int local = t - tab.tile0[lo];
+    const int tile = local % s.tiles, ns = local / s.tiles, seg = ns % s.segments, n = ns / s.segments;
+    int units = s.units;
+    if (s.timed) units = min(max(lengths[n], 0), units);
+    const long long bytes = units * s.unit;
+    if ((long long)tile * MOVE_ROWS * MOVE_THREADS * s.width >= bytes) continue;
+    __syncthreads();                              // the tile before has read its parents
+    if (threadIdx.x < K) {
+      const int p = parents[n * K + threadIdx.x];
+      par[threadIdx.x] = p >= 0 && p < B ? p : -1;
+    }
+    __syncthreads();
+    switch (s.width) {
+      case 16: move_tile<uint4, KB>(s, par, K, bytes, n, seg, tile); break;
+      case 8: move_tile<uint2, KB>(s, par, K, bytes, n, seg, tile); break;
+      case 4: move_tile<unsigned, KB>(s, par, K, bytes, n, seg, tile); break;
+      case 2: move_tile<unsigned short, KB>(s, par, K, bytes, n, seg, tile); break;
+      default: move_tile<unsigned char, KB>(s, par, K, bytes, n, seg, tile); break;
+    }
+  }
+}
+
+// The rows of a state's beams as byte ranges: base + i * outer + j * inner, i < N, j < rows, each `len` long.
+struct RowSet {
+  size_t base;
+  long long outer, inner, len;
+  int rows;
+  bool write;
+  size_t end(int N) const { return base + (size_t)((N - 1) * outer + (rows - 1) * inner + len); }
+};
+// Whether two sets of rows share a byte.  Exact where one set's rows repeat with the other's beam stride (views of
+// one buffer); otherwise ranges that interleave count as shared.
+bool rows_clash(const RowSet& a, const RowSet& b, int N) {
+  if (a.end(N) <= b.base || b.end(N) <= a.base) return false;
+  if (a.inner != b.inner || a.inner <= 0 || a.len > a.inner || b.len > b.inner) return true;
+  if (N > 1 && (a.outer % a.inner || b.outer % b.inner)) return true;
+  const long long d = (long long)((a.base > b.base ? a.base - b.base : b.base - a.base) % (size_t)a.inner);
+  const long long first = a.base > b.base ? b.len : a.len, second = a.base > b.base ? a.len : b.len;
+  return !(first <= d && d + second <= a.inner);
+}
+
+pctc_status_t check_move(const pctc_beam_state_t* st, int n, int N, int B, int K, const int32_t* lengths) {
+  if (n < 0 || N <= 0 || B <= 0 || K <= 0 || (n && !st)) return PCTC_ERR_INVALID_ARG;
+  if (B > SEL_MAX || K > SEL_MAX) return PCTC_ERR_UNSUPPORTED;
+  for (int i = 0; i < n; ++i) {
+    const pctc_beam_state_t& s = st[i];
+    if (!s.src || !s.dst || s.segments <= 0 || s.units < 0 || s.unit_bytes <= 0) return PCTC_ERR_INVALID_ARG;
+    if (s.timed & ~1) return PCTC_ERR_INVALID_ARG;
+    if (s.timed && !lengths) return PCTC_ERR_INVALID_ARG;
+    const long long most = 1LL << 46;
+    if (s.unit_bytes > most || s.units > most / s.unit_bytes || s.segments > 0x7fffffffLL || s.units > 0x7fffffffLL)
+      return PCTC_ERR_UNSUPPORTED;
+    const long long len = s.units * s.unit_bytes;
+    if (s.segments > 1 && (s.segment_stride < len || s.segment_stride > most / s.segments)) return PCTC_ERR_INVALID_ARG;
+    const long long row = (s.segments - 1) * s.segment_stride + len;
+    if (s.src_stride_b < 0 || s.dst_stride_b < 0 || s.src_stride_n < 0 || s.dst_stride_n < 0) return PCTC_ERR_INVALID_ARG;
+    if (s.src_stride_b > most || s.dst_stride_b > most || s.src_stride_n > most || s.dst_stride_n > most)
+      return PCTC_ERR_UNSUPPORTED;
+    // written rows are apart: beams inside utterances, or utterances inside beams
+    const long long sn = N > 1 ? s.dst_stride_n : most, sb = K > 1 ? s.dst_stride_b : most;
+    const bool by_utt = sb >= row && (N == 1 || sn >= (K > 1 ? (K - 1) * sb : 0) + row);
+    const bool by_beam = sn >= row && (K == 1 || sb >= (N > 1 ? (N - 1) * sn : 0) + row);
+    if (!by_utt && !by_beam) return PCTC_ERR_INVALID_ARG;
+    if (s.src == s.dst && (K != B || (B > 1 && s.src_stride_b != s.dst_stride_b) ||
+                           (N > 1 && s.src_stride_n != s.dst_stride_n)))
+      return PCTC_ERR_INVALID_ARG;
+  }
+  return PCTC_OK;
+}
+
+// What the call writes may overlap nothing else of the list (in place: a state's own rows, which are one set).
+pctc_status_t check_overlap(const pctc_beam_state_t* st, int n, int N, int B, int K) {
+  RowSet* r = new (std::nothrow) RowSet[2 * (size_t)(n > 0 ? n : 1)];
+  if (!r) return PCTC_ERR_HOST_MEMORY;
+  int m = 0;
+  for (int i = 0; i < n; ++i) {
+    const pctc_beam_state_t& s = st[i];
+    const long long row = (s.segments - 1) * s.segment_stride + s.units * s.unit_bytes;
+    if (row == 0) continue;
+    r[m++] = RowSet{(size_t)s.dst, s.dst_stride_n, s.dst_stride_b, row, K, true};
+    if (s.src != s.dst) r[m++] = RowSet{(size_t)s.src, s.src_stride_n, s.src_stride_b, row, B, false};
+  }
+  std::sort(r, r + m, [](const RowSet& a, const RowSet& b) { return a.base < b.base; });
+  bool clash = false;
+  for (int i = 0; i < m && !clash; ++i) {
+    const size_t end = r[i].end(N);
+    for (int j = i + 1; j < m && r[j].base < end && !clash; ++j)
+      if (r[i].write || r[j].write) clash = rows_clash(r[i], r[j], N);
+  }
+  delete[] r;
+  return clash ? PCTC_ERR_INVALID_ARG : PCTC_OK;
+}
+
+template <int LIM, int KB>
+cudaError_t launch_move(const MoveTable<LIM>& tab, const int* parents, const int* lengths, int N, int B, int K,
+                        cudaStream_t stream) {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    sms = 148;
+  const int total = tab.tile0[tab.n], most = sms * MOVE_CTAS_PER_SM;
+  k_beam_move<LIM, KB><<<total < most ? total : most, MOVE_THREADS, 0, stream>>>(tab, parents, lengths, N, B, K);
+  return cudaGetLastError();
+}
+
+template <int LIM>
+pctc_status_t move_all(const pctc_beam_state_t* st, int n, int N, int B, int K, const int* parents, const int* lengths,
+                       cudaStream_t stream) {
+  MoveTable<LIM> tab;
+  for (int i0 = 0; i0 < n; i0 += LIM) {
+    tab.n = 0;
+    long long tiles = 0;
+    for (int i = i0; i < n && i < i0 + LIM; ++i) {
+      const pctc_beam_state_t& s = st[i];
+      const long long len = s.units * s.unit_bytes;
+      if (len == 0) continue;
+      MoveState& m = tab.s[tab.n];
+      m.src = (const char*)s.src;
+      m.dst = (char*)s.dst;
+      m.src_n = N > 1 ? s.src_stride_n : 0;
+      m.src_b = B > 1 ? s.src_stride_b : 0;
+      m.dst_n = N > 1 ? s.dst_stride_n : 0;
+      m.dst_b = K > 1 ? s.dst_stride_b : 0;
+      m.seg = s.segments > 1 ? s.segment_stride : 0;
+      m.unit = s.timed ? s.unit_bytes : len;
+      m.units = s.timed ? (int)s.units : 1;
+      m.segments = (int)s.segments;
+      m.timed = s.timed;
+      // as wide as all addresses and lengths allow
+      const size_t all = (size_t)m.src | (size_t)m.dst | (size_t)(m.src_n | m.src_b | m.dst_n | m.dst_b | m.seg | m.unit);
+      m.width = 16;
+      while (all & (size_t)(m.width - 1)) m.width /= 2;
+      const long long per = (long long)MOVE_ROWS * MOVE_THREADS * m.width, t = (len + per - 1) / per;
+      if (t > 0x7fffffffLL) return PCTC_ERR_UNSUPPORTED;
+      m.tiles = (int)t;
+      tab.tile0[tab.n++] = (int)tiles;
+      if (t * N > 0x7fffffffLL / m.segments) return PCTC_ERR_UNSUPPORTED;
+      tiles += t * N * m.segments;
+      if (tiles > 0x7fff0000LL) return PCTC_ERR_UNSUPPORTED;
+    }
+    tab.tile0[tab.n] = (int)tiles;
+    if (!tab.n) continue;
+    const cudaError_t e = K <= 4 ? launch_move<LIM, 4>(tab, parents, lengths, N, B, K, stream)
+                        : K <= 8 ? launch_move<LIM, 8>(tab, parents, lengths, N, B, K, stream)
+                        : K <= 16 ? launch_move<LIM, 16>(tab, parents, lengths, N, B, K, stream)
+                                  : launch_move<LIM, 32>(tab, parents, lengths, N, B, K, stream);
+    if (e != cudaSuccess) return PCTC_ERR_CUDA;
+  }
+  return PCTC_OK;
+}
+
+}  // namespace
+}  // namespace pctc
+
+extern "C" {
+
+pctc_status_t pctc_beam_reorder(int32_t n_states, const pctc_beam_state_t* states, int32_t N, int32_t B, int32_t K,
+                                const int32_t* parents, const int32_t* lengths, void* stream_v) {
+  pctc_status_t st = check_move(states, n_states, N, B, K, lengths);
+  if (st != PCTC_OK) return st;
+  if (!parents || ((size_t)parents & 3) || ((size_t)lengths & 3)) return PCTC_ERR_INVALID_ARG;
+  st = check_overlap(states, n_states, N, B, K);
+  if (st != PCTC_OK) return st;
+  cudaStream_t stream = (cudaStream_t)stream_v;
+  return n_states <= MOVE_SMALL ? move_all<MOVE_SMALL>(states, n_states, N, B, K, parents, lengths, stream)
+                                : move_all<MOVE_LARGE>(states, n_states, N, B, K, parents, lengths, stream);
 }
 
 }  // extern "C"

@@ -65,3 +65,55 @@ def test_binding_refuses_what_it_cannot_hand_on():
         binding.beam_select(x.double(), s, 4)
     with pytest.raises(ValueError, match="bf16 or fp32"):
         binding.beam_select(x[0], s, 4)
+
+
+def _state(**kw):
+    d = dict(src=AT, dst=AT, src_stride_n=400, src_stride_b=100, dst_stride_n=400, dst_stride_b=100, segments=1,
+             segment_stride=0, units=25, unit_bytes=4, timed=0, reserved=0)
+    d.update(kw)
+    return binding.BeamState(*[d[f] for f, _ in binding.BeamState._fields_])
+
+
+def _reorder(lib, states, N=2, B=4, K=4, parents=AT, lengths=None, n=None):
+    table = (binding.BeamState * max(1, len(states)))(*states)
+    return lib.load().pctc_beam_reorder(len(states) if n is None else n, table, N, B, K, parents, lengths, None)
+
+
+FAR = AT * 16
+
+
+@pytest.mark.parametrize("states,kw,want", [
+    ([_state(src=None)], {}, 1), ([_state(dst=None)], {}, 1), ([_state(segments=0)], {}, 1), ([_state(units=-1)], {}, 1),
+    ([_state(unit_bytes=0)], {}, 1), ([_state(timed=2)], {}, 1), ([_state(timed=1)], {}, 1),
+    ([_state(unit_bytes=2 ** 50)], {}, 3),
+    ([_state(segments=2, segment_stride=99)], {}, 1),                       # segments into each other
+    ([_state(dst=FAR, dst_stride_b=99)], {}, 1),                            # written rows into each other
+    ([_state(dst=FAR, dst_stride_n=399)], {}, 1), ([_state(dst=FAR, dst_stride_n=0)], {}, 1),
+    ([_state(dst=FAR, src_stride_b=-100)], {}, 1),
+    ([_state(dst_stride_b=104, dst_stride_n=416)], {}, 1),                  # in place with other strides
+    ([_state()], dict(K=3), 1),                                             # in place with fewer beams
+    ([_state(dst=AT + 100)], {}, 1), ([_state(dst=AT - 96)], {}, 1),        # rows into each other
+    ([_state(), _state()], {}, 1),                                          # the same state twice
+    ([_state(), _state(dst=FAR, src=AT + 50)], {}, 1),                      # what one writes another reads
+    ([_state(dst=FAR), _state(src=FAR * 2, dst=FAR + 300)], {}, 1),
+    ([_state(src_stride_b=200, dst_stride_b=200, src_stride_n=800, dst_stride_n=800),
+      _state(src=AT + 99, dst=AT + 99, src_stride_b=200, dst_stride_b=200, src_stride_n=800, dst_stride_n=800)], {}, 1),
+    ([_state()], dict(N=0), 1), ([_state()], dict(B=0), 1), ([_state()], dict(B=33, K=33), 3), ([_state()], dict(n=-1), 1),
+    ([_state()], dict(parents=None), 1), ([_state()], dict(parents=AT + 2), 1),
+    ([_state(timed=1)], dict(lengths=AT + 1), 1),
+])
+def test_bad_states_are_refused_before_any_launch(lib, states, kw, want):
+    assert _reorder(lib, states, **kw) == want
+
+
+def test_nothing_to_move_is_no_error(lib):
+    assert _reorder(lib, []) == 0
+    assert _reorder(lib, [_state(units=0)]) == 0
+
+
+def test_reorder_binding_refuses_what_it_cannot_hand_on():
+    p = torch.zeros(2, 4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="at least one"):
+        binding.beam_reorder([], p)
+    with pytest.raises(ValueError, match="CUDA"):
+        binding.beam_reorder([torch.zeros(2, 4, 5)], p)
