@@ -64,220 +64,384 @@ __device__ __forceinline__ double round24(double p) {
   return __longlong_as_double(b & ~((1ll << 29) - 1));
 }
 
-struct Tile {                                     // staged frames
-  double p[PFX_TILE][PFX_MAX_K];
-  int cls[PFX_TILE][PFX_MAX_K];                   // -2: no class (absent, impossible, second of its kind)
+// Frames staged for the search: KM >= k classes a frame.  The blank stands in `blank` only; what does not count
+// (absent, impossible, the second of its kind, behind k) has class -2 and probability 0.
+template <int KM>
+struct Tile {
+  double p[PFX_TILE][KM];
+  int cls[PFX_TILE][KM];
   double blank[PFX_TILE];
   double shift[PFX_TILE];
 };
 
-// One warp a frame, one lane a class.
-__device__ void stage_frame(Tile& t, int f, const int* cls, const float* lp, int k, int blank, int* flags) {
-  const int lane = threadIdx.x & 31;
-  const int c = lane < k ? cls[lane] : -1;
-  const float v = lane < k ? lp[lane] : -CUDART_INF_F;
-  const bool bad = c >= 0 && (isnan(v) || v == CUDART_INF_F);
-  bool ok = c >= 0 && isfinite(v);
-  const unsigned same = __match_any_sync(0xffffffffu, ok ? c : -1 - lane);
-  ok = ok && (same & ((1u << lane) - 1)) == 0;    // a class given twice counts where it stands first
-  float top = ok ? v : -CUDART_INF_F;
+// Stages frames f0, f0 + step, ... of a tile: KM lanes a frame.
+template <int KM>
+__device__ __forceinline__ void stage(Tile<KM>& t, int nf, int warp, int warps, const int* cls, const float* lp, int k,
+                                      int blank, int* flags) {
+  constexpr int PER = 32 / KM;
+  const int lane = threadIdx.x & 31, j = lane % KM, sub = lane / KM;
+  for (int f0 = warp * PER; f0 < nf; f0 += warps * PER) {
+    const int f = f0 + sub;
+    const bool in = f < nf && j < k;
+    const int c = in ? cls[(size_t)f * k + j] : -1;
+    const float v = in ? lp[(size_t)f * k + j] : -CUDART_INF_F;
+    const bool bad = c >= 0 && (isnan(v) || v == CUDART_INF_F);
+    bool ok = c >= 0 && isfinite(v);
+    const int mine = ok ? c : -1 - lane;
+    bool again = false;                           // a class given twice counts where it stands first
 #pragma unroll
-  for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (top == -CUDART_INF_F) top = 0.f;
-  const double z = (double)v - (double)top;
-  ok = ok && z >= -700.0;
-  const double p = ok ? round24(exp(z)) : 0.0;
-  const unsigned isb = __ballot_sync(0xffffffffu, ok && c == blank);
-  const double pbl = __shfl_sync(0xffffffffu, p, isb ? __ffs(isb) - 1 : 0);
-  if (lane < k) {
-    t.p[f][lane] = p;
-    t.cls[f][lane] = ok ? c : -2;
+    for (int d = 1; d < KM; ++d) {
+      const int o = __shfl_up_sync(0xffffffffu, mine, d, KM);
+      again = again || (j >= d && o == mine);
+    }
+    ok = ok && !again;
+    float top = ok ? v : -CUDART_INF_F;
+#pragma unroll
+    for (int o = KM / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o, KM));
+    if (top == -CUDART_INF_F) top = 0.f;
+    const double z = (double)v - (double)top;
+    ok = ok && z >= -700.0;
+    const double p = ok ? round24(exp(z)) : 0.0;
+    const bool is_blank = ok && c == blank;
+    if (f < nf) {
+      t.p[f][j] = is_blank ? 0.0 : p;
+      t.cls[f][j] = ok && !is_blank ? c : -2;
+    }
+    double pbl = is_blank ? p : 0.0;
+#pragma unroll
+    for (int o = KM / 2; o; o >>= 1) pbl = fmax(pbl, __shfl_xor_sync(0xffffffffu, pbl, o, KM));
+    if (f < nf && j == 0) {
+      t.blank[f] = pbl;
+      t.shift[f] = (double)top;
+    }
+    if (bad) atomicOr(flags, PCTC_UTT_NONFINITE);
   }
-  if (lane == 0) {
-    t.blank[f] = isb ? pbl : 0.0;
-    t.shift[f] = (double)top;
-  }
-  if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(flags, PCTC_UTT_NONFINITE);
 }
 
+__device__ __forceinline__ unsigned hi_word(double x) { return (unsigned)__double2hiint(x); }
+
+// One CTA an utterance: warp 0 searches, one lane a slot, while the others stage the next frames.  The search is
+// a chain of dependent frames, so what counts is its latency: everything of a slot lives in its lane's
+// registers, lanes talk by shuffles and a few words of shared memory, and the only barrier is one per 32 frames.
+// Candidates are ranked by counting, in two steps: the `beams`-th largest of the stays and every slot's best
+// extension bounds the result from below (compared by the upper 32 bits, which order non-negative doubles up
+// to ties), and only what reaches the bound is ranked exactly; in most frames of speech the blank or the last
+// label takes nearly all, and no extension reaches even the worst stay.
+template <int KM>
 __global__ void __launch_bounds__(PFX_THREADS) k_prefix_advance(
     const int* __restrict__ classes, const float* __restrict__ logprobs, const __grid_constant__ Lengths len, int n0,
     int T, int k, int B, int blank, int max_frames, int fresh, char* __restrict__ states, int2* __restrict__ nodes) {
-  __shared__ Tile tile;
-  __shared__ Slots buf[2];
-  __shared__ double key[PFX_MAX_BEAMS * (PFX_MAX_K + 1)];
-  __shared__ double new_b[PFX_MAX_BEAMS], new_n[PFX_MAX_BEAMS];
-  __shared__ unsigned taken[PFX_MAX_BEAMS];
+  constexpr unsigned ALL = 0xffffffffu;
+  __shared__ Tile<KM> tiles[2];
+  __shared__ __align__(16) double key[PFX_MAX_BEAMS * (KM + 1) + 2];
+  __shared__ short code[PFX_MAX_BEAMS * (KM + 1) + 2];     // stay of slot r: r; slot r grown by class j: 32 + r * 32 + j
+  __shared__ __align__(16) unsigned bound[64];
+  __shared__ unsigned taken[32];
+  __shared__ int order[32], moved[32];
   __shared__ int flags;
-  const int n = n0 + blockIdx.x, tid = threadIdx.x, warp = tid >> 5;
+  const int n = n0 + blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int Tn = len.n[blockIdx.x];
   PrefixState* st = (PrefixState*)(states + (size_t)n * PFX_STATE_BYTES);
   int2* my_nodes = nodes + (size_t)n * nodes_per_utt(B, max_frames);
-  int frames0 = 0, power = 0;
-  double shift = 0.0;
-  if (fresh) {
-    if (tid < B) {
-      buf[0].pb[tid] = tid == 0 ? 1.0 : 0.0;
-      buf[0].pn[tid] = 0.0;
-      buf[0].hash[tid] = buf[0].up[tid] = 0;
-      buf[0].last[tid] = -1;
-      buf[0].size[tid] = buf[0].node[tid] = 0;
-    }
-    if (tid == 0) { flags = 0; my_nodes[0] = make_int2(-1, -1); }
-  } else {
+  if (!fresh) {
     // a state that was not started with these sizes, or has no room for the frames, takes nothing
-    if (st->magic != PFX_MAGIC || st->beams != B || st->max_frames != max_frames || st->frames < 0 ||
-        st->frames > max_frames - Tn) {
+    const bool fits = st->magic == PFX_MAGIC && st->beams == B && st->max_frames == max_frames && st->frames >= 0 &&
+                      st->frames <= max_frames - Tn;
+    if (!fits) {
       if (tid == 0) atomicOr(&st->flags, PCTC_UTT_STATE_FULL);
       return;
     }
-    frames0 = st->frames;
-    power = st->power;
-    shift = st->shift;
-    for (int i = tid; i < (int)(sizeof(Slots) / 4); i += PFX_THREADS) ((int*)&buf[0])[i] = ((const int*)&st->s)[i];
-    if (tid == 0) flags = st->flags;
   }
-  __syncthreads();
-  const int nc = B * (k + 1);
-  int cur = 0;
-  for (int t0 = 0; t0 < Tn; t0 += PFX_TILE) {
-    const int nf = Tn - t0 < PFX_TILE ? Tn - t0 : PFX_TILE;
-    for (int f = warp; f < nf; f += PFX_THREADS / 32) {
-      const size_t at = ((size_t)n * T + t0 + f) * k;
-      stage_frame(tile, f, classes + at, logprobs + at, k, blank, &flags);
+  int frames0 = 0, power = 0;
+  double shift = 0.0;
+  double pb = 0.0, pn = 0.0;
+  unsigned long long hash = 0, up = 0;
+  int last = -1, size = 0, node = 0, par = -1;    // par: the slot that holds the prefix without its last label
+  if (warp == 0) {
+    if (fresh) {
+      if (lane == 0) { pb = 1.0; my_nodes[0] = make_int2(-1, -1); }
+    } else {
+      frames0 = st->frames;
+      power = st->power;
+      shift = st->shift;
+      if (lane < B) {
+        pb = st->s.pb[lane]; pn = st->s.pn[lane];
+        hash = st->s.hash[lane]; up = st->s.up[lane];
+        last = st->s.last[lane]; size = st->s.size[lane]; node = st->s.node[lane];
+      }
+      for (int r = 0; r < B; ++r) {
+        const unsigned long long h = __shfl_sync(ALL, hash, r);
+        const bool live = __shfl_sync(ALL, pb + pn, r) > 0.0;
+        if (live && size > 0 && h == up) par = r;
+      }
     }
-    __syncthreads();
-    for (int f = 0; f < nf; ++f) {
-      Slots& a = buf[cur];
-      Slots& b = buf[cur ^ 1];
-      const int frame = frames0 + t0 + f;
-      if (tid < B) taken[tid] = 0;
-      __syncthreads();
-      if (tid < B) {
-        const int last = a.last[tid];
-        const double total = __dadd_rn(a.pb[tid], a.pn[tid]);
+    taken[lane] = 0;
+    moved[lane] = -1;
+  }
+  if (tid == 0) flags = fresh ? 0 : st->flags;
+  __syncthreads();
+  const int* cls_n = classes + (size_t)n * T * k;
+  const float* lp_n = logprobs + (size_t)n * T * k;
+  stage<KM>(tiles[0], min(Tn, PFX_TILE), warp, PFX_THREADS / 32, cls_n, lp_n, k, blank, &flags);
+  __syncthreads();
+
+  for (int t0 = 0; t0 < Tn; t0 += PFX_TILE) {
+    Tile<KM>& tile = tiles[(t0 / PFX_TILE) & 1];
+    const int nf = min(Tn - t0, PFX_TILE);
+    if (warp > 0) {
+      const int t1 = t0 + PFX_TILE;
+      if (t1 < Tn)
+        stage<KM>(tiles[(t1 / PFX_TILE) & 1], min(Tn - t1, PFX_TILE), warp - 1, PFX_THREADS / 32 - 1,
+                  cls_n + (size_t)t1 * k, lp_n + (size_t)t1 * k, k, blank, &flags);
+    } else {
+      for (int f = 0; f < nf; ++f) {
+        const int frame = frames0 + t0 + f;
+        // ---- candidates of this lane's slot ----
+        const double total = __dadd_rn(pb, pn);
+        double v[KM];
         int jl = -1;
-        for (int j = 0; j < k; ++j)
-          if (tile.cls[f][j] == last) jl = j;
+#pragma unroll
+        for (int j = 0; j < KM; ++j) {
+          const bool same = tile.cls[f][j] == last;
+          if (same) jl = j;
+          v[j] = __dmul_rn(same ? pb : total, tile.p[f][j]);
+        }
         const double pl = jl >= 0 ? tile.p[f][jl] : 0.0;
         const double sb = __dmul_rn(total, tile.blank[f]);
-        double sn = __dmul_rn(a.pn[tid], pl);
-        if (jl >= 0 && total > 0.0) {
-          for (int r = 0; r < B; ++r) {
-            const double rt = __dadd_rn(a.pb[r], a.pn[r]);
-            if (rt > 0.0 && a.hash[r] == a.up[tid] && a.size[r] + 1 == a.size[tid]) {
-              sn = __dadd_rn(sn, __dmul_rn(a.last[r] == last ? a.pb[r] : rt, pl));
-              atomicOr(&taken[r], 1u << jl);
-              break;
+        double sn = __dmul_rn(pn, pl);
+        const bool child = par >= 0 && jl >= 0 && total > 0.0;
+        if (__any_sync(ALL, child)) {             // slot par grown by `last` is this slot's prefix
+          const int r = child ? par : lane;
+          const int rl = __shfl_sync(ALL, last, r);
+          const double rb = __shfl_sync(ALL, pb, r), rt = __shfl_sync(ALL, total, r);
+          if (child) {
+            sn = __dadd_rn(sn, __dmul_rn(rl == last ? rb : rt, pl));
+            atomicOr(&taken[par], 1u << jl);
+          }
+          __syncwarp();
+          const unsigned gone = taken[lane];
+          taken[lane] = 0;
+          if (gone) {
+#pragma unroll
+            for (int j = 0; j < KM; ++j)
+              if (gone >> j & 1) v[j] = 0.0;
+          }
+        }
+        const double stay = __dadd_rn(sb, sn);
+
+        // ---- the bound, and who reaches it ----
+        unsigned best = 0;
+#pragma unroll
+        for (int j = 0; j < KM; ++j) best = max(best, hi_word(v[j]));
+        const unsigned sk = hi_word(stay);
+        const unsigned worst = __reduce_min_sync(ALL, lane < B ? sk : ALL);
+        int ns;
+        if (worst > 0 && !__any_sync(ALL, best >= worst)) {
+          ns = B;                                 // the stays, all of them
+          if (lane < B) { key[lane] = stay; code[lane] = (short)lane; }
+        } else {
+          unsigned least;
+          if (B <= 16) {
+            const unsigned other = __shfl_sync(ALL, best, lane & 15);
+            const unsigned mine = lane < 16 ? sk : other;
+            bound[lane] = mine;
+            __syncwarp();
+            int above = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint4 o = ((const uint4*)bound)[i];
+              above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+            }
+            least = __reduce_min_sync(ALL, above < B ? mine : ALL);
+          } else {
+            bound[lane] = sk;
+            bound[32 + lane] = best;
+            __syncwarp();
+            int a0 = 0, a1 = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const uint4 o = ((const uint4*)bound)[i];
+              a0 += (o.x > sk) + (o.y > sk) + (o.z > sk) + (o.w > sk);
+              a1 += (o.x > best) + (o.y > best) + (o.z > best) + (o.w > best);
+            }
+            least = __reduce_min_sync(ALL, min(a0 < B ? sk : ALL, a1 < B ? best : ALL));
+          }
+          const unsigned below = (1u << lane) - 1;
+          bool reach = stay > 0.0 && sk >= least;
+          unsigned m = __ballot_sync(ALL, reach);
+          if (reach) { const int i = __popc(m & below); key[i] = stay; code[i] = (short)lane; }
+          ns = __popc(m);
+#pragma unroll
+          for (int j = 0; j < KM; ++j) {
+            reach = v[j] > 0.0 && hi_word(v[j]) >= least;
+            m = __ballot_sync(ALL, reach);
+            if (m) {
+              if (reach) {
+                const int i = ns + __popc(m & below);
+                key[i] = v[j];
+                code[i] = (short)(32 + lane * 32 + j);
+              }
+              ns += __popc(m);
             }
           }
         }
-        new_b[tid] = sb;
-        new_n[tid] = sn;
-        key[tid] = __dadd_rn(sb, sn);
-        b.pb[tid] = b.pn[tid] = 0.0;
-        b.hash[tid] = b.up[tid] = 0;
-        b.last[tid] = -1;
-        b.size[tid] = b.node[tid] = 0;
-      }
-      __syncthreads();
-      for (int i = tid; i < B * k; i += PFX_THREADS) {
-        const int r = i / k, j = i % k, c = tile.cls[f][j];
-        double v = 0.0;
-        if (c >= 0 && c != blank && !((taken[r] >> j) & 1))
-          v = __dmul_rn(c == a.last[r] ? a.pb[r] : __dadd_rn(a.pb[r], a.pn[r]), tile.p[f][j]);
-        key[B + i] = v;
-      }
-      __syncthreads();
-      for (int i = tid; i < nc; i += PFX_THREADS) {
-        const double v = key[i];
-        if (!(v > 0.0)) continue;
-        int rank = 0;
-        for (int m = 0; m < nc; ++m) rank += key[m] > v || (key[m] == v && m < i);
-        if (rank >= B) continue;
-        if (i < B) {
-          b.pb[rank] = new_b[i];
-          b.pn[rank] = new_n[i];
-          b.hash[rank] = a.hash[i];
-          b.up[rank] = a.up[i];
-          b.last[rank] = a.last[i];
-          b.size[rank] = a.size[i];
-          b.node[rank] = a.node[i];
+        if (lane == 0) key[ns] = 0.0;             // pairs of keys are read below
+        __syncwarp();
+
+        // ---- exact ranks; equal keys (a rank that two hold) in the order of their codes ----
+        for (int i0 = 0; i0 < ns; i0 += 32) {
+          const int i = i0 + lane;
+          const double mine = i < ns ? key[i] : 0.0;
+          int rank = 0, twins = 0;
+          for (int q = 0; q < ns; q += 2) {
+            const double2 o = *(const double2*)&key[q];
+            rank += (__double_as_longlong(o.x) > __double_as_longlong(mine)) + (__double_as_longlong(o.y) > __double_as_longlong(mine));
+            twins += (__double_as_longlong(o.x) == __double_as_longlong(mine)) + (__double_as_longlong(o.y) == __double_as_longlong(mine));
+          }
+          if (__any_sync(ALL, i < ns && twins > 1) && i < ns) {
+            const int c = code[i];
+            for (int q = 0; q < ns; ++q) rank += key[q] == mine && code[q] < c;
+          }
+          if (i < ns && rank < B) order[rank] = i;
+        }
+        __syncwarp();
+
+        // ---- the new slots ----
+        const bool live = lane < min(ns, B);
+        const int i = live ? order[lane] : 0;
+        const double value = key[i];
+        const int what = live ? code[i] : lane;
+        const bool grown = what >= 32;
+        const int r = grown ? (what - 32) >> 5 : what;
+        const int c = grown ? tile.cls[f][(what - 32) & 31] : 0;
+        if (live && !grown) moved[r] = lane;
+        const double rb = __shfl_sync(ALL, sb, r), rn = __shfl_sync(ALL, sn, r);
+        const unsigned long long rh = __shfl_sync(ALL, hash, r), ru = __shfl_sync(ALL, up, r);
+        const int rlast = __shfl_sync(ALL, last, r), rsize = __shfl_sync(ALL, size, r);
+        const int rnode = __shfl_sync(ALL, node, r), rpar = __shfl_sync(ALL, par, r);
+        __syncwarp();
+        const int from = grown ? r : rpar;
+        par = live && from >= 0 ? moved[from] : -1;
+        __syncwarp();
+        moved[lane] = -1;
+        if (grown) {
+          pb = 0.0;
+          pn = value;
+          hash = grow_hash(rh, c);
+          up = rh;
+          last = c;
+          size = rsize + 1;
+          node = 1 + frame * B + lane;
+          my_nodes[node] = make_int2(rnode, c);
         } else {
-          const int r = (i - B) / k, c = tile.cls[f][(i - B) % k];
-          const int node = 1 + frame * B + rank;
-          b.pb[rank] = 0.0;
-          b.pn[rank] = v;
-          b.hash[rank] = grow_hash(a.hash[r], c);
-          b.up[rank] = a.hash[r];
-          b.last[rank] = c;
-          b.size[rank] = a.size[r] + 1;
-          b.node[rank] = node;
-          my_nodes[node] = make_int2(a.node[r], c);
+          pb = live ? rb : 0.0;
+          pn = live ? rn : 0.0;
+          hash = live ? rh : 0;
+          up = live ? ru : 0;
+          last = live ? rlast : -1;
+          size = live ? rsize : 0;
+          node = live ? rnode : 0;
         }
-      }
-      __syncthreads();
-      if (frame % PFX_RESCALE == PFX_RESCALE - 1) {
-        const double top = __dadd_rn(b.pb[0], b.pn[0]);
-        const int e = top > 0.0 ? (int)((__double_as_longlong(top) >> 52) & 0x7ff) - 1022 : 0;
-        const double s = __longlong_as_double((long long)(1023 - e) << 52);
-        power += e;
-        __syncthreads();
-        if (tid < B) {
-          b.pb[tid] = __dmul_rn(b.pb[tid], s);
-          b.pn[tid] = __dmul_rn(b.pn[tid], s);
+        // a prefix that had left the beam and is back is the parent of slots that stayed
+        const bool orphan = live && par < 0 && size > 0 && !grown;
+        if (__any_sync(ALL, orphan)) {
+          unsigned fresh_slots = __ballot_sync(ALL, grown);
+          while (fresh_slots) {
+            const int e = __ffs(fresh_slots) - 1;
+            fresh_slots &= fresh_slots - 1;
+            const unsigned long long h = __shfl_sync(ALL, hash, e);
+            if (orphan && h == up) par = e;
+          }
         }
-        __syncthreads();
+        if (frame % PFX_RESCALE == PFX_RESCALE - 1) {
+          const double top = __shfl_sync(ALL, __dadd_rn(pb, pn), 0);
+          const int e = top > 0.0 ? (int)(hi_word(top) >> 20 & 0x7ff) - 1022 : 0;
+          const double s = __longlong_as_double((long long)(1023 - e) << 52);
+          power += e;
+          pb = __dmul_rn(pb, s);
+          pn = __dmul_rn(pn, s);
+        }
+        shift += tile.shift[f];
       }
-      shift += tile.shift[f];
-      cur ^= 1;
     }
     __syncthreads();
   }
-  for (int i = tid; i < (int)(sizeof(Slots) / 4); i += PFX_THREADS) ((int*)&st->s)[i] = ((const int*)&buf[cur])[i];
-  if (tid == 0) {
-    st->magic = PFX_MAGIC;
-    st->beams = B;
-    st->max_frames = max_frames;
-    st->frames = frames0 + Tn;
-    st->power = power;
-    st->shift = shift;
-    st->flags = flags;
+  if (warp == 0) {
+    if (lane < B) {
+      st->s.pb[lane] = pb; st->s.pn[lane] = pn;
+      st->s.hash[lane] = hash; st->s.up[lane] = up;
+      st->s.last[lane] = last; st->s.size[lane] = size; st->s.node[lane] = node;
+    }
+    if (lane == 0) {
+      st->magic = PFX_MAGIC;
+      st->beams = B;
+      st->max_frames = max_frames;
+      st->frames = frames0 + Tn;
+      st->power = power;
+      st->shift = shift;
+      st->flags = flags;
+    }
   }
 }
 
-// The hypotheses of a state: every slot's labels from its chain of nodes, last label first.
-__global__ void __launch_bounds__(PFX_THREADS) k_prefix_read(
+// The hypotheses of a state: every slot's labels from its chain of nodes, last label first.  A chain is
+// as long as the hypothesis, and a node read from L2 a step would cost 0.3 us; nodes are numbered by frame, so the
+// table is taken through shared memory in windows from the last frame to the first, and all chains of an
+// utterance walk through a window before the next one is fetched.
+constexpr int PFX_READ_THREADS = 256;
+constexpr int PFX_WINDOW = 5120;                  // nodes, 40 KB
+__global__ void __launch_bounds__(PFX_READ_THREADS) k_prefix_read(
     const char* __restrict__ states, const int2* __restrict__ nodes, int B, int max_frames, int stride,
     int* __restrict__ tokens, int* __restrict__ sizes, float* __restrict__ scores, int* __restrict__ flags) {
+  __shared__ int2 window[PFX_WINDOW];
+  __shared__ int newest, oldest;
   const int n = blockIdx.x, tid = threadIdx.x;
   const PrefixState* st = (const PrefixState*)(states + (size_t)n * PFX_STATE_BYTES);
   const int2* my_nodes = nodes + (size_t)n * nodes_per_utt(B, max_frames);
   const bool valid = st->magic == PFX_MAGIC && st->beams == B && st->max_frames == max_frames;
+  const int most = (int)nodes_per_utt(B, max_frames);
   for (int b = 0; b < B; ++b) {
     const bool live = valid && st->s.pb[b] + st->s.pn[b] > 0.0;
     const int size = live ? st->s.size[b] : 0;
-    for (int i = size + tid; i < stride; i += PFX_THREADS) tokens[((size_t)n * B + b) * stride + i] = -1;
+    for (int i = size + tid; i < stride; i += PFX_READ_THREADS) tokens[((size_t)n * B + b) * stride + i] = -1;
   }
+  if (tid == 0) newest = 0;
+  __syncthreads();
+  int at = 0, node = 0;
+  int* out = nullptr;
   if (tid < B) {
     const double total = valid ? st->s.pb[tid] + st->s.pn[tid] : 0.0;
-    const int size = total > 0.0 ? st->s.size[tid] : 0;
-    int node = total > 0.0 ? st->s.node[tid] : 0;
-    int* out = tokens + ((size_t)n * B + tid) * stride;
-    for (int i = size - 1; i >= 0 && node > 0 && node < (int)nodes_per_utt(B, max_frames); --i) {
-      const int2 v = my_nodes[node];
-      if (i < stride) out[i] = v.y;
-      if (v.x >= node) break;                     // nodes are made after their parents
-      node = v.x;
-    }
-    sizes[n * B + tid] = size;
-    scores[n * B + tid] = total > 0.0 ? (float)(log(total) + st->power * 0.693147180559945309417 + st->shift)
-                                      : -CUDART_INF_F;
+    const bool live = total > 0.0;
+    at = live ? st->s.size[tid] : 0;
+    node = live ? st->s.node[tid] : 0;
+    if (node < 0 || node >= most) node = 0;
+    out = tokens + ((size_t)n * B + tid) * stride;
+    sizes[n * B + tid] = at;
+    scores[n * B + tid] = live ? (float)(log(total) + st->power * 0.693147180559945309417 + st->shift) : -CUDART_INF_F;
+    atomicMax(&newest, node);
   }
   if (tid == 0 && flags) {
     bool any = false;
     for (int b = 0; b < B && valid; ++b) any = any || st->s.pb[b] + st->s.pn[b] > 0.0;
     flags[n] = valid ? st->flags | (any ? 0 : PCTC_UTT_INFEASIBLE) : PCTC_UTT_STATE_FULL;
+  }
+  __syncthreads();
+  for (int hi = newest + 1; hi > 1;) {            // nodes [lo, hi); node 0 is the empty prefix
+    const int lo = max(1, hi - PFX_WINDOW);
+    for (int i = tid; i < hi - lo; i += PFX_READ_THREADS) window[i] = my_nodes[lo + i];
+    if (tid == 0) oldest = 0;
+    __syncthreads();
+    if (tid < B) {
+      while (node >= lo && at > 0) {
+        const int2 v = window[node - lo];
+        if (--at < stride) out[at] = v.y;
+        node = v.x >= 0 && v.x < node ? v.x : 0;  // nodes are made after their parents
+      }
+      atomicMax(&oldest, at > 0 ? node : 0);      // the newest node that is still to be read
+    }
+    __syncthreads();
+    hi = min(lo, oldest + 1);
+    __syncthreads();
   }
 }
 
@@ -322,8 +486,9 @@ pctc_status_t pctc_prefix_advance(const pctc_prefix_t* p, const int32_t* classes
     Lengths len;
     const int m = p->N - n0 < PFX_SLICE ? p->N - n0 : PFX_SLICE;
     for (int i = 0; i < m; ++i) len.n[i] = lengths[n0 + i];
-    k_prefix_advance<<<m, PFX_THREADS, 0, (cudaStream_t)stream_v>>>(classes, logprobs, len, n0, p->T, p->k, p->beams,
-                                                                    p->blank_id, p->max_frames, fresh, (char*)state, nodes);
+    auto kern = p->k <= 8 ? k_prefix_advance<8> : k_prefix_advance<32>;
+    kern<<<m, PFX_THREADS, 0, (cudaStream_t)stream_v>>>(classes, logprobs, len, n0, p->T, p->k, p->beams, p->blank_id,
+                                                        p->max_frames, fresh, (char*)state, nodes);
     if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
   }
   return PCTC_OK;
@@ -338,7 +503,7 @@ pctc_status_t pctc_prefix_read(const pctc_prefix_t* p, const void* state, size_t
     return PCTC_ERR_INVALID_ARG;
   if (bytes < state_bytes(p)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
   const int2* nodes = (const int2*)((const char*)state + (size_t)p->N * PFX_STATE_BYTES);
-  k_prefix_read<<<p->N, PFX_THREADS, 0, (cudaStream_t)stream_v>>>((const char*)state, nodes, p->beams, p->max_frames,
+  k_prefix_read<<<p->N, PFX_READ_THREADS, 0, (cudaStream_t)stream_v>>>((const char*)state, nodes, p->beams, p->max_frames,
                                                                   token_stride, tokens, token_lengths, scores, utt_flags);
   return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
 }
