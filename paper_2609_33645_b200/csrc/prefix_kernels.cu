@@ -118,28 +118,45 @@ __device__ __forceinline__ void stage(Tile<KM>& t, int nf, int warp, int warps, 
   }
 }
 
-__device__ __forceinline__ unsigned hi_word(double x) { return (unsigned)__double2hiint(x); }
+// Order of non-negative doubles up to ties: the upper word, at least 1 for what is not zero.
+__device__ __forceinline__ unsigned coarse(double x) {
+  const unsigned h = (unsigned)__double2hiint(x);
+  return h == 0 && x > 0.0 ? 1u : h;
+}
 
-// One CTA an utterance: warp 0 searches, one lane a slot, while the others stage the next frames.  The search is
-// a chain of dependent frames, so what counts is its latency: everything of a slot lives in its lane's
-// registers, lanes talk by shuffles and a few words of shared memory, and the only barrier is one per 32 frames.
-// Candidates are ranked by counting, in two steps: the `beams`-th largest of the stays and every slot's best
-// extension bounds the result from below (compared by the upper 32 bits, which order non-negative doubles up
-// to ties), and only what reaches the bound is ranked exactly; in most frames of speech the blank or the last
-// label takes nearly all, and no extension reaches even the worst stay.
-template <int KM>
-__global__ void __launch_bounds__(PFX_THREADS) k_prefix_advance(
+template <int KM, int BM>
+struct Search {                                   // what lanes hand each other within a frame
+  // coarse keys: BM stays, then (at first) every slot's best extension, then the extensions that are ranked; 16 of padding
+  __align__(16) unsigned key[BM + (KM > 1 ? KM : 1) * BM + 16];
+  double value[KM * BM];                          // of the extensions that are ranked ...
+  int2 from[KM * BM];                             // ... and 32 + slot * 32 + class number, and the class
+  double stay[BM];
+  double slot_value[32];                          // by new slot
+  int2 slot_from[32];
+  unsigned taken[32];
+};
+
+// One CTA an utterance: warp 0 searches while the other warps stage the next frames.  The search is a chain of
+// dependent frames, so what counts is its latency: a slot lives in registers of a lane, lanes talk by shuffles and a
+// few words of shared memory, and the only barrier is one per 32 frames.  BM >= B slots; with fewer than 32 every
+// slot is held by 32 / BM lanes alike, which share its classes.
+// Candidates are ranked by counting, in two steps: the B-th largest of the stays and every slot's best extension
+// bounds the result from below, and only what reaches the bound is ranked.  Both compare upper words (coarse());
+// where two of those tie, the ranks are taken again with all bits and the order of equals.  In most frames of
+// speech the blank or the last label takes nearly all, no extension reaches even the worst stay, the stays
+// keep their order, and neither step is needed.
+template <int KM, int BM>
+__global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
     const int* __restrict__ classes, const float* __restrict__ logprobs, const __grid_constant__ Lengths len, int n0,
     int T, int k, int B, int blank, int max_frames, int fresh, char* __restrict__ states, int2* __restrict__ nodes) {
   constexpr unsigned ALL = 0xffffffffu;
+  constexpr int REP = 32 / BM, KP = KM / REP;     // lanes a slot, classes a lane
+  constexpr unsigned SLOTS = BM == 32 ? ALL : (1u << BM) - 1;
   __shared__ Tile<KM> tiles[2];
-  __shared__ __align__(16) double key[PFX_MAX_BEAMS * (KM + 1) + 2];
-  __shared__ short code[PFX_MAX_BEAMS * (KM + 1) + 2];     // stay of slot r: r; slot r grown by class j: 32 + r * 32 + j
-  __shared__ __align__(16) unsigned bound[64];
-  __shared__ unsigned taken[32];
-  __shared__ int order[32], moved[32];
+  __shared__ Search<KM, BM> sh;
   __shared__ int flags;
   const int n = n0 + blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int slot = lane % BM, part = lane / BM;
   const int Tn = len.n[blockIdx.x];
   PrefixState* st = (PrefixState*)(states + (size_t)n * PFX_STATE_BYTES);
   int2* my_nodes = nodes + (size_t)n * nodes_per_utt(B, max_frames);
@@ -159,15 +176,16 @@ __global__ void __launch_bounds__(PFX_THREADS) k_prefix_advance(
   int last = -1, size = 0, node = 0, par = -1;    // par: the slot that holds the prefix without its last label
   if (warp == 0) {
     if (fresh) {
-      if (lane == 0) { pb = 1.0; my_nodes[0] = make_int2(-1, -1); }
+      if (slot == 0) pb = 1.0;
+      if (lane == 0) my_nodes[0] = make_int2(-1, -1);
     } else {
       frames0 = st->frames;
       power = st->power;
       shift = st->shift;
-      if (lane < B) {
-        pb = st->s.pb[lane]; pn = st->s.pn[lane];
-        hash = st->s.hash[lane]; up = st->s.up[lane];
-        last = st->s.last[lane]; size = st->s.size[lane]; node = st->s.node[lane];
+      if (slot < B) {
+        pb = st->s.pb[slot]; pn = st->s.pn[slot];
+        hash = st->s.hash[slot]; up = st->s.up[slot];
+        last = st->s.last[slot]; size = st->s.size[slot]; node = st->s.node[slot];
       }
       for (int r = 0; r < B; ++r) {
         const unsigned long long h = __shfl_sync(ALL, hash, r);
@@ -175,8 +193,7 @@ __global__ void __launch_bounds__(PFX_THREADS) k_prefix_advance(
         if (live && size > 0 && h == up) par = r;
       }
     }
-    taken[lane] = 0;
-    moved[lane] = -1;
+    sh.taken[lane] = 0;
   }
   if (tid == 0) flags = fresh ? 0 : st->flags;
   __syncthreads();
@@ -196,16 +213,19 @@ __global__ void __launch_bounds__(PFX_THREADS) k_prefix_advance(
     } else {
       for (int f = 0; f < nf; ++f) {
         const int frame = frames0 + t0 + f;
-        // ---- candidates of this lane's slot ----
+        // ---- this lane's candidates: its slot's stay, and the slot grown by its share of the classes ----
         const double total = __dadd_rn(pb, pn);
-        double v[KM];
+        double v[KP];
         int jl = -1;
 #pragma unroll
-        for (int j = 0; j < KM; ++j) {
+        for (int q = 0; q < KP; ++q) {
+          const int j = part * KP + q;
           const bool same = tile.cls[f][j] == last;
           if (same) jl = j;
-          v[j] = __dmul_rn(same ? pb : total, tile.p[f][j]);
+          v[q] = __dmul_rn(same ? pb : total, tile.p[f][j]);
         }
+#pragma unroll
+        for (int o = BM; o < 32; o *= 2) jl = max(jl, __shfl_xor_sync(ALL, jl, o));
         const double pl = jl >= 0 ? tile.p[f][jl] : 0.0;
         const double sb = __dmul_rn(total, tile.blank[f]);
         double sn = __dmul_rn(pn, pl);
@@ -216,152 +236,191 @@ __global__ void __launch_bounds__(PFX_THREADS) k_prefix_advance(
           const double rb = __shfl_sync(ALL, pb, r), rt = __shfl_sync(ALL, total, r);
           if (child) {
             sn = __dadd_rn(sn, __dmul_rn(rl == last ? rb : rt, pl));
-            atomicOr(&taken[par], 1u << jl);
+            atomicOr(&sh.taken[par], 1u << jl);
           }
           __syncwarp();
-          const unsigned gone = taken[lane];
-          taken[lane] = 0;
-          if (gone) {
+          const unsigned gone = sh.taken[slot] >> (part * KP);
+          __syncwarp();
+          sh.taken[lane] = 0;
+          __syncwarp();
 #pragma unroll
-            for (int j = 0; j < KM; ++j)
-              if (gone >> j & 1) v[j] = 0.0;
-          }
+          for (int q = 0; q < KP; ++q)
+            if (gone >> q & 1) v[q] = 0.0;
         }
         const double stay = __dadd_rn(sb, sn);
+        shift += tile.shift[f];
 
-        // ---- the bound, and who reaches it ----
         unsigned best = 0;
 #pragma unroll
-        for (int j = 0; j < KM; ++j) best = max(best, hi_word(v[j]));
-        const unsigned sk = hi_word(stay);
-        const unsigned worst = __reduce_min_sync(ALL, lane < B ? sk : ALL);
-        int ns;
-        if (worst > 0 && !__any_sync(ALL, best >= worst)) {
-          ns = B;                                 // the stays, all of them
-          if (lane < B) { key[lane] = stay; code[lane] = (short)lane; }
+        for (int q = 0; q < KP; ++q) best = max(best, coarse(v[q]));
+        const unsigned sk = coarse(stay);
+        const unsigned worst = __reduce_min_sync(ALL, slot < B ? sk : ALL);
+        const bool grows = __any_sync(ALL, best >= worst && best > 0);
+        const double ahead = __shfl_up_sync(ALL, stay, 1, BM);
+        if (!grows && worst > 0 && __all_sync(ALL, slot == 0 || slot >= B || ahead >= stay)) {
+          pb = sb;                                // all stay, in their order
+          pn = sn;
         } else {
-          unsigned least;
-          if (B <= 16) {
-            const unsigned other = __shfl_sync(ALL, best, lane & 15);
-            const unsigned mine = lane < 16 ? sk : other;
-            bound[lane] = mine;
+          // ---- the bound, and the extensions that reach it ----
+          int ne = 0;
+          if (part == 0) sh.key[slot] = sk;
+          if (grows) {
+#pragma unroll
+            for (int o = BM; o < 32; o *= 2) best = max(best, __shfl_xor_sync(ALL, best, o));
+            if (part == REP - 1) sh.key[BM + slot] = best;
             __syncwarp();
-            int above = 0;
+            unsigned least;
+            if (BM < 32) {
+              const unsigned mine = lane < BM ? sk : best;
+              int above = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint4 o = ((const uint4*)bound)[i];
-              above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
-            }
-            least = __reduce_min_sync(ALL, above < B ? mine : ALL);
-          } else {
-            bound[lane] = sk;
-            bound[32 + lane] = best;
-            __syncwarp();
-            int a0 = 0, a1 = 0;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const uint4 o = ((const uint4*)bound)[i];
-              a0 += (o.x > sk) + (o.y > sk) + (o.z > sk) + (o.w > sk);
-              a1 += (o.x > best) + (o.y > best) + (o.z > best) + (o.w > best);
-            }
-            least = __reduce_min_sync(ALL, min(a0 < B ? sk : ALL, a1 < B ? best : ALL));
-          }
-          const unsigned below = (1u << lane) - 1;
-          bool reach = stay > 0.0 && sk >= least;
-          unsigned m = __ballot_sync(ALL, reach);
-          if (reach) { const int i = __popc(m & below); key[i] = stay; code[i] = (short)lane; }
-          ns = __popc(m);
-#pragma unroll
-          for (int j = 0; j < KM; ++j) {
-            reach = v[j] > 0.0 && hi_word(v[j]) >= least;
-            m = __ballot_sync(ALL, reach);
-            if (m) {
-              if (reach) {
-                const int i = ns + __popc(m & below);
-                key[i] = v[j];
-                code[i] = (short)(32 + lane * 32 + j);
+              for (int i = 0; i < BM / 2; ++i) {
+                const uint4 o = ((const uint4*)sh.key)[i];
+                above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
               }
-              ns += __popc(m);
+              least = __reduce_min_sync(ALL, above < B ? mine : ALL);
+            } else {
+              int a0 = 0, a1 = 0;
+#pragma unroll
+              for (int i = 0; i < BM / 2; ++i) {
+                const uint4 o = ((const uint4*)sh.key)[i];
+                a0 += (o.x > sk) + (o.y > sk) + (o.z > sk) + (o.w > sk);
+                a1 += (o.x > best) + (o.y > best) + (o.z > best) + (o.w > best);
+              }
+              least = __reduce_min_sync(ALL, min(a0 < B ? sk : ALL, a1 < B ? best : ALL));
+            }
+            least = max(least, 1u);
+            int mine = 0;
+#pragma unroll
+            for (int q = 0; q < KP; ++q) mine += coarse(v[q]) >= least;
+            int at = 0;                           // places before this lane's: a scan over the bits of the counts
+#pragma unroll
+            for (int bit = 1; bit <= KP; bit *= 2) {
+              const unsigned m = __ballot_sync(ALL, mine & bit);
+              at += bit * __popc(m & ((1u << lane) - 1));
+              ne += bit * __popc(m);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int q = 0; q < KP; ++q) {
+              if (coarse(v[q]) >= least) {
+                const int j = part * KP + q;
+                sh.key[BM + at] = coarse(v[q]);
+                sh.value[at] = v[q];
+                sh.from[at] = make_int2(32 + slot * 32 + j, tile.cls[f][j]);
+                ++at;
+              }
             }
           }
-        }
-        if (lane == 0) key[ns] = 0.0;             // pairs of keys are read below
-        __syncwarp();
+          const int all = BM + ne;
+          if (lane < 16) sh.key[all + lane] = 0;
+          __syncwarp();
 
-        // ---- exact ranks; equal keys (a rank that two hold) in the order of their codes ----
-        for (int i0 = 0; i0 < ns; i0 += 32) {
-          const int i = i0 + lane;
-          const double mine = i < ns ? key[i] : 0.0;
-          int rank = 0, twins = 0;
-          for (int q = 0; q < ns; q += 2) {
-            const double2 o = *(const double2*)&key[q];
-            rank += (__double_as_longlong(o.x) > __double_as_longlong(mine)) + (__double_as_longlong(o.y) > __double_as_longlong(mine));
-            twins += (__double_as_longlong(o.x) == __double_as_longlong(mine)) + (__double_as_longlong(o.y) == __double_as_longlong(mine));
+          // ---- ranks among the stays and those extensions; the first B are the new slots ----
+          int place = -1;                         // of this lane's stay (lanes below BM)
+          int count = 0, sum = 0;
+          for (int x0 = 0; x0 < all; x0 += 32) {
+            const int x = x0 + lane;
+            const unsigned mine = x < all ? sh.key[x] : 0;
+            const int e = max(x - BM, 0);
+            const bool ext = x >= BM && x < all;
+            const double val = ext ? sh.value[e] : 0.0;
+            const int2 src = ext ? sh.from[e] : make_int2(lane, 0);
+            int rank = 0;
+            for (int y = 0; y < all; y += 16) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint4 o = *(const uint4*)&sh.key[y + 4 * i];
+                rank += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+              }
+            }
+            count += __popc(__ballot_sync(ALL, mine > 0));
+            sum += __reduce_add_sync(ALL, mine > 0 ? (unsigned)rank : 0u);
+            if (mine > 0 && rank < B) {
+              sh.slot_value[rank] = val;
+              sh.slot_from[rank] = src;
+              if (x < BM) place = rank;
+            }
           }
-          if (__any_sync(ALL, i < ns && twins > 1) && i < ns) {
-            const int c = code[i];
-            for (int q = 0; q < ns; ++q) rank += key[q] == mine && code[q] < c;
+          if (sum != count * (count - 1) / 2) {   // ties of upper words: all bits, and the order of equals
+            if (part == 0) sh.stay[slot] = stay;
+            place = -1;
+            __syncwarp();
+            for (int x = lane; x < all; x += 32) {
+              const double val = x < BM ? sh.stay[x] : sh.value[x - BM];
+              const int2 src = x < BM ? make_int2(x, 0) : sh.from[x - BM];
+              if (!(val > 0.0)) continue;
+              int rank = 0;
+              for (int y = 0; y < all; ++y) {
+                const double o = y < BM ? sh.stay[y] : sh.value[y - BM];
+                rank += o > val || (o == val && (y < BM ? y : sh.from[y - BM].x) < src.x);
+              }
+              if (rank < B) {
+                sh.slot_value[rank] = val;
+                sh.slot_from[rank] = src;
+                if (x < BM) place = rank;
+              }
+            }
           }
-          if (i < ns && rank < B) order[rank] = i;
-        }
-        __syncwarp();
+          __syncwarp();
 
-        // ---- the new slots ----
-        const bool live = lane < min(ns, B);
-        const int i = live ? order[lane] : 0;
-        const double value = key[i];
-        const int what = live ? code[i] : lane;
-        const bool grown = what >= 32;
-        const int r = grown ? (what - 32) >> 5 : what;
-        const int c = grown ? tile.cls[f][(what - 32) & 31] : 0;
-        if (live && !grown) moved[r] = lane;
-        const double rb = __shfl_sync(ALL, sb, r), rn = __shfl_sync(ALL, sn, r);
-        const unsigned long long rh = __shfl_sync(ALL, hash, r), ru = __shfl_sync(ALL, up, r);
-        const int rlast = __shfl_sync(ALL, last, r), rsize = __shfl_sync(ALL, size, r);
-        const int rnode = __shfl_sync(ALL, node, r), rpar = __shfl_sync(ALL, par, r);
-        __syncwarp();
-        const int from = grown ? r : rpar;
-        par = live && from >= 0 ? moved[from] : -1;
-        __syncwarp();
-        moved[lane] = -1;
-        if (grown) {
-          pb = 0.0;
-          pn = value;
-          hash = grow_hash(rh, c);
-          up = rh;
-          last = c;
-          size = rsize + 1;
-          node = 1 + frame * B + lane;
-          my_nodes[node] = make_int2(rnode, c);
-        } else {
-          pb = live ? rb : 0.0;
-          pn = live ? rn : 0.0;
-          hash = live ? rh : 0;
-          up = live ? ru : 0;
-          last = live ? rlast : -1;
-          size = live ? rsize : 0;
-          node = live ? rnode : 0;
-        }
-        // a prefix that had left the beam and is back is the parent of slots that stayed
-        const bool orphan = live && par < 0 && size > 0 && !grown;
-        if (__any_sync(ALL, orphan)) {
-          unsigned fresh_slots = __ballot_sync(ALL, grown);
-          while (fresh_slots) {
-            const int e = __ffs(fresh_slots) - 1;
-            fresh_slots &= fresh_slots - 1;
-            const unsigned long long h = __shfl_sync(ALL, hash, e);
-            if (orphan && h == up) par = e;
+          // ---- the new slots ----
+          const bool live = slot < min(count, B);
+          const double value = sh.slot_value[slot];
+          const int2 src = live ? sh.slot_from[slot] : make_int2(lane, 0);
+          const bool grown = src.x >= 32;
+          const int r = grown ? (src.x - 32) >> 5 : src.x;
+          const int moved = __shfl_sync(ALL, place, max(par, 0));        // where this slot's parent goes
+          const int stay_par = par >= 0 ? moved : -1;
+          const int grown_par = __shfl_sync(ALL, place, r);
+          par = __shfl_sync(ALL, stay_par, r);
+          const double rb = __shfl_sync(ALL, sb, r), rn = __shfl_sync(ALL, sn, r);
+          const unsigned long long rh = __shfl_sync(ALL, hash, r), ru = __shfl_sync(ALL, up, r);
+          last = __shfl_sync(ALL, last, r);
+          size = __shfl_sync(ALL, size, r);
+          node = __shfl_sync(ALL, node, r);
+          pb = rb;
+          pn = rn;
+          hash = rh;
+          up = ru;
+          if (grown) {
+            const int parent = node;
+            pb = 0.0;
+            pn = value;
+            hash = grow_hash(rh, src.y);
+            up = rh;
+            last = src.y;
+            size += 1;
+            node = 1 + frame * B + slot;
+            par = grown_par;
+            if (part == 0) my_nodes[node] = make_int2(parent, src.y);
+          }
+          if (!live) {
+            pb = pn = 0.0;
+            hash = up = 0;
+            last = par = -1;
+            size = node = 0;
+          }
+          // a prefix that had left the beam and is back is the parent of slots that stayed
+          const bool orphan = live && par < 0 && size > 0 && !grown;
+          if (__any_sync(ALL, orphan)) {
+            unsigned fresh_slots = __ballot_sync(ALL, grown) & SLOTS;
+            while (fresh_slots) {
+              const int e = __ffs(fresh_slots) - 1;
+              fresh_slots &= fresh_slots - 1;
+              const unsigned long long h = __shfl_sync(ALL, hash, e);
+              if (orphan && h == up) par = e;
+            }
           }
         }
         if (frame % PFX_RESCALE == PFX_RESCALE - 1) {
           const double top = __shfl_sync(ALL, __dadd_rn(pb, pn), 0);
-          const int e = top > 0.0 ? (int)(hi_word(top) >> 20 & 0x7ff) - 1022 : 0;
+          const int e = top > 0.0 ? (int)((unsigned)__double2hiint(top) >> 20 & 0x7ff) - 1022 : 0;
           const double s = __longlong_as_double((long long)(1023 - e) << 52);
           power += e;
           pb = __dmul_rn(pb, s);
           pn = __dmul_rn(pn, s);
         }
-        shift += tile.shift[f];
       }
     }
     __syncthreads();
@@ -486,7 +545,8 @@ pctc_status_t pctc_prefix_advance(const pctc_prefix_t* p, const int32_t* classes
     Lengths len;
     const int m = p->N - n0 < PFX_SLICE ? p->N - n0 : PFX_SLICE;
     for (int i = 0; i < m; ++i) len.n[i] = lengths[n0 + i];
-    auto kern = p->k <= 8 ? k_prefix_advance<8> : k_prefix_advance<32>;
+    auto kern = p->k <= 8 ? (p->beams <= 8 ? k_prefix_advance<8, 8> : p->beams <= 16 ? k_prefix_advance<8, 16> : k_prefix_advance<8, 32>)
+                          : (p->beams <= 8 ? k_prefix_advance<32, 8> : p->beams <= 16 ? k_prefix_advance<32, 16> : k_prefix_advance<32, 32>);
     kern<<<m, PFX_THREADS, 0, (cudaStream_t)stream_v>>>(classes, logprobs, len, n0, p->T, p->k, p->beams, p->blank_id,
                                                         p->max_frames, fresh, (char*)state, nodes);
     if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
