@@ -475,51 +475,26 @@ def topk_decode(hidden, W, bias, input_lengths, k, *, chunk=0, gemm_path=GEMM_AU
     return dict(classes=classes, logprobs=logprobs, workspace=workspace)
 
 
-def _run_on(dev, call, what, *args):
-    """`call(*args, stream)` on the current stream of `dev`, which is made the current device for the call."""
-    import torch
-
-    stream = ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
-    if torch.cuda.current_device() == dev.index:
-        st = call(*args, stream)
-    else:
-        with torch.cuda.device(dev):
-            st = call(*args, stream)
-    if st != 0:
-        raise PctcError(st, what)
+_marshal = None
 
 
-def _grad_list(grads, what):
-    """(device, pointers, element counts, dtype codes) of a list of contiguous bf16 / fp32 CUDA tensors."""
-    import torch
+def _native():
+    """The compiled argument marshalling (csrc/marshal.cpp), bound to the loaded library."""
+    global _marshal
+    if _marshal is None:
+        import torch  # noqa: F401  (its libraries come first)
 
-    if not grads:
-        raise ValueError(f"{what} must hold at least one tensor")
-    codes = {torch.bfloat16: PCTC_BF16, torch.float32: PCTC_FP32}
-    dev = grads[0].device
-    if dev.type != "cuda" or any(g.device != dev for g in grads):
-        raise ValueError(f"{what} must be CUDA tensors of one device")
-    try:
-        kinds = [codes[g.dtype] for g in grads]
-    except KeyError:
-        raise ValueError(f"{what} must be bf16 or fp32") from None
-    if not all([g.is_contiguous() for g in grads]):
-        raise ValueError(f"{what} must be contiguous")
-    n = len(grads)
-    return (dev, (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]), (ctypes.c_int64 * n)(*[g.numel() for g in grads]),
-            (ctypes.c_int32 * n)(*kinds))
-
-
-def _grad_outs(grads, out, dev):
-    """(pointers, dtype codes) of the tensors that the scaled gradients go to, or (None, None): in place."""
-    if out is None:
-        return None, None
-    if len(out) != len(grads) or any([o.shape != g.shape for o, g in zip(out, grads)]):
-        raise ValueError("out must hold one tensor of the same shape for every gradient")
-    odev, ptrs, _, kinds = _grad_list(out, "out")
-    if odev != dev:
-        raise ValueError("out must be on the gradients' device")
-    return ptrs, kinds
+        lib = load()
+        try:
+            from . import _marshal as module
+        except ImportError as e:
+            raise RuntimeError("_marshal.so is missing: run paper_2609_33645_b200.build.build() first; "
+                               "there is no fallback implementation") from e
+        names = ("pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
+                 "pctc_beam_select", "pctc_beam_reorder", "pctc_prefix_advance", "pctc_prefix_read")
+        module.bind([ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in names], PctcError)
+        _marshal = module
+    return _marshal
 
 
 def clip_workspace_bytes(n: int) -> int:
@@ -531,15 +506,6 @@ def clip_workspace_bytes(n: int) -> int:
     return int(need.value)
 
 
-def _clip_workspace(n, dev, workspace):
-    import torch
-
-    need = clip_workspace_bytes(n)
-    if workspace is None or workspace.numel() < need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    return workspace
-
-
 def clip_grad_norm(grads, max_norm, *, out=None, eps=1e-6, workspace=None):
     """Clip gradients by their global norm: every tensor times min(1, max_norm / (norm + eps)).
 
@@ -548,45 +514,25 @@ def clip_grad_norm(grads, max_norm, *, out=None, eps=1e-6, workspace=None):
     norm [1] fp32 on the device (nothing waits for it), grads (the scaled tensors) and the reusable
     workspace.  If the norm is not finite nothing is scaled.  The same tensor may not be given twice.
     """
-    import torch
-
     grads = list(grads)
-    dev, ptrs, numels, kinds = _grad_list(grads, "grads")
-    outs, out_kinds = _grad_outs(grads, out, dev)
-    workspace = _clip_workspace(len(grads), dev, workspace)
-    norm = torch.empty(1, dtype=torch.float32, device=dev)
-    _run_on(dev, load().pctc_clip_grad_norm, "pctc_clip_grad_norm", len(grads), ptrs, outs, numels, kinds, out_kinds,
-            float(max_norm), float(eps), _dptr(norm), _dptr(workspace), ctypes.c_size_t(workspace.numel()))
-    return dict(norm=norm, grads=grads if out is None else list(out), workspace=workspace)
+    out = None if out is None else list(out)
+    norm, workspace = _native().clip_grad_norm(grads, out, max_norm, eps, workspace)
+    return dict(norm=norm, grads=grads if out is None else out, workspace=workspace)
 
 
 def grad_sqsum(grads, *, workspace=None):
     """Sum of the squares of all values of `grads` (as in clip_grad_norm): sqsum [1] fp64 on the device, and
     the workspace.  Ranks that hold different shards add these up before grad_scale."""
-    import torch
-
-    grads = list(grads)
-    dev, ptrs, numels, kinds = _grad_list(grads, "grads")
-    workspace = _clip_workspace(len(grads), dev, workspace)
-    sqsum = torch.empty(1, dtype=torch.float64, device=dev)
-    _run_on(dev, load().pctc_grad_sqsum, "pctc_grad_sqsum", len(grads), ptrs, numels, kinds, _dptr(sqsum),
-            _dptr(workspace), ctypes.c_size_t(workspace.numel()))
+    sqsum, workspace = _native().grad_sqsum(list(grads), workspace)
     return dict(sqsum=sqsum, workspace=workspace)
 
 
 def grad_scale(grads, sqsum, max_norm, *, out=None, eps=1e-6):
     """The second half of clip_grad_norm, from a sum of squares [1] fp64 on the device."""
-    import torch
-
     grads = list(grads)
-    dev, ptrs, numels, kinds = _grad_list(grads, "grads")
-    outs, out_kinds = _grad_outs(grads, out, dev)
-    if sqsum.dtype != torch.float64 or sqsum.numel() != 1 or sqsum.device != dev:
-        raise ValueError("sqsum must be one fp64 value on the gradients' device")
-    norm = torch.empty(1, dtype=torch.float32, device=dev)
-    _run_on(dev, load().pctc_grad_scale, "pctc_grad_scale", len(grads), ptrs, outs, numels, kinds, out_kinds,
-            _dptr(sqsum), float(max_norm), float(eps), _dptr(norm))
-    return dict(norm=norm, grads=grads if out is None else list(out))
+    out = None if out is None else list(out)
+    norm = _native().grad_scale(grads, out, sqsum, max_norm, eps)
+    return dict(norm=norm, grads=grads if out is None else out)
 
 
 class PrefixBeam:
@@ -609,7 +555,7 @@ class PrefixBeam:
         st = load().pctc_prefix_state_bytes(ctypes.byref(self._problem(1, 1)), ctypes.byref(need))
         if st != 0:
             raise PctcError(st, "pctc_prefix_state_bytes")
-        self.frames = np.zeros(self.N, dtype=np.int64)
+        self.frames = [0] * self.N
         self.started = False
         self.state = torch.empty(int(need.value), dtype=torch.uint8, device=self.device)
 
@@ -617,46 +563,27 @@ class PrefixBeam:
         return PrefixProblem(self.N, int(T), int(k), self.beams, self.blank_id, self.max_frames)
 
     def advance(self, classes, logprobs, lengths=None):
-        import torch
-
-        if classes.dtype != torch.int32 or logprobs.dtype != torch.float32:
-            raise ValueError("classes must be int32 and logprobs fp32")
-        if classes.dim() != 3 or classes.shape[0] != self.N or logprobs.shape != classes.shape:
-            raise ValueError("classes and logprobs must be [N, frames, k]")
-        if classes.device != self.device or logprobs.device != self.device:
-            raise ValueError("classes and logprobs must be on the state's device")
-        if not (classes.is_contiguous() and logprobs.is_contiguous()):
-            raise ValueError("classes and logprobs must be contiguous")
-        T, k = classes.shape[1:]
-        ln = np.full(self.N, T, dtype=np.int32) if lengths is None else _i32(lengths)
-        if ln.shape != (self.N,):
+        native = _native()
+        native.prefix_inputs(classes, logprobs, self.N, -1 if self.device.index is None else self.device.index)
+        lengths = [classes.shape[1]] * self.N if lengths is None else [int(n) for n in lengths]
+        if len(lengths) != self.N:
             raise ValueError("one length per utterance is required")
-        if ((self.frames + ln) > self.max_frames).any():
+        frames = [f + n for f, n in zip(self.frames, lengths)]
+        if max(frames) > self.max_frames:
             raise ValueError("more frames than the state has room for")
-        _run_on(self.device, load().pctc_prefix_advance, "pctc_prefix_advance", ctypes.byref(self._problem(T, k)),
-                _dptr(classes), _dptr(logprobs), _ptr_i32(ln), 0 if self.started else 1, _dptr(self.state),
-                ctypes.c_size_t(self.state.numel()))
+        native.prefix_advance(self.state, classes, logprobs, lengths, self.N, self.beams, self.blank_id, self.max_frames,
+                              0 if self.started else 1)
         self.started = True
-        self.frames += ln
+        self.frames = frames
 
     def read(self, max_tokens=None):
         """Device tensors, best hypothesis first: tokens [N,beams,max_tokens] int32 (-1 behind the last; max_tokens
         defaults to the frames taken so far), token_lengths [N,beams], scores [N,beams] fp32 (log-probabilities,
         -inf where there are fewer hypotheses than beams), flags [N]."""
-        import torch
-
         if not self.started:
             raise ValueError("no frames yet")
-        width = max(1, int(self.frames.max()) if max_tokens is None else int(max_tokens))
-        o = dict(dtype=torch.int32, device=self.device)
-        res = dict(tokens=torch.empty((self.N, self.beams, width), **o),
-                   token_lengths=torch.empty((self.N, self.beams), **o),
-                   scores=torch.empty((self.N, self.beams), dtype=torch.float32, device=self.device),
-                   flags=torch.empty((self.N,), **o))
-        _run_on(self.device, load().pctc_prefix_read, "pctc_prefix_read", ctypes.byref(self._problem(1, 1)),
-                _dptr(self.state), ctypes.c_size_t(self.state.numel()), _dptr(res["tokens"]), width,
-                _dptr(res["token_lengths"]), _dptr(res["scores"]), _dptr(res["flags"]))
-        return res
+        width = max(1, max(self.frames)) if max_tokens is None else int(max_tokens)
+        return _native().prefix_read(self.state, self.N, self.beams, self.blank_id, self.max_frames, width)
 
 
 def prefix_beam_decode(classes, logprobs, input_lengths, blank_id, beams):
@@ -689,63 +616,7 @@ def beam_select(logits, scores, beams, *, finished=None, eos_id=None):
     fewer candidates than beams), finished [N,beams] bool and flags [N] int32 (UTT_NONFINITE).  Best
     first; among equals the lowest beam, then the lowest token.
     """
-    import torch
-
-    if logits.dim() != 3 or logits.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError("logits must be [N, B, V], bf16 or fp32")
-    N, B, V = logits.shape
-    if not logits.is_cuda or (V > 1 and logits.stride(2) != 1):
-        raise ValueError("logits must be a CUDA tensor with contiguous rows")
-    dev = logits.device
-    if scores.dtype != torch.float32 or scores.shape != (N, B) or not scores.is_contiguous() or scores.device != dev:
-        raise ValueError("scores must be contiguous fp32 [N, B] on the device of the logits")
-    if finished is not None:
-        if finished.dtype != torch.bool or finished.shape != (N, B) or not finished.is_contiguous() or finished.device != dev:
-            raise ValueError("finished must be contiguous bool [N, B] on the device of the logits")
-        if eos_id is None:
-            raise ValueError("finished needs an eos_id")
-    if eos_id is not None and not 0 <= int(eos_id) < V:
-        raise ValueError("eos_id must be a token")
-    K = int(beams)
-    if K < 1:
-        raise ValueError("beams must be at least 1")
-    # a dimension of size 1 has no stride that counts
-    stride_b = max(logits.stride(1), V) if B > 1 else V
-    if B > 1 and logits.stride(1) < V:
-        raise ValueError("rows of logits overlap")
-    prob = BeamProblem(N, B, K, V, logits.stride(0) if N > 1 else 0, stride_b,
-                       PCTC_BF16 if logits.dtype == torch.bfloat16 else PCTC_FP32, -1 if eos_id is None else int(eos_id))
-    o = dict(dtype=torch.int32, device=dev)
-    res = dict(scores=torch.empty((N, K), dtype=torch.float32, device=dev), parents=torch.empty((N, K), **o),
-               tokens=torch.empty((N, K), **o), finished=torch.empty((N, K), dtype=torch.bool, device=dev),
-               flags=torch.empty((N,), **o))
-    _run_on(dev, load().pctc_beam_select, "pctc_beam_select", ctypes.byref(prob), _dptr(logits), _dptr(scores),
-            _dptr(finished), _dptr(res["scores"]), _dptr(res["parents"]), _dptr(res["tokens"]), _dptr(res["finished"]),
-            _dptr(res["flags"]))
-    return res
-
-
-def _state_layout(x, axis, what):
-    """(utterance stride, beam stride, segments, segment stride, units, unit size) of a state [N, B, ...], in bytes."""
-    shape, strides, size = x.shape, x.stride(), x.element_size()
-    inner = 1
-    for d in range(x.dim() - 1, 1, -1):                     # contiguous behind the beam dimension
-        if shape[d] != 1 and strides[d] != inner:
-            raise ValueError(f"{what} must be contiguous behind the beam dimension")
-        inner *= shape[d]
-    if axis is None:
-        layout = (1, 0, 1, inner * size)
-    else:
-        if not 2 <= axis < x.dim():
-            raise ValueError("a time axis lies behind the beam dimension")
-        unit = size
-        for d in shape[axis + 1:]:
-            unit *= d
-        before = 1
-        for d in shape[2:axis]:
-            before *= d
-        layout = (before, shape[axis] * unit, shape[axis], unit)
-    return (strides[0] * size, strides[1] * size) + layout
+    return _native().beam_select(logits, scores, beams, finished, eos_id)
 
 
 def beam_reorder(states, parents, *, lengths=None, time_axes=None, out=None):
@@ -757,40 +628,7 @@ def beam_reorder(states, parents, *, lengths=None, time_axes=None, out=None):
     the first lengths[n] entries (lengths [N] int32 on the device) are moved, or None for whole rows; what lies
     behind is left as it is.  Returns the list of written tensors.
     """
-    import torch
-
     states = list(states)
-    if not states:
-        raise ValueError("states must hold at least one tensor")
-    dev = states[0].device
-    if dev.type != "cuda":
-        raise ValueError("states must be CUDA tensors")
-    if parents.dtype != torch.int32 or parents.dim() != 2 or not parents.is_contiguous() or parents.device != dev:
-        raise ValueError("parents must be contiguous int32 [N, K] on the states' device")
-    N, K = parents.shape
-    outs = states if out is None else list(out)
-    axes = [None] * len(states) if time_axes is None else list(time_axes)
-    if len(outs) != len(states) or len(axes) != len(states):
-        raise ValueError("out and time_axes must have one entry for every state")
-    if lengths is None:
-        if any(a is not None for a in axes):
-            raise ValueError("a time axis needs lengths")
-    elif lengths.dtype != torch.int32 or lengths.shape != (N,) or not lengths.is_contiguous() or lengths.device != dev:
-        raise ValueError("lengths must be contiguous int32 [N] on the states' device")
-    B = states[0].shape[1] if states[0].dim() > 1 else 0
-    table = (BeamState * len(states))()
-    used = 0
-    for x, o, axis in zip(states, outs, axes):
-        if x.dim() < 2 or x.shape[0] != N or x.shape[1] != B or x.device != dev:
-            raise ValueError("states must be [N, B, ...] on one device")
-        if o.shape != x.shape[:1] + (K,) + x.shape[2:] or o.dtype != x.dtype or o.device != dev:
-            raise ValueError("out must be [N, K, ...] tensors of the states' types" if out is not None else
-                             "in place, parents must have as many columns as the states have beams")
-        if x.numel() == 0:
-            continue
-        sn, sb, *row = _state_layout(x, axis, "states")
-        on, ob = (sn, sb) if o is x else _state_layout(o, axis, "out")[:2]
-        table[used] = BeamState(x.data_ptr(), o.data_ptr(), sn, sb, on, ob, *row, 0 if axis is None else 1, 0)
-        used += 1
-    _run_on(dev, load().pctc_beam_reorder, "pctc_beam_reorder", used, table, N, B, K, _dptr(parents), _dptr(lengths))
-    return outs
+    out = None if out is None else list(out)
+    _native().beam_reorder(states, parents, lengths, None if time_axes is None else list(time_axes), out)
+    return states if out is None else out

@@ -4,6 +4,8 @@
 ``libprunedctc.so`` next to this file and returns its path.  Objects are cached
 under ``build/`` and rebuilt only when a source or header is newer.
 ``build_variant(tag)`` builds a test variant of the same sources (see VARIANTS).
+``build()`` also compiles ``csrc/marshal.cpp``, the argument marshalling that the binding
+imports as ``_marshal`` (``_marshal.so``, built against the installed torch).
 """
 
 from __future__ import annotations
@@ -19,6 +21,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(ROOT, "build", "obj")
 LIB_PATH = os.path.join(HERE, "libprunedctc.so")
+MARSHAL_PATH = os.path.join(HERE, "_marshal.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -74,6 +77,36 @@ VARIANTS = {
 TEST_VARIANTS = ("shortwait", "bounds")           # the ones the test-suite loads
 
 
+def build_marshal() -> str:
+    """csrc/marshal.cpp -> _marshal.so next to this file, for the running interpreter and its torch."""
+    import sysconfig
+
+    import torch
+
+    src = os.path.join(CSRC, "marshal.cpp")
+    stamp = os.path.join(ROOT, "build", "marshal.stamp")
+    key = f"{torch.__version__} {sysconfig.get_config_var('SOABI')}"
+    inputs = [src, os.path.join(ROOT, "include", "prunedctc.h"), os.path.abspath(__file__)]
+    if os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= _newest(inputs):
+        # a tree that was copied without its build directory holds the file that fits it
+        if not os.path.exists(stamp) or open(stamp).read() == key:
+            return MARSHAL_PATH
+    base = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc()))
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(base, "include"),
+           "-I" + os.path.join(base, "include", "torch", "csrc", "api", "include"), "-I" + os.path.join(cuda, "include"),
+           src, "-o", MARSHAL_PATH, "-L" + os.path.join(base, "lib"),
+           "-ltorch", "-ltorch_cpu", "-ltorch_python", "-lc10", "-lc10_cuda"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
+    os.makedirs(os.path.dirname(stamp), exist_ok=True)
+    with open(stamp, "w") as f:
+        f.write(key)
+    return MARSHAL_PATH
+
+
 def variant_path(tag: str) -> str:
     return os.path.join(HERE, f"libprunedctc_{tag}.so")
 
@@ -108,6 +141,8 @@ def build(verbose: bool = False, extra_flags=(), tag: str = "") -> str:
             raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
         return r.stderr
 
+    if not tag:
+        build_marshal()
     if jobs:
         with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
             for out in ex.map(run, jobs):

@@ -57,7 +57,7 @@ def test_bad_pointers_are_refused_before_any_launch(lib):
     assert f(None, *good) == 1
 
 
-def test_binding_refuses_what_it_cannot_hand_on():
+def test_binding_refuses_what_it_cannot_hand_on(lib):
     x, s = torch.zeros(2, 4, 10), torch.zeros(2, 4)
     with pytest.raises(ValueError, match="CUDA"):
         binding.beam_select(x, s, 4)
@@ -111,7 +111,7 @@ def test_nothing_to_move_is_no_error(lib):
     assert _reorder(lib, [_state(units=0)]) == 0
 
 
-def test_reorder_binding_refuses_what_it_cannot_hand_on():
+def test_reorder_binding_refuses_what_it_cannot_hand_on(lib):
     p = torch.zeros(2, 4, dtype=torch.int32)
     with pytest.raises(ValueError, match="at least one"):
         binding.beam_reorder([], p)

@@ -60,7 +60,7 @@ def test_workspace_grows_by_launches_of_1024_tensors(lib):
     assert a == b and c == 2 * a
 
 
-def test_binding_refuses_what_it_cannot_hand_on():
+def test_binding_refuses_what_it_cannot_hand_on(lib):
     cpu = torch.zeros(4)
     with pytest.raises(ValueError, match="at least one"):
         binding.clip_grad_norm([], 1.0)
