@@ -10,18 +10,29 @@
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 
+#include <cooperative_groups.h>
+
 #include <cmath>
 #include <new>
+
+namespace cg = cooperative_groups;
 
 namespace pctc {
 namespace {
 
-// Work is cut into chunks of 8,192 values of one tensor: 256 threads with four (bf16) or eight (fp32)
-// 16-byte loads in flight each, eight such CTAs an SM.
+// Work is cut into chunks of 16 KB of one tensor: 256 threads with four 16-byte loads each, in a persistent grid of
+// CLIP_CTAS_PER_SM such CTAs an SM.
 constexpr int CLIP_THREADS = 256;
-constexpr int CLIP_CHUNK = 8192;
-constexpr int CLIP_CTAS_PER_SM = 8;
-constexpr int CLIP_MAX_GRID = 2048;              // most partial sums of one launch
+constexpr int CLIP_VECS = 4;
+constexpr int CLIP_CHUNK_BYTES = CLIP_THREADS * CLIP_VECS * 16;
+constexpr int CLIP_CTAS_PER_SM = 6;              // first pass: 26 us for 384 tensors of 128 MB (4: 30), 49 for 312 MB (4: 53)
+constexpr int CLIP_SCALE_CTAS_PER_SM = 4;        // second pass: 105 us for 312 MB in and out (6: 119)
+constexpr int CLIP_KEEP_CHUNKS = 4096;           // the last 64 MB of the first pass stay in L2, the rest goes past it
+constexpr int CLIP_EACH_CHUNKS = 2048;           // from so many chunks on (32 MB: 21.4 against 22.0 us; 312 MB: 150 against
+                                                 // 165) the second pass takes a CTA a chunk
+constexpr int CLIP_CLUSTER = 8;
+constexpr int CLIP_CLUSTER_CHUNKS = 32;          // up to so many chunks one cluster does all
+constexpr int CLIP_MAX_GRID = 1024;              // most partial sums of one launch
 
 enum : unsigned char { IN_F32 = 1, OUT_F32 = 2, OUT_VEC = 4, IN_PLACE = 8 };
 
@@ -34,25 +45,22 @@ struct ClipTable {
   int chunk0[LIM + 1];                           // chunks before tensor i
   unsigned char kind[LIM];
   int n;
+  int in_place;                                  // all of them
 };
-constexpr int CLIP_SMALL = 48, CLIP_LARGE = 1024;
+constexpr int CLIP_LARGE = 1024;                 // tensors of one launch; lists of up to 48, 192 and 512 take smaller tables
 static_assert(sizeof(ClipTable<CLIP_LARGE>) <= 32000, "kernel parameters");
 
-// The piece of a tensor that a chunk covers: values [lo, hi), of which [start, start + nvec * VE) can be
-// read 16 bytes at a time; chunk 0 also takes the `head` values in front of the first 16-byte boundary.
+// The piece of a tensor that a chunk covers: values [start, start + count), the first `nvec` groups of 16 bytes
+// read a group at a time; chunk 0 also takes the `head` values in front of the first 16-byte boundary.
 struct Piece {
-  long long start, hi;
-  int head;
+  const void* p;
+  long long start;
+  int count, nvec, head, kind, tensor;
 };
-__device__ __forceinline__ Piece piece_of(const void* p, long long numel, int es, int c) {
-  Piece r;
+__host__ __device__ __forceinline__ int head_of(const void* p, long long numel, int es) {
   const int mis = (int)((size_t)p & 15);
-  const long long head = mis ? (16 - mis) / es : 0;
-  r.head = (int)(head < numel ? head : numel);
-  r.start = r.head + (long long)c * CLIP_CHUNK;
-  r.hi = r.start + CLIP_CHUNK < numel ? r.start + CLIP_CHUNK : numel;
-  if (c) r.head = 0;
-  return r;
+  const int head = mis ? (16 - mis) / es : 0;
+  return head < numel ? head : (int)numel;
 }
 
 template <int LIM>
@@ -106,26 +114,47 @@ __device__ __forceinline__ double square_sum_vec(const uint4& v, bool f32) {
   return square_sum(x);
 }
 
-template <typename T>
-__device__ __forceinline__ double chunk_squares(const void* p, long long numel, int c) {
-  constexpr int VE = 16 / (int)sizeof(T), NV = CLIP_CHUNK / (VE * CLIP_THREADS);
-  const Piece r = piece_of(p, numel, (int)sizeof(T), c);
-  const int tid = threadIdx.x;
-  const uint4* body = (const uint4*)((const T*)p + r.start);
-  const int left = (int)(r.hi - r.start);        // may be <= 0 when the head is all there is
-  const int nvec = left > 0 ? left / VE : 0;
-  uint4 v[NV];
+template <int LIM>
+__device__ __forceinline__ Piece piece_of(const ClipTable<LIM>& tab, int c) {
+  Piece r;
+  r.tensor = tensor_of(tab, c);
+  r.p = tab.in[r.tensor];
+  r.kind = tab.kind[r.tensor];
+  const long long numel = tab.numel[r.tensor];
+  const int local = c - tab.chunk0[r.tensor], shift = r.kind & IN_F32 ? 2 : 1;
+  const int head = head_of(r.p, numel, 1 << shift);
+  r.start = head + ((long long)local << (14 - shift));
+  const long long left = numel - r.start;
+  r.count = (int)(left < (CLIP_CHUNK_BYTES >> shift) ? left : CLIP_CHUNK_BYTES >> shift);
+  r.nvec = r.count >> (4 - shift);
+  r.head = local ? 0 : head;
+  return r;
+}
+static_assert(CLIP_CHUNK_BYTES == 1 << 14, "chunks are 16 KB");
+
+__device__ __forceinline__ const uint4* vectors(const Piece& r) {
+  return (const uint4*)((const char*)r.p + (r.start << (r.kind & IN_F32 ? 2 : 1)));
+}
+// keep: leave the lines in L2 for the second pass.
+__device__ __forceinline__ void load_piece(uint4 (&v)[CLIP_VECS], const Piece& r, bool keep) {
+  const uint4* p = vectors(r);
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int i = tid + j * CLIP_THREADS;
-    v[j] = i < nvec ? body[i] : make_uint4(0, 0, 0, 0);
+  for (int j = 0; j < CLIP_VECS; ++j) {
+    const int i = threadIdx.x + j * CLIP_THREADS;
+    v[j] = i < r.nvec ? (keep ? p[i] : __ldcs(p + i)) : make_uint4(0, 0, 0, 0);
   }
+}
+__device__ __forceinline__ float one_value(const Piece& r, long long i) {
+  return r.kind & IN_F32 ? load1<float>(r.p, i) : load1<__nv_bfloat16>(r.p, i);
+}
+__device__ __forceinline__ double piece_squares(const uint4 (&v)[CLIP_VECS], const Piece& r) {
+  const bool f32 = r.kind & IN_F32;
   double acc = 0.0;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) acc += square_sum_vec(v[j], sizeof(T) == 4);
-  const int tail = left > 0 ? left - nvec * VE : 0;
-  if (tid < r.head) { const float x[1] = {load1<T>(p, tid)}; acc += square_sum(x); }
-  if (tid < tail) { const float x[1] = {load1<T>(p, r.start + nvec * VE + tid)}; acc += square_sum(x); }
+  for (int j = 0; j < CLIP_VECS; ++j) acc += square_sum_vec(v[j], f32);
+  const int body = r.nvec * (f32 ? 4 : 8);
+  if ((int)threadIdx.x < r.head) { const float x[1] = {one_value(r, threadIdx.x)}; acc += square_sum(x); }
+  if ((int)threadIdx.x < r.count - body) { const float x[1] = {one_value(r, r.start + body + threadIdx.x)}; acc += square_sum(x); }
   return acc;
 }
 
@@ -142,16 +171,22 @@ __device__ __forceinline__ double block_sum(double v) {
 }
 
 template <int LIM>
-__global__ void __launch_bounds__(CLIP_THREADS) k_square_sums(const __grid_constant__ ClipTable<LIM> tab,
-                                                              double* __restrict__ partial) {
+__device__ __forceinline__ double square_sums(const ClipTable<LIM>& tab, int first, int step) {
   double acc = 0.0;
   const int total = tab.chunk0[tab.n];
-  for (int c = blockIdx.x; c < total; c += gridDim.x) {
-    const int i = tensor_of(tab, c);
-    acc += (tab.kind[i] & IN_F32) ? chunk_squares<float>(tab.in[i], tab.numel[i], c - tab.chunk0[i])
-                                  : chunk_squares<__nv_bfloat16>(tab.in[i], tab.numel[i], c - tab.chunk0[i]);
+  for (int c = first; c < total; c += step) {
+    const Piece r = piece_of(tab, c);
+    uint4 v[CLIP_VECS];
+    load_piece(v, r, c >= total - CLIP_KEEP_CHUNKS);
+    acc += piece_squares(v, r);
   }
-  const double s = block_sum(acc);
+  return acc;
+}
+
+template <int LIM>
+__global__ void __launch_bounds__(CLIP_THREADS, CLIP_CTAS_PER_SM) k_square_sums(const __grid_constant__ ClipTable<LIM> tab,
+                                                                                double* __restrict__ partial) {
+  const double s = block_sum(square_sums(tab, blockIdx.x, gridDim.x));
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
@@ -163,7 +198,6 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_sum_partials(const double* __r
   if (threadIdx.x == 0) *sqsum = s;
 }
 
-template <typename T>
 __device__ __forceinline__ void store1(void* p, long long i, float x, bool f32) {
   if (f32) ((float*)p)[i] = x; else ((__nv_bfloat16*)p)[i] = __float2bfloat16_rn(x);
 }
@@ -177,60 +211,71 @@ __device__ __forceinline__ float scaled(float x, float f, double fd) {
   return f >= 1.1754944e-38f ? x * f : (float)((double)x * fd);
 }
 
-template <typename T>
-__device__ __forceinline__ void chunk_scale(const void* p, void* o, long long numel, int c, int kind, float f,
-                                            double fd) {
-  constexpr int VE = 16 / (int)sizeof(T), NV = CLIP_CHUNK / (VE * CLIP_THREADS);
-  const Piece r = piece_of(p, numel, (int)sizeof(T), c);
-  const int tid = threadIdx.x;
-  const bool of32 = kind & OUT_F32, vec = kind & OUT_VEC;
-  const uint4* body = (const uint4*)((const T*)p + r.start);
-  const int left = (int)(r.hi - r.start);
-  const int nvec = left > 0 ? left / VE : 0;
-  uint4 v[NV];
+template <bool F32>
+__device__ __forceinline__ void scale_piece(const uint4 (&v)[CLIP_VECS], const Piece& r, void* o, float f, double fd) {
+  constexpr int VE = F32 ? 4 : 8;
+  const bool of32 = r.kind & OUT_F32, vec = r.kind & OUT_VEC;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int i = tid + j * CLIP_THREADS;
-    if (i < nvec) v[j] = body[i];
-  }
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int i = tid + j * CLIP_THREADS;
-    if (i >= nvec) continue;
+  for (int j = 0; j < CLIP_VECS; ++j) {
+    const int i = threadIdx.x + j * CLIP_THREADS;
+    if (i >= r.nvec) continue;
+    const unsigned w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
     float x[VE];
-    if (sizeof(T) == 4) {
-      x[0] = __uint_as_float(v[j].x); x[1] = __uint_as_float(v[j].y);
-      x[2] = __uint_as_float(v[j].z); x[3] = __uint_as_float(v[j].w);
-    } else {
-      const unsigned w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
-      for (int q = 0; q < VE / 2; ++q) { x[2 * q] = bf16_lo(w[q & 3]); x[2 * q + 1] = bf16_hi(w[q & 3]); }
+    for (int q = 0; q < VE; ++q) {
+      const float g = F32 ? __uint_as_float(w[q & 3]) : q & 1 ? bf16_hi(w[q / 2]) : bf16_lo(w[q / 2]);
+      x[q] = scaled(g, f, fd);
     }
-#pragma unroll
-    for (int q = 0; q < VE; ++q) x[q] = scaled(x[q], f, fd);
     const long long at = r.start + (long long)i * VE;
     if (vec && of32) {
       float4* d = (float4*)((float*)o + at);
 #pragma unroll
-      for (int q = 0; q < VE / 4; ++q) d[q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
-    } else if (vec && sizeof(T) == 2) {
-      *(uint4*)((__nv_bfloat16*)o + at) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
-                                                     pack_bf16(x[VE - 4], x[VE - 3]), pack_bf16(x[VE - 2], x[VE - 1]));
+      for (int q = 0; q < VE / 4; ++q) __stcs(d + q, make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]));
+    } else if (vec && !F32) {
+      __stcs((uint4*)((__nv_bfloat16*)o + at), make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
+                                                          pack_bf16(x[VE - 4], x[VE - 3]), pack_bf16(x[VE - 2], x[VE - 1])));
     } else {
 #pragma unroll
-      for (int q = 0; q < VE; ++q) store1<T>(o, at + q, x[q], of32);
+      for (int q = 0; q < VE; ++q) store1(o, at + q, x[q], of32);
     }
   }
-  const int tail = left > 0 ? left - nvec * VE : 0;
-  if (tid < r.head) store1<T>(o, tid, scaled(load1<T>(p, tid), f, fd), of32);
-  if (tid < tail) {
-    const long long at = r.start + nvec * VE + tid;
-    store1<T>(o, at, scaled(load1<T>(p, at), f, fd), of32);
+}
+__device__ __forceinline__ void scale_one(const Piece& r, void* o, long long i, float f, double fd) {
+  store1(o, i, scaled(one_value(r, i), f, fd), r.kind & OUT_F32);
+}
+
+// Scales a chunk that has been loaded.
+template <int LIM>
+__device__ __forceinline__ void scale_chunk(const ClipTable<LIM>& tab, const Piece& r, const uint4 (&v)[CLIP_VECS], float f,
+                                            double fd) {
+  void* o = tab.out[r.tensor];
+  if (r.kind & IN_F32) scale_piece<true>(v, r, o, f, fd);
+  else scale_piece<false>(v, r, o, f, fd);
+  const int body = r.nvec * (r.kind & IN_F32 ? 4 : 8);
+  if ((int)threadIdx.x < r.head) scale_one(r, o, threadIdx.x, f, fd);
+  if ((int)threadIdx.x < r.count - body) scale_one(r, o, r.start + body + threadIdx.x, f, fd);
+}
+
+// Chunks first, first - step, ...  Backwards: those that the first pass read last are still in L2.
+template <int LIM>
+__device__ __forceinline__ void scale_all(const ClipTable<LIM>& tab, int first, int step, float f, double fd) {
+  for (int c = first; c >= 0; c -= step) {
+    const Piece r = piece_of(tab, c);
+    if (f == 1.0f && (r.kind & IN_PLACE)) continue;
+    uint4 v[CLIP_VECS];
+    load_piece(v, r, false);
+    scale_chunk(tab, r, v, f, fd);
   }
 }
 
-// norm and factor from the partial sums, then the scaled values.  The chunks are walked from the last to
-// the first: the ones that the first pass read last are still in L2.
+// The factor, in 64 bits.  A norm that is not finite (in fp32, as the caller sees it) scales nothing: no factor
+// would mend such a step.
+__device__ __forceinline__ double factor_of(double norm, float max_norm, float eps) {
+  const double ratio = (double)max_norm / (norm + (double)eps);
+  return isfinite((float)norm) && ratio < 1.0 ? ratio : 1.0;
+}
+
+// Norm and factor from the partial sums, then the scaled values.
 template <int LIM>
 __global__ void __launch_bounds__(CLIP_THREADS) k_scale(const __grid_constant__ ClipTable<LIM> tab,
                                                         const double* __restrict__ partial, int np, float max_norm,
@@ -238,19 +283,56 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_scale(const __grid_constant__ 
   double acc = 0.0;
   for (int i = threadIdx.x; i < np; i += CLIP_THREADS) acc += partial[i];
   const double norm = sqrt(block_sum(acc));
-  // a norm that is not finite (in fp32, as the caller sees it) scales nothing: no factor would mend such a step
-  const double ratio = (double)max_norm / (norm + (double)eps);
-  const double fd = (isfinite((float)norm) && ratio < 1.0) ? ratio : 1.0;
+  const double fd = factor_of(norm, max_norm, eps);
   const float f = (float)fd;
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-  const int total = tab.chunk0[tab.n];
-  for (int c = total - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
-    const int i = tensor_of(tab, c);
-    const int kind = tab.kind[i];
-    if (f == 1.0f && (kind & IN_PLACE)) continue;
-    if (kind & IN_F32) chunk_scale<float>(tab.in[i], tab.out[i], tab.numel[i], c - tab.chunk0[i], kind, f, fd);
-    else chunk_scale<__nv_bfloat16>(tab.in[i], tab.out[i], tab.numel[i], c - tab.chunk0[i], kind, f, fd);
+  if (f == 1.0f && tab.in_place) return;
+  scale_all(tab, tab.chunk0[tab.n] - 1 - (int)blockIdx.x, gridDim.x, f, fd);
+}
+
+// The same for many values that all have to be written, with one CTA a chunk: CTAs that start in order keep reads and
+// writes of HBM closer together than a persistent grid, whose CTAs drift apart (99 against 111 us for 327 MB in and
+// out).  The sum is a single value here, and a CTA's loads are under way while it makes the factor of it.
+template <int LIM>
+__global__ void __launch_bounds__(CLIP_THREADS) k_scale_each(const __grid_constant__ ClipTable<LIM> tab,
+                                                             const double* __restrict__ sqsum, float max_norm, float eps,
+                                                             float* __restrict__ norm_out) {
+  __shared__ double factor;
+  const Piece r = piece_of(tab, gridDim.x - 1 - blockIdx.x);
+  uint4 v[CLIP_VECS];
+  load_piece(v, r, false);
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(*sqsum);
+    factor = factor_of(norm, max_norm, eps);
+    if (norm_out && blockIdx.x == 0) *norm_out = (float)norm;
   }
+  __syncthreads();
+  const double fd = factor;
+  const float f = (float)fd;
+  if (f == 1.0f && (r.kind & IN_PLACE)) return;
+  scale_chunk(tab, r, v, f, fd);
+}
+
+// Few values: all of it in one launch, by one cluster of CTAs that add their sums up in distributed shared memory.
+template <int LIM>
+__global__ void __cluster_dims__(CLIP_CLUSTER, 1, 1) __launch_bounds__(CLIP_THREADS)
+    k_clip_small(const __grid_constant__ ClipTable<LIM> tab, float max_norm, float eps, float* __restrict__ norm_out) {
+  __shared__ double mine;
+  cg::cluster_group cluster = cg::this_cluster();
+  const double s = block_sum(square_sums(tab, blockIdx.x, CLIP_CLUSTER));
+  if (threadIdx.x == 0) mine = s;
+  cluster.sync();
+  double all = 0.0;
+#pragma unroll
+  for (int r = 0; r < CLIP_CLUSTER; ++r) all += *cluster.map_shared_rank(&mine, r);
+  cluster.sync();                                 // nobody leaves before all have read
+  const double norm = sqrt(all), fd = factor_of(norm, max_norm, eps);
+  const float f = (float)fd;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+  if (f == 1.0f && tab.in_place) return;
+  // first the chunk that this CTA read last
+  const int total = tab.chunk0[tab.n], rank = blockIdx.x;
+  if (rank < total) scale_all(tab, rank + (total - 1 - rank) / CLIP_CLUSTER * CLIP_CLUSTER, CLIP_CLUSTER, f, fd);
 }
 
 struct ClipList {
@@ -300,6 +382,7 @@ pctc_status_t check_list(const ClipList& l, bool writes) {
 template <int LIM>
 pctc_status_t fill_table(const ClipList& l, int i0, int i1, bool writes, ClipTable<LIM>* tab) {
   tab->n = 0;
+  tab->in_place = 1;
   long long chunks = 0;
   for (int i = i0; i < i1; ++i) {
     if (l.numels[i] == 0) continue;
@@ -312,66 +395,103 @@ pctc_status_t fill_table(const ClipList& l, int i0, int i1, bool writes, ClipTab
     void* out = nullptr;
     if (writes) {
       out = l.out(i);
-      if (out == l.in(i)) kind |= IN_PLACE;
+      if (out == l.in(i)) kind |= IN_PLACE; else tab->in_place = 0;
       if (l.out_dtype(i) == PCTC_FP32) kind |= OUT_F32;
       // stores are as wide as the loads where the output reaches a 16-byte boundary with the input
-      const size_t head = (((16 - ((size_t)l.in(i) & 15)) & 15) / es);
+      const size_t head = head_of(l.in(i), l.numels[i], es);
       if ((((size_t)out + head * elem_bytes(l.out_dtype(i))) & 15) == 0) kind |= OUT_VEC;
     }
     tab->out[k] = out;
     tab->kind[k] = kind;
-    const size_t mis = (size_t)l.in(i) & 15;
-    const long long head = mis ? (long long)((16 - mis) / es) : 0;
-    const long long body = l.numels[i] > head ? l.numels[i] - head : 0;
-    chunks += body ? (body + CLIP_CHUNK - 1) / CLIP_CHUNK : 1;
+    const long long body = l.numels[i] - head_of(l.in(i), l.numels[i], es), per = CLIP_CHUNK_BYTES / es;
+    chunks += body ? (body + per - 1) / per : 1;
     if (chunks > 0x7fff0000LL) return PCTC_ERR_UNSUPPORTED;
   }
   tab->chunk0[tab->n] = (int)chunks;
   return PCTC_OK;
 }
 
-int clip_grid(int chunks) {
+int clip_grid(int chunks, int per_sm) {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     sms = 148;
-  int most = sms * CLIP_CTAS_PER_SM;
+  int most = sms * per_sm;
   if (most > CLIP_MAX_GRID) most = CLIP_MAX_GRID;
   return chunks < 1 ? 1 : chunks < most ? chunks : most;
 }
 
 template <int LIM>
-pctc_status_t square_sums(const ClipList& l, double* partial, int* np, cudaStream_t stream) {
+pctc_status_t sum_launch(const ClipTable<LIM>& tab, double* partial, int* np, cudaStream_t stream) {
+  const int grid = clip_grid(tab.chunk0[tab.n], CLIP_CTAS_PER_SM);
+  k_square_sums<LIM><<<grid, CLIP_THREADS, 0, stream>>>(tab, partial + *np);
+  *np += grid;
+  return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+}
+
+// sums: np of them, and room for one more behind them (np == 1: the whole sum, which nothing is written to).
+template <int LIM>
+pctc_status_t scale_launch(const ClipTable<LIM>& tab, const double* sums, int np, float max_norm, float eps, float* norm,
+                           cudaStream_t stream) {
+  const int chunks = tab.chunk0[tab.n];
+  if (!tab.in_place && chunks >= CLIP_EACH_CHUNKS) {
+    if (np > 1) {
+      k_sum_partials<<<1, CLIP_THREADS, 0, stream>>>(sums, np, const_cast<double*>(sums) + np);
+      sums += np;
+    }
+    k_scale_each<LIM><<<chunks, CLIP_THREADS, 0, stream>>>(tab, sums, max_norm, eps, norm);
+  } else {
+    k_scale<LIM><<<clip_grid(chunks, CLIP_SCALE_CTAS_PER_SM), CLIP_THREADS, 0, stream>>>(tab, sums, np, max_norm, eps, norm);
+  }
+  return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+}
+
+// The launches of a call: the sums of all tensors (given == null), then the scaling (max_norm > 0), LIM tensors at a
+// time.  With one table for all tensors both passes share it, and few values need one launch.
+template <int LIM>
+pctc_status_t clip_launches(const ClipList& l, const double* given, double* partial, double* sqsum, float max_norm, float eps,
+                            float* norm, cudaStream_t stream) {
   ClipTable<LIM> tab;
-  *np = 0;
-  for (int i0 = 0; i0 == 0 || i0 < l.n; i0 += LIM) {
-    const pctc_status_t st = fill_table<LIM>(l, i0, l.n < i0 + LIM ? l.n : i0 + LIM, false, &tab);
+  const bool scaling = max_norm > 0.f, one = l.n <= LIM;
+  int np = 0;
+  for (int i0 = 0; !given && (i0 == 0 || i0 < l.n); i0 += LIM) {
+    pctc_status_t st = fill_table<LIM>(l, i0, one ? l.n : l.n < i0 + LIM ? l.n : i0 + LIM, scaling, &tab);
     if (st != PCTC_OK) return st;
-    const int grid = clip_grid(tab.chunk0[tab.n]);
-    k_square_sums<LIM><<<grid, CLIP_THREADS, 0, stream>>>(tab, partial + *np);
-    if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
-    *np += grid;
+    if (one && scaling && tab.chunk0[tab.n] <= CLIP_CLUSTER_CHUNKS) {
+      k_clip_small<LIM><<<CLIP_CLUSTER, CLIP_THREADS, 0, stream>>>(tab, max_norm, eps, norm);
+      return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+    }
+    st = sum_launch(tab, partial, &np, stream);
+    if (st != PCTC_OK) return st;
+  }
+  if (!scaling) {
+    k_sum_partials<<<1, CLIP_THREADS, 0, stream>>>(partial, np, sqsum);
+    return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+  }
+  for (int i0 = 0; i0 == 0 || i0 < l.n; i0 += LIM) {
+    if (given || !one) {
+      const pctc_status_t st = fill_table<LIM>(l, i0, l.n < i0 + LIM ? l.n : i0 + LIM, true, &tab);
+      if (st != PCTC_OK) return st;
+    }
+    const pctc_status_t st = scale_launch(tab, given ? given : partial, given ? 1 : np, max_norm, eps, i0 == 0 ? norm : nullptr, stream);
+    if (st != PCTC_OK) return st;
   }
   return PCTC_OK;
 }
 
-template <int LIM>
-pctc_status_t scale(const ClipList& l, const double* partial, int np, float max_norm, float eps, float* norm,
-                    cudaStream_t stream) {
-  ClipTable<LIM> tab;
-  for (int i0 = 0; i0 == 0 || i0 < l.n; i0 += LIM) {
-    const pctc_status_t st = fill_table<LIM>(l, i0, l.n < i0 + LIM ? l.n : i0 + LIM, true, &tab);
-    if (st != PCTC_OK) return st;
-    k_scale<LIM><<<clip_grid(tab.chunk0[tab.n]), CLIP_THREADS, 0, stream>>>(tab, partial, np, max_norm, eps,
-                                                                           i0 == 0 ? norm : nullptr);
-    if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
-  }
-  return PCTC_OK;
+pctc_status_t clip_call(const ClipList& l, const double* given, double* partial, double* sqsum, float max_norm, float eps,
+                        float* norm, void* stream_v) {
+  cudaStream_t stream = (cudaStream_t)stream_v;
+  // a launch copies its whole table, so the smallest that holds the list
+  return l.n <= 48    ? clip_launches<48>(l, given, partial, sqsum, max_norm, eps, norm, stream)
+         : l.n <= 192 ? clip_launches<192>(l, given, partial, sqsum, max_norm, eps, norm, stream)
+         : l.n <= 512 ? clip_launches<512>(l, given, partial, sqsum, max_norm, eps, norm, stream)
+                      : clip_launches<CLIP_LARGE>(l, given, partial, sqsum, max_norm, eps, norm, stream);
 }
 
 bool bad_limits(float max_norm, float eps) {
   return !(max_norm > 0.f) || !(eps >= 0.f) || std::isinf(eps);
 }
-size_t partial_count(int n) { return (size_t)CLIP_MAX_GRID * (n <= CLIP_LARGE ? 1 : ((size_t)n + CLIP_LARGE - 1) / CLIP_LARGE); }
+size_t partial_count(int n) { return 32 + (size_t)CLIP_MAX_GRID * (n <= CLIP_LARGE ? 1 : ((size_t)n + CLIP_LARGE - 1) / CLIP_LARGE); }
 
 }  // namespace
 }  // namespace pctc
@@ -393,13 +513,7 @@ pctc_status_t pctc_grad_sqsum(int32_t n, const void* const* grads, const int64_t
   if (st != PCTC_OK) return st;
   if (!sqsum || ((size_t)sqsum & 7) || !workspace || ((size_t)workspace & 255)) return PCTC_ERR_INVALID_ARG;
   if (workspace_bytes < partial_count(n) * sizeof(double)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
-  cudaStream_t stream = (cudaStream_t)stream_v;
-  double* partial = (double*)workspace;
-  int np = 0;
-  st = n <= CLIP_SMALL ? square_sums<CLIP_SMALL>(l, partial, &np, stream) : square_sums<CLIP_LARGE>(l, partial, &np, stream);
-  if (st != PCTC_OK) return st;
-  k_sum_partials<<<1, CLIP_THREADS, 0, stream>>>(partial, np, sqsum);
-  return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+  return clip_call(l, nullptr, (double*)workspace, sqsum, 0.f, 0.f, nullptr, stream_v);
 }
 
 pctc_status_t pctc_grad_scale(int32_t n, const void* const* grads, void* const* outs, const int64_t* numels,
@@ -409,9 +523,7 @@ pctc_status_t pctc_grad_scale(int32_t n, const void* const* grads, void* const* 
   pctc_status_t st = check_list(l, true);
   if (st != PCTC_OK) return st;
   if (!sqsum || ((size_t)sqsum & 7) || bad_limits(max_norm, eps)) return PCTC_ERR_INVALID_ARG;
-  cudaStream_t stream = (cudaStream_t)stream_v;
-  return n <= CLIP_SMALL ? scale<CLIP_SMALL>(l, sqsum, 1, max_norm, eps, norm, stream)
-                         : scale<CLIP_LARGE>(l, sqsum, 1, max_norm, eps, norm, stream);
+  return clip_call(l, sqsum, nullptr, nullptr, max_norm, eps, norm, stream_v);
 }
 
 pctc_status_t pctc_clip_grad_norm(int32_t n, const void* const* grads, void* const* outs, const int64_t* numels,
@@ -422,13 +534,7 @@ pctc_status_t pctc_clip_grad_norm(int32_t n, const void* const* grads, void* con
   if (st != PCTC_OK) return st;
   if (!norm || !workspace || ((size_t)workspace & 255) || bad_limits(max_norm, eps)) return PCTC_ERR_INVALID_ARG;
   if (workspace_bytes < partial_count(n) * sizeof(double)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
-  cudaStream_t stream = (cudaStream_t)stream_v;
-  double* partial = (double*)workspace;
-  int np = 0;
-  st = n <= CLIP_SMALL ? square_sums<CLIP_SMALL>(l, partial, &np, stream) : square_sums<CLIP_LARGE>(l, partial, &np, stream);
-  if (st != PCTC_OK) return st;
-  return n <= CLIP_SMALL ? scale<CLIP_SMALL>(l, partial, np, max_norm, eps, norm, stream)
-                         : scale<CLIP_LARGE>(l, partial, np, max_norm, eps, norm, stream);
+  return clip_call(l, nullptr, (double*)workspace, nullptr, max_norm, eps, norm, stream_v);
 }
 
 }  // extern "C"
