@@ -4,7 +4,7 @@
 //   cand(b, v) = score_b + (x_bv - lse_b),
 // and the K largest of an utterance's B * V candidates go on; among equals the lowest b * V + v.  Every logit
 // has to be read once for lse_b, and a candidate can be judged only after that: what is kept of the one
-// pass over HBM is the maximum of every 256 logits.  The K best candidates lie in the K blocks with the
+// pass over HBM is the maximum of every 512 logits.  The K best candidates lie in the K blocks with the
 // best maxima (K better ones stand against any other), so a few blocks are read again, from L2, and only there
 // single logits are compared.
 //
@@ -24,6 +24,7 @@
 #include <math_constants.h>
 
 #include <new>
+#include <utility>
 
 namespace cg = cooperative_groups;
 
@@ -31,9 +32,10 @@ namespace pctc {
 namespace {
 
 constexpr int SEL_MAX = 32;                       // beams in and out
-constexpr int SEL_THREADS = 512, SEL_WARPS = SEL_THREADS / 32;
-constexpr int SEL_BLOCK = 256;                    // logits per maximum: 8 a lane
-constexpr int SEL_BATCH = 4;                      // blocks a warp has in flight
+constexpr int SEL_MAX_WARPS = 16;                 // of a CTA: 16 where the utterances leave SMs over, else 8
+constexpr int SEL_MAX_CLUSTER = 16;
+constexpr int SEL_BLOCK = 512;                    // logits per maximum: 16 a lane
+constexpr int SEL_LANE = SEL_BLOCK / 32;
 constexpr int SEL_MAX_BLOCKS = 512;               // blocks a CTA reads again
 constexpr int SEL_MAX_CAND = 1280;
 constexpr long long SEL_MAX_V = 1 << 21;
@@ -59,81 +61,134 @@ __device__ __forceinline__ bool before(const Cand& a, const Cand& b) {
   return a.score > b.score || (a.score == b.score && a.at < b.at);
 }
 
+// Maxima here are NaN if an operand is: a block with a NaN shows by its maximum.
 __device__ __forceinline__ float warp_max(float v) {
   float r;
-  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float lane_max(const float (&x)[SEL_LANE]) {
+  float m = max3(x[0], x[1], x[2]), n = max3(x[3], x[4], x[5]);
+#pragma unroll
+  for (int e = 6; e + 3 < SEL_LANE; e += 4) {
+    m = max3(m, x[e], x[e + 1]);
+    n = max3(n, x[e + 2], x[e + 3]);
+  }
+  return max3(m, n, max3(x[SEL_LANE - 2], x[SEL_LANE - 1], x[SEL_LANE - 1]));
+}
+static_assert(SEL_LANE == 16, "lane_max");
 __device__ __forceinline__ float exp2_approx(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
-// Eight logits of a lane: 16-byte loads where every row starts on a 16-byte boundary, else one by one.
-template <typename T, bool VEC>
-struct Octet;
-template <>
-struct Octet<__nv_bfloat16, true> {
-  uint4 r;
-  static __device__ __forceinline__ int index(int lane, int e) { return lane * 8 + e; }
-  __device__ __forceinline__ void load(const __nv_bfloat16* p, int left, int lane) {
-    const int i = lane * 8;
-    if (i + 8 <= left) {
-      r = *(const uint4*)(p + i);
-    } else {
-      unsigned w[4];
+struct Pair { float a, b; };
+__device__ __forceinline__ Pair add2(Pair x, Pair y) {
+  Pair r;
+  asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%2, %3};\n\tmov.b64 v, {%4, %5};\n\tadd.rn.f32x2 u, u, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
+      : "=f"(r.a), "=f"(r.b) : "f"(x.a), "f"(x.b), "f"(y.a), "f"(y.b));
+  return r;
+}
+__device__ __forceinline__ Pair mul2(Pair x, Pair y) {
+  Pair r;
+  asm("{\n\t.reg .b64 u, v;\n\tmov.b64 u, {%2, %3};\n\tmov.b64 v, {%4, %5};\n\tmul.rn.f32x2 u, u, v;\n\tmov.b64 {%0, %1}, u;\n\t}"
+      : "=f"(r.a), "=f"(r.b) : "f"(x.a), "f"(x.b), "f"(y.a), "f"(y.b));
+  return r;
+}
+__device__ __forceinline__ Pair both(float v) { return Pair{v, v}; }
+
+// Sum of exp(x_i - z) of a lane's values: packed differences, products and sums, one ex2 each.
+__device__ __forceinline__ float lane_exp(const float (&x)[SEL_LANE], float z) {
+  Pair acc0 = both(0.f), acc1 = both(0.f);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const unsigned lo = i + 2 * e < left ? ((const unsigned short*)p)[i + 2 * e] : 0xff80u;
-        const unsigned hi = i + 2 * e + 1 < left ? ((const unsigned short*)p)[i + 2 * e + 1] : 0xff80u;
-        w[e] = lo | hi << 16;
-      }
-      r = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+  for (int e = 0; e < SEL_LANE; e += 4) {
+    const Pair y = mul2(add2(Pair{x[e], x[e + 1]}, both(-z)), both(1.44269504f));
+    const Pair w = mul2(add2(Pair{x[e + 2], x[e + 3]}, both(-z)), both(1.44269504f));
+    acc0 = add2(acc0, Pair{exp2_approx(y.a), exp2_approx(y.b)});
+    acc1 = add2(acc1, Pair{exp2_approx(w.a), exp2_approx(w.b)});
   }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-    const unsigned w[4] = {r.x, r.y, r.z, r.w};
+  acc0 = add2(acc0, acc1);
+  return acc0.a + acc0.b;
+}
+
+// A lane's 16 of a block of 512 logits: 16-byte loads where every row starts on a 16-byte boundary, else one by one.
+// load() takes the lane's first one; load_part() the block's first one, of which `left` exist (the others read -inf).
+template <typename T, bool VEC>
+struct Block;
+template <>
+struct Block<__nv_bfloat16, true> {
+  uint4 r[2];
+  static __device__ __forceinline__ int index(int lane, int e) { return (e < 8 ? 0 : 248) + lane * 8 + e; }
+  static __device__ __forceinline__ int first(int lane) { return lane * 8; }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    r[0] = ((const uint4*)p)[0];
+    r[1] = ((const uint4*)p)[32];
+  }
+  __device__ __forceinline__ void load_part(const __nv_bfloat16* p, int left, int lane) {
+    unsigned w[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 8; ++e) {
+      const int i = index(lane, 2 * e);
+      const unsigned lo = i < left ? ((const unsigned short*)p)[i] : 0xff80u;
+      const unsigned hi = i + 1 < left ? ((const unsigned short*)p)[i + 1] : 0xff80u;
+      w[e] = lo | hi << 16;
+    }
+    r[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    r[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+  __device__ __forceinline__ void get(float (&x)[SEL_LANE]) const {
+    const unsigned w[8] = {r[0].x, r[0].y, r[0].z, r[0].w, r[1].x, r[1].y, r[1].z, r[1].w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
       x[2 * e] = __uint_as_float(w[e] << 16);
       x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
     }
   }
 };
 template <>
-struct Octet<float, true> {
-  float4 a, b;
-  static __device__ __forceinline__ int index(int lane, int e) { return (e < 4 ? 0 : 124) + lane * 4 + e; }
-  static __device__ __forceinline__ float4 quad(const float* p, int i, int left) {
-    if (i + 4 <= left) return *(const float4*)(p + i);
-    float4 v;
-    v.x = i < left ? p[i] : -CUDART_INF_F;
-    v.y = i + 1 < left ? p[i + 1] : -CUDART_INF_F;
-    v.z = i + 2 < left ? p[i + 2] : -CUDART_INF_F;
-    v.w = -CUDART_INF_F;
-    return v;
+struct Block<float, true> {
+  float4 r[4];
+  static __device__ __forceinline__ int index(int lane, int e) { return e / 4 * 128 + lane * 4 + e % 4; }
+  static __device__ __forceinline__ int first(int lane) { return lane * 4; }
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) r[q] = ((const float4*)p)[32 * q];
   }
-  __device__ __forceinline__ void load(const float* p, int left, int lane) {
-    a = quad(p, lane * 4, left);
-    b = quad(p, 128 + lane * 4, left);
+  static __device__ __forceinline__ float one(const float* p, int i, int left) { return i < left ? p[i] : -CUDART_INF_F; }
+  __device__ __forceinline__ void load_part(const float* p, int left, int lane) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int i = index(lane, 4 * q);
+      r[q] = make_float4(one(p, i, left), one(p, i + 1, left), one(p, i + 2, left), one(p, i + 3, left));
+    }
   }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  __device__ __forceinline__ void get(float (&x)[SEL_LANE]) const {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) { x[4 * q] = r[q].x; x[4 * q + 1] = r[q].y; x[4 * q + 2] = r[q].z; x[4 * q + 3] = r[q].w; }
   }
 };
 template <typename T>
-struct Octet<T, false> {
-  T v[8];
+struct Block<T, false> {
+  T r[SEL_LANE];
   static __device__ __forceinline__ int index(int lane, int e) { return e * 32 + lane; }
-  __device__ __forceinline__ void load(const T* p, int left, int lane) {
+  static __device__ __forceinline__ int first(int lane) { return lane; }
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e * 32 + lane < left ? p[e * 32 + lane] : (T)(-CUDART_INF_F);
+    for (int e = 0; e < SEL_LANE; ++e) r[e] = p[e * 32];
   }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
+  __device__ __forceinline__ void load_part(const T* p, int left, int lane) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+    for (int e = 0; e < SEL_LANE; ++e) r[e] = index(lane, e) < left ? p[index(lane, e)] : (T)(-CUDART_INF_F);
+  }
+  __device__ __forceinline__ void get(float (&x)[SEL_LANE]) const {
+#pragma unroll
+    for (int e = 0; e < SEL_LANE; ++e) x[e] = (float)r[e];
   }
 };
 
@@ -142,21 +197,21 @@ struct SelShared {
   unsigned char kind[SEL_MAX];                    // 0 dead, 1 live, 2 ended
   int rows[SEL_MAX];                              // the live rows, ascending
   int nlive, bad;
-  float part_m[SEL_WARPS][SEL_MAX];               // per warp and live row
-  double part_s[SEL_WARPS][SEL_MAX];
-  float row_m[SEL_MAX];                           // of this CTA's columns
-  double row_s[SEL_MAX];
+  float part_m[SEL_MAX_WARPS][SEL_MAX];           // per warp and live row: reference and sum of exponentials
+  double part_s[SEL_MAX_WARPS][SEL_MAX];
+  float row_m[SEL_MAX_CLUSTER][SEL_MAX];          // per CTA of the cluster and live row
+  double row_s[SEL_MAX_CLUSTER][SEL_MAX];
   double lse[SEL_MAX];                            // by row; NaN: the row gives no candidates
   double group[32];
-  double thr;
-  int warp_count[SEL_WARPS];
-  int nblocks, ncand, overflow;
+  double bound[SEL_MAX_CLUSTER];                  // per CTA: K of its candidates reach this score
+  int warp_count[SEL_MAX_WARPS];
+  int nblocks, nequal, ncand, overflow;
   int blocks[SEL_MAX_BLOCKS];
   Cand cand[SEL_MAX_CAND];
-  Cand best[SEL_WARPS];
+  Cand best[SEL_MAX_WARPS];
 };
 
-// (max, sum) pairs of the lanes of a warp joined: m the largest, s = sum_i s_i exp(m_i - m), in 64 bits.
+// (reference, sum) pairs of the lanes of a warp joined: m the largest, s = sum_i s_i exp(m_i - m), in 64 bits.
 __device__ __forceinline__ void join(float& m, double& s) {
   const float mine = m;
 #pragma unroll
@@ -176,7 +231,7 @@ __device__ __forceinline__ Cand candidate(const SelShared& sh, const T* base, lo
 
 // The K best by K passes over all candidates, each for the best one behind the last: for inputs whose ties or
 // order leave more candidates than the lists hold.  Called by all threads of one CTA.
-template <typename T>
+template <typename T, int WARPS>
 __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   Cand last{CUDART_INF, 0};
@@ -186,7 +241,7 @@ __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base)
     for (int i = 0; i < sh.nlive; ++i) {
       const int b = sh.rows[i];
       if (isnan(sh.lse[b])) continue;
-      for (int v = tid; v < a.V; v += SEL_THREADS) {
+      for (int v = tid; v < a.V; v += WARPS * 32) {
         const Cand c = candidate(sh, base, a.stride_b, b, v);
         if (c.score > -CUDART_INF && before(last, c) && before(c, best)) best = c;
       }
@@ -203,7 +258,7 @@ __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base)
     if (lane == 0) sh.best[warp] = best;
     __syncthreads();
     best = sh.best[0];
-    for (int w = 1; w < SEL_WARPS; ++w)
+    for (int w = 1; w < WARPS; ++w)
       if (before(sh.best[w], best)) best = sh.best[w];
     if (best.score == -CUDART_INF) break;
     if (tid == 0) sh.cand[k] = best;
@@ -215,11 +270,13 @@ __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base)
   __syncthreads();
 }
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a) {
+template <typename T, bool VEC, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const SelArgs a) {
+  constexpr int THREADS = WARPS * 32;
   __shared__ SelShared sh;
   extern __shared__ float bmax[];                 // [live rows][blocks of this CTA]
   cg::cluster_group cluster = cg::this_cluster();
+  auto started = cluster.barrier_arrive();        // waited for before the first write to another CTA
   const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
   const int n = blockIdx.x / C;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -240,10 +297,10 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
     if (lane == 0) {
       sh.nlive = __popc(live);
       sh.bad = bad != 0;
-      sh.nblocks = sh.ncand = sh.overflow = 0;
+      sh.nblocks = sh.nequal = sh.ncand = sh.overflow = 0;
     }
   }
-  for (int i = tid; i < SEL_WARPS * SEL_MAX; i += SEL_THREADS) {
+  for (int i = tid; i < WARPS * SEL_MAX; i += THREADS) {
     (&sh.part_m[0][0])[i] = -CUDART_INF_F;
     (&sh.part_s[0][0])[i] = 0.0;
   }
@@ -254,145 +311,195 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
   // candidates tie.
   const int items = sh.nlive * nbl;
   {
-    const int w0 = nbl * warp / SEL_WARPS, w1 = nbl * (warp + 1) / SEL_WARPS;
-    const int end = sh.nlive * (w1 - w0);
-    int r = 0, blk = w0;
-    float ref = -CUDART_INF_F, sum = 0.f;
-    for (int it = 0; it < end; it += SEL_BATCH) {
-      Octet<T, VEC> raw[SEL_BATCH];
-      int lr = r, lb = blk;
-#pragma unroll
-      for (int u = 0; u < SEL_BATCH; ++u) {
-        if (it + u < end) {
-          const int v0 = (b0 + lb) * SEL_BLOCK;
-          raw[u].load(base + sh.rows[lr] * a.stride_b + v0, a.V - v0, lane);
-          if (++lb == w1) { lb = w0; ++lr; }
-        }
+    const int w0 = nbl * warp / WARPS, per_row = nbl * (warp + 1) / WARPS - w0;
+    const int steps = sh.nlive * per_row;
+    const int v0 = (b0 + w0) * SEL_BLOCK;
+    const bool part = per_row && (b0 + w0 + per_row) * SEL_BLOCK > a.V;      // the last block of a row is not whole
+    // AHEAD blocks a warp are in flight.  Sums refer to `ref`, not to the running maximum: it follows the maximum only
+    // when that is 40 ahead, far from where exp overflows, so that no block waits for its maximum.
+    constexpr int AHEAD = VEC && sizeof(T) == 2 ? 2 : 1;
+    Block<T, VEC> ring[AHEAD];
+    int fetched = 0, fr = 0, fleft = 0;           // of the fetches: the next row, and the blocks left in this one
+    const T* fp = nullptr;
+    auto fetch = [&](Block<T, VEC>& o) {
+      if (fetched >= steps) return;
+      if (fleft == 0) {
+        fp = base + sh.rows[fr] * a.stride_b + v0 + Block<T, VEC>::first(lane);
+        fleft = per_row;
+        ++fr;
       }
+      if (part && fleft == 1) {
+        const int at = v0 + (per_row - 1) * SEL_BLOCK;
+        o.load_part(base + sh.rows[fr - 1] * a.stride_b + at, a.V - at, lane);
+      } else {
+        o.load(fp);
+      }
+      fp += SEL_BLOCK;
+      --fleft;
+      ++fetched;
+    };
 #pragma unroll
-      for (int u = 0; u < SEL_BATCH; ++u) {
-        if (it + u < end) {
-          float x[8];
-          raw[u].get(x);
-          float m = x[0];
+    for (int u = 0; u < AHEAD; ++u) fetch(ring[u]);
+    int r = 0, left = per_row;
+    float* maxima = bmax + w0;
+    float ref = -CUDART_INF_F, sum = 0.f;
+    for (int it = 0; it < steps; it += AHEAD) {
 #pragma unroll
-          for (int e = 1; e < 8; ++e) m = fmaxf(m, x[e]);
-          m = warp_max(m);
-          if (lane == 0) bmax[r * nbl + blk] = m;
-          if (m > ref) {
-            sum *= exp2_approx((ref - m) * 1.44269504f);
-            ref = m;
-          }
-          const float z = ref == -CUDART_INF_F ? 0.f : ref;     // all masked so far: exp(-inf) = 0, NaN stays NaN
-          float t = 0.f;
+      for (int u = 0; u < AHEAD; ++u) {
+        if (u && it + u >= steps) break;
+        float x[SEL_LANE];
+        ring[u].get(x);
+        fetch(ring[u]);
+        const float m = warp_max(lane_max(x));
+        if (lane == 0) *maxima = m;
+        ++maxima;
+        float t = lane_exp(x, ref == -CUDART_INF_F ? 0.f : ref);
+        if (!(m <= ref + 40.f)) {                 // the first block of a row with anything in it, and rarely after
+          sum *= exp2_approx((ref - m) * 1.44269504f);
+          ref = m;
+          t = lane_exp(x, m);
+        }
+        sum += t;
+        if (--left == 0) {                        // the row ends for this warp
+          double s = sum;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) t += exp2_approx((x[e] - z) * 1.44269504f);
-          sum += t;
-          if (++blk == w1) {                      // the row ends for this warp
-            double s = sum;
-#pragma unroll
-            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (lane == 0) { sh.part_m[warp][r] = ref; sh.part_s[warp][r] = s; }
-            ref = -CUDART_INF_F;
-            sum = 0.f;
-            blk = w0;
-            ++r;
-          }
+          for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+          if (lane == 0) { sh.part_m[warp][r] = ref; sh.part_s[warp][r] = s; }
+          ref = -CUDART_INF_F;
+          sum = 0.f;
+          left = per_row;
+          ++r;
+          maxima = bmax + r * nbl + w0;
         }
       }
     }
   }
   __syncthreads();
-  for (int r = warp; r < sh.nlive; r += SEL_WARPS) {
-    float m = lane < SEL_WARPS ? sh.part_m[lane][r] : -CUDART_INF_F;
-    double s = lane < SEL_WARPS ? sh.part_s[lane][r] : 0.0;
+  // every CTA tells all others its part of every row: what follows reads its own shared memory only
+  cluster.barrier_wait(std::move(started));
+  for (int r = warp; r < sh.nlive; r += WARPS) {
+    float m = lane < WARPS ? sh.part_m[lane][r] : -CUDART_INF_F;
+    double s = lane < WARPS ? sh.part_s[lane][r] : 0.0;
     join(m, s);
-    if (lane == 0) { sh.row_m[r] = m; sh.row_s[r] = s; }
+    if (lane < C) {
+      SelShared* other = cluster.map_shared_rank(&sh, lane);
+      other->row_m[c][r] = m;
+      other->row_s[c][r] = s;
+    }
   }
   cluster.sync();
-  for (int r = warp; r < sh.nlive; r += SEL_WARPS) {
-    float m = -CUDART_INF_F;
-    double s = 0.0;
-    if (lane < C) {
-      const SelShared* other = cluster.map_shared_rank(&sh, lane);
-      m = other->row_m[r];
-      s = other->row_s[r];
-    }
+  for (int r = warp; r < sh.nlive; r += WARPS) {
+    float m = lane < C ? sh.row_m[lane][r] : -CUDART_INF_F;
+    double s = lane < C ? sh.row_s[lane][r] : 0.0;
     join(m, s);
     // nothing allowed, or a NaN or +inf among the logits: no candidates
     const double lse = (double)m + log(s);
     const bool fine = isfinite(lse);
     if (lane == 0) {
       sh.lse[sh.rows[r]] = fine ? lse : CUDART_NAN;
-      if (!fine && !(s == 0.0)) atomicOr(&sh.bad, 1);
+      if (isnan(s) || m == CUDART_INF_F) atomicOr(&sh.bad, 1);
     }
   }
   __syncthreads();
 
-  // ---- the blocks that can hold one of the K best: those from the K-th best of 32 groups' maxima on ----
+  // ---- the blocks that can hold one of the K best: those that reach the K-th best of 32 groups' maxima, of the CTA
+  // of the cluster where that is highest ----
   auto block_score = [&](int e) {
     const int r = e / nbl, b = sh.rows[r];
     const double s = (double)sh.score[b] + ((double)bmax[e] - sh.lse[b]);
     return isnan(s) ? -CUDART_INF : s;
   };
-  double top = -CUDART_INF;                       // group g: the blocks e with e % 32 == g, sixteen threads each
-  for (int e = (tid & 15) * 32 + (tid >> 4); e < items; e += SEL_THREADS) top = fmax(top, block_score(e));
+  constexpr int PER = THREADS / 32;               // group g: the blocks e with e % 32 == g, PER threads each
+  double top = -CUDART_INF;
+  for (int e = (tid % PER) * 32 + tid / PER; e < items; e += THREADS) top = fmax(top, block_score(e));
 #pragma unroll
-  for (int o = 8; o; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if ((lane & 15) == 0) sh.group[tid >> 4] = top;
+  for (int o = PER / 2; o; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (tid % PER == 0) sh.group[tid / PER] = top;
   __syncthreads();
   if (warp == 0) {
     const double mine = sh.group[lane];
     int rank = 0;
+#pragma unroll 8
     for (int i = 0; i < 32; ++i) {
-      const double o = __shfl_sync(0xffffffffu, mine, i);
+      const double o = sh.group[i];
       rank += o > mine || (o == mine && i < lane);
     }
-    if (rank == a.K - 1) sh.thr = mine;
+    const unsigned kth = __ballot_sync(0xffffffffu, rank == a.K - 1);
+    const double bound = __shfl_sync(0xffffffffu, mine, __ffs(kth) - 1);
+    if (lane < C) cluster.map_shared_rank(&sh, lane)->bound[c] = bound;
+  }
+  cluster.sync();
+  double thr = sh.bound[0];
+  for (int o = 1; o < C; ++o) thr = fmax(thr, sh.bound[o]);
+  for (int e = tid; e < items; e += THREADS) {
+    const double s = block_score(e);
+    if (s > -CUDART_INF && s >= thr) {
+      if (s == thr) atomicAdd(&sh.nequal, 1);
+      const int p = atomicAdd(&sh.nblocks, 1);
+      if (p < SEL_MAX_BLOCKS) sh.blocks[p] = e;
+    }
   }
   __syncthreads();
-  const double thr = sh.thr;
-  int equal = 0;                                  // blocks that tie with the threshold: the first K of them will do
-  for (int e0 = 0; e0 < items; e0 += SEL_THREADS) {
-    const int e = e0 + tid;
-    const double s = e < items ? block_score(e) : -CUDART_INF;
-    const bool some = s > -CUDART_INF;
-    const unsigned eq = __ballot_sync(0xffffffffu, some && s == thr);
-    if (lane == 0) sh.warp_count[warp] = __popc(eq);
+  if (sh.nequal > a.K || sh.nblocks > SEL_MAX_BLOCKS) {   // of the blocks that tie with the threshold the first K will do
     __syncthreads();
-    int prior = equal, all = equal;
-    for (int w = 0; w < SEL_WARPS; ++w) {
-      if (w < warp) prior += sh.warp_count[w];
-      all += sh.warp_count[w];
+    if (tid == 0) sh.nblocks = 0;
+    int equal = 0;
+    for (int e0 = 0; e0 < items; e0 += THREADS) {
+      const int e = e0 + tid;
+      const double s = e < items ? block_score(e) : -CUDART_INF;
+      const bool some = s > -CUDART_INF;
+      const unsigned eq = __ballot_sync(0xffffffffu, some && s == thr);
+      if (lane == 0) sh.warp_count[warp] = __popc(eq);
+      __syncthreads();
+      int prior = equal, all = equal;
+      for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) prior += sh.warp_count[w];
+        all += sh.warp_count[w];
+      }
+      equal = all;
+      if (some && (s > thr || (s == thr && prior + __popc(eq & ((1u << lane) - 1)) < a.K))) {
+        const int p = atomicAdd(&sh.nblocks, 1);
+        if (p < SEL_MAX_BLOCKS) sh.blocks[p] = e; else atomicOr(&cluster.map_shared_rank(&sh, 0)->overflow, 1);
+      }
+      __syncthreads();
     }
-    equal = all;
-    if (some && (s > thr || (s == thr && prior + __popc(eq & ((1u << lane) - 1)) < a.K))) {
-      const int p = atomicAdd(&sh.nblocks, 1);
-      if (p < SEL_MAX_BLOCKS) sh.blocks[p] = e; else sh.overflow = 1;
-    }
-    __syncthreads();
   }
 
-  // ---- single logits of those blocks ----
+  // ---- single logits of those blocks, to the first CTA's list ----
+  SelShared* head = cluster.map_shared_rank(&sh, 0);
+  auto found = [&](double score, int b, int v) {
+    const int p = atomicAdd(&head->ncand, 1);
+    if (p < SEL_MAX_CAND) head->cand[p] = Cand{score, (unsigned long long)b << 32 | (unsigned)v};
+  };
   const int nblk = sh.nblocks < SEL_MAX_BLOCKS ? sh.nblocks : SEL_MAX_BLOCKS;
-  for (int i = warp; i < nblk; i += SEL_WARPS) {
+  for (int i = warp; i < nblk; i += WARPS) {
     const int e = sh.blocks[i], r = e / nbl, b = sh.rows[r], v0 = (b0 + e - r * nbl) * SEL_BLOCK;
-    Octet<T, VEC> raw;
-    raw.load(base + b * a.stride_b + v0, a.V - v0, lane);
-    float x[8];
+    Block<T, VEC> raw;
+    const T* p = base + b * a.stride_b + v0;
+    if (v0 + SEL_BLOCK <= a.V) raw.load(p + Block<T, VEC>::first(lane)); else raw.load_part(p, a.V - v0, lane);
+    float x[SEL_LANE];
     raw.get(x);
-    double s[8];
+    const double offset = sh.lse[b], score = sh.score[b];
+    auto cand = [&](int q) { return score + ((double)x[q] - offset); };
+    int reach = 0;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) s[q] = (double)sh.score[b] + ((double)x[q] - sh.lse[b]);
+    for (int q = 0; q < SEL_LANE; ++q) reach += cand(q) >= thr && cand(q) > -CUDART_INF;
+    if ((int)__reduce_add_sync(0xffffffffu, reach) <= a.K) {
+#pragma unroll
+      for (int q = 0; q < SEL_LANE; ++q)
+        if (cand(q) >= thr && cand(q) > -CUDART_INF) found(cand(q), b, v0 + Block<T, VEC>::index(lane, q));
+      continue;
+    }
     unsigned used = 0;
-    for (int k = 0; k < a.K; ++k) {               // at most K of a block, best first, down to the threshold
+    for (int k = 0; k < a.K; ++k) {               // the K best of the block, one by one
       double best = -CUDART_INF;
       int at = 0x7fffffff, q0 = 0;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const int v = v0 + Octet<T, VEC>::index(lane, q);
-        if (!(used >> q & 1) && (s[q] > best || (s[q] == best && s[q] > -CUDART_INF && v < at))) {
-          best = s[q];
+      for (int q = 0; q < SEL_LANE; ++q) {
+        const double s = cand(q);
+        const int v = v0 + Block<T, VEC>::index(lane, q);
+        if (!(used >> q & 1) && (s > best || (s == best && s > -CUDART_INF && v < at))) {
+          best = s;
           at = v;
           q0 = q;
         }
@@ -400,61 +507,37 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
       double all = best;
 #pragma unroll
       for (int o = 16; o; o >>= 1) all = fmax(all, __shfl_xor_sync(0xffffffffu, all, o));
-      if (!(all >= thr) || all == -CUDART_INF) break;
       const int first = (int)__reduce_min_sync(0xffffffffu, best == all ? (unsigned)at : 0x7fffffffu);
       if (best == all && at == first) {
         used |= 1u << q0;
-        const int p = atomicAdd(&sh.ncand, 1);
-        if (p < SEL_MAX_CAND) sh.cand[p] = Cand{all, (unsigned long long)b << 32 | (unsigned)at}; else sh.overflow = 1;
+        found(all, b, at);
       }
     }
   }
-  cluster.sync();
+  cluster.sync();                                 // from here on nobody reads or writes another CTA's shared memory
+  if (c != 0) return;
 
   // ---- the first CTA ranks what all have found ----
-  if (c == 0) {
-    double least = thr;                           // K candidates of one CTA reach its threshold, so the best one holds for all
-    bool over = false;
-    for (int o = 0; o < C; ++o) {
-      const SelShared* other = cluster.map_shared_rank(&sh, o);
-      least = fmax(least, other->thr);
-      over = over || other->overflow;
-    }
-    __syncthreads();
-    for (int o = 1; o < C; ++o) {
-      const SelShared* other = cluster.map_shared_rank(&sh, o);
-      const int m = other->ncand < SEL_MAX_CAND ? other->ncand : SEL_MAX_CAND;
-      for (int i = tid; i < m; i += SEL_THREADS) {
-        const Cand x = other->cand[i];
-        if (x.score < least) continue;
-        const int p = atomicAdd(&sh.ncand, 1);
-        if (p < SEL_MAX_CAND) sh.cand[p] = x;
-      }
-    }
-    if (tid < a.B && sh.kind[tid] == 2) {
-      const int p = atomicAdd(&sh.ncand, 1);
-      if (p < SEL_MAX_CAND) sh.cand[p] = Cand{(double)sh.score[tid], (unsigned long long)tid << 32 | (unsigned)a.eos};
-    }
-    __syncthreads();
-    if (over || sh.ncand > SEL_MAX_CAND) select_by_passes(sh, a, base);
-    const int nc = sh.ncand;
-    auto put = [&](int k, double score, int parent, int token) {
-      const int o = n * a.K + k;
-      a.scores_out[o] = (float)score;
-      a.parents[o] = parent;
-      a.tokens[o] = token;
-      if (a.finished_out) a.finished_out[o] = parent >= 0 && (sh.kind[parent] == 2 || token == a.eos);
-    };
-    for (int i = tid; i < nc; i += SEL_THREADS) {
-      const Cand x = sh.cand[i];
-      int rank = 0;
-      for (int j = 0; j < nc; ++j) rank += before(sh.cand[j], x);
-      if (rank < a.K) put(rank, x.score, (int)(x.at >> 32), (int)(unsigned)x.at);
-    }
-    for (int k = nc + tid; k < a.K; k += SEL_THREADS) put(k, -CUDART_INF, -1, -1);
-    if (tid == 0 && a.flags) a.flags[n] = sh.bad ? PCTC_UTT_NONFINITE : 0;
+  if (tid < a.B && sh.kind[tid] == 2) found(sh.score[tid], tid, a.eos);
+  __syncthreads();
+  if (sh.overflow || sh.ncand > SEL_MAX_CAND) select_by_passes<T, WARPS>(sh, a, base);
+  const int nc = sh.ncand;
+  auto put = [&](int k, double score, int parent, int token) {
+    const int o = n * a.K + k;
+    a.scores_out[o] = (float)score;
+    a.parents[o] = parent;
+    a.tokens[o] = token;
+    if (a.finished_out) a.finished_out[o] = parent >= 0 && (sh.kind[parent] == 2 || token == a.eos);
+  };
+  for (int i = tid; i < nc; i += THREADS) {
+    const Cand x = sh.cand[i];
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < nc; ++j) rank += before(sh.cand[j], x);
+    if (rank < a.K) put(rank, x.score, (int)(x.at >> 32), (int)(unsigned)x.at);
   }
-  cluster.sync();                                 // nobody leaves while its shared memory is read
+  for (int k = nc + tid; k < a.K; k += THREADS) put(k, -CUDART_INF, -1, -1);
+  if (tid == 0 && a.flags) a.flags[n] = sh.bad ? PCTC_UTT_NONFINITE : 0;
 }
 
 pctc_status_t check(const pctc_beam_t* p) {
@@ -468,17 +551,21 @@ pctc_status_t check(const pctc_beam_t* p) {
   return PCTC_OK;
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, int WARPS>
 cudaError_t launch_select(const SelArgs& a, int C, cudaStream_t stream) {
   const size_t dyn = (size_t)a.B * ((a.nb + C - 1) / C) * 4;
-  auto kern = k_beam_select<T, VEC>;
+  auto kern = k_beam_select<T, VEC, WARPS>;
   if (dyn + sizeof(SelShared) > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_MAX_DYN);
     if (e != cudaSuccess) return e;
   }
+  if (C > 8) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.N * C);
-  cfg.blockDim = dim3(SEL_THREADS);
+  cfg.blockDim = dim3(WARPS * 32);
   cfg.dynamicSmemBytes = dyn;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -490,11 +577,28 @@ cudaError_t launch_select(const SelArgs& a, int C, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
-// CTAs of a cluster: up to the portable 8, while every warp has a block of every row.
-int cluster_size(int nb) {
-  int C = 1;
-  while (C < 8 && nb >= C * 2 * SEL_WARPS) C *= 2;
-  return C;
+// How a call is spread over the device.  One wave: with 8 warps four CTAs fit on an SM, and a cluster is as large as
+// that allows, so that no utterance waits for another's tail.  Few utterances: clusters of 16 with 16 warps a CTA.  A
+// warp has a block of every row, unless the vocabulary is smaller than that.
+struct Spread {
+  int C, warps;
+};
+Spread spread(int N, int B, int nb) {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    sms = 148;
+  Spread s{1, 8};
+  auto maxima = [&](int C) { return (long long)B * ((nb + C - 1) / C) * 4; };
+  while (s.C < 16 && nb >= s.C * 2 * s.warps && (long long)N * s.C * 2 <= (s.C < 8 ? 4 : 1) * sms) s.C *= 2;
+  while (s.C < 8 && maxima(s.C) > 96 * 1024) s.C *= 2;      // the maxima have to fit shared memory
+  if ((long long)N * s.C <= sms && nb >= s.C * 16) s.warps = 16;
+  return s;
+}
+
+template <typename T, bool VEC>
+cudaError_t launch_select(const SelArgs& a, cudaStream_t stream) {
+  const Spread s = spread(a.N, a.B, a.nb);
+  return s.warps == 16 ? launch_select<T, VEC, 16>(a, s.C, stream) : launch_select<T, VEC, 8>(a, s.C, stream);
 }
 
 }  // namespace
@@ -527,12 +631,11 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const f
   a.tokens = tokens;
   a.finished_out = finished_out;
   a.flags = utt_flags;
-  const int C = cluster_size(a.nb);
   const bool vec = (((size_t)logits | (size_t)p->stride_n * es | (size_t)p->stride_b * es) & 15) == 0;
   cudaStream_t stream = (cudaStream_t)stream_v;
   const cudaError_t e = p->dtype == PCTC_BF16
-      ? (vec ? launch_select<__nv_bfloat16, true>(a, C, stream) : launch_select<__nv_bfloat16, false>(a, C, stream))
-      : (vec ? launch_select<float, true>(a, C, stream) : launch_select<float, false>(a, C, stream));
+      ? (vec ? launch_select<__nv_bfloat16, true>(a, stream) : launch_select<__nv_bfloat16, false>(a, stream))
+      : (vec ? launch_select<float, true>(a, stream) : launch_select<float, false>(a, stream));
   return e == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
 }
 
