@@ -342,7 +342,7 @@ pctc_status_t pctc_prefix_read(const pctc_prefix_t* problem, const void* state, 
  * and the K largest candidates of every utterance, best first; among equals the lowest b * V + v.  The
  * comparisons are of 64-bit sums; the scores that come back are rounded once to fp32.
  *
- * A beam whose score is -inf is dead: its logits are not read and it gives no candidates (a first step with
+ * A beam whose score is -inf is dead: its logits count for nothing and it gives no candidates (a first step with
  * one hypothesis: all scores but one -inf).  An ended beam (finished[n,b] != 0) keeps its score in a single
  * candidate, token eos_id.  Logits of -inf are excluded tokens; a row with nothing else gives no candidates.
  * A row with a NaN or +inf, or a beam whose score is one, gives none either and flags its utterance
@@ -362,12 +362,15 @@ typedef struct {
  * Device pointers: logits, scores [N,B] fp32, finished [N,B] bytes or NULL (needs eos_id >= 0).  Outputs:
  * scores_out [N,K] fp32, parents [N,K] and tokens [N,K] int32, finished_out [N,K] bytes or NULL (1: the parent
  * had ended, or the token is eos_id), utt_flags [N] or NULL.  scores_out and finished_out may be
- * scores and finished themselves (K == B).  One launch, no workspace; may be captured into a CUDA graph and
- * issued from several threads.
+ * scores and finished themselves (K == B).
+ * workspace: >= pctc_beam_workspace_bytes() (about 1/100 of the logits), 256-byte aligned; nothing in it outlives the
+ * call.  May be captured into a CUDA graph and issued from several threads.
  */
+pctc_status_t pctc_beam_workspace_bytes(const pctc_beam_t* problem, size_t* bytes_out);
 pctc_status_t pctc_beam_select(const pctc_beam_t* problem, const void* logits, const float* scores,
                                const uint8_t* finished, float* scores_out, int32_t* parents, int32_t* tokens,
-                               uint8_t* finished_out, int32_t* utt_flags, void* stream);
+                               uint8_t* finished_out, int32_t* utt_flags,
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Reordering of decoder states after a selection: dst[n,k] = src[n, parents[n,k]] for every state of a

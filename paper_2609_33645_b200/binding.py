@@ -25,7 +25,7 @@ EXPORTS = ("pctc_workspace_bytes", "pctc_chunk_width", "pruned_ctc_fwd_bwd", "pr
            "pruned_ctc_fwd_bwd_host", "pctc_subset_relabel_noalloc", "pctc_greedy_workspace_bytes",
            "pctc_greedy_decode", "pctc_topk_workspace_bytes", "pctc_topk_decode",
            "pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
-           "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read", "pctc_beam_select",
+           "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read", "pctc_beam_workspace_bytes", "pctc_beam_select",
            "pctc_beam_reorder")
 NOALLOC_MAX_V = 262144
 
@@ -172,7 +172,9 @@ def _configure(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.pctc_prefix_read.restype = ctypes.c_int
     lib.pctc_prefix_read.argtypes = [prefix_p, vp, ctypes.c_size_t, vp, ctypes.c_int32, vp, vp, vp, vp]
     lib.pctc_beam_select.restype = ctypes.c_int
-    lib.pctc_beam_select.argtypes = [ctypes.POINTER(BeamProblem)] + [vp] * 9
+    lib.pctc_beam_select.argtypes = [ctypes.POINTER(BeamProblem)] + [vp] * 9 + [ctypes.c_size_t, vp]
+    lib.pctc_beam_workspace_bytes.restype = ctypes.c_int
+    lib.pctc_beam_workspace_bytes.argtypes = [ctypes.POINTER(BeamProblem), size_p]
     lib.pctc_beam_reorder.restype = ctypes.c_int
     lib.pctc_beam_reorder.argtypes = [ctypes.c_int32, ctypes.POINTER(BeamState), ctypes.c_int32, ctypes.c_int32,
                                       ctypes.c_int32, vp, vp, vp]
@@ -491,7 +493,7 @@ def _native():
             raise RuntimeError("_marshal.so is missing: run paper_2609_33645_b200.build.build() first; "
                                "there is no fallback implementation") from e
         names = ("pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
-                 "pctc_beam_select", "pctc_beam_reorder", "pctc_prefix_advance", "pctc_prefix_read")
+                 "pctc_beam_workspace_bytes", "pctc_beam_select", "pctc_beam_reorder", "pctc_prefix_advance", "pctc_prefix_read")
         module.bind([ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in names], PctcError)
         _marshal = module
     return _marshal

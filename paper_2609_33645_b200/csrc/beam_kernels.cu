@@ -8,10 +8,11 @@
 // best maxima (K better ones stand against any other), so a few blocks are read again, from L2, and only there
 // single logits are compared.
 //
-// One cluster of CTAs takes one utterance: every CTA streams its share of the columns of all rows, the
-// shares' (maximum, sum of exponentials) meet in distributed shared memory, every CTA finds the candidates in
-// its own blocks, and the first one ranks them all.  One launch, no workspace.  Bound by HBM when there are many rows,
-// by latency when there are few.
+// Two launches.  k_beam_stream makes the pass: short CTAs of 4 warps, each for a stretch of one row, in any order and
+// on any SM.  k_beam_select then needs the maxima only: one CTA of 16 warps an utterance (a cluster of up to 8 where they
+// are many), which find the blocks that matter, read those, and rank the candidates.  A first version did both in one
+// launch of a cluster per utterance; its clusters left SMs idle and all had their tails at the same time (64 x 8 x
+// 151,936 bf16: 55 us against 42, floor 24; 2 x 8: 24.5 against 15.3; 1 x 4 fp32: 14.4 against 13.3).
 //
 // Exponentials and their sums within a thread are fp32, of differences from a running maximum (so that
 // their errors are relative to the difference, not to the logit); everything after that, and every comparison
@@ -32,15 +33,16 @@ namespace pctc {
 namespace {
 
 constexpr int SEL_MAX = 32;                       // beams in and out
-constexpr int SEL_MAX_WARPS = 16;                 // of a CTA: 16 where the utterances leave SMs over, else 8
-constexpr int SEL_MAX_CLUSTER = 16;
+constexpr int SEL_WARPS = 16, SEL_THREADS = SEL_WARPS * 32;
+constexpr int SEL_MAX_CLUSTER = 8;
+constexpr int STREAM_WARPS = 4;
+constexpr int STREAM_CTAS = 592;                  // CTAs of the first launch that are worth shorter stretches
 constexpr int SEL_BLOCK = 512;                    // logits per maximum: 16 a lane
 constexpr int SEL_LANE = SEL_BLOCK / 32;
 constexpr int SEL_MAX_BLOCKS = 512;               // blocks a CTA reads again
 constexpr int SEL_MAX_CAND = 1280;
 constexpr long long SEL_MAX_V = 1 << 21;
-constexpr int SEL_MAX_DYN = SEL_MAX * (int)(SEL_MAX_V / SEL_BLOCK) / 8 * 4;      // maxima, at 8 CTAs a cluster
-
+constexpr int SEL_MAX_DYN = SEL_MAX * (int)(SEL_MAX_V / SEL_BLOCK) / SEL_MAX_CLUSTER * 4;   // maxima of a CTA
 struct SelArgs {
   const void* logits;
   long long stride_n, stride_b;                   // elements
@@ -51,6 +53,11 @@ struct SelArgs {
   int *parents, *tokens;
   unsigned char* finished_out;
   int* flags;
+  // what the first launch leaves for the second, by row (utterance, beam)
+  float* maxima;                                  // [N * B, nb]
+  float* part_m;                                  // [N * B, parts]: reference and sum of exponentials of each CTA's stretch
+  double* part_s;
+  int parts, per;                                 // CTAs a row, blocks a warp
 };
 
 struct Cand {
@@ -192,23 +199,42 @@ struct Block<T, false> {
   }
 };
 
+// Running sum of exponentials of a lane.  It refers to `ref`, not to the running maximum: that is followed only when
+// it is 40 ahead, far from where exp overflows, so that no block waits for its maximum.
+struct RunningSum {
+  float ref, sum;
+  __device__ __forceinline__ void clear() { ref = -CUDART_INF_F; sum = 0.f; }
+  // adds a lane's share of a block; m: the block's maximum
+  __device__ __forceinline__ void add(const float (&x)[SEL_LANE], float m) {
+    float t = lane_exp(x, ref == -CUDART_INF_F ? 0.f : ref);
+    if (!(m <= ref + 40.f)) {                     // the first block with anything in it (or a NaN), and rarely after
+      sum *= exp2_approx((ref - m) * 1.44269504f);
+      ref = m;
+      t = lane_exp(x, m);
+    }
+    sum += t;
+  }
+  __device__ __forceinline__ double total() const {
+    double s = sum;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+  }
+};
+
 struct SelShared {
   float score[SEL_MAX];
   unsigned char kind[SEL_MAX];                    // 0 dead, 1 live, 2 ended
   int rows[SEL_MAX];                              // the live rows, ascending
   int nlive, bad;
-  float part_m[SEL_MAX_WARPS][SEL_MAX];           // per warp and live row: reference and sum of exponentials
-  double part_s[SEL_MAX_WARPS][SEL_MAX];
-  float row_m[SEL_MAX_CLUSTER][SEL_MAX];          // per CTA of the cluster and live row
-  double row_s[SEL_MAX_CLUSTER][SEL_MAX];
   double lse[SEL_MAX];                            // by row; NaN: the row gives no candidates
   double group[32];
   double bound[SEL_MAX_CLUSTER];                  // per CTA: K of its candidates reach this score
-  int warp_count[SEL_MAX_WARPS];
+  int warp_count[SEL_WARPS];
   int nblocks, nequal, ncand, overflow;
   int blocks[SEL_MAX_BLOCKS];
   Cand cand[SEL_MAX_CAND];
-  Cand best[SEL_MAX_WARPS];
+  Cand best[SEL_WARPS];
 };
 
 // (reference, sum) pairs of the lanes of a warp joined: m the largest, s = sum_i s_i exp(m_i - m), in 64 bits.
@@ -231,7 +257,7 @@ __device__ __forceinline__ Cand candidate(const SelShared& sh, const T* base, lo
 
 // The K best by K passes over all candidates, each for the best one behind the last: for inputs whose ties or
 // order leave more candidates than the lists hold.  Called by all threads of one CTA.
-template <typename T, int WARPS>
+template <typename T>
 __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   Cand last{CUDART_INF, 0};
@@ -241,7 +267,7 @@ __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base)
     for (int i = 0; i < sh.nlive; ++i) {
       const int b = sh.rows[i];
       if (isnan(sh.lse[b])) continue;
-      for (int v = tid; v < a.V; v += WARPS * 32) {
+      for (int v = tid; v < a.V; v += SEL_THREADS) {
         const Cand c = candidate(sh, base, a.stride_b, b, v);
         if (c.score > -CUDART_INF && before(last, c) && before(c, best)) best = c;
       }
@@ -258,7 +284,7 @@ __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base)
     if (lane == 0) sh.best[warp] = best;
     __syncthreads();
     best = sh.best[0];
-    for (int w = 1; w < WARPS; ++w)
+    for (int w = 1; w < SEL_WARPS; ++w)
       if (before(sh.best[w], best)) best = sh.best[w];
     if (best.score == -CUDART_INF) break;
     if (tid == 0) sh.cand[k] = best;
@@ -270,9 +296,59 @@ __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base)
   __syncthreads();
 }
 
-template <typename T, bool VEC, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const SelArgs a) {
-  constexpr int THREADS = WARPS * 32;
+// The pass over the logits: a CTA takes 4 * per blocks of one row.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(STREAM_WARPS * 32, 8) k_beam_stream(const SelArgs a) {
+  __shared__ float sh_m[STREAM_WARPS];
+  __shared__ double sh_s[STREAM_WARPS];
+  const int row = blockIdx.x / a.parts, seg = blockIdx.x - row * a.parts;
+  const int n = row / a.B, b = row - n * a.B, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g0 = (seg * STREAM_WARPS + warp) * a.per, count = min(a.per, a.nb - g0);
+  float* maxima = a.maxima + (long long)row * a.nb + g0;
+  const T* p = (const T*)a.logits + n * a.stride_n + b * a.stride_b + (long long)g0 * SEL_BLOCK;
+  const int left = a.V - g0 * SEL_BLOCK;          // logits from p on
+  constexpr int AHEAD = VEC && sizeof(T) == 2 ? 2 : 1;      // blocks in flight: 2 KB a warp, 64 KB an SM
+  Block<T, VEC> ring[AHEAD];
+  auto fetch = [&](Block<T, VEC>& o, int i) {
+    if (i >= count) return;
+    if (left - i * SEL_BLOCK >= SEL_BLOCK) o.load(p + i * SEL_BLOCK + Block<T, VEC>::first(lane));
+    else o.load_part(p + i * SEL_BLOCK, left - i * SEL_BLOCK, lane);
+  };
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) fetch(ring[u], u);
+  // not waited for before the first loads: a dead or ended beam's logits count for nothing
+  if (!isfinite(a.scores[row]) || (a.finished && a.finished[row])) return;
+  RunningSum sum;
+  sum.clear();
+  for (int i0 = 0; i0 < count; i0 += AHEAD) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (u && i0 + u >= count) break;
+      float x[SEL_LANE];
+      ring[u].get(x);
+      fetch(ring[u], i0 + u + AHEAD);
+      const float m = warp_max(lane_max(x));
+      if (lane == 0) maxima[i0 + u] = m;
+      sum.add(x, m);
+    }
+  }
+  const double s = sum.total();
+  if (lane == 0) { sh_m[warp] = sum.ref; sh_s[warp] = s; }
+  __syncthreads();
+  if (warp == 0) {
+    float m = lane < STREAM_WARPS ? sh_m[lane] : -CUDART_INF_F;
+    double t = lane < STREAM_WARPS ? sh_s[lane] : 0.0;
+    join(m, t);
+    if (lane == 0) {
+      a.part_m[(long long)row * a.parts + seg] = m;
+      a.part_s[(long long)row * a.parts + seg] = t;
+    }
+  }
+}
+
+// Finds and ranks the candidates, from maxima and sums.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a) {
   __shared__ SelShared sh;
   extern __shared__ float bmax[];                 // [live rows][blocks of this CTA]
   cg::cluster_group cluster = cg::this_cluster();
@@ -281,11 +357,12 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const Se
   const int n = blockIdx.x / C;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const T* base = (const T*)a.logits + n * a.stride_n;
+  const long long row0 = (long long)n * a.B;
   const int b0 = (int)((long long)a.nb * c / C), b1 = (int)((long long)a.nb * (c + 1) / C), nbl = b1 - b0;
 
   if (warp == 0) {
-    const float s = lane < a.B ? a.scores[n * a.B + lane] : -CUDART_INF_F;
-    const bool done = lane < a.B && a.finished && a.finished[n * a.B + lane];
+    const float s = lane < a.B ? a.scores[row0 + lane] : -CUDART_INF_F;
+    const bool done = lane < a.B && a.finished && a.finished[row0 + lane];
     const int kind = !isfinite(s) ? 0 : done ? 2 : 1;
     const unsigned live = __ballot_sync(0xffffffffu, kind == 1);
     const unsigned bad = __ballot_sync(0xffffffffu, isnan(s) || s == CUDART_INF_F);
@@ -300,104 +377,33 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const Se
       sh.nblocks = sh.nequal = sh.ncand = sh.overflow = 0;
     }
   }
-  for (int i = tid; i < WARPS * SEL_MAX; i += THREADS) {
-    (&sh.part_m[0][0])[i] = -CUDART_INF_F;
-    (&sh.part_s[0][0])[i] = 0.0;
-  }
-  __syncthreads();
-
-  // ---- one pass over this CTA's columns of all live rows ----
-  // A warp takes the same columns of every row, so that equal rows have equal sums, bit for bit, and their
-  // candidates tie.
-  const int items = sh.nlive * nbl;
-  {
-    const int w0 = nbl * warp / WARPS, per_row = nbl * (warp + 1) / WARPS - w0;
-    const int steps = sh.nlive * per_row;
-    const int v0 = (b0 + w0) * SEL_BLOCK;
-    const bool part = per_row && (b0 + w0 + per_row) * SEL_BLOCK > a.V;      // the last block of a row is not whole
-    // AHEAD blocks a warp are in flight.  Sums refer to `ref`, not to the running maximum: it follows the maximum only
-    // when that is 40 ahead, far from where exp overflows, so that no block waits for its maximum.
-    constexpr int AHEAD = VEC && sizeof(T) == 2 ? 2 : 1;
-    Block<T, VEC> ring[AHEAD];
-    int fetched = 0, fr = 0, fleft = 0;           // of the fetches: the next row, and the blocks left in this one
-    const T* fp = nullptr;
-    auto fetch = [&](Block<T, VEC>& o) {
-      if (fetched >= steps) return;
-      if (fleft == 0) {
-        fp = base + sh.rows[fr] * a.stride_b + v0 + Block<T, VEC>::first(lane);
-        fleft = per_row;
-        ++fr;
-      }
-      if (part && fleft == 1) {
-        const int at = v0 + (per_row - 1) * SEL_BLOCK;
-        o.load_part(base + sh.rows[fr - 1] * a.stride_b + at, a.V - at, lane);
-      } else {
-        o.load(fp);
-      }
-      fp += SEL_BLOCK;
-      --fleft;
-      ++fetched;
-    };
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) fetch(ring[u]);
-    int r = 0, left = per_row;
-    float* maxima = bmax + w0;
-    float ref = -CUDART_INF_F, sum = 0.f;
-    for (int it = 0; it < steps; it += AHEAD) {
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        if (u && it + u >= steps) break;
-        float x[SEL_LANE];
-        ring[u].get(x);
-        fetch(ring[u]);
-        const float m = warp_max(lane_max(x));
-        if (lane == 0) *maxima = m;
-        ++maxima;
-        float t = lane_exp(x, ref == -CUDART_INF_F ? 0.f : ref);
-        if (!(m <= ref + 40.f)) {                 // the first block of a row with anything in it, and rarely after
-          sum *= exp2_approx((ref - m) * 1.44269504f);
-          ref = m;
-          t = lane_exp(x, m);
-        }
-        sum += t;
-        if (--left == 0) {                        // the row ends for this warp
-          double s = sum;
-#pragma unroll
-          for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-          if (lane == 0) { sh.part_m[warp][r] = ref; sh.part_s[warp][r] = s; }
-          ref = -CUDART_INF_F;
-          sum = 0.f;
-          left = per_row;
-          ++r;
-          maxima = bmax + r * nbl + w0;
-        }
-      }
+  // sums of all rows, those of dead and ended beams (which nothing was written for) among them: nobody looks at these
+  for (int b = warp; b < a.B; b += SEL_WARPS) {
+    float m = -CUDART_INF_F;
+    double s = 0.0;
+    for (int i = lane; i < a.parts; i += 32) {
+      const float pm = a.part_m[(row0 + b) * a.parts + i];
+      const double ps = a.part_s[(row0 + b) * a.parts + i];
+      const float nm = fmaxf(m, pm);
+      s = (s == 0.0 || m == nm ? s : s * exp((double)m - (double)nm)) + (ps == 0.0 || pm == nm ? ps : ps * exp((double)pm - (double)nm));
+      m = nm;
     }
-  }
-  __syncthreads();
-  // every CTA tells all others its part of every row: what follows reads its own shared memory only
-  cluster.barrier_wait(std::move(started));
-  for (int r = warp; r < sh.nlive; r += WARPS) {
-    float m = lane < WARPS ? sh.part_m[lane][r] : -CUDART_INF_F;
-    double s = lane < WARPS ? sh.part_s[lane][r] : 0.0;
-    join(m, s);
-    if (lane < C) {
-      SelShared* other = cluster.map_shared_rank(&sh, lane);
-      other->row_m[c][r] = m;
-      other->row_s[c][r] = s;
-    }
-  }
-  cluster.sync();
-  for (int r = warp; r < sh.nlive; r += WARPS) {
-    float m = lane < C ? sh.row_m[lane][r] : -CUDART_INF_F;
-    double s = lane < C ? sh.row_s[lane][r] : 0.0;
     join(m, s);
     // nothing allowed, or a NaN or +inf among the logits: no candidates
     const double lse = (double)m + log(s);
-    const bool fine = isfinite(lse);
-    if (lane == 0) {
-      sh.lse[sh.rows[r]] = fine ? lse : CUDART_NAN;
-      if (isnan(s) || m == CUDART_INF_F) atomicOr(&sh.bad, 1);
+    if (lane == 0) sh.lse[b] = isnan(s) || m == CUDART_INF_F ? CUDART_INF : isfinite(lse) ? lse : CUDART_NAN;
+  }
+  __syncthreads();
+  const int items = sh.nlive * nbl;
+  for (int e = tid; e < items; e += SEL_THREADS) {
+    const int r = e / nbl;
+    bmax[e] = a.maxima[(row0 + sh.rows[r]) * a.nb + b0 + e - r * nbl];
+  }
+  if (tid < sh.nlive) {
+    const int b = sh.rows[tid];
+    if (sh.lse[b] == CUDART_INF) {
+      sh.lse[b] = CUDART_NAN;
+      atomicOr(&sh.bad, 1);
     }
   }
   __syncthreads();
@@ -409,13 +415,14 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const Se
     const double s = (double)sh.score[b] + ((double)bmax[e] - sh.lse[b]);
     return isnan(s) ? -CUDART_INF : s;
   };
-  constexpr int PER = THREADS / 32;               // group g: the blocks e with e % 32 == g, PER threads each
+  constexpr int PER = SEL_THREADS / 32;               // group g: the blocks e with e % 32 == g, PER threads each
   double top = -CUDART_INF;
-  for (int e = (tid % PER) * 32 + tid / PER; e < items; e += THREADS) top = fmax(top, block_score(e));
+  for (int e = (tid % PER) * 32 + tid / PER; e < items; e += SEL_THREADS) top = fmax(top, block_score(e));
 #pragma unroll
   for (int o = PER / 2; o; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
   if (tid % PER == 0) sh.group[tid / PER] = top;
   __syncthreads();
+  cluster.barrier_wait(std::move(started));
   if (warp == 0) {
     const double mine = sh.group[lane];
     int rank = 0;
@@ -431,7 +438,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const Se
   cluster.sync();
   double thr = sh.bound[0];
   for (int o = 1; o < C; ++o) thr = fmax(thr, sh.bound[o]);
-  for (int e = tid; e < items; e += THREADS) {
+  for (int e = tid; e < items; e += SEL_THREADS) {
     const double s = block_score(e);
     if (s > -CUDART_INF && s >= thr) {
       if (s == thr) atomicAdd(&sh.nequal, 1);
@@ -444,7 +451,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const Se
     __syncthreads();
     if (tid == 0) sh.nblocks = 0;
     int equal = 0;
-    for (int e0 = 0; e0 < items; e0 += THREADS) {
+    for (int e0 = 0; e0 < items; e0 += SEL_THREADS) {
       const int e = e0 + tid;
       const double s = e < items ? block_score(e) : -CUDART_INF;
       const bool some = s > -CUDART_INF;
@@ -452,7 +459,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const Se
       if (lane == 0) sh.warp_count[warp] = __popc(eq);
       __syncthreads();
       int prior = equal, all = equal;
-      for (int w = 0; w < WARPS; ++w) {
+      for (int w = 0; w < SEL_WARPS; ++w) {
         if (w < warp) prior += sh.warp_count[w];
         all += sh.warp_count[w];
       }
@@ -472,7 +479,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const Se
     if (p < SEL_MAX_CAND) head->cand[p] = Cand{score, (unsigned long long)b << 32 | (unsigned)v};
   };
   const int nblk = sh.nblocks < SEL_MAX_BLOCKS ? sh.nblocks : SEL_MAX_BLOCKS;
-  for (int i = warp; i < nblk; i += WARPS) {
+  for (int i = warp; i < nblk; i += SEL_WARPS) {
     const int e = sh.blocks[i], r = e / nbl, b = sh.rows[r], v0 = (b0 + e - r * nbl) * SEL_BLOCK;
     Block<T, VEC> raw;
     const T* p = base + b * a.stride_b + v0;
@@ -520,7 +527,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const Se
   // ---- the first CTA ranks what all have found ----
   if (tid < a.B && sh.kind[tid] == 2) found(sh.score[tid], tid, a.eos);
   __syncthreads();
-  if (sh.overflow || sh.ncand > SEL_MAX_CAND) select_by_passes<T, WARPS>(sh, a, base);
+  if (sh.overflow || sh.ncand > SEL_MAX_CAND) select_by_passes<T>(sh, a, base);
   const int nc = sh.ncand;
   auto put = [&](int k, double score, int parent, int token) {
     const int o = n * a.K + k;
@@ -529,14 +536,14 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) k_beam_select(const Se
     a.tokens[o] = token;
     if (a.finished_out) a.finished_out[o] = parent >= 0 && (sh.kind[parent] == 2 || token == a.eos);
   };
-  for (int i = tid; i < nc; i += THREADS) {
+  for (int i = tid; i < nc; i += SEL_THREADS) {
     const Cand x = sh.cand[i];
     int rank = 0;
 #pragma unroll 8
     for (int j = 0; j < nc; ++j) rank += before(sh.cand[j], x);
     if (rank < a.K) put(rank, x.score, (int)(x.at >> 32), (int)(unsigned)x.at);
   }
-  for (int k = nc + tid; k < a.K; k += THREADS) put(k, -CUDART_INF, -1, -1);
+  for (int k = nc + tid; k < a.K; k += SEL_THREADS) put(k, -CUDART_INF, -1, -1);
   if (tid == 0 && a.flags) a.flags[n] = sh.bad ? PCTC_UTT_NONFINITE : 0;
 }
 
@@ -547,25 +554,45 @@ pctc_status_t check(const pctc_beam_t* p) {
   if (p->B > SEL_MAX || p->K > SEL_MAX || p->V > SEL_MAX_V) return PCTC_ERR_UNSUPPORTED;
   if (p->eos_id < -1 || (long long)p->eos_id >= p->V) return PCTC_ERR_INVALID_ARG;
   if (p->stride_b < p->V || p->stride_n < 0) return PCTC_ERR_INVALID_ARG;
+  if ((long long)p->N * p->B * ((p->V + SEL_BLOCK - 1) / SEL_BLOCK) > 0x3fffffffLL) return PCTC_ERR_UNSUPPORTED;
   if ((long long)p->N * SEL_MAX > 0x3fffffffLL) return PCTC_ERR_UNSUPPORTED;
   return PCTC_OK;
 }
 
-template <typename T, bool VEC, int WARPS>
-cudaError_t launch_select(const SelArgs& a, int C, cudaStream_t stream) {
+struct SelWorkspace {
+  size_t o_part_m, o_part_s, total;
+  int nb, parts, per;
+};
+SelWorkspace workspace_of(const pctc_beam_t* p) {
+  SelWorkspace w;
+  w.nb = (int)((p->V + SEL_BLOCK - 1) / SEL_BLOCK);
+  const size_t rows = (size_t)p->N * p->B;
+  w.per = 8;
+  do w.parts = (w.nb + STREAM_WARPS * w.per - 1) / (STREAM_WARPS * w.per);
+  while (rows * w.parts < STREAM_CTAS && w.per > 1 && (w.per /= 2));
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  w.o_part_m = up(rows * w.nb * 4);
+  w.o_part_s = w.o_part_m + up(rows * w.parts * 4);
+  w.total = w.o_part_s + up(rows * w.parts * 8);
+  return w;
+}
+
+template <typename T, bool VEC>
+cudaError_t launch_select(const SelArgs& a, cudaStream_t stream) {
+  k_beam_stream<T, VEC><<<a.N * a.B * a.parts, STREAM_WARPS * 32, 0, stream>>>(a);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  int C = 1;
+  while (C < SEL_MAX_CLUSTER && (long long)a.B * a.nb > 4096LL * C) C *= 2;
   const size_t dyn = (size_t)a.B * ((a.nb + C - 1) / C) * 4;
-  auto kern = k_beam_select<T, VEC, WARPS>;
+  auto kern = k_beam_select<T, VEC>;
   if (dyn + sizeof(SelShared) > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_MAX_DYN);
-    if (e != cudaSuccess) return e;
-  }
-  if (C > 8) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_MAX_DYN);
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.N * C);
-  cfg.blockDim = dim3(WARPS * 32);
+  cfg.blockDim = dim3(SEL_THREADS);
   cfg.dynamicSmemBytes = dyn;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -573,32 +600,8 @@ cudaError_t launch_select(const SelArgs& a, int C, cudaStream_t stream) {
   attr[0].val.clusterDim.x = C;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = C > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kern, a);
-}
-
-// How a call is spread over the device.  One wave: with 8 warps four CTAs fit on an SM, and a cluster is as large as
-// that allows, so that no utterance waits for another's tail.  Few utterances: clusters of 16 with 16 warps a CTA.  A
-// warp has a block of every row, unless the vocabulary is smaller than that.
-struct Spread {
-  int C, warps;
-};
-Spread spread(int N, int B, int nb) {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    sms = 148;
-  Spread s{1, 8};
-  auto maxima = [&](int C) { return (long long)B * ((nb + C - 1) / C) * 4; };
-  while (s.C < 16 && nb >= s.C * 2 * s.warps && (long long)N * s.C * 2 <= (s.C < 8 ? 4 : 1) * sms) s.C *= 2;
-  while (s.C < 8 && maxima(s.C) > 96 * 1024) s.C *= 2;      // the maxima have to fit shared memory
-  if ((long long)N * s.C <= sms && nb >= s.C * 16) s.warps = 16;
-  return s;
-}
-
-template <typename T, bool VEC>
-cudaError_t launch_select(const SelArgs& a, cudaStream_t stream) {
-  const Spread s = spread(a.N, a.B, a.nb);
-  return s.warps == 16 ? launch_select<T, VEC, 16>(a, s.C, stream) : launch_select<T, VEC, 8>(a, s.C, stream);
 }
 
 }  // namespace
@@ -608,11 +611,22 @@ using namespace pctc;
 
 extern "C" {
 
-pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const float* scores, const uint8_t* finished,
-                               float* scores_out, int32_t* parents, int32_t* tokens, uint8_t* finished_out,
-                               int32_t* utt_flags, void* stream_v) {
+pctc_status_t pctc_beam_workspace_bytes(const pctc_beam_t* p, size_t* bytes_out) {
   const pctc_status_t st = check(p);
   if (st != PCTC_OK) return st;
+  if (!bytes_out) return PCTC_ERR_INVALID_ARG;
+  *bytes_out = workspace_of(p).total;
+  return PCTC_OK;
+}
+
+pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const float* scores, const uint8_t* finished,
+                               float* scores_out, int32_t* parents, int32_t* tokens, uint8_t* finished_out,
+                               int32_t* utt_flags, void* workspace, size_t workspace_bytes, void* stream_v) {
+  const pctc_status_t st = check(p);
+  if (st != PCTC_OK) return st;
+  const SelWorkspace w = workspace_of(p);
+  if (!workspace || ((size_t)workspace & 255)) return PCTC_ERR_INVALID_ARG;
+  if (workspace_bytes < w.total) return PCTC_ERR_WORKSPACE_TOO_SMALL;
   if (!logits || !scores || !scores_out || !parents || !tokens) return PCTC_ERR_INVALID_ARG;
   if (finished && p->eos_id < 0) return PCTC_ERR_INVALID_ARG;
   const size_t es = p->dtype == PCTC_BF16 ? 2 : 4;
@@ -625,12 +639,17 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const f
   a.scores = scores;
   a.finished = finished;
   a.N = p->N; a.B = p->B; a.K = p->K; a.V = (int)p->V; a.eos = p->eos_id;
-  a.nb = (int)((p->V + SEL_BLOCK - 1) / SEL_BLOCK);
+  a.nb = w.nb;
   a.scores_out = scores_out;
   a.parents = parents;
   a.tokens = tokens;
   a.finished_out = finished_out;
   a.flags = utt_flags;
+  a.maxima = (float*)workspace;
+  a.part_m = (float*)((char*)workspace + w.o_part_m);
+  a.part_s = (double*)((char*)workspace + w.o_part_s);
+  a.parts = w.parts;
+  a.per = w.per;
   const bool vec = (((size_t)logits | (size_t)p->stride_n * es | (size_t)p->stride_b * es) & 15) == 0;
   cudaStream_t stream = (cudaStream_t)stream_v;
   const cudaError_t e = p->dtype == PCTC_BF16

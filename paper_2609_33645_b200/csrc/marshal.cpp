@@ -11,6 +11,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <vector>
 
@@ -23,6 +24,7 @@ struct {
   decltype(&pctc_clip_grad_norm) clip_grad_norm;
   decltype(&pctc_grad_sqsum) grad_sqsum;
   decltype(&pctc_grad_scale) grad_scale;
+  decltype(&pctc_beam_workspace_bytes) beam_workspace_bytes;
   decltype(&pctc_beam_select) beam_select;
   decltype(&pctc_beam_reorder) beam_reorder;
   decltype(&pctc_prefix_advance) prefix_advance;
@@ -80,6 +82,39 @@ double real(PyObject* o) {
 at::Tensor empty(at::IntArrayRef shape, at::ScalarType type, at::Device dev) {
   return at::empty(shape, at::TensorOptions().dtype(type).device(dev));
 }
+// Contiguous tensors that share one allocation: a decoding step's outputs cost the allocator one visit.
+class Shared {
+ public:
+  explicit Shared(at::Device dev) : dev_(dev) {}
+  size_t add(at::IntArrayRef shape, at::ScalarType type) {
+    int64_t n = 1;
+    for (const int64_t s : shape) n *= s;
+    parts_.push_back(Part{shape.vec(), type, bytes_});
+    bytes_ += ((int64_t)(n * c10::elementSize(type)) + 15) / 16 * 16;
+    return parts_.size() - 1;
+  }
+  void allocate() { base_ = empty({std::max<int64_t>(bytes_, 1)}, at::kByte, dev_); }
+  at::Tensor get(size_t i) const {
+    const Part& p = parts_[i];
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base_.storage()), base_.key_set(),
+                                                            c10::scalarTypeToTypeMeta(p.type));
+    t.unsafeGetTensorImpl()->set_storage_offset(base_.storage_offset() + p.at / (int64_t)c10::elementSize(p.type));
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(p.shape);
+    return t;
+  }
+
+ private:
+  struct Part {
+    std::vector<int64_t> shape;
+    at::ScalarType type;
+    int64_t at;
+  };
+  at::Device dev_;
+  std::vector<Part> parts_;
+  int64_t bytes_ = 0;
+  at::Tensor base_;
+};
+
 void* stream_of(at::Device dev) { return c10::cuda::getCurrentCUDAStream(dev.index()).stream(); }
 void* ptr(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 
@@ -230,12 +265,17 @@ PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
   p.dtype = x.scalar_type() == at::kFloat ? PCTC_FP32 : PCTC_BF16;
   p.eos_id = (int32_t)eos;
   const c10::cuda::CUDAGuard guard(dev);
-  const at::Tensor scores = empty({N, K}, at::kFloat, dev), parents = empty({N, K}, at::kInt, dev),
-                   tokens = empty({N, K}, at::kInt, dev), finished = empty({N, K}, at::kBool, dev),
-                   flags = empty({N}, at::kInt, dev);
+  Shared out(dev);
+  for (const at::ScalarType type : {at::kFloat, at::kInt, at::kInt, at::kBool}) out.add({N, K}, type);
+  out.add({N}, at::kInt);
+  out.allocate();
+  const at::Tensor scores = out.get(0), parents = out.get(1), tokens = out.get(2), finished = out.get(3), flags = out.get(4);
+  size_t need = 0;
+  check(api.beam_workspace_bytes(&p, &need), "pctc_beam_workspace_bytes");
+  const at::Tensor ws = need ? empty({(int64_t)need}, at::kByte, dev) : at::Tensor();
   check(api.beam_select(&p, ptr(x), (const float*)ptr(s), (const uint8_t*)ptr(f), (float*)ptr(scores),
                         (int32_t*)ptr(parents), (int32_t*)ptr(tokens), (uint8_t*)ptr(finished), (int32_t*)ptr(flags),
-                        stream_of(dev)),
+                        ptr(ws), need, stream_of(dev)),
         "pctc_beam_select");
   PyObject* d = PyDict_New();
   if (!d) return nullptr;
@@ -383,8 +423,13 @@ PyObject* prefix_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (width < 1 || width > INT32_MAX) fail(PyExc_ValueError, "max_tokens must be at least 1");
   const at::Device dev = state.device();
   const c10::cuda::CUDAGuard guard(dev);
-  const at::Tensor tokens = empty({p.N, p.beams, width}, at::kInt, dev), sizes = empty({p.N, p.beams}, at::kInt, dev),
-                   scores = empty({p.N, p.beams}, at::kFloat, dev), flags = empty({p.N}, at::kInt, dev);
+  Shared out(dev);
+  out.add({p.N, p.beams, width}, at::kInt);
+  out.add({p.N, p.beams}, at::kInt);
+  out.add({p.N, p.beams}, at::kFloat);
+  out.add({p.N}, at::kInt);
+  out.allocate();
+  const at::Tensor tokens = out.get(0), sizes = out.get(1), scores = out.get(2), flags = out.get(3);
   check(api.prefix_read(&p, ptr(state), (size_t)state.numel(), (int32_t*)ptr(tokens), (int32_t)width, (int32_t*)ptr(sizes),
                         (float*)ptr(scores), (int32_t*)ptr(flags), stream_of(dev)),
         "pctc_prefix_read");

@@ -39,12 +39,12 @@ def _problem(**kw):
 ])
 def test_bad_selections_are_refused_before_any_launch(lib, kw, want):
     p = _problem(**kw)
-    assert lib.load().pctc_beam_select(ctypes.byref(p), AT, AT, None, AT, AT, AT, None, None, None) == want
+    assert lib.load().pctc_beam_select(ctypes.byref(p), AT, AT, None, AT, AT, AT, None, None, AT, 1 << 20, None) == want
 
 
 def test_bad_pointers_are_refused_before_any_launch(lib):
     p, f = _problem(), lib.load().pctc_beam_select
-    good = [AT, AT, None, AT, AT, AT, None, None, None]
+    good = [AT, AT, None, AT, AT, AT, None, None, AT, 1 << 20, None]
     for i in (0, 1, 3, 4, 5):
         args = list(good)
         args[i] = None
@@ -55,6 +55,16 @@ def test_bad_pointers_are_refused_before_any_launch(lib):
     args[2] = AT                                            # ended beams without a token that ends
     assert f(ctypes.byref(p), *args) == 1
     assert f(None, *good) == 1
+    out = ctypes.c_size_t(1)
+    assert lib.load().pctc_beam_workspace_bytes(ctypes.byref(p), ctypes.byref(out)) == 0 and 0 < out.value < 1 << 20
+    assert lib.load().pctc_beam_workspace_bytes(ctypes.byref(p), None) == 1
+    p = _problem(N=64, B=8, V=151936, stride_n=8 * 151936, stride_b=151936)
+    assert lib.load().pctc_beam_workspace_bytes(ctypes.byref(p), ctypes.byref(out)) == 0 and out.value > 0
+    need = out.value
+    assert need < 64 * 8 * 151936 / 50                      # maxima and sums, not logits
+    assert f(ctypes.byref(p), *good[:8], None, need, None) == 1
+    assert f(ctypes.byref(p), *good[:8], AT + 8, need, None) == 1
+    assert f(ctypes.byref(p), *good[:8], AT, need - 1, None) == 2
 
 
 def test_binding_refuses_what_it_cannot_hand_on(lib):

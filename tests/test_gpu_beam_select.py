@@ -190,8 +190,11 @@ def test_scores_may_be_written_over():
     done = torch.zeros(3, 4, dtype=torch.bool, device=DEV)
     p = binding.BeamProblem(3, 4, 4, 20000, logits.stride(0), logits.stride(1), 0, 0)
     o = [torch.empty(3, 4, dtype=torch.int32, device=DEV) for _ in range(2)]
+    need = ctypes.c_size_t(0)
+    assert binding.load().pctc_beam_workspace_bytes(ctypes.byref(p), ctypes.byref(need)) == 0
+    ws = torch.empty(need.value, dtype=torch.uint8, device=DEV)
     st = binding.load().pctc_beam_select(ctypes.byref(p), logits.data_ptr(), scores.data_ptr(), done.data_ptr(),
                                          scores.data_ptr(), o[0].data_ptr(), o[1].data_ptr(), done.data_ptr(), None,
-                                         torch.cuda.current_stream().cuda_stream)
+                                         ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream)
     assert st == 0 and torch.equal(scores, want["scores"]) and torch.equal(o[0], want["parents"])
     assert torch.equal(o[1], want["tokens"]) and torch.equal(done, want["finished"])
