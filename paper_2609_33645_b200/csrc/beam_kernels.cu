@@ -673,8 +673,6 @@ namespace pctc {
 namespace {
 
 constexpr int MOVE_THREADS = 256;
-constexpr int MOVE_ROWS = 2;                      // 16-byte columns a thread works on at a time
-constexpr int MOVE_CTAS_PER_SM = 4;
 
 struct MoveState {
   const char* src;
@@ -696,59 +694,71 @@ struct MoveTable {
 constexpr int MOVE_SMALL = 32, MOVE_LARGE = 256;
 static_assert(sizeof(MoveTable<MOVE_LARGE>) <= 32000, "kernel parameters");
 
+// The parents of an utterance's slots: in registers, or, where 32 columns of 16 bytes need them all, in shared memory.
+template <int KB>
+struct Parents {
+  int p[KB];
+  __device__ __forceinline__ int operator[](int k) const { return p[k]; }
+};
+template <>
+struct Parents<32> {
+  const int* p;
+  __device__ __forceinline__ int operator[](int k) const { return p[k]; }
+};
+
 template <typename U, int KB>
-__device__ __forceinline__ void move_tile(const MoveState& s, const int* __restrict__ par, int K, long long bytes, int n,
-                                          int seg, int tile) {
+__device__ __forceinline__ void move_tile(const MoveState& s, const Parents<KB>& par, long long bytes, int n, int seg,
+                                          int tile) {
+  const long long at = ((long long)tile * MOVE_THREADS + threadIdx.x) * (int)sizeof(U);
+  if (at >= bytes) return;
   const bool in_place = s.src == s.dst;
-  const char* src = s.src + n * s.src_n + seg * s.seg;
-  char* dst = s.dst + n * s.dst_n + seg * s.seg;
-  const long long first = ((long long)tile * MOVE_ROWS * MOVE_THREADS + threadIdx.x) * (int)sizeof(U);
-#pragma unroll(KB <= 4 ? MOVE_ROWS : 1)          // a column of 8 beams or more is enough in flight
-  for (int q = 0; q < MOVE_ROWS; ++q) {
-    const long long at = first + (long long)q * MOVE_THREADS * (int)sizeof(U);
-    if (at >= bytes) return;
-    U v[KB];
+  const char* src = s.src + n * s.src_n + seg * s.seg + at;
+  char* dst = s.dst + n * s.dst_n + seg * s.seg + at;
+  U v[KB];
 #pragma unroll
-    for (int k = 0; k < KB; ++k)
-      if (k < K && par[k] >= 0 && !(in_place && par[k] == k)) v[k] = *(const U*)(src + par[k] * s.src_b + at);
+  for (int k = 0; k < KB; ++k)
+    if (par[k] >= 0 && !(in_place && par[k] == k)) v[k] = *(const U*)(src + par[k] * s.src_b);
 #pragma unroll
-    for (int k = 0; k < KB; ++k)
-      if (k < K && par[k] >= 0 && !(in_place && par[k] == k)) *(U*)(dst + k * s.dst_b + at) = v[k];
-  }
+  for (int k = 0; k < KB; ++k)
+    if (par[k] >= 0 && !(in_place && par[k] == k)) *(U*)(dst + k * s.dst_b) = v[k];
 }
 
 template <int LIM, int KB>
 __global__ void __launch_bounds__(MOVE_THREADS) k_beam_move(const __grid_constant__ MoveTable<LIM> tab,
                                                             const int* __restrict__ parents,
                                                             const int* __restrict__ lengths, int N, int B, int K) {
-  __shared__ int par[KB];
-  const int total = tab.tile0[tab.n];
-  for (int t = blockIdx.x; t < total; t += gridDim.x) {
-    int lo = 0, hi = tab.n - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (tab.tile0[mid] <= t) lo = mid; else hi = mid - 1;
-    }
-    const MoveState& s = tab.s[lo];
-    const int local = t - tab.tile0[lo];
-    const int tile = local % s.tiles, ns = local / s.tiles, seg = ns % s.segments, n = ns / s.segments;
-    int units = s.units;
-    if (s.timed) units = min(max(lengths[n], 0), units);
-    const long long bytes = units * s.unit;
-    if ((long long)tile * MOVE_ROWS * MOVE_THREADS * s.width >= bytes) continue;
-    __syncthreads();                              // the tile before has read its parents
-    if (threadIdx.x < K) {
-      const int p = parents[n * K + threadIdx.x];
-      par[threadIdx.x] = p >= 0 && p < B ? p : -1;
-    }
+  const int t = blockIdx.x;
+  int lo = 0, hi = tab.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (tab.tile0[mid] <= t) lo = mid; else hi = mid - 1;
+  }
+  const MoveState& s = tab.s[lo];
+  const int local = t - tab.tile0[lo];
+  const int ns = local / s.tiles, tile = local - ns * s.tiles, n = ns / s.segments, seg = ns - n * s.segments;
+  auto parent = [&](int k) {
+    const int p = k < K ? __ldg(parents + n * K + k) : -1;
+    return p >= 0 && p < B ? p : -1;
+  };
+  Parents<KB> par;
+  if constexpr (KB == 32) {
+    __shared__ int shared[KB];
+    if (threadIdx.x < KB) shared[threadIdx.x] = parent(threadIdx.x);
     __syncthreads();
-    switch (s.width) {
-      case 16: move_tile<uint4, KB>(s, par, K, bytes, n, seg, tile); break;
-      case 8: move_tile<uint2, KB>(s, par, K, bytes, n, seg, tile); break;
-      case 4: move_tile<unsigned, KB>(s, par, K, bytes, n, seg, tile); break;
-      case 2: move_tile<unsigned short, KB>(s, par, K, bytes, n, seg, tile); break;
-      default: move_tile<unsigned char, KB>(s, par, K, bytes, n, seg, tile); break;
-    }
+    par.p = shared;
+  } else {
+#pragma unroll
+    for (int k = 0; k < KB; ++k) par.p[k] = parent(k);
+  }
+  int units = s.units;
+  if (s.timed) units = min(max(__ldg(lengths + n), 0), units);
+  const long long bytes = units * s.unit;
+  switch (s.width) {
+    case 16: move_tile<uint4, KB>(s, par, bytes, n, seg, tile); break;
+    case 8: move_tile<uint2, KB>(s, par, bytes, n, seg, tile); break;
+    case 4: move_tile<unsigned, KB>(s, par, bytes, n, seg, tile); break;
+    case 2: move_tile<unsigned short, KB>(s, par, bytes, n, seg, tile); break;
+    default: move_tile<unsigned char, KB>(s, par, bytes, n, seg, tile); break;
   }
 }
 
@@ -826,11 +836,7 @@ pctc_status_t check_overlap(const pctc_beam_state_t* st, int n, int N, int B, in
 template <int LIM, int KB>
 cudaError_t launch_move(const MoveTable<LIM>& tab, const int* parents, const int* lengths, int N, int B, int K,
                         cudaStream_t stream) {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    sms = 148;
-  const int total = tab.tile0[tab.n], most = sms * MOVE_CTAS_PER_SM;
-  k_beam_move<LIM, KB><<<total < most ? total : most, MOVE_THREADS, 0, stream>>>(tab, parents, lengths, N, B, K);
+  k_beam_move<LIM, KB><<<tab.tile0[tab.n], MOVE_THREADS, 0, stream>>>(tab, parents, lengths, N, B, K);
   return cudaGetLastError();
 }
 
@@ -861,7 +867,7 @@ pctc_status_t move_all(const pctc_beam_state_t* st, int n, int N, int B, int K, 
       const size_t all = (size_t)m.src | (size_t)m.dst | (size_t)(m.src_n | m.src_b | m.dst_n | m.dst_b | m.seg | m.unit);
       m.width = 16;
       while (all & (size_t)(m.width - 1)) m.width /= 2;
-      const long long per = (long long)MOVE_ROWS * MOVE_THREADS * m.width, t = (len + per - 1) / per;
+      const long long per = (long long)MOVE_THREADS * m.width, t = (len + per - 1) / per;
       if (t > 0x7fffffffLL) return PCTC_ERR_UNSUPPORTED;
       m.tiles = (int)t;
       tab.tile0[tab.n++] = (int)tiles;
