@@ -68,8 +68,8 @@ __device__ __forceinline__ double round24(double p) {
 // (absent, impossible, the second of its kind, behind k) has class -2 and probability 0.
 template <int KM>
 struct Tile {
-  double p[PFX_TILE][KM];
-  int cls[PFX_TILE][KM];
+  __align__(16) double p[PFX_TILE][KM];
+  __align__(16) int cls[PFX_TILE][KM];
   double blank[PFX_TILE];
   double shift[PFX_TILE];
 };
@@ -124,6 +124,32 @@ __device__ __forceinline__ unsigned coarse(double x) {
   return h == 0 && x > 0.0 ? 1u : h;
 }
 
+// A lane's share of a frame: classes first, first + 1, ... (first a multiple of KP), and the blank.
+template <int KP>
+struct Share {
+  double p[KP], blank;
+  int cls[KP];
+  template <int KM>
+  __device__ __forceinline__ void load(const Tile<KM>& t, int f, int first) {
+    if constexpr (KP % 4 == 0) {
+#pragma unroll
+      for (int q = 0; q < KP; q += 4) {
+        const int4 c = *(const int4*)&t.cls[f][first + q];
+        cls[q] = c.x; cls[q + 1] = c.y; cls[q + 2] = c.z; cls[q + 3] = c.w;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < KP; ++q) cls[q] = t.cls[f][first + q];
+    }
+#pragma unroll
+    for (int q = 0; q < KP; q += 2) {
+      const double2 d = *(const double2*)&t.p[f][first + q];
+      p[q] = d.x; p[q + 1] = d.y;
+    }
+    blank = t.blank[f];
+  }
+};
+
 template <int KM, int BM>
 struct Search {                                   // what lanes hand each other within a frame
   // coarse keys: BM stays, then (at first) every slot's best extension, then the extensions that are ranked; 16 of padding
@@ -134,6 +160,7 @@ struct Search {                                   // what lanes hand each other 
   double slot_value[32];                          // by new slot
   int2 slot_from[32];
   unsigned taken[32];
+  __align__(16) unsigned grown[BM];               // lower words of the hashes of prefixes that have just been grown, else 0
 };
 
 // One CTA an utterance: warp 0 searches while the other warps stage the next frames.  The search is a chain of
@@ -211,23 +238,33 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
         stage<KM>(tiles[(t1 / PFX_TILE) & 1], min(Tn - t1, PFX_TILE), warp - 1, PFX_THREADS / 32 - 1,
                   cls_n + (size_t)t1 * k, lp_n + (size_t)t1 * k, k, blank, &flags);
     } else {
+      // the next frame's share is on its way while a frame is searched (where the registers allow)
+      constexpr bool PREFETCH = KP <= 8;
+      Share<KP> now;
+      if (PREFETCH) now.load(tile, 0, part * KP);
       for (int f = 0; f < nf; ++f) {
         const int frame = frames0 + t0 + f;
+        if (!PREFETCH) now.load(tile, f, part * KP);
+        const Share<KP> in = now;
+        if (PREFETCH && f + 1 < nf) now.load(tile, f + 1, part * KP);
         // ---- this lane's candidates: its slot's stay, and the slot grown by its share of the classes ----
         const double total = __dadd_rn(pb, pn);
         double v[KP];
         int jl = -1;
+        double pl = 0.0;                          // probability of this prefix's last label
 #pragma unroll
         for (int q = 0; q < KP; ++q) {
-          const int j = part * KP + q;
-          const bool same = tile.cls[f][j] == last;
-          if (same) jl = j;
-          v[q] = __dmul_rn(same ? pb : total, tile.p[f][j]);
+          const bool same = in.cls[q] == last;
+          if (same) { jl = part * KP + q; pl = in.p[q]; }
+          v[q] = __dmul_rn(same ? pb : total, in.p[q]);
         }
 #pragma unroll
-        for (int o = BM; o < 32; o *= 2) jl = max(jl, __shfl_xor_sync(ALL, jl, o));
-        const double pl = jl >= 0 ? tile.p[f][jl] : 0.0;
-        const double sb = __dmul_rn(total, tile.blank[f]);
+        for (int o = BM; o < 32; o *= 2) {
+          const int oj = __shfl_xor_sync(ALL, jl, o);
+          const double op = __shfl_xor_sync(ALL, pl, o);
+          if (oj > jl) { jl = oj; pl = op; }
+        }
+        const double sb = __dmul_rn(total, in.blank);
         double sn = __dmul_rn(pn, pl);
         const bool child = par >= 0 && jl >= 0 && total > 0.0;
         if (__any_sync(ALL, child)) {             // slot par grown by `last` is this slot's prefix
@@ -272,12 +309,13 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
             unsigned least;
             if (BM < 32) {
               const unsigned mine = lane < BM ? sk : best;
-              int above = 0;
+              int a0 = 0, a1 = 0, a2 = 0, a3 = 0;
 #pragma unroll
               for (int i = 0; i < BM / 2; ++i) {
                 const uint4 o = ((const uint4*)sh.key)[i];
-                above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+                a0 += o.x > mine; a1 += o.y > mine; a2 += o.z > mine; a3 += o.w > mine;
               }
+              const int above = a0 + a1 + a2 + a3;
               least = __reduce_min_sync(ALL, above < B ? mine : ALL);
             } else {
               int a0 = 0, a1 = 0;
@@ -307,7 +345,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
                 const int j = part * KP + q;
                 sh.key[BM + at] = coarse(v[q]);
                 sh.value[at] = v[q];
-                sh.from[at] = make_int2(32 + slot * 32 + j, tile.cls[f][j]);
+                sh.from[at] = make_int2(32 + slot * 32 + j, in.cls[q]);
                 ++at;
               }
             }
@@ -326,21 +364,22 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
             const bool ext = x >= BM && x < all;
             const double val = ext ? sh.value[e] : 0.0;
             const int2 src = ext ? sh.from[e] : make_int2(lane, 0);
-            int rank = 0;
+            int r0 = 0, r1 = 0, r2 = 0, r3 = 0;
             for (int y = 0; y < all; y += 16) {
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const uint4 o = *(const uint4*)&sh.key[y + 4 * i];
-                rank += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+                r0 += o.x > mine; r1 += o.y > mine; r2 += o.z > mine; r3 += o.w > mine;
               }
             }
-            count += __popc(__ballot_sync(ALL, mine > 0));
-            sum += __reduce_add_sync(ALL, mine > 0 ? (unsigned)rank : 0u);
+            const int rank = r0 + r1 + r2 + r3;
             if (mine > 0 && rank < B) {
               sh.slot_value[rank] = val;
               sh.slot_from[rank] = src;
               if (x < BM) place = rank;
             }
+            count += __popc(__ballot_sync(ALL, mine > 0));
+            sum += __reduce_add_sync(ALL, mine > 0 ? (unsigned)rank : 0u);
           }
           if (sum != count * (count - 1) / 2) {   // ties of upper words: all bits, and the order of equals
             if (part == 0) sh.stay[slot] = stay;
@@ -404,12 +443,26 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
           // a prefix that had left the beam and is back is the parent of slots that stayed
           const bool orphan = live && par < 0 && size > 0 && !grown;
           if (__any_sync(ALL, orphan)) {
-            unsigned fresh_slots = __ballot_sync(ALL, grown) & SLOTS;
-            while (fresh_slots) {
-              const int e = __ffs(fresh_slots) - 1;
-              fresh_slots &= fresh_slots - 1;
-              const unsigned long long h = __shfl_sync(ALL, hash, e);
-              if (orphan && h == up) par = e;
+            if (part == 0) sh.grown[slot] = grown ? (unsigned)hash : 0u;
+            __syncwarp();
+            const unsigned low = (unsigned)up;
+            int e = -1;
+#pragma unroll
+            for (int i = 0; i < BM; i += 4) {
+              const uint4 h = *(const uint4*)&sh.grown[i];
+              if (h.x == low) e = i;
+              if (h.y == low) e = i + 1;
+              if (h.z == low) e = i + 2;
+              if (h.w == low) e = i + 3;
+            }
+            if (__any_sync(ALL, orphan && e >= 0)) {      // all bits, one new prefix after the other
+              unsigned fresh_slots = __ballot_sync(ALL, grown) & SLOTS;
+              while (fresh_slots) {
+                e = __ffs(fresh_slots) - 1;
+                fresh_slots &= fresh_slots - 1;
+                const unsigned long long h = __shfl_sync(ALL, hash, e);
+                if (orphan && h == up) par = e;
+              }
             }
           }
         }
