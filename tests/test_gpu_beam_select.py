@@ -198,3 +198,47 @@ def test_scores_may_be_written_over():
                                          ws.data_ptr(), need.value, torch.cuda.current_stream().cuda_stream)
     assert st == 0 and torch.equal(scores, want["scores"]) and torch.equal(o[0], want["parents"])
     assert torch.equal(o[1], want["tokens"]) and torch.equal(done, want["finished"])
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_calls(seed):
+    """Sizes, types, alignment, dead, ended and masked beams in any mixture."""
+    rng = np.random.default_rng(seed)
+    N, B = int(rng.integers(1, 7)), int(rng.choice([1, 2, 3, 4, 7, 8, 16, 32]))
+    V = int(np.exp(rng.uniform(np.log(2), np.log(60000))))
+    K = int(rng.choice([1, B, 4, 32]))
+    dtype = torch.bfloat16 if rng.random() < 0.5 else torch.float32
+    logits, scores = make(N, B, V, dtype, seed, scale=float(rng.choice([0.5, 2.5, 8.0])), pad=int(rng.choice([0, 0, 1, 8, 64])))
+    if rng.random() < 0.3:                                  # a base address that is not a multiple of 16 bytes
+        buf = torch.zeros(N * B * V + 8, device=DEV, dtype=dtype)
+        shifted = buf[1:1 + N * B * V].view(N, B, V)
+        shifted.copy_(logits)
+        logits = shifted
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    if rng.random() < 0.4:
+        scores[torch.rand(N, B, generator=g, device=DEV) < 0.3] = -math.inf
+    finished = torch.rand(N, B, generator=g, device=DEV) < 0.25 if rng.random() < 0.5 else None
+    if rng.random() < 0.3:
+        logits.masked_fill_(torch.rand(V, generator=g, device=DEV) < rng.choice([0.1, 0.9, 0.999]), -math.inf)
+    if rng.random() < 0.15:
+        logits[N - 1, B - 1, V // 2] = math.nan
+    check(logits, scores, K, finished, int(rng.integers(0, V)) if finished is not None or rng.random() < 0.5 else None)
+
+
+def test_many_utterances():
+    logits, scores = make(700, 2, 1500, torch.bfloat16, 3)
+    check(logits, scores, 3)
+
+
+def test_equal_rows_tie():
+    """Rows with the same logits and score tie candidate by candidate, wherever their sums were computed."""
+    for dtype, V, pad in [(torch.float32, 100_003, 0), (torch.bfloat16, 151_936, 0), (torch.bfloat16, 30_001, 7)]:
+        logits, scores = make(2, 8, V, dtype, 11, pad=pad)
+        logits[:, 1:] = logits[:, :1]
+        scores[:, 1:] = scores[:, :1]
+        r = binding.beam_select(logits, scores, 8)
+        for n in range(2):
+            x = logits[n, 0].float().cpu().numpy()
+            best = np.argsort(-x, kind="stable")[:8]        # a row may hold its largest logit more than once
+            want = sorted(((-x[v], b, int(v)) for b in range(8) for v in best))[:8]
+            assert list(zip(r["parents"][n].tolist(), r["tokens"][n].tolist())) == [(b, v) for _, b, v in want]

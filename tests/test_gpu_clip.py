@@ -183,3 +183,86 @@ def test_gradients_of_the_head_are_clipped():
     assert float(c["norm"]) == pytest.approx(norm, rel=NORM_TOL) and norm > 0.5
     for x, w in zip(grads, want):
         close(x, w, x.dtype)
+
+
+@pytest.mark.parametrize("count", [48, 49, 192, 193, 512, 513, 1024, 1025, 2100])
+def test_lists_of_every_table_size(count):
+    for dtypes in ((torch.float32,), (torch.bfloat16, torch.float32)):
+        grads = make([1 + i % 37 for i in range(count)], dtypes, 0.5, count, offset=count % 3)
+        norm, want = reference([g.clone() for g in grads], 1.0)
+        r = binding.clip_grad_norm(grads, 1.0)
+        assert float(r["norm"]) == pytest.approx(norm, rel=NORM_TOL) and norm > 1.0
+        for g, w in zip(grads, want):
+            close(g, w, g.dtype)
+
+
+@pytest.mark.parametrize("offset", [0, 3])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_values(dtype, offset):
+    """Enough for a CTA a chunk in the second pass (32 MB and more), odd sizes, every kind of output."""
+    grads = make([17_000_001, 5, 12_345_677, 1], (dtype,), 0.01, 2, offset)
+    before = [g.clone() for g in grads]
+    norm, want = reference(before, 1.0)
+    for kind in ("same", "fp32", "shifted", "place"):
+        start = 1 if kind == "shifted" else offset
+        whole = [torch.full((g.numel() + 16,), 9.0, device=DEV, dtype=torch.float32 if kind == "fp32" else dtype) for g in grads]
+        outs = grads if kind == "place" else [o[start:start + g.numel()] for o, g in zip(whole, grads)]
+        r = binding.clip_grad_norm(grads, 1.0, out=None if kind == "place" else outs)
+        assert float(r["norm"]) == pytest.approx(norm, rel=NORM_TOL) and norm > 1.0
+        for x, w in zip(outs, want):
+            close(x, w, x.dtype)
+        if kind != "place":                                 # what lies around the outputs is left alone
+            for o, g in zip(whole, grads):
+                assert bool((o[:start] == 9.0).all()) and bool((o[start + g.numel():] == 9.0).all())
+
+
+def test_more_values_than_32_bits_count():
+    n = (1 << 31) + 4099
+    g = torch.zeros(n, device=DEV, dtype=torch.bfloat16)
+    at = [0, 5, (1 << 31) - 1, 1 << 31, n - 1]
+    for i in at:
+        g[i] = 2.0
+    r = binding.clip_grad_norm([g], 1.0)
+    assert float(r["norm"]) == pytest.approx(math.sqrt(20.0), rel=NORM_TOL)
+    want = 2.0 / (math.sqrt(20.0) + 1e-6)
+    for i in at:
+        assert abs(float(g[i]) - want) <= VALUE_TOL[torch.bfloat16] * want
+    assert float(g[1]) == 0.0 and float(g[n - 2]) == 0.0
+
+
+def test_capture_of_the_two_pass_form():
+    g = make([9_000_000, 33], (torch.float32,), 0.02, 9)
+    out = [torch.zeros_like(t) for t in g]
+    binding.clip_grad_norm(g, 1.0, out=out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = binding.clip_grad_norm(g, 1.0, out=out)
+    for t in g:
+        t.mul_(3.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    norm, want = reference(g, 1.0)
+    assert float(r["norm"]) == pytest.approx(norm, rel=NORM_TOL)
+    for o, w in zip(out, want):
+        close(o, w, o.dtype)
+
+
+def test_refusals_on_the_device():
+    g = torch.ones(64, device=DEV)
+    for grads, kw in [([g, g], {}), ([g, g[8:16]], {}), ([g[:32], g[16:48]], {}), ([g[:32]], dict(out=[g[8:40]]))]:
+        with pytest.raises(binding.PctcError):
+            binding.clip_grad_norm(grads, 1.0, **kw)
+    for grads, kw, match in [([g.double()], {}, "bf16 or fp32"), ([g.view(8, 8).t()], {}, "contiguous"),
+                             ([g, torch.ones(3)], {}, "one device"), ([g], dict(out=[]), "same shape"),
+                             ([g], dict(out=[g[:32]]), "same shape")]:
+        with pytest.raises(ValueError, match=match):
+            binding.clip_grad_norm(grads, 1.0, **kw)
+    for bad in (0.0, -1.0, math.nan):
+        with pytest.raises(binding.PctcError):
+            binding.clip_grad_norm([g], bad)
+    with pytest.raises(binding.PctcError):                  # bf16 gradients go to bf16 or fp32, fp32 ones to fp32
+        binding.clip_grad_norm([g], 1.0, out=[torch.empty(64, device=DEV, dtype=torch.bfloat16)])
+    assert bool((g == 1.0).all())
+    r = binding.clip_grad_norm([g, g[:0]], 100.0)           # an empty tensor is nothing
+    assert float(r["norm"]) == 8.0
+    assert float(binding.clip_grad_norm([g[:0]], 1.0)["norm"]) == 0.0

@@ -54,9 +54,9 @@ def run(classes, logprobs, lengths, blank, beams):
 @pytest.mark.parametrize("N,T,k,V,beams", [
     (1, 1, 1, 5, 1), (1, 1, 8, 50, 4), (2, 40, 1, 9, 4), (3, 40, 2, 4, 3), (2, 33, 8, 9, 1), (4, 65, 8, 12, 4),
     (2, 100, 8, 40, 16), (2, 50, 32, 40, 32), (1, 64, 5, 1000, 32), (2, 31, 7, 151936, 10), (1, 200, 4, 6, 8),
-    (2, 48, 32, 33, 2), (1, 60, 3, 4, 31),
+    (2, 48, 32, 33, 2), (1, 60, 3, 4, 31), (2, 40, 12, 30, 16), (1, 40, 9, 20, 9), (2, 64, 8, 9, 8), (1, 33, 8, 30, 17),
 ])
-@pytest.mark.parametrize("sharp", [0.3, 3.0])
+@pytest.mark.parametrize("sharp", [0.3, 3.0, 12.0])
 def test_against_the_oracle(N, T, k, V, beams, sharp):
     classes, logprobs = make(N, T, k, V, N * 1000 + T + k, sharp)
     lengths = [T] + [max(1, T - 7 * i - 1) for i in range(1, N)]
@@ -208,3 +208,45 @@ def test_with_the_head(dtype):
     one = binding.beam_decode(hidden, W, None, lengths, 0, 1, k=1)
     greedy = binding.greedy_decode(hidden, W, None, lengths, 0)
     assert torch.equal(one["tokens"][:, 0], greedy["tokens"]) and torch.equal(one["token_lengths"][:, 0], greedy["token_lengths"])
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_random_calls(seed):
+    """Sizes, confusable classes, absent and repeated entries and equal probabilities in any mixture."""
+    rng = np.random.default_rng(1000 + seed)
+    N, T = int(rng.integers(1, 4)), int(rng.integers(1, 90))
+    k, beams = int(rng.choice([1, 2, 3, 5, 8, 8, 13, 32])), int(rng.choice([1, 2, 4, 5, 8, 9, 16, 20, 32]))
+    V = k + int(rng.choice([1, 2, 5, 200]))
+    classes, logprobs = make(N, T, k, V, seed, float(rng.choice([0.2, 1.0, 4.0, 15.0])), int(rng.choice([1, 3, 9])))
+    if rng.random() < 0.4:
+        logprobs = np.round(logprobs * 2) / np.float32(2)   # many equal ones
+    if rng.random() < 0.4:
+        classes[rng.random(classes.shape) < 0.2] = -1
+    if rng.random() < 0.3:
+        classes[rng.random(classes.shape) < 0.2] = 1        # given twice
+    if rng.random() < 0.2:
+        logprobs[rng.random(logprobs.shape) < 0.02] = np.nan
+    lengths = [int(rng.integers(1, T + 1)) for _ in range(N)]
+    blank = int(rng.integers(0, 3))
+    check(run(classes, logprobs, lengths, blank, beams), classes, logprobs, lengths, blank, beams)
+
+
+def test_refusals_on_the_device():
+    c, l = torch.zeros(2, 5, 4, dtype=torch.int32, device=DEV), torch.zeros(2, 5, 4, device=DEV)
+    for kw, error in [(dict(lengths=[5, 6]), ValueError), (dict(lengths=[5, -1]), binding.PctcError),
+                      (dict(lengths=[5]), ValueError), (dict(beams=0), binding.PctcError), (dict(beams=33), binding.PctcError),
+                      (dict(blank=-1), binding.PctcError)]:
+        a = dict(lengths=[5, 5], beams=4, blank=0)
+        a.update(kw)
+        with pytest.raises(error):
+            binding.prefix_beam_decode(c, l, a["lengths"], a["blank"], a["beams"])
+    with pytest.raises(binding.PctcError):
+        binding.prefix_beam_decode(torch.zeros(1, 5, 33, dtype=torch.int32, device=DEV), torch.zeros(1, 5, 33, device=DEV), [5], 0, 4)
+    s = binding.PrefixBeam(2, 4, 9, 0, DEV)
+    with pytest.raises(ValueError, match="device"):
+        s.advance(c.cpu(), l.cpu())
+    s.advance(c, l)
+    with pytest.raises(ValueError, match="room"):
+        s.advance(c, l)
+    with pytest.raises(ValueError, match="max_tokens"):
+        s.read(max_tokens=0)
