@@ -228,7 +228,7 @@ struct SelShared {
   int rows[SEL_MAX];                              // the live rows, ascending
   int nlive, bad;
   double lse[SEL_MAX];                            // by row; NaN: the row gives no candidates
-  double group[32];
+  double top[SEL_WARPS][32];                      // per warp and group of blocks
   double bound[SEL_MAX_CLUSTER];                  // per CTA: K of its candidates reach this score
   int warp_count[SEL_WARPS];
   int nblocks, nequal, ncand, overflow;
@@ -360,92 +360,107 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
   const long long row0 = (long long)n * a.B;
   const int b0 = (int)((long long)a.nb * c / C), b1 = (int)((long long)a.nb * (c + 1) / C), nbl = b1 - b0;
 
+  // every warp looks at all beams' scores; warp 0 writes down what it finds
+  const float my_score = lane < a.B ? a.scores[row0 + lane] : -CUDART_INF_F;
+  const bool done = lane < a.B && a.finished && a.finished[row0 + lane];
+  const int kind = !isfinite(my_score) ? 0 : done ? 2 : 1;
+  const unsigned live = __ballot_sync(0xffffffffu, kind == 1);
+  const int nlive = __popc(live);
   if (warp == 0) {
-    const float s = lane < a.B ? a.scores[row0 + lane] : -CUDART_INF_F;
-    const bool done = lane < a.B && a.finished && a.finished[row0 + lane];
-    const int kind = !isfinite(s) ? 0 : done ? 2 : 1;
-    const unsigned live = __ballot_sync(0xffffffffu, kind == 1);
-    const unsigned bad = __ballot_sync(0xffffffffu, isnan(s) || s == CUDART_INF_F);
+    const unsigned bad = __ballot_sync(0xffffffffu, isnan(my_score) || my_score == CUDART_INF_F);
     if (lane < a.B) {
-      sh.score[lane] = s;
+      sh.score[lane] = my_score;
       sh.kind[lane] = (unsigned char)kind;
     }
     if (kind == 1) sh.rows[__popc(live & ((1u << lane) - 1))] = lane;
     if (lane == 0) {
-      sh.nlive = __popc(live);
+      sh.nlive = nlive;
       sh.bad = bad != 0;
       sh.nblocks = sh.nequal = sh.ncand = sh.overflow = 0;
     }
   }
-  // sums of all rows, those of dead and ended beams (which nothing was written for) among them: nobody looks at these
-  for (int b = warp; b < a.B; b += SEL_WARPS) {
+
+  // ---- a warp (few rows: several) a row: its maxima to shared memory, its log-sum-exp, and the best block in each of
+  // 32 groups ----
+  // Block e of the list [live rows][blocks of this CTA] belongs to group e % 32, which is a lane here.
+  int share = 1;                                  // warps a row
+  while (share < SEL_WARPS && share * 2 * nlive <= SEL_WARPS) share *= 2;
+  const int first_row = warp / share, row_step = SEL_WARPS / share, sub = warp % share;
+  double top = -CUDART_INF;
+  bool bad_row = false;
+  for (int r = first_row; r < nlive; r += row_step) {
+    const int b = (int)__fns(live, 0, r + 1);
+    const long long row = row0 + b;
+    float* mine = bmax + r * nbl;
+    const int i0 = ((lane - r * nbl) & 31) + 32 * sub;
+#pragma unroll 4
+    for (int i = i0; i < nbl; i += 32 * share) mine[i] = a.maxima[row * a.nb + b0 + i];
+    const float* pm = a.part_m + row * a.parts;
+    const double* ps = a.part_s + row * a.parts;
     float m = -CUDART_INF_F;
+#pragma unroll 2
+    for (int i = lane; i < a.parts; i += 32) m = fmaxf(m, pm[i]);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     double s = 0.0;
+#pragma unroll 2
     for (int i = lane; i < a.parts; i += 32) {
-      const float pm = a.part_m[(row0 + b) * a.parts + i];
-      const double ps = a.part_s[(row0 + b) * a.parts + i];
-      const float nm = fmaxf(m, pm);
-      s = (s == 0.0 || m == nm ? s : s * exp((double)m - (double)nm)) + (ps == 0.0 || pm == nm ? ps : ps * exp((double)pm - (double)nm));
-      m = nm;
+      const double t = ps[i];
+      s += t == 0.0 || pm[i] == m ? t : t * exp((double)pm[i] - (double)m);
     }
-    join(m, s);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     // nothing allowed, or a NaN or +inf among the logits: no candidates
     const double lse = (double)m + log(s);
-    if (lane == 0) sh.lse[b] = isnan(s) || m == CUDART_INF_F ? CUDART_INF : isfinite(lse) ? lse : CUDART_NAN;
+    const bool fine = isfinite(lse);
+    bad_row = bad_row || isnan(s) || m == CUDART_INF_F;
+    if (lane == 0 && sub == 0) sh.lse[b] = fine ? lse : CUDART_NAN;
+    const double score = __shfl_sync(0xffffffffu, my_score, b);
+    if (fine)
+#pragma unroll 4
+      for (int i = i0; i < nbl; i += 32 * share) top = fmax(top, score + ((double)mine[i] - lse));
   }
+  sh.top[warp][lane] = top;
   __syncthreads();
-  const int items = sh.nlive * nbl;
-  for (int e = tid; e < items; e += SEL_THREADS) {
-    const int r = e / nbl;
-    bmax[e] = a.maxima[(row0 + sh.rows[r]) * a.nb + b0 + e - r * nbl];
-  }
-  if (tid < sh.nlive) {
-    const int b = sh.rows[tid];
-    if (sh.lse[b] == CUDART_INF) {
-      sh.lse[b] = CUDART_NAN;
-      atomicOr(&sh.bad, 1);
-    }
-  }
-  __syncthreads();
+  if (bad_row && lane == 0) atomicOr(&sh.bad, 1);
+  const int items = nlive * nbl;
 
-  // ---- the blocks that can hold one of the K best: those that reach the K-th best of 32 groups' maxima, of the CTA
+  // ---- the blocks that can hold one of the K best: those that reach the K-th best of the groups' maxima, of the CTA
   // of the cluster where that is highest ----
-  auto block_score = [&](int e) {
-    const int r = e / nbl, b = sh.rows[r];
-    const double s = (double)sh.score[b] + ((double)bmax[e] - sh.lse[b]);
+  auto block_score = [&](int r, int i) {
+    const int b = sh.rows[r];
+    const double s = (double)sh.score[b] + ((double)bmax[r * nbl + i] - sh.lse[b]);
     return isnan(s) ? -CUDART_INF : s;
   };
-  constexpr int PER = SEL_THREADS / 32;               // group g: the blocks e with e % 32 == g, PER threads each
-  double top = -CUDART_INF;
-  for (int e = (tid % PER) * 32 + tid / PER; e < items; e += SEL_THREADS) top = fmax(top, block_score(e));
-#pragma unroll
-  for (int o = PER / 2; o; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (tid % PER == 0) sh.group[tid / PER] = top;
-  __syncthreads();
   cluster.barrier_wait(std::move(started));
   if (warp == 0) {
-    const double mine = sh.group[lane];
+#pragma unroll
+    for (int w = 1; w < SEL_WARPS; ++w) top = fmax(top, sh.top[w][lane]);
+    sh.top[0][lane] = top;
+    __syncwarp();
     int rank = 0;
 #pragma unroll 8
     for (int i = 0; i < 32; ++i) {
-      const double o = sh.group[i];
-      rank += o > mine || (o == mine && i < lane);
+      const double o = sh.top[0][i];
+      rank += o > top || (o == top && i < lane);
     }
     const unsigned kth = __ballot_sync(0xffffffffu, rank == a.K - 1);
-    const double bound = __shfl_sync(0xffffffffu, mine, __ffs(kth) - 1);
+    const double bound = __shfl_sync(0xffffffffu, top, __ffs(kth) - 1);
     if (lane < C) cluster.map_shared_rank(&sh, lane)->bound[c] = bound;
   }
   cluster.sync();
   double thr = sh.bound[0];
   for (int o = 1; o < C; ++o) thr = fmax(thr, sh.bound[o]);
-  for (int e = tid; e < items; e += SEL_THREADS) {
-    const double s = block_score(e);
-    if (s > -CUDART_INF && s >= thr) {
-      if (s == thr) atomicAdd(&sh.nequal, 1);
-      const int p = atomicAdd(&sh.nblocks, 1);
-      if (p < SEL_MAX_BLOCKS) sh.blocks[p] = e;
+  for (int r = first_row; r < nlive; r += row_step)
+#pragma unroll 4
+    for (int i = lane + 32 * sub; i < nbl; i += 32 * share) {
+      const double s = block_score(r, i);
+      if (s > -CUDART_INF && s >= thr) {
+        if (s == thr) atomicAdd(&sh.nequal, 1);
+        const int p = atomicAdd(&sh.nblocks, 1);
+        if (p < SEL_MAX_BLOCKS) sh.blocks[p] = r * nbl + i;
+      }
     }
-  }
   __syncthreads();
   if (sh.nequal > a.K || sh.nblocks > SEL_MAX_BLOCKS) {   // of the blocks that tie with the threshold the first K will do
     __syncthreads();
@@ -453,7 +468,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
     int equal = 0;
     for (int e0 = 0; e0 < items; e0 += SEL_THREADS) {
       const int e = e0 + tid;
-      const double s = e < items ? block_score(e) : -CUDART_INF;
+      const double s = e < items ? block_score(e / nbl, e % nbl) : -CUDART_INF;
       const bool some = s > -CUDART_INF;
       const unsigned eq = __ballot_sync(0xffffffffu, some && s == thr);
       if (lane == 0) sh.warp_count[warp] = __popc(eq);
