@@ -11,13 +11,20 @@
 // Two launches.  k_beam_stream makes the pass: short CTAs of 4 warps, each for a stretch of one row, in any order and
 // on any SM.  k_beam_select then needs the maxima only: one CTA of 16 warps an utterance (a cluster of up to 8 where they
 // are many), which find the blocks that matter, read those, and rank the candidates.  A first version did both in one
-// launch of a cluster per utterance; its clusters left SMs idle and all had their tails at the same time (64 x 8 x
-// 151,936 bf16: 55 us against 42, floor 24; 2 x 8: 24.5 against 15.3; 1 x 4 fp32: 14.4 against 13.3).
+// launch of a cluster per utterance; its clusters left SMs idle and all had their tails at the same time (utterances x
+// beams x 151,936: 64 x 8 bf16 55 us against 41, 2 x 8 bf16 24.5 against 13.0, 1 x 4 fp32 14.4 against 11.1).
+//
+// Measured: 64 x 8 x 151,936 bf16 with a tenth of the beams ended, 140 MB: 41 us (21 at the rate of a copy), of which the
+// stream takes 31 and the ranking 8 to 9; 1 x 4 fp32: 11 us, of which 3 and 7.  The stream is bound by no single thing:
+// special function unit 62% busy (16 exponentials a cycle and SM are hardly more than the 12 bf16 logits that HBM
+// delivers), issue slots 55%, HBM 68%.  More blocks in flight, more or fewer warps a CTA, and longer stretches measured
+// the same; a quarter of the exponentials as polynomials on the FMA pipe made the whole call 10% slower.  The ranking is a
+// chain of about ten dependent steps of 0.3 to 1 us each.
 //
 // Exponentials and their sums within a thread are fp32, of differences from a running maximum (so that
 // their errors are relative to the difference, not to the logit); everything after that, and every comparison
 // of candidates, is 64 bits: candidates of different beams are ordered by sums whose fp32 rounding
-// would be larger than their distance.
+// would be larger than their distance.  Scores are rounded to fp32 when they are stored.
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 
@@ -43,6 +50,7 @@ constexpr int SEL_MAX_BLOCKS = 512;               // blocks a CTA reads again
 constexpr int SEL_MAX_CAND = 1280;
 constexpr long long SEL_MAX_V = 1 << 21;
 constexpr int SEL_MAX_DYN = SEL_MAX * (int)(SEL_MAX_V / SEL_BLOCK) / SEL_MAX_CLUSTER * 4;   // maxima of a CTA
+
 struct SelArgs {
   const void* logits;
   long long stride_n, stride_b;                   // elements
@@ -684,6 +692,10 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const f
 // the same bytes of all beams of an utterance; a thread loads its 1 to 16 bytes of every parent before it
 // stores any.  So a parent that several beams share is read once, and in place needs no second buffer: nobody
 // else touches the column.  In place a beam that stays where it is moves nothing.
+// Bound by HBM.  A CTA takes one tile of 4 KB columns: a persistent grid of such tiles, whose CTAs drift apart, was slower
+// (16 caches [16, 8, 8, 151, 64] bf16: 83 us against 64; 12 caches [8, 4, 8, 2000, 64]: 252 against 194, 8 TB/s written
+// and read as seen by the caller, since shared parents are read once; 12 caches [8, 4, 8, 300, 64] in place with half of
+// the beams moving: 25 against 20).
 namespace pctc {
 namespace {
 

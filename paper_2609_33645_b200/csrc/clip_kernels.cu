@@ -7,6 +7,10 @@
 // CTA the same ones in the same order, so all agree on f) and scales.  In place with f = 1 the second
 // pass ends there: the usual step of a training run reads its gradients once and writes nothing.
 // Both are bound by HBM; the arithmetic is one multiply-add a value.
+//
+// Measured: 156M bf16 values into another buffer 145 us (three passes of 312 MB at the rate of a copy: 143; the last 64 MB
+// of the first pass are still in L2 for the second); 64M bf16 values in 384 tensors, in place below the limit, 28 us
+// (one pass: 20); 100,000 fp32 values in 7 tensors 8.7 us in one launch (5.5 in two, which cost the host 6 us more).
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 
