@@ -543,7 +543,9 @@ class PrefixBeam:
     `advance(classes, logprobs, lengths)` takes the next frames (classes [N,t,k] int32 and logprobs
     [N,t,k] fp32 as topk_decode gives them, any t; lengths: host integers, how many of the t count
     per utterance, None for all); `read()` returns the hypotheses so far.  The state lives in one device
-    buffer with room for max_frames frames an utterance.  Calls on one object belong on one stream.
+    buffer with room for max_frames frames an utterance.  Calls on one object belong on one stream.  An advance
+    that is captured into a CUDA graph replays with the lengths of its capture, and starts the search anew if it was
+    the first one; frames of replays are not counted here, but a state that is full still takes no more.
     """
 
     def __init__(self, N, beams, max_frames, blank_id, device):
@@ -551,6 +553,8 @@ class PrefixBeam:
 
         self.N, self.beams, self.max_frames, self.blank_id = int(N), int(beams), int(max_frames), int(blank_id)
         self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError("the state of a prefix search lives on a CUDA device")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         need = ctypes.c_size_t(0)

@@ -511,38 +511,33 @@ __global__ void __launch_bounds__(PFX_READ_THREADS) k_prefix_read(
     const char* __restrict__ states, const int2* __restrict__ nodes, int B, int max_frames, int stride,
     int* __restrict__ tokens, int* __restrict__ sizes, float* __restrict__ scores, int* __restrict__ flags) {
   __shared__ int2 window[PFX_WINDOW];
-  __shared__ int newest, oldest;
+  __shared__ int newest, oldest, size[PFX_MAX_BEAMS];
   const int n = blockIdx.x, tid = threadIdx.x;
   const PrefixState* st = (const PrefixState*)(states + (size_t)n * PFX_STATE_BYTES);
   const int2* my_nodes = nodes + (size_t)n * nodes_per_utt(B, max_frames);
   const bool valid = st->magic == PFX_MAGIC && st->beams == B && st->max_frames == max_frames;
   const int most = (int)nodes_per_utt(B, max_frames);
-  for (int b = 0; b < B; ++b) {
-    const bool live = valid && st->s.pb[b] + st->s.pn[b] > 0.0;
-    const int size = live ? st->s.size[b] : 0;
-    for (int i = size + tid; i < stride; i += PFX_READ_THREADS) tokens[((size_t)n * B + b) * stride + i] = -1;
-  }
   if (tid == 0) newest = 0;
   __syncthreads();
   int at = 0, node = 0;
   int* out = nullptr;
+  bool live = false;
   if (tid < B) {
     const double total = valid ? st->s.pb[tid] + st->s.pn[tid] : 0.0;
-    const bool live = total > 0.0;
+    live = total > 0.0;
     at = live ? st->s.size[tid] : 0;
     node = live ? st->s.node[tid] : 0;
     if (node < 0 || node >= most) node = 0;
     out = tokens + ((size_t)n * B + tid) * stride;
+    size[tid] = at;
     sizes[n * B + tid] = at;
     scores[n * B + tid] = live ? (float)(log(total) + st->power * 0.693147180559945309417 + st->shift) : -CUDART_INF_F;
     atomicMax(&newest, node);
   }
-  if (tid == 0 && flags) {
-    bool any = false;
-    for (int b = 0; b < B && valid; ++b) any = any || st->s.pb[b] + st->s.pn[b] > 0.0;
-    flags[n] = valid ? st->flags | (any ? 0 : PCTC_UTT_INFEASIBLE) : PCTC_UTT_STATE_FULL;
-  }
-  __syncthreads();
+  const bool any = __syncthreads_or(live);
+  if (tid == 0 && flags) flags[n] = valid ? st->flags | (any ? 0 : PCTC_UTT_INFEASIBLE) : PCTC_UTT_STATE_FULL;
+  for (int b = 0; b < B; ++b)
+    for (int i = size[b] + tid; i < stride; i += PFX_READ_THREADS) tokens[((size_t)n * B + b) * stride + i] = -1;
   for (int hi = newest + 1; hi > 1;) {            // nodes [lo, hi); node 0 is the empty prefix
     const int lo = max(1, hi - PFX_WINDOW);
     for (int i = tid; i < hi - lo; i += PFX_READ_THREADS) window[i] = my_nodes[lo + i];

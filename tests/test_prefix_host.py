@@ -108,3 +108,7 @@ def test_binding_refuses_before_it_calls(lib):
         s.advance(c, l)
     with pytest.raises(ValueError, match="no frames"):
         s.read()
+    with pytest.raises(ValueError, match="CUDA device"):
+        binding.PrefixBeam(2, 4, 9, 0, "cpu")
+    with pytest.raises(ValueError, match="CUDA device"):
+        binding.prefix_beam_decode(c, l, [5, 5], 0, 4)
