@@ -334,6 +334,14 @@ pctc_status_t pctc_prefix_advance(const pctc_prefix_t* problem, const int32_t* c
 pctc_status_t pctc_prefix_read(const pctc_prefix_t* problem, const void* state, size_t state_bytes,
                                int32_t* tokens, int32_t token_stride, int32_t* token_lengths, float* scores,
                                int32_t* utt_flags, void* stream);
+/*
+ * Both for whole utterances (pctc_prefix_advance with fresh = 1, then pctc_prefix_read): one launch where k <= 8.
+ * The state can be carried on with pctc_prefix_advance.
+ */
+pctc_status_t pctc_prefix_decode(const pctc_prefix_t* problem, const int32_t* classes, const float* logprobs,
+                                 const int32_t* lengths, void* state, size_t state_bytes,
+                                 int32_t* tokens, int32_t token_stride, int32_t* token_lengths, float* scores,
+                                 int32_t* utt_flags, void* stream);
 
 /*
  * Beam search's selection over beams and vocabulary, for a decoder that works beside or behind the CTC head

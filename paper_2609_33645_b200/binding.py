@@ -25,7 +25,8 @@ EXPORTS = ("pctc_workspace_bytes", "pctc_chunk_width", "pruned_ctc_fwd_bwd", "pr
            "pruned_ctc_fwd_bwd_host", "pctc_subset_relabel_noalloc", "pctc_greedy_workspace_bytes",
            "pctc_greedy_decode", "pctc_topk_workspace_bytes", "pctc_topk_decode",
            "pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
-           "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read", "pctc_beam_workspace_bytes", "pctc_beam_select",
+           "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read",
+           "pctc_prefix_decode", "pctc_beam_workspace_bytes", "pctc_beam_select",
            "pctc_beam_reorder")
 NOALLOC_MAX_V = 262144
 
@@ -171,6 +172,8 @@ def _configure(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.pctc_prefix_advance.argtypes = [prefix_p, vp, vp, i32p, ctypes.c_int32, vp, ctypes.c_size_t, vp]
     lib.pctc_prefix_read.restype = ctypes.c_int
     lib.pctc_prefix_read.argtypes = [prefix_p, vp, ctypes.c_size_t, vp, ctypes.c_int32, vp, vp, vp, vp]
+    lib.pctc_prefix_decode.restype = ctypes.c_int
+    lib.pctc_prefix_decode.argtypes = [prefix_p, vp, vp, i32p, vp, ctypes.c_size_t, vp, ctypes.c_int32, vp, vp, vp, vp]
     lib.pctc_beam_select.restype = ctypes.c_int
     lib.pctc_beam_select.argtypes = [ctypes.POINTER(BeamProblem)] + [vp] * 9 + [ctypes.c_size_t, vp]
     lib.pctc_beam_workspace_bytes.restype = ctypes.c_int
@@ -493,7 +496,8 @@ def _native():
             raise RuntimeError("_marshal.so is missing: run paper_2609_33645_b200.build.build() first; "
                                "there is no fallback implementation") from e
         names = ("pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
-                 "pctc_beam_workspace_bytes", "pctc_beam_select", "pctc_beam_reorder", "pctc_prefix_advance", "pctc_prefix_read")
+                 "pctc_beam_workspace_bytes", "pctc_beam_select", "pctc_beam_reorder", "pctc_prefix_state_bytes",
+                 "pctc_prefix_advance", "pctc_prefix_read", "pctc_prefix_decode")
         module.bind([ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in names], PctcError)
         _marshal = module
     return _marshal
@@ -557,20 +561,13 @@ class PrefixBeam:
             raise ValueError("the state of a prefix search lives on a CUDA device")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
-        need = ctypes.c_size_t(0)
-        st = load().pctc_prefix_state_bytes(ctypes.byref(self._problem(1, 1)), ctypes.byref(need))
-        if st != 0:
-            raise PctcError(st, "pctc_prefix_state_bytes")
         self.frames = [0] * self.N
         self.started = False
-        self.state = torch.empty(int(need.value), dtype=torch.uint8, device=self.device)
-
-    def _problem(self, T, k):
-        return PrefixProblem(self.N, int(T), int(k), self.beams, self.blank_id, self.max_frames)
+        self.state = _native().prefix_start(self.N, self.beams, self.blank_id, self.max_frames, self.device.index)
 
     def advance(self, classes, logprobs, lengths=None):
         native = _native()
-        native.prefix_inputs(classes, logprobs, self.N, -1 if self.device.index is None else self.device.index)
+        native.prefix_check(classes, logprobs, self.N, -1 if self.device.index is None else self.device.index)
         lengths = [classes.shape[1]] * self.N if lengths is None else [int(n) for n in lengths]
         if len(lengths) != self.N:
             raise ValueError("one length per utterance is required")
@@ -596,9 +593,11 @@ def prefix_beam_decode(classes, logprobs, input_lengths, blank_id, beams):
     """CTC prefix beam search over whole utterances: classes [N,T,k] int32 and logprobs [N,T,k] fp32 as
     topk_decode gives them, input_lengths host integers.  Returns the dict of PrefixBeam.read() with tokens
     [N,beams,T], plus the PrefixBeam itself as "search"."""
-    search = PrefixBeam(classes.shape[0], beams, max(1, classes.shape[1]), blank_id, classes.device)
-    search.advance(classes, logprobs, input_lengths)
-    res = search.read(max_tokens=classes.shape[1])
+    lengths = [int(n) for n in input_lengths]
+    res, state = _native().prefix_decode(classes, logprobs, lengths, beams, blank_id)
+    search = PrefixBeam.__new__(PrefixBeam)
+    search.N, search.beams, search.max_frames, search.blank_id = len(lengths), int(beams), classes.shape[1], int(blank_id)
+    search.device, search.state, search.frames, search.started = classes.device, state, lengths, True
     res["search"] = search
     return res
 

@@ -27,8 +27,10 @@ struct {
   decltype(&pctc_beam_workspace_bytes) beam_workspace_bytes;
   decltype(&pctc_beam_select) beam_select;
   decltype(&pctc_beam_reorder) beam_reorder;
+  decltype(&pctc_prefix_state_bytes) prefix_state_bytes;
   decltype(&pctc_prefix_advance) prefix_advance;
   decltype(&pctc_prefix_read) prefix_read;
+  decltype(&pctc_prefix_decode) prefix_decode;
 } api;
 PyObject* error_type = nullptr;       // PctcError(status, what)
 
@@ -365,6 +367,81 @@ PyObject* beam_reorder(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // ---- prefix search ----
 
+pctc_prefix_t prefix_problem(int64_t N, int64_t T, int64_t k, PyObject* beams, PyObject* blank, PyObject* max_frames) {
+  const int64_t b = integer(beams), bl = integer(blank), m = integer(max_frames);
+  for (const int64_t v : {N, T, k, b, bl, m})
+    if (v > INT32_MAX || v < INT32_MIN) check(PCTC_ERR_UNSUPPORTED, "prefix search");
+  return pctc_prefix_t{(int32_t)N, (int32_t)T, (int32_t)k, (int32_t)b, (int32_t)bl, (int32_t)m};
+}
+// The checks of a portion of frames.
+void prefix_inputs(const at::Tensor& c, const at::Tensor& l, int64_t N, int64_t index) {
+  if (c.scalar_type() != at::kInt || l.scalar_type() != at::kFloat) fail(PyExc_ValueError, "classes must be int32 and logprobs fp32");
+  if (c.dim() != 3 || c.size(0) != N || !l.sizes().equals(c.sizes())) fail(PyExc_ValueError, "classes and logprobs must be [N, frames, k]");
+  const bool there = index < 0 ? !c.is_cuda() && !l.is_cuda()
+                               : c.is_cuda() && l.is_cuda() && c.get_device() == index && l.get_device() == index;
+  if (!there) fail(PyExc_ValueError, "classes and logprobs must be on the state's device");
+  if (!c.is_contiguous() || !l.is_contiguous()) fail(PyExc_ValueError, "classes and logprobs must be contiguous");
+}
+std::vector<int32_t> prefix_lengths(PyObject* list, int64_t N) {
+  if (PyList_GET_SIZE(list) != N) fail(PyExc_ValueError, "one length per utterance is required");
+  std::vector<int32_t> lengths(N);
+  for (int64_t i = 0; i < N; ++i) {
+    const int64_t v = integer(PyList_GET_ITEM(list, i));
+    lengths[i] = (int32_t)(v < -1 ? -1 : v > INT32_MAX ? INT32_MAX : v);
+  }
+  return lengths;
+}
+at::Tensor prefix_state(const pctc_prefix_t& p, at::Device dev) {
+  size_t need = 0;
+  check(api.prefix_state_bytes(&p, &need), "pctc_prefix_state_bytes");
+  return empty({(int64_t)need}, at::kByte, dev);
+}
+
+// What a read writes, in one allocation.
+struct PrefixOut {
+  Shared shared;
+  at::Tensor tokens, sizes, scores, flags;
+  PrefixOut(const pctc_prefix_t& p, int64_t width, at::Device dev) : shared(dev) {
+    if (width < 1 || width > INT32_MAX) fail(PyExc_ValueError, "max_tokens must be at least 1");
+    shared.add({p.N, p.beams, width}, at::kInt);
+    shared.add({p.N, p.beams}, at::kInt);
+    shared.add({p.N, p.beams}, at::kFloat);
+    shared.add({p.N}, at::kInt);
+    shared.allocate();
+    tokens = shared.get(0);
+    sizes = shared.get(1);
+    scores = shared.get(2);
+    flags = shared.get(3);
+  }
+  PyObject* dict() const {
+    PyObject* d = PyDict_New();
+    if (!d) throw Failed{};
+    put(d, "tokens", tokens);
+    put(d, "token_lengths", sizes);
+    put(d, "scores", scores);
+    put(d, "flags", flags);
+    return d;
+  }
+};
+
+// prefix_check(classes, logprobs, N, device index): the checks of a portion of frames
+PyObject* prefix_check(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 4);
+  prefix_inputs(tensor(a[0], "classes"), tensor(a[1], "logprobs"), integer(a[2]), integer(a[3]));
+  Py_RETURN_NONE;
+  MARSHAL_END
+}
+// prefix_start(N, beams, blank, max_frames, device index) -> state
+PyObject* prefix_start(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 5);
+  const pctc_prefix_t p = prefix_problem(integer(a[0]), 1, 1, a[1], a[2], a[3]);
+  const at::Device dev(at::kCUDA, (c10::DeviceIndex)integer(a[4]));
+  const c10::cuda::CUDAGuard guard(dev);
+  return THPVariable_Wrap(prefix_state(p, dev));
+  MARSHAL_END
+}
 // prefix_advance(state, classes, logprobs, lengths list, N, beams, blank, max_frames, fresh)
 PyObject* prefix_advance(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MARSHAL_BEGIN
@@ -372,39 +449,14 @@ PyObject* prefix_advance(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor& state = tensor(a[0], "state");
   const at::Tensor& c = tensor(a[1], "classes");
   const at::Tensor& l = tensor(a[2], "logprobs");
-  const Py_ssize_t N = PyList_GET_SIZE(a[3]);
-  pctc_prefix_t p;
-  p.N = (int32_t)integer(a[4]);
-  p.T = (int32_t)c.size(1);
-  p.k = (int32_t)c.size(2);
-  p.beams = (int32_t)integer(a[5]);
-  p.blank_id = (int32_t)integer(a[6]);
-  p.max_frames = (int32_t)integer(a[7]);
-  if (N != p.N) fail(PyExc_ValueError, "one length per utterance is required");
-  std::vector<int32_t> lengths(N);
-  for (Py_ssize_t i = 0; i < N; ++i) lengths[i] = (int32_t)integer(PyList_GET_ITEM(a[3], i));
   const at::Device dev = state.device();
+  prefix_inputs(c, l, integer(a[4]), dev.index());
+  const pctc_prefix_t p = prefix_problem(c.size(0), c.size(1), c.size(2), a[5], a[6], a[7]);
+  const std::vector<int32_t> lengths = prefix_lengths(a[3], p.N);
   const c10::cuda::CUDAGuard guard(dev);
   check(api.prefix_advance(&p, (const int32_t*)ptr(c), (const float*)ptr(l), lengths.data(), (int32_t)integer(a[8]),
                            ptr(state), (size_t)state.numel(), stream_of(dev)),
         "pctc_prefix_advance");
-  Py_RETURN_NONE;
-  MARSHAL_END
-}
-// prefix_inputs(classes, logprobs, N, device index): the checks of a portion of frames
-PyObject* prefix_inputs(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  MARSHAL_BEGIN
-  want(n, 4);
-  const at::Tensor& c = tensor(a[0], "classes");
-  const at::Tensor& l = tensor(a[1], "logprobs");
-  const int64_t N = integer(a[2]), index = integer(a[3]);
-  if (c.scalar_type() != at::kInt || l.scalar_type() != at::kFloat) fail(PyExc_ValueError, "classes must be int32 and logprobs fp32");
-  if (c.dim() != 3 || c.size(0) != N || !l.sizes().equals(c.sizes())) fail(PyExc_ValueError, "classes and logprobs must be [N, frames, k]");
-  const bool there = index < 0 ? !c.is_cuda() && !l.is_cuda()
-                               : c.is_cuda() && l.is_cuda() && c.get_device() == index && l.get_device() == index;
-  if (!there) fail(PyExc_ValueError, "classes and logprobs must be on the state's device");
-  if (!c.is_contiguous() || !l.is_contiguous()) fail(PyExc_ValueError, "classes and logprobs must be contiguous");
-  if (c.size(1) > INT32_MAX || c.size(2) > INT32_MAX) check(PCTC_ERR_UNSUPPORTED, "pctc_prefix_advance");
   Py_RETURN_NONE;
   MARSHAL_END
 }
@@ -413,33 +465,51 @@ PyObject* prefix_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MARSHAL_BEGIN
   want(n, 6);
   const at::Tensor& state = tensor(a[0], "state");
-  pctc_prefix_t p;
-  p.N = (int32_t)integer(a[1]);
-  p.beams = (int32_t)integer(a[2]);
-  p.blank_id = (int32_t)integer(a[3]);
-  p.max_frames = (int32_t)integer(a[4]);
-  p.T = p.k = 1;
-  const int64_t width = integer(a[5]);
-  if (width < 1 || width > INT32_MAX) fail(PyExc_ValueError, "max_tokens must be at least 1");
+  const pctc_prefix_t p = prefix_problem(integer(a[1]), 1, 1, a[2], a[3], a[4]);
   const at::Device dev = state.device();
   const c10::cuda::CUDAGuard guard(dev);
-  Shared out(dev);
-  out.add({p.N, p.beams, width}, at::kInt);
-  out.add({p.N, p.beams}, at::kInt);
-  out.add({p.N, p.beams}, at::kFloat);
-  out.add({p.N}, at::kInt);
-  out.allocate();
-  const at::Tensor tokens = out.get(0), sizes = out.get(1), scores = out.get(2), flags = out.get(3);
-  check(api.prefix_read(&p, ptr(state), (size_t)state.numel(), (int32_t*)ptr(tokens), (int32_t)width, (int32_t*)ptr(sizes),
-                        (float*)ptr(scores), (int32_t*)ptr(flags), stream_of(dev)),
+  const PrefixOut o(p, integer(a[5]), dev);
+  check(api.prefix_read(&p, ptr(state), (size_t)state.numel(), (int32_t*)ptr(o.tokens), (int32_t)o.tokens.size(2),
+                        (int32_t*)ptr(o.sizes), (float*)ptr(o.scores), (int32_t*)ptr(o.flags), stream_of(dev)),
         "pctc_prefix_read");
-  PyObject* d = PyDict_New();
-  if (!d) return nullptr;
-  put(d, "tokens", tokens);
-  put(d, "token_lengths", sizes);
-  put(d, "scores", scores);
-  put(d, "flags", flags);
-  return d;
+  return o.dict();
+  MARSHAL_END
+}
+// prefix_decode(classes, logprobs, lengths list, beams, blank) -> (dict, state)
+PyObject* prefix_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 5);
+  const at::Tensor& c = tensor(a[0], "classes");
+  const at::Tensor& l = tensor(a[1], "logprobs");
+  if (!c.is_cuda()) fail(PyExc_ValueError, "the state of a prefix search lives on a CUDA device");
+  const at::Device dev = c.device();
+  prefix_inputs(c, l, c.dim() ? c.size(0) : 0, dev.index());
+  PyObject* frames = PyLong_FromLongLong(std::max<int64_t>(1, c.size(1)));
+  if (!frames) throw Failed{};
+  pctc_prefix_t p;
+  try {
+    p = prefix_problem(c.size(0), c.size(1), c.size(2), a[3], a[4], frames);
+  } catch (...) {
+    Py_DECREF(frames);
+    throw;
+  }
+  Py_DECREF(frames);
+  const std::vector<int32_t> lengths = prefix_lengths(a[2], p.N);
+  for (const int32_t v : lengths)
+    if (v > p.T) fail(PyExc_ValueError, "more frames than the state has room for");
+  const c10::cuda::CUDAGuard guard(dev);
+  const at::Tensor state = prefix_state(p, dev);
+  const PrefixOut o(p, p.max_frames, dev);
+  check(api.prefix_decode(&p, (const int32_t*)ptr(c), (const float*)ptr(l), lengths.data(), ptr(state), (size_t)state.numel(),
+                          (int32_t*)ptr(o.tokens), p.max_frames, (int32_t*)ptr(o.sizes), (float*)ptr(o.scores),
+                          (int32_t*)ptr(o.flags), stream_of(dev)),
+        "pctc_prefix_decode");
+  PyObject* d = o.dict();
+  PyObject* s = THPVariable_Wrap(state);
+  PyObject* both = s ? PyTuple_Pack(2, d, s) : nullptr;
+  Py_DECREF(d);
+  Py_XDECREF(s);
+  return both;
   MARSHAL_END
 }
 
@@ -459,7 +529,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind), FAST(clip_grad_norm), FAST(grad_sqsum), FAST(grad_scale), FAST(beam_select),
-                         FAST(beam_reorder), FAST(prefix_inputs), FAST(prefix_advance), FAST(prefix_read),
+                         FAST(beam_reorder), FAST(prefix_check), FAST(prefix_start), FAST(prefix_advance),
+                         FAST(prefix_read), FAST(prefix_decode),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -28,6 +28,7 @@ constexpr int PFX_MAX_BEAMS = 32, PFX_MAX_K = 32;
 constexpr int PFX_RESCALE = 16;                   // frames between rescalings: values move by at most 3^16
 constexpr int PFX_TILE = 32;                      // frames whose probabilities are staged at a time
 constexpr int PFX_THREADS = 128;
+constexpr int PFX_LAST_WINDOW = 3072;             // nodes of a window where the search itself reads its hypotheses out
 constexpr int PFX_SLICE = 1024;                   // utterances whose lengths one launch takes as a parameter
 
 struct Slots {
@@ -62,6 +63,70 @@ __device__ __forceinline__ unsigned long long grow_hash(unsigned long long h, in
 __device__ __forceinline__ double round24(double p) {
   const long long b = __double_as_longlong(p) + (1ll << 28);
   return __longlong_as_double(b & ~((1ll << 29) - 1));
+}
+
+// Where hypotheses go.
+struct Hypotheses {
+  int* tokens;                                    // [N, B, stride]; null: nowhere
+  int* sizes;
+  float* scores;
+  int* flags;                                     // or null
+  int stride;
+};
+template <int WINDOW>
+struct ReadShared {
+  int2 window[WINDOW];
+  int newest, oldest, size[PFX_MAX_BEAMS];
+};
+
+// The hypotheses of a state: every slot's labels from its chain of nodes, last label first.  A chain is
+// as long as the hypothesis, and a node read from L2 a step would cost 0.3 us; nodes are numbered by frame, so the
+// table is taken through shared memory in windows from the last frame to the first, and all chains of an
+// utterance walk through a window before the next one is fetched.  Called by all threads of a CTA.
+template <int THREADS, int WINDOW>
+__device__ void read_out(ReadShared<WINDOW>& sh, const PrefixState* st, const int2* my_nodes, int n, int B, int max_frames,
+                         const Hypotheses& h) {
+  const int tid = threadIdx.x;
+  const bool valid = st->magic == PFX_MAGIC && st->beams == B && st->max_frames == max_frames;
+  const int most = (int)nodes_per_utt(B, max_frames);
+  if (tid == 0) sh.newest = 0;
+  __syncthreads();
+  int at = 0, node = 0;
+  int* out = nullptr;
+  bool live = false;
+  if (tid < B) {
+    const double total = valid ? st->s.pb[tid] + st->s.pn[tid] : 0.0;
+    live = total > 0.0;
+    at = live ? st->s.size[tid] : 0;
+    node = live ? st->s.node[tid] : 0;
+    if (node < 0 || node >= most) node = 0;
+    out = h.tokens + ((size_t)n * B + tid) * h.stride;
+    sh.size[tid] = at;
+    h.sizes[n * B + tid] = at;
+    h.scores[n * B + tid] = live ? (float)(log(total) + st->power * 0.693147180559945309417 + st->shift) : -CUDART_INF_F;
+    atomicMax(&sh.newest, node);
+  }
+  const bool any = __syncthreads_or(live);
+  if (tid == 0 && h.flags) h.flags[n] = valid ? st->flags | (any ? 0 : PCTC_UTT_INFEASIBLE) : PCTC_UTT_STATE_FULL;
+  for (int b = 0; b < B; ++b)
+    for (int i = sh.size[b] + tid; i < h.stride; i += THREADS) h.tokens[((size_t)n * B + b) * h.stride + i] = -1;
+  for (int hi = sh.newest + 1; hi > 1;) {         // nodes [lo, hi); node 0 is the empty prefix
+    const int lo = max(1, hi - WINDOW);
+    for (int i = tid; i < hi - lo; i += THREADS) sh.window[i] = my_nodes[lo + i];
+    if (tid == 0) sh.oldest = 0;
+    __syncthreads();
+    if (tid < B) {
+      while (node >= lo && at > 0) {
+        const int2 v = sh.window[node - lo];
+        if (--at < h.stride) out[at] = v.y;
+        node = v.x >= 0 && v.x < node ? v.x : 0;  // nodes are made after their parents
+      }
+      atomicMax(&sh.oldest, at > 0 ? node : 0);   // the newest node that is still to be read
+    }
+    __syncthreads();
+    hi = min(lo, sh.oldest + 1);
+    __syncthreads();
+  }
 }
 
 // Frames staged for the search: KM >= k classes a frame.  The blank stands in `blank` only; what does not count
@@ -180,7 +245,7 @@ struct Search {                                   // what lanes hand each other 
 template <int KM, int BM>
 __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
     const int* __restrict__ classes, const float* __restrict__ logprobs, const __grid_constant__ Lengths len, int n0,
-    int T, int k, int B, int blank, int max_frames, int fresh, char* __restrict__ states, int2* __restrict__ nodes) {
+    int T, int k, int B, int blank, int max_frames, int fresh, char* states, int2* nodes, const Hypotheses out) {
   constexpr unsigned ALL = 0xffffffffu;
   constexpr int REP = 32 / BM, KP = KM / REP;     // lanes a slot, classes a lane
   constexpr unsigned SLOTS = BM == 32 ? ALL : (1u << BM) - 1;
@@ -499,62 +564,23 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
       st->flags = flags;
     }
   }
+  if constexpr (KM == 8) {                        // whole utterances: the hypotheses, in the same launch
+    if (out.tokens) {
+      __shared__ ReadShared<PFX_LAST_WINDOW> rd;
+      __syncthreads();
+      read_out<PFX_THREADS>(rd, st, my_nodes, n, B, max_frames, out);
+    }
+  }
 }
 
-// The hypotheses of a state: every slot's labels from its chain of nodes, last label first.  A chain is
-// as long as the hypothesis, and a node read from L2 a step would cost 0.3 us; nodes are numbered by frame, so the
-// table is taken through shared memory in windows from the last frame to the first, and all chains of an
-// utterance walk through a window before the next one is fetched.
-constexpr int PFX_READ_THREADS = 256;
-constexpr int PFX_WINDOW = 5120;                  // nodes, 40 KB
-__global__ void __launch_bounds__(PFX_READ_THREADS) k_prefix_read(
-    const char* __restrict__ states, const int2* __restrict__ nodes, int B, int max_frames, int stride,
-    int* __restrict__ tokens, int* __restrict__ sizes, float* __restrict__ scores, int* __restrict__ flags) {
-  __shared__ int2 window[PFX_WINDOW];
-  __shared__ int newest, oldest, size[PFX_MAX_BEAMS];
-  const int n = blockIdx.x, tid = threadIdx.x;
-  const PrefixState* st = (const PrefixState*)(states + (size_t)n * PFX_STATE_BYTES);
-  const int2* my_nodes = nodes + (size_t)n * nodes_per_utt(B, max_frames);
-  const bool valid = st->magic == PFX_MAGIC && st->beams == B && st->max_frames == max_frames;
-  const int most = (int)nodes_per_utt(B, max_frames);
-  if (tid == 0) newest = 0;
-  __syncthreads();
-  int at = 0, node = 0;
-  int* out = nullptr;
-  bool live = false;
-  if (tid < B) {
-    const double total = valid ? st->s.pb[tid] + st->s.pn[tid] : 0.0;
-    live = total > 0.0;
-    at = live ? st->s.size[tid] : 0;
-    node = live ? st->s.node[tid] : 0;
-    if (node < 0 || node >= most) node = 0;
-    out = tokens + ((size_t)n * B + tid) * stride;
-    size[tid] = at;
-    sizes[n * B + tid] = at;
-    scores[n * B + tid] = live ? (float)(log(total) + st->power * 0.693147180559945309417 + st->shift) : -CUDART_INF_F;
-    atomicMax(&newest, node);
-  }
-  const bool any = __syncthreads_or(live);
-  if (tid == 0 && flags) flags[n] = valid ? st->flags | (any ? 0 : PCTC_UTT_INFEASIBLE) : PCTC_UTT_STATE_FULL;
-  for (int b = 0; b < B; ++b)
-    for (int i = size[b] + tid; i < stride; i += PFX_READ_THREADS) tokens[((size_t)n * B + b) * stride + i] = -1;
-  for (int hi = newest + 1; hi > 1;) {            // nodes [lo, hi); node 0 is the empty prefix
-    const int lo = max(1, hi - PFX_WINDOW);
-    for (int i = tid; i < hi - lo; i += PFX_READ_THREADS) window[i] = my_nodes[lo + i];
-    if (tid == 0) oldest = 0;
-    __syncthreads();
-    if (tid < B) {
-      while (node >= lo && at > 0) {
-        const int2 v = window[node - lo];
-        if (--at < stride) out[at] = v.y;
-        node = v.x >= 0 && v.x < node ? v.x : 0;  // nodes are made after their parents
-      }
-      atomicMax(&oldest, at > 0 ? node : 0);      // the newest node that is still to be read
-    }
-    __syncthreads();
-    hi = min(lo, oldest + 1);
-    __syncthreads();
-  }
+constexpr int PFX_READ_THREADS = 256, PFX_READ_WINDOW = 5120;
+__global__ void __launch_bounds__(PFX_READ_THREADS) k_prefix_read(const char* __restrict__ states,
+                                                                  const int2* __restrict__ nodes, int B, int max_frames,
+                                                                  const Hypotheses out) {
+  __shared__ ReadShared<PFX_READ_WINDOW> sh;
+  const int n = blockIdx.x;
+  read_out<PFX_READ_THREADS>(sh, (const PrefixState*)(states + (size_t)n * PFX_STATE_BYTES),
+                             nodes + (size_t)n * nodes_per_utt(B, max_frames), n, B, max_frames, out);
 }
 
 pctc_status_t check(const pctc_prefix_t* p) {
@@ -567,6 +593,29 @@ pctc_status_t check(const pctc_prefix_t* p) {
 }
 size_t state_bytes(const pctc_prefix_t* p) {
   return p->N * (PFX_STATE_BYTES + nodes_per_utt(p->beams, p->max_frames) * sizeof(int2));
+}
+
+pctc_status_t advance(const pctc_prefix_t* p, const int32_t* classes, const float* logprobs, const int32_t* lengths,
+                      int32_t fresh, void* state, size_t bytes, const Hypotheses& out, void* stream) {
+  const pctc_status_t st = check(p);
+  if (st != PCTC_OK) return st;
+  if (!classes || !logprobs || !lengths || !state || ((size_t)state & 255) || (fresh & ~1)) return PCTC_ERR_INVALID_ARG;
+  if (((size_t)classes & 3) || ((size_t)logprobs & 3)) return PCTC_ERR_INVALID_ARG;
+  for (int n = 0; n < p->N; ++n)
+    if (lengths[n] < 0 || lengths[n] > p->T || lengths[n] > p->max_frames) return PCTC_ERR_INVALID_ARG;
+  if (bytes < state_bytes(p)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
+  int2* nodes = (int2*)((char*)state + (size_t)p->N * PFX_STATE_BYTES);
+  for (int n0 = 0; n0 < p->N; n0 += PFX_SLICE) {
+    Lengths len;
+    const int m = p->N - n0 < PFX_SLICE ? p->N - n0 : PFX_SLICE;
+    for (int i = 0; i < m; ++i) len.n[i] = lengths[n0 + i];
+    auto kern = p->k <= 8 ? (p->beams <= 8 ? k_prefix_advance<8, 8> : p->beams <= 16 ? k_prefix_advance<8, 16> : k_prefix_advance<8, 32>)
+                          : (p->beams <= 8 ? k_prefix_advance<32, 8> : p->beams <= 16 ? k_prefix_advance<32, 16> : k_prefix_advance<32, 32>);
+    kern<<<m, PFX_THREADS, 0, (cudaStream_t)stream>>>(classes, logprobs, len, n0, p->T, p->k, p->beams, p->blank_id,
+                                                      p->max_frames, fresh, (char*)state, nodes, out);
+    if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
+  }
+  return PCTC_OK;
 }
 
 }  // namespace
@@ -585,26 +634,8 @@ pctc_status_t pctc_prefix_state_bytes(const pctc_prefix_t* p, size_t* bytes_out)
 }
 
 pctc_status_t pctc_prefix_advance(const pctc_prefix_t* p, const int32_t* classes, const float* logprobs,
-                                  const int32_t* lengths, int32_t fresh, void* state, size_t bytes, void* stream_v) {
-  const pctc_status_t st = check(p);
-  if (st != PCTC_OK) return st;
-  if (!classes || !logprobs || !lengths || !state || ((size_t)state & 255) || (fresh & ~1)) return PCTC_ERR_INVALID_ARG;
-  if (((size_t)classes & 3) || ((size_t)logprobs & 3)) return PCTC_ERR_INVALID_ARG;
-  for (int n = 0; n < p->N; ++n)
-    if (lengths[n] < 0 || lengths[n] > p->T || lengths[n] > p->max_frames) return PCTC_ERR_INVALID_ARG;
-  if (bytes < state_bytes(p)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
-  int2* nodes = (int2*)((char*)state + (size_t)p->N * PFX_STATE_BYTES);
-  for (int n0 = 0; n0 < p->N; n0 += PFX_SLICE) {
-    Lengths len;
-    const int m = p->N - n0 < PFX_SLICE ? p->N - n0 : PFX_SLICE;
-    for (int i = 0; i < m; ++i) len.n[i] = lengths[n0 + i];
-    auto kern = p->k <= 8 ? (p->beams <= 8 ? k_prefix_advance<8, 8> : p->beams <= 16 ? k_prefix_advance<8, 16> : k_prefix_advance<8, 32>)
-                          : (p->beams <= 8 ? k_prefix_advance<32, 8> : p->beams <= 16 ? k_prefix_advance<32, 16> : k_prefix_advance<32, 32>);
-    kern<<<m, PFX_THREADS, 0, (cudaStream_t)stream_v>>>(classes, logprobs, len, n0, p->T, p->k, p->beams, p->blank_id,
-                                                        p->max_frames, fresh, (char*)state, nodes);
-    if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
-  }
-  return PCTC_OK;
+                                  const int32_t* lengths, int32_t fresh, void* state, size_t bytes, void* stream) {
+  return advance(p, classes, logprobs, lengths, fresh, state, bytes, Hypotheses{}, stream);
 }
 
 pctc_status_t pctc_prefix_read(const pctc_prefix_t* p, const void* state, size_t bytes, int32_t* tokens,
@@ -616,9 +647,20 @@ pctc_status_t pctc_prefix_read(const pctc_prefix_t* p, const void* state, size_t
     return PCTC_ERR_INVALID_ARG;
   if (bytes < state_bytes(p)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
   const int2* nodes = (const int2*)((const char*)state + (size_t)p->N * PFX_STATE_BYTES);
-  k_prefix_read<<<p->N, PFX_READ_THREADS, 0, (cudaStream_t)stream_v>>>((const char*)state, nodes, p->beams, p->max_frames,
-                                                                  token_stride, tokens, token_lengths, scores, utt_flags);
+  k_prefix_read<<<p->N, PFX_READ_THREADS, 0, (cudaStream_t)stream_v>>>(
+      (const char*)state, nodes, p->beams, p->max_frames, Hypotheses{tokens, token_lengths, scores, utt_flags, token_stride});
   return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+}
+
+pctc_status_t pctc_prefix_decode(const pctc_prefix_t* p, const int32_t* classes, const float* logprobs,
+                                 const int32_t* lengths, void* state, size_t bytes, int32_t* tokens, int32_t token_stride,
+                                 int32_t* token_lengths, float* scores, int32_t* utt_flags, void* stream) {
+  if (!tokens || token_stride <= 0 || !token_lengths || !scores) return PCTC_ERR_INVALID_ARG;
+  const bool one = p && p->k <= 8;
+  const pctc_status_t st = advance(p, classes, logprobs, lengths, 1, state, bytes,
+                                   one ? Hypotheses{tokens, token_lengths, scores, utt_flags, token_stride} : Hypotheses{}, stream);
+  if (st != PCTC_OK || one) return st;
+  return pctc_prefix_read(p, state, bytes, tokens, token_stride, token_lengths, scores, utt_flags, stream);
 }
 
 }  // extern "C"

@@ -142,6 +142,22 @@ def test_portions_make_the_whole(cuts):
     assert torch.equal(again["tokens"], got["tokens"][:, :, :5]) and torch.equal(again["token_lengths"], got["token_lengths"])
 
 
+def test_a_finished_search_goes_on():
+    """The search that prefix_beam_decode returns reads the same hypotheses, and its state is full."""
+    classes, logprobs = make(2, 40, 8, 30, 4)
+    r = run(classes, logprobs, [40, 17], 0, 8)
+    again = r["search"].read()
+    for x in ("tokens", "token_lengths", "scores", "flags"):
+        assert torch.equal(again[x], r[x])
+    c, l = torch.from_numpy(classes[:, :23].copy()).to(DEV), torch.from_numpy(logprobs[:, :23].copy()).to(DEV)
+    with pytest.raises(ValueError, match="room"):
+        r["search"].advance(c, l)
+    r["search"].advance(c, l, [0, 23])
+    two = [np.concatenate([x[1:, :17], x[1:, :23]], 1) for x in (classes, logprobs)]
+    got = r["search"].read()
+    check({x: got[x][1:] for x in ("tokens", "token_lengths", "scores", "flags")}, *two, [40], 0, 8)
+
+
 def test_more_utterances_than_one_launch_takes():
     classes, logprobs = make(1030, 3, 2, 4, 6)
     lengths = [1 + i % 3 for i in range(1030)]

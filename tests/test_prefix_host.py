@@ -91,6 +91,13 @@ def test_bad_calls_are_refused_before_any_launch(lib):
     assert read(tokens=None) == 1 and read(stride=0) == 1 and read(ln=None) == 1 and read(sc=None) == 1
     assert read(size=need - 1) == 2
 
+    def decode(lengths=(5, 0), cls=at, state=at, size=need, tokens=at, stride=9, sizes=at, scores=at):
+        ln = (ctypes.c_int32 * 2)(*lengths)
+        return cdll.pctc_prefix_decode(ctypes.byref(p), cls, at, ln, state, size, tokens, stride, sizes, scores, None, None)
+
+    assert decode(lengths=(6, 0)) == 1 and decode(cls=None) == 1 and decode(state=None) == 1 and decode(size=need - 1) == 2
+    assert decode(tokens=None) == 1 and decode(stride=0) == 1 and decode(sizes=None) == 1 and decode(scores=None) == 1
+
 
 def test_binding_refuses_before_it_calls(lib):
     s = binding.PrefixBeam.__new__(binding.PrefixBeam)
