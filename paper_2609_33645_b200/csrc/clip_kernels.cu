@@ -8,14 +8,16 @@
 // pass ends there: the usual step of a training run reads its gradients once and writes nothing.
 // Both are bound by HBM; the arithmetic is one multiply-add a value.
 //
-// Measured: 156M bf16 values into another buffer 145 us (three passes of 312 MB at the rate of a copy: 143; the last 64 MB
-// of the first pass are still in L2 for the second); 64M bf16 values in 384 tensors, in place below the limit, 28 us
-// (one pass: 20); 100,000 fp32 values in 7 tensors 8.7 us in one launch (5.5 in two, which cost the host 6 us more).
+// Measured: 156M bf16 values into another buffer 140 us (three passes of 312 MB at the rate of a copy: 143; the last 64 MB
+// of the first pass are still in L2 for the second); 64M bf16 values in 384 tensors, in place below the limit, 27 us
+// (one pass: 20; a bare read of the same bytes: 23); 100,000 fp32 values in 7 tensors 8.2 us in one launch (5.5 in two,
+// which cost the host 6 us more).
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 
 #include <cooperative_groups.h>
 
+#include <cfloat>
 #include <cmath>
 #include <new>
 
@@ -29,7 +31,7 @@ namespace {
 constexpr int CLIP_THREADS = 256;
 constexpr int CLIP_VECS = 4;
 constexpr int CLIP_CHUNK_BYTES = CLIP_THREADS * CLIP_VECS * 16;
-constexpr int CLIP_CTAS_PER_SM = 6;              // first pass: 26 us for 384 tensors of 128 MB (4: 30), 49 for 312 MB (4: 53)
+constexpr int CLIP_CTAS_PER_SM = 6;              // first pass: 49 us for 312 MB (4: 53)
 constexpr int CLIP_SCALE_CTAS_PER_SM = 4;        // second pass: 105 us for 312 MB in and out (6: 119)
 constexpr int CLIP_KEEP_CHUNKS = 4096;           // the last 64 MB of the first pass stay in L2, the rest goes past it
 constexpr int CLIP_EACH_CHUNKS = 2048;           // from so many chunks on (32 MB: 21.4 against 22.0 us; 312 MB: 150 against
@@ -67,14 +69,25 @@ __host__ __device__ __forceinline__ int head_of(const void* p, long long numel, 
   return head < numel ? head : (int)numel;
 }
 
-template <int LIM>
-__device__ __forceinline__ int tensor_of(const ClipTable<LIM>& tab, int c) {
-  int lo = 0, hi = tab.n - 1;                    // the last tensor whose first chunk is <= c
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (tab.chunk0[mid] <= c) lo = mid; else hi = mid - 1;
+// The last tensor whose first chunk is <= c, by a whole warp: 32 probes of the table at a time.  `chunk0` is a copy in
+// shared memory: a binary search of the parameter by every thread takes as many instructions as a chunk's sums (384
+// tensors of 128 MB: 25.3 us against 24.5).
+__device__ __forceinline__ int tensor_of(const int* chunk0, int n, int c) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + 31) >> 5, at = lane * step;
+    const unsigned m = __ballot_sync(0xffffffffu, at < n && chunk0[lo + min(at, n - 1)] <= c);
+    const int k = 31 - __clz(m);                 // the first probe always holds
+    lo += k * step;
+    n = min(step, n - k * step);
   }
   return lo;
+}
+template <int LIM>
+__device__ __forceinline__ void copy_chunks(int* chunk0, const ClipTable<LIM>& tab) {
+  for (int i = threadIdx.x; i < tab.n; i += CLIP_THREADS) chunk0[i] = tab.chunk0[i];
+  __syncthreads();
 }
 
 __device__ __forceinline__ float bf16_lo(unsigned v) { return __uint_as_float(v << 16); }
@@ -119,9 +132,9 @@ __device__ __forceinline__ double square_sum_vec(const uint4& v, bool f32) {
 }
 
 template <int LIM>
-__device__ __forceinline__ Piece piece_of(const ClipTable<LIM>& tab, int c) {
+__device__ __forceinline__ Piece piece_in(const ClipTable<LIM>& tab, int tensor, int c) {
   Piece r;
-  r.tensor = tensor_of(tab, c);
+  r.tensor = tensor;
   r.p = tab.in[r.tensor];
   r.kind = tab.kind[r.tensor];
   const long long numel = tab.numel[r.tensor];
@@ -133,6 +146,19 @@ __device__ __forceinline__ Piece piece_of(const ClipTable<LIM>& tab, int c) {
   r.nvec = r.count >> (4 - shift);
   r.head = local ? 0 : head;
   return r;
+}
+template <int LIM>
+__device__ __forceinline__ Piece piece_of(const ClipTable<LIM>& tab, const int* chunk0, int c) {
+  return piece_in(tab, tensor_of(chunk0, tab.n, c), c);
+}
+template <int LIM>
+__device__ __forceinline__ Piece piece_of(const ClipTable<LIM>& tab, int c) {
+  int lo = 0, hi = tab.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (tab.chunk0[mid] <= c) lo = mid; else hi = mid - 1;
+  }
+  return piece_in(tab, lo, c);
 }
 static_assert(CLIP_CHUNK_BYTES == 1 << 14, "chunks are 16 KB");
 
@@ -175,11 +201,11 @@ __device__ __forceinline__ double block_sum(double v) {
 }
 
 template <int LIM>
-__device__ __forceinline__ double square_sums(const ClipTable<LIM>& tab, int first, int step) {
+__device__ __forceinline__ double square_sums(const ClipTable<LIM>& tab, const int* chunk0, int first, int step) {
   double acc = 0.0;
   const int total = tab.chunk0[tab.n];
   for (int c = first; c < total; c += step) {
-    const Piece r = piece_of(tab, c);
+    const Piece r = piece_of(tab, chunk0, c);
     uint4 v[CLIP_VECS];
     load_piece(v, r, c >= total - CLIP_KEEP_CHUNKS);
     acc += piece_squares(v, r);
@@ -190,7 +216,9 @@ __device__ __forceinline__ double square_sums(const ClipTable<LIM>& tab, int fir
 template <int LIM>
 __global__ void __launch_bounds__(CLIP_THREADS, CLIP_CTAS_PER_SM) k_square_sums(const __grid_constant__ ClipTable<LIM> tab,
                                                                                 double* __restrict__ partial) {
-  const double s = block_sum(square_sums(tab, blockIdx.x, gridDim.x));
+  __shared__ int chunk0[LIM];
+  copy_chunks(chunk0, tab);
+  const double s = block_sum(square_sums(tab, chunk0, blockIdx.x, gridDim.x));
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
@@ -210,12 +238,13 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const unsigned*>(&h);
 }
 
-// g * f in fp32; by a factor below fp32's normal range in 64 bits.
+// g * f in fp32; by a factor below fp32's normal range (TINY) in 64 bits.
+template <bool TINY>
 __device__ __forceinline__ float scaled(float x, float f, double fd) {
-  return f >= 1.1754944e-38f ? x * f : (float)((double)x * fd);
+  return TINY ? (float)((double)x * fd) : x * f;
 }
 
-template <bool F32>
+template <bool F32, bool TINY>
 __device__ __forceinline__ void scale_piece(const uint4 (&v)[CLIP_VECS], const Piece& r, void* o, float f, double fd) {
   constexpr int VE = F32 ? 4 : 8;
   const bool of32 = r.kind & OUT_F32, vec = r.kind & OUT_VEC;
@@ -228,7 +257,7 @@ __device__ __forceinline__ void scale_piece(const uint4 (&v)[CLIP_VECS], const P
 #pragma unroll
     for (int q = 0; q < VE; ++q) {
       const float g = F32 ? __uint_as_float(w[q & 3]) : q & 1 ? bf16_hi(w[q / 2]) : bf16_lo(w[q / 2]);
-      x[q] = scaled(g, f, fd);
+      x[q] = scaled<TINY>(g, f, fd);
     }
     const long long at = r.start + (long long)i * VE;
     if (vec && of32) {
@@ -245,7 +274,7 @@ __device__ __forceinline__ void scale_piece(const uint4 (&v)[CLIP_VECS], const P
   }
 }
 __device__ __forceinline__ void scale_one(const Piece& r, void* o, long long i, float f, double fd) {
-  store1(o, i, scaled(one_value(r, i), f, fd), r.kind & OUT_F32);
+  store1(o, i, f >= FLT_MIN ? scaled<false>(one_value(r, i), f, fd) : scaled<true>(one_value(r, i), f, fd), r.kind & OUT_F32);
 }
 
 // Scales a chunk that has been loaded.
@@ -253,8 +282,13 @@ template <int LIM>
 __device__ __forceinline__ void scale_chunk(const ClipTable<LIM>& tab, const Piece& r, const uint4 (&v)[CLIP_VECS], float f,
                                             double fd) {
   void* o = tab.out[r.tensor];
-  if (r.kind & IN_F32) scale_piece<true>(v, r, o, f, fd);
-  else scale_piece<false>(v, r, o, f, fd);
+  if (f >= FLT_MIN) {
+    if (r.kind & IN_F32) scale_piece<true, false>(v, r, o, f, fd);
+    else scale_piece<false, false>(v, r, o, f, fd);
+  } else {
+    if (r.kind & IN_F32) scale_piece<true, true>(v, r, o, f, fd);
+    else scale_piece<false, true>(v, r, o, f, fd);
+  }
   const int body = r.nvec * (r.kind & IN_F32 ? 4 : 8);
   if ((int)threadIdx.x < r.head) scale_one(r, o, threadIdx.x, f, fd);
   if ((int)threadIdx.x < r.count - body) scale_one(r, o, r.start + body + threadIdx.x, f, fd);
@@ -262,9 +296,10 @@ __device__ __forceinline__ void scale_chunk(const ClipTable<LIM>& tab, const Pie
 
 // Chunks first, first - step, ...  Backwards: those that the first pass read last are still in L2.
 template <int LIM>
-__device__ __forceinline__ void scale_all(const ClipTable<LIM>& tab, int first, int step, float f, double fd) {
+__device__ __forceinline__ void scale_all(const ClipTable<LIM>& tab, const int* chunk0, int first, int step, float f,
+                                          double fd) {
   for (int c = first; c >= 0; c -= step) {
-    const Piece r = piece_of(tab, c);
+    const Piece r = piece_of(tab, chunk0, c);
     if (f == 1.0f && (r.kind & IN_PLACE)) continue;
     uint4 v[CLIP_VECS];
     load_piece(v, r, false);
@@ -291,7 +326,9 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_scale(const __grid_constant__ 
   const float f = (float)fd;
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   if (f == 1.0f && tab.in_place) return;
-  scale_all(tab, tab.chunk0[tab.n] - 1 - (int)blockIdx.x, gridDim.x, f, fd);
+  __shared__ int chunk0[LIM];
+  copy_chunks(chunk0, tab);
+  scale_all(tab, chunk0, tab.chunk0[tab.n] - 1 - (int)blockIdx.x, gridDim.x, f, fd);
 }
 
 // The same for many values that all have to be written, with one CTA a chunk: CTAs that start in order keep reads and
@@ -302,7 +339,7 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_scale_each(const __grid_consta
                                                              const double* __restrict__ sqsum, float max_norm, float eps,
                                                              float* __restrict__ norm_out) {
   __shared__ double factor;
-  const Piece r = piece_of(tab, gridDim.x - 1 - blockIdx.x);
+  const Piece r = piece_of(tab, gridDim.x - 1 - blockIdx.x);     // searches the parameter: one chunk is all there is
   uint4 v[CLIP_VECS];
   load_piece(v, r, false);
   if (threadIdx.x == 0) {
@@ -322,8 +359,10 @@ template <int LIM>
 __global__ void __cluster_dims__(CLIP_CLUSTER, 1, 1) __launch_bounds__(CLIP_THREADS)
     k_clip_small(const __grid_constant__ ClipTable<LIM> tab, float max_norm, float eps, float* __restrict__ norm_out) {
   __shared__ double mine;
+  __shared__ int chunk0[LIM];
   cg::cluster_group cluster = cg::this_cluster();
-  const double s = block_sum(square_sums(tab, blockIdx.x, CLIP_CLUSTER));
+  copy_chunks(chunk0, tab);
+  const double s = block_sum(square_sums(tab, chunk0, blockIdx.x, CLIP_CLUSTER));
   if (threadIdx.x == 0) mine = s;
   cluster.sync();
   double all = 0.0;
@@ -336,7 +375,7 @@ __global__ void __cluster_dims__(CLIP_CLUSTER, 1, 1) __launch_bounds__(CLIP_THRE
   if (f == 1.0f && tab.in_place) return;
   // first the chunk that this CTA read last
   const int total = tab.chunk0[tab.n], rank = blockIdx.x;
-  if (rank < total) scale_all(tab, rank + (total - 1 - rank) / CLIP_CLUSTER * CLIP_CLUSTER, CLIP_CLUSTER, f, fd);
+  if (rank < total) scale_all(tab, chunk0, rank + (total - 1 - rank) / CLIP_CLUSTER * CLIP_CLUSTER, CLIP_CLUSTER, f, fd);
 }
 
 struct ClipList {
