@@ -50,14 +50,15 @@ struct Lengths { int n[PFX_SLICE]; };
 
 __host__ __device__ inline size_t nodes_per_utt(int beams, int max_frames) { return 1 + (size_t)beams * max_frames; }
 
-// Hash of the prefix x c from that of x.  Two prefixes of one size are taken for equal when their 64-bit
-// hashes are (the finaliser of SplitMix64, Steele et al. 2014, over a sum of the parts): a false match among
-// the at most 32 x 32 pairs of a frame has probability 2^-54, 1e-11 over a million frames.
+// Hash of the prefix x c from that of x: two 32-bit halves, each a bijection of the half for a given label (additions,
+// exclusive ors, shifts and odd factors from the square roots of 2, 3, 5 and 7), short because the search waits for it.  Two prefixes are taken
+// for equal when both halves are: a false match among the at most 32 x 32 pairs of a frame has a chance of 2^-54, 1e-11
+// over a million frames.
 __device__ __forceinline__ unsigned long long grow_hash(unsigned long long h, int c) {
-  unsigned long long z = h + 0x9e3779b97f4a7c15ull * (unsigned long long)(c + 1);
-  z = (z ^ (z >> 30)) * 0xbf58476d1ce4e5b9ull;
-  z = (z ^ (z >> 27)) * 0x94d049bb133111ebull;
-  return z ^ (z >> 31);
+  unsigned lo = ((unsigned)h + (unsigned)c + 1u) * 0x6a09e667u, hi = ((unsigned)(h >> 32) ^ ((unsigned)c + 1u)) * 0xbb67ae85u;
+  lo = (lo ^ (lo >> 15)) * 0x3c6ef373u;
+  hi = (hi ^ (hi >> 13)) * 0xa54ff53bu;
+  return (unsigned long long)hi << 32 | lo;
 }
 
 __device__ __forceinline__ double round24(double p) {
@@ -512,7 +513,8 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
           }
           // a prefix that had left the beam and is back is the parent of slots that stayed
           const bool orphan = live && par < 0 && size > 0 && !grown;
-          if (__any_sync(ALL, orphan)) {
+          const unsigned grew = __ballot_sync(ALL, grown) & SLOTS;
+          if (__any_sync(ALL, orphan) && grew) {
             if (part == 0) sh.grown[slot] = grown ? (unsigned)hash : 0u;
             __syncwarp();
             const unsigned low = (unsigned)up;
@@ -526,7 +528,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
               if (h.w == low) e = i + 3;
             }
             if (__any_sync(ALL, orphan && e >= 0)) {      // all bits, one new prefix after the other
-              unsigned fresh_slots = __ballot_sync(ALL, grown) & SLOTS;
+              unsigned fresh_slots = grew;
               while (fresh_slots) {
                 e = __ffs(fresh_slots) - 1;
                 fresh_slots &= fresh_slots - 1;
