@@ -373,14 +373,14 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
   const bool done = lane < a.B && a.finished && a.finished[row0 + lane];
   const int kind = !isfinite(my_score) ? 0 : done ? 2 : 1;
   const unsigned live = __ballot_sync(0xffffffffu, kind == 1);
-  const int nlive = __popc(live);
+  const int nlive = __popc(live), place = __popc(live & ((1u << lane) - 1));     // of a live beam in the list of these
   if (warp == 0) {
     const unsigned bad = __ballot_sync(0xffffffffu, isnan(my_score) || my_score == CUDART_INF_F);
     if (lane < a.B) {
       sh.score[lane] = my_score;
       sh.kind[lane] = (unsigned char)kind;
     }
-    if (kind == 1) sh.rows[__popc(live & ((1u << lane) - 1))] = lane;
+    if (kind == 1) sh.rows[place] = lane;
     if (lane == 0) {
       sh.nlive = nlive;
       sh.bad = bad != 0;
@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
   double top = -CUDART_INF;
   bool bad_row = false;
   for (int r = first_row; r < nlive; r += row_step) {
-    const int b = (int)__fns(live, 0, r + 1);
+    const int b = __ffs(__ballot_sync(0xffffffffu, kind == 1 && place == r)) - 1;
     const long long row = row0 + b;
     float* mine = bmax + r * nbl;
     const int i0 = ((lane - r * nbl) & 31) + 32 * sub;
