@@ -695,7 +695,7 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const f
 // Bound by HBM.  A CTA takes one tile of 4 KB columns: a persistent grid of such tiles, whose CTAs drift apart, was slower
 // (16 caches [16, 8, 8, 151, 64] bf16: 83 us against 64; 12 caches [8, 4, 8, 2000, 64]: 252 against 194, 8 TB/s written
 // and read as seen by the caller, since shared parents are read once; 12 caches [8, 4, 8, 300, 64] in place with half of
-// the beams moving: 25 against 20).
+// the beams moving: 25 against 16).
 namespace pctc {
 namespace {
 
@@ -733,21 +733,37 @@ struct Parents<32> {
   __device__ __forceinline__ int operator[](int k) const { return p[k]; }
 };
 
+// Pieces of a column that a thread moves: with few beams one is too little work for a CTA's index arithmetic (12 caches
+// [8, 4, 8, 300, 64] in place: 20.5 us with one, 16.1 with two, 18.0 with four); with eight beams two took longer (73
+// against 64 us for 16 caches [16, 8, 8, 151, 64]).
+constexpr __host__ __device__ int move_rows(int KB) { return KB <= 4 ? 2 : 1; }
+
 template <typename U, int KB>
 __device__ __forceinline__ void move_tile(const MoveState& s, const Parents<KB>& par, long long bytes, int n, int seg,
                                           int tile) {
-  const long long at = ((long long)tile * MOVE_THREADS + threadIdx.x) * (int)sizeof(U);
+  constexpr int ROWS = move_rows(KB), STEP = MOVE_THREADS * (int)sizeof(U);
+  const long long at = (long long)tile * ROWS * STEP + threadIdx.x * (int)sizeof(U);
   if (at >= bytes) return;
   const bool in_place = s.src == s.dst;
   const char* src = s.src + n * s.src_n + seg * s.seg + at;
   char* dst = s.dst + n * s.dst_n + seg * s.seg + at;
-  U v[KB];
+  U v[ROWS][KB];
 #pragma unroll
-  for (int k = 0; k < KB; ++k)
-    if (par[k] >= 0 && !(in_place && par[k] == k)) v[k] = *(const U*)(src + par[k] * s.src_b);
+  for (int k = 0; k < KB; ++k) {
+    if (par[k] < 0 || (in_place && par[k] == k)) continue;
+    const char* from = src + par[k] * s.src_b;
 #pragma unroll
-  for (int k = 0; k < KB; ++k)
-    if (par[k] >= 0 && !(in_place && par[k] == k)) *(U*)(dst + k * s.dst_b) = v[k];
+    for (int q = 0; q < ROWS; ++q)
+      if (at + q * STEP < bytes) v[q][k] = *(const U*)(from + q * STEP);
+  }
+#pragma unroll
+  for (int k = 0; k < KB; ++k) {
+    if (par[k] < 0 || (in_place && par[k] == k)) continue;
+    char* to = dst + k * s.dst_b;
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q)
+      if (at + q * STEP < bytes) *(U*)(to + q * STEP) = v[q][k];
+  }
 }
 
 template <int LIM, int KB>
@@ -894,7 +910,7 @@ pctc_status_t move_all(const pctc_beam_state_t* st, int n, int N, int B, int K, 
       const size_t all = (size_t)m.src | (size_t)m.dst | (size_t)(m.src_n | m.src_b | m.dst_n | m.dst_b | m.seg | m.unit);
       m.width = 16;
       while (all & (size_t)(m.width - 1)) m.width /= 2;
-      const long long per = (long long)MOVE_THREADS * m.width, t = (len + per - 1) / per;
+      const long long per = (long long)move_rows(K) * MOVE_THREADS * m.width, t = (len + per - 1) / per;
       if (t > 0x7fffffffLL) return PCTC_ERR_UNSUPPORTED;
       m.tiles = (int)t;
       tab.tile0[tab.n++] = (int)tiles;
