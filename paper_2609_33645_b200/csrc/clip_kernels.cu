@@ -10,7 +10,7 @@
 //
 // Measured: 156M bf16 values into another buffer 140 us (three passes of 312 MB at the rate of a copy: 143; the last 64 MB
 // of the first pass are still in L2 for the second); 64M bf16 values in 384 tensors, in place below the limit, 27 us
-// (one pass: 20; a bare read of the same bytes: 23); 100,000 fp32 values in 7 tensors 8.2 us in one launch (5.5 in two,
+// (one pass: 20; a bare read of the same bytes: 23); 100,000 fp32 values in 7 tensors 6.8 us in one launch (5.5 in two,
 // which cost the host 6 us more).
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
@@ -354,28 +354,42 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_scale_each(const __grid_consta
   scale_chunk(tab, r, v, f, fd);
 }
 
-// Few values: all of it in one launch, by one cluster of CTAs that add their sums up in distributed shared memory.
+// Few values: all of it in one launch, by one cluster of CTAs that add their sums up in distributed shared memory.  A CTA
+// keeps its chunks (at most four) in registers from the sum to the scaling, so that every value is read once.
 template <int LIM>
 __global__ void __cluster_dims__(CLIP_CLUSTER, 1, 1) __launch_bounds__(CLIP_THREADS)
     k_clip_small(const __grid_constant__ ClipTable<LIM> tab, float max_norm, float eps, float* __restrict__ norm_out) {
+  constexpr int MOST = CLIP_CLUSTER_CHUNKS / CLIP_CLUSTER;
   __shared__ double mine;
-  __shared__ int chunk0[LIM];
   cg::cluster_group cluster = cg::this_cluster();
-  copy_chunks(chunk0, tab);
-  const double s = block_sum(square_sums(tab, chunk0, blockIdx.x, CLIP_CLUSTER));
+  const int total = tab.chunk0[tab.n], rank = blockIdx.x;
+  Piece r[MOST];
+  uint4 v[MOST][CLIP_VECS];
+#pragma unroll
+  for (int u = 0; u < MOST; ++u) {
+    const int c = rank + u * CLIP_CLUSTER;
+    if (c < total) {
+      r[u] = piece_of(tab, c);
+      load_piece(v[u], r[u], true);
+    }
+  }
+  double acc = 0.0;
+#pragma unroll
+  for (int u = 0; u < MOST; ++u)
+    if (rank + u * CLIP_CLUSTER < total) acc += piece_squares(v[u], r[u]);
+  const double s = block_sum(acc);
   if (threadIdx.x == 0) mine = s;
   cluster.sync();
   double all = 0.0;
 #pragma unroll
-  for (int r = 0; r < CLIP_CLUSTER; ++r) all += *cluster.map_shared_rank(&mine, r);
+  for (int o = 0; o < CLIP_CLUSTER; ++o) all += *cluster.map_shared_rank(&mine, o);
   cluster.sync();                                 // nobody leaves before all have read
   const double norm = sqrt(all), fd = factor_of(norm, max_norm, eps);
   const float f = (float)fd;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-  if (f == 1.0f && tab.in_place) return;
-  // first the chunk that this CTA read last
-  const int total = tab.chunk0[tab.n], rank = blockIdx.x;
-  if (rank < total) scale_all(tab, chunk0, rank + (total - 1 - rank) / CLIP_CLUSTER * CLIP_CLUSTER, CLIP_CLUSTER, f, fd);
+  if (rank == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+#pragma unroll
+  for (int u = 0; u < MOST; ++u)
+    if (rank + u * CLIP_CLUSTER < total && !(f == 1.0f && (r[u].kind & IN_PLACE))) scale_chunk(tab, r[u], v[u], f, fd);
 }
 
 struct ClipList {
