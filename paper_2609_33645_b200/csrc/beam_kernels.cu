@@ -15,7 +15,7 @@
 // beams x 151,936: 64 x 8 bf16 55 us against 41, 2 x 8 bf16 24.5 against 13.0, 1 x 4 fp32 14.4 against 11.1).
 //
 // Measured: 64 x 8 x 151,936 bf16 with a tenth of the beams ended, 140 MB: 41 us (21 at the rate of a copy), of which the
-// stream takes 31 and the ranking 8 to 9; 1 x 4 fp32: 11 us, of which 3 and 7.  The stream is bound by no single thing:
+// stream takes 31 and the ranking 9 to 10; 1 x 4 fp32: 12 us, of which 3 and 9.  The stream is bound by no single thing:
 // special function unit 62% busy (16 exponentials a cycle and SM are hardly more than the 12 bf16 logits that HBM
 // delivers), issue slots 55%, HBM 68%.  More blocks in flight, more or fewer warps a CTA, and longer stretches measured
 // the same; a quarter of the exponentials as polynomials on the FMA pipe made the whole call 10% slower.  The ranking is a
@@ -47,7 +47,7 @@ constexpr int STREAM_CTAS = 592;                  // CTAs of the first launch th
 constexpr int SEL_BLOCK = 512;                    // logits per maximum: 16 a lane
 constexpr int SEL_LANE = SEL_BLOCK / 32;
 constexpr int SEL_MAX_BLOCKS = 512;               // blocks a CTA reads again
-constexpr int SEL_MAX_CAND = 1280;
+constexpr int SEL_MAX_CAND = 2048;
 constexpr long long SEL_MAX_V = 1 << 21;
 constexpr int SEL_MAX_DYN = SEL_MAX * (int)(SEL_MAX_V / SEL_BLOCK) / SEL_MAX_CLUSTER * 4;   // maxima of a CTA
 
@@ -240,6 +240,7 @@ struct SelShared {
   double bound[SEL_MAX_CLUSTER];                  // per CTA: K of its candidates reach this score
   int warp_count[SEL_WARPS];
   int nblocks, nequal, ncand, overflow;
+  long long raised;                               // a higher threshold that K candidates of a block reach (see there)
   int blocks[SEL_MAX_BLOCKS];
   Cand cand[SEL_MAX_CAND];
   Cand best[SEL_WARPS];
@@ -385,6 +386,7 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
       sh.nlive = nlive;
       sh.bad = bad != 0;
       sh.nblocks = sh.nequal = sh.ncand = sh.overflow = 0;
+      sh.raised = (long long)0x8000000000000000ull;
     }
   }
 
@@ -496,32 +498,85 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
   }
 
   // ---- single logits of those blocks, to the first CTA's list ----
-  SelShared* head = cluster.map_shared_rank(&sh, 0);
-  auto found = [&](double score, int b, int v) {
-    const int p = atomicAdd(&head->ncand, 1);
-    if (p < SEL_MAX_CAND) head->cand[p] = Cand{score, (unsigned long long)b << 32 | (unsigned)v};
-  };
   const int nblk = sh.nblocks < SEL_MAX_BLOCKS ? sh.nblocks : SEL_MAX_BLOCKS;
-  for (int i = warp; i < nblk; i += SEL_WARPS) {
-    const int e = sh.blocks[i], r = e / nbl, b = sh.rows[r], v0 = (b0 + e - r * nbl) * SEL_BLOCK;
-    Block<T, VEC> raw;
+  float x[SEL_LANE];
+  int b = 0, v0 = 0, loaded = -1;                 // beam and first token of the block in x
+  auto load_block = [&](int i) {
+    if (loaded == i) return;
+    const int e = sh.blocks[i], r = e / nbl;
+    b = sh.rows[r];
+    v0 = (b0 + e - r * nbl) * SEL_BLOCK;
     const T* p = base + b * a.stride_b + v0;
+    Block<T, VEC> raw;
     if (v0 + SEL_BLOCK <= a.V) raw.load(p + Block<T, VEC>::first(lane)); else raw.load_part(p, a.V - v0, lane);
-    float x[SEL_LANE];
     raw.get(x);
-    const double offset = sh.lse[b], score = sh.score[b];
-    auto cand = [&](int q) { return score + ((double)x[q] - offset); };
-    int reach = 0;
+    loaded = i;
+  };
+  auto cand = [&](int q) { return (double)sh.score[b] + ((double)x[q] - sh.lse[b]); };
+  // A logit under this cannot reach `least` (64-bit rounding allowed for): single precision decides for nearly all.
+  auto floor_of = [&](double least) {
+    const double score = sh.score[b], lse = sh.lse[b], t = (least - score) + lse;
+    return __double2float_rd(t - (fabs(t) + fabs(score) + fabs(lse)) * 1e-12);
+  };
+  auto reaching = [&](float least) {              // of the block's logits
+    int n = 0;
 #pragma unroll
-    for (int q = 0; q < SEL_LANE; ++q) reach += cand(q) >= thr && cand(q) > -CUDART_INF;
-    if ((int)__reduce_add_sync(0xffffffffu, reach) <= a.K) {
+    for (int q = 0; q < SEL_LANE; ++q) n += x[q] >= least && x[q] > -CUDART_INF_F;
+    return (int)__reduce_add_sync(0xffffffffu, n);
+  };
+  // Where one beam is far ahead and a row has few blocks, these hold many logits that reach the threshold.  A block with
+  // more than K of them raises it, to the K-th best of the 64 maxima of eight of its logits each (47 x 16 x 3,719, K = 16:
+  // 24 us, 45 without; rows of many blocks have no need of it).
+  bool raised = false;
+  for (int i = warp; i < nblk && a.nb <= 8 * a.K; i += SEL_WARPS) {
+    load_block(i);
+    if (reaching(floor_of(thr)) <= a.K) continue;
+    float h0 = x[0], h1 = x[8];
+#pragma unroll
+    for (int q = 1; q < 8; ++q) { h0 = fmaxf(h0, x[q]); h1 = fmaxf(h1, x[q + 8]); }
+    int above0 = 0, above1 = 0;
+#pragma unroll 8
+    for (int l = 0; l < 32; ++l) {
+      const float o0 = __shfl_sync(0xffffffffu, h0, l), o1 = __shfl_sync(0xffffffffu, h1, l);
+      above0 += (o0 > h0) + (o1 > h0);
+      above1 += (o0 > h1) + (o1 > h1);
+    }
+    const float kth = -warp_max(-fminf(above0 < a.K ? h0 : CUDART_INF_F, above1 < a.K ? h1 : CUDART_INF_F));
+    const double bound = (double)sh.score[b] + ((double)kth - sh.lse[b]);
+    if (kth > -CUDART_INF_F && bound > thr) {
+      raised = true;
+      // doubles in the order of integers
+      long long key = __double_as_longlong(bound);
+      key ^= (key >> 63) & 0x7fffffffffffffffll;
+      if (lane == 0) atomicMax(&sh.raised, key);
+    }
+  }
+  if (__syncthreads_or(raised)) {
+    long long key = sh.raised;
+    key ^= (key >> 63) & 0x7fffffffffffffffll;
+    thr = __longlong_as_double(key);
+  }
+  SelShared* head = cluster.map_shared_rank(&sh, 0);
+  auto found = [&](double score, int beam, int v) {
+    const int p = atomicAdd(&head->ncand, 1);
+    if (p < SEL_MAX_CAND) head->cand[p] = Cand{score, (unsigned long long)beam << 32 | (unsigned)v};
+  };
+  for (int i = warp; i < nblk; i += SEL_WARPS) {
+    load_block(i);
+    const float least = floor_of(thr);
+    const int reach = reaching(least);
+    if (reach == 0) continue;
+    if (reach <= 2 * a.K) {
 #pragma unroll
       for (int q = 0; q < SEL_LANE; ++q)
-        if (cand(q) >= thr && cand(q) > -CUDART_INF) found(cand(q), b, v0 + Block<T, VEC>::index(lane, q));
+        if (x[q] >= least && x[q] > -CUDART_INF_F) {
+          const double s = cand(q);
+          if (s >= thr) found(s, b, v0 + Block<T, VEC>::index(lane, q));
+        }
       continue;
     }
     unsigned used = 0;
-    for (int k = 0; k < a.K; ++k) {               // the K best of the block, one by one
+    for (int k = 0; k < a.K; ++k) {               // ties: the K best of the block, one by one
       double best = -CUDART_INF;
       int at = 0x7fffffff, q0 = 0;
 #pragma unroll
@@ -590,7 +645,7 @@ SelWorkspace workspace_of(const pctc_beam_t* p) {
   SelWorkspace w;
   w.nb = (int)((p->V + SEL_BLOCK - 1) / SEL_BLOCK);
   const size_t rows = (size_t)p->N * p->B;
-  w.per = 8;
+  w.per = std::min(8, (w.nb + STREAM_WARPS - 1) / STREAM_WARPS);
   do w.parts = (w.nb + STREAM_WARPS * w.per - 1) / (STREAM_WARPS * w.per);
   while (rows * w.parts < STREAM_CTAS && w.per > 1 && (w.per /= 2));
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
