@@ -390,8 +390,8 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* problem, const void* logits, c
  * unit_bytes each; with timed = 1 only the first lengths[n] units of every piece are moved and those behind
  * are left as they are.  A cache [N,B,heads,L,D] is heads segments of L units of D values; a state [N,B,D]
  * is one segment of one unit.  src and dst share that layout and may have other beam and utterance strides.
- * What is written may overlap nothing else of the list: a state given twice, or rows into each other, is
- * refused (PCTC_ERR_INVALID_ARG); views of one buffer that interleave row by row are told apart where
+ * What is written may overlap nothing else of the call: a state given twice, rows into each other, or a state that
+ * holds the parents or lengths themselves, is refused (PCTC_ERR_INVALID_ARG); views of one buffer that interleave row by row are told apart where
  * their beam strides are equal.  16-byte aligned addresses, strides and units are moved fastest.
  */
 typedef struct {
@@ -424,7 +424,7 @@ pctc_status_t pctc_beam_reorder(int32_t n_states, const pctc_beam_state_t* state
  *          (grads[i] and outs[i] equally far from a 16-byte boundary) are read and written fastest.
  *   numels [n] (0 allowed, its pointers are then not looked at), dtypes [n] pctc_dtype_t,
  *   out_dtypes [n] or NULL (as dtypes): dtypes[i] or PCTC_FP32.
- * No written buffer may overlap another buffer of the list (PCTC_ERR_INVALID_ARG); the same gradient
+ * No written buffer may overlap another one of the call, norm and workspace included (PCTC_ERR_INVALID_ARG); the same gradient
  * may be read twice, and then counts twice.  max_norm > 0 (+inf: the norm only), eps >= 0.
  *
  * pctc_clip_grad_norm does it all; norm [1] fp32 (device).  For gradients that are sharded over ranks,

@@ -256,16 +256,10 @@ __device__ __forceinline__ void join(float& m, double& s) {
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
 }
 
-template <typename T>
-__device__ __forceinline__ Cand candidate(const SelShared& sh, const T* base, long long stride_b, int b, int v) {
-  Cand c;
-  c.score = (double)sh.score[b] + ((double)(float)base[b * stride_b + v] - sh.lse[b]);
-  c.at = (unsigned long long)b << 32 | (unsigned)v;
-  return c;
-}
-
 // The K best by K passes over all candidates, each for the best one behind the last: for inputs whose ties or
-// order leave more candidates than the lists hold.  Called by all threads of one CTA.
+// order leave more candidates than the lists hold.  A thread meets its candidates in their order, so that one that ties
+// with the last is the best it can find.  Called by all threads of one CTA.
+// Measured: 8 x 32 x 151,936 bf16, K = 32, all logits equal: 1.5 ms (79 one logit at a time and to the end of every row).
 template <typename T>
 __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -273,12 +267,21 @@ __device__ void select_by_passes(SelShared& sh, const SelArgs& a, const T* base)
   int found = 0;
   for (int k = 0; k < a.K; ++k) {
     Cand best{-CUDART_INF, ~0ull};
-    for (int i = 0; i < sh.nlive; ++i) {
+    for (int i = 0; i < sh.nlive && best.score != last.score; ++i) {
       const int b = sh.rows[i];
-      if (isnan(sh.lse[b])) continue;
-      for (int v = tid; v < a.V; v += SEL_THREADS) {
-        const Cand c = candidate(sh, base, a.stride_b, b, v);
-        if (c.score > -CUDART_INF && before(last, c) && before(c, best)) best = c;
+      const double score = sh.score[b], lse = sh.lse[b];
+      if (isnan(lse)) continue;
+      const T* row = base + b * a.stride_b;
+      constexpr int AHEAD = 8;
+      for (int v0 = tid; v0 < a.V && best.score != last.score; v0 += AHEAD * SEL_THREADS) {
+        float x[AHEAD];
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) x[q] = v0 + q * SEL_THREADS < a.V ? (float)row[v0 + q * SEL_THREADS] : -CUDART_INF_F;
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+          const Cand c{score + ((double)x[q] - lse), (unsigned long long)b << 32 | (unsigned)(v0 + q * SEL_THREADS)};
+          if (c.score > -CUDART_INF && before(last, c) && before(c, best)) best = c;
+        }
       }
     }
     if (tid < a.B && sh.kind[tid] == 2) {
@@ -707,6 +710,7 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const f
   if (workspace_bytes < w.total) return PCTC_ERR_WORKSPACE_TOO_SMALL;
   if (!logits || !scores || !scores_out || !parents || !tokens) return PCTC_ERR_INVALID_ARG;
   if (finished && p->eos_id < 0) return PCTC_ERR_INVALID_ARG;
+  if (p->K != p->B && (scores_out == scores || (finished && finished_out == finished))) return PCTC_ERR_INVALID_ARG;
   const size_t es = p->dtype == PCTC_BF16 ? 2 : 4;
   if ((size_t)logits & (es - 1)) return PCTC_ERR_INVALID_ARG;
   if (((size_t)scores | (size_t)scores_out | (size_t)parents | (size_t)tokens) & 3) return PCTC_ERR_INVALID_ARG;
@@ -881,7 +885,7 @@ bool rows_clash(const RowSet& a, const RowSet& b, int N) {
 
 pctc_status_t check_move(const pctc_beam_state_t* st, int n, int N, int B, int K, const int32_t* lengths) {
   if (n < 0 || N <= 0 || B <= 0 || K <= 0 || (n && !st)) return PCTC_ERR_INVALID_ARG;
-  if (B > SEL_MAX || K > SEL_MAX) return PCTC_ERR_UNSUPPORTED;
+  if (B > SEL_MAX || K > SEL_MAX || N > 0x7fffffff / SEL_MAX) return PCTC_ERR_UNSUPPORTED;
   for (int i = 0; i < n; ++i) {
     const pctc_beam_state_t& s = st[i];
     if (!s.src || !s.dst || s.segments <= 0 || s.units < 0 || s.unit_bytes <= 0) return PCTC_ERR_INVALID_ARG;
@@ -894,7 +898,7 @@ pctc_status_t check_move(const pctc_beam_state_t* st, int n, int N, int B, int K
     if (s.segments > 1 && (s.segment_stride < len || s.segment_stride > most / s.segments)) return PCTC_ERR_INVALID_ARG;
     const long long row = (s.segments - 1) * s.segment_stride + len;
     if (s.src_stride_b < 0 || s.dst_stride_b < 0 || s.src_stride_n < 0 || s.dst_stride_n < 0) return PCTC_ERR_INVALID_ARG;
-    if (s.src_stride_b > most || s.dst_stride_b > most || s.src_stride_n > most || s.dst_stride_n > most)
+    if (s.src_stride_b > most || s.dst_stride_b > most || s.src_stride_n > most / N || s.dst_stride_n > most / N)
       return PCTC_ERR_UNSUPPORTED;
     // written rows are apart: beams inside utterances, or utterances inside beams
     const long long sn = N > 1 ? s.dst_stride_n : most, sb = K > 1 ? s.dst_stride_b : most;
@@ -908,11 +912,14 @@ pctc_status_t check_move(const pctc_beam_state_t* st, int n, int N, int B, int K
   return PCTC_OK;
 }
 
-// What the call writes may overlap nothing else of the list (in place: a state's own rows, which are one set).
-pctc_status_t check_overlap(const pctc_beam_state_t* st, int n, int N, int B, int K) {
-  RowSet* r = new (std::nothrow) RowSet[2 * (size_t)(n > 0 ? n : 1)];
+// What the call writes may overlap nothing else that it takes (in place: a state's own rows, which are one set).
+pctc_status_t check_overlap(const pctc_beam_state_t* st, int n, int N, int B, int K, const int32_t* parents,
+                            const int32_t* lengths) {
+  RowSet* r = new (std::nothrow) RowSet[2 * (size_t)n + 2];
   if (!r) return PCTC_ERR_HOST_MEMORY;
   int m = 0;
+  r[m++] = RowSet{(size_t)parents, 4LL * K, 4LL * K, 4LL * K, 1, false};
+  if (lengths) r[m++] = RowSet{(size_t)lengths, 4, 4, 4, 1, false};
   for (int i = 0; i < n; ++i) {
     const pctc_beam_state_t& s = st[i];
     const long long row = (s.segments - 1) * s.segment_stride + s.units * s.unit_bytes;
@@ -994,7 +1001,7 @@ pctc_status_t pctc_beam_reorder(int32_t n_states, const pctc_beam_state_t* state
   pctc_status_t st = check_move(states, n_states, N, B, K, lengths);
   if (st != PCTC_OK) return st;
   if (!parents || ((size_t)parents & 3) || ((size_t)lengths & 3)) return PCTC_ERR_INVALID_ARG;
-  st = check_overlap(states, n_states, N, B, K);
+  st = check_overlap(states, n_states, N, B, K, parents, lengths);
   if (st != PCTC_OK) return st;
   cudaStream_t stream = (cudaStream_t)stream_v;
   return n_states <= MOVE_SMALL ? move_all<MOVE_SMALL>(states, n_states, N, B, K, parents, lengths, stream)

@@ -406,8 +406,9 @@ struct ClipList {
 
 int elem_bytes(int dtype) { return dtype == PCTC_BF16 ? 2 : 4; }
 
-// Host checks of the list.  `writes`: the call scales, so that what it writes may overlap nothing else.
-pctc_status_t check_list(const ClipList& l, bool writes) {
+// Host checks of the list.  `writes`: the call scales, so that what it writes may overlap nothing else; `own` is the
+// norm, and the workspace or the sum of squares.
+pctc_status_t check_list(const ClipList& l, bool writes, Span own0, Span own1) {
   if (l.n < 0) return PCTC_ERR_INVALID_ARG;
   if (l.n && (!l.grads || !l.numels || !l.dtypes)) return PCTC_ERR_INVALID_ARG;
   for (int i = 0; i < l.n; ++i) {
@@ -421,15 +422,17 @@ pctc_status_t check_list(const ClipList& l, bool writes) {
     if (!l.out(i) || ((size_t)l.out(i) & (elem_bytes(l.out_dtype(i)) - 1))) return PCTC_ERR_INVALID_ARG;
     if (l.out(i) == l.in(i) && l.out_dtype(i) != l.dtypes[i]) return PCTC_ERR_INVALID_ARG;
   }
-  if (!writes || l.n == 0) return PCTC_OK;
-  Span* spans = new (std::nothrow) Span[2 * (size_t)l.n];
+  if (l.n == 0) return PCTC_OK;
+  Span* spans = new (std::nothrow) Span[2 * (size_t)l.n + 2];
   if (!spans) return PCTC_ERR_HOST_MEMORY;
   size_t ns = 0;
+  for (const Span& own : {own0, own1})
+    if (own.lo < own.hi) spans[ns++] = own;
   for (int i = 0; i < l.n; ++i) {
     if (l.numels[i] == 0) continue;
     const size_t a = (size_t)l.in(i), b = (size_t)l.out(i);
-    spans[ns++] = Span{b, b + (size_t)l.numels[i] * elem_bytes(l.out_dtype(i)), true};
-    if (a != b) spans[ns++] = Span{a, a + (size_t)l.numels[i] * elem_bytes(l.dtypes[i]), false};
+    if (writes) spans[ns++] = Span{b, b + (size_t)l.numels[i] * elem_bytes(l.out_dtype(i)), true};
+    if (!writes || a != b) spans[ns++] = Span{a, a + (size_t)l.numels[i] * elem_bytes(l.dtypes[i]), false};
   }
   const bool clash = spans_conflict(spans, ns);
   delete[] spans;
@@ -548,6 +551,7 @@ pctc_status_t clip_call(const ClipList& l, const double* given, double* partial,
 bool bad_limits(float max_norm, float eps) {
   return !(max_norm > 0.f) || !(eps >= 0.f) || std::isinf(eps);
 }
+Span span(const void* p, size_t bytes, bool write) { return Span{(size_t)p, p ? (size_t)p + bytes : 0, write}; }
 size_t partial_count(int n) { return 32 + (size_t)CLIP_MAX_GRID * (n <= CLIP_LARGE ? 1 : ((size_t)n + CLIP_LARGE - 1) / CLIP_LARGE); }
 
 }  // namespace
@@ -566,10 +570,11 @@ pctc_status_t pctc_clip_workspace_bytes(int32_t n, size_t* bytes_out) {
 pctc_status_t pctc_grad_sqsum(int32_t n, const void* const* grads, const int64_t* numels, const int32_t* dtypes,
                               double* sqsum, void* workspace, size_t workspace_bytes, void* stream_v) {
   const ClipList l{n, grads, nullptr, numels, dtypes, nullptr};
-  pctc_status_t st = check_list(l, false);
+  const size_t need = partial_count(n) * sizeof(double);
+  pctc_status_t st = check_list(l, false, span(sqsum, 8, true), span(workspace, need, true));
   if (st != PCTC_OK) return st;
   if (!sqsum || ((size_t)sqsum & 7) || !workspace || ((size_t)workspace & 255)) return PCTC_ERR_INVALID_ARG;
-  if (workspace_bytes < partial_count(n) * sizeof(double)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < need) return PCTC_ERR_WORKSPACE_TOO_SMALL;
   return clip_call(l, nullptr, (double*)workspace, sqsum, 0.f, 0.f, nullptr, stream_v);
 }
 
@@ -577,7 +582,7 @@ pctc_status_t pctc_grad_scale(int32_t n, const void* const* grads, void* const* 
                               const int32_t* dtypes, const int32_t* out_dtypes, const double* sqsum, float max_norm,
                               float eps, float* norm, void* stream_v) {
   const ClipList l{n, grads, outs, numels, dtypes, out_dtypes};
-  pctc_status_t st = check_list(l, true);
+  pctc_status_t st = check_list(l, true, span(norm, 4, true), span(sqsum, 8, false));
   if (st != PCTC_OK) return st;
   if (!sqsum || ((size_t)sqsum & 7) || bad_limits(max_norm, eps)) return PCTC_ERR_INVALID_ARG;
   return clip_call(l, sqsum, nullptr, nullptr, max_norm, eps, norm, stream_v);
@@ -587,10 +592,11 @@ pctc_status_t pctc_clip_grad_norm(int32_t n, const void* const* grads, void* con
                                   const int32_t* dtypes, const int32_t* out_dtypes, float max_norm, float eps,
                                   float* norm, void* workspace, size_t workspace_bytes, void* stream_v) {
   const ClipList l{n, grads, outs, numels, dtypes, out_dtypes};
-  pctc_status_t st = check_list(l, true);
+  const size_t need = partial_count(n) * sizeof(double);
+  pctc_status_t st = check_list(l, true, span(norm, 4, true), span(workspace, need, true));
   if (st != PCTC_OK) return st;
   if (!norm || !workspace || ((size_t)workspace & 255) || bad_limits(max_norm, eps)) return PCTC_ERR_INVALID_ARG;
-  if (workspace_bytes < partial_count(n) * sizeof(double)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < need) return PCTC_ERR_WORKSPACE_TOO_SMALL;
   return clip_call(l, nullptr, (double*)workspace, nullptr, max_norm, eps, norm, stream_v);
 }
 

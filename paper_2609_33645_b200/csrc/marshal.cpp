@@ -267,14 +267,14 @@ PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
   p.dtype = x.scalar_type() == at::kFloat ? PCTC_FP32 : PCTC_BF16;
   p.eos_id = (int32_t)eos;
   const c10::cuda::CUDAGuard guard(dev);
+  size_t need = 0;
+  check(api.beam_workspace_bytes(&p, &need), "pctc_beam_workspace_bytes");
   Shared out(dev);
   for (const at::ScalarType type : {at::kFloat, at::kInt, at::kInt, at::kBool}) out.add({N, K}, type);
   out.add({N}, at::kInt);
   out.allocate();
   const at::Tensor scores = out.get(0), parents = out.get(1), tokens = out.get(2), finished = out.get(3), flags = out.get(4);
-  size_t need = 0;
-  check(api.beam_workspace_bytes(&p, &need), "pctc_beam_workspace_bytes");
-  const at::Tensor ws = need ? empty({(int64_t)need}, at::kByte, dev) : at::Tensor();
+  const at::Tensor ws = empty({(int64_t)need}, at::kByte, dev);
   check(api.beam_select(&p, ptr(x), (const float*)ptr(s), (const uint8_t*)ptr(f), (float*)ptr(scores),
                         (int32_t*)ptr(parents), (int32_t*)ptr(tokens), (uint8_t*)ptr(finished), (int32_t*)ptr(flags),
                         ptr(ws), need, stream_of(dev)),

@@ -28,7 +28,7 @@ constexpr int PFX_MAX_BEAMS = 32, PFX_MAX_K = 32;
 constexpr int PFX_RESCALE = 16;                   // frames between rescalings: values move by at most 3^16
 constexpr int PFX_TILE = 32;                      // frames whose probabilities are staged at a time
 constexpr int PFX_THREADS = 128;
-constexpr int PFX_LAST_WINDOW = 3072;             // nodes of a window where the search itself reads its hypotheses out
+constexpr int PFX_LAST_WINDOW = 2560;             // nodes of a window where the search itself reads its hypotheses out
 constexpr int PFX_SLICE = 1024;                   // utterances whose lengths one launch takes as a parameter
 
 struct Slots {

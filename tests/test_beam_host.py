@@ -116,6 +116,26 @@ def test_bad_states_are_refused_before_any_launch(lib, states, kw, want):
     assert _reorder(lib, states, **kw) == want
 
 
+@pytest.mark.parametrize("states,kw,want", [
+    ([_state()], dict(parents=AT + 300), 1),                                # the parents are among what is written
+    ([_state(dst=FAR)], dict(parents=FAR + 800 - 4), 1),                   # their first value is the last one written
+    ([_state(dst=FAR)], dict(parents=FAR - 28), 1),                         # their last value the first
+    ([_state(timed=1)], dict(parents=FAR, lengths=AT + 796), 1),
+    ([_state(dst=FAR, src_stride_n=2 ** 46)], {}, 3), ([_state(dst=FAR, dst_stride_n=2 ** 46)], {}, 3),
+    ([_state(dst=FAR)], dict(N=2 ** 26), 3),
+])
+def test_states_that_clash_with_the_rest_of_the_call_are_refused(lib, states, kw, want):
+    assert _reorder(lib, states, **kw) == want
+
+
+@pytest.mark.parametrize("alias", ["scores", "finished"])
+def test_selection_in_place_needs_as_many_beams(lib, alias):
+    p = _problem(K=3, eos_id=0)
+    out, done = (FAR, FAR * 4) if alias == "scores" else (FAR * 2, FAR * 3)
+    assert lib.load().pctc_beam_select(ctypes.byref(p), AT, FAR, FAR * 3, out, FAR * 5, FAR * 6, done, None, FAR * 7,
+                                       1 << 20, None) == 1
+
+
 def test_nothing_to_move_is_no_error(lib):
     assert _reorder(lib, []) == 0
     assert _reorder(lib, [_state(units=0)]) == 0

@@ -18,7 +18,7 @@ def _arr(ctype, values):
     return (ctype * len(values))(*values)
 
 
-def _call(lib, ptrs, numels, dtypes, outs=None, out_dtypes=None, max_norm=1.0, eps=1e-6, norm=BASE, ws=BASE * 64,
+def _call(lib, ptrs, numels, dtypes, outs=None, out_dtypes=None, max_norm=1.0, eps=1e-6, norm=BASE * 32, ws=BASE * 64,
           ws_bytes=1 << 20, n=None):
     return lib.pctc_clip_grad_norm(
         len(ptrs) if n is None else n, _arr(ctypes.c_void_p, ptrs), None if outs is None else _arr(ctypes.c_void_p, outs),
@@ -53,6 +53,25 @@ def _call(lib, ptrs, numels, dtypes, outs=None, out_dtypes=None, max_norm=1.0, e
 ])
 def test_bad_lists_are_refused_before_any_launch(lib, kw, want):
     assert _call(lib.load(), **kw) == want
+
+
+@pytest.mark.parametrize("kw", [
+    dict(ptrs=[BASE * 2], numels=[8], dtypes=[1], norm=BASE * 2 + 28),       # the norm on a gradient's last value
+    dict(ptrs=[BASE * 2], numels=[8], dtypes=[0], norm=BASE, ws=BASE * 2),   # the workspace on a gradient
+    dict(ptrs=[BASE * 2], numels=[8], dtypes=[0], outs=[BASE * 64 + 512]),   # an output in the workspace
+    dict(ptrs=[BASE * 2], numels=[8], dtypes=[0], norm=BASE * 64 + 8),       # the norm in the workspace
+])
+def test_norm_and_workspace_lie_apart_from_the_list(lib, kw):
+    assert _call(lib.load(), **kw) == 1
+
+
+def test_sum_of_squares_lies_apart_from_the_list(lib):
+    f, n = lib.load(), _arr(ctypes.c_int64, [8])
+    grads, kinds = _arr(ctypes.c_void_p, [BASE * 2]), _arr(ctypes.c_int32, [1])
+    assert f.pctc_grad_sqsum(1, grads, n, kinds, BASE * 2 + 24, BASE * 64, 1 << 20, None) == 1
+    assert f.pctc_grad_sqsum(1, grads, n, kinds, BASE, BASE * 2, 1 << 20, None) == 1
+    assert f.pctc_grad_scale(1, grads, None, n, kinds, None, BASE * 2 + 8, 1.0, 1e-6, BASE, None) == 1
+    assert f.pctc_grad_scale(1, grads, None, n, kinds, None, BASE, 1.0, 1e-6, BASE * 2, None) == 1
 
 
 def test_workspace_grows_by_launches_of_1024_tensors(lib):
