@@ -93,6 +93,24 @@ def test_more_ties_than_the_lists_hold():
     check(logits, scores, 32)
 
 
+@pytest.mark.parametrize("V", [151936, 150001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_ties_all_over_a_wide_call(dtype, V):
+    # equal rows of three levels: one token of the highest, a tenth of the middle one, all others of the lowest
+    row = torch.zeros(V, device=DEV)
+    row[torch.randperm(V, generator=torch.Generator().manual_seed(1))[:V // 10].to(DEV)] = 1.0
+    row[V // 2] = 2.0
+    mid = (row == 1.0).nonzero().flatten().cpu().numpy()
+    for B, K in ((31, 32), (32, 32), (28, 30)):
+        r = binding.beam_select(row.to(dtype).expand(2, B, V).contiguous(), torch.full((2, B), -3.0, device=DEV), K)
+        want = [(b, V // 2) for b in range(B)] + [(0, int(v)) for v in mid]
+        for n in range(2):
+            assert list(zip(r["parents"][n].tolist(), r["tokens"][n].tolist())) == want[:K]
+        flat = torch.zeros(2, B, V, device=DEV, dtype=dtype)
+        r = binding.beam_select(flat, torch.zeros(2, B, device=DEV), K)
+        assert r["parents"].eq(0).all() and r["tokens"].eq(torch.arange(K, device=DEV)).all()
+
+
 def test_dead_ended_and_masked():
     logits, scores = make(8, 4, 3000, torch.float32, 5)
     finished = torch.zeros(8, 4, dtype=torch.bool, device=DEV)
