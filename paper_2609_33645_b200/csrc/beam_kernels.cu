@@ -208,14 +208,15 @@ struct Block<T, false> {
 };
 
 // Running sum of exponentials of a lane.  It refers to `ref`, not to the running maximum: that is followed only when
-// it is 40 ahead, far from where exp overflows, so that no block waits for its maximum.
+// it is 4 ahead, so that hardly a block waits for its maximum.  (An exponent d is off by the rounding of the difference, of
+// the product and of log2 e, together under 1.4e-7 |d|: at 4, with the 2^-22 of ex2, 8e-7.)
 struct RunningSum {
   float ref, sum;
   __device__ __forceinline__ void clear() { ref = -CUDART_INF_F; sum = 0.f; }
   // adds a lane's share of a block; m: the block's maximum
   __device__ __forceinline__ void add(const float (&x)[SEL_LANE], float m) {
     float t = lane_exp(x, ref == -CUDART_INF_F ? 0.f : ref);
-    if (!(m <= ref + 40.f)) {                     // the first block with anything in it (or a NaN), and rarely after
+    if (!(m <= ref + 4.f)) {                     // the first block with anything in it (or a NaN), and rarely after
       sum *= exp2_approx((ref - m) * 1.44269504f);
       ref = m;
       t = lane_exp(x, m);

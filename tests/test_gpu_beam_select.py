@@ -93,6 +93,17 @@ def test_more_ties_than_the_lists_hold():
     check(logits, scores, 32)
 
 
+@pytest.mark.parametrize("rise", [0.7, 3.9, 4.1, 7.3, 17.9, 39.37, 41.3, 95.1])
+def test_late_peaks(rise):
+    # a row's sum of exponentials is nearly all its last tokens, whose logits lie `rise` above those before them (so
+    # many rows that a warp goes through several blocks of one)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    logits = torch.randn(160, 4, 9000, generator=g, device=DEV) * 0.05 - rise
+    logits[:, :, -3:] = torch.rand(160, 4, 3, generator=g, device=DEV) * 0.3
+    check(logits, torch.rand(160, 4, generator=g, device=DEV) * 0.1, 4)
+    check(logits.to(torch.bfloat16), torch.rand(160, 4, generator=g, device=DEV) * 0.1, 4)
+
+
 @pytest.mark.parametrize("V", [151936, 150001])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_ties_all_over_a_wide_call(dtype, V):
