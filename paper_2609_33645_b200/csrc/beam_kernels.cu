@@ -565,7 +565,8 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
     const int p = atomicAdd(&head->ncand, 1);
     if (p < SEL_MAX_CAND) head->cand[p] = Cand{score, (unsigned long long)beam << 32 | (unsigned)v};
   };
-  for (int i = warp; i < nblk; i += SEL_WARPS) {
+  // backwards: the last one is in registers still
+  for (int i = nblk > warp ? warp + (nblk - 1 - warp) / SEL_WARPS * SEL_WARPS : -1; i >= 0; i -= SEL_WARPS) {
     load_block(i);
     const float least = floor_of(thr);
     const int reach = reaching(least);
@@ -618,12 +619,16 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
     a.tokens[o] = token;
     if (a.finished_out) a.finished_out[o] = parent >= 0 && (sh.kind[parent] == 2 || token == a.eos);
   };
-  for (int i = tid; i < nc; i += SEL_THREADS) {
-    const Cand x = sh.cand[i];
+  int lanes = 1;                                  // that count for one candidate
+  while (lanes < 32 && 2 * lanes * nc <= SEL_THREADS) lanes *= 2;
+  for (int i0 = 0; i0 < nc; i0 += SEL_THREADS / lanes) {
+    const int i = i0 + tid / lanes;
+    const Cand x = sh.cand[min(i, nc - 1)];
     int rank = 0;
 #pragma unroll 8
-    for (int j = 0; j < nc; ++j) rank += before(sh.cand[j], x);
-    if (rank < a.K) put(rank, x.score, (int)(x.at >> 32), (int)(unsigned)x.at);
+    for (int j = tid % lanes; j < nc; j += lanes) rank += before(sh.cand[j], x);
+    for (int o = 1; o < lanes; o *= 2) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+    if (i < nc && tid % lanes == 0 && rank < a.K) put(rank, x.score, (int)(x.at >> 32), (int)(unsigned)x.at);
   }
   for (int k = nc + tid; k < a.K; k += SEL_THREADS) put(k, -CUDART_INF, -1, -1);
   if (tid == 0 && a.flags) a.flags[n] = sh.bad ? PCTC_UTT_NONFINITE : 0;
