@@ -530,9 +530,9 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
   };
   // Where one beam is far ahead and a row has few blocks, these hold many logits that reach the threshold.  A block with
   // more than K of them raises it, to the K-th best of the 64 maxima of eight of its logits each (47 x 16 x 3,719, K = 16:
-  // 24 us, 45 without; rows of many blocks have no need of it).
+  // 20 us, 45 without; rows of many blocks have no need of it).
   bool raised = false;
-  for (int i = warp; i < nblk && a.nb <= 8 * a.K; i += SEL_WARPS) {
+  for (int i = warp; i < nblk && a.nb <= 2 * a.K; i += SEL_WARPS) {
     load_block(i);
     if (reaching(floor_of(thr)) <= a.K) continue;
     float h0 = x[0], h1 = x[8];
