@@ -391,8 +391,8 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* problem, const void* logits, c
  * are left as they are.  A cache [N,B,heads,L,D] is heads segments of L units of D values; a state [N,B,D]
  * is one segment of one unit.  src and dst share that layout and may have other beam and utterance strides.
  * What is written may overlap nothing else of the call: a state given twice, rows into each other, or a state that
- * holds the parents or lengths themselves, is refused (PCTC_ERR_INVALID_ARG); views of one buffer that interleave row by row are told apart where
- * their beam strides are equal.  16-byte aligned addresses, strides and units are moved fastest.
+ * holds the parents or lengths themselves, is refused (PCTC_ERR_INVALID_ARG).  Views of one buffer that interleave by beam or by
+ * utterance are told apart where their strides are equal ([N,2,B,...] and [N,B,2,...] among them).  16-byte aligned addresses, strides and units are moved fastest.
  */
 typedef struct {
   const void* src;

@@ -878,15 +878,39 @@ struct RowSet {
   bool write;
   size_t end(int N) const { return base + (size_t)((N - 1) * outer + (rows - 1) * inner + len); }
 };
-// Whether two sets of rows share a byte.  Exact where one set's rows repeat with the other's beam stride (views of
-// one buffer); otherwise ranges that interleave count as shared.
+// One of the two levels of a pair of such sets: how often each repeats, and the stride that they have in common.
+struct Level {
+  long long na, nb, stride;
+};
+// Whether f(d + t * stride) holds for one of the shifts t that bring an extent of b, d behind a's, to a's extent.
+template <typename F>
+bool meets(const Level& l, long long d, long long extent_a, long long extent_b, F f) {
+  if (l.na == 1 && l.nb == 1) return d < extent_a && -d < extent_b && f(d);
+  if (l.stride <= 0) return true;
+  const long long least = -extent_b - d, down = least / l.stride - (least % l.stride < 0);
+  for (long long t = std::max(down + 1, 1 - l.na); t < l.nb && d + t * l.stride < extent_a; ++t)
+    if (f(d + t * l.stride)) return true;
+  return false;
+}
+// Whether two sets of rows share a byte.  Exact where they repeat with the same strides (views of one buffer, whether
+// they interleave by beam or by utterance), or lie apart within one beam stride; other ranges that interleave count as
+// shared.
 bool rows_clash(const RowSet& a, const RowSet& b, int N) {
   if (a.end(N) <= b.base || b.end(N) <= a.base) return false;
-  if (a.inner != b.inner || a.inner <= 0 || a.len > a.inner || b.len > b.inner) return true;
-  if (N > 1 && (a.outer % a.inner || b.outer % b.inner)) return true;
-  const long long d = (long long)((a.base > b.base ? a.base - b.base : b.base - a.base) % (size_t)a.inner);
-  const long long first = a.base > b.base ? b.len : a.len, second = a.base > b.base ? a.len : b.len;
-  return !(first <= d && d + second <= a.inner);
+  if (a.inner == b.inner && a.len <= a.inner && b.len <= b.inner &&
+      (N == 1 || (a.outer % a.inner == 0 && b.outer % b.inner == 0))) {
+    const long long d = (long long)((a.base > b.base ? a.base - b.base : b.base - a.base) % (size_t)a.inner);
+    const long long first = a.base > b.base ? b.len : a.len, second = a.base > b.base ? a.len : b.len;
+    if (first <= d && d + second <= a.inner) return false;
+  }
+  if (N > 1 && a.outer != b.outer) return true;
+  if (a.rows > 1 && b.rows > 1 && a.inner != b.inner) return true;
+  const Level utts{N, N, a.outer}, beams{a.rows, b.rows, a.rows > 1 ? a.inner : b.inner};
+  const bool by_utt = utts.stride >= beams.stride;          // the level with the larger stride first
+  const Level &big = by_utt ? utts : beams, &small = by_utt ? beams : utts;
+  return meets(big, (long long)(b.base - a.base), (small.na - 1) * small.stride + a.len,
+               (small.nb - 1) * small.stride + b.len,
+               [&](long long d) { return meets(small, d, a.len, b.len, [](long long) { return true; }); });
 }
 
 pctc_status_t check_move(const pctc_beam_state_t* st, int n, int N, int B, int K, const int32_t* lengths) {

@@ -1,5 +1,6 @@
 """Reordering of beam states on the GPU: copies, so that every byte has to be equal."""
 
+import numpy as np
 import pytest
 import torch
 
@@ -214,3 +215,57 @@ def test_a_decoding_loop():
             # steps of fp32 products of 16 terms of size up to 4: within 1e-4
             assert abs(float(scores[n, b]) - hyps[n][b][0]) < 1e-4
             assert bool(finished[n, b]) == hyps[n][b][3]
+
+
+@pytest.mark.parametrize("N,B", [(1, 4), (2, 4), (3, 1), (4, 32)])
+@pytest.mark.parametrize("parts", [2, 5])
+def test_views_that_interleave_by_utterance(N, B, parts):
+    """Keys and values, or layers, of one batch-first buffer [N, parts, B, ...]."""
+    g = torch.Generator(device=DEV).manual_seed(N * B + parts)
+    packed = torch.randn(N, parts, B, 6, 16, generator=g, device=DEV)
+    keep = packed.clone()
+    parents = torch.randint(0, B, (N, B), generator=g, device=DEV, dtype=torch.int32)
+    lengths = torch.randint(0, 7, (N,), generator=g, device=DEV, dtype=torch.int32)
+    views = [packed[:, i] for i in range(parts)]
+    binding.beam_reorder(views, parents, lengths=lengths, time_axes=[2] * parts)
+    for i, x in enumerate(views):
+        assert torch.equal(x, plain(keep[:, i], keep[:, i], parents, lengths, 2))
+    keep.copy_(packed)
+    binding.beam_reorder([views[0]], parents, out=[views[1]])                # from one part into another
+    assert torch.equal(packed[:, 1], plain(keep[:, 0], keep[:, 1], parents, None, None))
+    for bad in ([views[0], packed[:, 0, :, 2:]], [views[1], views[1]], [packed.flatten(0, 1)[:N], views[0]]):
+        with pytest.raises(binding.PctcError):
+            binding.beam_reorder(bad, parents)
+
+
+def shared_bytes(N, B, D, sn, sb, first, second):
+    at = torch.arange(200)
+    x, y = (set(at.as_strided((N, B, D), (sn, sb, 1), o).flatten().tolist()) for o in (first, second))
+    return bool(x & y)
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_random_views_of_one_buffer(seed):
+    """Views with the strides of one layout, anywhere in one buffer: those that share a byte are refused, all others move."""
+    rng = np.random.default_rng(seed)
+    N, B, D = int(rng.integers(1, 4)), int(rng.integers(1, 4)), int(rng.integers(1, 5))
+    if rng.random() < 0.5:                                                   # beams inside utterances, or the other way
+        sb = D + int(rng.integers(0, 6))
+        sn = B * sb + int(rng.integers(0, 25))
+    else:
+        sn = D + int(rng.integers(0, 6))
+        sb = N * sn + int(rng.integers(0, 25))
+    first, second = 4, 4 + int(rng.integers(0, 40))
+    buf = torch.arange(200, device=DEV).to(torch.uint8)
+    x, y = (buf.as_strided((N, B, D), (sn, sb, 1), at) for at in (first, second))
+    parents = torch.from_numpy(rng.integers(0, B, (N, B)).astype(np.int32)).to(DEV)
+    if shared_bytes(N, B, D, sn, sb, first, second):
+        with pytest.raises(binding.PctcError):
+            binding.beam_reorder([x, y], parents)
+        return
+    want = buf.clone()
+    for at in (first, second):
+        v = want.as_strided((N, B, D), (sn, sb, 1), at)
+        v.copy_(plain(v.clone(), v, parents, None, None))
+    binding.beam_reorder([x, y], parents)
+    assert torch.equal(buf, want)
