@@ -719,7 +719,7 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const f
   if (p->K != p->B && (scores_out == scores || (finished && finished_out == finished))) return PCTC_ERR_INVALID_ARG;
   const size_t es = p->dtype == PCTC_BF16 ? 2 : 4;
   if ((size_t)logits & (es - 1)) return PCTC_ERR_INVALID_ARG;
-  if (((size_t)scores | (size_t)scores_out | (size_t)parents | (size_t)tokens) & 3) return PCTC_ERR_INVALID_ARG;
+  if (((size_t)scores | (size_t)scores_out | (size_t)parents | (size_t)tokens | (size_t)utt_flags) & 3) return PCTC_ERR_INVALID_ARG;
   SelArgs a;
   a.logits = logits;
   a.stride_n = p->stride_n;

@@ -584,7 +584,7 @@ pctc_status_t pctc_grad_scale(int32_t n, const void* const* grads, void* const* 
   const ClipList l{n, grads, outs, numels, dtypes, out_dtypes};
   pctc_status_t st = check_list(l, true, span(norm, 4, true), span(sqsum, 8, false));
   if (st != PCTC_OK) return st;
-  if (!sqsum || ((size_t)sqsum & 7) || bad_limits(max_norm, eps)) return PCTC_ERR_INVALID_ARG;
+  if (!sqsum || ((size_t)sqsum & 7) || ((size_t)norm & 3) || bad_limits(max_norm, eps)) return PCTC_ERR_INVALID_ARG;
   return clip_call(l, sqsum, nullptr, nullptr, max_norm, eps, norm, stream_v);
 }
 
@@ -595,7 +595,7 @@ pctc_status_t pctc_clip_grad_norm(int32_t n, const void* const* grads, void* con
   const size_t need = partial_count(n) * sizeof(double);
   pctc_status_t st = check_list(l, true, span(norm, 4, true), span(workspace, need, true));
   if (st != PCTC_OK) return st;
-  if (!norm || !workspace || ((size_t)workspace & 255) || bad_limits(max_norm, eps)) return PCTC_ERR_INVALID_ARG;
+  if (!norm || ((size_t)norm & 3) || !workspace || ((size_t)workspace & 255) || bad_limits(max_norm, eps)) return PCTC_ERR_INVALID_ARG;
   if (workspace_bytes < need) return PCTC_ERR_WORKSPACE_TOO_SMALL;
   return clip_call(l, nullptr, (double*)workspace, nullptr, max_norm, eps, norm, stream_v);
 }

@@ -597,6 +597,11 @@ size_t state_bytes(const pctc_prefix_t* p) {
   return p->N * (PFX_STATE_BYTES + nodes_per_utt(p->beams, p->max_frames) * sizeof(int2));
 }
 
+bool bad_outputs(const Hypotheses& h) {
+  return !h.tokens || h.stride <= 0 || !h.sizes || !h.scores ||
+         (((size_t)h.tokens | (size_t)h.sizes | (size_t)h.scores | (size_t)h.flags) & 3);
+}
+
 pctc_status_t advance(const pctc_prefix_t* p, const int32_t* classes, const float* logprobs, const int32_t* lengths,
                       int32_t fresh, void* state, size_t bytes, const Hypotheses& out, void* stream) {
   const pctc_status_t st = check(p);
@@ -645,22 +650,22 @@ pctc_status_t pctc_prefix_read(const pctc_prefix_t* p, const void* state, size_t
                                void* stream_v) {
   const pctc_status_t st = check(p);
   if (st != PCTC_OK) return st;
-  if (!state || ((size_t)state & 255) || !tokens || token_stride <= 0 || !token_lengths || !scores)
-    return PCTC_ERR_INVALID_ARG;
+  const Hypotheses out{tokens, token_lengths, scores, utt_flags, token_stride};
+  if (!state || ((size_t)state & 255) || bad_outputs(out)) return PCTC_ERR_INVALID_ARG;
   if (bytes < state_bytes(p)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
   const int2* nodes = (const int2*)((const char*)state + (size_t)p->N * PFX_STATE_BYTES);
   k_prefix_read<<<p->N, PFX_READ_THREADS, 0, (cudaStream_t)stream_v>>>(
-      (const char*)state, nodes, p->beams, p->max_frames, Hypotheses{tokens, token_lengths, scores, utt_flags, token_stride});
+      (const char*)state, nodes, p->beams, p->max_frames, out);
   return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
 }
 
 pctc_status_t pctc_prefix_decode(const pctc_prefix_t* p, const int32_t* classes, const float* logprobs,
                                  const int32_t* lengths, void* state, size_t bytes, int32_t* tokens, int32_t token_stride,
                                  int32_t* token_lengths, float* scores, int32_t* utt_flags, void* stream) {
-  if (!tokens || token_stride <= 0 || !token_lengths || !scores) return PCTC_ERR_INVALID_ARG;
+  const Hypotheses out{tokens, token_lengths, scores, utt_flags, token_stride};
+  if (bad_outputs(out)) return PCTC_ERR_INVALID_ARG;
   const bool one = p && p->k <= 8;
-  const pctc_status_t st = advance(p, classes, logprobs, lengths, 1, state, bytes,
-                                   one ? Hypotheses{tokens, token_lengths, scores, utt_flags, token_stride} : Hypotheses{}, stream);
+  const pctc_status_t st = advance(p, classes, logprobs, lengths, 1, state, bytes, one ? out : Hypotheses{}, stream);
   if (st != PCTC_OK || one) return st;
   return pctc_prefix_read(p, state, bytes, tokens, token_stride, token_lengths, scores, utt_flags, stream);
 }

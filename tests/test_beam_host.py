@@ -136,6 +136,13 @@ def test_selection_in_place_needs_as_many_beams(lib, alias):
                                        1 << 20, None) == 1
 
 
+def test_misaligned_flags_are_refused(lib):
+    p = _problem()
+    for off in (1, 2, 3):
+        assert lib.load().pctc_beam_select(ctypes.byref(p), AT, AT * 2, None, AT * 3, AT * 4, AT * 5, None, AT * 6 + off, AT * 7,
+                                           1 << 20, None) == 1
+
+
 def test_nothing_to_move_is_no_error(lib):
     assert _reorder(lib, []) == 0
     assert _reorder(lib, [_state(units=0)]) == 0

@@ -74,6 +74,14 @@ def test_sum_of_squares_lies_apart_from_the_list(lib):
     assert f.pctc_grad_scale(1, grads, None, n, kinds, None, BASE, 1.0, 1e-6, BASE * 2, None) == 1
 
 
+def test_a_misaligned_norm_is_refused(lib):
+    for off in (1, 2, 3):
+        assert _call(lib.load(), [BASE], [8], [0], norm=BASE * 32 + off) == 1
+        f = lib.load().pctc_grad_scale
+        assert f(1, _arr(ctypes.c_void_p, [BASE]), None, _arr(ctypes.c_int64, [8]), _arr(ctypes.c_int32, [1]), None, BASE * 2, 1.0,
+                 1e-6, BASE * 32 + off, None) == 1
+
+
 def test_workspace_grows_by_launches_of_1024_tensors(lib):
     a, b, c = (lib.clip_workspace_bytes(n) for n in (1, 1024, 1025))
     assert a == b and a < c < 2 * a + 256

@@ -99,6 +99,20 @@ def test_bad_calls_are_refused_before_any_launch(lib):
     assert decode(tokens=None) == 1 and decode(stride=0) == 1 and decode(sizes=None) == 1 and decode(scores=None) == 1
 
 
+@pytest.mark.parametrize("which", ["tokens", "sizes", "scores", "flags"])
+def test_misaligned_outputs_are_refused(lib, which):
+    cdll, p, at = lib.load(), _problem(), 1 << 20
+    out = ctypes.c_size_t(0)
+    assert cdll.pctc_prefix_state_bytes(ctypes.byref(p), ctypes.byref(out)) == 0
+    ln = (ctypes.c_int32 * 2)(5, 0)
+    for off in (1, 2, 3):
+        o = dict(tokens=at * 4, sizes=at * 5, scores=at * 6, flags=at * 7)
+        o[which] += off
+        assert cdll.pctc_prefix_read(ctypes.byref(p), at, out.value, o["tokens"], 9, o["sizes"], o["scores"], o["flags"], None) == 1
+        assert cdll.pctc_prefix_decode(ctypes.byref(p), at * 2, at * 3, ln, at, out.value, o["tokens"], 9, o["sizes"], o["scores"],
+                                       o["flags"], None) == 1
+
+
 def test_binding_refuses_before_it_calls(lib):
     s = binding.PrefixBeam.__new__(binding.PrefixBeam)
     s.N, s.beams, s.max_frames, s.blank_id, s.started = 2, 4, 9, 0, False
