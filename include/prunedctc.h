@@ -370,7 +370,8 @@ typedef struct {
  * Device pointers: logits, scores [N,B] fp32, finished [N,B] bytes or NULL (needs eos_id >= 0).  Outputs:
  * scores_out [N,K] fp32, parents [N,K] and tokens [N,K] int32, finished_out [N,K] bytes or NULL (1: the parent
  * had ended, or the token is eos_id), utt_flags [N] or NULL.  scores_out and finished_out may be
- * scores and finished themselves (K == B).
+ * scores and finished themselves (K == B); apart from that, what is written, the workspace among it, may overlap nothing
+ * else of the call (PCTC_ERR_INVALID_ARG).
  * workspace: >= pctc_beam_workspace_bytes() (about 1/100 of the logits), 256-byte aligned; nothing in it outlives the
  * call.  May be captured into a CUDA graph and issued from several threads.
  */

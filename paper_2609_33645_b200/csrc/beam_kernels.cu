@@ -634,6 +634,42 @@ __global__ void __launch_bounds__(SEL_THREADS, 2) k_beam_select(const SelArgs a)
   if (tid == 0 && a.flags) a.flags[n] = sh.bad ? PCTC_UTT_NONFINITE : 0;
 }
 
+// Host checks: the rows of the beams of logits or of a state as byte ranges, base + i * outer + j * inner, i < N, j < rows, each `len` long.
+struct RowSet {
+  size_t base;
+  long long outer, inner, len;
+  int rows;
+  bool write;
+  size_t end(int N) const { return base + (size_t)((N - 1) * outer + (rows - 1) * inner + len); }
+};
+// One of the two levels of a pair of such sets: how often each repeats, and the stride that they have in common.
+struct Level {
+  long long na, nb, stride;
+};
+// Whether f(d + t * stride) holds for one of the shifts t that bring an extent of b, d behind a's, to a's extent.
+template <typename F>
+bool meets(const Level& l, long long d, long long extent_a, long long extent_b, F f) {
+  if (l.na == 1 && l.nb == 1) return d < extent_a && -d < extent_b && f(d);
+  if (l.stride <= 0) return true;
+  const long long least = -extent_b - d, down = least / l.stride - (least % l.stride < 0);
+  for (long long t = std::max(down + 1, 1 - l.na); t < l.nb && d + t * l.stride < extent_a; ++t)
+    if (f(d + t * l.stride)) return true;
+  return false;
+}
+// The level with the larger stride first.
+template <typename F>
+bool larger_first(const Level& x, const Level& y, F f) { return x.stride >= y.stride ? f(x, y) : f(y, x); }
+// Whether a range shares a byte with one of the rows.
+bool range_clash(const RowSet& r, int N, const Span& s) {
+  if (r.end(N) <= s.lo || s.hi <= r.base) return false;
+  const Level utts{r.outer ? N : 1, 1, r.outer}, beams{r.inner ? r.rows : 1, 1, r.inner};
+  const long long len = (long long)(s.hi - s.lo);
+  return larger_first(utts, beams, [&](const Level& big, const Level& small) {
+    return meets(big, (long long)(s.lo - r.base), (small.na - 1) * small.stride + r.len, len,
+                 [&](long long d) { return meets(small, d, r.len, len, [](long long) { return true; }); });
+  });
+}
+
 pctc_status_t check(const pctc_beam_t* p) {
   if (!p) return PCTC_ERR_INVALID_ARG;
   if (p->N <= 0 || p->B <= 0 || p->K <= 0 || p->V <= 0) return PCTC_ERR_INVALID_ARG;
@@ -662,6 +698,28 @@ SelWorkspace workspace_of(const pctc_beam_t* p) {
   w.o_part_s = w.o_part_m + up(rows * w.parts * 4);
   w.total = w.o_part_s + up(rows * w.parts * 8);
   return w;
+}
+
+// What the call writes may overlap nothing else that it takes; scores and finished may be written over as they are (K == B).
+bool select_overlaps(const SelArgs& a, size_t es, size_t workspace_bytes) {
+  const size_t in = (size_t)a.N * a.B, out = (size_t)a.N * a.K;
+  Span s[8];
+  size_t n = 0;
+  auto add = [&](const void* p, size_t bytes, bool write) {
+    if (p) s[n++] = Span{(size_t)p, (size_t)p + bytes, write};
+  };
+  add(a.maxima, workspace_bytes, true);
+  add(a.scores_out, 4 * out, true);
+  add(a.parents, 4 * out, true);
+  add(a.tokens, 4 * out, true);
+  add(a.finished_out, out, true);
+  add(a.flags, 4 * (size_t)a.N, true);
+  const RowSet logits{(size_t)a.logits, (long long)(a.stride_n * es), (long long)(a.stride_b * es), (long long)(a.V * es), a.B, false};
+  for (size_t i = 0; i < n; ++i)
+    if (range_clash(logits, a.N, s[i])) return true;
+  if (a.scores != a.scores_out) add(a.scores, 4 * in, false);
+  if (a.finished != a.finished_out) add(a.finished, in, false);
+  return spans_conflict(s, n);
 }
 
 template <typename T, bool VEC>
@@ -738,6 +796,7 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* p, const void* logits, const f
   a.part_s = (double*)((char*)workspace + w.o_part_s);
   a.parts = w.parts;
   a.per = w.per;
+  if (select_overlaps(a, es, w.total)) return PCTC_ERR_INVALID_ARG;
   const bool vec = (((size_t)logits | (size_t)p->stride_n * es | (size_t)p->stride_b * es) & 15) == 0;
   cudaStream_t stream = (cudaStream_t)stream_v;
   const cudaError_t e = p->dtype == PCTC_BF16
@@ -870,28 +929,6 @@ __global__ void __launch_bounds__(MOVE_THREADS) k_beam_move(const __grid_constan
   }
 }
 
-// The rows of a state's beams as byte ranges: base + i * outer + j * inner, i < N, j < rows, each `len` long.
-struct RowSet {
-  size_t base;
-  long long outer, inner, len;
-  int rows;
-  bool write;
-  size_t end(int N) const { return base + (size_t)((N - 1) * outer + (rows - 1) * inner + len); }
-};
-// One of the two levels of a pair of such sets: how often each repeats, and the stride that they have in common.
-struct Level {
-  long long na, nb, stride;
-};
-// Whether f(d + t * stride) holds for one of the shifts t that bring an extent of b, d behind a's, to a's extent.
-template <typename F>
-bool meets(const Level& l, long long d, long long extent_a, long long extent_b, F f) {
-  if (l.na == 1 && l.nb == 1) return d < extent_a && -d < extent_b && f(d);
-  if (l.stride <= 0) return true;
-  const long long least = -extent_b - d, down = least / l.stride - (least % l.stride < 0);
-  for (long long t = std::max(down + 1, 1 - l.na); t < l.nb && d + t * l.stride < extent_a; ++t)
-    if (f(d + t * l.stride)) return true;
-  return false;
-}
 // Whether two sets of rows share a byte.  Exact where they repeat with the same strides (views of one buffer, whether
 // they interleave by beam or by utterance), or lie apart within one beam stride; other ranges that interleave count as
 // shared.
@@ -906,11 +943,11 @@ bool rows_clash(const RowSet& a, const RowSet& b, int N) {
   if (N > 1 && a.outer != b.outer) return true;
   if (a.rows > 1 && b.rows > 1 && a.inner != b.inner) return true;
   const Level utts{N, N, a.outer}, beams{a.rows, b.rows, a.rows > 1 ? a.inner : b.inner};
-  const bool by_utt = utts.stride >= beams.stride;          // the level with the larger stride first
-  const Level &big = by_utt ? utts : beams, &small = by_utt ? beams : utts;
-  return meets(big, (long long)(b.base - a.base), (small.na - 1) * small.stride + a.len,
-               (small.nb - 1) * small.stride + b.len,
-               [&](long long d) { return meets(small, d, a.len, b.len, [](long long) { return true; }); });
+  return larger_first(utts, beams, [&](const Level& big, const Level& small) {
+    return meets(big, (long long)(b.base - a.base), (small.na - 1) * small.stride + a.len,
+                 (small.nb - 1) * small.stride + b.len,
+                 [&](long long d) { return meets(small, d, a.len, b.len, [](long long) { return true; }); });
+  });
 }
 
 pctc_status_t check_move(const pctc_beam_state_t* st, int n, int N, int B, int K, const int32_t* lengths) {

@@ -143,6 +143,23 @@ def test_misaligned_flags_are_refused(lib):
                                            1 << 20, None) == 1
 
 
+@pytest.mark.parametrize("name,at", [
+    ("scores_out", "scores+4"), ("scores_out", "parents"), ("parents", "scores+28"), ("tokens", "parents+28"), ("flags", "tokens"),
+    ("finished_out", "finished+7"), ("finished_out", "scores_out+31"), ("tokens", "finished+4"), ("finished", "tokens+8"),
+    ("workspace", "scores-256"), ("workspace", "logits+256"), ("parents", "workspace+256"), ("flags", "workspace+0"),
+    ("scores_out", "logits+1596"), ("tokens", "logits-28"), ("flags", "logits+196"), ("finished_out", "logits+1599"),
+    ("finished_out", "logits-7"),
+])
+def test_outputs_of_a_selection_lie_apart(lib, name, at):
+    """Logits of 2 x 4 rows of 200 bytes, 400 apart; 8 scores in and out."""
+    p = _problem(stride_n=800, stride_b=200, eos_id=0)
+    a = {x: FAR * (i + 1) for i, x in enumerate(("logits", "scores", "finished", "scores_out", "parents", "tokens", "finished_out",
+                                                 "flags", "workspace"))}
+    base = at.split("+")[0].split("-")[0]
+    a[name] = a[base] + int(at[len(base):] or 0)
+    assert lib.load().pctc_beam_select(ctypes.byref(p), *list(a.values()), 1 << 20, None) == 1
+
+
 def test_nothing_to_move_is_no_error(lib):
     assert _reorder(lib, []) == 0
     assert _reorder(lib, [_state(units=0)]) == 0

@@ -271,3 +271,24 @@ def test_equal_rows_tie():
             best = np.argsort(-x, kind="stable")[:8]        # a row may hold its largest logit more than once
             want = sorted(((-x[v], b, int(v)) for b in range(8) for v in best))[:8]
             assert list(zip(r["parents"][n].tolist(), r["tokens"][n].tolist())) == [(b, v) for _, b, v in want]
+
+
+def test_outputs_in_the_padding_of_the_logits():
+    """What is written may lie between the rows (nothing there is read), but not on them."""
+    import ctypes
+    logits, scores = make(2, 4, 1000, torch.float32, 3, pad=24)
+    want = binding.beam_select(logits.clone(), scores, 4)
+    p = binding.BeamProblem(2, 4, 4, 1000, logits.stride(0), logits.stride(1), 1, -1)
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def call(first):
+        out = [logits.data_ptr() + 4 * (b * logits.stride(1) + first) for b in range(3)]
+        return binding.load().pctc_beam_select(ctypes.byref(p), logits.data_ptr(), scores.data_ptr(), None, *out, None, None,
+                                               ws.data_ptr(), ws.numel(), stream)
+
+    assert call(999) == 1 and call(1017) == 1               # the last token of a row, and the first one of the next
+    assert call(1000) == 0
+    rows = logits.as_strided((3, 8), (logits.stride(1), 1), logits.storage_offset() + 1000)
+    for x, row in zip(("scores", "parents", "tokens"), rows):
+        assert torch.equal(row.contiguous().view(want[x].dtype), want[x].flatten())
