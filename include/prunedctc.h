@@ -301,6 +301,8 @@ pctc_status_t pctc_topk_decode(const pctc_problem_t* problem,
  *
  * The search lives in a caller-owned state buffer, so that frames can arrive in any portions (one at a
  * time, too); the result does not depend on how they are cut.  Probabilities are carried in 64 bits.
+ * What a call writes (the state, in pctc_prefix_advance and pctc_prefix_decode) may overlap nothing else that it
+ * takes (PCTC_ERR_INVALID_ARG).
  */
 typedef struct {
   int32_t N;             /* utterances                                                        */

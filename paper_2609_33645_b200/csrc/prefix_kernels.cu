@@ -602,8 +602,28 @@ bool bad_outputs(const Hypotheses& h) {
          (((size_t)h.tokens | (size_t)h.sizes | (size_t)h.scores | (size_t)h.flags) & 3);
 }
 
+// Whether something that the call writes overlaps something else that it takes.  Null: not part of the call.
+bool overlaps(const pctc_prefix_t* p, const void* classes, const void* logprobs, const void* state, bool advances,
+              const Hypotheses& h) {
+  Span s[7];
+  size_t n = 0;
+  auto add = [&](const void* at, size_t bytes, bool write) {
+    if (at) s[n++] = Span{(size_t)at, (size_t)at + bytes, write};
+  };
+  const size_t frames = 4 * (size_t)p->N * p->T * p->k, slots = 4 * (size_t)p->N * p->beams;
+  add(classes, frames, false);
+  add(logprobs, frames, false);
+  add(state, state_bytes(p), advances);
+  add(h.tokens, slots * h.stride, true);
+  add(h.sizes, slots, true);
+  add(h.scores, slots, true);
+  add(h.flags, 4 * (size_t)p->N, true);
+  return spans_conflict(s, n);
+}
+
+// out: what the call returns, if it does; read: in the same launch.
 pctc_status_t advance(const pctc_prefix_t* p, const int32_t* classes, const float* logprobs, const int32_t* lengths,
-                      int32_t fresh, void* state, size_t bytes, const Hypotheses& out, void* stream) {
+                      int32_t fresh, void* state, size_t bytes, const Hypotheses& out, bool read, void* stream) {
   const pctc_status_t st = check(p);
   if (st != PCTC_OK) return st;
   if (!classes || !logprobs || !lengths || !state || ((size_t)state & 255) || (fresh & ~1)) return PCTC_ERR_INVALID_ARG;
@@ -611,6 +631,7 @@ pctc_status_t advance(const pctc_prefix_t* p, const int32_t* classes, const floa
   for (int n = 0; n < p->N; ++n)
     if (lengths[n] < 0 || lengths[n] > p->T || lengths[n] > p->max_frames) return PCTC_ERR_INVALID_ARG;
   if (bytes < state_bytes(p)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
+  if (overlaps(p, classes, logprobs, state, true, out)) return PCTC_ERR_INVALID_ARG;
   int2* nodes = (int2*)((char*)state + (size_t)p->N * PFX_STATE_BYTES);
   for (int n0 = 0; n0 < p->N; n0 += PFX_SLICE) {
     Lengths len;
@@ -619,7 +640,7 @@ pctc_status_t advance(const pctc_prefix_t* p, const int32_t* classes, const floa
     auto kern = p->k <= 8 ? (p->beams <= 8 ? k_prefix_advance<8, 8> : p->beams <= 16 ? k_prefix_advance<8, 16> : k_prefix_advance<8, 32>)
                           : (p->beams <= 8 ? k_prefix_advance<32, 8> : p->beams <= 16 ? k_prefix_advance<32, 16> : k_prefix_advance<32, 32>);
     kern<<<m, PFX_THREADS, 0, (cudaStream_t)stream>>>(classes, logprobs, len, n0, p->T, p->k, p->beams, p->blank_id,
-                                                      p->max_frames, fresh, (char*)state, nodes, out);
+                                                      p->max_frames, fresh, (char*)state, nodes, read ? out : Hypotheses{});
     if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
   }
   return PCTC_OK;
@@ -642,7 +663,7 @@ pctc_status_t pctc_prefix_state_bytes(const pctc_prefix_t* p, size_t* bytes_out)
 
 pctc_status_t pctc_prefix_advance(const pctc_prefix_t* p, const int32_t* classes, const float* logprobs,
                                   const int32_t* lengths, int32_t fresh, void* state, size_t bytes, void* stream) {
-  return advance(p, classes, logprobs, lengths, fresh, state, bytes, Hypotheses{}, stream);
+  return advance(p, classes, logprobs, lengths, fresh, state, bytes, Hypotheses{}, false, stream);
 }
 
 pctc_status_t pctc_prefix_read(const pctc_prefix_t* p, const void* state, size_t bytes, int32_t* tokens,
@@ -653,6 +674,7 @@ pctc_status_t pctc_prefix_read(const pctc_prefix_t* p, const void* state, size_t
   const Hypotheses out{tokens, token_lengths, scores, utt_flags, token_stride};
   if (!state || ((size_t)state & 255) || bad_outputs(out)) return PCTC_ERR_INVALID_ARG;
   if (bytes < state_bytes(p)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
+  if (overlaps(p, nullptr, nullptr, state, false, out)) return PCTC_ERR_INVALID_ARG;
   const int2* nodes = (const int2*)((const char*)state + (size_t)p->N * PFX_STATE_BYTES);
   k_prefix_read<<<p->N, PFX_READ_THREADS, 0, (cudaStream_t)stream_v>>>(
       (const char*)state, nodes, p->beams, p->max_frames, out);
@@ -665,7 +687,7 @@ pctc_status_t pctc_prefix_decode(const pctc_prefix_t* p, const int32_t* classes,
   const Hypotheses out{tokens, token_lengths, scores, utt_flags, token_stride};
   if (bad_outputs(out)) return PCTC_ERR_INVALID_ARG;
   const bool one = p && p->k <= 8;
-  const pctc_status_t st = advance(p, classes, logprobs, lengths, 1, state, bytes, one ? out : Hypotheses{}, stream);
+  const pctc_status_t st = advance(p, classes, logprobs, lengths, 1, state, bytes, out, one, stream);
   if (st != PCTC_OK || one) return st;
   return pctc_prefix_read(p, state, bytes, tokens, token_stride, token_lengths, scores, utt_flags, stream);
 }

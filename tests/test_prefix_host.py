@@ -113,6 +113,32 @@ def test_misaligned_outputs_are_refused(lib, which):
                                        o["flags"], None) == 1
 
 
+@pytest.mark.parametrize("a,b,off", [
+    ("state", "classes", 159), ("state", "logprobs", 0), ("classes", "state", 0), ("tokens", "state", 0), ("flags", "state", 4),
+    ("sizes", "tokens", 284), ("scores", "tokens", 0), ("flags", "scores", 28), ("scores", "sizes", 28), ("tokens", "classes", 156),
+    ("flags", "logprobs", 156),
+])
+def test_what_a_search_writes_lies_apart(lib, a, b, off):
+    """2 utterances of 5 frames of 4 classes (160 bytes), 4 beams of 9 labels (288 bytes)."""
+    cdll, p = lib.load(), _problem()
+    out = ctypes.c_size_t(0)
+    assert cdll.pctc_prefix_state_bytes(ctypes.byref(p), ctypes.byref(out)) == 0
+    at = {x: (1 << 20) * (i + 1) for i, x in enumerate(("classes", "logprobs", "state", "tokens", "sizes", "scores", "flags"))}
+    at[a] = at[b] + off
+    if a == "state":
+        at[a] = at[b] - at[b] % 256
+        at[b] = at[a] + out.value - 4                       # on the state's last bytes
+    ln = (ctypes.c_int32 * 2)(5, 0)
+    args = [at[x] for x in ("classes", "logprobs")]
+    outs = [at["tokens"], 9, at["sizes"], at["scores"], at["flags"]]
+    if a not in ("tokens", "sizes", "scores", "flags"):
+        assert cdll.pctc_prefix_advance(ctypes.byref(p), *args, ln, 1, at["state"], out.value, None) == 1
+    elif b not in ("classes", "logprobs"):
+        assert cdll.pctc_prefix_read(ctypes.byref(p), at["state"], out.value, *outs, None) == 1
+    for k in (4, 9):                                        # in one launch, and in two
+        assert cdll.pctc_prefix_decode(ctypes.byref(_problem(k=k)), *args, ln, at["state"], out.value, *outs, None) == 1
+
+
 def test_binding_refuses_before_it_calls(lib):
     s = binding.PrefixBeam.__new__(binding.PrefixBeam)
     s.N, s.beams, s.max_frames, s.blank_id, s.started = 2, 4, 9, 0, False
