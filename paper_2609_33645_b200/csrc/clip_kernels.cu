@@ -422,7 +422,6 @@ pctc_status_t check_list(const ClipList& l, bool writes, Span own0, Span own1) {
     if (!l.out(i) || ((size_t)l.out(i) & (elem_bytes(l.out_dtype(i)) - 1))) return PCTC_ERR_INVALID_ARG;
     if (l.out(i) == l.in(i) && l.out_dtype(i) != l.dtypes[i]) return PCTC_ERR_INVALID_ARG;
   }
-  if (l.n == 0) return PCTC_OK;
   Span* spans = new (std::nothrow) Span[2 * (size_t)l.n + 2];
   if (!spans) return PCTC_ERR_HOST_MEMORY;
   size_t ns = 0;

@@ -74,6 +74,13 @@ def test_sum_of_squares_lies_apart_from_the_list(lib):
     assert f.pctc_grad_scale(1, grads, None, n, kinds, None, BASE, 1.0, 1e-6, BASE * 2, None) == 1
 
 
+def test_norm_workspace_and_sum_lie_apart_without_any_tensor(lib):
+    f = lib.load()
+    assert _call(f, [], [], [], norm=BASE * 64 + 8) == 1
+    assert f.pctc_grad_scale(0, None, None, None, None, None, BASE, 1.0, 1e-6, BASE + 4, None) == 1
+    assert f.pctc_grad_sqsum(0, None, None, None, BASE * 64 + 16, BASE * 64, 1 << 20, None) == 1
+
+
 def test_a_misaligned_norm_is_refused(lib):
     for off in (1, 2, 3):
         assert _call(lib.load(), [BASE], [8], [0], norm=BASE * 32 + off) == 1
