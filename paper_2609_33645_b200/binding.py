@@ -626,7 +626,8 @@ def beam_select(logits, scores, beams, *, finished=None, eos_id=None):
 
 def beam_reorder(states, parents, *, lengths=None, time_axes=None, out=None):
     """Move decoder states to the beams that were selected: state[n, k] = state[n, parents[n, k]] for every tensor
-    of `states` ([N, B, ...] of any type, contiguous behind the beam dimension), in one launch.
+    of `states` ([N, B, ...] of any type, contiguous behind the beam dimension), in one launch.  Bytes are moved, so
+    a lazily conjugated or negated view has to be resolved first.
 
     parents [N, K] int32 (beam_select's; entries outside [0, B) leave their slot as it is).  out: tensors
     [N, K, ...] to write to; None: in place (K == B).  time_axes: for each state the dimension of which only

@@ -63,7 +63,11 @@ void check(pctc_status_t st, const char* what) {
 
 const at::Tensor& tensor(PyObject* o, const char* what) {
   if (!THPVariable_Check(o)) fail(PyExc_TypeError, "%s must be a tensor", what);
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  // the memory of such a view holds other values than the view
+  if (t.is_conj() || t.is_neg())
+    fail(PyExc_ValueError, "%s must not be a lazily conjugated or negated view (resolve_conj, resolve_neg)", what);
+  return t;
 }
 at::Tensor optional_tensor(PyObject* o, const char* what) { return o == Py_None ? at::Tensor() : tensor(o, what); }
 

@@ -171,3 +171,16 @@ def test_reorder_binding_refuses_what_it_cannot_hand_on(lib):
         binding.beam_reorder([], p)
     with pytest.raises(ValueError, match="CUDA"):
         binding.beam_reorder([torch.zeros(2, 4, 5)], p)
+
+
+def test_lazily_conjugated_and_negated_views_are_refused(lib):
+    """Their memory holds other values than they do."""
+    p = torch.zeros(2, 4, dtype=torch.int32)
+    z = torch.zeros(2, 4, 5, dtype=torch.complex64)
+    for bad in (z.conj(), torch._neg_view(z.real.contiguous())):
+        with pytest.raises(ValueError, match="resolve_conj"):
+            binding.beam_reorder([bad], p)
+        with pytest.raises(ValueError, match="resolve_conj"):
+            binding.clip_grad_norm([bad], 1.0)
+    with pytest.raises(ValueError, match="resolve_conj"):
+        binding.beam_select(torch._neg_view(torch.zeros(2, 4, 10)), torch.zeros(2, 4), 4)

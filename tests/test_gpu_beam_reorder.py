@@ -269,3 +269,15 @@ def test_random_views_of_one_buffer(seed):
         v.copy_(plain(v.clone(), v, parents, None, None))
     binding.beam_reorder([x, y], parents)
     assert torch.equal(buf, want)
+
+
+def test_conjugated_states_are_moved_when_resolved():
+    z = torch.randn(2, 3, 7, device=DEV, dtype=torch.complex64)
+    parents = torch.tensor([[2, 0, 0], [1, 1, 2]], dtype=torch.int32, device=DEV)
+    out = torch.zeros_like(z)
+    for args, kw in [(([z.conj()], parents), dict(out=[out])), (([z], parents), dict(out=[out.conj()])), (([z.conj()], parents), {})]:
+        with pytest.raises(ValueError, match="resolve_conj"):
+            binding.beam_reorder(*args, **kw)
+    assert not out.any()
+    binding.beam_reorder([z.conj().resolve_conj()], parents, out=[out])
+    assert torch.equal(out, plain(z.conj().resolve_conj(), out, parents, None, None))
