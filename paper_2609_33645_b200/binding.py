@@ -518,7 +518,8 @@ def clip_grad_norm(grads, max_norm, *, out=None, eps=1e-6, workspace=None):
     grads: contiguous CUDA tensors of one device, bf16 and fp32 in any mixture, scaled in place, or
     into the tensors of `out` (same shapes; each of its gradient's type or fp32).  Returns a dict:
     norm [1] fp32 on the device (nothing waits for it), grads (the scaled tensors) and the reusable
-    workspace.  If the norm is not finite nothing is scaled.  The same tensor may not be given twice.
+    workspace.  If the norm is not finite nothing is scaled.  The same tensor may not be given twice.  Autograd does not
+    record the scaling; the written tensors' versions count up.
     """
     grads = list(grads)
     out = None if out is None else list(out)
@@ -619,7 +620,7 @@ def beam_select(logits, scores, beams, *, finished=None, eos_id=None):
     keep their score in one candidate with token eos_id), eos_id the token that ends a hypothesis or None.
     Returns device tensors: scores [N,beams] fp32, parents and tokens [N,beams] int32 (-1 where there are
     fewer candidates than beams), finished [N,beams] bool and flags [N] int32 (UTT_NONFINITE).  Best
-    first; among equals the lowest beam, then the lowest token.
+    first; among equals the lowest beam, then the lowest token.  Not differentiable: the scores carry no gradient.
     """
     return _native().beam_select(logits, scores, beams, finished, eos_id)
 
@@ -632,7 +633,8 @@ def beam_reorder(states, parents, *, lengths=None, time_axes=None, out=None):
     parents [N, K] int32 (beam_select's; entries outside [0, B) leave their slot as it is).  out: tensors
     [N, K, ...] to write to; None: in place (K == B).  time_axes: for each state the dimension of which only
     the first lengths[n] entries (lengths [N] int32 on the device) are moved, or None for whole rows; what lies
-    behind is left as it is.  Returns the list of written tensors.
+    behind is left as it is.  Returns the list of written tensors; autograd does not record the move, and their
+    versions count up.
     """
     states = list(states)
     out = None if out is None else list(out)

@@ -123,6 +123,14 @@ class Shared {
 
 void* stream_of(at::Device dev) { return c10::cuda::getCurrentCUDAStream(dev.index()).stream(); }
 void* ptr(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+// A tensor of the caller's that has been written to counts up, as by torch's own in-place operations, so that a backward
+// pass that has saved it does not go on with other values.
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void written(PyObject* list) {
+  for (Py_ssize_t i = 0; i < PyList_GET_SIZE(list); ++i) written(THPVariable_Unpack(PyList_GET_ITEM(list, i)));
+}
 
 // ---- gradients ----
 
@@ -193,6 +201,7 @@ PyObject* clip_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
                            o.n() ? o.kinds.data() : nullptr, (float)max_norm, (float)eps, (float*)ptr(norm), ptr(ws),
                            (size_t)ws.numel(), stream_of(g.dev)),
         "pctc_clip_grad_norm");
+  written(a[1] == Py_None ? a[0] : a[1]);
   return pair(norm, ws);
   MARSHAL_END
 }
@@ -224,6 +233,7 @@ PyObject* grad_scale(PyObject*, PyObject* const* a, Py_ssize_t n) {
                        o.n() ? o.kinds.data() : nullptr, (const double*)ptr(sq), (float)max_norm, (float)eps,
                        (float*)ptr(norm), stream_of(g.dev)),
         "pctc_grad_scale");
+  written(a[1] == Py_None ? a[0] : a[1]);
   return THPVariable_Wrap(norm);
   MARSHAL_END
 }
@@ -365,6 +375,7 @@ PyObject* beam_reorder(PyObject*, PyObject* const* a, Py_ssize_t n) {
   check(api.beam_reorder((int32_t)table.size(), table.data(), (int32_t)N, (int32_t)B, (int32_t)K, (const int32_t*)ptr(parents),
                          (const int32_t*)ptr(lengths), stream_of(dev)),
         "pctc_beam_reorder");
+  written(in_place ? a[0] : a[4]);
   Py_RETURN_NONE;
   MARSHAL_END
 }

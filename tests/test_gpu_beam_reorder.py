@@ -281,3 +281,23 @@ def test_conjugated_states_are_moved_when_resolved():
     assert not out.any()
     binding.beam_reorder([z.conj().resolve_conj()], parents, out=[out])
     assert torch.equal(out, plain(z.conj().resolve_conj(), out, parents, None, None))
+
+
+def test_saved_states_are_not_overwritten_unnoticed():
+    parents = torch.tensor([[1, 0]], dtype=torch.int32, device=DEV)
+    for into in (False, True):
+        x = torch.randn(1, 2, 5, device=DEV, requires_grad=True)
+        y, other = x * 2, torch.randn(1, 2, 5, device=DEV)
+        loss = (y * y).sum()                                # saves y
+        if into:
+            binding.beam_reorder([other], parents, out=[y.detach()])
+        else:
+            binding.beam_reorder([y.detach()], parents)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+        assert other._version == 0                          # read only
+    with torch.inference_mode():
+        z = torch.randn(1, 2, 5, device=DEV)
+    want = z[:, [1, 0]].clone()
+    binding.beam_reorder([z], parents)                      # has no version to count
+    assert torch.equal(z, want)

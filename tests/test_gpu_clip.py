@@ -266,3 +266,21 @@ def test_refusals_on_the_device():
     r = binding.clip_grad_norm([g, g[:0]], 100.0)           # an empty tensor is nothing
     assert float(r["norm"]) == 8.0
     assert float(binding.clip_grad_norm([g[:0]], 1.0)["norm"]) == 0.0
+
+
+def test_written_gradients_count_up():
+    """As by torch's own in-place operations, so that autograd notices a saved tensor that was scaled."""
+    g, out = torch.ones(100, device=DEV), torch.empty(100, device=DEV)
+    binding.clip_grad_norm([g], 1.0, out=[out])
+    assert g._version == 0 and out._version == 1
+    binding.clip_grad_norm([g], 1.0)
+    sq = binding.grad_sqsum([g])["sqsum"]
+    assert g._version == 1 and sq._version == 0
+    binding.grad_scale([g], sq, 1.0)
+    assert g._version == 2 and sq._version == 0
+    x = torch.ones(100, device=DEV, requires_grad=True)
+    y = x * 3
+    loss = (y * y).sum()
+    binding.clip_grad_norm([y.detach()], 1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
