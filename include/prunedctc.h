@@ -313,7 +313,7 @@ typedef struct {
   int32_t max_frames;    /* frames the state has room for, per utterance, over all its calls  */
 } pctc_prefix_t;
 
-/* Size of the state (T and k do not matter): per utterance 1.7 KB and 8 bytes per beam and frame. */
+/* Size of the state (T and k do not matter): per utterance 1.8 KB and 8 bytes per beam and frame. */
 pctc_status_t pctc_prefix_state_bytes(const pctc_prefix_t* problem, size_t* bytes_out);
 
 /*

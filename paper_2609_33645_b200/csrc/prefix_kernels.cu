@@ -36,6 +36,7 @@ struct Slots {
   unsigned long long hash[PFX_MAX_BEAMS];         // of the prefix
   unsigned long long up[PFX_MAX_BEAMS];           // of the prefix without its last label
   int last[PFX_MAX_BEAMS], size[PFX_MAX_BEAMS], node[PFX_MAX_BEAMS];
+  int par[PFX_MAX_BEAMS];                         // slot of the prefix without its last label, or -1
 };
 struct PrefixState {                              // one utterance, between calls
   unsigned magic;
@@ -43,7 +44,7 @@ struct PrefixState {                              // one utterance, between call
   double shift;                                   // log scale: shift + power * ln 2
   Slots s;
 };
-constexpr unsigned PFX_MAGIC = 0x70667831u;
+constexpr unsigned PFX_MAGIC = 0x70667832u;
 constexpr size_t PFX_STATE_BYTES = (sizeof(PrefixState) + 255) / 256 * 256;
 
 struct Lengths { int n[PFX_SLICE]; };
@@ -51,14 +52,27 @@ struct Lengths { int n[PFX_SLICE]; };
 __host__ __device__ inline size_t nodes_per_utt(int beams, int max_frames) { return 1 + (size_t)beams * max_frames; }
 
 // Hash of the prefix x c from that of x: two 32-bit halves, each a bijection of the half for a given label (additions,
-// exclusive ors, shifts and odd factors from the square roots of 2, 3, 5 and 7), short because the search waits for it.  Two prefixes are taken
-// for equal when both halves are: a false match among the at most 32 x 32 pairs of a frame has a chance of 2^-54, 1e-11
-// over a million frames.
+// exclusive ors, shifts and odd factors from the square roots of 2, 3, 5 and 7), short because the search waits for it.
+// Prefixes of different hashes are different; those of equal ones are compared label by label (same_prefix): pairs that
+// differ can be solved for, and among the two-label prefixes over 2^18 labels there is one.
 __device__ __forceinline__ unsigned long long grow_hash(unsigned long long h, int c) {
   unsigned lo = ((unsigned)h + (unsigned)c + 1u) * 0x6a09e667u, hi = ((unsigned)(h >> 32) ^ ((unsigned)c + 1u)) * 0xbb67ae85u;
   lo = (lo ^ (lo >> 15)) * 0x3c6ef373u;
   hi = (hi ^ (hi >> 13)) * 0xa54ff53bu;
   return (unsigned long long)hi << 32 | lo;
+}
+
+// Whether two nodes stand for the same labels.  Their chains mostly meet after a step or two: a prefix that comes back
+// is grown from the node that it was grown from before.
+__device__ __forceinline__ bool same_prefix(const int2* nodes, int x, int y) {
+  while (x != y) {
+    if (x <= 0 || y <= 0) return false;           // one of them is the empty prefix
+    const int2 u = nodes[x], v = nodes[y];
+    if (u.y != v.y || u.x >= x || v.x >= y) return false;      // nodes are made after their parents
+    x = u.x;
+    y = v.x;
+  }
+  return true;
 }
 
 __device__ __forceinline__ double round24(double p) {
@@ -284,11 +298,10 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
         pb = st->s.pb[slot]; pn = st->s.pn[slot];
         hash = st->s.hash[slot]; up = st->s.up[slot];
         last = st->s.last[slot]; size = st->s.size[slot]; node = st->s.node[slot];
-      }
-      for (int r = 0; r < B; ++r) {
-        const unsigned long long h = __shfl_sync(ALL, hash, r);
-        const bool live = __shfl_sync(ALL, pb + pn, r) > 0.0;
-        if (live && size > 0 && h == up) par = r;
+        par = st->s.par[slot];
+        // indexes of a state that something else has written to stay in range
+        if (node < 0 || node >= (int)nodes_per_utt(B, max_frames)) node = 0;
+        if (par < -1 || par >= B) par = -1;
       }
     }
     sh.taken[lane] = 0;
@@ -527,13 +540,14 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
               if (h.z == low) e = i + 2;
               if (h.w == low) e = i + 3;
             }
-            if (__any_sync(ALL, orphan && e >= 0)) {      // all bits, one new prefix after the other
+            if (__any_sync(ALL, orphan && e >= 0)) {      // all bits and all labels, one new prefix after the other
               unsigned fresh_slots = grew;
               while (fresh_slots) {
                 e = __ffs(fresh_slots) - 1;
                 fresh_slots &= fresh_slots - 1;
                 const unsigned long long h = __shfl_sync(ALL, hash, e);
-                if (orphan && h == up) par = e;
+                const int come = __shfl_sync(ALL, node, e);
+                if (orphan && h == up && same_prefix(my_nodes, my_nodes[node].x, come)) par = e;
               }
             }
           }
@@ -555,6 +569,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
       st->s.pb[lane] = pb; st->s.pn[lane] = pn;
       st->s.hash[lane] = hash; st->s.up[lane] = up;
       st->s.last[lane] = last; st->s.size[lane] = size; st->s.node[lane] = node;
+      st->s.par[lane] = par;
     }
     if (lane == 0) {
       st->magic = PFX_MAGIC;

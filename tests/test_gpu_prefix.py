@@ -266,3 +266,38 @@ def test_refusals_on_the_device():
         s.advance(c, l)
     with pytest.raises(ValueError, match="max_tokens"):
         s.read(max_tokens=0)
+
+
+# Label sequences whose 64-bit hashes are equal (found by solving for them; labels of a vocabulary of 2^18 and 2^21, and,
+# of different lengths, of any 32-bit labels).
+TWINS = [((141360, 45075), (158416, 213418)), ((1580687, 180223), (1368230, 1849779)), ((837479, 2220), (1184745, 1717519)),
+         ((336947217,), (59540, 1632145480)), ((59540, 1632145480), (336947217,)), ((474014802,), (126093, 18546947))]
+
+
+@pytest.mark.parametrize("beams", [16, 32])
+@pytest.mark.parametrize("first,second", TWINS)
+def test_prefixes_with_equal_hashes_are_kept_apart(first, second, beams):
+    """The first prefix is grown by c and leaves the beam, the second comes up later, and then c is its best extension:
+    it may not be taken for the parent of the first one's child."""
+    c, quiet = 7, -1
+    a, p = first[0], second[0]
+    frames = [[(a, 0.5), (p, 0.5)] if len(second) > 1 else [(a, 0.5), (99, 0.5)]]
+    keep = p if len(second) > 1 else 99                     # what the second prefix will be grown from, or next to
+    if len(first) > 1:
+        frames.append([(first[1], 0.9), (keep, 0.5)])
+    frames.append([(c, 0.9), (keep, 0.5)])
+    if len(second) > 1:
+        frames.append([(second[1], 0.9), (c, 0.5)])
+    else:                                                   # a single label grows only from the empty prefix: keep that by blanks
+        frames = [[(0, 0.5)] + f for f in frames] + [[(second[0], 0.9), (c, 0.5)]]
+    frames += [[(c, 1.0)], [(c, 0.6), (0, 0.4)], [(c, 0.5), (a, 0.5)]]
+    k = max(len(f) for f in frames)
+    classes = np.array([[[x for x, _ in f] + [quiet] * (k - len(f)) for f in frames]], dtype=np.int32)
+    logprobs = np.log(np.array([[[x for _, x in f] + [1.0] * (k - len(f)) for f in frames]])).astype(np.float32)
+    T = len(frames)
+    check(run(classes, logprobs, [T], 0, beams), classes, logprobs, [T], 0, beams)
+    s = binding.PrefixBeam(1, beams, T, 0, DEV)             # the same, a frame at a time
+    for t in range(T):
+        s.advance(torch.from_numpy(classes[:, t:t + 1].copy()).to(DEV), torch.from_numpy(logprobs[:, t:t + 1].copy()).to(DEV))
+        got = s.read()
+        check(got, classes, logprobs, [t + 1], 0, beams)
