@@ -546,7 +546,7 @@ class PrefixBeam:
     """A CTC prefix beam search in progress, for frames that arrive in portions.
 
     `advance(classes, logprobs, lengths)` takes the next frames (classes [N,t,k] int32 and logprobs
-    [N,t,k] fp32 as topk_decode gives them, any t; lengths: host integers, how many of the t count
+    [N,t,k] fp32 as topk_decode gives them, any t, 0 too; lengths: host integers, how many of the t count
     per utterance, None for all); `read()` returns the hypotheses so far.  The state lives in one device
     buffer with room for max_frames frames an utterance.  Calls on one object belong on one stream.  An advance
     that is captured into a CUDA graph replays with the lengths of its capture, and starts the search anew if it was
@@ -593,11 +593,11 @@ class PrefixBeam:
 def prefix_beam_decode(classes, logprobs, input_lengths, blank_id, beams):
     """CTC prefix beam search over whole utterances: classes [N,T,k] int32 and logprobs [N,T,k] fp32 as
     topk_decode gives them, input_lengths host integers.  Returns the dict of PrefixBeam.read() with tokens
-    [N,beams,T], plus the PrefixBeam itself as "search"."""
+    [N,beams,T] (one label wide where T is 0), plus the PrefixBeam itself as "search"."""
     lengths = [int(n) for n in input_lengths]
     res, state = _native().prefix_decode(classes, logprobs, lengths, beams, blank_id)
     search = PrefixBeam.__new__(PrefixBeam)
-    search.N, search.beams, search.max_frames, search.blank_id = len(lengths), int(beams), classes.shape[1], int(blank_id)
+    search.N, search.beams, search.blank_id, search.max_frames = len(lengths), int(beams), int(blank_id), max(1, classes.shape[1])
     search.device, search.state, search.frames, search.started = classes.device, state, lengths, True
     res["search"] = search
     return res

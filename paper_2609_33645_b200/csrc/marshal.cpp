@@ -397,15 +397,27 @@ void prefix_inputs(const at::Tensor& c, const at::Tensor& l, int64_t N, int64_t 
   if (!there) fail(PyExc_ValueError, "classes and logprobs must be on the state's device");
   if (!c.is_contiguous() || !l.is_contiguous()) fail(PyExc_ValueError, "classes and logprobs must be contiguous");
 }
-std::vector<int32_t> prefix_lengths(PyObject* list, int64_t N) {
+// Lengths that are none of 0 .. T become -1, which the C entry points refuse.
+std::vector<int32_t> prefix_lengths(PyObject* list, int64_t N, int64_t T) {
   if (PyList_GET_SIZE(list) != N) fail(PyExc_ValueError, "one length per utterance is required");
   std::vector<int32_t> lengths(N);
   for (int64_t i = 0; i < N; ++i) {
     const int64_t v = integer(PyList_GET_ITEM(list, i));
-    lengths[i] = (int32_t)(v < -1 ? -1 : v > INT32_MAX ? INT32_MAX : v);
+    lengths[i] = (int32_t)(v < 0 || v > T ? -1 : v);
   }
   return lengths;
 }
+// The frames of a portion; one without any (which the C ABI has no form for) becomes one frame of which nothing is read.
+struct Frames {
+  at::Tensor none;
+  const int32_t* classes;
+  const float* logprobs;
+  Frames(const at::Tensor& c, const at::Tensor& l, at::Device dev) {
+    if (c.numel() == 0) none = empty({std::max<int64_t>(1, c.size(0) * c.size(2))}, at::kInt, dev);
+    classes = (const int32_t*)ptr(none.defined() ? none : c);
+    logprobs = (const float*)ptr(none.defined() ? none : l);
+  }
+};
 at::Tensor prefix_state(const pctc_prefix_t& p, at::Device dev) {
   size_t need = 0;
   check(api.prefix_state_bytes(&p, &need), "pctc_prefix_state_bytes");
@@ -466,10 +478,11 @@ PyObject* prefix_advance(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor& l = tensor(a[2], "logprobs");
   const at::Device dev = state.device();
   prefix_inputs(c, l, integer(a[4]), dev.index());
-  const pctc_prefix_t p = prefix_problem(c.size(0), c.size(1), c.size(2), a[5], a[6], a[7]);
-  const std::vector<int32_t> lengths = prefix_lengths(a[3], p.N);
+  const pctc_prefix_t p = prefix_problem(c.size(0), std::max<int64_t>(1, c.size(1)), c.size(2), a[5], a[6], a[7]);
+  const std::vector<int32_t> lengths = prefix_lengths(a[3], p.N, c.size(1));
   const c10::cuda::CUDAGuard guard(dev);
-  check(api.prefix_advance(&p, (const int32_t*)ptr(c), (const float*)ptr(l), lengths.data(), (int32_t)integer(a[8]),
+  const Frames in(c, l, dev);
+  check(api.prefix_advance(&p, in.classes, in.logprobs, lengths.data(), (int32_t)integer(a[8]),
                            ptr(state), (size_t)state.numel(), stream_of(dev)),
         "pctc_prefix_advance");
   Py_RETURN_NONE;
@@ -503,19 +516,20 @@ PyObject* prefix_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!frames) throw Failed{};
   pctc_prefix_t p;
   try {
-    p = prefix_problem(c.size(0), c.size(1), c.size(2), a[3], a[4], frames);
+    p = prefix_problem(c.size(0), std::max<int64_t>(1, c.size(1)), c.size(2), a[3], a[4], frames);
   } catch (...) {
     Py_DECREF(frames);
     throw;
   }
   Py_DECREF(frames);
-  const std::vector<int32_t> lengths = prefix_lengths(a[2], p.N);
-  for (const int32_t v : lengths)
-    if (v > p.T) fail(PyExc_ValueError, "more frames than the state has room for");
+  for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[2]); ++i)
+    if (integer(PyList_GET_ITEM(a[2], i)) > c.size(1)) fail(PyExc_ValueError, "more frames than the state has room for");
+  const std::vector<int32_t> lengths = prefix_lengths(a[2], p.N, c.size(1));
   const c10::cuda::CUDAGuard guard(dev);
   const at::Tensor state = prefix_state(p, dev);
   const PrefixOut o(p, p.max_frames, dev);
-  check(api.prefix_decode(&p, (const int32_t*)ptr(c), (const float*)ptr(l), lengths.data(), ptr(state), (size_t)state.numel(),
+  const Frames in(c, l, dev);
+  check(api.prefix_decode(&p, in.classes, in.logprobs, lengths.data(), ptr(state), (size_t)state.numel(),
                           (int32_t*)ptr(o.tokens), p.max_frames, (int32_t*)ptr(o.sizes), (float*)ptr(o.scores),
                           (int32_t*)ptr(o.flags), stream_of(dev)),
         "pctc_prefix_decode");

@@ -301,3 +301,30 @@ def test_prefixes_with_equal_hashes_are_kept_apart(first, second, beams):
         s.advance(torch.from_numpy(classes[:, t:t + 1].copy()).to(DEV), torch.from_numpy(logprobs[:, t:t + 1].copy()).to(DEV))
         got = s.read()
         check(got, classes, logprobs, [t + 1], 0, beams)
+
+
+def test_portions_without_frames():
+    """A recogniser's empty portions, at the start, in between and as the whole utterance."""
+    classes, logprobs = make(2, 20, 8, 30, 4)
+    c, l = torch.from_numpy(classes).to(DEV), torch.from_numpy(logprobs).to(DEV)
+    none = c[:, :0].contiguous(), l[:, :0].contiguous()
+    s = binding.PrefixBeam(2, 8, 20, 0, DEV)
+    s.advance(*none)
+    r = s.read()
+    assert r["token_lengths"].eq(0).all() and r["scores"][:, 0].eq(0).all() and r["scores"][:, 1:].eq(-math.inf).all()
+    s.advance(c[:, :7].contiguous(), l[:, :7].contiguous())
+    s.advance(*none, [0, 0])
+    s.advance(c[:, 7:].contiguous(), l[:, 7:].contiguous())
+    s.advance(*none)
+    check(s.read(), classes, logprobs, [20, 20], 0, 8)
+    whole = binding.prefix_beam_decode(*none, [0, 0], 0, 4)
+    again = whole["search"].read()
+    for r in (whole, again):
+        assert r["token_lengths"].eq(0).all() and r["tokens"].eq(-1).all() and r["flags"].eq(0).all()
+        assert r["scores"].tolist() == [[0.0] + [-math.inf] * 3] * 2
+    with pytest.raises(ValueError):
+        binding.prefix_beam_decode(*none, [1, 0], 0, 4)
+    with pytest.raises(binding.PctcError):
+        s.advance(*none, [-1, 0])
+    with pytest.raises((binding.PctcError, ValueError)):
+        binding.PrefixBeam(2, 8, 20, 0, DEV).advance(*none, [1, 0])
