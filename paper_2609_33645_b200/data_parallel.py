@@ -158,13 +158,21 @@ def clip_grad_norm_data_parallel(grads, max_norm, *, group=None, sharded=False, 
     Replicated gradients (sharded=False, what `allreduce_rows` leaves): every rank holds the same values
     and computes the same norm, bit for bit, so nothing is exchanged.  sharded=True: every value of the
     gradient is held by one rank of `group`; the ranks add up their sums of squares (one fp64 number)
-    and each scales its own shard.  Returns norm [1] and grads.
+    and each scales its own shard.  A rank may hold nothing (an empty list); it takes its part in the sum all
+    the same.  Returns norm [1] and grads.
     """
+    import torch
     import torch.distributed as dist
 
+    grads = list(grads)
     if not sharded or not dist.is_initialized():
         r = binding.clip_grad_norm(grads, max_norm, out=out, eps=eps)
         return dict(norm=r["norm"], grads=r["grads"])
-    sq = binding.grad_sqsum(grads)["sqsum"]
+    if grads:
+        sq = binding.grad_sqsum(grads)["sqsum"]
+    else:
+        sq = torch.zeros(1, dtype=torch.float64, device="cuda" if torch.cuda.is_available() else "cpu")
     dist.all_reduce(sq, group=group)
+    if not grads:
+        return dict(norm=sq.sqrt().float(), grads=[])
     return binding.grad_scale(grads, sq, max_norm, out=out, eps=eps)

@@ -3,6 +3,7 @@ exchange step of sharded gradients over two gloo ranks."""
 
 import ctypes
 import os
+from datetime import timedelta
 
 import pytest
 import torch
@@ -142,3 +143,31 @@ def test_sharded_ranks_agree_on_the_norm_of_the_whole():
     parts = torch.cat([torch.from_numpy(g[2]) for g in got]).double()
     # the factor and the product each round once to fp32
     assert float(((parts - want).abs() / want).max()) <= 3 * 2.0 ** -24
+
+
+def _rank_without_a_shard(rank, port, queue):
+    os.environ.update(MASTER_ADDR="127.0.0.1", MASTER_PORT=str(port), RANK=str(rank), WORLD_SIZE="2")
+    dist.init_process_group("gloo", timeout=timedelta(seconds=20))
+    given = binding.grad_sqsum
+    binding.grad_sqsum = lambda g: dict(sqsum=sum(t.double().square().sum() for t in g).reshape(1)) if g else given(g)
+    binding.grad_scale = lambda g, sq, max_norm, out=None, eps=1e-6: dict(norm=sq.sqrt().float(), grads=g)
+    mine = [torch.full((4,), 3.0)] if rank == 0 else []
+    try:
+        r = data_parallel.clip_grad_norm_data_parallel(iter(mine), 2.0, sharded=True)
+        queue.put((rank, float(r["norm"]), len(r["grads"])))
+    except Exception as e:
+        queue.put((rank, repr(e), -1))
+    dist.destroy_process_group()
+
+
+def test_a_rank_without_a_shard_takes_its_part():
+    ctx = mp.get_context("spawn")
+    queue = ctx.Queue()
+    port = 30000 + os.getpid() % 1000
+    ranks = [ctx.Process(target=_rank_without_a_shard, args=(r, port, queue)) for r in range(2)]
+    for p in ranks:
+        p.start()
+    got = sorted((queue.get(timeout=120) for _ in ranks), key=lambda e: e[0])
+    for p in ranks:
+        p.join(60)
+    assert got == [(0, 6.0, 1), (1, 6.0, 0)]
