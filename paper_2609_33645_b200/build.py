@@ -77,6 +77,21 @@ VARIANTS = {
 TEST_VARIANTS = ("shortwait", "bounds")           # the ones the test-suite loads
 
 
+def _make(cmd, out: str, what: str) -> str:
+    """Runs a compiler whose result goes to `out`: written beside it and moved there when it is whole, so that processes
+    that build the same tree never see half a file.  Returns the compiler's messages."""
+    part = f"{out}.{os.getpid()}.part"
+    try:
+        r = subprocess.run([*cmd, "-o", part], capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"{what} failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
+        os.replace(part, out)
+    finally:
+        if os.path.exists(part):
+            os.remove(part)
+    return r.stderr
+
+
 def build_marshal() -> str:
     """csrc/marshal.cpp -> _marshal.so next to this file, for the running interpreter and its torch."""
     import sysconfig
@@ -93,17 +108,16 @@ def build_marshal() -> str:
             return MARSHAL_PATH
     base = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc()))
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+    _make(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
            "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(base, "include"),
            "-I" + os.path.join(base, "include", "torch", "csrc", "api", "include"), "-I" + os.path.join(cuda, "include"),
-           src, "-o", MARSHAL_PATH, "-L" + os.path.join(base, "lib"),
-           "-ltorch", "-ltorch_cpu", "-ltorch_python", "-lc10", "-lc10_cuda"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError("g++ failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
+           src, "-L" + os.path.join(base, "lib"),
+           "-ltorch", "-ltorch_cpu", "-ltorch_python", "-lc10", "-lc10_cuda"], MARSHAL_PATH, "g++")
     os.makedirs(os.path.dirname(stamp), exist_ok=True)
-    with open(stamp, "w") as f:
+    part = f"{stamp}.{os.getpid()}.part"
+    with open(part, "w") as f:
         f.write(key)
+    os.replace(part, stamp)
     return MARSHAL_PATH
 
 
@@ -129,27 +143,21 @@ def build(verbose: bool = False, extra_flags=(), tag: str = "") -> str:
         objs.append(obj)
         if os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(src), hdr_time):
             continue
-        cmd = [nvcc, *NVCC_FLAGS, *extra_flags, "-c", src, "-o", obj]
+        cmd = [nvcc, *NVCC_FLAGS, *extra_flags, "-c", src]
         if verbose:
             cmd.insert(1, "-Xptxas")
             cmd.insert(2, "-v")
-        jobs.append(cmd)
-
-    def run(cmd):
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
-        return r.stderr
+        jobs.append((cmd, obj))
 
     if not tag:
         build_marshal()
     if jobs:
         with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
-            for out in ex.map(run, jobs):
+            for out in ex.map(lambda job: _make(*job, "nvcc"), jobs):
                 if verbose and out:
                     sys.stderr.write(out)
     if jobs or not os.path.exists(lib_path) or os.path.getmtime(lib_path) < _newest(objs):
-        run([nvcc, "-shared", "-o", lib_path, *objs])   # static cudart (nvcc default)
+        _make([nvcc, "-shared", *objs], lib_path, "nvcc")   # static cudart (nvcc default)
     return lib_path
 
 

@@ -1,0 +1,48 @@
+"""The build step with compilers that are replaced: what is written where, and what it needs."""
+
+import os
+import subprocess
+
+import pytest
+
+from paper_2609_33645_b200 import build
+
+
+class Compilers:
+    """Stands in for subprocess.run: writes the output file, and remembers what was asked for."""
+
+    def __init__(self, monkeypatch):
+        self.calls, self.fails, self.seen = [], False, []
+        monkeypatch.setattr(build.subprocess, "run", self)
+
+    def __call__(self, cmd, **kw):
+        out = cmd[cmd.index("-o") + 1]
+        self.calls.append((os.path.basename(cmd[0]), out))
+        with open(out, "w") as f:
+            f.write("half")
+        self.seen.append(open(build.MARSHAL_PATH).read() if os.path.exists(build.MARSHAL_PATH) else None)
+        if not self.fails:
+            with open(out, "w") as f:
+                f.write("whole")
+        return subprocess.CompletedProcess(cmd, int(self.fails), "", "no such luck")
+
+
+@pytest.fixture
+def tree(monkeypatch, tmp_path):
+    monkeypatch.setattr(build, "MARSHAL_PATH", str(tmp_path / "_marshal.so"))
+    monkeypatch.setattr(build, "LIB_PATH", str(tmp_path / "lib.so"))
+    monkeypatch.setattr(build, "OBJ_DIR", str(tmp_path / "build" / "obj"))
+    return tmp_path
+
+
+def test_the_module_is_moved_into_place_when_it_is_whole(tree, monkeypatch):
+    c = Compilers(monkeypatch)
+    (tree / "_marshal.so").write_text("old")
+    build.build_marshal()
+    assert c.seen == ["old"] and (tree / "_marshal.so").read_text() == "whole"
+    c.fails = True
+    os.utime(tree / "_marshal.so", (0, 0))
+    with pytest.raises(RuntimeError, match="no such luck"):
+        build.build_marshal()
+    assert (tree / "_marshal.so").read_text() == "whole"
+    assert not [p for p in tree.iterdir() if p.name.endswith(".part")]        # no parts are left
