@@ -99,13 +99,13 @@ def build_marshal() -> str:
     import torch
 
     src = os.path.join(CSRC, "marshal.cpp")
-    stamp = os.path.join(ROOT, "build", "marshal.stamp")
+    stamp = MARSHAL_PATH + ".built_for"               # travels with the module when a tree is copied
     key = f"{torch.__version__} {sysconfig.get_config_var('SOABI')}"
     inputs = [src, os.path.join(ROOT, "include", "prunedctc.h"), os.path.abspath(__file__)]
-    if os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= _newest(inputs):
-        # a tree that was copied without its build directory holds the file that fits it
-        if not os.path.exists(stamp) or open(stamp).read() == key:
-            return MARSHAL_PATH
+    if os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= _newest(inputs) and os.path.exists(stamp):
+        with open(stamp) as f:
+            if f.read() == key:
+                return MARSHAL_PATH
     base = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc()))
     _make(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
@@ -113,7 +113,6 @@ def build_marshal() -> str:
            "-I" + os.path.join(base, "include", "torch", "csrc", "api", "include"), "-I" + os.path.join(cuda, "include"),
            src, "-L" + os.path.join(base, "lib"),
            "-ltorch", "-ltorch_cpu", "-ltorch_python", "-lc10", "-lc10_cuda"], MARSHAL_PATH, "g++")
-    os.makedirs(os.path.dirname(stamp), exist_ok=True)
     part = f"{stamp}.{os.getpid()}.part"
     with open(part, "w") as f:
         f.write(key)

@@ -41,8 +41,22 @@ def test_the_module_is_moved_into_place_when_it_is_whole(tree, monkeypatch):
     build.build_marshal()
     assert c.seen == ["old"] and (tree / "_marshal.so").read_text() == "whole"
     c.fails = True
-    os.utime(tree / "_marshal.so", (0, 0))
+    (tree / "_marshal.so.built_for").unlink()
     with pytest.raises(RuntimeError, match="no such luck"):
         build.build_marshal()
     assert (tree / "_marshal.so").read_text() == "whole"
-    assert not [p for p in tree.iterdir() if p.name.endswith(".part")]        # no parts are left
+    assert sorted(p.name for p in tree.iterdir()) == ["_marshal.so"]        # no parts are left
+
+
+def test_a_copied_tree_is_built_for_its_own_torch(tree, monkeypatch):
+    import torch
+
+    c = Compilers(monkeypatch)
+    (tree / "_marshal.so").write_text("made elsewhere")                     # nothing says for which torch
+    build.build_marshal()
+    assert len(c.calls) == 1
+    build.build_marshal()
+    assert len(c.calls) == 1                                                # up to date
+    monkeypatch.setattr(torch, "__version__", "0.0")
+    build.build_marshal()
+    assert len(c.calls) == 2
