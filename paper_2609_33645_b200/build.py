@@ -4,8 +4,9 @@
 ``libprunedctc.so`` next to this file and returns its path.  Objects are cached
 under ``build/`` and rebuilt only when a source or header is newer.
 ``build_variant(tag)`` builds a test variant of the same sources (see VARIANTS).
-``build()`` also compiles ``csrc/marshal.cpp``, the argument marshalling that the binding
-imports as ``_marshal`` (``_marshal.so``, built against the installed torch).
+``build()`` then compiles ``csrc/marshal.cpp``, the argument marshalling that the binding
+imports as ``_marshal`` (``_marshal.so``, built with g++ against the installed torch; a program
+that calls the C ABI alone needs neither).
 """
 
 from __future__ import annotations
@@ -148,8 +149,6 @@ def build(verbose: bool = False, extra_flags=(), tag: str = "") -> str:
             cmd.insert(2, "-v")
         jobs.append((cmd, obj))
 
-    if not tag:
-        build_marshal()
     if jobs:
         with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
             for out in ex.map(lambda job: _make(*job, "nvcc"), jobs):
@@ -157,6 +156,13 @@ def build(verbose: bool = False, extra_flags=(), tag: str = "") -> str:
                     sys.stderr.write(out)
     if jobs or not os.path.exists(lib_path) or os.path.getmtime(lib_path) < _newest(objs):
         _make([nvcc, "-shared", *objs], lib_path, "nvcc")   # static cudart (nvcc default)
+    if not tag:
+        try:
+            import torch  # noqa: F401
+        except ImportError:
+            sys.stderr.write("torch cannot be imported: the library is built, the binding's _marshal.so is not\n")
+        else:
+            build_marshal()
     return lib_path
 
 

@@ -2,6 +2,7 @@
 
 import os
 import subprocess
+import sys
 
 import pytest
 
@@ -60,3 +61,12 @@ def test_a_copied_tree_is_built_for_its_own_torch(tree, monkeypatch):
     monkeypatch.setattr(torch, "__version__", "0.0")
     build.build_marshal()
     assert len(c.calls) == 2
+
+
+def test_the_library_needs_no_torch(tree, monkeypatch, capsys):
+    c = Compilers(monkeypatch)
+    monkeypatch.setitem(sys.modules, "torch", None)                         # import torch fails
+    assert build.build() == str(tree / "lib.so") and (tree / "lib.so").read_text() == "whole"
+    assert len(c.calls) == len(build.sources()) + 1 and {name for name, _ in c.calls} == {"nvcc"}
+    assert all(out.endswith(".part") for _, out in c.calls)
+    assert "torch" in capsys.readouterr().err and not (tree / "_marshal.so").exists()
