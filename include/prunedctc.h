@@ -350,7 +350,9 @@ pctc_status_t pctc_prefix_decode(const pctc_prefix_t* problem, const int32_t* cl
  * (rescoring, transcription with a language model's head): with logits x and lse_b = log sum_v exp x[b,v],
  *   cand(b,v) = score_b + (x[b,v] - lse_b)
  * and the K largest candidates of every utterance, best first; among equals the lowest b * V + v.  The
- * comparisons are of 64-bit sums; the scores that come back are rounded once to fp32.
+ * comparisons are of 64-bit sums; the scores that come back are rounded once to fp32.  An lse is made of fp32
+ * exponentials (within 2e-7 measured, 6e-7 + 1.4e-7 ln V at most, and never below the row's maximum, so that no
+ * candidate's score exceeds its parent's): candidates of different beams that are nearer than that may come in either order.
  *
  * A beam whose score is -inf is dead: its logits count for nothing and it gives no candidates (a first step with
  * one hypothesis: all scores but one -inf).  An ended beam (finished[n,b] != 0) keeps its score in a single

@@ -292,3 +292,36 @@ def test_outputs_in_the_padding_of_the_logits():
     rows = logits.as_strided((3, 8), (logits.stride(1), 1), logits.storage_offset() + 1000)
     for x, row in zip(("scores", "parents", "tokens"), rows):
         assert torch.equal(row.contiguous().view(want[x].dtype), want[x].flatten())
+
+
+@pytest.mark.parametrize("rise", [0.5, 1.5, 2.5, 3.5, 3.9])
+@pytest.mark.parametrize("low", [-20.0, -14.0])
+def test_a_peak_a_little_above_the_blocks_before_it(rise, low):
+    """Rows of one token at 0, a few blocks behind two at about -rise and all else at `low`.
+
+    The largest logit counts exactly 1; an exponential d below it is off by (2^-22 + 1.4e-7 |d|) of its share of
+    the row, a lane's sum of 16 takes five roundings, and the score one more."""
+    V, R = 32768, 512
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.full((R, 8, V), low, device=DEV)
+    x[:, :, 0] = -rise * (1 - 1e-3 * torch.rand(R, 8, generator=g, device=DEV))
+    x[:, :, 4000] = x[:, :, 0]
+    x[:, :, 600] = 0
+    scores = -torch.rand(R, 8, generator=g, device=DEV)
+    r = binding.beam_select(x.view(R * 8, 1, V), scores.view(-1, 1), 1)
+    got = r["scores"].view(R, 8).double()
+    want = scores.double() - torch.logsumexp(x.double(), -1)
+    rest = 1 - torch.exp(-torch.logsumexp(x.double(), -1))
+    tol = 5 * 2.0 ** -24 + rest * (2.0 ** -22 + 1.4e-7 * -low) + 2.0 ** -24 * want.abs()
+    assert r["tokens"].eq(600).all() and bool(((got - want).abs() <= tol).all())
+    assert bool((r["scores"].view(R, 8) <= scores).all())
+
+
+def test_no_candidate_scores_above_its_parent():
+    for dtype in (torch.float32, torch.bfloat16):
+        for gap in (15.0, 17.0, 20.0, 90.0):                # what is not the best adds up to about nothing
+            logits, _ = make(40, 4, 20011, dtype, 3, 0.5)
+            logits[:, :, 7777] = logits.float().amax(-1).to(dtype) + gap
+            scores = torch.tensor([0.0, -1e-7, -1e-3, -2.0], device=DEV).expand(40, 4).contiguous()
+            r = binding.beam_select(logits, scores, 4)
+            assert bool((r["scores"] <= scores.gather(1, r["parents"].long())).all()) and r["tokens"].eq(7777).all()
