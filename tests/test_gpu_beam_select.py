@@ -325,3 +325,40 @@ def test_no_candidate_scores_above_its_parent():
             scores = torch.tensor([0.0, -1e-7, -1e-3, -2.0], device=DEV).expand(40, 4).contiguous()
             r = binding.beam_select(logits, scores, 4)
             assert bool((r["scores"] <= scores.gather(1, r["parents"].long())).all()) and r["tokens"].eq(7777).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,blocks,pad", [(8, 128, 5), (8, 128, 3), (32, 512, 3)])
+def test_ties_beyond_the_lists_among_other_beams(B, blocks, pad, dtype):
+    """More candidates than the lists hold, beside ended, dead, masked and not finite beams.
+
+    Blocks are 512 logits and the threshold is the K-th best of the maxima of 32 groups of blocks (by block number
+    modulo 32), so the six groups that reach 0.5 only put it there; all other blocks hold 40 logits of 1.0 and give K
+    candidates each: 104 blocks in a row of 128, so more than 2,048 candidates in one row.  (More than 2 K blocks a row:
+    the threshold is not raised.)"""
+    V = 512 * blocks - 3
+    g = torch.Generator(device=DEV).manual_seed(B)
+    full = torch.full((1, B, V + pad), -50.0, device=DEV)
+    full[:, :, V:] = 1e4
+    x = full[:, :, :V]
+    at = torch.stack([torch.randperm(508, generator=torch.Generator().manual_seed(i))[:40] + 512 * i for i in range(blocks)])
+    low = torch.arange(blocks) % 32 >= 26
+    x[:, :, at[~low].flatten().to(DEV)] = 1.0
+    x[:, :, at[low, 0].to(DEV)] = 0.5
+    x[0, :, [512 * 5 + 100, 512 * 33, 7]] = 1.25            # three winners a row, in blocks that reach 1.0 anyway
+    x = full.to(dtype)[:, :, :V]
+    scores = torch.full((1, B), -3.0, device=DEV)           # beams 0 and 2 tie candidate by candidate
+    scores[0, 1], scores[0, 3] = -3.01, -3.2
+    finished = torch.zeros(1, B, dtype=torch.bool, device=DEV)
+    finished[0, 4] = True
+    scores[0, 4] = -3.0 - float(torch.logsumexp(x[0, 0].double(), 0)) + 1.1      # between the winners and the ties
+    scores[0, 5] = -math.inf
+    x[0, 6, 1000] = math.nan
+    x[0, 7] = -math.inf
+    for b in range(8, B):
+        scores[0, b] = -4.0 - b / 64
+    for K in (32, 27):
+        r = check(x, scores, K, finished, 9)
+        assert r["flags"].item() == 2
+        # 1.25 from beams 0 and 2, 1.24, the ended one at 1.1, 1.25 - 0.2, then the ties at 1.0 of beam 0
+        assert r["parents"][0].tolist() == [0] * 3 + [2] * 3 + [1] * 3 + [4] + [3] * 3 + [0] * (K - 13)
