@@ -420,7 +420,8 @@ pctc_status_t pctc_beam_reorder(int32_t n_states, const pctc_beam_state_t* state
  *   S = sum over all tensors and values of g^2,  norm = sqrt(S),
  *   f = min(1, max_norm / (norm + eps)),         out = f * g, rounded once to out's type.
  * Values are squared in fp32 and summed in 64 bits in a fixed order (values that fp32 squares would
- * lose are squared in 64 bits), so repeated calls agree bit for bit.  If the norm is not finite in fp32, f is 1:
+ * lose are squared in 64 bits), so repeated calls agree bit for bit, and so do calls on equal values at
+ * other addresses if these are equally far from a 16-byte boundary (on GPUs with equally many SMs).  If the norm is not finite in fp32, f is 1:
  * nothing is scaled, and the norm tells the caller.
  *
  * n tensors (any n >= 0; more than 1,024 take several launches), HOST arrays:

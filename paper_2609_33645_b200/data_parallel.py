@@ -155,8 +155,11 @@ def pruned_ctc_fwd_bwd_data_parallel(hidden, W, bias, targets, input_lengths, ta
 def clip_grad_norm_data_parallel(grads, max_norm, *, group=None, sharded=False, out=None, eps=1e-6):
     """Clip by the global gradient norm after the exchange step (`binding.clip_grad_norm` over ranks).
 
-    Replicated gradients (sharded=False, what `allreduce_rows` leaves): every rank holds the same values
-    and computes the same norm, bit for bit, so nothing is exchanged.  sharded=True: every value of the
+    Replicated gradients (sharded=False, what `allreduce_rows` leaves): nothing is exchanged.  Ranks that hold the
+    same values compute the same norm, bit for bit, if their tensors also start equally far from a 16-byte
+    boundary and their GPUs have equally many SMs (which values are added first follows from both), as ranks of one
+    program on one kind of GPU do.  Elsewhere norms can differ in the last bit: take the sum from one rank
+    (`binding.grad_sqsum`, `dist.broadcast`, `binding.grad_scale`), which scales alike everywhere.  sharded=True: every value of the
     gradient is held by one rank of `group`; the ranks add up their sums of squares (one fp64 number)
     and each scales its own shard.  A rank may hold nothing (an empty list); it takes its part in the sum all
     the same.  Returns norm [1] and grads.

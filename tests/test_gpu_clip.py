@@ -284,3 +284,26 @@ def test_written_gradients_count_up():
     binding.clip_grad_norm([y.detach()], 1.0)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("size", [50_000, 5_000_000])
+def test_replicas_agree_bit_for_bit_when_equally_aligned(size, dtype):
+    whole = torch.randn(size, device=DEV).to(dtype)
+
+    def copy(offset):
+        buf = torch.empty(size + 64, device=DEV, dtype=dtype)
+        v = buf[offset:offset + size]
+        v.copy_(whole)
+        return v
+
+    group = 16 // dtype.itemsize
+    one, two, other = copy(1), copy(1 + 3 * group), copy(2)
+    norms = [binding.clip_grad_norm([t], 1.0)["norm"] for t in (one, two, other)]
+    assert torch.equal(norms[0], norms[1]) and torch.equal(one, two)
+    assert abs(float(norms[2]) - float(norms[0])) <= 2 * NORM_TOL * float(norms[0])
+    # the sum of one replica scales all of them alike, wherever they lie
+    one, other = copy(1), copy(2)
+    sq = binding.grad_sqsum([one])["sqsum"]
+    norms = [binding.grad_scale([t], sq, 1.0)["norm"] for t in (one, other)]
+    assert torch.equal(norms[0], norms[1]) and torch.equal(one, other)
