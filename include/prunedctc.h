@@ -319,9 +319,9 @@ pctc_status_t pctc_prefix_state_bytes(const pctc_prefix_t* problem, size_t* byte
 /*
  * Takes lengths[n] frames (HOST, 0 <= lengths[n] <= T and max_frames) of every utterance.
  *   classes [N,T,k] int32, logprobs [N,T,k] fp32 (device); frames from lengths[n] on are not read.
- *   fresh 1: starts the state (whatever it held), 0: goes on.  A call that goes on with other sizes than the
- *   state was started with, or beyond max_frames, leaves that utterance's hypotheses as they are and
- *   flags it PCTC_UTT_STATE_FULL.
+ *   fresh 1: starts the state (whatever it held), 0: goes on.  A call that goes on with other sizes (N, beams,
+ *   max_frames) than the state was started with, or beyond max_frames, leaves that utterance's hypotheses as they
+ *   are and flags it PCTC_UTT_STATE_FULL.
  *   state: >= pctc_prefix_state_bytes(), 256-byte aligned, state_bytes its size.
  */
 pctc_status_t pctc_prefix_advance(const pctc_prefix_t* problem, const int32_t* classes, const float* logprobs,

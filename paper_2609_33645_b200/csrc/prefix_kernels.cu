@@ -40,7 +40,7 @@ struct Slots {
 };
 struct PrefixState {                              // one utterance, between calls
   unsigned magic;
-  int beams, max_frames, frames, flags, power;
+  int utts, beams, max_frames, frames, flags, power;
   double shift;                                   // log scale: shift + power * ln 2
   Slots s;
 };
@@ -48,6 +48,13 @@ constexpr unsigned PFX_MAGIC = 0x70667832u;
 constexpr size_t PFX_STATE_BYTES = (sizeof(PrefixState) + 255) / 256 * 256;
 
 struct Lengths { int n[PFX_SLICE]; };
+
+// Whether the state that begins at `states` was started for these sizes.  The first utterance's tells: where the
+// others lie does not depend on the sizes, but what lies there does.
+__device__ __forceinline__ bool started_for(const char* states, int N, int B, int max_frames) {
+  const PrefixState* first = (const PrefixState*)states;
+  return first->magic == PFX_MAGIC && first->utts == N && first->beams == B && first->max_frames == max_frames;
+}
 
 __host__ __device__ inline size_t nodes_per_utt(int beams, int max_frames) { return 1 + (size_t)beams * max_frames; }
 
@@ -99,10 +106,9 @@ struct ReadShared {
 // table is taken through shared memory in windows from the last frame to the first, and all chains of an
 // utterance walk through a window before the next one is fetched.  Called by all threads of a CTA.
 template <int THREADS, int WINDOW>
-__device__ void read_out(ReadShared<WINDOW>& sh, const PrefixState* st, const int2* my_nodes, int n, int B, int max_frames,
-                         const Hypotheses& h) {
+__device__ void read_out(ReadShared<WINDOW>& sh, bool valid, const PrefixState* st, const int2* my_nodes, int n, int B,
+                         int max_frames, const Hypotheses& h) {
   const int tid = threadIdx.x;
-  const bool valid = st->magic == PFX_MAGIC && st->beams == B && st->max_frames == max_frames;
   const int most = (int)nodes_per_utt(B, max_frames);
   if (tid == 0) sh.newest = 0;
   __syncthreads();
@@ -260,7 +266,7 @@ struct Search {                                   // what lanes hand each other 
 template <int KM, int BM>
 __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
     const int* __restrict__ classes, const float* __restrict__ logprobs, const __grid_constant__ Lengths len, int n0,
-    int T, int k, int B, int blank, int max_frames, int fresh, char* states, int2* nodes, const Hypotheses out) {
+    int N, int T, int k, int B, int blank, int max_frames, int fresh, char* states, int2* nodes, const Hypotheses out) {
   constexpr unsigned ALL = 0xffffffffu;
   constexpr int REP = 32 / BM, KP = KM / REP;     // lanes a slot, classes a lane
   constexpr unsigned SLOTS = BM == 32 ? ALL : (1u << BM) - 1;
@@ -274,10 +280,11 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
   int2* my_nodes = nodes + (size_t)n * nodes_per_utt(B, max_frames);
   if (!fresh) {
     // a state that was not started with these sizes, or has no room for the frames, takes nothing
-    const bool fits = st->magic == PFX_MAGIC && st->beams == B && st->max_frames == max_frames && st->frames >= 0 &&
-                      st->frames <= max_frames - Tn;
+    const PrefixState* first = (const PrefixState*)states;
+    const bool fits = started_for(states, N, B, max_frames) && st->frames >= 0 && st->frames <= max_frames - Tn;
     if (!fits) {
-      if (tid == 0) atomicOr(&st->flags, PCTC_UTT_STATE_FULL);
+      // (of a state for fewer utterances there may be something else in this place)
+      if (tid == 0 && first->magic == PFX_MAGIC && n < first->utts) atomicOr(&st->flags, PCTC_UTT_STATE_FULL);
       return;
     }
   }
@@ -573,6 +580,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
     }
     if (lane == 0) {
       st->magic = PFX_MAGIC;
+      st->utts = N;
       st->beams = B;
       st->max_frames = max_frames;
       st->frames = frames0 + Tn;
@@ -585,7 +593,7 @@ __global__ void __launch_bounds__(PFX_THREADS, 1) k_prefix_advance(
     if (out.tokens) {
       __shared__ ReadShared<PFX_LAST_WINDOW> rd;
       __syncthreads();
-      read_out<PFX_THREADS>(rd, st, my_nodes, n, B, max_frames, out);
+      read_out<PFX_THREADS>(rd, true, st, my_nodes, n, B, max_frames, out);
     }
   }
 }
@@ -596,7 +604,7 @@ __global__ void __launch_bounds__(PFX_READ_THREADS) k_prefix_read(const char* __
                                                                   const Hypotheses out) {
   __shared__ ReadShared<PFX_READ_WINDOW> sh;
   const int n = blockIdx.x;
-  read_out<PFX_READ_THREADS>(sh, (const PrefixState*)(states + (size_t)n * PFX_STATE_BYTES),
+  read_out<PFX_READ_THREADS>(sh, started_for(states, gridDim.x, B, max_frames), (const PrefixState*)(states + (size_t)n * PFX_STATE_BYTES),
                              nodes + (size_t)n * nodes_per_utt(B, max_frames), n, B, max_frames, out);
 }
 
@@ -654,7 +662,7 @@ pctc_status_t advance(const pctc_prefix_t* p, const int32_t* classes, const floa
     for (int i = 0; i < m; ++i) len.n[i] = lengths[n0 + i];
     auto kern = p->k <= 8 ? (p->beams <= 8 ? k_prefix_advance<8, 8> : p->beams <= 16 ? k_prefix_advance<8, 16> : k_prefix_advance<8, 32>)
                           : (p->beams <= 8 ? k_prefix_advance<32, 8> : p->beams <= 16 ? k_prefix_advance<32, 16> : k_prefix_advance<32, 32>);
-    kern<<<m, PFX_THREADS, 0, (cudaStream_t)stream>>>(classes, logprobs, len, n0, p->T, p->k, p->beams, p->blank_id,
+    kern<<<m, PFX_THREADS, 0, (cudaStream_t)stream>>>(classes, logprobs, len, n0, p->N, p->T, p->k, p->beams, p->blank_id,
                                                       p->max_frames, fresh, (char*)state, nodes, read ? out : Hypotheses{});
     if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
   }

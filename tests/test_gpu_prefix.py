@@ -328,3 +328,35 @@ def test_portions_without_frames():
         s.advance(*none, [-1, 0])
     with pytest.raises((binding.PctcError, ValueError)):
         binding.PrefixBeam(2, 8, 20, 0, DEV).advance(*none, [1, 0])
+
+
+@pytest.mark.parametrize("N,beams,max_frames", [(1, 4, 12), (2, 4, 12), (4, 4, 12), (9, 4, 12), (3, 5, 12), (3, 4, 11)])
+def test_a_state_of_other_sizes_is_left_as_it_is(N, beams, max_frames):
+    import ctypes
+    lib = binding.load()
+    classes, logprobs = make(9, 6, 4, 9, 1)
+    c, l = torch.from_numpy(classes).to(DEV), torch.from_numpy(logprobs).to(DEV)
+    s = binding.PrefixBeam(3, 4, 12, 0, DEV)
+    s.state = torch.zeros(1 << 16, dtype=torch.uint8, device=DEV)          # room for every size that is tried
+    s.advance(c[:3].contiguous(), l[:3].contiguous())
+    before, state = s.read(max_tokens=12), s.state.clone()
+    p = binding.PrefixProblem(N, 3, 4, beams, 0, max_frames)
+    need = ctypes.c_size_t(0)
+    assert lib.pctc_prefix_state_bytes(ctypes.byref(p), ctypes.byref(need)) == 0 and need.value <= s.state.numel()
+    ln, stream = (ctypes.c_int32 * N)(*[3] * N), torch.cuda.current_stream().cuda_stream
+    assert lib.pctc_prefix_advance(ctypes.byref(p), c.data_ptr(), l.data_ptr(), ln, 0, s.state.data_ptr(), s.state.numel(), stream) == 0
+    out = [torch.empty(n, dtype=torch.int32, device=DEV) for n in (N * beams * 12, N * beams, N * beams, N)]
+    assert lib.pctc_prefix_read(ctypes.byref(p), s.state.data_ptr(), s.state.numel(), out[0].data_ptr(), 12, out[1].data_ptr(),
+                                out[2].data_ptr(), out[3].data_ptr(), stream) == 0
+    assert out[3].eq(binding.UTT_STATE_FULL).all() and out[1].eq(0).all() and out[0].eq(-1).all()
+    after = s.read(max_tokens=12)
+    for x in ("tokens", "token_lengths", "scores"):
+        assert torch.equal(after[x], before[x])
+    assert after["flags"].tolist() == [binding.UTT_STATE_FULL if n < N else 0 for n in range(3)]
+    assert int((s.state != state).sum()) == min(N, 3)       # a flag each
+    c2, l2 = (x[:3, :6].contiguous() for x in (c, l))
+    s.advance(c2, l2)                                       # and goes on as if nothing had been
+    two = [np.concatenate([x[:3], x[:3]], 1) for x in (classes, logprobs)]
+    got = s.read(max_tokens=12)
+    got["flags"] = got["flags"] & ~binding.UTT_STATE_FULL
+    check(got, *two, [12] * 3, 0, 4)
