@@ -377,7 +377,7 @@ typedef struct {
  * scores and finished themselves (K == B); apart from that, what is written, the workspace among it, may overlap nothing
  * else of the call (PCTC_ERR_INVALID_ARG).
  * workspace: >= pctc_beam_workspace_bytes() (about 1/100 of the logits), 256-byte aligned; nothing in it outlives the
- * call.  May be captured into a CUDA graph and issued from several threads.
+ * call (calls that may run at the same time, replays of captured ones among them, need one each).  May be captured into a CUDA graph and issued from several threads.
  */
 pctc_status_t pctc_beam_workspace_bytes(const pctc_beam_t* problem, size_t* bytes_out);
 pctc_status_t pctc_beam_select(const pctc_beam_t* problem, const void* logits, const float* scores,
@@ -436,7 +436,8 @@ pctc_status_t pctc_beam_reorder(int32_t n_states, const pctc_beam_state_t* state
  * pctc_clip_grad_norm does it all; norm [1] fp32 (device).  For gradients that are sharded over ranks,
  * pctc_grad_sqsum leaves S of this rank's values in sqsum [1] (device, fp64), the ranks add these up,
  * and pctc_grad_scale does the rest (norm [1] or NULL).
- * workspace: >= pctc_clip_workspace_bytes(n), 256-byte aligned; nothing in it outlives the call.
+ * workspace: >= pctc_clip_workspace_bytes(n), 256-byte aligned; nothing in it outlives the call (calls that may run at the
+ * same time, replays of captured ones among them, need one each).
  * These calls use `stream` only, may be captured into a CUDA graph and may be issued from several threads.
  */
 pctc_status_t pctc_clip_workspace_bytes(int32_t n, size_t* bytes_out);

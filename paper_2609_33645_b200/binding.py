@@ -517,8 +517,8 @@ def clip_grad_norm(grads, max_norm, *, out=None, eps=1e-6, workspace=None):
 
     grads: contiguous CUDA tensors of one device, bf16 and fp32 in any mixture, scaled in place, or
     into the tensors of `out` (same shapes; each of its gradient's type or fp32).  Returns a dict:
-    norm [1] fp32 on the device (nothing waits for it), grads (the scaled tensors) and the reusable
-    workspace.  If the norm is not finite nothing is scaled.  The same tensor may not be given twice.  Autograd does not
+    norm [1] fp32 on the device (nothing waits for it), grads (the scaled tensors) and the workspace, which
+    later calls on the same stream may take.  If the norm is not finite nothing is scaled.  The same tensor may not be given twice.  Autograd does not
     record the scaling; the written tensors' versions count up.
     """
     grads = list(grads)

@@ -56,8 +56,8 @@ def headers():
 # Variants of the library for tests: same sources, extra compile-time definitions, a file of their own.
 #   shortwait  every bounded device wait gives up after a few thousand cycles, so that an ordinary
 #              call exercises the give-up path (status word, drain, clean return)
-#   bounds     every index that a kernel gathers or scatters through (selected classes, relabelled
-#              targets, row tables) is range-checked first; a bad one is recorded in the status word
+#   bounds     every index that a kernel of the head and loss gathers or scatters through (selected
+#              classes, relabelled targets, row tables) is range-checked first; a bad one is recorded in the status word
 #              and the access is skipped
 #   probe_*    measurement probes for `bench.py --lib-variant`: one part of the tensor-core kernel is
 #              knocked out (results are wrong on purpose) to show what a launch is bound by

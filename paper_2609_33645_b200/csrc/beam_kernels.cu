@@ -14,12 +14,11 @@
 // launch of a cluster per utterance; its clusters left SMs idle and all had their tails at the same time (utterances x
 // beams x 151,936: 64 x 8 bf16 55 us against 41, 2 x 8 bf16 24.5 against 13.0, 1 x 4 fp32 14.4 against 11.1).
 //
-// Measured: 64 x 8 x 151,936 bf16 with a tenth of the beams ended, 140 MB: 41 us (21 at the rate of a copy), of which the
-// stream takes 31 and the ranking 9 to 10; 1 x 4 fp32: 12 us, of which 3 and 9.  The stream is bound by no single thing:
-// special function unit 62% busy (16 exponentials a cycle and SM are hardly more than the 12 bf16 logits that HBM
-// delivers), issue slots 55%, HBM 68%.  More blocks in flight, more or fewer warps a CTA, and longer stretches measured
-// the same; a quarter of the exponentials as polynomials on the FMA pipe made the whole call 10% slower.  The ranking is a
-// chain of about ten dependent steps of 0.3 to 1 us each.
+// Measured: 64 x 8 x 151,936 bf16 with a tenth of the beams ended, 140 MB: 41.7 us (21 at the rate of a copy), of which the
+// stream takes 31 and the ranking 10; 1 x 4 fp32: 11.4 us, of which 3 and 8.  The stream is bound by no single thing:
+// special function unit 60% busy (16 exponentials a cycle and SM are hardly more than the 12 bf16 logits that HBM
+// delivers), issue slots 60%, HBM 64% of a copy's rate.  More blocks in flight, more or fewer warps a CTA, and longer
+// stretches measured the same.  The ranking is a chain of about ten dependent steps of 0.3 to 1 us each.
 //
 // Exponentials and the sums of 16 of them are fp32, of differences from a running maximum (so that their errors are
 // relative to the difference, not to the logit); everything after that, and every comparison of candidates, is 64
@@ -44,7 +43,7 @@ constexpr int SEL_MAX = 32;                       // beams in and out
 constexpr int SEL_WARPS = 16, SEL_THREADS = SEL_WARPS * 32;
 constexpr int SEL_MAX_CLUSTER = 8;
 constexpr int STREAM_WARPS = 4;
-constexpr int STREAM_CTAS = 592;                  // CTAs of the first launch that are worth shorter stretches
+constexpr int STREAM_CTAS = 4 * 148;              // CTAs of the first launch that are worth shorter stretches: four an SM
 constexpr int SEL_BLOCK = 512;                    // logits per maximum: 16 a lane
 constexpr int SEL_LANE = SEL_BLOCK / 32;
 constexpr int SEL_MAX_BLOCKS = 512;               // blocks a CTA reads again

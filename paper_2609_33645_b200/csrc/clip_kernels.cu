@@ -10,7 +10,7 @@
 //
 // Measured: 156M bf16 values into another buffer 140 us (three passes of 312 MB at the rate of a copy: 143; the last 64 MB
 // of the first pass are still in L2 for the second); 64M bf16 values in 384 tensors, in place below the limit, 27 us
-// (one pass: 20; a bare read of the same bytes: 23); 100,000 fp32 values in 7 tensors 6.6 us in one launch (two
+// (one pass: 20; a bare read of the same bytes: 23); 100,000 fp32 values in 7 tensors 6.3 us in one launch (two
 // launches cost the host 6 us more).
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"

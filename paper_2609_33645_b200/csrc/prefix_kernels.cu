@@ -258,8 +258,8 @@ struct Search {                                   // what lanes hand each other 
 // where two of those tie, the ranks are taken again with all bits and the order of equals.  In most frames of
 // speech the blank or the last label takes nearly all, no extension reaches even the worst stay, the stays
 // keep their order, and neither step is needed.
-// Measured on confusable posteriors, of which a third of the frames are such: 0.65 us a frame at beam 4 and 0.93 us at
-// beam 16, k = 8 (8 utterances of up to 1500 frames: 1.40 ms; a CTA of 128 threads with three barriers a frame that
+// Measured on confusable posteriors, of which a third of the frames are such: 0.65 us a frame at beam 4 and 0.95 us at
+// beam 16, k = 8 (8 utterances of up to 1500 frames: 1.42 ms; a CTA of 128 threads with three barriers a frame that
 // ranks all candidates: 7.6 ms).  A frame is about 330 dependent instructions at 5 cycles each; shuffles, votes, reductions
 // and shared-memory loads take 25 to 45 cycles each.  Taking the B winners one after the other by warp-wide maxima, in
 // place of bound and ranks, measured the same at beam 4 and 30% slower at beam 16.
