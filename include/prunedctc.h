@@ -377,7 +377,8 @@ typedef struct {
  * scores and finished themselves (K == B); apart from that, what is written, the workspace among it, may overlap nothing
  * else of the call (PCTC_ERR_INVALID_ARG).
  * workspace: >= pctc_beam_workspace_bytes() (about 1/100 of the logits), 256-byte aligned; nothing in it outlives the
- * call (calls that may run at the same time, replays of captured ones among them, need one each).  May be captured into a CUDA graph and issued from several threads.
+ * call (calls that may run at the same time, replays of captured ones among them, need one each).  May be captured
+ * into a CUDA graph and issued from several threads.
  */
 pctc_status_t pctc_beam_workspace_bytes(const pctc_beam_t* problem, size_t* bytes_out);
 pctc_status_t pctc_beam_select(const pctc_beam_t* problem, const void* logits, const float* scores,
@@ -396,8 +397,8 @@ pctc_status_t pctc_beam_select(const pctc_beam_t* problem, const void* logits, c
  * are left as they are.  A cache [N,B,heads,L,D] is heads segments of L units of D values; a state [N,B,D]
  * is one segment of one unit.  src and dst share that layout and may have other beam and utterance strides.
  * What is written may overlap nothing else of the call: a state given twice, rows into each other, or a state that
- * holds the parents or lengths themselves, is refused (PCTC_ERR_INVALID_ARG).  Views of one buffer that interleave by beam or by
- * utterance are told apart where their strides are equal ([N,2,B,...] and [N,B,2,...] among them).  16-byte aligned addresses, strides and units are moved fastest.
+ * holds the parents or lengths themselves, is refused (PCTC_ERR_INVALID_ARG).  Views of one buffer that interleave by
+ * beam or by utterance are told apart where their strides are equal ([N,2,B,...] and [N,B,2,...] among them).  16-byte aligned addresses, strides and units are moved fastest.
  */
 typedef struct {
   const void* src;
@@ -421,8 +422,8 @@ pctc_status_t pctc_beam_reorder(int32_t n_states, const pctc_beam_state_t* state
  *   f = min(1, max_norm / (norm + eps)),         out = f * g, rounded once to out's type.
  * Values are squared in fp32 and summed in 64 bits in a fixed order (values that fp32 squares would
  * lose are squared in 64 bits), so repeated calls agree bit for bit, and so do calls on equal values at
- * other addresses if these are equally far from a 16-byte boundary (on GPUs with equally many SMs).  If the norm is not finite in fp32, f is 1:
- * nothing is scaled, and the norm tells the caller.
+ * other addresses if these are equally far from a 16-byte boundary (on GPUs with equally many SMs).  If the norm is
+ * not finite in fp32, f is 1: nothing is scaled, and the norm tells the caller.
  *
  * n tensors (any n >= 0; more than 1,024 take several launches), HOST arrays:
  *   grads  [n] device pointers to contiguous values;  outs [n] likewise, or NULL: every tensor in place.

@@ -518,8 +518,8 @@ def clip_grad_norm(grads, max_norm, *, out=None, eps=1e-6, workspace=None):
     grads: contiguous CUDA tensors of one device, bf16 and fp32 in any mixture, scaled in place, or
     into the tensors of `out` (same shapes; each of its gradient's type or fp32).  Returns a dict:
     norm [1] fp32 on the device (nothing waits for it), grads (the scaled tensors) and the workspace, which
-    later calls on the same stream may take.  If the norm is not finite nothing is scaled.  The same tensor may not be given twice.  Autograd does not
-    record the scaling; the written tensors' versions count up.
+    later calls on the same stream may take.  If the norm is not finite nothing is scaled.  The same tensor may
+    not be given twice.  Autograd does not record the scaling; the written tensors' versions count up.
     """
     grads = list(grads)
     out = None if out is None else list(out)
@@ -597,7 +597,8 @@ def prefix_beam_decode(classes, logprobs, input_lengths, blank_id, beams):
     lengths = [int(n) for n in input_lengths]
     res, state = _native().prefix_decode(classes, logprobs, lengths, beams, blank_id)
     search = PrefixBeam.__new__(PrefixBeam)
-    search.N, search.beams, search.blank_id, search.max_frames = len(lengths), int(beams), int(blank_id), max(1, classes.shape[1])
+    search.N, search.beams, search.blank_id = len(lengths), int(beams), int(blank_id)
+    search.max_frames = max(1, classes.shape[1])
     search.device, search.state, search.frames, search.started = classes.device, state, lengths, True
     res["search"] = search
     return res

@@ -159,10 +159,11 @@ def clip_grad_norm_data_parallel(grads, max_norm, *, group=None, sharded=False, 
     same values compute the same norm, bit for bit, if their tensors also start equally far from a 16-byte
     boundary and their GPUs have equally many SMs (which values are added first follows from both), as ranks of one
     program on one kind of GPU do.  Elsewhere norms can differ in the last bit: take the sum from one rank
-    (`binding.grad_sqsum`, `dist.broadcast`, `binding.grad_scale`), which scales alike everywhere.  sharded=True: every value of the
-    gradient is held by one rank of `group`; the ranks add up their sums of squares (one fp64 number)
-    and each scales its own shard.  A rank may hold nothing (an empty list); it takes its part in the sum all
-    the same.  Returns norm [1] and grads.
+    (`binding.grad_sqsum`, `dist.broadcast`, `binding.grad_scale`), which scales alike everywhere.
+
+    sharded=True: every value of the gradient is held by one rank of `group`; the ranks add up their sums of
+    squares (one fp64 number) and each scales its own shard.  A rank may hold nothing (an empty list); it
+    takes its part in the sum all the same.  Returns norm [1] and grads.
     """
     import torch
     import torch.distributed as dist
