@@ -308,7 +308,7 @@ typedef struct {
   int32_t N;             /* utterances                                                        */
   int32_t T;             /* row count of classes[n] and logprobs[n] in this call              */
   int32_t k;             /* classes per frame, 1 .. 32                                        */
-  int32_t beams;         /* prefixes kept, 1 .. 32                                            */
+  int32_t beams;         /* prefixes kept, 1 .. 32; N * beams and max_frames * beams < 2^31   */
   int32_t blank_id;
   int32_t max_frames;    /* frames the state has room for, per utterance, over all its calls  */
 } pctc_prefix_t;

@@ -614,6 +614,7 @@ pctc_status_t check(const pctc_prefix_t* p) {
     return PCTC_ERR_INVALID_ARG;
   if (p->k > PFX_MAX_K || p->beams > PFX_MAX_BEAMS) return PCTC_ERR_UNSUPPORTED;
   if ((long long)p->max_frames * p->beams >= 0x7fffffffLL) return PCTC_ERR_UNSUPPORTED;
+  if ((long long)p->N * p->beams > 0x7fffffffLL) return PCTC_ERR_UNSUPPORTED;      // places of hypotheses are 32 bits
   return PCTC_OK;
 }
 size_t state_bytes(const pctc_prefix_t* p) {

@@ -99,6 +99,16 @@ def test_bad_calls_are_refused_before_any_launch(lib):
     assert decode(tokens=None) == 1 and decode(stride=0) == 1 and decode(sizes=None) == 1 and decode(scores=None) == 1
 
 
+def test_more_hypotheses_than_32_bits_count_are_refused(lib):
+    out = ctypes.c_size_t(0)
+    for N, beams, want in ((2 ** 26, 32, 3), (2 ** 26 - 1, 32, 0), (2 ** 31 - 1, 2, 3), (2 ** 31 - 1, 1, 0)):
+        p = _problem(N=N, beams=beams)
+        assert lib.load().pctc_prefix_state_bytes(ctypes.byref(p), ctypes.byref(out)) == want
+        if want:
+            args = [ctypes.byref(p), 1 << 20, 2 ** 62, (1 << 20) * 2, 9, (1 << 20) * 3, (1 << 20) * 4, None, None]
+            assert lib.load().pctc_prefix_read(*args) == want
+
+
 @pytest.mark.parametrize("which", ["tokens", "sizes", "scores", "flags"])
 def test_misaligned_outputs_are_refused(lib, which):
     cdll, p, at = lib.load(), _problem(), 1 << 20
