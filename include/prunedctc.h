@@ -41,7 +41,11 @@ typedef enum {
   PCTC_ERR_HOST_MEMORY = 7          /* the host could not allocate a small table for its checks  */
 } pctc_status_t;
 
-typedef enum { PCTC_BF16 = 0, PCTC_FP32 = 1 } pctc_dtype_t;
+typedef enum {
+  PCTC_BF16 = 0,
+  PCTC_FP32 = 1,
+  PCTC_INT8 = 2                     /* pctc_embed's matrix only */
+} pctc_dtype_t;
 
 /* Which contraction kernels run.  AUTO: tcgen05 tensor-core kernels for bf16,
  * fp32 FMA kernels for fp32.  SIMT: the FMA kernels for either dtype (bf16
@@ -453,6 +457,143 @@ pctc_status_t pctc_grad_scale(int32_t n, const void* const* grads, void* const* 
                               const double* sqsum, float max_norm, float eps, float* norm, void* stream);
 
 /*
+ * Rows of the vocabulary matrix for tokens (the input side of a model whose head is tied to its embedding, and of a
+ * decoder that goes on with beam search's tokens):
+ *   out[i,:] = T(scale * W[tokens[i],:]),  in 8 bits T((scale * row_scales[v]) * q[v,:]),  i < M,
+ * in fp32, rounded once.  A token outside [0, V) (the -1 of padded targets and of beams without a candidate) is a row
+ * of zeros, whatever W holds.
+ */
+typedef struct {
+  int64_t M;             /* tokens, >= 0                                                      */
+  int64_t V;             /* rows of W                                                         */
+  int64_t D;
+  int64_t ld_w;          /* elements between rows of W (dW) ...                               */
+  int64_t ld_x;          /* ... and of out (grad).  Fastest with D % 8 == 0 and rows that start 16-byte aligned */
+  int32_t dtype_w;       /* pctc_dtype_t of W (dW); PCTC_INT8 in pctc_embed only              */
+  int32_t dtype_x;       /* of out (grad): PCTC_BF16 or PCTC_FP32                             */
+  float   scale;         /* finite                                                            */
+  int32_t accumulate;    /* pctc_embed_grad: 1 adds to dW (the dW that pruned_ctc_fwd_bwd has written, for a tied
+                            head) and touches only rows of tokens that occur; 0 writes every row */
+} pctc_embed_t;
+
+/* tokens [M] int32, W [V,D], row_scales [V] fp32 (PCTC_INT8) or NULL, out [M,D]: device.  out may overlap nothing else. */
+pctc_status_t pctc_embed(const pctc_embed_t* problem, const int32_t* tokens, const void* W, const float* row_scales,
+                         void* out, void* stream);
+
+/*
+ * Its gradient:  dW[v,:] = T(scale * sum over i with tokens[i] == v of grad[i,:])  (+ dW[v,:] with accumulate = 1).
+ * Sums are fp32, in ascending i cut at places that depend on M and D alone, rounded once: repeated calls agree bit for bit.
+ *   workspace: >= pctc_embed_grad_workspace_bytes(), 256-byte aligned; nothing in it outlives the call (calls that may
+ *   run at the same time, replays of captured ones among them, need one each).  dW and the workspace may overlap nothing else.
+ */
+pctc_status_t pctc_embed_grad_workspace_bytes(const pctc_embed_t* problem, size_t* bytes_out);
+pctc_status_t pctc_embed_grad(const pctc_embed_t* problem, const int32_t* tokens, const void* grad, void* dW,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Dropout (in front of the head, say), forward and backward, with a mask that is a function of the value's index and
+ * never stored.  Value e (row * cols + column) belongs to block b = e / 8 and takes the 16-bit word u = half e % 8 (low half
+ * first) of the four 32-bit words of Philox-4x32-10 with counter (b, offset), low words first, and key seed:
+ *   limit = floor(p * 65536 + 0.5)  (at most 65535 unless p = 1),
+ *   out = u < limit ? 0 : x * 65536 / (65536 - limit)   (+ residual),   in fp32, rounded once.
+ * The expectation is exact for the p that is carried out, limit / 65536.  A dropped value is 0 even if it is not finite.
+ * The gradient with respect to x is the same call on the gradient, with the same seed and offset and no residual.
+ */
+typedef struct {
+  int64_t rows, cols;    /* >= 0                                                              */
+  int64_t ld_x, ld_res, ld_out;   /* elements between rows                                    */
+  int32_t dtype;         /* PCTC_BF16 or PCTC_FP32, of all three                              */
+  int32_t reserved;
+  double  p;             /* in [0, 1]                                                         */
+  uint64_t seed, offset;
+} pctc_dropout_t;
+
+/* x, out, residual (or NULL): device [rows, cols].  out may be x or residual (with the same stride); apart from that it may
+ * overlap nothing.  step: device int64 word that is added to offset, or NULL; a captured call whose program counts it up
+ * draws another mask at every replay. */
+pctc_status_t pctc_dropout(const pctc_dropout_t* problem, const void* x, const void* residual, const int64_t* step,
+                           void* out, void* stream);
+
+/*
+ * Clipped policy loss with a KL term over log-probabilities of sampled tokens (or, with T = 1, of whole sequences: what
+ * pruned_ctc_fwd_bwd returns as losses are log-probabilities with the other sign, and the gradient is its utt_weights).
+ * With d = logp - old_logp, r = exp(d), A the advantage, f = ref_logp - logp:
+ *   token = -min(A r, A min(max(r, 1 - clip_low), 1 + clip_high)) + kl_weight * (exp(f) - 1 - f)
+ *   loss  = sum over counted tokens of w * token,     grad = d loss / d logp,
+ * where a token is counted if it lies before its row's length and its mask is not 0, and
+ *   w = 1 / (counted tokens)                                            PCTC_POLICY_TOKENS
+ *   w = 1 / (counted tokens of the row * rows with a counted token)     PCTC_POLICY_SEQUENCES
+ *   w = 1                                                               PCTC_POLICY_SUM.
+ * At r = 1 + clip_high (1 - clip_low) exactly the gradient is that of the ratio.  What lies in uncounted places is not
+ * looked at, and its gradient is 0; with nothing counted the loss is 0.  Counted values that are not finite give what the
+ * formula gives.  Differences and sums are 64 bits, exponentials fp32; repeated calls agree bit for bit.
+ */
+typedef enum { PCTC_POLICY_TOKENS = 0, PCTC_POLICY_SEQUENCES = 1, PCTC_POLICY_SUM = 2 } pctc_policy_reduction_t;
+typedef struct {
+  int64_t N, T;          /* rows and tokens, N * T < 2^31                                     */
+  int64_t ld_logp, ld_old, ld_ref;   /* elements between rows                                 */
+  int64_t ld_adv;        /* of advantages [N,T]; 0: advantages [N], one a row                 */
+  int64_t ld_mask, ld_grad;
+  double  clip_low;      /* in [0, 1]                                                         */
+  double  clip_high;     /* >= 0; +inf: ratios are not clipped upwards                        */
+  double  kl_weight;     /* finite                                                            */
+  int32_t reduction;     /* pctc_policy_reduction_t                                           */
+  int32_t negated;       /* 1: logp, old_logp and ref_logp are given with the other sign (as losses), and so is grad */
+} pctc_policy_t;
+
+/*
+ * Device pointers: logp, old_logp [N,T] fp32, ref_logp likewise or NULL (no KL term), advantages fp32, mask [N,T] bytes or NULL,
+ * lengths [N] int32 or NULL (cut to 0 .. T).  Outputs: grad [N,T] fp32 or NULL (the loss alone), stats [3] fp32: the loss,
+ * the mean over counted tokens of exp(f) - 1 - f, and the share of them whose ratio is clipped; count [1] int32.
+ * Outputs and workspace may overlap nothing else.
+ * workspace: >= pctc_policy_workspace_bytes(), 256-byte aligned; nothing in it outlives the call (calls that may run at the
+ * same time, replays of captured ones among them, need one each).
+ */
+pctc_status_t pctc_policy_workspace_bytes(const pctc_policy_t* problem, size_t* bytes_out);
+pctc_status_t pctc_policy_loss(const pctc_policy_t* problem, const float* logp, const float* old_logp, const float* ref_logp,
+                               const float* advantages, const uint8_t* mask, const int32_t* lengths, float* grad,
+                               float* stats, int32_t* count, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The head in 8-bit integers with a scale for every token and every channel, for recognition:
+ *   rows:     s = max|x| / 127,  q = round(x * (127 / max|x|))   in fp32, ties to even, 127 / max rounded to fp32 first;
+ *             a row with max|x| < 2^-100 gives q = 0, s = 0; one with NaN or infinities gives q = 0, s = NaN
+ *   product:  C[i,j] = T(float(sum_k A[i,k] B[j,k]) * (a_scales[i] * b_scales[j]) + bias[j]),
+ *             the sum exact, the rest fp32, rounded once.
+ * pctc_i8_quantize makes both operands (the head once, states at every call), pctc_i8_matmul multiplies them, and
+ * pctc_i8_logits does both for states x.
+ */
+#define PCTC_I8_MAX_K 131071
+typedef struct {
+  int32_t m, n, k;       /* tokens (>= 0), channels, contraction (<= PCTC_I8_MAX_K)           */
+  int32_t out_dtype;     /* PCTC_BF16 or PCTC_FP32                                            */
+  int64_t lda;           /* elements between rows of A (pctc_i8_logits: of x) ...             */
+  int64_t ldb, ldc;      /* ... of B and of C; 8-bit rows are a multiple of 16 apart          */
+  int32_t bias_dtype;    /* PCTC_BF16 or PCTC_FP32 (looked at with a bias only)               */
+  int32_t reserved;
+} pctc_i8_t;
+
+/* x [rows, cols] (dtype) -> q [rows, cols] int8, scales [rows] fp32; device.  Outputs may overlap nothing else. */
+pctc_status_t pctc_i8_quantize(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ld_x, int8_t* q, int64_t ld_q,
+                               float* scales, void* stream);
+/* A [m,k], a_scales [m], B [n,k], b_scales [n], bias [n] or NULL, C [m,n]: device; A and B 16-byte aligned.
+ * device_status [1] or NULL: receives a code if a bounded wait gives up (see pctc_workspace_status; the caller zeroes it). */
+pctc_status_t pctc_i8_matmul(const pctc_i8_t* problem, const int8_t* A, const float* a_scales, const int8_t* B,
+                             const float* b_scales, const void* bias, void* C, int32_t* device_status, void* stream);
+/* x [m,k] (x_dtype).  workspace: >= pctc_i8_logits_workspace_bytes(), 256-byte aligned, with a status word at its start;
+ * nothing else in it outlives the call (calls that may run at the same time need one each). */
+pctc_status_t pctc_i8_logits_workspace_bytes(const pctc_i8_t* problem, size_t* bytes_out);
+pctc_status_t pctc_i8_logits(const pctc_i8_t* problem, const void* x, int32_t x_dtype, const int8_t* B, const float* b_scales,
+                             const void* bias, void* C, void* workspace, size_t workspace_bytes, void* stream);
+/* pctc_topk_decode with the head in 8 bits: W [V,D] of pitch ld_w with w_scales [V]; hidden and bias of problem->dtype. */
+pctc_status_t pctc_i8_topk_workspace_bytes(const pctc_problem_t* problem, const int32_t* input_lengths_host, int32_t k,
+                                           size_t* bytes_out);
+pctc_status_t pctc_i8_topk_decode(const pctc_problem_t* problem, const void* hidden, const int8_t* W, int64_t ld_w,
+                                  const float* w_scales, const void* bias, const int32_t* input_lengths, int32_t k,
+                                  int32_t* topk_classes, float* topk_logprobs, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
+/*
  * Contraction kernel on its own, for validation of the tensor-core path:
  *   C[i,j] = sum_k A(i,k) B(j,k),  i < m, j < n, k < k,  C fp32 [m, n] row-major.
  * a_mn_major == 0: A is stored [m, k] (k contiguous); else A is stored [k, m].
@@ -519,7 +660,7 @@ pctc_status_t pctc_subset_relabel_noalloc(const int32_t* targets, const int32_t*
  *                about to gather or scatter through was out of range (0x200 + checking site);
  *                the access was skipped                                 -> PCTC_ERR_INVALID_ARG
  * `workspace` may be any device word that received a status, e.g. the device_status of
- * pctc_gemm_bf16.
+ * pctc_gemm_bf16 or pctc_i8_matmul, or the workspace of pctc_i8_logits.
  */
 pctc_status_t pctc_workspace_status(const void* workspace, void* stream, int32_t* status_host);
 

@@ -9,14 +9,14 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libprunedctc.so")
 
-PCTC_BF16, PCTC_FP32 = 0, 1
+PCTC_BF16, PCTC_FP32, PCTC_INT8 = 0, 1, 2
 GEMM_AUTO, GEMM_SIMT = 0, 1
 UTT_INFEASIBLE, UTT_NONFINITE, UTT_BAD_TARGET, UTT_SUBSET_OVERFLOW, UTT_STATE_FULL = 1, 2, 4, 8, 16
 
@@ -27,7 +27,10 @@ EXPORTS = ("pctc_workspace_bytes", "pctc_chunk_width", "pruned_ctc_fwd_bwd", "pr
            "pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
            "pctc_prefix_state_bytes", "pctc_prefix_advance", "pctc_prefix_read",
            "pctc_prefix_decode", "pctc_beam_workspace_bytes", "pctc_beam_select",
-           "pctc_beam_reorder")
+           "pctc_beam_reorder",
+           "pctc_embed", "pctc_embed_grad_workspace_bytes", "pctc_embed_grad", "pctc_dropout",
+           "pctc_policy_workspace_bytes", "pctc_policy_loss", "pctc_i8_quantize", "pctc_i8_matmul",
+           "pctc_i8_logits_workspace_bytes", "pctc_i8_logits", "pctc_i8_topk_workspace_bytes", "pctc_i8_topk_decode")
 NOALLOC_MAX_V = 262144
 
 PHASES = ("prep", "lse", "subset_logp", "dp", "dlogits", "dh", "dw", "dbias", "finish")
@@ -63,6 +66,28 @@ class BeamState(ctypes.Structure):
                 ("segments", ctypes.c_int64), ("segment_stride", ctypes.c_int64),
                 ("units", ctypes.c_int64), ("unit_bytes", ctypes.c_int64),
                 ("timed", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class EmbedProblem(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int64) for name in ("M", "V", "D", "ld_w", "ld_x")] + [
+        ("dtype_w", ctypes.c_int32), ("dtype_x", ctypes.c_int32), ("scale", ctypes.c_float), ("accumulate", ctypes.c_int32)]
+
+
+class DropoutProblem(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int64) for name in ("rows", "cols", "ld_x", "ld_res", "ld_out")] + [
+        ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32), ("p", ctypes.c_double), ("seed", ctypes.c_uint64),
+        ("offset", ctypes.c_uint64)]
+
+
+class PolicyProblem(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int64) for name in ("N", "T", "ld_logp", "ld_old", "ld_ref", "ld_adv", "ld_mask", "ld_grad")] + [
+        ("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double), ("kl_weight", ctypes.c_double),
+        ("reduction", ctypes.c_int32), ("negated", ctypes.c_int32)]
+
+
+class I8Problem(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("m", "n", "k", "out_dtype")] + [
+        (name, ctypes.c_int64) for name in ("lda", "ldb", "ldc")] + [("bias_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class TraceStruct(ctypes.Structure):
@@ -181,6 +206,32 @@ def _configure(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.pctc_beam_reorder.restype = ctypes.c_int
     lib.pctc_beam_reorder.argtypes = [ctypes.c_int32, ctypes.POINTER(BeamState), ctypes.c_int32, ctypes.c_int32,
                                       ctypes.c_int32, vp, vp, vp]
+    lib.pctc_embed.restype = ctypes.c_int
+    lib.pctc_embed.argtypes = [ctypes.POINTER(EmbedProblem)] + [vp] * 5
+    lib.pctc_embed_grad_workspace_bytes.restype = ctypes.c_int
+    lib.pctc_embed_grad_workspace_bytes.argtypes = [ctypes.POINTER(EmbedProblem), size_p]
+    lib.pctc_embed_grad.restype = ctypes.c_int
+    lib.pctc_embed_grad.argtypes = [ctypes.POINTER(EmbedProblem)] + [vp] * 4 + [ctypes.c_size_t, vp]
+    lib.pctc_dropout.restype = ctypes.c_int
+    lib.pctc_dropout.argtypes = [ctypes.POINTER(DropoutProblem)] + [vp] * 5
+    lib.pctc_policy_workspace_bytes.restype = ctypes.c_int
+    lib.pctc_policy_workspace_bytes.argtypes = [ctypes.POINTER(PolicyProblem), size_p]
+    lib.pctc_policy_loss.restype = ctypes.c_int
+    lib.pctc_policy_loss.argtypes = [ctypes.POINTER(PolicyProblem)] + [vp] * 10 + [ctypes.c_size_t, vp]
+    lib.pctc_i8_quantize.restype = ctypes.c_int
+    lib.pctc_i8_quantize.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, vp, ctypes.c_int64, vp, ctypes.c_int64,
+                                     vp, vp]
+    lib.pctc_i8_matmul.restype = ctypes.c_int
+    lib.pctc_i8_matmul.argtypes = [ctypes.POINTER(I8Problem)] + [vp] * 8
+    lib.pctc_i8_logits_workspace_bytes.restype = ctypes.c_int
+    lib.pctc_i8_logits_workspace_bytes.argtypes = [ctypes.POINTER(I8Problem), size_p]
+    lib.pctc_i8_logits.restype = ctypes.c_int
+    lib.pctc_i8_logits.argtypes = [ctypes.POINTER(I8Problem), vp, ctypes.c_int32] + [vp] * 5 + [ctypes.c_size_t, vp]
+    lib.pctc_i8_topk_workspace_bytes.restype = ctypes.c_int
+    lib.pctc_i8_topk_workspace_bytes.argtypes = lib.pctc_topk_workspace_bytes.argtypes
+    lib.pctc_i8_topk_decode.restype = ctypes.c_int
+    lib.pctc_i8_topk_decode.argtypes = [ctypes.POINTER(Problem), vp, vp, ctypes.c_int64, vp, vp, i32p, ctypes.c_int32, vp, vp, vp,
+                                        ctypes.c_size_t, vp]
     lib.pctc_gemm_bf16.restype = ctypes.c_int
     lib.pctc_gemm_bf16.argtypes = [vp, vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                    ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp]
@@ -417,6 +468,34 @@ def subset_relabel_noalloc(targets, target_lengths, V, blank_id, out):
     return out
 
 
+class QuantizedHead(NamedTuple):
+    """A head [V, D] in 8-bit integers: q int8 [V, D] whose rows start 16-byte aligned (a multiple of 16 bytes apart) and
+    scales fp32 [V], so that W[v, d] is about q[v, d] * scales[v].  quantize_rows makes one.  embed, quantized_logits,
+    topk_decode and beam_decode take it."""
+
+    q: "torch.Tensor"          # noqa: F821
+    scales: "torch.Tensor"     # noqa: F821
+
+
+def _pitch(q) -> int:
+    return int(q.stride(0)) if q.shape[0] > 1 else (int(q.shape[1]) + 15) // 16 * 16
+
+
+def _checked_head(head: QuantizedHead, hidden) -> QuantizedHead:
+    import torch
+
+    q, scales = head
+    if not (hidden.is_cuda and hidden.is_contiguous() and hidden.dtype in (torch.bfloat16, torch.float32)):
+        raise ValueError("hidden must be a contiguous bf16 or fp32 CUDA tensor")
+    if q.dtype != torch.int8 or q.dim() != 2 or q.device != hidden.device or (q.shape[1] > 1 and q.stride(1) != 1):
+        raise ValueError("a quantized head's q must be int8 [V, D] with contiguous rows, on the device of hidden")
+    if scales.dtype != torch.float32 or tuple(scales.shape) != (q.shape[0],) or not scales.is_contiguous() or scales.device != q.device:
+        raise ValueError("a quantized head's scales must be contiguous fp32 [V] on the device of hidden")
+    if q.shape[1] != hidden.shape[-1]:
+        raise ValueError("hidden must be [N, T, D] for a head [V, D]")
+    return head
+
+
 def greedy_decode(hidden, W, bias, input_lengths, blank_id, *, gemm_path=GEMM_AUTO, workspace=None):
     """Greedy CTC recognition: frame arg-max of the head, repeats merged, blanks dropped.
 
@@ -453,30 +532,38 @@ def greedy_decode(hidden, W, bias, input_lengths, blank_id, *, gemm_path=GEMM_AU
 def topk_decode(hidden, W, bias, input_lengths, k, *, chunk=0, gemm_path=GEMM_AUTO, workspace=None):
     """The k best classes of every frame (k in 1, 2, 4, 8) and their log-probabilities under the
     full-vocabulary softmax: device tensors classes [N,T,k] int32 (-1 on padded frames) and logprobs
-    [N,T,k] fp32 (-inf there), plus the reusable workspace."""
+    [N,T,k] fp32 (-inf there), plus the reusable workspace.  W may be a QuantizedHead: the frames are then quantized
+    row by row and multiplied in 8-bit integers (gemm_path does not matter)."""
     import torch
 
     lib = load()
+    head8 = W if isinstance(W, QuantizedHead) else None
+    if head8 is not None:
+        W = _checked_head(head8, hidden).q
     dt = PCTC_BF16 if hidden.dtype == torch.bfloat16 else PCTC_FP32
     N, T, D = hidden.shape
     V = W.shape[0]
     il = _i32(input_lengths)
     prob = make_problem(N, T, D, V, dt, 0, chunk=chunk, gemm_path=gemm_path)
     need = ctypes.c_size_t(0)
-    st = lib.pctc_topk_workspace_bytes(ctypes.byref(prob), _ptr_i32(il), int(k), ctypes.byref(need))
+    size_of = lib.pctc_topk_workspace_bytes if head8 is None else lib.pctc_i8_topk_workspace_bytes
+    st = size_of(ctypes.byref(prob), _ptr_i32(il), int(k), ctypes.byref(need))
     if st != 0:
-        raise PctcError(st, "pctc_topk_workspace_bytes")
+        raise PctcError(st, size_of.__name__)
     dev = hidden.device
     if workspace is None or workspace.numel() < need.value:
         workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
     classes = torch.empty((N, T, k), dtype=torch.int32, device=dev)
     logprobs = torch.empty((N, T, k), dtype=torch.float32, device=dev)
     stream = ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
-    st = lib.pctc_topk_decode(ctypes.byref(prob), _dptr(hidden), _dptr(W), _dptr(bias), _ptr_i32(il), int(k),
-                              _dptr(classes), _dptr(logprobs), _dptr(workspace), ctypes.c_size_t(workspace.numel()),
-                              stream)
+    rest = [_dptr(bias), _ptr_i32(il), int(k), _dptr(classes), _dptr(logprobs), _dptr(workspace),
+            ctypes.c_size_t(workspace.numel()), stream]
+    if head8 is None:
+        st = lib.pctc_topk_decode(ctypes.byref(prob), _dptr(hidden), _dptr(W), *rest)
+    else:
+        st = lib.pctc_i8_topk_decode(ctypes.byref(prob), _dptr(hidden), _dptr(W), _pitch(W), _dptr(head8.scales), *rest)
     if st != 0:
-        raise PctcError(st, "pctc_topk_decode")
+        raise PctcError(st, "pctc_topk_decode" if head8 is None else "pctc_i8_topk_decode")
     return dict(classes=classes, logprobs=logprobs, workspace=workspace)
 
 
@@ -497,7 +584,9 @@ def _native():
                                "there is no fallback implementation") from e
         names = ("pctc_clip_workspace_bytes", "pctc_clip_grad_norm", "pctc_grad_sqsum", "pctc_grad_scale",
                  "pctc_beam_workspace_bytes", "pctc_beam_select", "pctc_beam_reorder", "pctc_prefix_state_bytes",
-                 "pctc_prefix_advance", "pctc_prefix_read", "pctc_prefix_decode")
+                 "pctc_prefix_advance", "pctc_prefix_read", "pctc_prefix_decode", "pctc_embed",
+                 "pctc_embed_grad_workspace_bytes", "pctc_embed_grad", "pctc_dropout", "pctc_policy_workspace_bytes",
+                 "pctc_policy_loss", "pctc_i8_quantize", "pctc_i8_matmul", "pctc_i8_logits_workspace_bytes", "pctc_i8_logits")
         module.bind([ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in names], PctcError)
         _marshal = module
     return _marshal
@@ -606,7 +695,7 @@ def prefix_beam_decode(classes, logprobs, input_lengths, blank_id, beams):
 
 def beam_decode(hidden, W, bias, input_lengths, blank_id, beams, *, k=8, chunk=0, gemm_path=GEMM_AUTO, workspace=None):
     """CTC prefix beam search with the head: topk_decode's k best classes of every frame, then
-    prefix_beam_decode over them.  Returns the latter's dict plus the head's workspace."""
+    prefix_beam_decode over them.  W may be a QuantizedHead.  Returns the latter's dict plus the head's workspace."""
     best = topk_decode(hidden, W, bias, input_lengths, k, chunk=chunk, gemm_path=gemm_path, workspace=workspace)
     res = prefix_beam_decode(best["classes"], best["logprobs"], input_lengths, blank_id, beams)
     res["workspace"] = best["workspace"]
@@ -641,3 +730,105 @@ def beam_reorder(states, parents, *, lengths=None, time_axes=None, out=None):
     out = None if out is None else list(out)
     _native().beam_reorder(states, parents, lengths, None if time_axes is None else list(time_axes), out)
     return states if out is None else out
+
+
+def embed(tokens, W, *, scale=1.0, dtype=None, out=None):
+    """Rows of the vocabulary matrix: out[i] = scale * W[tokens[i]], a row of zeros where the token is outside [0, V) (-1).
+
+    tokens: contiguous int32 CUDA tensor of any shape; W [V,D] bf16 or fp32 with contiguous rows, or a QuantizedHead.
+    Returns [*tokens.shape, D] of type `dtype` (bf16 or fp32; default W's, bf16 from a QuantizedHead), or `out`.  Not
+    recorded by autograd: embed_grad is its gradient.
+    """
+    if isinstance(W, QuantizedHead):
+        return _native().embed(tokens, W.q, W.scales, scale, dtype, out)
+    return _native().embed(tokens, W, None, scale, dtype, out)
+
+
+def embed_grad(tokens, grad, vocab=None, *, dW=None, scale=1.0, accumulate=False, dtype=None, workspace=None):
+    """The gradient of embed with respect to W: dW[v] = scale * the sum of grad[i] over all i with tokens[i] == v.
+
+    grad [*tokens.shape, D] bf16 or fp32.  dW [V,D] is written whole (rows without a token: zeros), or, with
+    accumulate=True, added to: a tied head's gradient as pruned_ctc_fwd_bwd has left it.  Without dW one is made for `vocab`
+    rows, of type `dtype` (default grad's).  Sums are fp32 in a fixed order: repeated calls agree bit for bit.  Returns a
+    dict: dW and the workspace, which later calls on the same stream may take.  A written dW's version counts up.
+    """
+    dW, workspace = _native().embed_grad(tokens, grad, vocab, dW, scale, accumulate, dtype, workspace)
+    return dict(dW=dW, workspace=workspace)
+
+
+def dropout(x, p, seed, *, offset=0, step=None, residual=None, out=None):
+    """x with a share p of its values zeroed and the others scaled up, plus `residual`; also the backward pass:
+    dropout(grad, p, seed, offset=offset, step=step) is the gradient with respect to x.
+
+    The mask is a function of seed, offset (integers, taken modulo 2^64) and a value's index alone (prunedctc.h has the
+    formula); it is never stored.  p counts in steps of 1/65536, and the scale is exact for the step taken.  x bf16 or fp32
+    [..., D] whose rows lie one stride apart, residual and out likewise; out may be x or residual.  step: one int64 on the
+    device that is added to offset, for calls captured into a CUDA graph.  Not recorded by autograd; a written `out`'s
+    version counts up.
+    """
+    return _native().dropout(x, p, seed, offset, step, residual, out)
+
+
+POLICY_REDUCTIONS = ("tokens", "sequences", "sum")
+
+
+def policy_loss(logp, old_logp, advantages, *, ref_logp=None, mask=None, lengths=None, clip=(0.2, 0.2), kl_weight=0.0,
+                reduction="tokens", negated=False, want_grad=True, workspace=None):
+    """Clipped policy loss over log-probabilities of sampled tokens, with a KL term, and its gradient.
+
+    logp, old_logp, ref_logp (or None): fp32 [N,T] with contiguous rows, or [N] (whole sequences); advantages fp32 [N], or of
+    logp's shape.  Counted are the tokens before lengths[n] (int32 [N] on the device, or None) whose mask (bool, or None)
+    is set.  With r = exp(logp - old_logp) and f = ref_logp - logp a token's loss is
+    -min(A r, A min(max(r, 1 - clip[0]), 1 + clip[1])) + kl_weight * (exp(f) - 1 - f), averaged over the counted tokens
+    ("tokens"), over each row's and then over the rows that have any ("sequences"), or added up ("sum").
+    negated: logp, old_logp, ref_logp are losses (-log p), as pruned_ctc_fwd_bwd returns them, and so is the gradient taken.
+    Returns a dict of device tensors: loss, kl (mean of exp(f) - 1 - f), clipped (share of clipped tokens), each [1] fp32,
+    count [1] int32, grad (logp's shape, 0 where nothing is counted; not with want_grad=False), and the workspace.
+    """
+    if reduction not in POLICY_REDUCTIONS:
+        raise ValueError(f"reduction must be one of {POLICY_REDUCTIONS}")
+    low, high = clip
+    return _native().policy_loss(logp, old_logp, advantages, ref_logp, mask, lengths, low, high, kl_weight,
+                                 POLICY_REDUCTIONS.index(reduction), negated, want_grad, workspace)
+
+
+def ctc_policy_fwd_bwd(hidden, W, bias, targets, input_lengths, target_lengths, blank_id, old_losses, advantages, *,
+                       ref_losses=None, clip=(0.2, 0.2), kl_weight=0.0, reduction="sequences", **kw):
+    """A policy step over sampled transcripts: the CTC losses of the targets, the clipped policy loss over them, and the
+    gradients of that loss with respect to hidden, W and bias.
+
+    old_losses, ref_losses [N] fp32: the same transcripts' CTC losses under the sampling and the reference model;
+    advantages [N] fp32.  Utterances that pruned_ctc_fwd_bwd flags (infeasible and the like) are not counted.  kw goes to
+    pruned_ctc_fwd_bwd.  Returns its dict plus "policy", policy_loss's.
+    """
+    if kw.get("utt_weights") is not None or kw.get("forward_only"):
+        raise ValueError("utt_weights are the policy loss's, and both passes are run")
+    given = {k: v for k, v in kw.items() if k not in ("accumulate_dW", "trace", "out")}
+    first = pruned_ctc_fwd_bwd(hidden, W, bias, targets, input_lengths, target_lengths, blank_id, forward_only=True, **given)
+    policy = policy_loss(first["loss"], old_losses, advantages, ref_logp=ref_losses, mask=first["flags"] == 0, clip=clip,
+                         kl_weight=kl_weight, reduction=reduction, negated=True)
+    res = pruned_ctc_fwd_bwd(hidden, W, bias, targets, input_lengths, target_lengths, blank_id,
+                             **{**kw, "utt_weights": policy["grad"]})
+    res["policy"] = policy
+    return res
+
+
+def quantize_rows(x):
+    """The rows of x [rows, D] (bf16 or fp32) in 8-bit integers: q = round(x * (127 / max|x|)), scales = max|x| / 127.
+    Returns a QuantizedHead (q int8 [rows, D], rows a multiple of 16 bytes apart; scales fp32 [rows]).  A row with values
+    that are not finite gets the scale NaN."""
+    return QuantizedHead(*_native().quantize_rows(x))
+
+
+def matmul_i8(a, b, *, bias=None, dtype=None, status=None):
+    """C[i,j] = sum_k a.q[i,k] b.q[j,k] * a.scales[i] * b.scales[j] + bias[j] for two QuantizedHeads (rows of tokens and of
+    channels), fp32 or bf16 by `dtype`.  status: zeroed int32 CUDA tensor that receives a code if a bounded device wait
+    gives up."""
+    return _native().matmul_i8(a.q, a.scales, b.q, b.scales, bias, dtype, status)
+
+
+def quantized_logits(hidden, head, *, bias=None, dtype=None, workspace=None):
+    """Logits [..., V] of states hidden [..., D] (bf16 or fp32) under a QuantizedHead: the states are quantized row by row
+    and multiplied in 8-bit integers.  dtype: bf16 or fp32 (default hidden's).  workspace: a uint8 CUDA tensor to use (its
+    first word is the status word that workspace_status reads).  Not differentiable."""
+    return _native().quantized_logits(hidden, head.q, head.scales, bias, dtype, workspace)[0]

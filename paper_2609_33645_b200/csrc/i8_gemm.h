@@ -1,0 +1,18 @@
+// The head in 8-bit integers, as the recognition path calls it (host-side launch wrappers).
+#pragma once
+
+#include <cuda_runtime.h>
+
+namespace pctc {
+
+// C[i,j] = sum_k A[i,k] B[j,k] * a_scale[i] * b_scale[j] + bias[j]; A [m, k] and B [n, k] 16-byte aligned, pitches multiples
+// of 16.  status: device word that receives a non-zero code if a bounded wait gives up, or null.
+cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, const signed char* B, long long ldb,
+                    const float* b_scale, const void* bias, bool bias_bf16, int m, int n, int k, void* C, long long ldc,
+                    bool out_bf16, int* status, cudaStream_t stream);
+
+// q[r,:] = round(x[r,:] * 127 / max|x[r]|), scales[r] = max|x[r]| / 127; zeroes *clear (null: nothing).
+cudaError_t i8_quantize(const void* x, bool bf16, long long rows, long long cols, long long ld_x, signed char* q, long long ld_q,
+                        float* scales, int* clear, cudaStream_t stream);
+
+}  // namespace pctc

@@ -8,6 +8,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -31,6 +32,16 @@ struct {
   decltype(&pctc_prefix_advance) prefix_advance;
   decltype(&pctc_prefix_read) prefix_read;
   decltype(&pctc_prefix_decode) prefix_decode;
+  decltype(&pctc_embed) embed;
+  decltype(&pctc_embed_grad_workspace_bytes) embed_grad_workspace_bytes;
+  decltype(&pctc_embed_grad) embed_grad;
+  decltype(&pctc_dropout) dropout;
+  decltype(&pctc_policy_workspace_bytes) policy_workspace_bytes;
+  decltype(&pctc_policy_loss) policy_loss;
+  decltype(&pctc_i8_quantize) i8_quantize;
+  decltype(&pctc_i8_matmul) i8_matmul;
+  decltype(&pctc_i8_logits_workspace_bytes) i8_logits_workspace_bytes;
+  decltype(&pctc_i8_logits) i8_logits;
 } api;
 PyObject* error_type = nullptr;       // PctcError(status, what)
 
@@ -542,6 +553,310 @@ PyObject* prefix_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MARSHAL_END
 }
 
+// ---- the head's matrix and the loss ----
+
+bool is_float(at::ScalarType t) { return t == at::kBFloat16 || t == at::kFloat; }
+int32_t kind_of(at::ScalarType t) { return t == at::kFloat ? PCTC_FP32 : t == at::kBFloat16 ? PCTC_BF16 : PCTC_INT8; }
+at::ScalarType dtype_or(PyObject* o, at::ScalarType other) {
+  if (o == Py_None) return other;
+  if (!THPDtype_Check(o)) fail(PyExc_TypeError, "dtype must be a torch.dtype");
+  const at::ScalarType t = ((THPDtype*)o)->scalar_type;
+  if (!is_float(t)) fail(PyExc_ValueError, "dtype must be bf16 or fp32");
+  return t;
+}
+// A tensor [..., cols] as rows with one stride.
+struct RowView {
+  int64_t rows = 1, cols = 1, ld = 1;
+};
+RowView rows_of(const at::Tensor& t, const char* what) {
+  if (t.dim() < 1) fail(PyExc_ValueError, "%s must have a dimension", what);
+  RowView v;
+  v.cols = t.size(-1);
+  v.ld = std::max<int64_t>(1, v.cols);
+  if (t.numel() == 0) {
+    for (int64_t d = 0; d + 1 < t.dim(); ++d) v.rows *= t.size(d);
+    return v;
+  }
+  if (v.cols > 1 && t.stride(-1) != 1) fail(PyExc_ValueError, "%s must be contiguous in its last dimension", what);
+  int64_t next = 0;                       // the stride that the next dimension outwards has to have; 0: any
+  for (int64_t d = t.dim() - 2; d >= 0; --d) {
+    if (t.size(d) == 1) continue;
+    if (next == 0) v.ld = t.stride(d);
+    else if (t.stride(d) != next) fail(PyExc_ValueError, "the rows of %s must lie one stride apart", what);
+    next = t.stride(d) * t.size(d);
+    v.rows *= t.size(d);
+  }
+  if (v.rows > 1 && v.ld < v.cols) fail(PyExc_ValueError, "rows of %s overlap", what);
+  return v;
+}
+std::vector<int64_t> with_last(const at::Tensor& t, int64_t last, bool replace) {
+  std::vector<int64_t> s = t.sizes().vec();
+  if (replace) s.pop_back();
+  s.push_back(last);
+  return s;
+}
+bool has_shape(const at::Tensor& t, const std::vector<int64_t>& s) { return t.sizes().equals(s); }
+at::Tensor bytes_or(PyObject* given, size_t need, at::Device dev) {
+  const at::Tensor w = optional_tensor(given, "workspace");
+  if (w.defined() && (w.device() != dev || w.scalar_type() != at::kByte || !w.is_contiguous()))
+    fail(PyExc_ValueError, "workspace must be contiguous bytes on the device of the call");
+  return w.defined() && (size_t)w.numel() >= need ? w : empty({(int64_t)need}, at::kByte, dev);
+}
+uint64_t word(PyObject* o, const char* what) {
+  if (!PyLong_Check(o)) fail(PyExc_TypeError, "%s must be an integer", what);
+  return PyLong_AsUnsignedLongLongMask(o);
+}
+bool truth(PyObject* o) {
+  const int t = PyObject_IsTrue(o);
+  if (t < 0) throw Failed{};
+  return t != 0;
+}
+const at::Tensor& token_ids(PyObject* o) {
+  const at::Tensor& t = tensor(o, "tokens");
+  if (!t.is_cuda() || t.scalar_type() != at::kInt || !t.is_contiguous()) fail(PyExc_ValueError, "tokens must be a contiguous int32 CUDA tensor");
+  return t;
+}
+// An 8-bit matrix [rows, cols] with a scale a row.
+void check_i8(const at::Tensor& q, const at::Tensor& s, at::Device dev, const char* what) {
+  if (q.scalar_type() != at::kChar || q.dim() != 2 || q.device() != dev || s.device() != dev || s.scalar_type() != at::kFloat ||
+      s.dim() != 1 || s.size(0) != q.size(0) || !s.is_contiguous())
+    fail(PyExc_ValueError, "%s must be int8 [rows, D] with contiguous fp32 scales [rows], on one device", what);
+}
+// The pitch of its rows for the product (of a single row, any that will do).
+int64_t i8_pitch(const RowView& v) { return v.rows > 1 ? v.ld : (v.cols + 15) / 16 * 16; }
+
+// embed(tokens, W, row_scales or None, scale, dtype or None, out or None) -> out
+PyObject* embed(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 6);
+  const at::Tensor& t = token_ids(a[0]);
+  const at::Tensor& W = tensor(a[1], "W");
+  const at::Tensor s = optional_tensor(a[2], "row_scales");
+  const at::Device dev = t.device();
+  if (W.dim() != 2 || W.device() != dev) fail(PyExc_ValueError, "W must be [V, D] on the tokens' device");
+  if (s.defined()) check_i8(W, s, dev, "a quantized head");
+  else if (!is_float(W.scalar_type())) fail(PyExc_ValueError, "W must be bf16 or fp32, or a quantized head");
+  const RowView w = rows_of(W, "W");
+  const at::Tensor given = optional_tensor(a[5], "out");
+  const at::ScalarType type = dtype_or(a[4], given.defined() ? given.scalar_type() : s.defined() ? at::kBFloat16 : W.scalar_type());
+  const std::vector<int64_t> shape = with_last(t, W.size(1), false);
+  if (given.defined() && (given.device() != dev || given.scalar_type() != type || !is_float(type) || !has_shape(given, shape)))
+    fail(PyExc_ValueError, "out must be [*tokens.shape, D] of the asked type (bf16 or fp32) on the tokens' device");
+  const c10::cuda::CUDAGuard guard(dev);
+  const at::Tensor out = given.defined() ? given : empty(shape, type, dev);
+  const RowView o = rows_of(out, "out");
+  const pctc_embed_t p{t.numel(), W.size(0), W.size(1), w.ld, o.ld, kind_of(W.scalar_type()), kind_of(type), (float)real(a[3]), 0};
+  check(api.embed(&p, (const int32_t*)ptr(t), ptr(W), (const float*)ptr(s), ptr(out), stream_of(dev)), "pctc_embed");
+  if (given.defined()) written(given);
+  return THPVariable_Wrap(out);
+  MARSHAL_END
+}
+// embed_grad(tokens, grad, V or None, dW or None, scale, accumulate, dtype or None, workspace) -> (dW, workspace)
+PyObject* embed_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 8);
+  const at::Tensor& t = token_ids(a[0]);
+  const at::Tensor& g = tensor(a[1], "grad");
+  const at::Device dev = t.device();
+  if (g.device() != dev || !is_float(g.scalar_type()) || g.dim() != t.dim() + 1 || !g.sizes().slice(0, t.dim()).equals(t.sizes()))
+    fail(PyExc_ValueError, "grad must be [*tokens.shape, D], bf16 or fp32, on the tokens' device");
+  const int64_t D = g.size(-1);
+  const at::Tensor given = optional_tensor(a[3], "dW");
+  const bool accumulate = truth(a[5]);
+  if (!given.defined() && (accumulate || a[2] == Py_None)) fail(PyExc_ValueError, "%s", accumulate ? "accumulating needs a dW" : "vocab or dW must be given");
+  const at::ScalarType type = dtype_or(a[6], given.defined() ? given.scalar_type() : g.scalar_type());
+  const int64_t V = given.defined() && given.dim() == 2 ? given.size(0) : a[2] == Py_None ? 0 : integer(a[2]);
+  if (given.defined() && (given.dim() != 2 || given.size(1) != D || given.device() != dev || given.scalar_type() != type ||
+                          !is_float(type) || (a[2] != Py_None && integer(a[2]) != V)))
+    fail(PyExc_ValueError, "dW must be [V, D], bf16 or fp32, on the tokens' device");
+  if (V < 1 || D < 1) fail(PyExc_ValueError, "vocab and D must be at least 1");
+  const c10::cuda::CUDAGuard guard(dev);
+  const RowView x = rows_of(g, "grad");
+  const int64_t ld_w = given.defined() ? rows_of(given, "dW").ld : D;
+  const pctc_embed_t p{t.numel(), V, D, ld_w, x.ld, kind_of(type), kind_of(g.scalar_type()), (float)real(a[4]), accumulate ? 1 : 0};
+  size_t need = 0;
+  check(api.embed_grad_workspace_bytes(&p, &need), "pctc_embed_grad_workspace_bytes");
+  const at::Tensor dW = given.defined() ? given : empty({V, D}, type, dev), ws = bytes_or(a[7], need, dev);
+  check(api.embed_grad(&p, (const int32_t*)ptr(t), ptr(g), ptr(dW), ptr(ws), (size_t)ws.numel(), stream_of(dev)), "pctc_embed_grad");
+  if (given.defined()) written(given);
+  return pair(dW, ws);
+  MARSHAL_END
+}
+// dropout(x, p, seed, offset, step or None, residual or None, out or None) -> out
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 7);
+  const at::Tensor& x = tensor(a[0], "x");
+  if (!x.is_cuda() || !is_float(x.scalar_type())) fail(PyExc_ValueError, "x must be a bf16 or fp32 CUDA tensor");
+  const at::Device dev = x.device();
+  const at::Tensor step = optional_tensor(a[4], "step"), res = optional_tensor(a[5], "residual"), given = optional_tensor(a[6], "out");
+  if (step.defined() && (step.scalar_type() != at::kLong || step.numel() != 1 || step.device() != dev))
+    fail(PyExc_ValueError, "step must be one int64 value on the device of x");
+  for (const at::Tensor* t : {&res, &given})
+    if (t->defined() && (t->device() != dev || t->scalar_type() != x.scalar_type() || !t->sizes().equals(x.sizes())))
+      fail(PyExc_ValueError, "residual and out must be of x's shape, type and device");
+  const c10::cuda::CUDAGuard guard(dev);
+  const at::Tensor out = given.defined() ? given : empty(x.sizes(), x.scalar_type(), dev);
+  const RowView v = rows_of(x, "x"), o = rows_of(out, "out");
+  RowView r;
+  if (res.defined()) r = rows_of(res, "residual");
+  pctc_dropout_t p{v.rows, v.cols, v.ld, r.ld, o.ld, kind_of(x.scalar_type()), 0, real(a[1]), word(a[2], "seed"), word(a[3], "offset")};
+  check(api.dropout(&p, ptr(x), ptr(res), (const int64_t*)ptr(step), ptr(out), stream_of(dev)), "pctc_dropout");
+  if (given.defined()) written(given);
+  return THPVariable_Wrap(out);
+  MARSHAL_END
+}
+// policy_loss(logp, old_logp, advantages, ref_logp, mask, lengths (each or None), low, high, kl_weight, reduction, negated,
+//             want_grad, workspace) -> dict
+PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 13);
+  const at::Tensor& x = tensor(a[0], "logp");
+  if (!x.is_cuda() || x.scalar_type() != at::kFloat || x.dim() < 1 || x.dim() > 2) fail(PyExc_ValueError, "logp must be an fp32 CUDA tensor [N, T] or [N]");
+  const at::Device dev = x.device();
+  const int64_t N = x.size(0), T = x.dim() == 2 ? x.size(1) : 1;
+  const auto same = [&](PyObject* o, at::ScalarType type, const char* what) {
+    const at::Tensor t = optional_tensor(o, what);
+    if (t.defined() && (t.scalar_type() != type || !t.sizes().equals(x.sizes()) || t.device() != dev))
+      fail(PyExc_ValueError, "%s must be %s of logp's shape on its device", what, type == at::kBool ? "bool" : "fp32");
+    return t;
+  };
+  const auto stride = [&](const at::Tensor& t, const char* what) -> int64_t {
+    if (!t.defined() || t.numel() == 0) return T;
+    if (T > 1 && t.stride(1) != 1) fail(PyExc_ValueError, "%s must be contiguous in its last dimension", what);
+    if (N > 1 && t.stride(0) < T) fail(PyExc_ValueError, "rows of %s overlap", what);
+    return N > 1 ? t.stride(0) : T;
+  };
+  tensor(a[1], "old_logp");
+  const at::Tensor old = same(a[1], at::kFloat, "old_logp"), ref = same(a[3], at::kFloat, "ref_logp"), mask = same(a[4], at::kBool, "mask");
+  const at::Tensor& adv = tensor(a[2], "advantages");
+  const bool each = adv.sizes().equals(x.sizes());
+  if (adv.scalar_type() != at::kFloat || adv.device() != dev ||
+      (!each && (adv.dim() != 1 || adv.size(0) != N || !adv.is_contiguous())))
+    fail(PyExc_ValueError, "advantages must be fp32, contiguous [N] or of logp's shape, on its device");
+  const at::Tensor lengths = optional_tensor(a[5], "lengths");
+  if (lengths.defined() && (lengths.scalar_type() != at::kInt || lengths.dim() != 1 || lengths.size(0) != N || !lengths.is_contiguous() || lengths.device() != dev))
+    fail(PyExc_ValueError, "lengths must be contiguous int32 [N] on the device of logp");
+  pctc_policy_t p = {};
+  p.N = N;
+  p.T = T;
+  p.ld_logp = stride(x, "logp");
+  p.ld_old = stride(old, "old_logp");
+  p.ld_ref = stride(ref, "ref_logp");
+  p.ld_adv = each ? stride(adv, "advantages") : 0;
+  p.ld_mask = stride(mask, "mask");
+  p.ld_grad = T;
+  p.clip_low = real(a[6]);
+  p.clip_high = real(a[7]);
+  p.kl_weight = real(a[8]);
+  p.reduction = (int32_t)integer(a[9]);
+  p.negated = truth(a[10]) ? 1 : 0;
+  const c10::cuda::CUDAGuard guard(dev);
+  size_t need = 0;
+  check(api.policy_workspace_bytes(&p, &need), "pctc_policy_workspace_bytes");
+  const at::Tensor ws = bytes_or(a[12], need, dev);
+  const bool want_grad = truth(a[11]);
+  Shared out(dev);                          // what the call writes side by side: loss, KL, share of clipped tokens
+  out.add({3}, at::kFloat);
+  out.add({1}, at::kInt);
+  if (want_grad) out.add(x.sizes(), at::kFloat);
+  out.allocate();
+  const at::Tensor stats = out.get(0), count = out.get(1), grad = want_grad ? out.get(2) : at::Tensor();
+  check(api.policy_loss(&p, (const float*)ptr(x), (const float*)ptr(old), (const float*)ptr(ref), (const float*)ptr(adv),
+                        (const uint8_t*)ptr(mask), (const int32_t*)ptr(lengths), want_grad ? (float*)ptr(grad) : nullptr,
+                        (float*)ptr(stats), (int32_t*)ptr(count), ptr(ws), (size_t)ws.numel(), stream_of(dev)),
+        "pctc_policy_loss");
+  PyObject* d = PyDict_New();
+  if (!d) return nullptr;
+  put(d, "loss", stats.narrow(0, 0, 1));
+  put(d, "kl", stats.narrow(0, 1, 1));
+  put(d, "clipped", stats.narrow(0, 2, 1));
+  put(d, "count", count);
+  if (want_grad) put(d, "grad", grad);
+  put(d, "workspace", ws);
+  return d;
+  MARSHAL_END
+}
+// quantize_rows(x) -> (q, scales)
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 1);
+  const at::Tensor& x = tensor(a[0], "x");
+  if (!x.is_cuda() || !is_float(x.scalar_type()) || x.dim() != 2 || x.size(1) < 1) fail(PyExc_ValueError, "x must be a bf16 or fp32 CUDA tensor [rows, D]");
+  const at::Device dev = x.device();
+  const RowView v = rows_of(x, "x");
+  const int64_t ld = (v.cols + 15) / 16 * 16;
+  const c10::cuda::CUDAGuard guard(dev);
+  const at::Tensor whole = empty({v.rows, ld}, at::kChar, dev), scales = empty({v.rows}, at::kFloat, dev);
+  check(api.i8_quantize(v.rows, v.cols, kind_of(x.scalar_type()), ptr(x), v.ld, (int8_t*)ptr(whole), ld, (float*)ptr(scales), stream_of(dev)),
+        "pctc_i8_quantize");
+  return pair(ld == v.cols ? whole : whole.narrow(1, 0, v.cols), scales);
+  MARSHAL_END
+}
+at::Tensor bias_of(PyObject* o, int64_t n, at::Device dev) {
+  const at::Tensor b = optional_tensor(o, "bias");
+  if (b.defined() && (!is_float(b.scalar_type()) || b.dim() != 1 || b.size(0) != n || !b.is_contiguous() || b.device() != dev))
+    fail(PyExc_ValueError, "bias must be contiguous [channels], bf16 or fp32, on the operands' device");
+  return b;
+}
+pctc_i8_t i8_problem(int64_t m, int64_t n, int64_t k, at::ScalarType type, int64_t lda, int64_t ldb, const at::Tensor& bias) {
+  for (const int64_t v : {m, n, k})
+    if (v > INT32_MAX) check(PCTC_ERR_UNSUPPORTED, "8-bit product");
+  return pctc_i8_t{(int32_t)m, (int32_t)n, (int32_t)k, kind_of(type), lda, ldb, n, bias.defined() ? kind_of(bias.scalar_type()) : 0, 0};
+}
+// matmul_i8(a, a_scales, b, b_scales, bias or None, dtype or None, status or None) -> [m, n]
+PyObject* matmul_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 7);
+  const at::Tensor& A = tensor(a[0], "a");
+  const at::Tensor& as = tensor(a[1], "a_scales");
+  const at::Tensor& B = tensor(a[2], "b");
+  const at::Tensor& bs = tensor(a[3], "b_scales");
+  const at::Device dev = A.device();
+  if (!A.is_cuda()) fail(PyExc_ValueError, "the operands must be CUDA tensors");
+  check_i8(A, as, dev, "a");
+  check_i8(B, bs, dev, "b");
+  if (A.size(1) != B.size(1)) fail(PyExc_ValueError, "the operands must have rows of one length");
+  const at::Tensor bias = bias_of(a[4], B.size(0), dev), status = optional_tensor(a[6], "status");
+  if (status.defined() && (status.scalar_type() != at::kInt || status.numel() < 1 || status.device() != dev || !status.is_contiguous()))
+    fail(PyExc_ValueError, "status must be an int32 tensor on the operands' device");
+  const at::ScalarType type = dtype_or(a[5], at::kFloat);
+  const pctc_i8_t p = i8_problem(A.size(0), B.size(0), A.size(1), type, i8_pitch(rows_of(A, "a")), i8_pitch(rows_of(B, "b")), bias);
+  const c10::cuda::CUDAGuard guard(dev);
+  const at::Tensor C = empty({A.size(0), B.size(0)}, type, dev);
+  check(api.i8_matmul(&p, (const int8_t*)ptr(A), (const float*)ptr(as), (const int8_t*)ptr(B), (const float*)ptr(bs), ptr(bias), ptr(C),
+                      (int32_t*)ptr(status), stream_of(dev)),
+        "pctc_i8_matmul");
+  if (status.defined()) written(status);
+  return THPVariable_Wrap(C);
+  MARSHAL_END
+}
+// quantized_logits(x, q, scales, bias or None, dtype or None, workspace) -> (logits, workspace)
+PyObject* quantized_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  MARSHAL_BEGIN
+  want(n, 6);
+  const at::Tensor& x = tensor(a[0], "hidden");
+  const at::Tensor& q = tensor(a[1], "q");
+  const at::Tensor& s = tensor(a[2], "scales");
+  const at::Device dev = x.device();
+  if (!x.is_cuda() || !is_float(x.scalar_type())) fail(PyExc_ValueError, "hidden must be a bf16 or fp32 CUDA tensor");
+  check_i8(q, s, dev, "the head");
+  const RowView v = rows_of(x, "hidden");
+  if (v.cols != q.size(1)) fail(PyExc_ValueError, "hidden must be [..., D] for a head [V, D]");
+  const at::Tensor bias = bias_of(a[3], q.size(0), dev);
+  const at::ScalarType type = dtype_or(a[4], x.scalar_type());
+  const pctc_i8_t p = i8_problem(v.rows, q.size(0), v.cols, type, v.ld, i8_pitch(rows_of(q, "the head")), bias);
+  const c10::cuda::CUDAGuard guard(dev);
+  size_t need = 0;
+  check(api.i8_logits_workspace_bytes(&p, &need), "pctc_i8_logits_workspace_bytes");
+  const at::Tensor C = empty(with_last(x, q.size(0), true), type, dev), ws = bytes_or(a[5], need, dev);
+  check(api.i8_logits(&p, ptr(x), kind_of(x.scalar_type()), (const int8_t*)ptr(q), (const float*)ptr(s), ptr(bias), ptr(C), ptr(ws),
+                      (size_t)ws.numel(), stream_of(dev)),
+        "pctc_i8_logits");
+  return pair(C, ws);
+  MARSHAL_END
+}
+
 // bind(addresses of the C entry points in the order of `api`, PctcError)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MARSHAL_BEGIN
@@ -559,7 +874,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind), FAST(clip_grad_norm), FAST(grad_sqsum), FAST(grad_scale), FAST(beam_select),
                          FAST(beam_reorder), FAST(prefix_check), FAST(prefix_start), FAST(prefix_advance),
-                         FAST(prefix_read), FAST(prefix_decode),
+                         FAST(prefix_read), FAST(prefix_decode), FAST(embed), FAST(embed_grad), FAST(dropout),
+                         FAST(policy_loss), FAST(quantize_rows), FAST(matmul_i8), FAST(quantized_logits),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

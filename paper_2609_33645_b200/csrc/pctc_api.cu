@@ -1,6 +1,7 @@
 // C ABI of libprunedctc: argument validation, workspace layout and the stream
 // order of Algorithm 1.  All arithmetic happens in the kernels this file launches.
 #include "../../include/prunedctc.h"
+#include "i8_gemm.h"
 #include "pctc_internal.h"
 
 #include <cmath>
@@ -786,17 +787,41 @@ pctc_status_t pctc_topk_workspace_bytes(const pctc_problem_t* problem, const int
   return PCTC_OK;
 }
 
-pctc_status_t pctc_topk_decode(const pctc_problem_t* p, const void* hidden, const void* W, const void* bias,
-                               const int32_t* input_lengths, int32_t k, int32_t* topk_classes, float* topk_logprobs,
-                               void* workspace, size_t workspace_bytes, void* stream_v) {
+namespace {
+// The head in 8 bits: rows q [V, D] of pitch ld with a scale each.  The frames are quantized behind the rest of the plan.
+struct Head8 {
+  const int8_t* q;
+  long long ld;
+  const float* scales;
+};
+struct Head8Plan {
+  long long ld;
+  size_t o_q, o_scales, total;
+};
+Head8Plan head8_plan(const TopkPlan& t) {
+  Head8Plan h;
+  h.ld = ((long long)t.g.D + 15) / 16 * 16;
+  h.o_q = t.total;
+  h.o_scales = h.o_q + up((size_t)t.g.M * h.ld);
+  h.total = h.o_scales + up((size_t)t.g.M * 4);
+  return h;
+}
+
+// head8 null: the head is W.
+pctc_status_t topk_call(const pctc_problem_t* p, const void* hidden, const void* W, const Head8* head8, const void* bias,
+                        const int32_t* input_lengths, int32_t k, int32_t* topk_classes, float* topk_logprobs,
+                        void* workspace, size_t workspace_bytes, void* stream_v) {
   TopkPlan t;
   pctc_status_t st = topk_plan(p, input_lengths, k, &t);
   if (st != PCTC_OK) return st;
   const GreedyPlan& g = t.g;
   if (!hidden || !W || !topk_classes || !workspace) return PCTC_ERR_INVALID_ARG;
-  if (workspace_bytes < t.total) return PCTC_ERR_WORKSPACE_TOO_SMALL;
+  if (head8 && (g.D > PCTC_I8_MAX_K || head8->ld >= MAX_ELEMENTS)) return PCTC_ERR_UNSUPPORTED;
+  if (head8 && (head8->ld < g.D || head8->ld % 16 || !head8->scales || ((size_t)head8->scales & 3))) return PCTC_ERR_INVALID_ARG;
+  const Head8Plan h8 = head8_plan(t);
+  if (workspace_bytes < (head8 ? h8.total : t.total)) return PCTC_ERR_WORKSPACE_TOO_SMALL;
   if (((size_t)workspace & (ALIGN - 1)) || ((size_t)hidden & 15) || ((size_t)W & 15)) return PCTC_ERR_INVALID_ARG;
-  if (g.use_umma && !umma_available()) return PCTC_ERR_CUDA;
+  if ((g.use_umma || head8) && !umma_available()) return PCTC_ERR_CUDA;
   cudaStream_t stream = (cudaStream_t)stream_v;
   if (stream_is_capturing(stream)) return PCTC_ERR_UNSUPPORTED;
   char* ws = (char*)workspace;
@@ -816,19 +841,51 @@ pctc_status_t pctc_topk_decode(const pctc_problem_t* p, const void* hidden, cons
   int* d_idx = (int*)(ws + t.o_idx);
   float2* d_ms = (float2*)(ws + t.o_ms);
   PCTC_CUDA(stack_frames(hidden, d_X, N, g.T, D, g.elem, d_meta + 2 * N + 1, d_meta + N, M, d_status, stream));
+  signed char* d_q = (signed char*)(ws + h8.o_q);
+  float* d_scales = (float*)(ws + h8.o_scales);
+  if (head8) PCTC_CUDA(i8_quantize(d_X, g.bf16, M, D, D, d_q, h8.ld, d_scales, nullptr, stream));
   for (long long v0 = 0; v0 < g.V; v0 += t.chunk) {          // the head in vocabulary chunks, logits never kept
     const int Cc = (int)((g.V - v0 < t.chunk) ? (g.V - v0) : t.chunk);
-    Epilogue e;
-    e.kind = EPI_STORE_F32;
-    e.out = d_logits;
-    e.ld = t.chunk;
-    GemmCall c{d_X, D, false, (const char*)W + (size_t)v0 * D * g.elem, D, false, M, Cc, D};
-    PCTC_CUDA(run_gemm(g.use_umma, g.bf16, c, e, d_status, stream));
+    if (head8) {
+      PCTC_CUDA(i8_gemm(d_q, h8.ld, d_scales, (const signed char*)head8->q + v0 * head8->ld, head8->ld, head8->scales + v0,
+                        nullptr, false, M, Cc, D, d_logits, t.chunk, false, d_status, stream));
+    } else {
+      Epilogue e;
+      e.kind = EPI_STORE_F32;
+      e.out = d_logits;
+      e.ld = t.chunk;
+      GemmCall c{d_X, D, false, (const char*)W + (size_t)v0 * D * g.elem, D, false, M, Cc, D};
+      PCTC_CUDA(run_gemm(g.use_umma, g.bf16, c, e, d_status, stream));
+    }
     PCTC_CUDA(topk_update(k, d_logits, t.chunk, M, Cc, v0, bias, g.bf16, d_val, d_idx, d_ms, v0 == 0, stream));
   }
   PCTC_CUDA(topk_finish(k, d_val, d_idx, d_ms, d_meta + N, d_meta, N, g.T, topk_classes, topk_logprobs, stream));
 #undef PCTC_CUDA
   return PCTC_OK;
+}
+}  // namespace
+
+pctc_status_t pctc_topk_decode(const pctc_problem_t* p, const void* hidden, const void* W, const void* bias,
+                               const int32_t* input_lengths, int32_t k, int32_t* topk_classes, float* topk_logprobs,
+                               void* workspace, size_t workspace_bytes, void* stream_v) {
+  return topk_call(p, hidden, W, nullptr, bias, input_lengths, k, topk_classes, topk_logprobs, workspace, workspace_bytes, stream_v);
+}
+
+pctc_status_t pctc_i8_topk_workspace_bytes(const pctc_problem_t* problem, const int32_t* input_lengths_host, int32_t k,
+                                           size_t* bytes_out) {
+  if (!bytes_out) return PCTC_ERR_INVALID_ARG;
+  TopkPlan t;
+  const pctc_status_t st = topk_plan(problem, input_lengths_host, k, &t);
+  if (st != PCTC_OK) return st;
+  *bytes_out = head8_plan(t).total;
+  return PCTC_OK;
+}
+
+pctc_status_t pctc_i8_topk_decode(const pctc_problem_t* p, const void* hidden, const int8_t* W, int64_t ld_w, const float* w_scales,
+                                  const void* bias, const int32_t* input_lengths, int32_t k, int32_t* topk_classes,
+                                  float* topk_logprobs, void* workspace, size_t workspace_bytes, void* stream_v) {
+  const Head8 head{W, ld_w, w_scales};
+  return topk_call(p, hidden, W, &head, bias, input_lengths, k, topk_classes, topk_logprobs, workspace, workspace_bytes, stream_v);
 }
 
 pctc_status_t pctc_greedy_workspace_bytes(const pctc_problem_t* problem, const int32_t* input_lengths_host,

@@ -54,6 +54,26 @@ inline bool spans_conflict(Span* s, size_t n) {
   return false;
 }
 
+// `rows` rows of `cols` values of `size` bytes, `ld` values apart (p null: nothing).
+struct Rows {
+  const void* p;
+  long long rows, ld, cols;
+  size_t size;
+  size_t lo() const { return (size_t)p; }
+  size_t hi() const { return lo() + ((size_t)(rows - 1) * ld + cols) * size; }
+  bool empty() const { return !p || rows <= 0 || cols <= 0; }
+  bool same(const Rows& o) const { return p == o.p && size == o.size && (rows == 1 || ld == o.ld); }
+  // Rows of one pitch that interleave (columns of one buffer) are told apart; other pitches count as one range.
+  bool overlaps(const Rows& o) const {
+    if (empty() || o.empty() || hi() <= o.lo() || o.hi() <= lo()) return false;
+    const size_t pitch = (size_t)ld * size;
+    if (rows == 1 || o.rows == 1 || pitch != (size_t)o.ld * o.size) return true;
+    const size_t d = o.lo() >= lo() ? (o.lo() - lo()) % pitch : (pitch - (lo() - o.lo()) % pitch) % pitch;
+    return d < (size_t)cols * size || pitch - d < (size_t)o.cols * o.size;
+  }
+};
+constexpr long long MAX_ELEMENTS = 1LL << 40;   // of one array of the operators around the head
+
 // ---------------------------------------------------------------------------
 // Contractions:  acc(i,j) = sum_k A(i,k) * B(j,k),  then an epilogue.
 // ---------------------------------------------------------------------------
