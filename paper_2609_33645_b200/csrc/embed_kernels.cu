@@ -5,11 +5,14 @@
 //
 // The gradient is made without atomics on values: the positions are sorted by token, positions of one token in
 // ascending order, and the sums run over the sorted positions, so repeated calls agree bit for bit.
-//   k_sort_tokens  one CTA for each of about 148 ranges of the vocabulary reads all tokens twice (they are in L2) and
-//                  lays its own out in order: no CTA needs another's result, so one launch sorts.
+//   k_sort_tokens  a CTA for each of about 148 ranges of the vocabulary reads all tokens (they are in L2) and
+//                  lays its own out in order: no CTA needs another's result, so one launch sorts.  Meanwhile
+//                  other CTAs of that launch fill dW with zeros, whatever the tokens are.
 //   k_embed_grad   a thread sums eight columns over a window of sorted positions.  A token whose positions pass the
 //                  end of a window leaves a partial sum for each window, and the last of its threads adds these up in
-//                  order.  The same launch fills the rows of tokens that do not occur with zeros.
+//                  order.
+//   k_embed_grad_few  few tokens: all of it in one launch.  A CTA fills its rows with zeros, finds its own among all
+//                  tokens meanwhile and writes their sums behind the zeros.
 // Both directions are bound by HBM.
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
@@ -94,41 +97,106 @@ constexpr int SORT_THREADS = 512;
 constexpr int SORT_WARPS = SORT_THREADS / 32;
 constexpr int SORT_BUCKETS = 148;                // ranges of the vocabulary: one CTA on every SM of a B200
 constexpr int SORT_MAX_WIDTH = 2048;             // tokens of a range: a counter for each and every warp, 128 KB
+constexpr int SORT_AHEAD = 4;                    // groups of four tokens that a thread loads before it looks at the first
+constexpr int SORT_KEEP = 256;                   // tokens of its range that a warp keeps; one with more reads its run again
+constexpr int SORT_RUN_BITS = 21;                // a kept token: 11 bits of token, 21 of position in the warp's run
+
+// Zeros into a matrix, in pieces of about ZERO_BYTES: of rows, or of the bytes of a matrix without gaps.
+constexpr int ZERO_BYTES = 32768;
+struct ZeroArgs {
+  char* p;
+  long long rows, ld, width;                     // bytes
+  long long piece;                               // rows a piece
+  long long pieces;
+};
+__device__ __forceinline__ void zero_row(char* row, long long n, int lane, int lanes) {
+  const long long head = min((long long)((16 - ((size_t)row & 15)) & 15), n) / 2, vecs = (n - 2 * head) / 16;
+  for (long long i = lane; i < head; i += lanes) reinterpret_cast<short*>(row)[i] = 0;
+  uint4* body = reinterpret_cast<uint4*>(row + 2 * head);
+#pragma unroll 4
+  for (long long i = lane; i < vecs; i += lanes) body[i] = make_uint4(0u, 0u, 0u, 0u);
+  for (long long i = head + vecs * 8 + lane; i < n / 2; i += lanes) reinterpret_cast<short*>(row)[i] = 0;
+}
+template <int THREADS>
+__device__ __forceinline__ void zero_piece(const ZeroArgs& a, long long piece) {
+  const long long r0 = piece * a.piece, r1 = min(r0 + a.piece, a.rows);
+  if (a.width == a.ld) {
+    zero_row(a.p + r0 * a.ld, (r1 - r0) * a.ld, threadIdx.x, THREADS);
+  } else {
+    for (long long r = r0 + (threadIdx.x >> 5); r < r1; r += THREADS / 32) zero_row(a.p + r * a.ld, a.width, threadIdx.x & 31, 32);
+  }
+}
 
 struct SortArgs {
   const int* tokens;
   int M;
   long long V;
   int width;                                     // tokens of a range
-  int* order;                                    // [M] positions by (token, position)
-  int* key;                                      // [M] their tokens
+  int2* sorted;                                  // [M] (position, token) by token, then position; (0, -1) behind them
   int* first;                                    // [V + 1] where a token's positions begin
   int* clear;                                    // counters of k_embed_grad, zeroed here
   long long n_clear;
+  unsigned buckets;                              // blocks that sort; the others fill dW with zeros
+  ZeroArgs zero;
 };
 
+// Tokens p .. p + 3 of a run that ends at p1 (p is a multiple of 4); -1 behind the end.
+__device__ __forceinline__ int4 four_tokens(const int* tokens, bool aligned, int p, int p1) {
+  if (aligned && p + 4 <= p1) return *reinterpret_cast<const int4*>(tokens + p);
+  return make_int4(p < p1 ? tokens[p] : -1, p + 1 < p1 ? tokens[p + 1] : -1, p + 2 < p1 ? tokens[p + 2] : -1,
+                   p + 3 < p1 ? tokens[p + 3] : -1);
+}
+
 __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) {
-  extern __shared__ int count[];                 // [SORT_WARPS][width], then the offsets of the warps
-  __shared__ int below_sum[SORT_WARPS], scan_sum[SORT_WARPS];
+  extern __shared__ int count[];                 // [SORT_WARPS][width]: counts, then where each warp's next one goes
+  __shared__ unsigned kept[SORT_WARPS][SORT_KEEP];
+  __shared__ int below_sum[SORT_WARPS], scan_sum[SORT_WARPS], count_end;
+  if (blockIdx.x >= a.buckets) {
+    zero_piece<SORT_THREADS>(a.zero, blockIdx.x - a.buckets);
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long lo = (long long)blockIdx.x * a.width;
-  const int width = (int)min((long long)a.width, a.V - lo);
-  for (long long i = (long long)blockIdx.x * SORT_THREADS + threadIdx.x; i < a.n_clear; i += (long long)gridDim.x * SORT_THREADS)
+  const int lo = (int)blockIdx.x * a.width, width = (int)min((long long)a.width, a.V - lo);
+  for (long long i = (long long)blockIdx.x * SORT_THREADS + threadIdx.x; i < a.n_clear; i += (long long)a.buckets * SORT_THREADS)
     a.clear[i] = 0;
   for (int i = threadIdx.x; i < SORT_WARPS * a.width; i += SORT_THREADS) count[i] = 0;
   __syncthreads();
 
-  // a warp takes a run of positions, so that warps, steps and lanes in order are positions in order
-  const int run = (int)(((long long)a.M + SORT_WARPS * 32 - 1) / (SORT_WARPS * 32)) * 32;
+  // a warp takes a run of positions, so that warps, steps, lanes and a lane's four in order are positions in order
+  const int run = (int)(((long long)a.M + SORT_WARPS * 128 - 1) / (SORT_WARPS * 128)) * 128;
   const int p0 = (int)min((long long)warp * run, (long long)a.M), p1 = (int)min((long long)p0 + run, (long long)a.M);
+  const bool aligned = ((size_t)a.tokens & 15) == 0;
+  const unsigned lower = (1u << lane) - 1;
   int* mine = count + warp * a.width;
-  int below = 0;
-#pragma unroll 8
-  for (int p = p0 + lane; p < p1; p += 32) {
-    const int t = a.tokens[p];
-    if (t < 0) continue;
-    if (t < lo) ++below;
-    else if (t - lo < width) atomicAdd(&mine[t - lo], 1);
+  int below = 0, n = 0;
+  for (int p = p0 + lane * 4; p - lane * 4 < p1; p += 128 * SORT_AHEAD) {
+    int4 t[SORT_AHEAD];
+#pragma unroll
+    for (int k = 0; k < SORT_AHEAD; ++k) t[k] = four_tokens(a.tokens, aligned, p + k * 128, p1);
+#pragma unroll
+    for (int k = 0; k < SORT_AHEAD; ++k) {
+      const int v[4] = {t[k].x - lo, t[k].y - lo, t[k].z - lo, t[k].w - lo};
+      const bool any = (unsigned)v[0] < (unsigned)width || (unsigned)v[1] < (unsigned)width || (unsigned)v[2] < (unsigned)width ||
+                       (unsigned)v[3] < (unsigned)width;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) below += v[j] < 0 && v[j] >= -lo;      // tokens 0 .. lo - 1
+      if (!__any_sync(0xffffffffu, any)) continue;
+      int before = 0, all = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const unsigned hits = __ballot_sync(0xffffffffu, (unsigned)v[j] < (unsigned)width);
+        before += __popc(hits & lower);
+        all += __popc(hits);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if ((unsigned)v[j] < (unsigned)width) {
+          atomicAdd(&mine[v[j]], 1);
+          const int at = n + before++;
+          if (at < SORT_KEEP) kept[warp][at] = ((unsigned)v[j] << SORT_RUN_BITS) | (unsigned)(p + k * 128 + j - p0);
+        }
+      n += all;
+    }
   }
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) below_sum[warp] = below;
@@ -138,6 +206,7 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
   const int per = (width + SORT_THREADS - 1) / SORT_THREADS, k0 = threadIdx.x * per;
   int sum = 0;
   for (int k = k0; k < k0 + per && k < width; ++k)
+#pragma unroll
     for (int w = 0; w < SORT_WARPS; ++w) sum += count[w * a.width + k];
   int scan = sum;
 #pragma unroll
@@ -148,167 +217,258 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
   if (lane == 31) scan_sum[warp] = scan;
   __syncthreads();
   int at = scan - sum;
+#pragma unroll
   for (int w = 0; w < SORT_WARPS; ++w) at += below_sum[w] + (w < warp ? scan_sum[w] : 0);
   for (int k = k0; k < k0 + per && k < width; ++k) {
     a.first[lo + k] = at;
+    int c[SORT_WARPS];
+#pragma unroll
+    for (int w = 0; w < SORT_WARPS; ++w) c[w] = count[w * a.width + k];
+#pragma unroll
     for (int w = 0; w < SORT_WARPS; ++w) {
-      const int c = count[w * a.width + k];
       count[w * a.width + k] = at;
-      at += c;
+      at += c[w];
     }
   }
-  if (k0 < width && k0 + per >= width && lo + width == a.V) a.first[a.V] = at;
+  if (k0 < width && k0 + per >= width) {
+    count_end = at;
+    if (lo + (long long)width == a.V) a.first[a.V] = at;
+  }
   __syncthreads();
+  if (lo + (long long)width == a.V)              // positions without a token
+    for (int i = count_end + threadIdx.x; i < a.M; i += SORT_THREADS) a.sorted[i] = make_int2(0, -1);
 
-  for (int p = p0; p < p1; p += 32) {
-    const int t = p + lane < p1 ? a.tokens[p + lane] : -1;
-    const bool hit = t >= lo && t - lo < width;
-    const unsigned hits = __ballot_sync(0xffffffffu, hit);
-    if (hits == 0) continue;
-    if (hit) {
-      const unsigned equal = __match_any_sync(hits, t);
-      const int rank = __popc(equal & ((1u << lane) - 1));
-      const int to = mine[t - lo] + rank;
+  // 32 of the warp's tokens in order: equal ones by lane
+  const auto place = [&](bool there, int key, int position) {
+    const unsigned hits = __ballot_sync(0xffffffffu, there);
+    if (there) {
+      const unsigned equal = __match_any_sync(hits, key);
+      const int rank = __popc(equal & lower), to = mine[key] + rank;
       __syncwarp(hits);
-      if (rank == 0) mine[t - lo] = to + __popc(equal);
-      a.order[to] = p + lane;
-      a.key[to] = t;
+      if (rank == 0) mine[key] = to + __popc(equal);
+      a.sorted[to] = make_int2(position, lo + key);
     }
     __syncwarp();
+  };
+  if (n <= SORT_KEEP && run <= 1 << SORT_RUN_BITS) {
+    for (int i = lane; i - lane < n; i += 32) {
+      const unsigned x = i < n ? kept[warp][i] : 0u;
+      place(i < n, (int)(x >> SORT_RUN_BITS), p0 + (int)(x & ((1u << SORT_RUN_BITS) - 1)));
+    }
+  } else {
+    for (int p = p0 + lane; p - lane < p1; p += 32 * SORT_AHEAD) {
+      int t[SORT_AHEAD];
+#pragma unroll
+      for (int k = 0; k < SORT_AHEAD; ++k) t[k] = p + k * 32 < p1 ? a.tokens[p + k * 32] - lo : -1;
+#pragma unroll
+      for (int k = 0; k < SORT_AHEAD; ++k)
+        if (__any_sync(0xffffffffu, (unsigned)t[k] < (unsigned)width)) place((unsigned)t[k] < (unsigned)width, t[k], p + k * 32);
+    }
   }
 }
 
 struct GradArgs {
   const void* g;
   void* dW;
-  const int* order;
-  const int* key;
+  const int2* sorted;
   const int* first;
-  float* part;                                   // [windows][2][per_row * VEC]
+  float* part;                                   // [windows][2][per_row * N]
   int* arrived;                                  // [windows][per_row]
-  long long ld_g, ld_w, V;
+  long long ld_g, ld_w, M;
   long long windows;
-  unsigned per_row;                              // groups of eight (or single values) a row
+  unsigned per_row;                              // groups of N values a row
   int window;                                    // sorted positions a thread takes
-  int accumulate;
-  unsigned sum_blocks;                           // blocks that sum; the others fill rows with zeros
   float scale;
 };
 
-template <typename T, int VEC>
-struct Piece {                                   // VEC consecutive values of a row
-  Vec8<T> v;
-  __device__ __forceinline__ void load(const T* p) { v.load_once(p); }
-  __device__ __forceinline__ void add(float (&x)[8]) const {
-    float y[8];
-    v.get(y);
+template <bool ADD, typename T, int N>
+__device__ __forceinline__ void write_row(T* p, const float (&sum)[N], float scale) {
+  float x[N];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] += y[j];
+  for (int j = 0; j < N; ++j) x[j] = sum[j] * scale;
+  if (ADD) {
+    VecN<T, N> old;
+    old.load(p);
+    old.add_to(x);
   }
-};
-template <typename T>
-struct Piece<T, 1> {
-  T v;
-  __device__ __forceinline__ void load(const T* p) { v = *p; }
-  __device__ __forceinline__ void add(float (&x)[1]) const { x[0] += to_float(v); }
-};
-template <typename T, int VEC>
-__device__ __forceinline__ void write_row(T* p, const float (&sum)[VEC], float scale, bool accumulate) {
-  float x[VEC];
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) x[j] = sum[j] * scale;
-  if constexpr (VEC == 8) {
-    if (accumulate) {
-      Vec8<T> old;
-      old.load(p);
-      float y[8];
-      old.get(y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] += y[j];
-    }
-    Vec8<T>::store(p, x);
-  } else {
-    if (accumulate) x[0] += to_float(*p);
-    *p = from_float<T>(x[0]);
-  }
+  VecN<T, N>::store(p, x);
 }
 
 constexpr int GRAD_THREADS = 256;
-constexpr int GRAD_ZERO_VECS = 8;
-constexpr int GRAD_AHEAD = 8;                    // rows that a thread loads before it adds the first
+constexpr int GRAD_AHEAD = 8;                    // rows that a thread loads before it adds the first; windows are a multiple of it
+constexpr int GRAD_MOST = 64;                    // sorted positions of a window, at most
+constexpr int GRAD_STAGED = 2048;                // sorted positions of a block's windows, at most
+constexpr int GRAD_PER_SM = 2;                   // blocks that run on an SM at a time: three spill registers (72 -> 74 us)
+constexpr int GRAD_WAVE = 148 * GRAD_PER_SM * GRAD_THREADS;
 
-template <typename G, typename T, int VEC>
-__global__ void __launch_bounds__(GRAD_THREADS) k_embed_grad(const GradArgs a) {
-  if (blockIdx.x >= a.sum_blocks) {              // rows of tokens that do not occur
-    const long long total = a.V * a.per_row;
-    long long g = (long long)(blockIdx.x - a.sum_blocks) * (GRAD_THREADS * GRAD_ZERO_VECS) + threadIdx.x;
-    const float none[VEC] = {};
-#pragma unroll
-    for (int k = 0; k < GRAD_ZERO_VECS; ++k, g += GRAD_THREADS) {
-      if (g >= total) break;
-      const long long v = g / a.per_row;
-      if (a.first[v] == a.first[v + 1])
-        write_row<T, VEC>((T*)a.dW + v * a.ld_w + (g - v * a.per_row) * VEC, none, 0.f, false);
-    }
-    return;
+// N: as many values as 16 bytes of g hold where all is aligned for that, else 2 or 1.
+template <bool ADD, typename G, typename T, int N>
+__global__ void __launch_bounds__(GRAD_THREADS, GRAD_PER_SM) k_embed_grad(const GradArgs a) {
+  __shared__ int2 staged[GRAD_STAGED + 2];       // the block's sorted positions, with one before and one behind
+  const long long id0 = (long long)blockIdx.x * GRAD_THREADS, block_w = id0 / a.per_row;
+  const unsigned id = (unsigned)(id0 - block_w * a.per_row) + threadIdx.x, nth = id / a.per_row, c = id - nth * a.per_row;
+  const long long from = block_w * a.window, w = block_w + nth;
+  const int count = (int)min((long long)((unsigned)(id0 - block_w * a.per_row) + GRAD_THREADS - 1) / a.per_row + 1, a.windows - block_w) * a.window;
+  for (int i = threadIdx.x; i < count + 2; i += GRAD_THREADS) {
+    const long long at = from + i - 1;
+    staged[i] = at >= 0 && at < a.M ? a.sorted[at] : make_int2(0, -1);
   }
-  const long long id = (long long)blockIdx.x * GRAD_THREADS + threadIdx.x;
-  const long long w = id / a.per_row;
-  const unsigned c = (unsigned)(id - w * a.per_row);
-  const int n = a.first[a.V];                    // positions with a token
-  const long long s0 = w * a.window;
-  if (s0 >= n) return;
-  const int s1 = (int)min(s0 + a.window, (long long)n);
-  const G* g = (const G*)a.g + (long long)c * VEC;
+  __syncthreads();
+  if (w >= a.windows) return;
+  const int2* mine = staged + 1 + nth * a.window;
+  const int v0 = mine[0].y;                      // -1: nothing but positions without a token from here on
+  if (v0 < 0) return;
+  const G* g = (const G*)a.g + (long long)c * N;
+  T* dW = (T*)a.dW + (long long)c * N;
+  // a token whose positions pass an end of the window leaves a part of its sum; what the end of its sum will need is
+  // loaded ahead
+  const int last = mine[a.window - 1].y;
+  const bool head = v0 == mine[-1].y, tail = last >= 0 && last == mine[a.window].y;
+  int2 head_range, tail_range;
+  if (head) head_range = make_int2(a.first[v0], a.first[v0 + 1]);
+  if (tail) tail_range = make_int2(a.first[last], a.first[last + 1]);
 
-  // the sum of a token's positions [begin, end) of this window: final, or a part of the token's sum
-  const auto flush = [&](int v, const float (&sum)[VEC]) {
-    const int from = a.first[v], to = a.first[v + 1];
-    T* row = (T*)a.dW + v * a.ld_w + (long long)c * VEC;
-    if (from >= s0 && to <= s1) {
-      write_row<T, VEC>(row, sum, a.scale, a.accumulate);
-      return;
-    }
-    const long long width = (long long)a.per_row * VEC, w0 = from / a.window, w1 = (to - 1) / a.window;
-    float* p = a.part + (w * 2 + (from >= s0 ? 1 : 0)) * width + (long long)c * VEC;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) __stcg(p + j, sum[j]);
-    __threadfence();
-    if (atomicAdd(&a.arrived[w0 * a.per_row + c], 1) != (int)(w1 - w0)) return;
-    __threadfence();
-    float all[VEC] = {};
-    for (long long u = w0; u <= w1; ++u) {       // in order, whoever comes last
-      const float* q = a.part + (u * 2 + (u == w0 ? 1 : 0)) * width + (long long)c * VEC;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) all[j] += __ldcg(q + j);
-    }
-    write_row<T, VEC>(row, all, a.scale, a.accumulate);
-  };
-
-  float sum[VEC] = {};
-  int v = a.key[s0];
-  for (int s = (int)s0; s < s1; s += GRAD_AHEAD) {
-    Piece<G, VEC> x[GRAD_AHEAD];
-    int key[GRAD_AHEAD];
+  float sum[N] = {}, head_sum[N];
+  int v = v0;
+  bool aside = head;                             // the sum that runs goes to head_sum
+  for (int s = 0; s < a.window; s += GRAD_AHEAD) {
+    VecN<G, N> x[GRAD_AHEAD];
 #pragma unroll
     for (int k = 0; k < GRAD_AHEAD; ++k)
-      if (s + k < s1) {
-        key[k] = a.key[s + k];
-        x[k].load(g + a.order[s + k] * a.ld_g);
-      }
+      if (mine[s + k].y >= 0) x[k].load(g + mine[s + k].x * a.ld_g);
 #pragma unroll
-    for (int k = 0; k < GRAD_AHEAD; ++k)
-      if (s + k < s1) {
-        if (key[k] != v) {
-          flush(v, sum);
-          v = key[k];
+    for (int k = 0; k < GRAD_AHEAD; ++k) {
+      const int key = mine[s + k].y;
+      if (key < 0) break;
+      if (key != v) {
+        if (aside) {
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
+          for (int j = 0; j < N; ++j) head_sum[j] = sum[j];
+        } else {
+          write_row<ADD>(dW + v * a.ld_w, sum, a.scale);
         }
-        x[k].add(sum);
+        aside = false;
+        v = key;
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] = 0.f;
       }
+      x[k].add_to(sum);
+    }
   }
-  flush(v, sum);
+  if (!aside && !tail) write_row<ADD>(dW + v * a.ld_w, sum, a.scale);
+  if (!head && !tail) return;
+
+  // parts: those of a window's first token at 0, those of a token that begins in it at `width`
+  const long long width = (long long)a.per_row * N;
+  float* part = a.part + w * 2 * width + (long long)c * N;
+  if (head) {
+    if (aside) VecN<float, N>::store(part, sum); else VecN<float, N>::store(part, head_sum);
+  }
+  if (tail && !aside) VecN<float, N>::store(part + width, sum);
+  // whoever comes last adds the parts of a token up, in the order of the windows
+  __threadfence();
+#pragma unroll 1
+  for (int e = 0; e < 2; ++e) {
+    if (e == 0 ? !head : !tail || aside) continue;
+    const int2 range = e == 0 ? head_range : tail_range;
+    const long long w0 = range.x / a.window, w1 = (range.y - 1) / a.window;
+    if (atomicAdd(&a.arrived[w0 * a.per_row + c], 1) != (int)(w1 - w0)) continue;
+    __threadfence();
+    float all[N] = {};
+    const float* p = a.part + (w0 * 2 + 1) * width + (long long)c * N;
+    for (long long u = w0; u <= w1; u += GRAD_AHEAD) {
+      VecN<float, N> q[GRAD_AHEAD];
+#pragma unroll
+      for (int k = 0; k < GRAD_AHEAD; ++k)
+        if (u + k <= w1) q[k].load_l2(u + k == w0 ? p : p + ((u + k - w0) * 2 - 1) * width);
+#pragma unroll
+      for (int k = 0; k < GRAD_AHEAD; ++k)
+        if (u + k <= w1) q[k].add_to(all);
+    }
+    write_row<ADD>(dW + (e == 0 ? v0 : last) * a.ld_w, all, a.scale);
+  }
+}
+
+// Up to GRAD_FEW tokens.  Block (x, y) takes every gridDim.x-th piece of rows from piece x on, and columns y * GRAD_SLICE ..
+constexpr int GRAD_FEW = GRAD_THREADS;           // a token a thread
+constexpr int GRAD_SLICE = 1024;                 // columns of a block
+
+struct FewArgs {
+  const int* tokens;
+  const void* g;
+  void* dW;
+  long long ld_g, ld_w, V, D;
+  int M;
+  int accumulate;
+  float scale;
+  ZeroArgs zero;                                 // the pieces (and, if the block has all columns, where the zeros go)
+};
+
+template <typename G, typename T, int N>
+__global__ void __launch_bounds__(GRAD_THREADS) k_embed_grad_few(const FewArgs a) {
+  __shared__ int found[GRAD_FEW], row_of[GRAD_FEW + 1], position[GRAD_FEW], begin[GRAD_FEW];
+  __shared__ int warp_count[GRAD_THREADS / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long c0 = (long long)blockIdx.y * GRAD_SLICE;
+  const int cols = (int)min((long long)GRAD_SLICE, a.D - c0);
+  const int token = threadIdx.x < a.M ? a.tokens[threadIdx.x] : -1;
+  if (!a.accumulate) {                           // before any token is known: the stores go out while the first load is on its way
+    ZeroArgs z = a.zero;
+    z.p += c0 * sizeof(T);
+    if (gridDim.y > 1) z.width = cols * (long long)sizeof(T);
+    for (long long piece = blockIdx.x; piece < z.pieces; piece += gridDim.x) zero_piece<GRAD_THREADS>(z, piece);
+  }
+  const bool hit = token >= 0 && token < a.V && (token / a.zero.piece) % gridDim.x == blockIdx.x;
+  // the block's tokens, in order of their positions
+  const auto compact = [&](bool yes, int& n) {   // the place of a thread that says yes, and how many do
+    const unsigned all = __ballot_sync(0xffffffffu, yes);
+    __syncthreads();
+    if (lane == 0) warp_count[warp] = __popc(all);
+    __syncthreads();
+    int at = __popc(all & ((1u << lane) - 1));
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < GRAD_THREADS / 32; ++w) {
+      if (w < warp) at += warp_count[w];
+      n += warp_count[w];
+    }
+    return at;
+  };
+  int n, rows;
+  const int at = compact(hit, n);
+  if (n == 0) return;
+  if (hit) found[at] = token;
+  __syncthreads();
+  if (hit) {                                     // by row, then position
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += found[j] < token || (found[j] == token && j < at);
+    row_of[rank] = token;
+    position[rank] = threadIdx.x;
+  }
+  if (threadIdx.x == 0) row_of[n] = -1;
+  __syncthreads();
+  const bool first = (int)threadIdx.x < n && (threadIdx.x == 0 || row_of[threadIdx.x - 1] != row_of[threadIdx.x]);
+  const int nth = compact(first, rows);
+  if (first) begin[nth] = threadIdx.x;
+  __syncthreads();                               // the zeros of the block's rows come before their sums, too
+
+  const int per_row = cols / N;
+  for (int i = threadIdx.x; i < rows * per_row; i += GRAD_THREADS) {
+    const int r = i / per_row, c = (i - r * per_row) * N, s = begin[r], row = row_of[s];
+    const int end = r + 1 < rows ? begin[r + 1] : n;
+    float sum[N] = {};
+    for (int e = s; e < end; e += GRAD_AHEAD) {
+      VecN<G, N> x[GRAD_AHEAD];
+#pragma unroll
+      for (int k = 0; k < GRAD_AHEAD; ++k)
+        if (e + k < end) x[k].load((const G*)a.g + position[e + k] * a.ld_g + c0 + c);
+#pragma unroll
+      for (int k = 0; k < GRAD_AHEAD; ++k)
+        if (e + k < end) x[k].add_to(sum);
+    }
+    T* to = (T*)a.dW + row * a.ld_w + c0 + c;
+    if (a.accumulate) write_row<true>(to, sum, a.scale); else write_row<false>(to, sum, a.scale);
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -320,20 +480,20 @@ size_t up(size_t b) { return (b + EMBED_ALIGN - 1) / EMBED_ALIGN * EMBED_ALIGN; 
 struct GradPlan {
   int window;
   long long windows;
-  size_t order, key, first, part, arrived, total;
+  size_t sorted, first, part, arrived, total;
 };
-// The window: enough threads to fill the GPU, and no more partial sums than that takes.
+// The window: as many threads as run at a time, and no more partial sums than that takes.
 GradPlan grad_plan(const pctc_embed_t* p) {
   GradPlan g;
-  const double threads = (double)p->M * ((p->D + 7) / 8);
-  int window = 8;
-  while (window < 64 && threads / window > 148.0 * 2048) window *= 2;
+  const long long groups = (p->D + 7) / 8, rows = (p->M * groups + GRAD_WAVE - 1) / GRAD_WAVE;
+  // a block's windows fit its staging, with as few as one group a row
+  const long long fit = GRAD_STAGED / (GRAD_THREADS / groups + 2) / 8 * 8, most = fit < 8 ? 8 : fit < GRAD_MOST ? fit : GRAD_MOST;
+  const int window = (int)(rows < 8 ? 8 : rows > most ? most : (rows + 7) / 8 * 8);
   g.window = window;
   g.windows = (p->M + window - 1) / window;
   size_t o = 0;
   const auto take = [&](size_t bytes) { const size_t r = o; o += up(bytes); return r; };
-  g.order = take((size_t)p->M * 4);
-  g.key = take((size_t)p->M * 4);
+  g.sorted = take((size_t)p->M * 8);
   g.first = take(((size_t)p->V + 1) * 4);
   g.arrived = take((size_t)g.windows * p->D * 4);       // a counter a group of eight, or a value
   g.part = take((size_t)g.windows * 2 * p->D * 4);
@@ -368,15 +528,52 @@ cudaError_t embed_launch(const EmbedArgs& a, int out, bool vec, cudaStream_t str
   return out == PCTC_BF16 ? embed_launch<W, __nv_bfloat16>(a, vec, stream) : embed_launch<W, float>(a, vec, stream);
 }
 
+ZeroArgs zero_args(void* dW, long long V, long long D, long long ld, size_t size, long long least_pieces) {
+  ZeroArgs z;
+  z.p = (char*)dW;
+  z.rows = V;
+  z.ld = ld * (long long)size;
+  z.width = D * (long long)size;
+  const long long fit = ZERO_BYTES / z.width, spread = V / least_pieces;   // rows: that fill a piece, that leave enough pieces
+  z.piece = fit < spread ? fit : spread;
+  if (z.piece < 1) z.piece = 1;
+  z.pieces = (V + z.piece - 1) / z.piece;
+  return z;
+}
+
+// The widest groups of g's values that every row of both matrices is cut into evenly and aligned for.
+int group_of(const void* g, long long ld_g, size_t gs, const void* dW, long long ld_w, size_t ws, long long D) {
+  const auto fits = [&](long long n) {
+    const size_t gb = n * gs < 16 ? n * gs : 16, wb = n * ws < 16 ? n * ws : 16;
+    return D % n == 0 && (size_t)g % gb == 0 && (size_t)dW % wb == 0 && ld_g * gs % gb == 0 && ld_w * ws % wb == 0;
+  };
+  return fits(16 / (long long)gs) ? (int)(16 / gs) : fits(2) ? 2 : 1;
+}
+
+template <typename G, typename T, int N>
+cudaError_t grad_launch(GradArgs a, long long D, bool add, cudaStream_t stream) {
+  a.per_row = (unsigned)(D / N);
+  const long long blocks = (a.windows * a.per_row + GRAD_THREADS - 1) / GRAD_THREADS;
+  if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
+  if (add) k_embed_grad<true, G, T, N><<<(unsigned)blocks, GRAD_THREADS, 0, stream>>>(a);
+  else k_embed_grad<false, G, T, N><<<(unsigned)blocks, GRAD_THREADS, 0, stream>>>(a);
+  return cudaGetLastError();
+}
 template <typename G, typename T>
-cudaError_t grad_launch(GradArgs a, long long D, bool vec, cudaStream_t stream) {
-  a.per_row = (unsigned)(vec ? D / 8 : D);
-  const long long sums = (a.windows * a.per_row + GRAD_THREADS - 1) / GRAD_THREADS;
-  const long long zeros = a.accumulate ? 0 : (a.V * a.per_row + GRAD_THREADS * GRAD_ZERO_VECS - 1) / (GRAD_THREADS * GRAD_ZERO_VECS);
-  if (sums + zeros > 0x7fffffffLL) return cudaErrorInvalidValue;
-  a.sum_blocks = (unsigned)sums;
-  if (vec) k_embed_grad<G, T, 8><<<(unsigned)(sums + zeros), GRAD_THREADS, 0, stream>>>(a);
-  else k_embed_grad<G, T, 1><<<(unsigned)(sums + zeros), GRAD_THREADS, 0, stream>>>(a);
+cudaError_t grad_launch(const GradArgs& a, long long D, int group, bool add, cudaStream_t stream) {
+  return group == 1 ? grad_launch<G, T, 1>(a, D, add, stream) : group == 2 ? grad_launch<G, T, 2>(a, D, add, stream)
+                    : grad_launch<G, T, 16 / (int)sizeof(G)>(a, D, add, stream);
+}
+
+constexpr long long FEW_BLOCKS = 148 * 8;
+template <typename G, typename T>
+cudaError_t few_launch(FewArgs a, int group, cudaStream_t stream) {
+  const long long slices = (a.D + GRAD_SLICE - 1) / GRAD_SLICE, most = (FEW_BLOCKS + slices - 1) / slices;
+  a.zero = zero_args(a.dW, a.V, a.D, a.ld_w, sizeof(T), most);
+  const dim3 grid((unsigned)(a.zero.pieces < most ? a.zero.pieces : most), (unsigned)slices);
+  if (group == 1) k_embed_grad_few<G, T, 1><<<grid, GRAD_THREADS, 0, stream>>>(a);
+  else if (group == 2) k_embed_grad_few<G, T, 2><<<grid, GRAD_THREADS, 0, stream>>>(a);
+  else k_embed_grad_few<G, T, 16 / (int)sizeof(G)><<<grid, GRAD_THREADS, 0, stream>>>(a);
   return cudaGetLastError();
 }
 
@@ -448,46 +645,56 @@ pctc_status_t pctc_embed_grad(const pctc_embed_t* p, const int32_t* tokens, cons
 
   cudaStream_t stream = (cudaStream_t)stream_v;
   char* w = (char*)workspace;
-  const bool vec = p->D % 8 == 0 && wide(dW, p->ld_w, ws) && wide(grad, p->ld_x, xs);
+  const int group = group_of(grad, p->ld_x, xs, dW, p->ld_w, ws, p->D);
+  cudaError_t e;
+  if (p->M <= GRAD_FEW) {
+    const FewArgs a{tokens, grad, dW, p->ld_x, p->ld_w, p->V, p->D, (int)p->M, p->accumulate, p->scale, {}};
+    if (p->dtype_x == PCTC_BF16)
+      e = p->dtype_w == PCTC_BF16 ? few_launch<__nv_bfloat16, __nv_bfloat16>(a, group, stream) : few_launch<__nv_bfloat16, float>(a, group, stream);
+    else
+      e = p->dtype_w == PCTC_BF16 ? few_launch<float, __nv_bfloat16>(a, group, stream) : few_launch<float, float>(a, group, stream);
+    return status_of(e);
+  }
   const long long width = (p->V + SORT_BUCKETS - 1) / SORT_BUCKETS;
   SortArgs s = {};
   s.tokens = tokens;
   s.M = (int)p->M;
   s.V = p->V;
   s.width = (int)(width < SORT_MAX_WIDTH ? width : SORT_MAX_WIDTH);
-  s.order = (int*)(w + g.order);
-  s.key = (int*)(w + g.key);
+  s.sorted = (int2*)(w + g.sorted);
   s.first = (int*)(w + g.first);
   s.clear = (int*)(w + g.arrived);
-  s.n_clear = g.windows * (vec ? p->D / 8 : p->D);
+  s.n_clear = g.windows * (p->D / group);
   const int smem = SORT_WARPS * s.width * 4;
-  cudaError_t e = cudaFuncSetAttribute(k_sort_tokens, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_WARPS * SORT_MAX_WIDTH * 4);
+  e = cudaFuncSetAttribute(k_sort_tokens, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_WARPS * SORT_MAX_WIDTH * 4);
   if (e != cudaSuccess) return PCTC_ERR_CUDA;
-  k_sort_tokens<<<(unsigned)((p->V + s.width - 1) / s.width), SORT_THREADS, smem, stream>>>(s);
+  s.buckets = (unsigned)((p->V + s.width - 1) / s.width);
+  if (!p->accumulate) s.zero = zero_args(dW, p->V, p->D, p->ld_w, ws, 1);
+  const long long blocks = s.buckets + s.zero.pieces;
+  if (blocks > 0x7fffffffLL) return PCTC_ERR_UNSUPPORTED;
+  k_sort_tokens<<<(unsigned)blocks, SORT_THREADS, smem, stream>>>(s);
   e = cudaGetLastError();
   if (e != cudaSuccess) return PCTC_ERR_CUDA;
 
   GradArgs a = {};
   a.g = grad;
   a.dW = dW;
-  a.order = s.order;
-  a.key = s.key;
+  a.sorted = s.sorted;
   a.first = s.first;
   a.part = (float*)(w + g.part);
   a.arrived = s.clear;
   a.ld_g = p->ld_x;
   a.ld_w = p->ld_w;
-  a.V = p->V;
+  a.M = p->M;
   a.windows = g.windows;
   a.window = g.window;
-  a.accumulate = p->accumulate;
   a.scale = p->scale;
   if (p->dtype_x == PCTC_BF16)
-    e = p->dtype_w == PCTC_BF16 ? grad_launch<__nv_bfloat16, __nv_bfloat16>(a, p->D, vec, stream)
-                                : grad_launch<__nv_bfloat16, float>(a, p->D, vec, stream);
+    e = p->dtype_w == PCTC_BF16 ? grad_launch<__nv_bfloat16, __nv_bfloat16>(a, p->D, group, p->accumulate != 0, stream)
+                                : grad_launch<__nv_bfloat16, float>(a, p->D, group, p->accumulate != 0, stream);
   else
-    e = p->dtype_w == PCTC_BF16 ? grad_launch<float, __nv_bfloat16>(a, p->D, vec, stream)
-                                : grad_launch<float, float>(a, p->D, vec, stream);
+    e = p->dtype_w == PCTC_BF16 ? grad_launch<float, __nv_bfloat16>(a, p->D, group, p->accumulate != 0, stream)
+                                : grad_launch<float, float>(a, p->D, group, p->accumulate != 0, stream);
   return status_of(e);
 }
 

@@ -1,5 +1,5 @@
-// Eight consecutive values of a row, moved 16 bytes at a time (8 at a time for 8-bit values), and the conversions
-// between storage types and fp32.
+// Consecutive values of a row: eight, moved 16 bytes at a time (8 at a time for 8-bit values), or N in one or two accesses;
+// and the conversions between storage types and fp32.
 #pragma once
 
 #include "pctc_internal.h"
@@ -70,6 +70,79 @@ struct Vec8<signed char> {
     const unsigned u[2] = {w.x, w.y};
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)(signed char)(u[i >> 2] >> (8 * (i & 3)));
+  }
+};
+
+// N values, N * sizeof(T) bytes aligned (16 where that is more): fp32 N = 1, 2, 4, 8, bf16 N = 1, 2, 4, 8.
+template <typename T, int N>
+struct VecN {
+  static constexpr int BYTES = N * (int)sizeof(T), WORDS = BYTES < 4 ? 1 : BYTES / 4;
+  unsigned u[WORDS];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (BYTES >= 16) {
+#pragma unroll
+      for (int i = 0; i < BYTES / 16; ++i) {
+        const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+        u[4 * i] = v.x; u[4 * i + 1] = v.y; u[4 * i + 2] = v.z; u[4 * i + 3] = v.w;
+      }
+    } else if constexpr (BYTES == 8) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      u[0] = v.x; u[1] = v.y;
+    } else if constexpr (BYTES == 4) {
+      u[0] = *reinterpret_cast<const unsigned*>(p);
+    } else {
+      u[0] = *reinterpret_cast<const unsigned short*>(p);
+    }
+  }
+  // what another SM has written during this kernel: not from this SM's cache
+  __device__ __forceinline__ void load_l2(const T* p) {
+    if constexpr (BYTES >= 16) {
+#pragma unroll
+      for (int i = 0; i < BYTES / 16; ++i) {
+        const uint4 v = __ldcg(reinterpret_cast<const uint4*>(p) + i);
+        u[4 * i] = v.x; u[4 * i + 1] = v.y; u[4 * i + 2] = v.z; u[4 * i + 3] = v.w;
+      }
+    } else if constexpr (BYTES == 8) {
+      const uint2 v = __ldcg(reinterpret_cast<const uint2*>(p));
+      u[0] = v.x; u[1] = v.y;
+    } else if constexpr (BYTES == 4) {
+      u[0] = __ldcg(reinterpret_cast<const unsigned*>(p));
+    } else {
+      u[0] = __ldcg(reinterpret_cast<const unsigned short*>(p));
+    }
+  }
+  __device__ __forceinline__ float value(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(u[i]);
+    else return __uint_as_float((i & 1) ? u[i >> 1] & 0xffff0000u : u[i >> 1] << 16);
+  }
+  __device__ __forceinline__ void add_to(float (&x)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += value(i);
+  }
+  static __device__ __forceinline__ void store(T* p, const float (&x)[N]) {
+    unsigned w[WORDS];
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = __float_as_uint(x[i]);
+    } else if constexpr (N == 1) {
+      *p = from_float<T>(x[0]);
+      return;
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        w[i] = *reinterpret_cast<const unsigned*>(&b);
+      }
+    }
+    if constexpr (BYTES >= 16) {
+#pragma unroll
+      for (int i = 0; i < BYTES / 16; ++i)
+        reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    } else if constexpr (BYTES == 8) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    } else {
+      *reinterpret_cast<unsigned*>(p) = w[0];
+    }
   }
 };
 
