@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
   extern __shared__ int count[];                 // [SORT_WARPS][width]: counts, then where each warp's next one goes
   __shared__ unsigned kept[SORT_WARPS][SORT_KEEP];
   __shared__ int below_sum[SORT_WARPS], scan_sum[SORT_WARPS], count_end;
+  launch_next();
   if (blockIdx.x >= a.buckets) {
     zero_piece<SORT_THREADS>(a.zero, blockIdx.x - a.buckets);
     return;
@@ -303,12 +304,13 @@ constexpr int GRAD_WAVE = 148 * GRAD_PER_SM * GRAD_THREADS;
 
 // N: as many values as 16 bytes of g hold where all is aligned for that, else 2 or 1.
 template <bool ADD, typename G, typename T, int N>
-__global__ void __launch_bounds__(GRAD_THREADS, GRAD_PER_SM) k_embed_grad(const GradArgs a) {
+__global__ void __launch_bounds__(GRAD_THREADS, N >= 4 ? GRAD_PER_SM : 4) k_embed_grad(const GradArgs a) {
   __shared__ int2 staged[GRAD_STAGED + 2];       // the block's sorted positions, with one before and one behind
   const long long id0 = (long long)blockIdx.x * GRAD_THREADS, block_w = id0 / a.per_row;
   const unsigned id = (unsigned)(id0 - block_w * a.per_row) + threadIdx.x, nth = id / a.per_row, c = id - nth * a.per_row;
   const long long from = block_w * a.window, w = block_w + nth;
   const int count = (int)min((long long)((unsigned)(id0 - block_w * a.per_row) + GRAD_THREADS - 1) / a.per_row + 1, a.windows - block_w) * a.window;
+  wait_for_previous();
   for (int i = threadIdx.x; i < count + 2; i += GRAD_THREADS) {
     const long long at = from + i - 1;
     staged[i] = at >= 0 && at < a.M ? a.sorted[at] : make_int2(0, -1);
@@ -555,9 +557,7 @@ cudaError_t grad_launch(GradArgs a, long long D, bool add, cudaStream_t stream) 
   a.per_row = (unsigned)(D / N);
   const long long blocks = (a.windows * a.per_row + GRAD_THREADS - 1) / GRAD_THREADS;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
-  if (add) k_embed_grad<true, G, T, N><<<(unsigned)blocks, GRAD_THREADS, 0, stream>>>(a);
-  else k_embed_grad<false, G, T, N><<<(unsigned)blocks, GRAD_THREADS, 0, stream>>>(a);
-  return cudaGetLastError();
+  return launch_behind(add ? k_embed_grad<true, G, T, N> : k_embed_grad<false, G, T, N>, (unsigned)blocks, GRAD_THREADS, 0, stream, a);
 }
 template <typename G, typename T>
 cudaError_t grad_launch(const GradArgs& a, long long D, int group, bool add, cudaStream_t stream) {

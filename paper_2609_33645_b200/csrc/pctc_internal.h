@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace pctc {
 
@@ -73,6 +74,31 @@ struct Rows {
   }
 };
 constexpr long long MAX_ELEMENTS = 1LL << 40;   // of one array of the operators around the head
+
+// ---------------------------------------------------------------------------
+// Two launches of one call, the second set up while the first still runs: the first says launch_next() as soon as it
+// has begun, the second goes on behind wait_for_previous() when all of the first's writes are there, and touches
+// nothing of it (and nothing that it reads) before.
+// ---------------------------------------------------------------------------
+#ifdef __CUDACC__
+__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+#endif
+template <typename Args>
+cudaError_t launch_behind(void (*kernel)(Args), unsigned blocks, unsigned threads, size_t smem, cudaStream_t stream,
+                          const typename std::remove_const<Args>::type& args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args);
+}
 
 // ---------------------------------------------------------------------------
 // Contractions:  acc(i,j) = sum_k A(i,k) * B(j,k),  then an epilogue.

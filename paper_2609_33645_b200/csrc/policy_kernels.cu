@@ -7,14 +7,16 @@
 //
 // The weights need the counts before the first gradient can be written: where a mask or lengths are given,
 // k_policy_count goes over them first (a quarter of a byte and less for a byte that the second pass moves).  k_policy then
-// reads every value once.  Few values are done by one cluster in one launch (k_policy_small).  Sums are 64 bits, in a fixed
-// order.  Large calls are bound by HBM, small ones by the launch.
+// reads every value once.  Few values are done by one cluster in one launch (k_policy_small).  Differences are exact (two
+// fp32 numbers), sums 64 bits, in a fixed order.  Large calls are bound by the exponentials and the loads, about alike,
+// small ones by the launch.
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 
 #include <cooperative_groups.h>
 
 #include <cmath>
+#include <math_constants.h>
 
 namespace cg = cooperative_groups;
 
@@ -22,19 +24,30 @@ namespace pctc {
 namespace {
 
 constexpr int POLICY_THREADS = 256;
-constexpr int POLICY_EACH = 4;                   // values a thread
+constexpr int POLICY_EACH = 4;                   // values of a group
+constexpr long long POLICY_MANY = 148 * 4 * POLICY_THREADS * POLICY_EACH;   // more values than run at a time in groups of their
+                                                 // own take two groups a thread (1M values: 14.6 -> 13.3 us; 64,000: 7.2 -> 9.1)
 constexpr int POLICY_SMALL_THREADS = 512;
 constexpr int POLICY_CLUSTER = 8;
-constexpr long long POLICY_SMALL = 32768;        // up to so many values one cluster does all
-constexpr int POLICY_SHORT_ROW = 32;             // rows up to this length are counted by one thread each
+constexpr long long POLICY_SMALL = 16384;        // up to so many values one cluster does all (15,000 values: 6.1 us against 9.4)
+static_assert(POLICY_SMALL <= POLICY_CLUSTER * POLICY_SMALL_THREADS * POLICY_EACH, "one round");
+constexpr int POLICY_SHORT_ROW = 32;             // masks of rows up to this length are counted by a thread each,
+constexpr int POLICY_LONG_ROW = 2048;            // up to this one by a warp, longer ones by a block
+constexpr int POLICY_COUNT_BLOCKS = 148;         // blocks that count, at most
 
-struct Totals {
-  long long count;                               // counted tokens
-  long long rows;                                // rows that have one
+struct Totals {                                  // fewer than 2^31 values
+  int count;                                     // counted tokens
+  int rows;                                      // rows that have one
 };
 struct PolicyHead {                              // start of the workspace
-  Totals totals;
   unsigned ticket;
+  unsigned blocks;                               // that have counted
+  Totals totals[POLICY_COUNT_BLOCKS];            // of each of them
+};
+
+struct alignas(16) BlockSums {                   // the sums of a block's tokens
+  double loss, kl;
+  int count, clipped;
 };
 
 struct PolicyArgs {
@@ -49,10 +62,10 @@ struct PolicyArgs {
   int* count_out;
   PolicyHead* head;
   int* row_count;                                // [N], made where the weights need it and a mask is given
-  double* partial;                               // [blocks][3]
+  BlockSums* partial;                            // [blocks]
   long long N, T, total;
   long long ld_logp, ld_old, ld_ref, ld_adv, ld_mask, ld_grad;   // ld_adv 0: one advantage a row
-  double log_low, log_high;                      // where ratios are clipped
+  float2 log_low, log_high;                      // logarithms of where ratios are clipped, as a number and its rest
   float low, high, kl_weight, sign;
   int reduction;
   int counting;                                  // counts come from k_policy_count
@@ -62,81 +75,101 @@ __device__ __forceinline__ int length_of(const PolicyArgs& a, long long n) {
   return a.lengths ? (int)min((long long)max(a.lengths[n], 0), a.T) : (int)a.T;
 }
 
-// The sums of one token.
+// The sums of a thread's four tokens; beyond a thread they are 64 bits.
 struct TokenSums {
-  double loss = 0.0, kl = 0.0;
-  int clipped = 0;
+  float loss = 0.f, kl = 0.f;
+  int clipped = 0, count = 0;
 };
 
-// exp(d) - 1 - d and exp(d) - 1.  Near 0 the first by its series (d^2 (1/2 + d/6 + ... + d^6/40320): the next term is under
-// 1e-9 of the sum for |d| < 1/4), where the difference would cancel.
-__device__ __forceinline__ void kl_terms(double d, float& kl, float& e) {
-  const float hi = (float)d;
-  const float lo = isinf(hi) ? 0.f : (float)(d - (double)hi);
-  e = expm1f(hi);
-  if (!isinf(e)) e = fmaf(e + 1.f, lo, e);
-  if (fabsf(hi) < 0.25f) {
-    float s = fmaf(hi, 1.f / 40320.f, 1.f / 5040.f);
-    s = fmaf(hi, s, 1.f / 720.f);
-    s = fmaf(hi, s, 1.f / 120.f);
-    s = fmaf(hi, s, 1.f / 24.f);
-    s = fmaf(hi, s, 1.f / 6.f);
-    s = fmaf(hi, s, 0.5f);
-    kl = hi * hi * s;
+// a - b without a rounding: a number and its rest (Knuth's two-sum).  Where the difference is not finite the rest is 0.
+__device__ __forceinline__ float2 difference(float a, float b) {
+  const float s = __fsub_rn(a, b), back = __fsub_rn(s, a);
+  const float rest = __fsub_rn(__fsub_rn(a, __fsub_rn(s, back)), __fadd_rn(b, back));
+  return make_float2(s, fabsf(s) < CUDART_INF_F ? rest : 0.f);
+}
+__device__ __forceinline__ bool above(float2 a, float2 b) { return a.x > b.x || (a.x == b.x && a.y > b.y); }
+
+// exp(b - a) - 1 - (b - a) and exp(b - a) - 1.  For |d| < 1 the first by its series d^2 (1/2 + d/6 + ... + d^11 / 13!), where
+// the difference would cancel (the next term is under 1e-10 of the sum), and the second from it; the rounding of d itself
+// is one of 2^-24 there.
+__device__ __forceinline__ void kl_terms(float a, float b, float& kl, float& e) {
+  const float d = b - a;
+  if (fabsf(d) < 1.f) {
+    constexpr float c[] = {1.f / 6227020800.f, 1.f / 479001600.f, 1.f / 39916800.f, 1.f / 3628800.f, 1.f / 362880.f, 1.f / 40320.f,
+                           1.f / 5040.f, 1.f / 720.f, 1.f / 120.f, 1.f / 24.f, 1.f / 6.f, 1.f / 2.f};
+    float s = c[0];
+#pragma unroll
+    for (int j = 1; j < 12; ++j) s = fmaf(d, s, c[j]);
+    kl = d * d * s;
+    e = d + kl;
   } else {
-    kl = isinf(e) ? e : (e - hi) - lo;
+    const float2 f = difference(b, a);
+    e = expm1f(f.x);
+    if (!isinf(e)) e = fmaf(e + 1.f, f.y, e);
+    kl = isinf(e) ? e : (e - f.x) - f.y;
   }
 }
 
-// One counted token: adds to the sums and returns its gradient, both before the weight.
-__device__ __forceinline__ float policy_token(const PolicyArgs& a, float x, float x_old, float x_ref, float A, double w,
-                                              TokenSums& s) {
-  // differences in 64 bits: whether a ratio is clipped does not depend on their rounding
-  const double d = (double)a.sign * ((double)x - (double)x_old);
-  const float hi = (float)d;
-  const float lo = isinf(hi) ? 0.f : (float)(d - (double)hi);
-  const float r0 = expf(hi), r = isinf(r0) ? r0 : fmaf(r0, lo, r0);
-  const bool over = A > 0.f && d > a.log_high, under = A < 0.f && d < a.log_low, clipped = over || under;
+// One token: adds to the sums and returns its gradient before the weight.  Values come with the sign of log-probabilities;
+// what does not count comes as zeros with no advantage, and gives zeros.
+__device__ __forceinline__ float policy_token(const PolicyArgs& a, float x, float x_old, float x_ref, float A, float w, TokenSums& s) {
+  const float2 d = difference(x, x_old);         // exact: whether a ratio is clipped does not depend on a rounding
+  const float r0 = expf(d.x), r = isinf(r0) ? r0 : fmaf(r0, d.y, r0);
+  const bool over = A > 0.f && above(d, a.log_high), under = A < 0.f && above(a.log_low, d), clipped = over || under;
   const float used = over ? a.high : under ? a.low : r;
   const float gain = A == 0.f ? (r == r ? 0.f : r) : A * used;   // no 0 * inf where the ratio overflows
   float loss = -gain, g = clipped ? 0.f : -gain;
   if (a.ref) {
     float kl, e;
-    kl_terms((double)a.sign * ((double)x_ref - (double)x), kl, e);
+    kl_terms(x, x_ref, kl, e);
     loss = fmaf(a.kl_weight, kl, loss);
     g = fmaf(-a.kl_weight, e, g);
-    s.kl += (double)kl;
+    s.kl += kl;
   }
-  s.loss += w * (double)loss;
+  s.loss = fmaf(w, loss, s.loss);
   s.clipped += clipped ? 1 : 0;
   return g;
 }
 
-// The weight of the tokens of a row with `count` of them.
-__device__ __forceinline__ float weight_of(const PolicyArgs& a, const Totals& t, long long count) {
-  if (a.reduction == PCTC_POLICY_SUM) return 1.f;
-  if (a.reduction == PCTC_POLICY_TOKENS) return 1.f / (float)max(t.count, 1ll);
-  return 1.f / ((float)max(count, 1ll) * (float)max(t.rows, 1ll));
+// What all weights have in common, and the weight of the tokens of a row with `count` of them.
+__device__ __forceinline__ float weight_part(const PolicyArgs& a, const Totals& t) {
+  return a.reduction == PCTC_POLICY_SUM ? 1.f : a.reduction == PCTC_POLICY_TOKENS ? 1.f / (float)max(t.count, 1) : (float)max(t.rows, 1);
+}
+__device__ __forceinline__ float weight_of(const PolicyArgs& a, float part, int count) {
+  return a.reduction == PCTC_POLICY_SEQUENCES ? 1.f / ((float)max(count, 1) * part) : part;
 }
 
-// Counts the tokens of row n with `lanes` threads (1, or a warp).
-template <int LANES>
-__device__ __forceinline__ int count_row(const PolicyArgs& a, long long n) {
-  const int len = length_of(a, n);
-  if (!a.mask) return len;
-  const unsigned char* m = a.mask + n * a.ld_mask;
+// How many of bytes 0 .. n - 1 are not zero, of the `lanes` threads' shares.
+__device__ __forceinline__ int count_bytes(const unsigned char* m, int n, int lane, int lanes) {
   int c = 0;
-  for (int t = LANES == 1 ? 0 : (int)(threadIdx.x & 31); t < len; t += LANES) c += m[t] != 0;
-  return LANES == 1 ? c : __reduce_add_sync(0xffffffffu, c);
+  const int head = min((int)((16 - ((size_t)m & 15)) & 15), n), vecs = (n - head) / 16;
+  for (int t = lane; t < head; t += lanes) c += m[t] != 0;
+  const uint4* body = reinterpret_cast<const uint4*>(m + head);
+#pragma unroll 4
+  for (int i = lane; i < vecs; i += lanes) {
+    const uint4 v = body[i];
+    c += (__popc(__vcmpne4(v.x, 0u)) + __popc(__vcmpne4(v.y, 0u)) + __popc(__vcmpne4(v.z, 0u)) + __popc(__vcmpne4(v.w, 0u))) >> 3;
+  }
+  for (int t = head + vecs * 16 + lane; t < n; t += lanes) c += m[t] != 0;
+  return c;
 }
-// Rows first, first + step, ...: `worker` is one of `workers` threads (or warps).
-template <int LANES>
-__device__ __forceinline__ Totals count_rows(const PolicyArgs& a, long long worker, long long workers) {
+// Rows worker, worker + workers, ...: a worker is `lanes` threads (1, 32, or the block).
+template <int THREADS>
+__device__ __forceinline__ Totals count_rows(const PolicyArgs& a, int lanes, long long worker, long long workers) {
+  __shared__ int scratch[THREADS / 32];
   Totals t{0, 0};
-  const bool writes = LANES == 1 || (threadIdx.x & 31) == 0;
+  const int lane = threadIdx.x & (lanes - 1);
   for (long long n = worker; n < a.N; n += workers) {
-    const int c = count_row<LANES>(a, n);
-    if (!writes) continue;
+    int c = a.mask ? count_bytes(a.mask + n * a.ld_mask, length_of(a, n), lane, lanes) : lane == 0 ? length_of(a, n) : 0;
+    if (lanes > 1) c = __reduce_add_sync(0xffffffffu, c);
+    if (lanes > 32) {
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = c;
+      __syncthreads();
+      c = 0;
+      for (int i = 0; i < THREADS / 32; ++i) c += scratch[i];
+    }
+    if (lane != 0) continue;
     if (a.row_count) a.row_count[n] = c;
     t.count += c;
     t.rows += c > 0;
@@ -144,139 +177,236 @@ __device__ __forceinline__ Totals count_rows(const PolicyArgs& a, long long work
   return t;
 }
 
-template <int THREADS, typename V>
-__device__ __forceinline__ V block_sum(V v, V* scratch) {          // valid in thread 0; scratch [THREADS / 32]
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) v += __shfl_down_sync(0xffffffffu, v, d);
+__device__ __forceinline__ Totals warp_sum(Totals t) {
+  return Totals{__reduce_add_sync(0xffffffffu, t.count), __reduce_add_sync(0xffffffffu, t.rows)};
+}
+// Sums over a block, valid in thread 0.
+template <int THREADS>
+__device__ __forceinline__ Totals count_all(const PolicyArgs& a, int block, int blocks) {
+  __shared__ Totals scratch[THREADS / 32];
+  const int lanes = !a.mask || a.T <= POLICY_SHORT_ROW ? 1 : a.T <= POLICY_LONG_ROW ? 32 : THREADS, each = THREADS / lanes;
+  Totals t = warp_sum(count_rows<THREADS>(a, lanes, (long long)block * each + threadIdx.x / lanes, (long long)blocks * each));
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = t;
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+  if (threadIdx.x < 32) t = warp_sum(threadIdx.x < THREADS / 32 ? scratch[threadIdx.x] : Totals{0, 0});
+  return t;
+}
+// The sums of tokens of a block, valid in thread 0.
+template <int THREADS>
+__device__ __forceinline__ BlockSums block_sum(double loss, double kl, int count, int clipped) {
+  __shared__ BlockSums scratch[THREADS / 32];
+  const auto warp = [&](int from) {
+    for (int d = from; d > 0; d >>= 1) {
+      loss += __shfl_xor_sync(0xffffffffu, loss, d);
+      kl += __shfl_xor_sync(0xffffffffu, kl, d);
+    }
+    count = __reduce_add_sync(0xffffffffu, count);
+    clipped = __reduce_add_sync(0xffffffffu, clipped);
+  };
+  warp(16);
   __syncthreads();
-  V sum = 0;
-  if (threadIdx.x == 0)
-    for (int i = 0; i < THREADS / 32; ++i) sum += scratch[i];
-  return sum;
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = BlockSums{loss, kl, count, clipped};
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    const BlockSums s = threadIdx.x < THREADS / 32 ? scratch[threadIdx.x] : BlockSums{0.0, 0.0, 0, 0};
+    loss = s.loss; kl = s.kl; count = s.count; clipped = s.clipped;
+    warp(THREADS / 64);
+  }
+  return BlockSums{loss, kl, count, clipped};
 }
 
 __global__ void __launch_bounds__(POLICY_THREADS) k_policy_count(const PolicyArgs a) {
-  __shared__ long long scratch[POLICY_THREADS / 32];
-  const long long thread = (long long)blockIdx.x * POLICY_THREADS + threadIdx.x, threads = (long long)gridDim.x * POLICY_THREADS;
-  const Totals t = a.T <= POLICY_SHORT_ROW ? count_rows<1>(a, thread, threads) : count_rows<32>(a, thread >> 5, threads >> 5);
-  const long long count = block_sum<POLICY_THREADS>(t.count, scratch), rows = block_sum<POLICY_THREADS>(t.rows, scratch);
-  if (threadIdx.x == 0) {                        // whole numbers: their order does not matter
-    atomicAdd((unsigned long long*)&a.head->totals.count, (unsigned long long)count);
-    atomicAdd((unsigned long long*)&a.head->totals.rows, (unsigned long long)rows);
+  launch_next();
+  if (a.counting) {
+    const Totals t = count_all<POLICY_THREADS>(a, blockIdx.x, gridDim.x);
+    if (threadIdx.x == 0) a.head->totals[blockIdx.x] = t;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    a.head->ticket = 0;
+    a.head->blocks = gridDim.x;
   }
 }
 
-// Values first, first + step, ... of the flattened array, `each` of them.
-template <int EACH>
-__device__ __forceinline__ void policy_values(const PolicyArgs& a, const Totals& t, long long first, long long step, TokenSums& s) {
-  float x[EACH], o[EACH], q[EACH], A[EACH];
-  bool counted[EACH], inside[EACH];
-  long long rows[EACH];
-  int cols[EACH];
+// Four values of a thread: those from `first` on, in one row and 16-byte aligned (VEC), or first, first + step, ...
+template <bool VEC>
+struct Values {
+  static constexpr int ROWS = VEC ? 1 : POLICY_EACH;
+  float x[POLICY_EACH], o[POLICY_EACH], q[POLICY_EACH], A[POLICY_EACH];
+  int row[ROWS], col[ROWS], length[ROWS];        // length -1: behind the last value
+  unsigned masks;                                // bit k: value k counts
+
+  // All loads at once; what a mask leaves out is read, but not looked at.
+  __device__ __forceinline__ void load(const PolicyArgs& a, long long first, long long step) {
+    masks = 0;
 #pragma unroll
-  for (int k = 0; k < EACH; ++k) {
-    const long long i = first + k * step;
-    inside[k] = i < a.total;
-    const long long n = (unsigned)i / (unsigned)a.T;         // fewer than 2^31 values
-    rows[k] = n;
-    cols[k] = (int)(i - n * a.T);
-    counted[k] = inside[k] && cols[k] < length_of(a, n) && (!a.mask || a.mask[n * a.ld_mask + cols[k]] != 0);
-    if (!counted[k]) continue;
-    x[k] = a.logp[n * a.ld_logp + cols[k]];
-    o[k] = a.old_logp[n * a.ld_old + cols[k]];
-    if (a.ref) q[k] = a.ref[n * a.ld_ref + cols[k]];
-    A[k] = a.ld_adv ? a.adv[n * a.ld_adv + cols[k]] : a.adv[n];
-  }
-#pragma unroll
-  for (int k = 0; k < EACH; ++k) {
-    if (!inside[k]) continue;
-    float g = 0.f;
-    if (counted[k]) {
-      const float w = weight_of(a, t, a.reduction != PCTC_POLICY_SEQUENCES ? 0
-                                      : a.mask ? a.row_count[rows[k]] : length_of(a, rows[k]));
-      g = a.sign * w * policy_token(a, x[k], o[k], q[k], A[k], (double)w, s);
+    for (int k = 0; k < ROWS; ++k) {
+      const long long i = first + k * step;
+      row[k] = (int)((unsigned)i / (unsigned)a.T);                // fewer than 2^31 values
+      col[k] = (int)(i - row[k] * a.T);
+      length[k] = i < a.total ? length_of(a, row[k]) : -1;
     }
-    if (a.grad) a.grad[rows[k] * a.ld_grad + cols[k]] = g;
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      if (col[k] >= length[k]) continue;
+      const long long n = row[k];
+      const int c = col[k];
+      if constexpr (VEC) {
+        const float4 fx = *reinterpret_cast<const float4*>(a.logp + n * a.ld_logp + c);
+        const float4 fo = *reinterpret_cast<const float4*>(a.old_logp + n * a.ld_old + c);
+        float4 fq = make_float4(0.f, 0.f, 0.f, 0.f), fa;
+        if (a.ref) fq = *reinterpret_cast<const float4*>(a.ref + n * a.ld_ref + c);
+        if (a.ld_adv) fa = *reinterpret_cast<const float4*>(a.adv + n * a.ld_adv + c);
+        else fa.x = fa.y = fa.z = fa.w = a.adv[n];
+        unsigned m = 0x01010101u;
+        if (a.mask) m = *reinterpret_cast<const unsigned*>(a.mask + n * a.ld_mask + c);
+        x[0] = fx.x; x[1] = fx.y; x[2] = fx.z; x[3] = fx.w;
+        o[0] = fo.x; o[1] = fo.y; o[2] = fo.z; o[3] = fo.w;
+        q[0] = fq.x; q[1] = fq.y; q[2] = fq.z; q[3] = fq.w;
+        A[0] = fa.x; A[1] = fa.y; A[2] = fa.z; A[3] = fa.w;
+#pragma unroll
+        for (int j = 0; j < POLICY_EACH; ++j)
+          if (((m >> (8 * j)) & 0xffu) != 0 && c + j < length[k]) masks |= 1u << j;
+      } else {
+        x[k] = a.logp[n * a.ld_logp + c];
+        o[k] = a.old_logp[n * a.ld_old + c];
+        q[k] = a.ref ? a.ref[n * a.ld_ref + c] : 0.f;
+        A[k] = a.ld_adv ? a.adv[n * a.ld_adv + c] : a.adv[n];
+        if (!a.mask || a.mask[n * a.ld_mask + c] != 0) masks |= 1u << k;
+      }
+    }
   }
+  __device__ __forceinline__ void finish(const PolicyArgs& a, float part, TokenSums& s) const {
+    float g[POLICY_EACH] = {};
+    if (masks) {
+      float w = part;
+#pragma unroll
+      for (int k = 0; k < POLICY_EACH; ++k) {
+        if (k < ROWS && a.reduction == PCTC_POLICY_SEQUENCES)
+          w = weight_of(a, part, !VEC && !(masks >> k & 1) ? 1 : a.mask ? a.row_count[row[k]] : length[k]);
+        const bool on = masks >> k & 1;
+        const float v = policy_token(a, on ? a.sign * x[k] : 0.f, on ? a.sign * o[k] : 0.f, on ? a.sign * q[k] : 0.f, on ? A[k] : 0.f, w, s);
+        g[k] = on ? a.sign * w * v : 0.f;
+      }
+    }
+    s.count += __popc(masks);
+    if (!a.grad) return;
+    if constexpr (VEC) {
+      if (length[0] >= 0) *reinterpret_cast<float4*>(a.grad + row[0] * a.ld_grad + col[0]) = make_float4(g[0], g[1], g[2], g[3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < POLICY_EACH; ++k)
+        if (length[k] >= 0) a.grad[row[k] * a.ld_grad + col[k]] = g[k];
+    }
+  }
+};
+
+__device__ __forceinline__ void write_stats(const PolicyArgs& a, const BlockSums& s) {
+  const double n = (double)max(s.count, 1);
+  a.stats[0] = (float)s.loss;
+  a.stats[1] = (float)(s.kl / n);
+  a.stats[2] = (float)((double)s.clipped / n);
+  *a.count_out = s.count;
 }
 
-__device__ __forceinline__ void write_stats(const PolicyArgs& a, const Totals& t, double loss, double kl, double clipped) {
-  const double n = (double)max(t.count, 1ll);
-  a.stats[0] = (float)loss;
-  a.stats[1] = (float)(kl / n);
-  a.stats[2] = (float)(clipped / n);
-  *a.count_out = (int)t.count;
-}
-
+template <bool VEC, int GROUPS>
 __global__ void __launch_bounds__(POLICY_THREADS) k_policy(const PolicyArgs a) {
-  __shared__ double scratch[POLICY_THREADS / 32];
+  __shared__ float shared_part;
   __shared__ bool last;
-  const Totals t = a.counting ? a.head->totals : Totals{a.total, a.N};
+  const long long tile = (long long)blockIdx.x * (POLICY_THREADS * POLICY_EACH * GROUPS);
+  Values<VEC> v[GROUPS];
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) {
+    const long long first = tile + i * (POLICY_THREADS * POLICY_EACH);
+    v[i].load(a, VEC ? first + threadIdx.x * POLICY_EACH : first + threadIdx.x, VEC ? 1 : POLICY_THREADS);
+  }
+  wait_for_previous();                           // the inputs are older than the launch before this one; the counts are its own
+  Totals t{(int)a.total, (int)a.N};
+  if (a.counting) {
+    if (threadIdx.x < 32) {
+      t = Totals{0, 0};
+      const int blocks = a.head->blocks;
+#pragma unroll
+      for (int i = 0; i < (POLICY_COUNT_BLOCKS + 31) / 32; ++i)
+        if (i * 32 + (int)threadIdx.x < blocks) {
+          const Totals u = a.head->totals[i * 32 + threadIdx.x];
+          t.count += u.count;
+          t.rows += u.rows;
+        }
+      t = warp_sum(t);
+      if (threadIdx.x == 0) shared_part = weight_part(a, t);
+    }
+    __syncthreads();
+  }
+  const float part = a.counting ? shared_part : weight_part(a, t);
   TokenSums s;
-  policy_values<POLICY_EACH>(a, t, (long long)blockIdx.x * (POLICY_THREADS * POLICY_EACH) + threadIdx.x, POLICY_THREADS, s);
-  const double loss = block_sum<POLICY_THREADS>(s.loss, scratch), kl = block_sum<POLICY_THREADS>(s.kl, scratch),
-               clipped = block_sum<POLICY_THREADS>((double)s.clipped, scratch);
+#pragma unroll
+  for (int i = 0; i < GROUPS; ++i) v[i].finish(a, part, s);
+  BlockSums sums = block_sum<POLICY_THREADS>((double)s.loss, (double)s.kl, s.count, s.clipped);
   if (threadIdx.x == 0) {
-    double* p = a.partial + 3ll * blockIdx.x;
-    __stcg(p, loss);
-    __stcg(p + 1, kl);
-    __stcg(p + 2, clipped);
+    BlockSums* p = a.partial + blockIdx.x;
+    __stcg(reinterpret_cast<double2*>(p), make_double2(sums.loss, sums.kl));
+    __stcg(reinterpret_cast<int2*>(&p->count), make_int2(sums.count, sums.clipped));
     __threadfence();
     last = atomicAdd(&a.head->ticket, 1u) == gridDim.x - 1;
     __threadfence();
   }
   __syncthreads();
   if (!last) return;
-  double sum[3] = {0.0, 0.0, 0.0};               // every thread the same blocks, whoever comes last
-  for (long long b = threadIdx.x; b < gridDim.x; b += POLICY_THREADS)
-#pragma unroll
-    for (int j = 0; j < 3; ++j) sum[j] += __ldcg(a.partial + 3 * b + j);
-#pragma unroll
-  for (int j = 0; j < 3; ++j) sum[j] = block_sum<POLICY_THREADS>(sum[j], scratch);
-  if (threadIdx.x == 0) write_stats(a, t, sum[0], sum[1], sum[2]);
+  sums = BlockSums{0.0, 0.0, 0, 0};              // every thread the same blocks, whoever comes last
+#pragma unroll 4
+  for (long long b = threadIdx.x; b < gridDim.x; b += POLICY_THREADS) {
+    const BlockSums* p = a.partial + b;
+    const double2 u = __ldcg(reinterpret_cast<const double2*>(p));
+    const int2 c = __ldcg(reinterpret_cast<const int2*>(&p->count));
+    sums.loss += u.x;
+    sums.kl += u.y;
+    sums.count += c.x;
+    sums.clipped += c.y;
+  }
+  sums = block_sum<POLICY_THREADS>(sums.loss, sums.kl, sums.count, sums.clipped);
+  if (threadIdx.x == 0) write_stats(a, sums);
 }
 
 // All of it by one cluster (of one block or more): the counts and the sums cross shared memory.
+template <bool VEC>
 __global__ void __launch_bounds__(POLICY_SMALL_THREADS) k_policy_small(const PolicyArgs a) {
-  __shared__ double scratch[POLICY_SMALL_THREADS / 32];
-  __shared__ long long whole[POLICY_SMALL_THREADS / 32];
   __shared__ Totals counts;
-  __shared__ double sums[3];
+  __shared__ float shared_part;
+  __shared__ BlockSums block_sums;
   cg::cluster_group cluster = cg::this_cluster();
   const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const long long thread = rank * POLICY_SMALL_THREADS + threadIdx.x, threads = blocks * POLICY_SMALL_THREADS;
-  Totals t{a.total, a.N};
+  Values<VEC> v;
+  v.load(a, VEC ? thread * POLICY_EACH : thread, VEC ? 1 : threads);
+  Totals t{(int)a.total, (int)a.N};
   if (a.counting) {
-    const Totals mine = a.T <= POLICY_SHORT_ROW ? count_rows<1>(a, thread, threads) : count_rows<32>(a, thread >> 5, threads >> 5);
-    const long long count = block_sum<POLICY_SMALL_THREADS>(mine.count, whole), rows = block_sum<POLICY_SMALL_THREADS>(mine.rows, whole);
-    if (threadIdx.x == 0) counts = Totals{count, rows};
+    t = count_all<POLICY_SMALL_THREADS>(a, rank, blocks);
+    if (threadIdx.x == 0) counts = t;
     cluster.sync();                              // the row counts in global memory are visible, too
-    t = Totals{0, 0};
-    for (int b = 0; b < blocks; ++b) {
-      const Totals* other = cluster.map_shared_rank(&counts, b);
-      t.count += other->count;
-      t.rows += other->rows;
+    if (threadIdx.x < 32) {
+      t = warp_sum((int)threadIdx.x < blocks ? *cluster.map_shared_rank(&counts, (int)threadIdx.x) : Totals{0, 0});
+      if (threadIdx.x == 0) shared_part = weight_part(a, t);
     }
+    __syncthreads();
   }
   TokenSums s;
-  for (long long i = thread; i < a.total; i += threads * POLICY_EACH) policy_values<POLICY_EACH>(a, t, i, threads, s);
-  const double loss = block_sum<POLICY_SMALL_THREADS>(s.loss, scratch), kl = block_sum<POLICY_SMALL_THREADS>(s.kl, scratch),
-               clipped = block_sum<POLICY_SMALL_THREADS>((double)s.clipped, scratch);
-  if (threadIdx.x == 0) {
-    sums[0] = loss;
-    sums[1] = kl;
-    sums[2] = clipped;
+  v.finish(a, a.counting ? shared_part : weight_part(a, t), s);
+  BlockSums sums = block_sum<POLICY_SMALL_THREADS>((double)s.loss, (double)s.kl, s.count, s.clipped);
+  if (blocks == 1) {
+    if (threadIdx.x == 0) write_stats(a, sums);
+    return;
   }
+  if (threadIdx.x == 0) block_sums = sums;
   cluster.sync();
   if (rank == 0 && threadIdx.x == 0) {
-    double all[3] = {0.0, 0.0, 0.0};
-    for (int b = 0; b < blocks; ++b) {
-      const double* other = cluster.map_shared_rank(&sums[0], b);
-      for (int j = 0; j < 3; ++j) all[j] += other[j];
+    for (int b = 1; b < blocks; ++b) {
+      const BlockSums* other = cluster.map_shared_rank(&block_sums, b);
+      sums.loss += other->loss;
+      sums.kl += other->kl;
+      sums.count += other->count;
+      sums.clipped += other->clipped;
     }
-    write_stats(a, t, all[0], all[1], all[2]);
+    write_stats(a, sums);
   }
   cluster.sync();                                // nobody leaves before all have been read
 }
@@ -285,16 +415,23 @@ __global__ void __launch_bounds__(POLICY_SMALL_THREADS) k_policy_small(const Pol
 // Host side
 // ---------------------------------------------------------------------------------------------
 struct PolicyPlan {
+  bool many;
   long long blocks;
   size_t rows, partial, total;
 };
 PolicyPlan policy_plan(const pctc_policy_t* p) {
   PolicyPlan w;
-  w.blocks = (p->N * p->T + POLICY_THREADS * POLICY_EACH - 1) / (POLICY_THREADS * POLICY_EACH);
-  w.rows = 256;
+  w.many = p->N * p->T > POLICY_MANY;
+  const long long tile = POLICY_THREADS * POLICY_EACH * (w.many ? 2 : 1);
+  w.blocks = (p->N * p->T + tile - 1) / tile;
+  w.rows = (sizeof(PolicyHead) + 255) / 256 * 256;
   w.partial = w.rows + ((size_t)p->N * 4 + 255) / 256 * 256;
-  w.total = w.partial + (size_t)w.blocks * 3 * sizeof(double);
+  w.total = w.partial + (size_t)w.blocks * sizeof(BlockSums);
   return w;
+}
+float2 number_and_rest(double v) {
+  const float x = (float)v;
+  return make_float2(x, std::isinf(x) ? 0.f : (float)(v - (double)x));
 }
 pctc_status_t check_policy(const pctc_policy_t* p) {
   if (!p || p->N < 1 || p->T < 1) return PCTC_ERR_INVALID_ARG;
@@ -366,7 +503,7 @@ pctc_status_t pctc_policy_loss(const pctc_policy_t* p, const float* logp, const 
   a.count_out = count;
   a.head = (PolicyHead*)workspace;
   a.row_count = mask && p->reduction == PCTC_POLICY_SEQUENCES ? (int*)((char*)workspace + w.rows) : nullptr;
-  a.partial = (double*)((char*)workspace + w.partial);
+  a.partial = (BlockSums*)((char*)workspace + w.partial);
   a.N = p->N;
   a.T = p->T;
   a.total = p->N * p->T;
@@ -376,14 +513,18 @@ pctc_status_t pctc_policy_loss(const pctc_policy_t* p, const float* logp, const 
   a.ld_adv = p->ld_adv;
   a.ld_mask = p->ld_mask;
   a.ld_grad = p->ld_grad;
-  a.log_low = std::log1p(-p->clip_low);
-  a.log_high = std::log1p(p->clip_high);
+  a.log_low = number_and_rest(std::log1p(-p->clip_low));
+  a.log_high = number_and_rest(std::log1p(p->clip_high));
   a.low = (float)(1.0 - p->clip_low);
   a.high = (float)(1.0 + p->clip_high);
   a.kl_weight = (float)p->kl_weight;
   a.sign = p->negated ? -1.f : 1.f;
   a.reduction = p->reduction;
-  a.counting = mask || lengths;
+  a.counting = (mask || lengths) && p->reduction != PCTC_POLICY_SUM;
+  // groups of four values of one row, 16-byte aligned in every array
+  const bool vec = p->T % 4 == 0 && (((size_t)logp | (size_t)old_logp | (size_t)ref_logp | (size_t)grad) & 15) == 0 && ((size_t)mask & 3) == 0 &&
+                   ((p->ld_logp | p->ld_old | (ref_logp ? p->ld_ref : 0) | (mask ? p->ld_mask : 0) | (grad ? p->ld_grad : 0)) & 3) == 0 &&
+                   (!p->ld_adv || (((size_t)advantages & 15) == 0 && (p->ld_adv & 3) == 0));
   cudaStream_t stream = (cudaStream_t)stream_v;
   if (a.total <= POLICY_SMALL) {
     cudaLaunchAttribute attr[1];
@@ -396,16 +537,14 @@ pctc_status_t pctc_policy_loss(const pctc_policy_t* p, const float* logp, const 
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_policy_small, a) == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, vec ? k_policy_small<true> : k_policy_small<false>, a) == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
   }
-  if (cudaMemsetAsync(workspace, 0, sizeof(PolicyHead), stream) != cudaSuccess) return PCTC_ERR_CUDA;
-  if (a.counting) {
-    const long long workers = a.T <= POLICY_SHORT_ROW ? a.N : a.N * 32, blocks = (workers + POLICY_THREADS - 1) / POLICY_THREADS;
-    k_policy_count<<<(unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), POLICY_THREADS, 0, stream>>>(a);
-    if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
-  }
-  k_policy<<<(unsigned)w.blocks, POLICY_THREADS, 0, stream>>>(a);
-  return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+  const long long threads = !a.counting ? 1 : !mask || a.T <= POLICY_SHORT_ROW ? a.N : a.T <= POLICY_LONG_ROW ? a.N * 32 : a.N * POLICY_THREADS;
+  const long long blocks = (threads + POLICY_THREADS - 1) / POLICY_THREADS;
+  k_policy_count<<<(unsigned)(blocks < POLICY_COUNT_BLOCKS ? blocks : POLICY_COUNT_BLOCKS), POLICY_THREADS, 0, stream>>>(a);
+  if (cudaGetLastError() != cudaSuccess) return PCTC_ERR_CUDA;
+  auto kernel = w.many ? (vec ? k_policy<true, 2> : k_policy<false, 2>) : vec ? k_policy<true, 1> : k_policy<false, 1>;
+  return launch_behind(kernel, (unsigned)w.blocks, POLICY_THREADS, 0, stream, a) == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
 }
 
 }  // extern "C"
