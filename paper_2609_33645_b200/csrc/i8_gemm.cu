@@ -2,11 +2,14 @@
 //   s = max|x| / 127,   q = round(x * (127 / max|x|)).
 // Sums are whole numbers of 32 bits (exact for k < 2^17); nothing is rounded before the scales.
 //
-// k_i8_gemm is a persistent tcgen05 kernel (kind::i8).  The rows of its accumulators are the channels j (the head's rows) and
-// the columns the tokens i: with few tokens the head streams through a deep ring as the wide operand of 128 x 16 ..
-// 128 x 128 tiles, and 32 lanes of a warp hold 32 neighbouring channels of a token, which is the order of C.  Many tokens
-// take 256 x 256 tiles of CTA pairs (cta_group::2).  Roles, rings and bounded waits are those of the bf16 kernel in umma_gemm.cu.
-//   few tokens: bound by HBM, the head's bytes once;   many: by the tensor pipe.
+// k_i8_gemm is a persistent tcgen05 kernel (kind::i8) in two forms; roles, ring and bounded waits are those of the bf16
+// kernel in umma_gemm.cu.
+//   few tokens (up to 128), CTAS = 1: the rows of the accumulators are channels (rows of the head), the columns tokens, tiles
+//     128 x 16 .. 128 x 128: the head streams once through a deep ring, and 32 lanes of a warp hold 32 neighbouring
+//     channels of a token, which is the order of C.  Bound by HBM.
+//   many tokens, CTAS = 2: 256 tokens x 256 channels a CTA pair (cta_group::2), the rows are tokens, and results leave
+//     through shared memory and TMA stores as in the bf16 kernel (with channels as rows a result took 10 instructions and
+//     more: 512 x 151,936 x 512 113 us).  Bound by the tensor pipe, or by the results where sums are short.
 #include "../../include/prunedctc.h"
 #include "i8_gemm.h"
 #include "pctc_internal.h"
@@ -54,27 +57,24 @@ __device__ __forceinline__ int quantize_one(float x, float f) {
   return max(-127, min(127, __float2int_rn(x * f)));
 }
 
-// GROUP threads hold a row: NV groups of eight values each.
-template <typename T, int GROUP, int NV>
+// GROUP threads hold a row: NV pieces of N values each, loaded once.
+template <typename T, int N, int GROUP, int NV>
 __global__ void __launch_bounds__(QUANT_THREADS) k_quantize(const QuantArgs a) {
   __shared__ unsigned tops[QUANT_THREADS / 32];
+  launch_next();
   if (a.clear && blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
   const long long row = (long long)blockIdx.x * (QUANT_THREADS / GROUP) + threadIdx.x / GROUP;
-  const int at = threadIdx.x % GROUP, per_row = (int)(a.cols / 8);
-  const bool there = row < a.rows;
-  Vec8<T> v[NV];
+  const int at = threadIdx.x % GROUP, per_row = row < a.rows ? (int)(a.cols / N) : 0;
+  VecN<T, N> v[NV];
   unsigned top = 0;
 #pragma unroll
   for (int k = 0; k < NV; ++k)
-    if (there && at + k * GROUP < per_row) v[k].load((const T*)a.x + row * a.ld_x + (at + k * GROUP) * 8);
+    if (at + k * GROUP < per_row) v[k].load((const T*)a.x + row * a.ld_x + (at + k * GROUP) * N);
 #pragma unroll
   for (int k = 0; k < NV; ++k)
-    if (there && at + k * GROUP < per_row) {
-      float x[8];
-      v[k].get(x);
+    if (at + k * GROUP < per_row)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, magnitude(x[j]));
-    }
+      for (int j = 0; j < N; ++j) top = max(top, magnitude(v[k].value(j)));
   top = __reduce_max_sync(0xffffffffu, top);
   if (GROUP > 32) {
     if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
@@ -82,19 +82,21 @@ __global__ void __launch_bounds__(QUANT_THREADS) k_quantize(const QuantArgs a) {
 #pragma unroll
     for (int w = 0; w < QUANT_THREADS / 32; ++w) top = max(top, tops[w]);
   }
-  if (!there) return;
+  if (per_row == 0) return;
   float scale;
   const float f = row_factor(top, scale);
   if (at == 0) a.scales[row] = scale;
 #pragma unroll
   for (int k = 0; k < NV; ++k)
     if (at + k * GROUP < per_row) {
-      float x[8];
-      v[k].get(x);
       unsigned w[2] = {0u, 0u};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j >> 2] |= ((unsigned)quantize_one(x[j], f) & 0xffu) << (8 * (j & 3));
-      *reinterpret_cast<uint2*>(a.q + row * a.ld_q + (at + k * GROUP) * 8) = make_uint2(w[0], w[1]);
+      for (int j = 0; j < N; ++j) w[j >> 2] |= ((unsigned)quantize_one(v[k].value(j), f) & 0xffu) << (8 * (j & 3));
+      signed char* to = a.q + row * a.ld_q + (at + k * GROUP) * N;
+      if constexpr (N == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+      else if constexpr (N == 4) *reinterpret_cast<unsigned*>(to) = w[0];
+      else if constexpr (N == 2) *reinterpret_cast<unsigned short*>(to) = (unsigned short)w[0];
+      else *to = (signed char)w[0];
     }
 }
 
@@ -102,6 +104,7 @@ __global__ void __launch_bounds__(QUANT_THREADS) k_quantize(const QuantArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(QUANT_THREADS) k_quantize_any(const QuantArgs a) {
   __shared__ unsigned tops[QUANT_THREADS / 32];
+  launch_next();
   if (a.clear && blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
   const long long row = blockIdx.x;
   const T* x = (const T*)a.x + row * a.ld_x;
@@ -119,23 +122,34 @@ __global__ void __launch_bounds__(QUANT_THREADS) k_quantize_any(const QuantArgs 
     a.q[row * a.ld_q + c] = (signed char)quantize_one(to_float(x[c]), f);
 }
 
-template <typename T, int GROUP, int NV>
+template <typename T, int N, int GROUP, int NV>
 void quantize_rows(const QuantArgs& a, cudaStream_t stream) {
   constexpr int per = QUANT_THREADS / GROUP;
-  k_quantize<T, GROUP, NV><<<(unsigned)((a.rows + per - 1) / per), QUANT_THREADS, 0, stream>>>(a);
+  k_quantize<T, N, GROUP, NV><<<(unsigned)((a.rows + per - 1) / per), QUANT_THREADS, 0, stream>>>(a);
+}
+// A warp a row up to 128 pieces, a block up to 2,048.
+template <typename T, int N>
+void quantize_pieces(const QuantArgs& a, cudaStream_t stream) {
+  const long long v = a.cols / N;
+  if (v <= 32) quantize_rows<T, N, 32, 1>(a, stream);
+  else if (v <= 64) quantize_rows<T, N, 32, 2>(a, stream);
+  else if (v <= 128) quantize_rows<T, N, 32, 4>(a, stream);
+  else if (v <= 256) quantize_rows<T, N, 256, 1>(a, stream);
+  else if (v <= 512) quantize_rows<T, N, 256, 2>(a, stream);
+  else if (v <= 1024) quantize_rows<T, N, 256, 4>(a, stream);
+  else if (v <= 2048 && N <= 4) quantize_rows<T, N, 256, 8>(a, stream);
+  else k_quantize_any<T><<<(unsigned)a.rows, QUANT_THREADS, 0, stream>>>(a);
 }
 template <typename T>
 cudaError_t quantize_launch(const QuantArgs& a, cudaStream_t stream) {
-  const bool vec = a.cols % 8 == 0 && ((size_t)a.x & 15) == 0 && (a.ld_x * (long long)sizeof(T)) % 16 == 0 &&
-                   ((size_t)a.q & 7) == 0 && a.ld_q % 8 == 0;
-  const long long v = a.cols / 8;
-  if (!vec || v > 256 * 4) k_quantize_any<T><<<(unsigned)a.rows, QUANT_THREADS, 0, stream>>>(a);
-  else if (v <= 32) quantize_rows<T, 32, 1>(a, stream);
-  else if (v <= 64) quantize_rows<T, 32, 2>(a, stream);
-  else if (v <= 128) quantize_rows<T, 32, 4>(a, stream);
-  else if (v <= 256) quantize_rows<T, 256, 1>(a, stream);
-  else if (v <= 512) quantize_rows<T, 256, 2>(a, stream);
-  else quantize_rows<T, 256, 4>(a, stream);
+  const auto fits = [&](int n) {
+    const size_t bytes = n * sizeof(T) < 16 ? n * sizeof(T) : 16;
+    return a.cols % n == 0 && (size_t)a.x % bytes == 0 && a.ld_x * sizeof(T) % bytes == 0 && (size_t)a.q % n == 0 && a.ld_q % n == 0;
+  };
+  if (fits(8)) quantize_pieces<T, 8>(a, stream);
+  else if (fits(4)) quantize_pieces<T, 4>(a, stream);
+  else if (fits(2)) quantize_pieces<T, 2>(a, stream);
+  else quantize_pieces<T, 1>(a, stream);
   return cudaGetLastError();
 }
 
@@ -148,24 +162,30 @@ constexpr int I8_W_STAGE = I8_ROWS * I8_BK;
 constexpr int I8_EPI_WARPS = 8;
 constexpr int I8_THREADS = 64 + 32 * I8_EPI_WARPS;
 constexpr int I8_MAX_STAGES = 12;
-constexpr int I8_RING = 216 * 1024;              // shared memory for the ring
 constexpr int I8_TMEM_COLS = 512;
 
 struct I8Args {
   int n, m, k;                                   // channels, tokens, contraction
-  int cols;                                      // tokens of a tile
+  int cols;                                      // columns of a tile: tokens (CTAS = 1) or channels (CTAS = 2)
   int stages;
-  int band;                                      // token tiles that are walked together (their rows stay in L2)
+  int band;                                      // CTAS = 2: token tiles that are walked together (their rows stay in L2)
   const float* a_scale;                          // [m]
   const float* b_scale;                          // [n]
   const void* bias;                              // [n] or null
   int bias_bf16;
   void* C;
   long long ldc;
-  int pairs;                                     // two neighbouring bf16 channels can be stored as one word
+  int aligned;                                   // CTAS = 1: two neighbouring bf16 channels can be stored as one word;
+                                                 // CTAS = 2: rows of C can be stored by TMA
+  int behind;                                    // the launch before this one makes the tokens (and nothing else that is read here)
   int* status;
 };
 
+// Shared memory behind the ring: CTAS = 1: the tokens' scales; CTAS = 2: of every epilogue warp two boxes of 32 rows x 64 bytes on
+// their way out (64-byte swizzle), and the scales and biases of its channels.
+constexpr int I8_BOX = 2048, I8_WARP_COLS = 128;
+constexpr int i8_ring(int ctas) { return ctas == 2 ? 5 * 2 * I8_ROWS * I8_BK : 216 * 1024; }
+constexpr int i8_extra(int ctas) { return ctas == 2 ? I8_EPI_WARPS * (2 * I8_BOX + I8_WARP_COLS * 8) : I8_ROWS * 4; }
 struct I8Tail {
   unsigned long long full[I8_MAX_STAGES];
   unsigned long long empty[I8_MAX_STAGES];
@@ -174,10 +194,9 @@ struct I8Tail {
   unsigned long long done;
   unsigned tmem_base;
   int abort;
-  float scale[I8_EPI_WARPS][32];                 // token scales of the columns that a warp works on
 };
-constexpr int I8_SMEM = 1024 + I8_RING + (int)((sizeof(I8Tail) + 255) / 256 * 256);
-static_assert(I8_SMEM <= 227 * 1024, "shared memory budget");
+constexpr int i8_smem(int ctas) { return 1024 + i8_ring(ctas) + i8_extra(ctas) + (int)sizeof(I8Tail); }
+static_assert(i8_smem(1) <= 227 * 1024 && i8_smem(2) <= 227 * 1024, "shared memory budget");
 
 __device__ __forceinline__ void tc_mma_i8_pair(unsigned tmem_d, unsigned long long adesc, unsigned long long bdesc,
                                                unsigned idesc, unsigned accumulate) {
@@ -203,25 +222,37 @@ __device__ __forceinline__ unsigned long long i8_smem_desc(unsigned addr) {
          (2ull << 61);
 }
 
-// Tile u: token tiles run fastest inside a band, so that the head's rows are read once a band while the band's token
-// rows stay in L2.
-__device__ __forceinline__ void i8_tile(int u, int n_tiles, int m_tiles, int band, int& nt, int& mt) {
-  const int b = u / (band * n_tiles), r = u - b * band * n_tiles, rows = min(band, m_tiles - b * band);
-  nt = r / rows;
-  mt = b * band + (r - nt * rows);
+// Unit u -> first channel and first token of its tile.  With pairs the token tiles run fastest inside a band, so that the
+// head's rows are read once a band while the band's token rows stay in L2.
+template <int CTAS>
+__device__ __forceinline__ void i8_tile(const I8Args& a, int u, int n_tiles, int m_tiles, int& channel, int& token) {
+  if (CTAS == 1) {
+    channel = u * I8_ROWS;
+    token = 0;
+    return;
+  }
+  const int b = u / (a.band * n_tiles), r = u - b * a.band * n_tiles, rows = min(a.band, m_tiles - b * a.band), nt = r / rows;
+  channel = nt * a.cols;
+  token = (b * a.band + (r - nt * rows)) * (2 * I8_ROWS);
 }
 
 template <typename T, int CTAS>
 __global__ void __launch_bounds__(I8_THREADS, 1)
-k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const I8Args a) {
+k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmC,
+          const I8Args a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((size_t)smem_raw + 1023) & ~(size_t)1023);
-  I8Tail* st = (I8Tail*)(smem + I8_RING);
+  unsigned char* extra = smem + i8_ring(CTAS);
+  I8Tail* st = (I8Tail*)(extra + i8_extra(CTAS));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = CTAS == 2 ? (int)cluster_ctarank() : 0;
   const int group = blockIdx.x / CTAS, ngroups = gridDim.x / CTAS;
-  const int x_stage = a.cols / CTAS * I8_BK, stage_bytes = I8_W_STAGE + x_stage;   // this CTA's part of a stage
-  const int n_tiles = (a.n + I8_ROWS * CTAS - 1) / (I8_ROWS * CTAS), m_tiles = (a.m + a.cols - 1) / a.cols;
+  // a stage of this CTA: 128 rows of the accumulators' rows, then its part of their columns
+  const int stage_bytes = I8_W_STAGE + a.cols / CTAS * I8_BK;
+  const int w_offset = CTAS == 1 ? 0 : I8_W_STAGE, x_offset = CTAS == 1 ? I8_W_STAGE : 0;
+  const int w_rows = CTAS == 1 ? 0 : rank * (a.cols / CTAS), x_rows = CTAS == 1 ? 0 : rank * I8_ROWS;   // this CTA's part of a tile
+  const int n_tiles = CTAS == 1 ? (a.n + I8_ROWS - 1) / I8_ROWS : (a.n + a.cols - 1) / a.cols;
+  const int m_tiles = CTAS == 1 ? 1 : (a.m + 2 * I8_ROWS - 1) / (2 * I8_ROWS);
   const int units = n_tiles * m_tiles, k_blocks = (a.k + I8_BK - 1) / I8_BK;
 
   if (threadIdx.x == 0) {
@@ -259,21 +290,34 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
       int s = 0;
       unsigned ph = 0;
       bool ok = true;
-      for (int u = group; u < units && ok; u += ngroups) {
-        int nt, mt;
-        i8_tile(u, n_tiles, m_tiles, a.band, nt, mt);
-        const int row_w = nt * (I8_ROWS * CTAS) + rank * I8_ROWS, row_x = mt * a.cols + rank * (a.cols / CTAS);
-        for (int kb = 0; kb < k_blocks; ++kb, ++g) {
-          if (!mbar_wait(&st->empty[s], ph ^ 1u, abort_flag, a.status, 1)) { ok = false; break; }
-          if (rank == 0) mbar_expect_tx(&st->full[s], CTAS * stage_bytes);   // the leader's barrier counts both CTAs
-          unsigned char* dst = smem + (size_t)s * stage_bytes;
-          if (CTAS == 2) {
-            tma_load_2d_pair(dst, &tmW, kb * I8_BK, row_w, &st->full[s]);
-            tma_load_2d_pair(dst + I8_W_STAGE, &tmX, kb * I8_BK, row_x, &st->full[s]);
-          } else {
-            tma_load_2d(dst, &tmW, kb * I8_BK, row_w, &st->full[s]);
-            tma_load_2d(dst + I8_W_STAGE, &tmX, kb * I8_BK, row_x, &st->full[s]);
+      const auto load = [&](unsigned char* dst, const CUtensorMap* map, int k, int row, unsigned long long* bar) {
+        if (CTAS == 2) tma_load_2d_pair(dst, map, k, row, bar); else tma_load_2d(dst, map, k, row, bar);
+      };
+      const auto load_w = [&](int stage, int kb, int channel) {
+        load(smem + (size_t)stage * stage_bytes + w_offset, &tmW, kb * I8_BK, channel + w_rows, &st->full[stage]);
+      };
+      // the head does not depend on the launch before: what the first ring of it takes is under way before that ends
+      int early = 0, channel, token;
+      if (a.behind) {
+        if (group < units) {
+          i8_tile<CTAS>(a, group, n_tiles, m_tiles, channel, token);
+          early = min(a.stages, k_blocks);
+          for (int j = 0; j < early; ++j) {
+            if (rank == 0) mbar_expect_tx(&st->full[j], CTAS * stage_bytes);
+            load_w(j, j, channel);
           }
+        }
+        wait_for_previous();
+      }
+      for (int u = group; u < units && ok; u += ngroups) {
+        i8_tile<CTAS>(a, u, n_tiles, m_tiles, channel, token);
+        for (int kb = 0; kb < k_blocks; ++kb, ++g) {
+          if ((int)g >= early) {
+            if (!mbar_wait(&st->empty[s], ph ^ 1u, abort_flag, a.status, 1)) { ok = false; break; }
+            if (rank == 0) mbar_expect_tx(&st->full[s], CTAS * stage_bytes);   // the leader's barrier counts both CTAs
+            load_w(s, kb, channel);
+          }
+          load(smem + (size_t)s * stage_bytes + x_offset, &tmX, kb * I8_BK, token + x_rows, &st->full[s]);
           if (++s == a.stages) { s = 0; ph ^= 1u; }
         }
       }
@@ -289,6 +333,7 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
       // accumulators of 32-bit integers, both operands signed 8-bit, k contiguous
       const unsigned idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)(a.cols >> 3) << 17) |
                              ((unsigned)((I8_ROWS * CTAS) >> 4) << 24);
+      const auto commit = [&](unsigned long long* bar) { if (CTAS == 2) tc_commit_pair(bar); else tc_commit(bar); };
       unsigned it = 0, ph = 0;
       int s = 0;
       bool ok = true;
@@ -301,17 +346,17 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
           if (!mbar_wait(&st->full[s], ph, abort_flag, a.status, 3)) { ok = false; break; }
           tc_fence_after();
           const unsigned at = smem_u32(smem + (size_t)s * stage_bytes);
-          const unsigned long long wdesc = i8_smem_desc(at), xdesc = i8_smem_desc(at + I8_W_STAGE);
+          const unsigned long long rdesc = i8_smem_desc(at), cdesc = i8_smem_desc(at + I8_W_STAGE);
 #pragma unroll
           for (int kk = 0; kk < I8_BK / 32; ++kk) {               // 32 k an instruction: 32 bytes further on
             const unsigned more = (kb != 0 || kk != 0) ? 1u : 0u;
-            if (CTAS == 2) tc_mma_i8_pair(d_tmem, wdesc + kk * 2, xdesc + kk * 2, idesc, more);
-            else tc_mma_i8(d_tmem, wdesc + kk * 2, xdesc + kk * 2, idesc, more);
+            if (CTAS == 2) tc_mma_i8_pair(d_tmem, rdesc + kk * 2, cdesc + kk * 2, idesc, more);
+            else tc_mma_i8(d_tmem, rdesc + kk * 2, cdesc + kk * 2, idesc, more);
           }
-          if (CTAS == 2) tc_commit_pair(&st->empty[s]); else tc_commit(&st->empty[s]);
+          commit(&st->empty[s]);
           if (++s == a.stages) { s = 0; ph ^= 1u; }
         }
-        if (ok) { if (CTAS == 2) tc_commit_pair(&st->tmem_full[acc]); else tc_commit(&st->tmem_full[acc]); }
+        if (ok) commit(&st->tmem_full[acc]);
       }
       if (CTAS == 2) tc_commit_pair_local(&st->done); else tc_commit(&st->done);
       mbar_wait_drain(&st->done, 0);
@@ -319,73 +364,157 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
   } else {
     // ===================== epilogue warps: two for each quarter of the lanes =====================
     const int ew = warp - 2, q = warp & 3;
-    const int groups = (a.cols + 31) / 32;                        // groups of 32 tokens; the two warps take turns
-    float* sa = st->scale[ew];
     T* C = (T*)a.C;
-    unsigned it = 0;
+    unsigned it = 0, boxes = 0;
     bool ok = true;
-    for (int u = group; u < units && ok; u += ngroups, ++it) {
-      int nt, mt;
-      i8_tile(u, n_tiles, m_tiles, a.band, nt, mt);
-      const int j = nt * (I8_ROWS * CTAS) + rank * I8_ROWS + q * 32 + lane;          // this lane's channel
-      const bool row_ok = j < a.n;
-      const float sb = row_ok ? a.b_scale[j] : 0.f;
-      float bias = 0.f;
-      if (a.bias && row_ok) bias = a.bias_bf16 ? __bfloat162float(((const __nv_bfloat16*)a.bias)[j]) : ((const float*)a.bias)[j];
-      const unsigned acc = it & 1u, aph = (it >> 1) & 1u;
+    const auto bias_of = [&](int j) {
+      return !a.bias ? 0.f : a.bias_bf16 ? __bfloat162float(((const __nv_bfloat16*)a.bias)[j]) : ((const float*)a.bias)[j];
+    };
+    const auto sums_ready = [&](unsigned acc, unsigned aph) {
       int got = 0;
       if (lane == 0) got = mbar_wait(&st->tmem_full[acc], aph, abort_flag, a.status, 4) ? 1 : 0;
       got = __shfl_sync(0xffffffffu, got, 0);
-      if (!got) { ok = false; break; }
-      tc_fence_after();
-      const unsigned taddr = tmem_base + ((unsigned)(q * 32) << 16) + acc * 256;
-      for (int cg = ew >> 2; cg < groups; cg += 2) {
-        const int i0 = mt * a.cols + cg * 32;
-        const int cnt = min(min(32, a.cols - cg * 32), a.m - i0);                     // tokens of this group
-        if (cnt <= 0) break;
-        __syncwarp();
-        sa[lane] = lane < cnt ? a.a_scale[i0 + lane] : 0.f;
-        float v[32];
-        tmem_ld32(taddr + cg * 32, v);
-        __syncwarp();
-#pragma unroll
-        for (int c = 0; c < 32; c += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(sa + c);
-          v[c] = fmaf((float)__float_as_int(v[c]), f.x * sb, bias);
-          v[c + 1] = fmaf((float)__float_as_int(v[c + 1]), f.y * sb, bias);
-          v[c + 2] = fmaf((float)__float_as_int(v[c + 2]), f.z * sb, bias);
-          v[c + 3] = fmaf((float)__float_as_int(v[c + 3]), f.w * sb, bias);
-        }
-        if constexpr (sizeof(T) == 4) {
-          if (row_ok) {
-            T* to = C + (long long)i0 * a.ldc + j;
-#pragma unroll
-            for (int c = 0; c < 32; ++c)
-              if (c < cnt) to[c * a.ldc] = v[c];
-          }
-        } else {
-          // lanes 2l and 2l + 1 hold neighbouring channels: the even one stores both of token c, the odd one of token c + 1
-          const bool odd = lane & 1, both = (j | 1) < a.n && a.pairs;
-          T* to = C + (long long)(i0 + (odd ? 1 : 0)) * a.ldc + (j & ~1);
-#pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(v[c], v[c + 1]);
-            const unsigned mine = *reinterpret_cast<const unsigned*>(&p);
-            const unsigned other = __shfl_xor_sync(0xffffffffu, mine, 1);
-            if (both) {
-              const unsigned w = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
-              if (c + (odd ? 1 : 0) < cnt) *reinterpret_cast<unsigned*>(to + c * a.ldc) = w;
-            } else if (row_ok) {
-              T* one = C + (long long)(i0 + c) * a.ldc + j;
-              if (c < cnt) one[0] = p.x;
-              if (c + 1 < cnt) one[a.ldc] = p.y;
-            }
-          }
-        }
-      }
+      if (got) tc_fence_after();
+      return got != 0;
+    };
+    const auto sums_read = [&](unsigned acc) {
       tc_fence_before();
       __syncwarp();
       if (lane == 0) { if (CTAS == 2) mbar_arrive_leader(&st->tmem_empty[acc]); else mbar_arrive(&st->tmem_empty[acc]); }
+    };
+    if (a.behind) wait_for_previous();
+    if constexpr (CTAS == 1) {
+      // a lane is a channel; the columns are all tokens there are, in groups of 32 that the two warps take in turn
+      float* sa = (float*)extra;
+      for (int i = lane; i < I8_ROWS; i += 32) sa[i] = i < a.m ? a.a_scale[i] : 0.f;   // the same by every warp
+      __syncwarp();
+      for (int u = group; u < units && ok; u += ngroups, ++it) {
+        const int j = u * I8_ROWS + q * 32 + lane;                // what a tile needs beside its sums is loaded before they are there
+        const bool row_ok = j < a.n;
+        const float sb = row_ok ? a.b_scale[j] : 0.f, bias = row_ok ? bias_of(j) : 0.f;
+        const unsigned acc = it & 1u;
+        if (!sums_ready(acc, (it >> 1) & 1u)) { ok = false; break; }
+        for (int i0 = (ew >> 2) * 32; i0 < a.m; i0 += 64) {
+          const int cnt = min(32, a.m - i0);
+          float v[32];
+          tmem_ld32(tmem_base + ((unsigned)(q * 32) << 16) + acc * 256 + i0, v);
+#pragma unroll
+          for (int c = 0; c < 32; c += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(sa + i0 + c);
+            v[c] = fmaf((float)__float_as_int(v[c]), f.x * sb, bias);
+            v[c + 1] = fmaf((float)__float_as_int(v[c + 1]), f.y * sb, bias);
+            v[c + 2] = fmaf((float)__float_as_int(v[c + 2]), f.z * sb, bias);
+            v[c + 3] = fmaf((float)__float_as_int(v[c + 3]), f.w * sb, bias);
+          }
+          if constexpr (sizeof(T) == 4) {
+            if (row_ok) {
+              T* to = C + (long long)i0 * a.ldc + j;
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                if (c < cnt) to[c * a.ldc] = v[c];
+            }
+          } else {
+            // lanes 2l and 2l + 1 hold neighbouring channels: the even one stores both of token c, the odd one of token c + 1
+            const bool odd = lane & 1, both = (j | 1) < a.n && a.aligned;
+            T* to = C + (long long)(i0 + (odd ? 1 : 0)) * a.ldc + (j & ~1);
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) {
+              const __nv_bfloat162 p = __floats2bfloat162_rn(v[c], v[c + 1]);
+              const unsigned mine = *reinterpret_cast<const unsigned*>(&p);
+              const unsigned other = __shfl_xor_sync(0xffffffffu, mine, 1);
+              if (both) {
+                const unsigned w = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
+                if (c + (odd ? 1 : 0) < cnt) *reinterpret_cast<unsigned*>(to + c * a.ldc) = w;
+              } else if (row_ok) {
+                T* one = C + (long long)(i0 + c) * a.ldc + j;
+                if (c < cnt) one[0] = p.x;
+                if (c + 1 < cnt) one[a.ldc] = p.y;
+              }
+            }
+          }
+        }
+        sums_read(acc);
+      }
+    } else {
+      // a lane is a token; a warp takes 128 channels, 32 at a time
+      unsigned char* stage = extra + ew * (2 * I8_BOX);
+      float* sb = (float*)(extra + I8_EPI_WARPS * 2 * I8_BOX) + ew * (2 * I8_WARP_COLS);
+      float* bias = sb + I8_WARP_COLS;
+      const unsigned swizzle = (unsigned)((lane >> 1) & 3);       // 64-byte swizzle of a row of a box
+      for (int u = group; u < units && ok; u += ngroups, ++it) {
+        int channel, token;
+        i8_tile<2>(a, u, n_tiles, m_tiles, channel, token);
+        const int row0 = token + rank * I8_ROWS + q * 32, i = row0 + lane, j0 = channel + (ew >> 2) * I8_WARP_COLS;
+        const float sa = i < a.m ? a.a_scale[i] : 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < I8_WARP_COLS; c += 32) {
+          const int j = j0 + c + lane;
+          sb[c + lane] = j < a.n ? a.b_scale[j] : 0.f;
+          bias[c + lane] = j < a.n ? bias_of(j) : 0.f;
+        }
+        __syncwarp();
+        const unsigned acc = it & 1u;
+        if (!sums_ready(acc, (it >> 1) & 1u)) { ok = false; break; }
+        const unsigned taddr = tmem_base + ((unsigned)(q * 32) << 16) + acc * 256 + (ew >> 2) * I8_WARP_COLS;
+#pragma unroll 1
+        for (int c0 = 0; c0 < I8_WARP_COLS && j0 + c0 < a.n; c0 += 32) {
+          float v[32];
+          tmem_ld32(taddr + c0, v);
+#pragma unroll
+          for (int c = 0; c < 32; c += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(sb + c0 + c), b = *reinterpret_cast<const float4*>(bias + c0 + c);
+            v[c] = fmaf((float)__float_as_int(v[c]), sa * f.x, b.x);
+            v[c + 1] = fmaf((float)__float_as_int(v[c + 1]), sa * f.y, b.y);
+            v[c + 2] = fmaf((float)__float_as_int(v[c + 2]), sa * f.z, b.z);
+            v[c + 3] = fmaf((float)__float_as_int(v[c + 3]), sa * f.w, b.w);
+          }
+          if (a.aligned) {
+            // 32 bf16 channels a box, or 16 fp32 ones; one box fills while the other is read out
+#pragma unroll
+            for (int b = 0; b < (int)sizeof(T) / 2; ++b) {
+              if (j0 + c0 + b * 16 >= a.n) break;
+              if (lane == 0) bulk_wait_read1();
+              __syncwarp();
+              unsigned char* box = stage + (boxes++ & 1u) * I8_BOX;
+              unsigned char* row = box + lane * 64;
+#pragma unroll
+              for (int p = 0; p < 4; ++p) {
+                uint4 w;
+                if constexpr (sizeof(T) == 4) {
+                  const float* x = v + b * 16 + p * 4;
+                  w = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+                } else {
+                  const float x[8] = {v[p * 8], v[p * 8 + 1], v[p * 8 + 2], v[p * 8 + 3], v[p * 8 + 4], v[p * 8 + 5], v[p * 8 + 6], v[p * 8 + 7]};
+                  w = Vec8<__nv_bfloat16>::pack(x);
+                }
+                *reinterpret_cast<uint4*>(row + (((unsigned)p ^ swizzle) << 4)) = w;
+              }
+              fence_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_2d(&tmC, box, j0 + c0 + b * 16, row0);  // rows and channels past the extents are clipped
+                bulk_commit();
+              }
+            }
+          } else {
+            // turned in shared memory, so that a row's 32 channels are stored by 32 lanes
+            float* turn = (float*)stage;
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 32; ++c) turn[lane * 32 + (c ^ lane)] = v[c];
+            __syncwarp();
+            const int rows = min(32, a.m - row0), j = j0 + c0 + lane;
+            if (j < a.n) {
+              T* to = C + (long long)row0 * a.ldc + j;
+#pragma unroll 8
+              for (int r = 0; r < rows; ++r, to += a.ldc) *to = from_float<T>(turn[r * 32 + (lane ^ r)]);
+            }
+          }
+        }
+        sums_read(acc);
+      }
+      if (lane == 0) bulk_wait0();                                // this warp's stores have completed
     }
   }
 
@@ -409,6 +538,17 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
 // ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
+bool i8_map_out(CUtensorMap* map, void* C, long long n, long long m, long long ldc, bool bf16) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)n, (cuuint64_t)m};
+  cuuint64_t strides[1] = {(cuuint64_t)(ldc * (bf16 ? 2 : 4))};
+  cuuint32_t box[2] = {bf16 ? 32u : 16u, 32};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, C, dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 bool i8_map(CUtensorMap* map, const void* base, long long k, long long rows, long long ld, unsigned box_rows) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
@@ -422,22 +562,24 @@ bool i8_map(CUtensorMap* map, const void* base, long long k, long long rows, lon
 }
 
 template <typename T, int CTAS>
-cudaError_t i8_launch(const CUtensorMap& tmW, const CUtensorMap& tmX, const I8Args& a, int units, cudaStream_t stream) {
+cudaError_t i8_launch(const CUtensorMap& tmW, const CUtensorMap& tmX, const CUtensorMap& tmC, const I8Args& a, int units, cudaStream_t stream) {
   static std::atomic<int> groups_on[MAX_DEVICES];       // CTA groups that can be resident at once; 0: not configured there yet
   auto kern = k_i8_gemm<T, CTAS>;
   const int dev = current_device();
   int most = groups_on[dev].load(std::memory_order_acquire);
   if (most == 0) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, I8_SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, i8_smem(CTAS));
     if (e != cudaSuccess) return e;
   }
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = CTAS;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(I8_THREADS);
-  cfg.dynamicSmemBytes = I8_SMEM;
+  cfg.dynamicSmemBytes = i8_smem(CTAS);
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
@@ -449,7 +591,8 @@ cudaError_t i8_launch(const CUtensorMap& tmW, const CUtensorMap& tmX, const I8Ar
     groups_on[dev].store(n, std::memory_order_release);
   }
   cfg.gridDim = dim3((unsigned)((units < most ? units : most) * CTAS));
-  return cudaLaunchKernelEx(&cfg, kern, tmW, tmX, a);
+  cfg.numAttrs = a.behind ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, tmW, tmX, tmC, a);
 }
 
 constexpr long long I8_BAND_BYTES = 32LL << 20;         // token rows of a band: a quarter of the L2
@@ -458,19 +601,18 @@ constexpr long long I8_BAND_BYTES = 32LL << 20;         // token rows of a band:
 
 cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, const signed char* B, long long ldb,
                     const float* b_scale, const void* bias, bool bias_bf16, int m, int n, int k, void* C, long long ldc,
-                    bool out_bf16, int* status, cudaStream_t stream) {
+                    bool out_bf16, int* status, bool behind, cudaStream_t stream) {
   if (m <= 0 || n <= 0) return cudaSuccess;
   // up to 128 tokens: tiles as wide as the tokens, so that the head is read once and the ring is deep
-  const bool pair = m > 128;
+  const bool pair = m > I8_ROWS;
   I8Args a = {};
   a.n = n; a.m = m; a.k = k;
   a.cols = pair ? 256 : (m + 15) / 16 * 16;
-  const int stage = I8_W_STAGE + a.cols / (pair ? 2 : 1) * I8_BK;
-  a.stages = I8_RING / stage < I8_MAX_STAGES ? I8_RING / stage : I8_MAX_STAGES;
-  const int rows = I8_ROWS * (pair ? 2 : 1);
-  const long long n_tiles = ((long long)n + rows - 1) / rows, m_tiles = ((long long)m + a.cols - 1) / a.cols;
+  const int stage = I8_W_STAGE + a.cols / (pair ? 2 : 1) * I8_BK, fit = i8_ring(pair ? 2 : 1) / stage;
+  a.stages = fit < I8_MAX_STAGES ? fit : I8_MAX_STAGES;
+  const long long n_tiles = pair ? ((long long)n + 255) / 256 : ((long long)n + I8_ROWS - 1) / I8_ROWS, m_tiles = pair ? ((long long)m + 255) / 256 : 1;
   if (n_tiles * m_tiles > 0x7fffffffLL - (1 << 20)) return cudaErrorInvalidValue;
-  long long band = I8_BAND_BYTES / ((long long)a.cols * k);
+  long long band = I8_BAND_BYTES / (256LL * k);
   band = band < 1 ? 1 : band > m_tiles ? m_tiles : band;
   if (band * n_tiles > 0x7fffffffLL) band = 1;
   a.band = (int)band;
@@ -480,15 +622,17 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
   a.bias_bf16 = bias_bf16 ? 1 : 0;
   a.C = C;
   a.ldc = ldc;
-  a.pairs = ((size_t)C & 3) == 0 && ldc % 2 == 0;
+  // (a TMA store clips a row at 16 bytes, not at its last value)
+  const int es = out_bf16 ? 2 : 4;
+  a.aligned = pair ? ((size_t)C & 15) == 0 && ldc * es % 16 == 0 && (long long)n * es % 16 == 0 : ((size_t)C & 3) == 0 && ldc % 2 == 0;
   a.status = status;
-  alignas(64) CUtensorMap tmW, tmX;
-  if (!i8_map(&tmW, B, k, n, ldb, I8_ROWS) || !i8_map(&tmX, A, k, m, lda, (unsigned)(a.cols / (pair ? 2 : 1))))
-    return cudaErrorInvalidValue;
+  a.behind = behind ? 1 : 0;
+  alignas(64) CUtensorMap tmW, tmX, tmC = {};
+  if (!i8_map(&tmW, B, k, n, ldb, I8_ROWS) || !i8_map(&tmX, A, k, m, lda, pair ? I8_ROWS : (unsigned)a.cols)) return cudaErrorInvalidValue;
+  if (pair && a.aligned && !i8_map_out(&tmC, C, n, m, ldc, out_bf16)) return cudaErrorInvalidValue;
   const int units = (int)(n_tiles * m_tiles);
-  if (pair)
-    return out_bf16 ? i8_launch<__nv_bfloat16, 2>(tmW, tmX, a, units, stream) : i8_launch<float, 2>(tmW, tmX, a, units, stream);
-  return out_bf16 ? i8_launch<__nv_bfloat16, 1>(tmW, tmX, a, units, stream) : i8_launch<float, 1>(tmW, tmX, a, units, stream);
+  if (pair) return out_bf16 ? i8_launch<__nv_bfloat16, 2>(tmW, tmX, tmC, a, units, stream) : i8_launch<float, 2>(tmW, tmX, tmC, a, units, stream);
+  return out_bf16 ? i8_launch<__nv_bfloat16, 1>(tmW, tmX, tmC, a, units, stream) : i8_launch<float, 1>(tmW, tmX, tmC, a, units, stream);
 }
 
 cudaError_t i8_quantize(const void* x, bool bf16, long long rows, long long cols, long long ld_x, signed char* q, long long ld_q,
@@ -567,7 +711,7 @@ pctc_status_t pctc_i8_matmul(const pctc_i8_t* p, const int8_t* A, const float* a
     if (to.overlaps(r) || word.overlaps(r)) return PCTC_ERR_INVALID_ARG;
   if (!umma_available()) return PCTC_ERR_CUDA;
   const cudaError_t e = i8_gemm((const signed char*)A, p->lda, a_scales, (const signed char*)B, p->ldb, b_scales, bias,
-                                p->bias_dtype == PCTC_BF16, p->m, p->n, p->k, C, p->ldc, p->out_dtype == PCTC_BF16, device_status,
+                                p->bias_dtype == PCTC_BF16, p->m, p->n, p->k, C, p->ldc, p->out_dtype == PCTC_BF16, device_status, false,
                                 (cudaStream_t)stream_v);
   return e == cudaSuccess ? PCTC_OK : e == cudaErrorInvalidValue ? PCTC_ERR_UNSUPPORTED : PCTC_ERR_CUDA;
 }
@@ -605,7 +749,7 @@ pctc_status_t pctc_i8_logits(const pctc_i8_t* p, const void* x, int32_t x_dtype,
   cudaStream_t stream = (cudaStream_t)stream_v;
   if (i8_quantize(x, x_dtype == PCTC_BF16, p->m, p->k, p->lda, q, w.ld, scales, (int*)ws, stream) != cudaSuccess) return PCTC_ERR_CUDA;
   const cudaError_t e = i8_gemm(q, w.ld, scales, (const signed char*)B, p->ldb, b_scales, bias, p->bias_dtype == PCTC_BF16, p->m, p->n,
-                                p->k, C, p->ldc, p->out_dtype == PCTC_BF16, (int*)ws, stream);
+                                p->k, C, p->ldc, p->out_dtype == PCTC_BF16, (int*)ws, true, stream);
   return e == cudaSuccess ? PCTC_OK : e == cudaErrorInvalidValue ? PCTC_ERR_UNSUPPORTED : PCTC_ERR_CUDA;
 }
 

@@ -848,7 +848,7 @@ pctc_status_t topk_call(const pctc_problem_t* p, const void* hidden, const void*
     const int Cc = (int)((g.V - v0 < t.chunk) ? (g.V - v0) : t.chunk);
     if (head8) {
       PCTC_CUDA(i8_gemm(d_q, h8.ld, d_scales, (const signed char*)head8->q + v0 * head8->ld, head8->ld, head8->scales + v0,
-                        nullptr, false, M, Cc, D, d_logits, t.chunk, false, d_status, stream));
+                        nullptr, false, M, Cc, D, d_logits, t.chunk, false, d_status, false, stream));
     } else {
       Epilogue e;
       e.kind = EPI_STORE_F32;
