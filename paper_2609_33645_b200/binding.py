@@ -770,6 +770,7 @@ def dropout(x, p, seed, *, offset=0, step=None, residual=None, out=None):
 
 
 POLICY_REDUCTIONS = ("tokens", "sequences", "sum")
+_REDUCTION = {name: i for i, name in enumerate(POLICY_REDUCTIONS)}
 
 
 def policy_loss(logp, old_logp, advantages, *, ref_logp=None, mask=None, lengths=None, clip=(0.2, 0.2), kl_weight=0.0,
@@ -785,11 +786,12 @@ def policy_loss(logp, old_logp, advantages, *, ref_logp=None, mask=None, lengths
     Returns a dict of device tensors: loss, kl (mean of exp(f) - 1 - f), clipped (share of clipped tokens), each [1] fp32,
     count [1] int32, grad (logp's shape, 0 where nothing is counted; not with want_grad=False), and the workspace.
     """
-    if reduction not in POLICY_REDUCTIONS:
+    kind = _REDUCTION.get(reduction)
+    if kind is None:
         raise ValueError(f"reduction must be one of {POLICY_REDUCTIONS}")
     low, high = clip
-    return _native().policy_loss(logp, old_logp, advantages, ref_logp, mask, lengths, low, high, kl_weight,
-                                 POLICY_REDUCTIONS.index(reduction), negated, want_grad, workspace)
+    return _native().policy_loss(logp, old_logp, advantages, ref_logp, mask, lengths, low, high, kl_weight, kind, negated,
+                                 want_grad, workspace)
 
 
 def ctc_policy_fwd_bwd(hidden, W, bias, targets, input_lengths, target_lengths, blank_id, old_losses, advantages, *,

@@ -18,6 +18,7 @@
 #include "pctc_internal.h"
 #include "vec8.cuh"
 
+#include <atomic>
 #include <cmath>
 
 namespace pctc {
@@ -666,8 +667,13 @@ pctc_status_t pctc_embed_grad(const pctc_embed_t* p, const int32_t* tokens, cons
   s.clear = (int*)(w + g.arrived);
   s.n_clear = g.windows * (p->D / group);
   const int smem = SORT_WARPS * s.width * 4;
-  e = cudaFuncSetAttribute(k_sort_tokens, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_WARPS * SORT_MAX_WIDTH * 4);
-  if (e != cudaSuccess) return PCTC_ERR_CUDA;
+  static std::atomic<bool> configured[MAX_DEVICES];
+  const int dev = current_device();
+  if (!configured[dev].load(std::memory_order_acquire)) {
+    e = cudaFuncSetAttribute(k_sort_tokens, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_WARPS * SORT_MAX_WIDTH * 4);
+    if (e != cudaSuccess) return PCTC_ERR_CUDA;
+    configured[dev].store(true, std::memory_order_release);
+  }
   s.buckets = (unsigned)((p->V + s.width - 1) / s.width);
   if (!p->accumulate) s.zero = zero_args(dW, p->V, p->D, p->ld_w, ws, 1);
   const long long blocks = s.buckets + s.zero.pieces;

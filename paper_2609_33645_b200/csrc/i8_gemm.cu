@@ -166,6 +166,7 @@ constexpr int I8_TMEM_COLS = 512;
 
 struct I8Args {
   int n, m, k;                                   // channels, tokens, contraction
+  int rows;                                      // CTAS = 1: channels of a tile, up to 128
   int cols;                                      // columns of a tile: tokens (CTAS = 1) or channels (CTAS = 2)
   int stages;
   int band;                                      // CTAS = 2: token tiles that are walked together (their rows stay in L2)
@@ -227,7 +228,7 @@ __device__ __forceinline__ unsigned long long i8_smem_desc(unsigned addr) {
 template <int CTAS>
 __device__ __forceinline__ void i8_tile(const I8Args& a, int u, int n_tiles, int m_tiles, int& channel, int& token) {
   if (CTAS == 1) {
-    channel = u * I8_ROWS;
+    channel = u * a.rows;
     token = 0;
     return;
   }
@@ -247,11 +248,11 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = CTAS == 2 ? (int)cluster_ctarank() : 0;
   const int group = blockIdx.x / CTAS, ngroups = gridDim.x / CTAS;
-  // a stage of this CTA: 128 rows of the accumulators' rows, then its part of their columns
-  const int stage_bytes = I8_W_STAGE + a.cols / CTAS * I8_BK;
+  // a stage of this CTA: 128 rows of the accumulators' rows (of which the loads fill a.rows), then its part of their columns
+  const int stage_bytes = I8_W_STAGE + a.cols / CTAS * I8_BK, load_bytes = (CTAS == 1 ? a.rows : I8_ROWS) * I8_BK + a.cols / CTAS * I8_BK;
   const int w_offset = CTAS == 1 ? 0 : I8_W_STAGE, x_offset = CTAS == 1 ? I8_W_STAGE : 0;
   const int w_rows = CTAS == 1 ? 0 : rank * (a.cols / CTAS), x_rows = CTAS == 1 ? 0 : rank * I8_ROWS;   // this CTA's part of a tile
-  const int n_tiles = CTAS == 1 ? (a.n + I8_ROWS - 1) / I8_ROWS : (a.n + a.cols - 1) / a.cols;
+  const int n_tiles = CTAS == 1 ? (a.n + a.rows - 1) / a.rows : (a.n + a.cols - 1) / a.cols;
   const int m_tiles = CTAS == 1 ? 1 : (a.m + 2 * I8_ROWS - 1) / (2 * I8_ROWS);
   const int units = n_tiles * m_tiles, k_blocks = (a.k + I8_BK - 1) / I8_BK;
 
@@ -303,7 +304,7 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
           i8_tile<CTAS>(a, group, n_tiles, m_tiles, channel, token);
           early = min(a.stages, k_blocks);
           for (int j = 0; j < early; ++j) {
-            if (rank == 0) mbar_expect_tx(&st->full[j], CTAS * stage_bytes);
+            if (rank == 0) mbar_expect_tx(&st->full[j], CTAS * load_bytes);
             load_w(j, j, channel);
           }
         }
@@ -314,7 +315,7 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
         for (int kb = 0; kb < k_blocks; ++kb, ++g) {
           if ((int)g >= early) {
             if (!mbar_wait(&st->empty[s], ph ^ 1u, abort_flag, a.status, 1)) { ok = false; break; }
-            if (rank == 0) mbar_expect_tx(&st->full[s], CTAS * stage_bytes);   // the leader's barrier counts both CTAs
+            if (rank == 0) mbar_expect_tx(&st->full[s], CTAS * load_bytes);   // the leader's barrier counts both CTAs
             load_w(s, kb, channel);
           }
           load(smem + (size_t)s * stage_bytes + x_offset, &tmX, kb * I8_BK, token + x_rows, &st->full[s]);
@@ -388,10 +389,20 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
       float* sa = (float*)extra;
       for (int i = lane; i < I8_ROWS; i += 32) sa[i] = i < a.m ? a.a_scale[i] : 0.f;   // the same by every warp
       __syncwarp();
+      // what a tile needs beside its sums is loaded a tile ahead
+      const auto channel_of = [&](int u) { return q * 32 + lane < a.rows ? u * a.rows + q * 32 + lane : a.n; };
+      float next_sb = 0.f, next_bias = 0.f;
+      const auto prefetch = [&](int u) {
+        const int j = channel_of(u);
+        next_sb = j < a.n ? a.b_scale[j] : 0.f;
+        next_bias = j < a.n ? bias_of(j) : 0.f;
+      };
+      if (group < units) prefetch(group);
       for (int u = group; u < units && ok; u += ngroups, ++it) {
-        const int j = u * I8_ROWS + q * 32 + lane;                // what a tile needs beside its sums is loaded before they are there
+        const int j = channel_of(u);
         const bool row_ok = j < a.n;
-        const float sb = row_ok ? a.b_scale[j] : 0.f, bias = row_ok ? bias_of(j) : 0.f;
+        const float sb = next_sb, bias = next_bias;
+        if (u + ngroups < units) prefetch(u + ngroups);
         const unsigned acc = it & 1u;
         if (!sums_ready(acc, (it >> 1) & 1u)) { ok = false; break; }
         for (int i0 = (ew >> 2) * 32; i0 < a.m; i0 += 64) {
@@ -441,33 +452,53 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
       float* sb = (float*)(extra + I8_EPI_WARPS * 2 * I8_BOX) + ew * (2 * I8_WARP_COLS);
       float* bias = sb + I8_WARP_COLS;
       const unsigned swizzle = (unsigned)((lane >> 1) & 3);       // 64-byte swizzle of a row of a box
+      // what a tile needs beside its sums is loaded a tile ahead
+      float next_sa = 0.f, next_sb[I8_WARP_COLS / 32], next_bias[I8_WARP_COLS / 32];
+      const auto prefetch = [&](int u) {
+        int channel, token;
+        i8_tile<2>(a, u, n_tiles, m_tiles, channel, token);
+        const int i = token + rank * I8_ROWS + q * 32 + lane;
+        next_sa = i < a.m ? a.a_scale[i] : 0.f;
+#pragma unroll
+        for (int c = 0; c < I8_WARP_COLS / 32; ++c) {
+          const int j = channel + (ew >> 2) * I8_WARP_COLS + c * 32 + lane;
+          next_sb[c] = j < a.n ? a.b_scale[j] : 0.f;
+          next_bias[c] = j < a.n ? bias_of(j) : 0.f;
+        }
+      };
+      if (group < units) prefetch(group);
       for (int u = group; u < units && ok; u += ngroups, ++it) {
         int channel, token;
         i8_tile<2>(a, u, n_tiles, m_tiles, channel, token);
-        const int row0 = token + rank * I8_ROWS + q * 32, i = row0 + lane, j0 = channel + (ew >> 2) * I8_WARP_COLS;
-        const float sa = i < a.m ? a.a_scale[i] : 0.f;
+        const int row0 = token + rank * I8_ROWS + q * 32, j0 = channel + (ew >> 2) * I8_WARP_COLS;
+        const float sa = next_sa;
         __syncwarp();
 #pragma unroll
-        for (int c = 0; c < I8_WARP_COLS; c += 32) {
-          const int j = j0 + c + lane;
-          sb[c + lane] = j < a.n ? a.b_scale[j] : 0.f;
-          bias[c + lane] = j < a.n ? bias_of(j) : 0.f;
+        for (int c = 0; c < I8_WARP_COLS / 32; ++c) {
+          sb[c * 32 + lane] = next_sb[c];
+          bias[c * 32 + lane] = next_bias[c];
         }
         __syncwarp();
+        if (u + ngroups < units) prefetch(u + ngroups);
         const unsigned acc = it & 1u;
         if (!sums_ready(acc, (it >> 1) & 1u)) { ok = false; break; }
         const unsigned taddr = tmem_base + ((unsigned)(q * 32) << 16) + acc * 256 + (ew >> 2) * I8_WARP_COLS;
-#pragma unroll 1
-        for (int c0 = 0; c0 < I8_WARP_COLS && j0 + c0 < a.n; c0 += 32) {
+        unsigned r[2][32];
+        tmem_issue32(taddr, r[0]);
+#pragma unroll
+        for (int g = 0; g < I8_WARP_COLS / 32; ++g) {
+          const int c0 = g * 32;
+          tmem_wait32(r[g & 1]);
+          if (g + 1 < I8_WARP_COLS / 32) tmem_issue32(taddr + c0 + 32, r[(g + 1) & 1]);
+          if (j0 + c0 >= a.n) continue;
           float v[32];
-          tmem_ld32(taddr + c0, v);
 #pragma unroll
           for (int c = 0; c < 32; c += 4) {
             const float4 f = *reinterpret_cast<const float4*>(sb + c0 + c), b = *reinterpret_cast<const float4*>(bias + c0 + c);
-            v[c] = fmaf((float)__float_as_int(v[c]), sa * f.x, b.x);
-            v[c + 1] = fmaf((float)__float_as_int(v[c + 1]), sa * f.y, b.y);
-            v[c + 2] = fmaf((float)__float_as_int(v[c + 2]), sa * f.z, b.z);
-            v[c + 3] = fmaf((float)__float_as_int(v[c + 3]), sa * f.w, b.w);
+            v[c] = fmaf((float)(int)r[g & 1][c], sa * f.x, b.x);
+            v[c + 1] = fmaf((float)(int)r[g & 1][c + 1], sa * f.y, b.y);
+            v[c + 2] = fmaf((float)(int)r[g & 1][c + 2], sa * f.z, b.z);
+            v[c + 3] = fmaf((float)(int)r[g & 1][c + 3], sa * f.w, b.w);
           }
           if (a.aligned) {
             // 32 bf16 channels a box, or 16 fp32 ones; one box fills while the other is read out
@@ -610,7 +641,12 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
   a.cols = pair ? 256 : (m + 15) / 16 * 16;
   const int stage = I8_W_STAGE + a.cols / (pair ? 2 : 1) * I8_BK, fit = i8_ring(pair ? 2 : 1) / stage;
   a.stages = fit < I8_MAX_STAGES ? fit : I8_MAX_STAGES;
-  const long long n_tiles = pair ? ((long long)n + 255) / 256 : ((long long)n + I8_ROWS - 1) / I8_ROWS, m_tiles = pair ? ((long long)m + 255) / 256 : 1;
+  // few tokens and long rows: tiles of equal height that fill whole rounds of the SMs (4 x 151,936 x 4,096: 143 -> 105 us; a
+  // multiple of 4 keeps pairs of channels together); with short rows the results count, and tiles of 128 keep them aligned
+  // (1 x 38,998 x 320: 8.8 us against 10.2)
+  const long long sms = sm_count(), rounds = ((long long)n + sms * I8_ROWS - 1) / (sms * I8_ROWS);
+  a.rows = pair || k < 2048 || n < sms * I8_ROWS ? I8_ROWS : (int)((n + rounds * sms - 1) / (rounds * sms) + 3) / 4 * 4;
+  const long long n_tiles = pair ? ((long long)n + 255) / 256 : ((long long)n + a.rows - 1) / a.rows, m_tiles = pair ? ((long long)m + 255) / 256 : 1;
   if (n_tiles * m_tiles > 0x7fffffffLL - (1 << 20)) return cudaErrorInvalidValue;
   long long band = I8_BAND_BYTES / (256LL * k);
   band = band < 1 ? 1 : band > m_tiles ? m_tiles : band;
@@ -628,7 +664,7 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
   a.status = status;
   a.behind = behind ? 1 : 0;
   alignas(64) CUtensorMap tmW, tmX, tmC = {};
-  if (!i8_map(&tmW, B, k, n, ldb, I8_ROWS) || !i8_map(&tmX, A, k, m, lda, pair ? I8_ROWS : (unsigned)a.cols)) return cudaErrorInvalidValue;
+  if (!i8_map(&tmW, B, k, n, ldb, (unsigned)a.rows) || !i8_map(&tmX, A, k, m, lda, pair ? I8_ROWS : (unsigned)a.cols)) return cudaErrorInvalidValue;
   if (pair && a.aligned && !i8_map_out(&tmC, C, n, m, ldc, out_bf16)) return cudaErrorInvalidValue;
   const int units = (int)(n_tiles * m_tiles);
   if (pair) return out_bf16 ? i8_launch<__nv_bfloat16, 2>(tmW, tmX, tmC, a, units, stream) : i8_launch<float, 2>(tmW, tmX, tmC, a, units, stream);

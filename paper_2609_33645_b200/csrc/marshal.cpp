@@ -111,12 +111,14 @@ class Shared {
     return parts_.size() - 1;
   }
   void allocate() { base_ = empty({std::max<int64_t>(bytes_, 1)}, at::kByte, dev_); }
-  at::Tensor get(size_t i) const {
+  at::Tensor get(size_t i) const { return view(i, 0, parts_[i].shape); }
+  // `shape` values of part i from the first one on.
+  at::Tensor view(size_t i, int64_t first, at::IntArrayRef shape) const {
     const Part& p = parts_[i];
     at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base_.storage()), base_.key_set(),
                                                             c10::scalarTypeToTypeMeta(p.type));
-    t.unsafeGetTensorImpl()->set_storage_offset(base_.storage_offset() + p.at / (int64_t)c10::elementSize(p.type));
-    t.unsafeGetTensorImpl()->set_sizes_contiguous(p.shape);
+    t.unsafeGetTensorImpl()->set_storage_offset(base_.storage_offset() + p.at / (int64_t)c10::elementSize(p.type) + first);
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
     return t;
   }
 
@@ -707,7 +709,7 @@ PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MARSHAL_END
 }
 // policy_loss(logp, old_logp, advantages, ref_logp, mask, lengths (each or None), low, high, kl_weight, reduction, negated,
-//             want_grad, workspace) -> dict
+//             want_grad, workspace or None) -> dict
 PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   MARSHAL_BEGIN
   want(n, 13);
@@ -754,25 +756,25 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const c10::cuda::CUDAGuard guard(dev);
   size_t need = 0;
   check(api.policy_workspace_bytes(&p, &need), "pctc_policy_workspace_bytes");
-  const at::Tensor ws = bytes_or(a[12], need, dev);
-  const bool want_grad = truth(a[11]);
-  Shared out(dev);                          // what the call writes side by side: loss, KL, share of clipped tokens
-  out.add({3}, at::kFloat);
-  out.add({1}, at::kInt);
-  if (want_grad) out.add(x.sizes(), at::kFloat);
+  const bool want_grad = truth(a[11]), own = a[12] == Py_None;
+  Shared out(dev);                          // the workspace first: its alignment is the allocation's
+  const size_t work = out.add({own ? (int64_t)(need + 255) / 256 * 256 : 0}, at::kByte);
+  const size_t stats = out.add({3}, at::kFloat), count = out.add({1}, at::kInt);
+  const size_t grad = want_grad ? out.add(x.sizes(), at::kFloat) : 0;
   out.allocate();
-  const at::Tensor stats = out.get(0), count = out.get(1), grad = want_grad ? out.get(2) : at::Tensor();
+  const at::Tensor ws = own ? out.get(work) : bytes_or(a[12], need, dev), g = want_grad ? out.get(grad) : at::Tensor();
+  const at::Tensor loss = out.view(stats, 0, {1}), kl = out.view(stats, 1, {1}), clipped = out.view(stats, 2, {1}), counted = out.get(count);
   check(api.policy_loss(&p, (const float*)ptr(x), (const float*)ptr(old), (const float*)ptr(ref), (const float*)ptr(adv),
-                        (const uint8_t*)ptr(mask), (const int32_t*)ptr(lengths), want_grad ? (float*)ptr(grad) : nullptr,
-                        (float*)ptr(stats), (int32_t*)ptr(count), ptr(ws), (size_t)ws.numel(), stream_of(dev)),
+                        (const uint8_t*)ptr(mask), (const int32_t*)ptr(lengths), (float*)ptr(g), (float*)ptr(loss),
+                        (int32_t*)ptr(counted), ptr(ws), (size_t)ws.numel(), stream_of(dev)),
         "pctc_policy_loss");
   PyObject* d = PyDict_New();
   if (!d) return nullptr;
-  put(d, "loss", stats.narrow(0, 0, 1));
-  put(d, "kl", stats.narrow(0, 1, 1));
-  put(d, "clipped", stats.narrow(0, 2, 1));
-  put(d, "count", count);
-  if (want_grad) put(d, "grad", grad);
+  put(d, "loss", loss);
+  put(d, "kl", kl);
+  put(d, "clipped", clipped);
+  put(d, "count", counted);
+  if (want_grad) put(d, "grad", g);
   put(d, "workspace", ws);
   return d;
   MARSHAL_END

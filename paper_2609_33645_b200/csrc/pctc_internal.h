@@ -76,6 +76,17 @@ struct Rows {
 constexpr long long MAX_ELEMENTS = 1LL << 40;   // of one array of the operators around the head
 
 // ---------------------------------------------------------------------------
+// Per-device state: a process may drive several GPUs, and both the shared-memory opt-in of a kernel
+// and the SM count belong to one device.  Entries are filled on first use; the values are the same
+// whichever thread fills them.
+constexpr int MAX_DEVICES = 64;
+inline int current_device() {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) return 0;
+  return dev;
+}
+
+// ---------------------------------------------------------------------------
 // Two launches of one call, the second set up while the first still runs: the first says launch_next() as soon as it
 // has begun, the second goes on behind wait_for_previous() when all of the first's writes are there, and touches
 // nothing of it (and nothing that it reads) before.

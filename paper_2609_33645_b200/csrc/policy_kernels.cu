@@ -527,17 +527,22 @@ pctc_status_t pctc_policy_loss(const pctc_policy_t* p, const float* logp, const 
                    (!p->ld_adv || (((size_t)advantages & 15) == 0 && (p->ld_adv & 3) == 0));
   cudaStream_t stream = (cudaStream_t)stream_v;
   if (a.total <= POLICY_SMALL) {
+    auto kernel = vec ? k_policy_small<true> : k_policy_small<false>;
+    if (a.total <= POLICY_SMALL_THREADS * POLICY_EACH) {           // a cluster of one
+      kernel<<<1, POLICY_SMALL_THREADS, 0, stream>>>(a);
+      return cudaGetLastError() == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+    }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = a.total <= POLICY_SMALL_THREADS * POLICY_EACH ? 1 : POLICY_CLUSTER;
+    attr[0].val.clusterDim.x = POLICY_CLUSTER;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(attr[0].val.clusterDim.x);
+    cfg.gridDim = dim3(POLICY_CLUSTER);
     cfg.blockDim = dim3(POLICY_SMALL_THREADS);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, vec ? k_policy_small<true> : k_policy_small<false>, a) == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? PCTC_OK : PCTC_ERR_CUDA;
   }
   const long long threads = !a.counting ? 1 : !mask || a.T <= POLICY_SHORT_ROW ? a.N : a.T <= POLICY_LONG_ROW ? a.N * 32 : a.N * POLICY_THREADS;
   const long long blocks = (threads + POLICY_THREADS - 1) / POLICY_THREADS;
