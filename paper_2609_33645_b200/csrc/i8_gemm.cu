@@ -2,8 +2,10 @@
 //   s = max|x| / 127,   q = round(x * (127 / max|x|)).
 // Sums are whole numbers of 32 bits (exact for k < 2^17); nothing is rounded before the scales.
 //
-// k_i8_gemm is a persistent tcgen05 kernel (kind::i8) in two forms; roles, ring and bounded waits are those of the bf16
+// k_i8_gemm is a persistent tcgen05 kernel (kind::i8) in three forms; roles, ring and bounded waits are those of the bf16
 // kernel in umma_gemm.cu.
+//   very few tokens (up to 8,192 values): as below, and every CTA quantizes the tokens itself, into the operand's place in
+//     shared memory, while its first ring of the head is on its way: one launch.
 //   few tokens (up to 128), CTAS = 1: the rows of the accumulators are channels (rows of the head), the columns tokens, tiles
 //     128 x 16 .. 128 x 128: the head streams once through a deep ring, and 32 lanes of a warp hold 32 neighbouring
 //     channels of a token, which is the order of C.  Bound by HBM.
@@ -163,6 +165,8 @@ constexpr int I8_EPI_WARPS = 8;
 constexpr int I8_THREADS = 64 + 32 * I8_EPI_WARPS;
 constexpr int I8_MAX_STAGES = 12;
 constexpr int I8_TMEM_COLS = 512;
+constexpr int I8_OWN_VALUES = 8192;              // up to so many values of tokens are quantized by the product itself
+                                                 // (4 x 151,936 x 1,024: 33.2 -> 31.5 us; 16 x 1,024 values: 32.8 -> 35.2)
 
 struct I8Args {
   int n, m, k;                                   // channels, tokens, contraction
@@ -179,6 +183,9 @@ struct I8Args {
   int aligned;                                   // CTAS = 1: two neighbouring bf16 channels can be stored as one word;
                                                  // CTAS = 2: rows of C can be stored by TMA
   int behind;                                    // the launch before this one makes the tokens (and nothing else that is read here)
+  const void* x;                                 // tokens that are quantized here [m, k] (then there is no a_scale)
+  long long ld_x;
+  int wide_x;                                    // ... whose rows can be read in groups of eight
   int* status;
 };
 
@@ -195,6 +202,7 @@ struct I8Tail {
   unsigned long long done;
   unsigned tmem_base;
   int abort;
+  unsigned tops[I8_ROWS];                        // tokens quantized here: the largest magnitude of each
 };
 constexpr int i8_smem(int ctas) { return 1024 + i8_ring(ctas) + i8_extra(ctas) + (int)sizeof(I8Tail); }
 static_assert(i8_smem(1) <= 227 * 1024 && i8_smem(2) <= 227 * 1024, "shared memory budget");
@@ -237,24 +245,106 @@ __device__ __forceinline__ void i8_tile(const I8Args& a, int u, int n_tiles, int
   token = (b * a.band + (r - nt * rows)) * (2 * I8_ROWS);
 }
 
-template <typename T, int CTAS>
+// The tokens in 8 bits as the tensor core reads them (blocks of 128 k, rows of 128 bytes with the 128-byte swizzle), and
+// their scales.  A thread takes groups of eight values, whatever row they are in; they are loaded before anything else of the
+// kernel, since behind the first loads of the head they would wait for microseconds.  Rows and k past the last are left as
+// they are: their products are not looked at, or zero.
+template <typename X>
+struct OwnTokens {
+  static constexpr int MOST = (I8_OWN_VALUES / 8 + I8_THREADS - 1) / I8_THREADS;
+  Vec8<X> v[MOST];
+
+  __device__ __forceinline__ void load(const I8Args& a) {
+    if (!a.wide_x) return;
+    const unsigned per = a.k / 8, groups = per * a.m;
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) {
+      const unsigned g = threadIdx.x + i * I8_THREADS, row = g / per;
+      if (g < groups) v[i].load((const X*)a.x + row * a.ld_x + (g - row * per) * 8);
+    }
+  }
+  // tops: zeros [m]; all threads of the block
+  __device__ __forceinline__ void store(const I8Args& a, unsigned char* tokens, unsigned* tops, float* scales) const {
+    const unsigned per = a.wide_x ? a.k / 8 : a.k, groups = per * a.m;
+    const auto place = [&](unsigned row, unsigned c) {
+      return tokens + (c >> 7) * a.cols * I8_BK + row * I8_BK + (((c >> 4 & 7) ^ (row & 7)) << 4) + (c & 15);
+    };
+    if (a.wide_x) {
+#pragma unroll
+      for (int i = 0; i < MOST; ++i) {
+        const unsigned g = threadIdx.x + i * I8_THREADS;
+        if (g >= groups) continue;
+        float x[8];
+        v[i].get(x);
+        unsigned top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, magnitude(x[j]));
+        atomicMax(&tops[g / per], top);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < MOST; ++i) {
+        const unsigned g = threadIdx.x + i * I8_THREADS, row = g / per;
+        if (g >= groups) continue;
+        float x[8], scale;
+        v[i].get(x);
+        const float f = row_factor(tops[row], scale);
+        unsigned w[2] = {0u, 0u};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j >> 2] |= ((unsigned)quantize_one(x[j], f) & 0xffu) << (8 * (j & 3));
+        *reinterpret_cast<uint2*>(place(row, (g - row * per) * 8)) = make_uint2(w[0], w[1]);
+        if (g == row * per) scales[row] = scale;
+      }
+    } else {
+#pragma unroll 4
+      for (unsigned g = threadIdx.x; g < groups; g += I8_THREADS) {
+        const unsigned row = g / per;
+        atomicMax(&tops[row], magnitude(to_float(((const X*)a.x)[row * a.ld_x + (g - row * per)])));
+      }
+      __syncthreads();
+#pragma unroll 4
+      for (unsigned g = threadIdx.x; g < groups; g += I8_THREADS) {
+        const unsigned row = g / per, c = g - row * per;
+        float scale;
+        const float f = row_factor(tops[row], scale);
+        *place(row, c) = (unsigned char)quantize_one(to_float(((const X*)a.x)[row * a.ld_x + c]), f);
+        if (c == 0) scales[row] = scale;
+      }
+    }
+  }
+};
+struct NoTokens {};
+
+template <typename T, int CTAS, typename X>
 __global__ void __launch_bounds__(I8_THREADS, 1)
 k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmC,
           const I8Args a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((size_t)smem_raw + 1023) & ~(size_t)1023);
+  constexpr bool OWN = !std::is_void<X>::value;  // this kernel quantizes the tokens (CTAS = 1); they lie in front of the ring
   unsigned char* extra = smem + i8_ring(CTAS);
   I8Tail* st = (I8Tail*)(extra + i8_extra(CTAS));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = CTAS == 2 ? (int)cluster_ctarank() : 0;
   const int group = blockIdx.x / CTAS, ngroups = gridDim.x / CTAS;
   // a stage of this CTA: 128 rows of the accumulators' rows (of which the loads fill a.rows), then its part of their columns
-  const int stage_bytes = I8_W_STAGE + a.cols / CTAS * I8_BK, load_bytes = (CTAS == 1 ? a.rows : I8_ROWS) * I8_BK + a.cols / CTAS * I8_BK;
+  const int x_stage = OWN ? 0 : a.cols / CTAS * I8_BK, stage_bytes = I8_W_STAGE + x_stage;
+  const int load_bytes = (CTAS == 1 ? a.rows : I8_ROWS) * I8_BK + x_stage;
   const int w_offset = CTAS == 1 ? 0 : I8_W_STAGE, x_offset = CTAS == 1 ? I8_W_STAGE : 0;
   const int w_rows = CTAS == 1 ? 0 : rank * (a.cols / CTAS), x_rows = CTAS == 1 ? 0 : rank * I8_ROWS;   // this CTA's part of a tile
   const int n_tiles = CTAS == 1 ? (a.n + a.rows - 1) / a.rows : (a.n + a.cols - 1) / a.cols;
   const int m_tiles = CTAS == 1 ? 1 : (a.m + 2 * I8_ROWS - 1) / (2 * I8_ROWS);
   const int units = n_tiles * m_tiles, k_blocks = (a.k + I8_BK - 1) / I8_BK;
+  unsigned char* tokens = smem;
+  typename std::conditional<OWN, OwnTokens<X>, NoTokens>::type own;
+  if constexpr (OWN) {
+    smem += k_blocks * a.cols * I8_BK;
+    own.load(a);
+    if (threadIdx.x < I8_ROWS) {
+      ((float*)extra)[threadIdx.x] = 0.f;        // the scales,
+      st->tops[threadIdx.x] = 0;                 // and the largest magnitudes
+    }
+  }
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < a.stages; ++s) { mbar_init(&st->full[s], 1); mbar_init(&st->empty[s], 1); }
@@ -284,6 +374,30 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
   const unsigned tmem_base = st->tmem_base;
   volatile int* abort_flag = &st->abort;
 
+  // the head does not depend on the tokens: what the first ring takes of it is under way before these are there
+  int early = 0;
+  if ((OWN || a.behind) && group < units) {
+    early = min(a.stages, k_blocks);
+    if (warp == 0 && lane == 0) {
+      int channel, token;
+      i8_tile<CTAS>(a, group, n_tiles, m_tiles, channel, token);
+      for (int j = 0; j < early; ++j) {
+        if (rank == 0) mbar_expect_tx(&st->full[j], CTAS * load_bytes);
+        unsigned char* dst = smem + (size_t)j * stage_bytes + w_offset;
+        if (CTAS == 2) tma_load_2d_pair(dst, &tmW, j * I8_BK, channel + w_rows, &st->full[j]);
+        else tma_load_2d(dst, &tmW, j * I8_BK, channel + w_rows, &st->full[j]);
+      }
+    }
+    __syncwarp();
+  }
+  if constexpr (OWN) {
+    // nobody gives up a wait within two seconds, so that this comes before whatever is reported
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = 0;
+    own.store(a, tokens, st->tops, (float*)extra);
+    fence_async_smem();                  // the tensor core reads what was stored here
+    __syncthreads();
+  }
+
   if (warp == 0) {
     // ===================== TMA producer =====================
     if (lane == 0) {
@@ -297,19 +411,8 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
       const auto load_w = [&](int stage, int kb, int channel) {
         load(smem + (size_t)stage * stage_bytes + w_offset, &tmW, kb * I8_BK, channel + w_rows, &st->full[stage]);
       };
-      // the head does not depend on the launch before: what the first ring of it takes is under way before that ends
-      int early = 0, channel, token;
-      if (a.behind) {
-        if (group < units) {
-          i8_tile<CTAS>(a, group, n_tiles, m_tiles, channel, token);
-          early = min(a.stages, k_blocks);
-          for (int j = 0; j < early; ++j) {
-            if (rank == 0) mbar_expect_tx(&st->full[j], CTAS * load_bytes);
-            load_w(j, j, channel);
-          }
-        }
-        wait_for_previous();
-      }
+      int channel, token;
+      if (a.behind) wait_for_previous();
       for (int u = group; u < units && ok; u += ngroups) {
         i8_tile<CTAS>(a, u, n_tiles, m_tiles, channel, token);
         for (int kb = 0; kb < k_blocks; ++kb, ++g) {
@@ -318,7 +421,7 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
             if (rank == 0) mbar_expect_tx(&st->full[s], CTAS * load_bytes);   // the leader's barrier counts both CTAs
             load_w(s, kb, channel);
           }
-          load(smem + (size_t)s * stage_bytes + x_offset, &tmX, kb * I8_BK, token + x_rows, &st->full[s]);
+          if (!OWN) load(smem + (size_t)s * stage_bytes + x_offset, &tmX, kb * I8_BK, token + x_rows, &st->full[s]);
           if (++s == a.stages) { s = 0; ph ^= 1u; }
         }
       }
@@ -347,7 +450,8 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
           if (!mbar_wait(&st->full[s], ph, abort_flag, a.status, 3)) { ok = false; break; }
           tc_fence_after();
           const unsigned at = smem_u32(smem + (size_t)s * stage_bytes);
-          const unsigned long long rdesc = i8_smem_desc(at), cdesc = i8_smem_desc(at + I8_W_STAGE);
+          const unsigned long long rdesc = i8_smem_desc(at);
+          const unsigned long long cdesc = i8_smem_desc(OWN ? smem_u32(tokens) + kb * a.cols * I8_BK : at + I8_W_STAGE);
 #pragma unroll
           for (int kk = 0; kk < I8_BK / 32; ++kk) {               // 32 k an instruction: 32 bytes further on
             const unsigned more = (kb != 0 || kk != 0) ? 1u : 0u;
@@ -387,8 +491,10 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
     if constexpr (CTAS == 1) {
       // a lane is a channel; the columns are all tokens there are, in groups of 32 that the two warps take in turn
       float* sa = (float*)extra;
-      for (int i = lane; i < I8_ROWS; i += 32) sa[i] = i < a.m ? a.a_scale[i] : 0.f;   // the same by every warp
-      __syncwarp();
+      if (!OWN) {
+        for (int i = lane; i < I8_ROWS; i += 32) sa[i] = i < a.m ? a.a_scale[i] : 0.f;   // the same by every warp
+        __syncwarp();
+      }
       // what a tile needs beside its sums is loaded a tile ahead
       const auto channel_of = [&](int u) { return q * 32 + lane < a.rows ? u * a.rows + q * 32 + lane : a.n; };
       float next_sb = 0.f, next_bias = 0.f;
@@ -406,42 +512,42 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
         const unsigned acc = it & 1u;
         if (!sums_ready(acc, (it >> 1) & 1u)) { ok = false; break; }
         for (int i0 = (ew >> 2) * 32; i0 < a.m; i0 += 64) {
-          const int cnt = min(32, a.m - i0);
           float v[32];
           tmem_ld32(tmem_base + ((unsigned)(q * 32) << 16) + acc * 256 + i0, v);
+          T* to = C + (long long)i0 * a.ldc + j;
+          // lanes 2l and 2l + 1 hold neighbouring channels: of bf16 the even one stores both of token c, the odd one of token c + 1
+          const bool odd = lane & 1, pairs = sizeof(T) == 2 && a.aligned && __all_sync(0xffffffffu, !row_ok || (j | 1) < a.n);
+          const unsigned pick = odd ? 0x3276u : 0x5410u;
 #pragma unroll
-          for (int c = 0; c < 32; c += 4) {
-            const float4 f = *reinterpret_cast<const float4*>(sa + i0 + c);
-            v[c] = fmaf((float)__float_as_int(v[c]), f.x * sb, bias);
-            v[c + 1] = fmaf((float)__float_as_int(v[c + 1]), f.y * sb, bias);
-            v[c + 2] = fmaf((float)__float_as_int(v[c + 2]), f.z * sb, bias);
-            v[c + 3] = fmaf((float)__float_as_int(v[c + 3]), f.w * sb, bias);
-          }
-          if constexpr (sizeof(T) == 4) {
-            if (row_ok) {
-              T* to = C + (long long)i0 * a.ldc + j;
+          for (int b = 0; b < 32; b += 8) {
+            const int cnt = min(8, a.m - i0 - b);                 // tokens of this eighth
+            if (cnt <= 0) break;
 #pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (c < cnt) to[c * a.ldc] = v[c];
+            for (int c = b; c < b + 8; c += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(sa + i0 + c);
+              v[c] = fmaf((float)__float_as_int(v[c]), f.x * sb, bias);
+              v[c + 1] = fmaf((float)__float_as_int(v[c + 1]), f.y * sb, bias);
+              v[c + 2] = fmaf((float)__float_as_int(v[c + 2]), f.z * sb, bias);
+              v[c + 3] = fmaf((float)__float_as_int(v[c + 3]), f.w * sb, bias);
             }
-          } else {
-            // lanes 2l and 2l + 1 hold neighbouring channels: the even one stores both of token c, the odd one of token c + 1
-            const bool odd = lane & 1, both = (j | 1) < a.n && a.aligned;
-            T* to = C + (long long)(i0 + (odd ? 1 : 0)) * a.ldc + (j & ~1);
+            T* at = to + (long long)b * a.ldc;
+            if constexpr (sizeof(T) == 2) {
+              if (pairs) {
+                at += odd ? a.ldc - 1 : 0;
 #pragma unroll
-            for (int c = 0; c < 32; c += 2) {
-              const __nv_bfloat162 p = __floats2bfloat162_rn(v[c], v[c + 1]);
-              const unsigned mine = *reinterpret_cast<const unsigned*>(&p);
-              const unsigned other = __shfl_xor_sync(0xffffffffu, mine, 1);
-              if (both) {
-                const unsigned w = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
-                if (c + (odd ? 1 : 0) < cnt) *reinterpret_cast<unsigned*>(to + c * a.ldc) = w;
-              } else if (row_ok) {
-                T* one = C + (long long)(i0 + c) * a.ldc + j;
-                if (c < cnt) one[0] = p.x;
-                if (c + 1 < cnt) one[a.ldc] = p.y;
+                for (int c = 0; c < 8; c += 2, at += 2 * a.ldc) {
+                  const __nv_bfloat162 p = __floats2bfloat162_rn(v[b + c], v[b + c + 1]);
+                  const unsigned mine = *reinterpret_cast<const unsigned*>(&p);
+                  const unsigned w = __byte_perm(mine, __shfl_xor_sync(0xffffffffu, mine, 1), pick);
+                  if (row_ok && c + (odd ? 1 : 0) < cnt) *reinterpret_cast<unsigned*>(at) = w;
+                }
+                continue;
               }
             }
+            if (row_ok)
+#pragma unroll
+              for (int c = 0; c < 8; ++c, at += a.ldc)
+                if (c < cnt) *at = from_float<T>(v[b + c]);
           }
         }
         sums_read(acc);
@@ -592,10 +698,10 @@ bool i8_map(CUtensorMap* map, const void* base, long long k, long long rows, lon
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int CTAS>
+template <typename T, int CTAS, typename X>
 cudaError_t i8_launch(const CUtensorMap& tmW, const CUtensorMap& tmX, const CUtensorMap& tmC, const I8Args& a, int units, cudaStream_t stream) {
   static std::atomic<int> groups_on[MAX_DEVICES];       // CTA groups that can be resident at once; 0: not configured there yet
-  auto kern = k_i8_gemm<T, CTAS>;
+  auto kern = k_i8_gemm<T, CTAS, X>;
   const int dev = current_device();
   int most = groups_on[dev].load(std::memory_order_acquire);
   if (most == 0) {
@@ -632,14 +738,15 @@ constexpr long long I8_BAND_BYTES = 32LL << 20;         // token rows of a band:
 
 cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, const signed char* B, long long ldb,
                     const float* b_scale, const void* bias, bool bias_bf16, int m, int n, int k, void* C, long long ldc,
-                    bool out_bf16, int* status, bool behind, cudaStream_t stream) {
+                    bool out_bf16, int* status, bool behind, cudaStream_t stream, const void* x, long long ld_x, bool x_bf16) {
   if (m <= 0 || n <= 0) return cudaSuccess;
   // up to 128 tokens: tiles as wide as the tokens, so that the head is read once and the ring is deep
   const bool pair = m > I8_ROWS;
   I8Args a = {};
   a.n = n; a.m = m; a.k = k;
   a.cols = pair ? 256 : (m + 15) / 16 * 16;
-  const int stage = I8_W_STAGE + a.cols / (pair ? 2 : 1) * I8_BK, fit = i8_ring(pair ? 2 : 1) / stage;
+  const int blocks = (k + I8_BK - 1) / I8_BK, stage = I8_W_STAGE + (x ? 0 : a.cols / (pair ? 2 : 1) * I8_BK);
+  const int fit = (i8_ring(pair ? 2 : 1) - (x ? blocks * a.cols * I8_BK : 0)) / stage;
   a.stages = fit < I8_MAX_STAGES ? fit : I8_MAX_STAGES;
   // few tokens and long rows: tiles of equal height that fill whole rounds of the SMs (4 x 151,936 x 4,096: 143 -> 105 us; a
   // multiple of 4 keeps pairs of channels together); with short rows the results count, and tiles of 128 keep them aligned
@@ -663,13 +770,25 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
   a.aligned = pair ? ((size_t)C & 15) == 0 && ldc * es % 16 == 0 && (long long)n * es % 16 == 0 : ((size_t)C & 3) == 0 && ldc % 2 == 0;
   a.status = status;
   a.behind = behind ? 1 : 0;
-  alignas(64) CUtensorMap tmW, tmX, tmC = {};
-  if (!i8_map(&tmW, B, k, n, ldb, (unsigned)a.rows) || !i8_map(&tmX, A, k, m, lda, pair ? I8_ROWS : (unsigned)a.cols)) return cudaErrorInvalidValue;
+  a.x = x;
+  a.ld_x = ld_x;
+  a.wide_x = k % 8 == 0 && ((size_t)x & 15) == 0 && ld_x * (x_bf16 ? 2 : 4) % 16 == 0;
+  alignas(64) CUtensorMap tmW, tmX = {}, tmC = {};
+  if (!i8_map(&tmW, B, k, n, ldb, (unsigned)a.rows)) return cudaErrorInvalidValue;
+  if (!x && !i8_map(&tmX, A, k, m, lda, pair ? I8_ROWS : (unsigned)a.cols)) return cudaErrorInvalidValue;
   if (pair && a.aligned && !i8_map_out(&tmC, C, n, m, ldc, out_bf16)) return cudaErrorInvalidValue;
   const int units = (int)(n_tiles * m_tiles);
-  if (pair) return out_bf16 ? i8_launch<__nv_bfloat16, 2>(tmW, tmX, tmC, a, units, stream) : i8_launch<float, 2>(tmW, tmX, tmC, a, units, stream);
-  return out_bf16 ? i8_launch<__nv_bfloat16, 1>(tmW, tmX, tmC, a, units, stream) : i8_launch<float, 1>(tmW, tmX, tmC, a, units, stream);
+  const auto launch = [&](auto out) {
+    using T = decltype(out);
+    if (pair) return i8_launch<T, 2, void>(tmW, tmX, tmC, a, units, stream);
+    if (!x) return i8_launch<T, 1, void>(tmW, tmX, tmC, a, units, stream);
+    return x_bf16 ? i8_launch<T, 1, __nv_bfloat16>(tmW, tmX, tmC, a, units, stream) : i8_launch<T, 1, float>(tmW, tmX, tmC, a, units, stream);
+  };
+  return out_bf16 ? launch(__nv_bfloat16()) : launch(float());
 }
+
+// Whether the product quantizes so many tokens itself: they fit beside a ring of 100 KB and more.
+bool i8_own_tokens(int m, int k) { return (long long)m * k <= I8_OWN_VALUES && (long long)(m + 15) / 16 * 16 * ((k + 127) / 128 * 128) <= 98304; }
 
 cudaError_t i8_quantize(const void* x, bool bf16, long long rows, long long cols, long long ld_x, signed char* q, long long ld_q,
                         float* scales, int* clear, cudaStream_t stream) {
@@ -748,7 +867,7 @@ pctc_status_t pctc_i8_matmul(const pctc_i8_t* p, const int8_t* A, const float* a
   if (!umma_available()) return PCTC_ERR_CUDA;
   const cudaError_t e = i8_gemm((const signed char*)A, p->lda, a_scales, (const signed char*)B, p->ldb, b_scales, bias,
                                 p->bias_dtype == PCTC_BF16, p->m, p->n, p->k, C, p->ldc, p->out_dtype == PCTC_BF16, device_status, false,
-                                (cudaStream_t)stream_v);
+                                (cudaStream_t)stream_v, nullptr, 0, false);
   return e == cudaSuccess ? PCTC_OK : e == cudaErrorInvalidValue ? PCTC_ERR_UNSUPPORTED : PCTC_ERR_CUDA;
 }
 
@@ -783,9 +902,11 @@ pctc_status_t pctc_i8_logits(const pctc_i8_t* p, const void* x, int32_t x_dtype,
   signed char* q = (signed char*)(ws + w.q);
   float* scales = (float*)(ws + w.scales);
   cudaStream_t stream = (cudaStream_t)stream_v;
-  if (i8_quantize(x, x_dtype == PCTC_BF16, p->m, p->k, p->lda, q, w.ld, scales, (int*)ws, stream) != cudaSuccess) return PCTC_ERR_CUDA;
+  const bool fused = i8_own_tokens(p->m, p->k);
+  if (!fused && i8_quantize(x, x_dtype == PCTC_BF16, p->m, p->k, p->lda, q, w.ld, scales, (int*)ws, stream) != cudaSuccess) return PCTC_ERR_CUDA;
   const cudaError_t e = i8_gemm(q, w.ld, scales, (const signed char*)B, p->ldb, b_scales, bias, p->bias_dtype == PCTC_BF16, p->m, p->n,
-                                p->k, C, p->ldc, p->out_dtype == PCTC_BF16, (int*)ws, true, stream);
+                                p->k, C, p->ldc, p->out_dtype == PCTC_BF16, (int*)ws, !fused, stream, fused ? x : nullptr, p->lda,
+                                x_dtype == PCTC_BF16);
   return e == cudaSuccess ? PCTC_OK : e == cudaErrorInvalidValue ? PCTC_ERR_UNSUPPORTED : PCTC_ERR_CUDA;
 }
 
