@@ -189,11 +189,13 @@ struct I8Args {
   int* status;
 };
 
-// Shared memory behind the ring: CTAS = 1: the tokens' scales; CTAS = 2: of every epilogue warp two boxes of 32 rows x 64 bytes on
-// their way out (64-byte swizzle), and the scales and biases of its channels.
-constexpr int I8_BOX = 2048, I8_WARP_COLS = 128;
-constexpr int i8_ring(int ctas) { return ctas == 2 ? 5 * 2 * I8_ROWS * I8_BK : 216 * 1024; }
-constexpr int i8_extra(int ctas) { return ctas == 2 ? I8_EPI_WARPS * (2 * I8_BOX + I8_WARP_COLS * 8) : I8_ROWS * 4; }
+// Shared memory behind the ring: CTAS = 1: the tokens' scales; CTAS = 2: the scales and biases of every epilogue warp's channels,
+// and its results on their way out: two boxes of 32 rows x 64 bytes (64-byte swizzle) for TMA, or, where rows of C are not
+// 16-byte aligned, 32 rows of 256 bytes each as far from a 16-byte boundary as they will be in C (a stage of the ring less).
+constexpr int I8_BOX = 2048, I8_WARP_COLS = 128, I8_ROW_BYTES = 256, I8_ROW_PITCH = I8_ROW_BYTES + 16;
+constexpr int i8_ring(int ctas, bool aligned) { return ctas == 2 ? (aligned ? 5 : 4) * 2 * I8_ROWS * I8_BK : 216 * 1024; }
+constexpr int i8_out(bool aligned) { return aligned ? 2 * I8_BOX : 32 * I8_ROW_PITCH; }
+constexpr int i8_extra(int ctas, bool aligned) { return ctas == 2 ? I8_EPI_WARPS * (i8_out(aligned) + I8_WARP_COLS * 8) : I8_ROWS * 4; }
 struct I8Tail {
   unsigned long long full[I8_MAX_STAGES];
   unsigned long long empty[I8_MAX_STAGES];
@@ -204,7 +206,10 @@ struct I8Tail {
   int abort;
   unsigned tops[I8_ROWS];                        // tokens quantized here: the largest magnitude of each
 };
-constexpr int i8_smem(int ctas) { return 1024 + i8_ring(ctas) + i8_extra(ctas) + (int)sizeof(I8Tail); }
+constexpr int i8_smem(int ctas) {
+  const int more = i8_ring(ctas, true) + i8_extra(ctas, true), less = i8_ring(ctas, false) + i8_extra(ctas, false);
+  return 1024 + (more > less ? more : less) + (int)sizeof(I8Tail);
+}
 static_assert(i8_smem(1) <= 227 * 1024 && i8_smem(2) <= 227 * 1024, "shared memory budget");
 
 __device__ __forceinline__ void tc_mma_i8_pair(unsigned tmem_d, unsigned long long adesc, unsigned long long bdesc,
@@ -315,6 +320,34 @@ struct OwnTokens {
 };
 struct NoTokens {};
 
+// 32 rows of 256 bytes from `stage` to `to` (rows `pitch` bytes apart, `rows` of them there): whole 16-byte pieces by half a
+// warp a row, then the pieces at both ends, a row a lane.
+__device__ __forceinline__ void store_rows(const unsigned char* stage, unsigned char* to, long long pitch, int rows, int lane) {
+  const unsigned c = lane & 15;
+  unsigned char* row = to + (lane >> 4) * pitch;
+#pragma unroll 8
+  for (int i = 0; i < 16; ++i, row += 2 * pitch) {
+    const unsigned a = (unsigned)(size_t)row & 15u;
+    const int r = 2 * i + (lane >> 4);
+    if (r < rows && (c > 0 || a == 0))
+      *reinterpret_cast<uint4*>(row - a + c * 16) = *reinterpret_cast<const uint4*>(stage + r * I8_ROW_PITCH + c * 16);
+  }
+  if (lane < rows) {
+    row = to + lane * pitch;
+    const unsigned a = (unsigned)(size_t)row & 15u;
+    const unsigned char* from = stage + lane * I8_ROW_PITCH;
+    row -= a;
+    unsigned x = a;
+    if (x & 2) { *reinterpret_cast<unsigned short*>(row + x) = *reinterpret_cast<const unsigned short*>(from + x); x += 2; }
+    if (x & 4) { *reinterpret_cast<unsigned*>(row + x) = *reinterpret_cast<const unsigned*>(from + x); x += 4; }
+    if (x & 8) *reinterpret_cast<uint2*>(row + x) = *reinterpret_cast<const uint2*>(from + x);
+    x = I8_ROW_BYTES;
+    if (a & 8) { *reinterpret_cast<uint2*>(row + x) = *reinterpret_cast<const uint2*>(from + x); x += 8; }
+    if (a & 4) { *reinterpret_cast<unsigned*>(row + x) = *reinterpret_cast<const unsigned*>(from + x); x += 4; }
+    if (a & 2) *reinterpret_cast<unsigned short*>(row + x) = *reinterpret_cast<const unsigned short*>(from + x);
+  }
+}
+
 template <typename T, int CTAS, typename X>
 __global__ void __launch_bounds__(I8_THREADS, 1)
 k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmC,
@@ -322,8 +355,9 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((size_t)smem_raw + 1023) & ~(size_t)1023);
   constexpr bool OWN = !std::is_void<X>::value;  // this kernel quantizes the tokens (CTAS = 1); they lie in front of the ring
-  unsigned char* extra = smem + i8_ring(CTAS);
-  I8Tail* st = (I8Tail*)(extra + i8_extra(CTAS));
+  const bool boxes_out = CTAS == 1 || a.aligned;
+  unsigned char* extra = smem + (boxes_out ? i8_ring(CTAS, true) : i8_ring(CTAS, false));
+  I8Tail* st = (I8Tail*)(extra + (boxes_out ? i8_extra(CTAS, true) : i8_extra(CTAS, false)));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = CTAS == 2 ? (int)cluster_ctarank() : 0;
   const int group = blockIdx.x / CTAS, ngroups = gridDim.x / CTAS;
@@ -376,16 +410,18 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
 
   // the head does not depend on the tokens: what the first ring takes of it is under way before these are there
   int early = 0;
-  if ((OWN || a.behind) && group < units) {
-    early = min(a.stages, k_blocks);
+  if (OWN || a.behind) {
+    const int mine = group < units ? (units - 1 - group) / ngroups + 1 : 0;      // tiles of this CTA (pair)
+    early = (long long)mine * k_blocks < a.stages ? mine * k_blocks : a.stages;
     if (warp == 0 && lane == 0) {
-      int channel, token;
-      i8_tile<CTAS>(a, group, n_tiles, m_tiles, channel, token);
-      for (int j = 0; j < early; ++j) {
+      for (int j = 0, u = group, kb = 0; j < early; ++j) {
+        int channel, token;
+        i8_tile<CTAS>(a, u, n_tiles, m_tiles, channel, token);
         if (rank == 0) mbar_expect_tx(&st->full[j], CTAS * load_bytes);
         unsigned char* dst = smem + (size_t)j * stage_bytes + w_offset;
-        if (CTAS == 2) tma_load_2d_pair(dst, &tmW, j * I8_BK, channel + w_rows, &st->full[j]);
-        else tma_load_2d(dst, &tmW, j * I8_BK, channel + w_rows, &st->full[j]);
+        if (CTAS == 2) tma_load_2d_pair(dst, &tmW, kb * I8_BK, channel + w_rows, &st->full[j]);
+        else tma_load_2d(dst, &tmW, kb * I8_BK, channel + w_rows, &st->full[j]);
+        if (++kb == k_blocks) { kb = 0; u += ngroups; }
       }
     }
     __syncwarp();
@@ -554,29 +590,33 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
       }
     } else {
       // a lane is a token; a warp takes 128 channels, 32 at a time
-      unsigned char* stage = extra + ew * (2 * I8_BOX);
-      float* sb = (float*)(extra + I8_EPI_WARPS * 2 * I8_BOX) + ew * (2 * I8_WARP_COLS);
+      unsigned char* stage = extra + ew * i8_out(true);
+      float* sb = (float*)(extra + I8_EPI_WARPS * i8_out(true)) + ew * (2 * I8_WARP_COLS);
+      if (!a.aligned) {
+        stage = extra + ew * i8_out(false);
+        sb = (float*)(extra + I8_EPI_WARPS * i8_out(false)) + ew * (2 * I8_WARP_COLS);
+      }
       float* bias = sb + I8_WARP_COLS;
       const unsigned swizzle = (unsigned)((lane >> 1) & 3);       // 64-byte swizzle of a row of a box
       // what a tile needs beside its sums is loaded a tile ahead
+      int next_row0 = 0, next_j0 = 0;
       float next_sa = 0.f, next_sb[I8_WARP_COLS / 32], next_bias[I8_WARP_COLS / 32];
       const auto prefetch = [&](int u) {
         int channel, token;
         i8_tile<2>(a, u, n_tiles, m_tiles, channel, token);
-        const int i = token + rank * I8_ROWS + q * 32 + lane;
-        next_sa = i < a.m ? a.a_scale[i] : 0.f;
+        next_row0 = token + rank * I8_ROWS + q * 32;
+        next_j0 = channel + (ew >> 2) * I8_WARP_COLS;
+        next_sa = next_row0 + lane < a.m ? a.a_scale[next_row0 + lane] : 0.f;
 #pragma unroll
         for (int c = 0; c < I8_WARP_COLS / 32; ++c) {
-          const int j = channel + (ew >> 2) * I8_WARP_COLS + c * 32 + lane;
+          const int j = next_j0 + c * 32 + lane;
           next_sb[c] = j < a.n ? a.b_scale[j] : 0.f;
-          next_bias[c] = j < a.n ? bias_of(j) : 0.f;
+          next_bias[c] = a.bias && j < a.n ? bias_of(j) : 0.f;
         }
       };
       if (group < units) prefetch(group);
       for (int u = group; u < units && ok; u += ngroups, ++it) {
-        int channel, token;
-        i8_tile<2>(a, u, n_tiles, m_tiles, channel, token);
-        const int row0 = token + rank * I8_ROWS + q * 32, j0 = channel + (ew >> 2) * I8_WARP_COLS;
+        const int row0 = next_row0, j0 = next_j0, rows = min(32, a.m - row0);
         const float sa = next_sa;
         __syncwarp();
 #pragma unroll
@@ -585,12 +625,15 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
           bias[c * 32 + lane] = next_bias[c];
         }
         __syncwarp();
-        if (u + ngroups < units) prefetch(u + ngroups);
         const unsigned acc = it & 1u;
         if (!sums_ready(acc, (it >> 1) & 1u)) { ok = false; break; }
         const unsigned taddr = tmem_base + ((unsigned)(q * 32) << 16) + acc * 256 + (ew >> 2) * I8_WARP_COLS;
         unsigned r[2][32];
         tmem_issue32(taddr, r[0]);
+        if (u + ngroups < units) prefetch(u + ngroups);
+        const bool whole = j0 + I8_WARP_COLS <= a.n;
+        unsigned carry = 0;                                       // the last two bf16 values of the group before
+        const unsigned shift = (unsigned)(size_t)(C + (long long)(row0 + lane) * a.ldc + j0) & 15u;   // how far this lane's row is from 16 bytes
 #pragma unroll
         for (int g = 0; g < I8_WARP_COLS / 32; ++g) {
           const int c0 = g * 32;
@@ -634,18 +677,42 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
                 bulk_commit();
               }
             }
+          } else if (whole) {
+            // rows of 256 bytes are gathered, each as far from a 16-byte boundary as it will be in C
+            constexpr int PER = 32 * (int)sizeof(T) / 4;           // words of a group
+            constexpr int GROUPS = I8_ROW_BYTES / (32 * (int)sizeof(T));
+            unsigned* to = reinterpret_cast<unsigned*>(stage + lane * I8_ROW_PITCH) + (shift >> 2) + (g % GROUPS) * PER;
+            if (g % GROUPS == 0) __syncwarp();
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+              for (int c = 0; c < 32; ++c) to[c] = __float_as_uint(v[c]);
+            } else {
+              const unsigned pick = (shift & 2) ? 0x5432u : 0x7654u;   // half a word further on: the value before and this one
+#pragma unroll
+              for (int c = 0; c < 32; c += 2) {
+                const __nv_bfloat162 p = __floats2bfloat162_rn(v[c], v[c + 1]);
+                const unsigned w = *reinterpret_cast<const unsigned*>(&p);
+                to[c / 2] = __byte_perm(carry, w, pick);
+                carry = w;
+              }
+              if (g % GROUPS == GROUPS - 1 && (shift & 2)) to[PER] = carry >> 16;
+            }
+            if (g % GROUPS == GROUPS - 1) {
+              __syncwarp();
+              store_rows(stage, (unsigned char*)(C + (long long)row0 * a.ldc + j0 + c0 + 32) - I8_ROW_BYTES, a.ldc * (long long)sizeof(T), rows, lane);
+            }
           } else {
-            // turned in shared memory, so that a row's 32 channels are stored by 32 lanes
+            // the last channels: turned in shared memory, so that a row's 32 are stored by 32 lanes
             float* turn = (float*)stage;
             __syncwarp();
 #pragma unroll
             for (int c = 0; c < 32; ++c) turn[lane * 32 + (c ^ lane)] = v[c];
             __syncwarp();
-            const int rows = min(32, a.m - row0), j = j0 + c0 + lane;
+            const int j = j0 + c0 + lane;
             if (j < a.n) {
               T* to = C + (long long)row0 * a.ldc + j;
 #pragma unroll 8
-              for (int r = 0; r < rows; ++r, to += a.ldc) *to = from_float<T>(turn[r * 32 + (lane ^ r)]);
+              for (int i = 0; i < rows; ++i, to += a.ldc) *to = from_float<T>(turn[i * 32 + (lane ^ i)]);
             }
           }
         }
@@ -744,9 +811,12 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
   const bool pair = m > I8_ROWS;
   I8Args a = {};
   a.n = n; a.m = m; a.k = k;
+  // (a TMA store clips a row at 16 bytes, not at its last value)
+  const int es = out_bf16 ? 2 : 4;
+  a.aligned = pair ? ((size_t)C & 15) == 0 && ldc * es % 16 == 0 && (long long)n * es % 16 == 0 : ((size_t)C & 3) == 0 && ldc % 2 == 0;
   a.cols = pair ? 256 : (m + 15) / 16 * 16;
   const int blocks = (k + I8_BK - 1) / I8_BK, stage = I8_W_STAGE + (x ? 0 : a.cols / (pair ? 2 : 1) * I8_BK);
-  const int fit = (i8_ring(pair ? 2 : 1) - (x ? blocks * a.cols * I8_BK : 0)) / stage;
+  const int fit = (i8_ring(pair ? 2 : 1, a.aligned) - (x ? blocks * a.cols * I8_BK : 0)) / stage;
   a.stages = fit < I8_MAX_STAGES ? fit : I8_MAX_STAGES;
   // few tokens and long rows: tiles of equal height that fill whole rounds of the SMs (4 x 151,936 x 4,096: 143 -> 105 us; a
   // multiple of 4 keeps pairs of channels together); with short rows the results count, and tiles of 128 keep them aligned
@@ -765,9 +835,6 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
   a.bias_bf16 = bias_bf16 ? 1 : 0;
   a.C = C;
   a.ldc = ldc;
-  // (a TMA store clips a row at 16 bytes, not at its last value)
-  const int es = out_bf16 ? 2 : 4;
-  a.aligned = pair ? ((size_t)C & 15) == 0 && ldc * es % 16 == 0 && (long long)n * es % 16 == 0 : ((size_t)C & 3) == 0 && ldc % 2 == 0;
   a.status = status;
   a.behind = behind ? 1 : 0;
   a.x = x;
