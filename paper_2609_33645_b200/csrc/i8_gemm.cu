@@ -873,7 +873,7 @@ struct I8Plan {
 };
 I8Plan i8_plan(const pctc_i8_t* p) {
   I8Plan w;
-  w.ld = ((long long)p->k + 15) / 16 * 16;
+  w.ld = ((long long)p->k + 127) / 128 * 128;    // (a row that is loaded from 128-byte boundaries on comes in whole lines)
   w.q = 256;                                     // the status word comes first
   w.scales = w.q + up((size_t)p->m * w.ld);
   w.total = w.scales + up((size_t)p->m * 4);

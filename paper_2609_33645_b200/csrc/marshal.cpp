@@ -787,7 +787,7 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!x.is_cuda() || !is_float(x.scalar_type()) || x.dim() != 2 || x.size(1) < 1) fail(PyExc_ValueError, "x must be a bf16 or fp32 CUDA tensor [rows, D]");
   const at::Device dev = x.device();
   const RowView v = rows_of(x, "x");
-  const int64_t ld = (v.cols + 15) / 16 * 16;
+  const int64_t line = v.cols < 512 ? 16 : 128, ld = (v.cols + line - 1) / line * line;   // long rows start on whole lines
   const c10::cuda::CUDAGuard guard(dev);
   const at::Tensor whole = empty({v.rows, ld}, at::kChar, dev), scales = empty({v.rows}, at::kFloat, dev);
   check(api.i8_quantize(v.rows, v.cols, kind_of(x.scalar_type()), ptr(x), v.ld, (int8_t*)ptr(whole), ld, (float*)ptr(scales), stream_of(dev)),

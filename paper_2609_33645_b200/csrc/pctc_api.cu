@@ -800,7 +800,7 @@ struct Head8Plan {
 };
 Head8Plan head8_plan(const TopkPlan& t) {
   Head8Plan h;
-  h.ld = ((long long)t.g.D + 15) / 16 * 16;
+  h.ld = ((long long)t.g.D + 127) / 128 * 128;
   h.o_q = t.total;
   h.o_scales = h.o_q + up((size_t)t.g.M * h.ld);
   h.total = h.o_scales + up((size_t)t.g.M * 4);

@@ -181,7 +181,7 @@ def test_topk_with_the_head_in_8_bits_is_refused_before_any_launch(lib):
     a, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
     assert f.pctc_topk_workspace_bytes(ctypes.byref(p), n, 4, ctypes.byref(a)) == 0
     assert f.pctc_i8_topk_workspace_bytes(ctypes.byref(p), n, 4, ctypes.byref(b)) == 0
-    assert a.value < b.value <= a.value + 15 * 48 + 15 * 4 + 512
+    assert a.value < b.value <= a.value + 15 * 128 + 15 * 4 + 512
 
 
 def test_binding_refuses_what_it_cannot_hand_on(lib):
