@@ -66,7 +66,8 @@ struct PolicyArgs {
   long long N, T, total;
   long long ld_logp, ld_old, ld_ref, ld_adv, ld_mask, ld_grad;   // ld_adv 0: one advantage a row
   float2 log_low, log_high;                      // logarithms of where ratios are clipped, as a number and its rest
-  float low, high, kl_weight, sign;
+  double low, high;                              // the clipped ratios
+  float kl_weight, sign;
   int reduction;
   int counting;                                  // counts come from k_policy_count
 };
@@ -75,9 +76,10 @@ __device__ __forceinline__ int length_of(const PolicyArgs& a, long long n) {
   return a.lengths ? (int)min((long long)max(a.lengths[n], 0), a.T) : (int)a.T;
 }
 
-// The sums of a thread's four tokens; beyond a thread they are 64 bits.
+// The sums of a thread's few tokens.  Gains A r of both signs cancel, so they are 64 bits; the KL terms do not.
 struct TokenSums {
-  float loss = 0.f, kl = 0.f;
+  double gain = 0.0;
+  float kl_loss = 0.f, kl = 0.f;                 // loss = kl_loss - gain
   int clipped = 0, count = 0;
 };
 
@@ -89,18 +91,21 @@ __device__ __forceinline__ float2 difference(float a, float b) {
 }
 __device__ __forceinline__ bool above(float2 a, float2 b) { return a.x > b.x || (a.x == b.x && a.y > b.y); }
 
-// exp(b - a) - 1 - (b - a) and exp(b - a) - 1.  For |d| < 1 the first by its series d^2 (1/2 + d/6 + ... + d^11 / 13!), where
-// the difference would cancel (the next term is under 1e-10 of the sum), and the second from it; the rounding of d itself
-// is one of 2^-24 there.
+// exp(d) - 1 - d for |d| < 1 by its series d^2 (1/2 + d/6 + ... + d^11 / 13!), where the difference would cancel (the next term
+// is under 1e-10 of the sum).
+__device__ __forceinline__ float exp_tail(float d) {
+  constexpr float c[] = {1.f / 6227020800.f, 1.f / 479001600.f, 1.f / 39916800.f, 1.f / 3628800.f, 1.f / 362880.f, 1.f / 40320.f,
+                         1.f / 5040.f, 1.f / 720.f, 1.f / 120.f, 1.f / 24.f, 1.f / 6.f, 1.f / 2.f};
+  float s = c[0];
+#pragma unroll
+  for (int j = 1; j < 12; ++j) s = fmaf(d, s, c[j]);
+  return d * d * s;
+}
+// exp(b - a) - 1 - (b - a) and exp(b - a) - 1; the rounding of a difference under 1 is one of 2^-24.
 __device__ __forceinline__ void kl_terms(float a, float b, float& kl, float& e) {
   const float d = b - a;
   if (fabsf(d) < 1.f) {
-    constexpr float c[] = {1.f / 6227020800.f, 1.f / 479001600.f, 1.f / 39916800.f, 1.f / 3628800.f, 1.f / 362880.f, 1.f / 40320.f,
-                           1.f / 5040.f, 1.f / 720.f, 1.f / 120.f, 1.f / 24.f, 1.f / 6.f, 1.f / 2.f};
-    float s = c[0];
-#pragma unroll
-    for (int j = 1; j < 12; ++j) s = fmaf(d, s, c[j]);
-    kl = d * d * s;
+    kl = exp_tail(d);
     e = d + kl;
   } else {
     const float2 f = difference(b, a);
@@ -110,33 +115,39 @@ __device__ __forceinline__ void kl_terms(float a, float b, float& kl, float& e) 
   }
 }
 
-// One token: adds to the sums and returns its gradient before the weight.  Values come with the sign of log-probabilities;
-// what does not count comes as zeros with no advantage, and gives zeros.
-__device__ __forceinline__ float policy_token(const PolicyArgs& a, float x, float x_old, float x_ref, float A, float w, TokenSums& s) {
+// One token: adds to the sums and returns its gradient before the weight w (wd: the same in 64 bits).  Values come with the
+// sign of log-probabilities; what does not count comes as zeros with no advantage, and gives zeros.
+__device__ __forceinline__ float policy_token(const PolicyArgs& a, float x, float x_old, float x_ref, float A, float w, double wd,
+                                              TokenSums& s) {
   const float2 d = difference(x, x_old);         // exact: whether a ratio is clipped does not depend on a rounding
-  const float r0 = expf(d.x), r = isinf(r0) ? r0 : fmaf(r0, d.y, r0);
   const bool over = A > 0.f && above(d, a.log_high), under = A < 0.f && above(a.log_low, d), clipped = over || under;
-  const float used = over ? a.high : under ? a.low : r;
-  const float gain = A == 0.f ? (r == r ? 0.f : r) : A * used;   // no 0 * inf where the ratio overflows
-  float loss = -gain, g = clipped ? 0.f : -gain;
+  // near 1 the ratio is 1 + d in 64 bits and what is left, a hundredth and less, in 32
+  const double dd = (double)d.x + (double)d.y;
+  const double r = fabsf(d.x) < 1.f ? (1.0 + dd) + (double)exp_tail(d.x) : exp(dd);
+  const float r32 = (float)r;
+  float g = clipped || (A == 0.f && r32 == r32) ? 0.f : -A * r32;    // no 0 * inf where the ratio overflows
   if (a.ref) {
     float kl, e;
     kl_terms(x, x_ref, kl, e);
-    loss = fmaf(a.kl_weight, kl, loss);
+    s.kl_loss = fmaf(w, a.kl_weight * kl, s.kl_loss);
     g = fmaf(-a.kl_weight, e, g);
     s.kl += kl;
   }
-  s.loss = fmaf(w, loss, s.loss);
+  if (A != 0.f || r32 != r32) s.gain = fma(wd, (double)A * (over ? a.high : under ? a.low : r), s.gain);
   s.clipped += clipped ? 1 : 0;
   return g;
 }
 
-// What all weights have in common, and the weight of the tokens of a row with `count` of them.
-__device__ __forceinline__ float weight_part(const PolicyArgs& a, const Totals& t) {
-  return a.reduction == PCTC_POLICY_SUM ? 1.f : a.reduction == PCTC_POLICY_TOKENS ? 1.f / (float)max(t.count, 1) : (float)max(t.rows, 1);
+// The weight of the tokens of a row with `count` of them, in 64 bits: 1 / n for a whole number n.
+__device__ __forceinline__ double inverse(double n) {
+  const float w = 1.f / (float)n;
+  return fma((double)w, fma(-(double)w, n, 1.0), (double)w);      // one step of Newton's: 2^-48
 }
-__device__ __forceinline__ float weight_of(const PolicyArgs& a, float part, int count) {
-  return a.reduction == PCTC_POLICY_SEQUENCES ? 1.f / ((float)max(count, 1) * part) : part;
+__device__ __forceinline__ double weight_part(const PolicyArgs& a, const Totals& t) {
+  return a.reduction == PCTC_POLICY_SUM ? 1.0 : a.reduction == PCTC_POLICY_TOKENS ? inverse((double)max(t.count, 1)) : (double)max(t.rows, 1);
+}
+__device__ __forceinline__ double weight_of(const PolicyArgs& a, double part, int count) {
+  return a.reduction == PCTC_POLICY_SEQUENCES ? inverse((double)max(count, 1) * part) : part;
 }
 
 // How many of bytes 0 .. n - 1 are not zero, of the `lanes` threads' shares.
@@ -275,16 +286,17 @@ struct Values {
       }
     }
   }
-  __device__ __forceinline__ void finish(const PolicyArgs& a, float part, TokenSums& s) const {
+  __device__ __forceinline__ void finish(const PolicyArgs& a, double part, TokenSums& s) const {
     float g[POLICY_EACH] = {};
     if (masks) {
-      float w = part;
+      double wd = part;
 #pragma unroll
       for (int k = 0; k < POLICY_EACH; ++k) {
         if (k < ROWS && a.reduction == PCTC_POLICY_SEQUENCES)
-          w = weight_of(a, part, !VEC && !(masks >> k & 1) ? 1 : a.mask ? a.row_count[row[k]] : length[k]);
+          wd = weight_of(a, part, !VEC && !(masks >> k & 1) ? 1 : a.mask ? a.row_count[row[k]] : length[k]);
         const bool on = masks >> k & 1;
-        const float v = policy_token(a, on ? a.sign * x[k] : 0.f, on ? a.sign * o[k] : 0.f, on ? a.sign * q[k] : 0.f, on ? A[k] : 0.f, w, s);
+        const float w = (float)wd;
+        const float v = policy_token(a, on ? a.sign * x[k] : 0.f, on ? a.sign * o[k] : 0.f, on ? a.sign * q[k] : 0.f, on ? A[k] : 0.f, w, wd, s);
         g[k] = on ? a.sign * w * v : 0.f;
       }
     }
@@ -310,7 +322,7 @@ __device__ __forceinline__ void write_stats(const PolicyArgs& a, const BlockSums
 
 template <bool VEC, int GROUPS>
 __global__ void __launch_bounds__(POLICY_THREADS) k_policy(const PolicyArgs a) {
-  __shared__ float shared_part;
+  __shared__ double shared_part;
   __shared__ bool last;
   const long long tile = (long long)blockIdx.x * (POLICY_THREADS * POLICY_EACH * GROUPS);
   Values<VEC> v[GROUPS];
@@ -337,11 +349,11 @@ __global__ void __launch_bounds__(POLICY_THREADS) k_policy(const PolicyArgs a) {
     }
     __syncthreads();
   }
-  const float part = a.counting ? shared_part : weight_part(a, t);
+  const double part = a.counting ? shared_part : weight_part(a, t);
   TokenSums s;
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) v[i].finish(a, part, s);
-  BlockSums sums = block_sum<POLICY_THREADS>((double)s.loss, (double)s.kl, s.count, s.clipped);
+  BlockSums sums = block_sum<POLICY_THREADS>((double)s.kl_loss - s.gain, (double)s.kl, s.count, s.clipped);
   if (threadIdx.x == 0) {
     BlockSums* p = a.partial + blockIdx.x;
     __stcg(reinterpret_cast<double2*>(p), make_double2(sums.loss, sums.kl));
@@ -371,7 +383,7 @@ __global__ void __launch_bounds__(POLICY_THREADS) k_policy(const PolicyArgs a) {
 template <bool VEC>
 __global__ void __launch_bounds__(POLICY_SMALL_THREADS) k_policy_small(const PolicyArgs a) {
   __shared__ Totals counts;
-  __shared__ float shared_part;
+  __shared__ double shared_part;
   __shared__ BlockSums block_sums;
   cg::cluster_group cluster = cg::this_cluster();
   const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -391,7 +403,7 @@ __global__ void __launch_bounds__(POLICY_SMALL_THREADS) k_policy_small(const Pol
   }
   TokenSums s;
   v.finish(a, a.counting ? shared_part : weight_part(a, t), s);
-  BlockSums sums = block_sum<POLICY_SMALL_THREADS>((double)s.loss, (double)s.kl, s.count, s.clipped);
+  BlockSums sums = block_sum<POLICY_SMALL_THREADS>((double)s.kl_loss - s.gain, (double)s.kl, s.count, s.clipped);
   if (blocks == 1) {
     if (threadIdx.x == 0) write_stats(a, sums);
     return;
@@ -515,8 +527,8 @@ pctc_status_t pctc_policy_loss(const pctc_policy_t* p, const float* logp, const 
   a.ld_grad = p->ld_grad;
   a.log_low = number_and_rest(std::log1p(-p->clip_low));
   a.log_high = number_and_rest(std::log1p(p->clip_high));
-  a.low = (float)(1.0 - p->clip_low);
-  a.high = (float)(1.0 + p->clip_high);
+  a.low = 1.0 - p->clip_low;
+  a.high = 1.0 + p->clip_high;
   a.kl_weight = (float)p->kl_weight;
   a.sign = p->negated ? -1.f : 1.f;
   a.reduction = p->reduction;

@@ -252,3 +252,20 @@ def test_a_policy_step_over_transcripts():
     ref = H.run_oracle(batch, utt_weights=want["grad"][:, 0].cpu().numpy())
     for name in ("dH", "dW"):
         assert H.rel_fro(r[name].double().cpu().numpy(), ref[name]) < 1e-2
+
+
+@pytest.mark.parametrize("N,T", [(2000, 1), (40, 400), (300, 300)])
+def test_gains_that_cancel(N, T):
+    """Advantages of both signs whose gains add up to almost nothing: the sum is no worse than its last rounding and the
+    32-bit part of each token, exp(d) - 1 - d within 4 EPS."""
+    k = inputs(N, T, 11, each=True, ref=False, garbage=False, moved=0.1)
+    r = torch.exp(k["logp"].double() - k["old"].double()).clamp(0.8, 1.2)
+    k["adv"] = k["adv"] - ((k["adv"].double() * r).sum() / r.sum()).float()
+    for reduction in binding.POLICY_REDUCTIONS:
+        want = reference(**k, reduction=reduction)
+        d = k["logp"].double() - k["old"].double()
+        w = 1.0 if reduction == "sum" else 1.0 / (N * T)
+        part = float((k["adv"].double().abs() * (torch.expm1(d) - d)).sum()) * w
+        got = float(call(k, reduction=reduction)["loss"])
+        assert abs(want["loss"]) < 1e-3 * float(want["size"].sum())
+        assert abs(got - want["loss"]) <= EPS * abs(want["loss"]) + 4 * EPS * part
