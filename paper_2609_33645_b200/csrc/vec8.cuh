@@ -1,5 +1,4 @@
-// Consecutive values of a row: eight, moved 16 bytes at a time (8 at a time for 8-bit values), or N in one or two accesses;
-// and the conversions between storage types and fp32.
+// Consecutive values of a row: eight, moved 16 bytes at a time, or N in one or two accesses; and the conversions between storage types and fp32.
 #pragma once
 
 #include "pctc_internal.h"
@@ -62,18 +61,7 @@ struct Vec8<float> {
     *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
   }
 };
-template <>
-struct Vec8<signed char> {
-  uint2 w;
-  __device__ __forceinline__ void load(const signed char* p) { w = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    const unsigned u[2] = {w.x, w.y};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)(signed char)(u[i >> 2] >> (8 * (i & 3)));
-  }
-};
-
-// N values, N * sizeof(T) bytes aligned (16 where that is more): fp32 N = 1, 2, 4, 8, bf16 N = 1, 2, 4, 8.
+// N = 1, 2, 4 or 8 values, N * sizeof(T) bytes aligned (16 where that is more): fp32, bf16, or 8 bits (to be read).
 template <typename T, int N>
 struct VecN {
   static constexpr int BYTES = N * (int)sizeof(T), WORDS = BYTES < 4 ? 1 : BYTES / 4;
@@ -90,8 +78,10 @@ struct VecN {
       u[0] = v.x; u[1] = v.y;
     } else if constexpr (BYTES == 4) {
       u[0] = *reinterpret_cast<const unsigned*>(p);
-    } else {
+    } else if constexpr (BYTES == 2) {
       u[0] = *reinterpret_cast<const unsigned short*>(p);
+    } else {
+      u[0] = *reinterpret_cast<const unsigned char*>(p);
     }
   }
   // what another SM has written during this kernel: not from this SM's cache
@@ -113,6 +103,7 @@ struct VecN {
   }
   __device__ __forceinline__ float value(int i) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(u[i]);
+    else if constexpr (sizeof(T) == 1) return (float)(signed char)(u[i >> 2] >> (8 * (i & 3)));
     else return __uint_as_float((i & 1) ? u[i >> 1] & 0xffff0000u : u[i >> 1] << 16);
   }
   __device__ __forceinline__ void add_to(float (&x)[N]) const {
