@@ -750,7 +750,8 @@ def embed_grad(tokens, grad, vocab=None, *, dW=None, scale=1.0, accumulate=False
     grad [*tokens.shape, D] bf16 or fp32.  dW [V,D] is written whole (rows without a token: zeros), or, with
     accumulate=True, added to: a tied head's gradient as pruned_ctc_fwd_bwd has left it.  Without dW one is made for `vocab`
     rows, of type `dtype` (default grad's).  Sums are fp32 in a fixed order: repeated calls agree bit for bit.  Returns a
-    dict: dW and the workspace, which later calls on the same stream may take.  A written dW's version counts up.
+    dict: dW and the workspace (the given one, or a new one where that was too small), which later calls on the same stream may
+    take.  A written dW's version counts up.
     """
     dW, workspace = _native().embed_grad(tokens, grad, vocab, dW, scale, accumulate, dtype, workspace)
     return dict(dW=dW, workspace=workspace)
@@ -831,6 +832,6 @@ def matmul_i8(a, b, *, bias=None, dtype=None, status=None):
 
 def quantized_logits(hidden, head, *, bias=None, dtype=None, workspace=None):
     """Logits [..., V] of states hidden [..., D] (bf16 or fp32) under a QuantizedHead: the states are quantized row by row
-    and multiplied in 8-bit integers.  dtype: bf16 or fp32 (default hidden's).  workspace: a uint8 CUDA tensor to use (its
-    first word is the status word that workspace_status reads).  Not differentiable."""
+    and multiplied in 8-bit integers.  dtype: bf16 or fp32 (default hidden's).  workspace: a uint8 CUDA tensor to use, refused
+    if it is too small (its first word is the status word that workspace_status reads).  Not differentiable."""
     return _native().quantized_logits(hidden, head.q, head.scales, bias, dtype, workspace)[0]

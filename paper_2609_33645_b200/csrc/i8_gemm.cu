@@ -807,6 +807,7 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
                     const float* b_scale, const void* bias, bool bias_bf16, int m, int n, int k, void* C, long long ldc,
                     bool out_bf16, int* status, bool behind, cudaStream_t stream, const void* x, long long ld_x, bool x_bf16) {
   if (m <= 0 || n <= 0) return cudaSuccess;
+  if (x && !i8_own_tokens(m, k)) return cudaErrorInvalidValue;
   // up to 128 tokens: tiles as wide as the tokens, so that the head is read once and the ring is deep
   const bool pair = m > I8_ROWS;
   I8Args a = {};
@@ -854,8 +855,10 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
   return out_bf16 ? launch(__nv_bfloat16()) : launch(float());
 }
 
-// Whether the product quantizes so many tokens itself: they fit beside a ring of 100 KB and more.
-bool i8_own_tokens(int m, int k) { return (long long)m * k <= I8_OWN_VALUES && (long long)(m + 15) / 16 * 16 * ((k + 127) / 128 * 128) <= 98304; }
+// Whether the product quantizes so many tokens itself: they are columns of one tile, and fit beside a ring of 100 KB and more.
+bool i8_own_tokens(int m, int k) {
+  return m <= I8_ROWS && (long long)m * k <= I8_OWN_VALUES && (long long)(m + 15) / 16 * 16 * ((k + 127) / 128 * 128) <= 98304;
+}
 
 cudaError_t i8_quantize(const void* x, bool bf16, long long rows, long long cols, long long ld_x, signed char* q, long long ld_q,
                         float* scales, int* clear, cudaStream_t stream) {

@@ -598,11 +598,12 @@ std::vector<int64_t> with_last(const at::Tensor& t, int64_t last, bool replace) 
   return s;
 }
 bool has_shape(const at::Tensor& t, const std::vector<int64_t>& s) { return t.sizes().equals(s); }
-at::Tensor bytes_or(PyObject* given, size_t need, at::Device dev) {
+// The given bytes; new ones where there are none or, if they come back to the caller (`back`), too few.
+at::Tensor bytes_or(PyObject* given, size_t need, at::Device dev, bool back = true) {
   const at::Tensor w = optional_tensor(given, "workspace");
   if (w.defined() && (w.device() != dev || w.scalar_type() != at::kByte || !w.is_contiguous()))
     fail(PyExc_ValueError, "workspace must be contiguous bytes on the device of the call");
-  return w.defined() && (size_t)w.numel() >= need ? w : empty({(int64_t)need}, at::kByte, dev);
+  return w.defined() && (!back || (size_t)w.numel() >= need) ? w : empty({(int64_t)need}, at::kByte, dev);
 }
 uint64_t word(PyObject* o, const char* what) {
   if (!PyLong_Check(o)) fail(PyExc_TypeError, "%s must be an integer", what);
@@ -851,7 +852,7 @@ PyObject* quantized_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const c10::cuda::CUDAGuard guard(dev);
   size_t need = 0;
   check(api.i8_logits_workspace_bytes(&p, &need), "pctc_i8_logits_workspace_bytes");
-  const at::Tensor C = empty(with_last(x, q.size(0), true), type, dev), ws = bytes_or(a[5], need, dev);
+  const at::Tensor C = empty(with_last(x, q.size(0), true), type, dev), ws = bytes_or(a[5], need, dev, false);
   check(api.i8_logits(&p, ptr(x), kind_of(x.scalar_type()), (const int8_t*)ptr(q), (const float*)ptr(s), ptr(bias), ptr(C), ptr(ws),
                       (size_t)ws.numel(), stream_of(dev)),
         "pctc_i8_logits");

@@ -122,6 +122,23 @@ def test_rows_of_the_result_may_lie_apart():
             assert bool((C[:, n:] == 7).all()) and bool((C[m] == 7).all())
 
 
+@pytest.mark.parametrize("m", [1, 16, 17, 127, 128, 129, 130, 256, 257, 600, 768, 769, 8192])
+@pytest.mark.parametrize("k", [1, 8, 10, 31, 63, 64])
+def test_short_rows(m, k):
+    """Few values, and yet more tokens than a tile of few tokens holds."""
+    hidden = torch.randn(m, k, generator=gen(m), device=DEV)
+    head = binding.quantize_rows(torch.randn(300, k, generator=gen(k), device=DEV))
+    got = binding.quantized_logits(hidden, head)
+    check(got, *product(binding.QuantizedHead(*quantized(hidden)), head))
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    head = binding.quantize_rows(torch.randn(300, 64, generator=gen(1), device=DEV))
+    with pytest.raises(binding.PctcError) as e:
+        binding.quantized_logits(torch.randn(200, 64, device=DEV), head, workspace=torch.empty(4096, dtype=torch.uint8, device=DEV))
+    assert e.value.status == 2
+
+
 def test_scales_that_are_not_finite_spoil_their_rows_and_channels_alone():
     x, W = torch.randn(6, 64, generator=gen(1), device=DEV), torch.randn(200, 64, generator=gen(2), device=DEV)
     x[2, 3], W[100, 5] = float("nan"), float("inf")
