@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int lo = (int)blockIdx.x * a.width, width = (int)min((long long)a.width, a.V - lo);
+  const unsigned lo = blockIdx.x * (unsigned)a.width, width = (unsigned)min((long long)a.width, a.V - lo);
   for (long long i = (long long)blockIdx.x * SORT_THREADS + threadIdx.x; i < a.n_clear; i += (long long)a.buckets * SORT_THREADS)
     a.clear[i] = 0;
   for (int i = threadIdx.x; i < SORT_WARPS * a.width; i += SORT_THREADS) count[i] = 0;
@@ -164,25 +164,23 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
     for (int k = 0; k < SORT_AHEAD; ++k) t[k] = four_tokens(a.tokens, aligned, p + k * 128, p1);
 #pragma unroll
     for (int k = 0; k < SORT_AHEAD; ++k) {
-      const int v[4] = {t[k].x - lo, t[k].y - lo, t[k].z - lo, t[k].w - lo};
-      const bool any = (unsigned)v[0] < (unsigned)width || (unsigned)v[1] < (unsigned)width || (unsigned)v[2] < (unsigned)width ||
-                       (unsigned)v[3] < (unsigned)width;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) below += v[j] < 0 && v[j] >= -lo;      // tokens 0 .. lo - 1
+      const unsigned v[4] = {(unsigned)t[k].x - lo, (unsigned)t[k].y - lo, (unsigned)t[k].z - lo, (unsigned)t[k].w - lo};
+      const bool any = v[0] < width || v[1] < width || v[2] < width || v[3] < width;
+      below += ((unsigned)t[k].x < lo) + ((unsigned)t[k].y < lo) + ((unsigned)t[k].z < lo) + ((unsigned)t[k].w < lo);   // none below 0
       if (!__any_sync(0xffffffffu, any)) continue;
       int before = 0, all = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const unsigned hits = __ballot_sync(0xffffffffu, (unsigned)v[j] < (unsigned)width);
+        const unsigned hits = __ballot_sync(0xffffffffu, v[j] < width);
         before += __popc(hits & lower);
         all += __popc(hits);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if ((unsigned)v[j] < (unsigned)width) {
+        if (v[j] < width) {
           atomicAdd(&mine[v[j]], 1);
           const int at = n + before++;
-          if (at < SORT_KEEP) kept[warp][at] = ((unsigned)v[j] << SORT_RUN_BITS) | (unsigned)(p + k * 128 + j - p0);
+          if (at < SORT_KEEP) kept[warp][at] = (v[j] << SORT_RUN_BITS) | (unsigned)(p + k * 128 + j - p0);
         }
       n += all;
     }
@@ -192,9 +190,9 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
   __syncthreads();
 
   // counts -> where each warp's first position of each token goes
-  const int per = (width + SORT_THREADS - 1) / SORT_THREADS, k0 = threadIdx.x * per;
+  const unsigned per = (width + SORT_THREADS - 1) / SORT_THREADS, k0 = threadIdx.x * per;
   int sum = 0;
-  for (int k = k0; k < k0 + per && k < width; ++k)
+  for (unsigned k = k0; k < k0 + per && k < width; ++k)
 #pragma unroll
     for (int w = 0; w < SORT_WARPS; ++w) sum += count[w * a.width + k];
   int scan = sum;
@@ -208,7 +206,7 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
   int at = scan - sum;
 #pragma unroll
   for (int w = 0; w < SORT_WARPS; ++w) at += below_sum[w] + (w < warp ? scan_sum[w] : 0);
-  for (int k = k0; k < k0 + per && k < width; ++k) {
+  for (unsigned k = k0; k < k0 + per && k < width; ++k) {
     a.first[lo + k] = at;
     int c[SORT_WARPS];
 #pragma unroll
@@ -235,7 +233,7 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
       const int rank = __popc(equal & lower), to = mine[key] + rank;
       __syncwarp(hits);
       if (rank == 0) mine[key] = to + __popc(equal);
-      a.sorted[to] = make_int2(position, lo + key);
+      a.sorted[to] = make_int2(position, (int)lo + key);
     }
     __syncwarp();
   };
@@ -246,12 +244,12 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
     }
   } else {
     for (int p = p0 + lane; p - lane < p1; p += 32 * SORT_AHEAD) {
-      int t[SORT_AHEAD];
+      unsigned v[SORT_AHEAD];
 #pragma unroll
-      for (int k = 0; k < SORT_AHEAD; ++k) t[k] = p + k * 32 < p1 ? a.tokens[p + k * 32] - lo : -1;
+      for (int k = 0; k < SORT_AHEAD; ++k) v[k] = (unsigned)(p + k * 32 < p1 ? a.tokens[p + k * 32] : -1) - lo;
 #pragma unroll
       for (int k = 0; k < SORT_AHEAD; ++k)
-        if (__any_sync(0xffffffffu, (unsigned)t[k] < (unsigned)width)) place((unsigned)t[k] < (unsigned)width, t[k], p + k * 32);
+        if (__any_sync(0xffffffffu, v[k] < width)) place(v[k] < width, (int)v[k], p + k * 32);
     }
   }
 }
@@ -494,7 +492,8 @@ GradPlan grad_plan(const pctc_embed_t* p) {
 pctc_status_t check_embed(const pctc_embed_t* p) {
   if (!p || p->M < 0 || p->V < 1 || p->D < 1 || !std::isfinite(p->scale)) return PCTC_ERR_INVALID_ARG;
   if (p->ld_w < p->D || p->ld_x < p->D) return PCTC_ERR_INVALID_ARG;
-  if (p->M > 0x7fffffffLL - 64 || p->V > 0x7fffffffLL - 1 || p->D > (1 << 24)) return PCTC_ERR_UNSUPPORTED;
+  // (the sort's steps of positions run past M by up to 128 * SORT_AHEAD * 2)
+  if (p->M > 0x7fffffffLL - 4096 || p->V > 0x7fffffffLL - 1 || p->D > (1 << 24)) return PCTC_ERR_UNSUPPORTED;
   if (p->ld_w > MAX_ELEMENTS / p->V || p->ld_x > MAX_ELEMENTS / (p->M + 1)) return PCTC_ERR_UNSUPPORTED;
   return PCTC_OK;
 }

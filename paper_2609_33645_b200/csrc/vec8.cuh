@@ -1,4 +1,5 @@
-// Consecutive values of a row: eight, moved 16 bytes at a time, or N in one or two accesses; and the conversions between storage types and fp32.
+// Consecutive values of a row: eight, moved 16 bytes at a time, or N in one or two accesses; and the conversions between
+// storage types and fp32.
 #pragma once
 
 #include "pctc_internal.h"
@@ -21,7 +22,6 @@ template <>
 struct Vec8<__nv_bfloat16> {
   uint4 w;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void load_once(const __nv_bfloat16* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
   __device__ __forceinline__ void get(float (&v)[8]) const {
     const unsigned u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -47,10 +47,6 @@ struct Vec8<float> {
   __device__ __forceinline__ void load(const float* p) {
     a = *reinterpret_cast<const float4*>(p);
     b = *reinterpret_cast<const float4*>(p + 4);
-  }
-  __device__ __forceinline__ void load_once(const float* p) {
-    a = __ldcs(reinterpret_cast<const float4*>(p));
-    b = __ldcs(reinterpret_cast<const float4*>(p + 4));
   }
   __device__ __forceinline__ void get(float (&v)[8]) const {
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;

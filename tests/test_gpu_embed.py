@@ -85,6 +85,21 @@ def test_tokens_outside_the_vocabulary_give_zeros_and_no_gradient():
         assert bool((dW[0] == 2).all()) and bool((dW[1:] == 0).all())
 
 
+@pytest.mark.parametrize("M", [4, 300, 20_000])
+def test_tokens_of_any_32_bits(M):
+    V, D = 5000, 24
+    t = torch.randint(-2 ** 31, 2 ** 31, (M,), generator=gen(1), device=DEV, dtype=torch.int64)
+    t[::3] %= V
+    t[:4] = torch.tensor([-2 ** 31, 2 ** 31 - 1, V, V - 1], device=DEV)
+    t, there = t.int(), (t >= 0) & (t < V)
+    W, g = rows(V, D, FP, 2), rows(M, D, FP, 3)
+    assert torch.equal(binding.embed(t, W), torch.where(there[:, None], W[torch.where(there, t, 0).long()], 0.0))
+    want = torch.zeros(V, D, device=DEV, dtype=torch.float64).index_add_(0, t[there].long(), g[there].double())
+    sums = torch.zeros(V, D, device=DEV, dtype=torch.float64).index_add_(0, t[there].long(), g[there].double().abs())
+    got = binding.embed_grad(t, g, V)["dW"].double()
+    assert bool(((got - want).abs() <= M * EPS * sums).all())
+
+
 def test_lookup_leaves_its_neighbours_alone():
     for D, dt in ((24, BF), (23, BF), (9, FP)):
         buf = torch.full((7, D + 9), 5.0, device=DEV, dtype=dt)
