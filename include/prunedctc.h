@@ -464,8 +464,8 @@ pctc_status_t pctc_grad_scale(int32_t n, const void* const* grads, void* const* 
  * of zeros, whatever W holds.
  */
 typedef struct {
-  int64_t M;             /* tokens, >= 0                                                      */
-  int64_t V;             /* rows of W                                                         */
+  int64_t M;             /* tokens, 0 .. 2^31 - 4097                                          */
+  int64_t V;             /* rows of W, up to 2^31 - 2                                         */
   int64_t D;
   int64_t ld_w;          /* elements between rows of W (dW) ...                               */
   int64_t ld_x;          /* ... and of out (grad).  Fastest with D % 8 == 0 and rows that start 16-byte aligned */
@@ -526,7 +526,8 @@ pctc_status_t pctc_dropout(const pctc_dropout_t* problem, const void* x, const v
  *   w = 1                                                               PCTC_POLICY_SUM.
  * At r = 1 + clip_high (1 - clip_low) exactly the gradient is that of the ratio.  What lies in uncounted places is not
  * looked at, and its gradient is 0; with nothing counted the loss is 0.  Counted values that are not finite give what the
- * formula gives.  Differences and sums are 64 bits, exponentials fp32; repeated calls agree bit for bit.
+ * formula gives (A = 0 times the ratio of a d that fp32 holds is 0, however large).  Differences are exact, ratios, gains A r and sums
+ * 64 bits, KL terms and gradients fp32; repeated calls agree bit for bit.
  */
 typedef enum { PCTC_POLICY_TOKENS = 0, PCTC_POLICY_SEQUENCES = 1, PCTC_POLICY_SUM = 2 } pctc_policy_reduction_t;
 typedef struct {
@@ -536,7 +537,7 @@ typedef struct {
   int64_t ld_mask, ld_grad;
   double  clip_low;      /* in [0, 1]                                                         */
   double  clip_high;     /* >= 0; +inf: ratios are not clipped upwards                        */
-  double  kl_weight;     /* finite                                                            */
+  double  kl_weight;     /* finite as fp32                                                    */
   int32_t reduction;     /* pctc_policy_reduction_t                                           */
   int32_t negated;       /* 1: logp, old_logp and ref_logp are given with the other sign (as losses), and so is grad */
 } pctc_policy_t;
@@ -580,8 +581,8 @@ pctc_status_t pctc_i8_quantize(int64_t rows, int64_t cols, int32_t dtype, const 
  * device_status [1] or NULL: receives a code if a bounded wait gives up (see pctc_workspace_status; the caller zeroes it). */
 pctc_status_t pctc_i8_matmul(const pctc_i8_t* problem, const int8_t* A, const float* a_scales, const int8_t* B,
                              const float* b_scales, const void* bias, void* C, int32_t* device_status, void* stream);
-/* x [m,k] (x_dtype).  workspace: >= pctc_i8_logits_workspace_bytes(), 256-byte aligned, with a status word at its start;
- * nothing else in it outlives the call (calls that may run at the same time need one each). */
+/* x [m,k] (x_dtype).  workspace: >= pctc_i8_logits_workspace_bytes(), 256-byte aligned, with a status word at its start
+ * (not written with m = 0); nothing else in it outlives the call (calls that may run at the same time need one each). */
 pctc_status_t pctc_i8_logits_workspace_bytes(const pctc_i8_t* problem, size_t* bytes_out);
 pctc_status_t pctc_i8_logits(const pctc_i8_t* problem, const void* x, int32_t x_dtype, const int8_t* B, const float* b_scales,
                              const void* bias, void* C, void* workspace, size_t workspace_bytes, void* stream);

@@ -8,8 +8,9 @@
 // The weights need the counts before the first gradient can be written: where a mask or lengths are given,
 // k_policy_count goes over them first (a quarter of a byte and less for a byte that the second pass moves).  k_policy then
 // reads every value once.  Few values are done by one cluster in one launch (k_policy_small).  Differences are exact (two
-// fp32 numbers), sums 64 bits, in a fixed order.  Large calls are bound by the exponentials and the loads, about alike,
-// small ones by the launch.
+// fp32 numbers), gains and sums 64 bits, in a fixed order; KL terms, which never cancel one another, 32 bits.  Large calls are
+// bound by the arithmetic of a token and its loads, about alike (1M tokens with a mask: 14.5 us, of which 2.6 us are bytes at
+// HBM's rate), small ones by the launches (128 x 501: 7.8 us) and the length of one token's chain (64 values: 3.9 us).
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 
@@ -125,7 +126,8 @@ __device__ __forceinline__ float policy_token(const PolicyArgs& a, float x, floa
   const double dd = (double)d.x + (double)d.y;
   const double r = fabsf(d.x) < 1.f ? (1.0 + dd) + (double)exp_tail(d.x) : exp(dd);
   const float r32 = (float)r;
-  float g = clipped || (A == 0.f && r32 == r32) ? 0.f : -A * r32;    // no 0 * inf where the ratio overflows
+  const bool none = A == 0.f && fabsf(d.x) < CUDART_INF_F;           // no 0 * inf where exp(d) overflows for a finite d
+  float g = clipped || none ? 0.f : -A * r32;
   if (a.ref) {
     float kl, e;
     kl_terms(x, x_ref, kl, e);
@@ -133,7 +135,7 @@ __device__ __forceinline__ float policy_token(const PolicyArgs& a, float x, floa
     g = fmaf(-a.kl_weight, e, g);
     s.kl += kl;
   }
-  if (A != 0.f || r32 != r32) s.gain = fma(wd, (double)A * (over ? a.high : under ? a.low : r), s.gain);
+  if (!none) s.gain = fma(wd, (double)A * (over ? a.high : under ? a.low : r), s.gain);
   s.clipped += clipped ? 1 : 0;
   return g;
 }
@@ -448,7 +450,7 @@ float2 number_and_rest(double v) {
 pctc_status_t check_policy(const pctc_policy_t* p) {
   if (!p || p->N < 1 || p->T < 1) return PCTC_ERR_INVALID_ARG;
   if (p->N > 0x7fffffffLL / p->T) return PCTC_ERR_UNSUPPORTED;
-  if (!(p->clip_low >= 0.0 && p->clip_low <= 1.0) || !(p->clip_high >= 0.0) || !std::isfinite(p->kl_weight)) return PCTC_ERR_INVALID_ARG;
+  if (!(p->clip_low >= 0.0 && p->clip_low <= 1.0) || !(p->clip_high >= 0.0) || !std::isfinite((float)p->kl_weight)) return PCTC_ERR_INVALID_ARG;
   if (p->reduction != PCTC_POLICY_TOKENS && p->reduction != PCTC_POLICY_SEQUENCES && p->reduction != PCTC_POLICY_SUM)
     return PCTC_ERR_INVALID_ARG;
   return PCTC_OK;

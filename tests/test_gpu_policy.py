@@ -1,8 +1,8 @@
 """The clipped policy loss on the GPU against the same formula in 64 bits, and its gradient against differences of that.
 
-Tolerances, in roundings of 2^-24 (EPS): a ratio is expf (two steps: 4 EPS) with one product for the rest of the exponent;
-a token's loss and gradient two products and a sum more, the KL terms expm1f (one step: 2 EPS), a series of seven
-operations and two products; the weight two products and a quotient.  16 EPS of the sum of the terms' magnitudes covers them all; sums are 64 bits."""
+Tolerances, in roundings of 2^-24 (EPS): a ratio is 64 bits (where |d| < 1: with a series of fourteen fp32
+operations for what goes beyond 1 + d, at most 0.72 of it) and rounded once; a gradient two products and a sum more, the KL
+terms expm1f (one step: 2 EPS) or that series and two products; the weight 2^-48 and a rounding.  16 EPS of the sum of the terms' magnitudes covers them all; sums are 64 bits."""
 
 import math
 
@@ -171,6 +171,10 @@ def test_values_that_are_not_finite():
     assert float(r["kl"]) == inf and float(r["grad"]) == 0.0     # exp(-inf) - 1 + inf; -A r - (0 - 1)
     r = binding.policy_loss(one - inf, one, torch.ones(1, device=DEV), ref_logp=one, kl_weight=1.0)
     assert float(r["kl"]) == inf and float(r["grad"]) == -inf
+    # no advantage: nothing times the ratio of a finite difference, however large; 0 * inf of an infinite one
+    for x, o, nan in ((1000.0, 0.0, False), (-1.0, -inf, True), (-inf, -1.0, False), (-inf, -inf, True)):
+        r = binding.policy_loss(torch.full((1, 1), x, device=DEV), torch.full((1, 1), o, device=DEV), torch.zeros(1, device=DEV))
+        assert all(math.isnan(float(r[k])) == nan and (nan or float(r[k]) == 0.0) for k in ("loss", "grad")), (x, o)
 
 
 def test_nothing_counted():

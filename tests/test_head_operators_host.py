@@ -29,7 +29,7 @@ def embed_grad(lib, tokens=A[0], grad=A[2], dW=A[1], ws=A[5], ws_bytes=1 << 20, 
 @pytest.mark.parametrize("kw,want", [
     (dict(M=-1), INVALID), (dict(V=0), INVALID), (dict(D=0), INVALID), (dict(ld_w=15), INVALID), (dict(ld_x=15), INVALID),
     (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID),
-    (dict(M=1 << 31), UNSUPPORTED), (dict(V=1 << 31), UNSUPPORTED), (dict(D=(1 << 24) + 1, ld_w=1 << 25, ld_x=1 << 25), UNSUPPORTED),
+    (dict(M=1 << 31), UNSUPPORTED), (dict(M=(1 << 31) - 4096), UNSUPPORTED), (dict(V=1 << 31), UNSUPPORTED), (dict(D=(1 << 24) + 1, ld_w=1 << 25, ld_x=1 << 25), UNSUPPORTED),
     (dict(ld_x=1 << 40), UNSUPPORTED), (dict(ld_w=1 << 40), UNSUPPORTED),
     (dict(dtype_w=3), UNSUPPORTED), (dict(dtype_x=2), UNSUPPORTED),
     (dict(dtype_w=2), INVALID),                                # 8 bits need scales ...
@@ -104,7 +104,7 @@ def policy(lib, logp=A[0], old=A[1], ref=None, adv=A[3], mask=None, lengths=None
 @pytest.mark.parametrize("kw,want", [
     (dict(N=0), INVALID), (dict(T=0), INVALID), (dict(N=1 << 20, T=1 << 11), UNSUPPORTED),
     (dict(clip_low=-0.1), INVALID), (dict(clip_low=1.1), INVALID), (dict(clip_high=-0.1), INVALID), (dict(clip_high=float("nan")), INVALID),
-    (dict(kl_weight=float("inf")), INVALID), (dict(reduction=3), INVALID), (dict(reduction=-1), INVALID),
+    (dict(kl_weight=float("inf")), INVALID), (dict(kl_weight=1e39), INVALID), (dict(reduction=3), INVALID), (dict(reduction=-1), INVALID),
     (dict(logp=None), INVALID), (dict(old=None), INVALID), (dict(adv=None), INVALID), (dict(stats=None), INVALID),
     (dict(count=None), INVALID), (dict(ws=None), INVALID), (dict(ws=A[9] + 8), INVALID), (dict(ws_bytes=8), SMALL),
     (dict(logp=A[0] + 2), INVALID), (dict(grad=A[6] + 1), INVALID), (dict(lengths=A[5] + 2), INVALID),
