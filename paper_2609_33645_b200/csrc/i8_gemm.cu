@@ -4,7 +4,7 @@
 //
 // k_i8_gemm is a persistent tcgen05 kernel (kind::i8) in three forms; roles, ring and bounded waits are those of the bf16
 // kernel in umma_gemm.cu.
-//   very few tokens (up to 8,192 values): as below, and every CTA quantizes the tokens itself, into the operand's place in
+//   very few tokens (up to 8,192 values, of rows that are read in eights): as below, and every CTA quantizes the tokens itself, into the operand's place in
 //     shared memory, while its first ring of the head is on its way: one launch.
 //   few tokens (up to 128), CTAS = 1: the rows of the accumulators are channels (rows of the head), the columns tokens, tiles
 //     128 x 16 .. 128 x 128: the head streams once through a deep ring, and 32 lanes of a warp hold 32 neighbouring
@@ -166,7 +166,9 @@ constexpr int I8_THREADS = 64 + 32 * I8_EPI_WARPS;
 constexpr int I8_MAX_STAGES = 12;
 constexpr int I8_TMEM_COLS = 512;
 constexpr int I8_OWN_VALUES = 8192;              // up to so many values of tokens are quantized by the product itself
-                                                 // (4 x 151,936 x 1,024: 33.2 -> 31.5 us; 16 x 1,024 values: 32.8 -> 35.2)
+                                                 // (4 x 151,936 x 1,024: 33.2 -> 31.5 us; 16 x 1,024 values: 32.8 -> 35.2),
+constexpr int I8_OWN_SINGLE = 1024;              // or so many that are read one by one (50,001 x 516, 1 and 4 tokens: 12.4 and 14.8 us
+                                                 // against 13.0 and 13.2 with a launch ahead)
 
 struct I8Args {
   int n, m, k;                                   // channels, tokens, contraction
@@ -799,6 +801,11 @@ cudaError_t i8_launch(const CUtensorMap& tmW, const CUtensorMap& tmX, const CUte
   return cudaLaunchKernelEx(&cfg, kern, tmW, tmX, tmC, a);
 }
 
+// Whether the rows of the tokens can be read in aligned groups of eight.
+bool in_eights(const void* x, long long ld_x, bool bf16, int k) {
+  return k % 8 == 0 && ((size_t)x & 15) == 0 && ld_x * (bf16 ? 2 : 4) % 16 == 0;
+}
+
 constexpr long long I8_BAND_BYTES = 32LL << 20;         // token rows of a band: a quarter of the L2
 
 }  // namespace
@@ -807,7 +814,7 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
                     const float* b_scale, const void* bias, bool bias_bf16, int m, int n, int k, void* C, long long ldc,
                     bool out_bf16, int* status, bool behind, cudaStream_t stream, const void* x, long long ld_x, bool x_bf16) {
   if (m <= 0 || n <= 0) return cudaSuccess;
-  if (x && !i8_own_tokens(m, k)) return cudaErrorInvalidValue;
+  if (x && !i8_own_tokens(x, ld_x, x_bf16, m, k)) return cudaErrorInvalidValue;
   // up to 128 tokens: tiles as wide as the tokens, so that the head is read once and the ring is deep
   const bool pair = m > I8_ROWS;
   I8Args a = {};
@@ -840,7 +847,7 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
   a.behind = behind ? 1 : 0;
   a.x = x;
   a.ld_x = ld_x;
-  a.wide_x = k % 8 == 0 && ((size_t)x & 15) == 0 && ld_x * (x_bf16 ? 2 : 4) % 16 == 0;
+  a.wide_x = in_eights(x, ld_x, x_bf16, k);
   alignas(64) CUtensorMap tmW, tmX = {}, tmC = {};
   if (!i8_map(&tmW, B, k, n, ldb, (unsigned)a.rows)) return cudaErrorInvalidValue;
   if (!x && !i8_map(&tmX, A, k, m, lda, pair ? I8_ROWS : (unsigned)a.cols)) return cudaErrorInvalidValue;
@@ -856,8 +863,8 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
 }
 
 // Whether the product quantizes so many tokens itself: they are columns of one tile, and fit beside a ring of 100 KB and more.
-bool i8_own_tokens(int m, int k) {
-  return m <= I8_ROWS && (long long)m * k <= I8_OWN_VALUES && (long long)(m + 15) / 16 * 16 * ((k + 127) / 128 * 128) <= 98304;
+bool i8_own_tokens(const void* x, long long ld_x, bool bf16, int m, int k) {
+  return m <= I8_ROWS && (long long)m * k <= (in_eights(x, ld_x, bf16, k) ? I8_OWN_VALUES : I8_OWN_SINGLE) && (long long)(m + 15) / 16 * 16 * ((k + 127) / 128 * 128) <= 98304;
 }
 
 cudaError_t i8_quantize(const void* x, bool bf16, long long rows, long long cols, long long ld_x, signed char* q, long long ld_q,
@@ -972,7 +979,7 @@ pctc_status_t pctc_i8_logits(const pctc_i8_t* p, const void* x, int32_t x_dtype,
   signed char* q = (signed char*)(ws + w.q);
   float* scales = (float*)(ws + w.scales);
   cudaStream_t stream = (cudaStream_t)stream_v;
-  const bool fused = i8_own_tokens(p->m, p->k);
+  const bool fused = i8_own_tokens(x, p->lda, x_dtype == PCTC_BF16, p->m, p->k);
   if (!fused && i8_quantize(x, x_dtype == PCTC_BF16, p->m, p->k, p->lda, q, w.ld, scales, (int*)ws, stream) != cudaSuccess) return PCTC_ERR_CUDA;
   const cudaError_t e = i8_gemm(q, w.ld, scales, (const signed char*)B, p->ldb, b_scales, bias, p->bias_dtype == PCTC_BF16, p->m, p->n,
                                 p->k, C, p->ldc, p->out_dtype == PCTC_BF16, (int*)ws, !fused, stream, fused ? x : nullptr, p->lda,

@@ -13,7 +13,7 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
                     const float* b_scale, const void* bias, bool bias_bf16, int m, int n, int k, void* C, long long ldc,
                     bool out_bf16, int* status, bool behind, cudaStream_t stream, const void* x = nullptr,
                     long long ld_x = 0, bool x_bf16 = false);
-bool i8_own_tokens(int m, int k);
+bool i8_own_tokens(const void* x, long long ld_x, bool bf16, int m, int k);
 
 // q[r,:] = round(x[r,:] * 127 / max|x[r]|), scales[r] = max|x[r]| / 127; zeroes *clear (null: nothing).
 cudaError_t i8_quantize(const void* x, bool bf16, long long rows, long long cols, long long ld_x, signed char* q, long long ld_q,
