@@ -4,7 +4,8 @@
 // stored: the backward pass is the same call on the gradient.  The words are those of Philox-4x32 with ten rounds
 // (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011): block b = index / 8 as counter, one
 // 16-bit half for each of its eight values.  Halves instead of whole words: a block of ten rounds is some 75
-// instructions, and with four values a block a bf16 call would be bound by them and not by HBM.
+// instructions, and with four values a block a bf16 call would be bound by them and not by HBM.  With eight it is bound by HBM
+// (64,000 x 1,024 bf16 with a residual: 7.0 TB/s), a small one by the launch.
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 #include "vec8.cuh"
@@ -61,38 +62,28 @@ __device__ __forceinline__ float drop_one(float x, unsigned u, unsigned limit, f
   return u < limit ? 0.f : x * scale;
 }
 
-// Groups that lie in one row, 16-byte aligned in every array.
-template <typename T, bool RES, bool ROWS, int U>
+// Groups that lie in one row, 16-byte aligned in every array.  One a thread: two or four, loaded ahead, were slower at every size
+// (64,000 x 1,024 bf16 with a residual: 56.3, 56.8 and 57.5 us; 4,800 x 1,024: 5.6, 6.0 and 6.5).
+template <typename T, bool RES, bool ROWS>
 __global__ void __launch_bounds__(DROP_THREADS) k_dropout_vec(const DropArgs a) {
   const unsigned long long offset = a.offset + (a.step ? (unsigned long long)*a.step : 0ull);
-  const long long g0 = (long long)blockIdx.x * (DROP_THREADS * U) + threadIdx.x;
-  Vec8<T> x[U], r[U];
+  const long long g = (long long)blockIdx.x * DROP_THREADS + threadIdx.x;
+  if (g >= a.groups) return;
+  const long long row = ROWS ? g / a.groups_per_row : 0, col = (g - row * a.groups_per_row) * 8;
+  Vec8<T> x, r;
+  x.load((const T*)a.x + row * a.ld_x + col);
+  if (RES) r.load((const T*)a.residual + row * a.ld_res + col);
+  unsigned c[4];
+  philox(c, (unsigned long long)g, offset, a.seed);
+  float v[8], add[8];
+  x.get(v);
+  if (RES) r.get(add);
 #pragma unroll
-  for (int k = 0; k < U; ++k) {
-    const long long g = g0 + k * DROP_THREADS;
-    if (g >= a.groups) continue;
-    const long long row = ROWS ? g / a.groups_per_row : 0, col = (g - row * a.groups_per_row) * 8;
-    x[k].load((const T*)a.x + row * a.ld_x + col);
-    if (RES) r[k].load((const T*)a.residual + row * a.ld_res + col);
+  for (int j = 0; j < 8; ++j) {
+    v[j] = drop_one(v[j], half_of(c, j), a.limit, a.scale);
+    if (RES) v[j] += add[j];
   }
-#pragma unroll
-  for (int k = 0; k < U; ++k) {
-    const long long g = g0 + k * DROP_THREADS;
-    if (g >= a.groups) continue;
-    const long long row = ROWS ? g / a.groups_per_row : 0, col = (g - row * a.groups_per_row) * 8;
-    unsigned c[4];
-    philox(c, (unsigned long long)g, offset, a.seed);
-    float v[8];
-    x[k].get(v);
-    float add[8];
-    if (RES) r[k].get(add);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[j] = drop_one(v[j], half_of(c, j), a.limit, a.scale);
-      if (RES) v[j] += add[j];
-    }
-    Vec8<T>::store((T*)a.out + row * a.ld_out + col, v);
-  }
+  Vec8<T>::store((T*)a.out + row * a.ld_out + col, v);
 }
 
 // Any strides and addresses; also what is left behind the last whole group (from group `first` on).
@@ -122,18 +113,11 @@ cudaError_t dropout_launch(DropArgs a, bool aligned, cudaStream_t stream) {
   if (aligned && (a.rows == 1 || a.cols % 8 == 0)) {
     a.groups_per_row = a.cols / 8;
     a.groups = a.rows * a.groups_per_row;
-    // four groups a thread once that leaves every SM several blocks
-    const bool many = a.groups >= 148LL * 4 * 4 * DROP_THREADS;
-    const long long blocks = (a.groups + DROP_THREADS * (many ? 4 : 1) - 1) / (DROP_THREADS * (many ? 4 : 1));
+    const long long blocks = (a.groups + DROP_THREADS - 1) / DROP_THREADS;
     if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
     if (blocks > 0) {
-      if (a.rows == 1) {
-        if (many) k_dropout_vec<T, RES, false, 4><<<(unsigned)blocks, DROP_THREADS, 0, stream>>>(a);
-        else k_dropout_vec<T, RES, false, 1><<<(unsigned)blocks, DROP_THREADS, 0, stream>>>(a);
-      } else {
-        if (many) k_dropout_vec<T, RES, true, 4><<<(unsigned)blocks, DROP_THREADS, 0, stream>>>(a);
-        else k_dropout_vec<T, RES, true, 1><<<(unsigned)blocks, DROP_THREADS, 0, stream>>>(a);
-      }
+      if (a.rows == 1) k_dropout_vec<T, RES, false><<<(unsigned)blocks, DROP_THREADS, 0, stream>>>(a);
+      else k_dropout_vec<T, RES, true><<<(unsigned)blocks, DROP_THREADS, 0, stream>>>(a);
       const cudaError_t e = cudaGetLastError();
       if (e != cudaSuccess) return e;
     }

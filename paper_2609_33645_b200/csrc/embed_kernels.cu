@@ -13,7 +13,9 @@
 //                  order.
 //   k_embed_grad_few  few tokens: all of it in one launch.  A CTA fills its rows with zeros, finds its own among all
 //                  tokens meanwhile and writes their sums behind the zeros.
-// Both directions are bound by HBM.
+// Both directions are bound by HBM where they are large (32,768 tokens of 151,936 x 2,560 bf16: 51.5 us, 5.9 TB/s; the
+// gradient of as many into 151,936 x 1,024: 70 us, 5.2 TB/s), by their launches where they are small (64 tokens: 2.7 us; 1,999 into
+// 5,003 x 510: 11 us, two launches and the chain from a token to its last partial sum).
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 #include "vec8.cuh"
@@ -377,7 +379,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, N >= 4 ? GRAD_PER_SM : 4) k_embe
   }
 }
 
-// Up to GRAD_FEW tokens.  Block (x, y) takes every gridDim.x-th piece of rows from piece x on, and columns y * GRAD_SLICE ..
+// Up to GRAD_FEW tokens (1 to 256 into 5,003 x 510 fp32: 4.3 to 6.4 us, by sorting 5.4 to 9.9).  Block (x, y) takes every gridDim.x-th piece of rows from piece x on, and columns y * GRAD_SLICE ..
 constexpr int GRAD_FEW = GRAD_THREADS;           // a token a thread
 constexpr int GRAD_SLICE = 1024;                 // columns of a block
 
@@ -558,10 +560,14 @@ cudaError_t grad_launch(const GradArgs& a, long long D, int group, bool add, cud
                     : grad_launch<G, T, 16 / (int)sizeof(G)>(a, D, add, stream);
 }
 
-constexpr long long FEW_BLOCKS = 148 * 8;
+// A block for 48 KB of dW, at least 8 an SM and at most 32: every one of them goes over all tokens, and few blocks leave the
+// memory idle at the end (148 * 8, 16 and 32 blocks: 10 MB 4.7, 6.6 and 11 us, 116 MB 18.4, 17.6 and 17.7, 622 MB 93, 89 and 88).
+constexpr long long FEW_BYTES = 49152, FEW_LEAST = 148 * 8, FEW_MOST = 148 * 32;
 template <typename G, typename T>
 cudaError_t few_launch(FewArgs a, int group, cudaStream_t stream) {
-  const long long slices = (a.D + GRAD_SLICE - 1) / GRAD_SLICE, most = (FEW_BLOCKS + slices - 1) / slices;
+  const long long pieces = a.accumulate ? 0 : a.V * a.D * (long long)sizeof(T) / FEW_BYTES;
+  const long long blocks = pieces < FEW_LEAST ? FEW_LEAST : pieces > FEW_MOST ? FEW_MOST : pieces;
+  const long long slices = (a.D + GRAD_SLICE - 1) / GRAD_SLICE, most = (blocks + slices - 1) / slices;
   a.zero = zero_args(a.dW, a.V, a.D, a.ld_w, sizeof(T), most);
   const dim3 grid((unsigned)(a.zero.pieces < most ? a.zero.pieces : most), (unsigned)slices);
   if (group == 1) k_embed_grad_few<G, T, 1><<<grid, GRAD_THREADS, 0, stream>>>(a);

@@ -8,10 +8,12 @@
 //     shared memory, while its first ring of the head is on its way: one launch.
 //   few tokens (up to 128), CTAS = 1: the rows of the accumulators are channels (rows of the head), the columns tokens, tiles
 //     128 x 16 .. 128 x 128: the head streams once through a deep ring, and 32 lanes of a warp hold 32 neighbouring
-//     channels of a token, which is the order of C.  Bound by HBM.
+//     channels of a token, which is the order of C.  Bound by HBM (4 x 151,936 x 1,024: 31 us, 5.1 TB/s).
 //   many tokens, CTAS = 2: 256 tokens x 256 channels a CTA pair (cta_group::2), the rows are tokens, and results leave
 //     through shared memory and TMA stores as in the bf16 kernel (with channels as rows a result took 10 instructions and
-//     more: 512 x 151,936 x 512 113 us).  Bound by the tensor pipe, or by the results where sums are short.
+//     more: 512 x 151,936 x 512 113 us against 56).  Bound by the tensor pipe (2,048 x 151,936 x 4,096: 870 to 1,000 us under
+//     the power cap, 2.6 to 2.9 POP/s), or by the results where sums are short.  (72 and 128 tokens in pairs, 151,936 x 1,024: 38 and
+//     39 us against 32 and 35 as few.)
 #include "../../include/prunedctc.h"
 #include "i8_gemm.h"
 #include "pctc_internal.h"
@@ -129,13 +131,15 @@ void quantize_rows(const QuantArgs& a, cudaStream_t stream) {
   constexpr int per = QUANT_THREADS / GROUP;
   k_quantize<T, N, GROUP, NV><<<(unsigned)((a.rows + per - 1) / per), QUANT_THREADS, 0, stream>>>(a);
 }
-// A warp a row up to 128 pieces, a block up to 2,048.
+// A warp a row up to 128 pieces, a block up to 2,048; of few rows a block from 33 pieces on (128 x 1,024 bf16: 2.8 -> 2.0 us; 592:
+// 2.9 -> 2.4, 2,048: 3.4 -> 5.1).
+constexpr long long QUANT_FEW = 148 * 4;
 template <typename T, int N>
 void quantize_pieces(const QuantArgs& a, cudaStream_t stream) {
   const long long v = a.cols / N;
   if (v <= 32) quantize_rows<T, N, 32, 1>(a, stream);
-  else if (v <= 64) quantize_rows<T, N, 32, 2>(a, stream);
-  else if (v <= 128) quantize_rows<T, N, 32, 4>(a, stream);
+  else if (v <= 64 && a.rows > QUANT_FEW) quantize_rows<T, N, 32, 2>(a, stream);
+  else if (v <= 128 && a.rows > QUANT_FEW) quantize_rows<T, N, 32, 4>(a, stream);
   else if (v <= 256) quantize_rows<T, N, 256, 1>(a, stream);
   else if (v <= 512) quantize_rows<T, N, 256, 2>(a, stream);
   else if (v <= 1024) quantize_rows<T, N, 256, 4>(a, stream);
