@@ -10,12 +10,12 @@
 //                  other CTAs of that launch fill dW with zeros, whatever the tokens are.
 //   k_embed_grad   a thread sums eight columns over a window of sorted positions.  A token whose positions pass the
 //                  end of a window leaves a partial sum for each window, and the last of its threads adds these up in
-//                  order.
+//                  order (in two steps where they are many).
 //   k_embed_grad_few  few tokens: all of it in one launch.  A CTA fills its rows with zeros, finds its own among all
 //                  tokens meanwhile and writes their sums behind the zeros.
 // Both directions are bound by HBM where they are large (32,768 tokens of 151,936 x 2,560 bf16: 51.5 us, 5.9 TB/s; the
 // gradient of as many into 151,936 x 1,024: 70 us, 5.2 TB/s), by their launches where they are small (64 tokens: 2.7 us; 1,999 into
-// 5,003 x 510: 11 us, two launches and the chain from a token to its last partial sum).
+// 5,003 x 510: 12 us, two launches and the chain from a token to its last partial sum).
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 #include "vec8.cuh"
@@ -91,6 +91,7 @@ constexpr int SORT_BUCKETS = 148;                // ranges of the vocabulary: on
 constexpr int SORT_MAX_WIDTH = 2048;             // tokens of a range: a counter for each and every warp, 128 KB
 constexpr int SORT_AHEAD = 4;                    // groups of four tokens that a thread loads before it looks at the first
 constexpr int SORT_KEEP = 256;                   // tokens of its range that a warp keeps; one with more reads its run again
+                                                 // (three blocks an SM: with two 70,000 x 512 takes 23.8 us for 22.0)
 constexpr int SORT_RUN_BITS = 21;                // a kept token: 11 bits of token, 21 of position in the warp's run
 
 // Zeros into a matrix, in pieces of about ZERO_BYTES: of rows, or of the bytes of a matrix without gaps.
@@ -139,7 +140,7 @@ __device__ __forceinline__ int4 four_tokens(const int* tokens, bool aligned, int
                    p + 3 < p1 ? tokens[p + 3] : -1);
 }
 
-__global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) {
+__global__ void __launch_bounds__(SORT_THREADS, 3) k_sort_tokens(const SortArgs a) {
   extern __shared__ int count[];                 // [SORT_WARPS][width]: counts, then where each warp's next one goes
   __shared__ unsigned kept[SORT_WARPS][SORT_KEEP];
   __shared__ int below_sum[SORT_WARPS], scan_sum[SORT_WARPS], count_end;
@@ -162,33 +163,39 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
   const unsigned lower = (1u << lane) - 1;
   int* mine = count + warp * a.width;
   int below = 0, n = 0;
-  for (int p = p0 + lane * 4; p - lane * 4 < p1; p += 128 * SORT_AHEAD) {
-    int4 t[SORT_AHEAD];
+  // 128 tokens a step, SORT_AHEAD steps loaded at once; f(v, first position of the lane) for those with a token of the range
+  const auto for_all = [&](auto f) {
+    for (int p = p0 + lane * 4; p - lane * 4 < p1; p += 128 * SORT_AHEAD) {
+      int4 t[SORT_AHEAD];
 #pragma unroll
-    for (int k = 0; k < SORT_AHEAD; ++k) t[k] = four_tokens(a.tokens, aligned, p + k * 128, p1);
+      for (int k = 0; k < SORT_AHEAD; ++k) t[k] = four_tokens(a.tokens, aligned, p + k * 128, p1);
 #pragma unroll
-    for (int k = 0; k < SORT_AHEAD; ++k) {
-      const unsigned v[4] = {(unsigned)t[k].x - lo, (unsigned)t[k].y - lo, (unsigned)t[k].z - lo, (unsigned)t[k].w - lo};
-      const bool any = v[0] < width || v[1] < width || v[2] < width || v[3] < width;
-      below += ((unsigned)t[k].x < lo) + ((unsigned)t[k].y < lo) + ((unsigned)t[k].z < lo) + ((unsigned)t[k].w < lo);   // none below 0
-      if (!__any_sync(0xffffffffu, any)) continue;
-      int before = 0, all = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const unsigned hits = __ballot_sync(0xffffffffu, v[j] < width);
-        before += __popc(hits & lower);
-        all += __popc(hits);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (v[j] < width) {
-          atomicAdd(&mine[v[j]], 1);
-          const int at = n + before++;
-          if (at < SORT_KEEP) kept[warp][at] = (v[j] << SORT_RUN_BITS) | (unsigned)(p + k * 128 + j - p0);
-        }
-      n += all;
+      for (int k = 0; k < SORT_AHEAD; ++k) f(t[k], p + k * 128);
     }
-  }
+  };
+  // keeps those of the four that are in the range, in order, behind the n that are there; counts them
+  const auto keep = [&](const unsigned (&v)[4], unsigned position, bool count_them) {
+    int before = n;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned hits = __ballot_sync(0xffffffffu, v[j] < width);
+      before += __popc(hits & lower);
+      n += __popc(hits);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (v[j] < width) {
+        if (count_them) atomicAdd(&mine[v[j]], 1);
+        if (before < SORT_KEEP) kept[warp][before] = (v[j] << SORT_RUN_BITS) | (position + j);
+        ++before;
+      }
+  };
+  for_all([&](const int4& t, int p) {
+    const unsigned v[4] = {(unsigned)t.x - lo, (unsigned)t.y - lo, (unsigned)t.z - lo, (unsigned)t.w - lo};
+    below += ((unsigned)t.x < lo) + ((unsigned)t.y < lo) + ((unsigned)t.z < lo) + ((unsigned)t.w < lo);   // none below 0
+    if (!__any_sync(0xffffffffu, v[0] < width || v[1] < width || v[2] < width || v[3] < width)) return;
+    keep(v, (unsigned)(p - p0), true);
+  });
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) below_sum[warp] = below;
   __syncthreads();
@@ -229,33 +236,41 @@ __global__ void __launch_bounds__(SORT_THREADS) k_sort_tokens(const SortArgs a) 
   if (lo + (long long)width == a.V)              // positions without a token
     for (int i = count_end + threadIdx.x; i < a.M; i += SORT_THREADS) a.sorted[i] = make_int2(0, -1);
 
-  // 32 of the warp's tokens in order: equal ones by lane
-  const auto place = [&](bool there, int key, int position) {
-    const unsigned hits = __ballot_sync(0xffffffffu, there);
-    if (there) {
-      const unsigned equal = __match_any_sync(hits, key);
-      const int rank = __popc(equal & lower), to = mine[key] + rank;
-      __syncwarp(hits);
-      if (rank == 0) mine[key] = to + __popc(equal);
-      a.sorted[to] = make_int2(position, (int)lo + key);
-    }
+  // the kept ones, 32 at a time: equal ones by lane
+  const auto place = [&](int from) {
     __syncwarp();
+    for (int i = lane; i - lane < n; i += 32) {
+      const bool there = i < n;
+      const unsigned x = there ? kept[warp][i] : 0u;
+      const int key = (int)(x >> SORT_RUN_BITS);
+      const unsigned hits = __ballot_sync(0xffffffffu, there);
+      if (there) {
+        const unsigned equal = __match_any_sync(hits, key);
+        const int rank = __popc(equal & lower), to = mine[key] + rank;
+        __syncwarp(hits);
+        if (rank == 0) mine[key] = to + __popc(equal);
+        a.sorted[to] = make_int2(from + (int)(x & ((1u << SORT_RUN_BITS) - 1)), (int)lo + key);
+      }
+      __syncwarp();
+    }
+    n = 0;
   };
   if (n <= SORT_KEEP && run <= 1 << SORT_RUN_BITS) {
-    for (int i = lane; i - lane < n; i += 32) {
-      const unsigned x = i < n ? kept[warp][i] : 0u;
-      place(i < n, (int)(x >> SORT_RUN_BITS), p0 + (int)(x & ((1u << SORT_RUN_BITS) - 1)));
-    }
-  } else {
-    for (int p = p0 + lane; p - lane < p1; p += 32 * SORT_AHEAD) {
-      unsigned v[SORT_AHEAD];
-#pragma unroll
-      for (int k = 0; k < SORT_AHEAD; ++k) v[k] = (unsigned)(p + k * 32 < p1 ? a.tokens[p + k * 32] : -1) - lo;
-#pragma unroll
-      for (int k = 0; k < SORT_AHEAD; ++k)
-        if (__any_sync(0xffffffffu, v[k] < width)) place(v[k] < width, (int)v[k], p + k * 32);
-    }
+    place(p0);
+    return;
   }
+  // more than are kept: once more over the run, in portions that fit
+  n = 0;
+  int from = p0;
+  for_all([&](const int4& t, int p) {
+    const unsigned v[4] = {(unsigned)t.x - lo, (unsigned)t.y - lo, (unsigned)t.z - lo, (unsigned)t.w - lo};
+    if (!__any_sync(0xffffffffu, v[0] < width || v[1] < width || v[2] < width || v[3] < width)) return;
+    const int first = p - lane * 4;
+    if (n > SORT_KEEP - 128 || first - from > (1 << SORT_RUN_BITS) - 128) place(from);
+    if (n == 0) from = first;
+    keep(v, (unsigned)(p - from), false);
+  });
+  place(from);
 }
 
 struct GradArgs {
@@ -264,7 +279,7 @@ struct GradArgs {
   const int2* sorted;
   const int* first;
   float* part;                                   // [windows][2][per_row * N]
-  int* arrived;                                  // [windows][per_row]
+  int* arrived;                                  // [windows][2][per_row]
   long long ld_g, ld_w, M;
   long long windows;
   unsigned per_row;                              // groups of N values a row
@@ -287,7 +302,9 @@ __device__ __forceinline__ void write_row(T* p, const float (&sum)[N], float sca
 
 constexpr int GRAD_THREADS = 256;
 constexpr int GRAD_AHEAD = 8;                    // rows that a thread loads before it adds the first; windows are a multiple of it
-constexpr int GRAD_MOST = 64;                    // sorted positions of a window, at most
+constexpr int GRAD_MOST = 64;                    // sorted positions of a window, at most (32: 70 -> 74 us)
+constexpr int GRAD_JOIN = 32;                    // windows whose parts one thread adds up, of a token of more than twice as many (65,536
+                                                 // tokens of 500, as frequent as in text, D = 64: 96 -> 39 us)
 constexpr int GRAD_STAGED = 2048;                // sorted positions of a block's windows, at most
 constexpr int GRAD_PER_SM = 2;                   // blocks that run on an SM at a time: three spill registers (72 -> 74 us)
 constexpr int GRAD_WAVE = 148 * GRAD_PER_SM * GRAD_THREADS;
@@ -357,27 +374,54 @@ __global__ void __launch_bounds__(GRAD_THREADS, N >= 4 ? GRAD_PER_SM : 4) k_embe
     if (aside) VecN<float, N>::store(part, sum); else VecN<float, N>::store(part, head_sum);
   }
   if (tail && !aside) VecN<float, N>::store(part + width, sum);
-  // whoever comes last adds the parts of a token up, in the order of the windows
+  // Whoever comes last adds up the parts of a token, in the order of the windows.  Those of a token of more than 2 GRAD_JOIN windows
+  // are added up by GRAD_JOIN of them (from every multiple of it on), and these sums by the last of these.  A part's place and
+  // counter are those of its first window.
   __threadfence();
+  constexpr int JOIN_AHEAD = N == 8 ? 4 : 8;     // parts loaded at once
+  float* parts = a.part + (long long)c * N;
 #pragma unroll 1
   for (int e = 0; e < 2; ++e) {
     if (e == 0 ? !head : !tail || aside) continue;
     const int2 range = e == 0 ? head_range : tail_range;
-    const long long w0 = range.x / a.window, w1 = (range.y - 1) / a.window;
-    if (atomicAdd(&a.arrived[w0 * a.per_row + c], 1) != (int)(w1 - w0)) continue;
-    __threadfence();
-    float all[N] = {};
-    const float* p = a.part + (w0 * 2 + 1) * width + (long long)c * N;
-    for (long long u = w0; u <= w1; u += GRAD_AHEAD) {
-      VecN<float, N> q[GRAD_AHEAD];
-#pragma unroll
-      for (int k = 0; k < GRAD_AHEAD; ++k)
-        if (u + k <= w1) q[k].load_l2(u + k == w0 ? p : p + ((u + k - w0) * 2 - 1) * width);
-#pragma unroll
-      for (int k = 0; k < GRAD_AHEAD; ++k)
-        if (u + k <= w1) q[k].add_to(all);
+    const int w0 = range.x / a.window, w1 = (range.y - 1) / a.window, start = (int)w & -GRAD_JOIN;
+    const bool all_at_once = w1 - w0 < 2 * GRAD_JOIN;
+    const int u0 = all_at_once || start < w0 ? w0 : start, u1 = all_at_once || start + GRAD_JOIN > w1 ? w1 : start + GRAD_JOIN - 1;
+    const auto place = [&](int u) { return (long long)(u * 2 + (u == w0 ? 1 : 0)); };
+    if (u1 > u0) {
+      if (atomicAdd(&a.arrived[place(u0) * a.per_row + c], 1) % (4 * GRAD_JOIN) != u1 - u0) continue;
+      __threadfence();
     }
-    write_row<ADD>(dW + (e == 0 ? v0 : last) * a.ld_w, all, a.scale);
+    // first the parts of windows u0 .. u1, then the sums at w0 and at every multiple of GRAD_JOIN behind it
+    int first = u0, base = u0, step = 1, n = u1 - u0 + 1;
+    bool whole = u0 == w0 && u1 == w1;
+#pragma unroll 1
+    while (true) {
+      float all[N] = {};
+#pragma unroll 1
+      for (int i = 0; i < n; i += JOIN_AHEAD) {
+        VecN<float, N> q[JOIN_AHEAD];
+#pragma unroll
+        for (int k = 0; k < JOIN_AHEAD; ++k)
+          if (i + k < n) q[k].load_l2(parts + place(i + k == 0 ? first : base + (i + k) * step) * width);
+#pragma unroll
+        for (int k = 0; k < JOIN_AHEAD; ++k)
+          if (i + k < n) q[k].add_to(all);
+      }
+      if (whole) {
+        write_row<ADD>(dW + (e == 0 ? v0 : last) * a.ld_w, all, a.scale);
+        break;
+      }
+      VecN<float, N>::store(parts + place(u0) * width, all);
+      __threadfence();
+      base = w0 & -GRAD_JOIN;
+      n = (w1 - base) / GRAD_JOIN + 1;
+      if (atomicAdd(&a.arrived[place(w0) * a.per_row + c], 4 * GRAD_JOIN) / (4 * GRAD_JOIN) != n - 1) break;
+      __threadfence();
+      first = w0;
+      step = GRAD_JOIN;
+      whole = true;
+    }
   }
 }
 
@@ -487,7 +531,7 @@ GradPlan grad_plan(const pctc_embed_t* p) {
   const auto take = [&](size_t bytes) { const size_t r = o; o += up(bytes); return r; };
   g.sorted = take((size_t)p->M * 8);
   g.first = take(((size_t)p->V + 1) * 4);
-  g.arrived = take((size_t)g.windows * p->D * 4);       // a counter a group of eight, or a value
+  g.arrived = take((size_t)g.windows * 2 * p->D * 4);   // a counter a group of values, or a value
   g.part = take((size_t)g.windows * 2 * p->D * 4);
   g.total = o;
   return g;
@@ -664,7 +708,7 @@ pctc_status_t pctc_embed_grad(const pctc_embed_t* p, const int32_t* tokens, cons
   s.sorted = (int2*)(w + g.sorted);
   s.first = (int*)(w + g.first);
   s.clear = (int*)(w + g.arrived);
-  s.n_clear = g.windows * (p->D / group);
+  s.n_clear = g.windows * 2 * (p->D / group);
   const int smem = SORT_WARPS * s.width * 4;
   static std::atomic<bool> configured[MAX_DEVICES];
   const int dev = current_device();

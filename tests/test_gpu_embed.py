@@ -143,7 +143,8 @@ def check_grad(got, t, g, V, scale, base=None):
 @pytest.mark.parametrize("M,V,D,none,hot", [
     (1, 1, 1, 0.0, 0.0), (1, 1000, 64, 0.0, 0.0), (5, 3, 24, 0.0, 0.0), (100, 1, 40, 0.0, 0.0), (513, 40, 8, 0.2, 0.0),
     (1000, 5003, 510, 0.1, 0.0), (2049, 300, 72, 0.0, 0.7), (3000, 151936, 16, 0.2, 0.0), (4097, 500_000, 8, 0.0, 0.3),
-    (20_000, 2000, 256, 0.2, 0.0), (70_001, 50, 33, 0.5, 0.0), (9000, 1000, 128, 0.0, 1.0), (300, 700, 100, 1.0, 0.0)])
+    (20_000, 2000, 256, 0.2, 0.0), (70_001, 50, 33, 0.5, 0.0), (9000, 1000, 128, 0.0, 1.0), (300, 700, 100, 1.0, 0.0),
+    (262_145, 7, 8, 0.0, 0.5), (40_000, 3, 64, 0.3, 0.0), (2600, 2, 512, 0.0, 0.0), (66_000, 30, 1, 0.1, 0.3)])
 @pytest.mark.parametrize("dtype,to", [(BF, BF), (FP, FP), (BF, FP), (FP, BF)])
 def test_gradient(M, V, D, none, hot, dtype, to):
     t, g = ids((M,), V, 3, none, hot), rows(M, D, dtype, 4)
@@ -153,6 +154,15 @@ def test_gradient(M, V, D, none, hot, dtype, to):
         check_grad(r["dW"], t, g, V, scale)
         again = binding.embed_grad(t, g, dW=torch.full((V, D), float("nan"), device=DEV, dtype=to), scale=scale, workspace=r["workspace"])
         assert torch.equal(again["dW"], r["dW"])
+
+
+def test_gradient_of_very_many_tokens():
+    """More than a warp of the sort has bits for the positions of."""
+    M, V = 40_000_000, 5
+    t, g = ids((M,), V, 1, 0.1, 0.2), rows(M, 1, FP, 2)
+    r = binding.embed_grad(t, g, V)
+    check_grad(r["dW"], t, g, V, 1.0)
+    assert torch.equal(binding.embed_grad(t, g, V, workspace=r["workspace"])["dW"], r["dW"])
 
 
 @pytest.mark.parametrize("M,V,D", [(700, 500, 64), (700, 500, 63), (5000, 37, 40)])
