@@ -482,7 +482,8 @@ pctc_status_t pctc_embed(const pctc_embed_t* problem, const int32_t* tokens, con
 
 /*
  * Its gradient:  dW[v,:] = T(scale * sum over i with tokens[i] == v of grad[i,:])  (+ dW[v,:] with accumulate = 1).
- * Sums are fp32, in ascending i cut at places that depend on M and D alone, rounded once: repeated calls agree bit for bit.
+ * Sums are fp32, in ascending i cut at places that depend on M, D and the tokens alone, rounded once: repeated calls agree bit
+ * for bit.
  *   workspace: >= pctc_embed_grad_workspace_bytes(), 256-byte aligned; nothing in it outlives the call (calls that may
  *   run at the same time, replays of captured ones among them, need one each).  dW and the workspace may overlap nothing else.
  */

@@ -425,7 +425,8 @@ __global__ void __launch_bounds__(GRAD_THREADS, N >= 4 ? GRAD_PER_SM : 4) k_embe
   }
 }
 
-// Up to GRAD_FEW tokens (1 to 256 into 5,003 x 510 fp32: 4.3 to 6.4 us, by sorting 5.4 to 9.9).  Block (x, y) takes every gridDim.x-th piece of rows from piece x on, and columns y * GRAD_SLICE ..
+// Up to GRAD_FEW tokens (1 to 256 into 5,003 x 510 fp32: 4.3 to 6.4 us, by sorting 5.4 to 9.9).  Block (x, y) takes every
+// gridDim.x-th piece of rows from piece x on, and columns y * GRAD_SLICE ..
 constexpr int GRAD_FEW = GRAD_THREADS;           // a token a thread
 constexpr int GRAD_SLICE = 1024;                 // columns of a block
 

@@ -4,8 +4,8 @@
 //
 // k_i8_gemm is a persistent tcgen05 kernel (kind::i8) in three forms; roles, ring and bounded waits are those of the bf16
 // kernel in umma_gemm.cu.
-//   very few tokens (up to 8,192 values, of rows that are read in eights): as below, and every CTA quantizes the tokens itself, into the operand's place in
-//     shared memory, while its first ring of the head is on its way: one launch.
+//   very few tokens (up to 8,192 values, of rows that are read in eights): as below, and every CTA quantizes the tokens itself,
+//     into the operand's place in shared memory, while its first ring of the head is on its way: one launch.
 //   few tokens (up to 128), CTAS = 1: the rows of the accumulators are channels (rows of the head), the columns tokens, tiles
 //     128 x 16 .. 128 x 128: the head streams once through a deep ring, and 32 lanes of a warp hold 32 neighbouring
 //     channels of a token, which is the order of C.  Bound by HBM (4 x 151,936 x 1,024: 31 us, 5.1 TB/s).
@@ -868,7 +868,8 @@ cudaError_t i8_gemm(const signed char* A, long long lda, const float* a_scale, c
 
 // Whether the product quantizes so many tokens itself: they are columns of one tile, and fit beside a ring of 100 KB and more.
 bool i8_own_tokens(const void* x, long long ld_x, bool bf16, int m, int k) {
-  return m <= I8_ROWS && (long long)m * k <= (in_eights(x, ld_x, bf16, k) ? I8_OWN_VALUES : I8_OWN_SINGLE) && (long long)(m + 15) / 16 * 16 * ((k + 127) / 128 * 128) <= 98304;
+  return m <= I8_ROWS && (long long)m * k <= (in_eights(x, ld_x, bf16, k) ? I8_OWN_VALUES : I8_OWN_SINGLE) &&
+         (long long)(m + 15) / 16 * 16 * ((k + 127) / 128 * 128) <= 98304;
 }
 
 cudaError_t i8_quantize(const void* x, bool bf16, long long rows, long long cols, long long ld_x, signed char* q, long long ld_q,
