@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(EMBED_THREADS) k_embed(const EmbedArgs a) {
 // ---------------------------------------------------------------------------------------------
 constexpr int SORT_THREADS = 512;
 constexpr int SORT_WARPS = SORT_THREADS / 32;
+static_assert(SORT_WARPS % 8 == 0, "the counters of eight warps at a time");
 constexpr int SORT_BUCKETS = 148;                // ranges of the vocabulary: one CTA on every SM of a B200
 constexpr int SORT_MAX_WIDTH = 2048;             // tokens of a range: a counter for each and every warp, 128 KB
 constexpr int SORT_AHEAD = 4;                    // groups of four tokens that a thread loads before it looks at the first
@@ -219,13 +220,16 @@ __global__ void __launch_bounds__(SORT_THREADS, 3) k_sort_tokens(const SortArgs 
   for (int w = 0; w < SORT_WARPS; ++w) at += below_sum[w] + (w < warp ? scan_sum[w] : 0);
   for (unsigned k = k0; k < k0 + per && k < width; ++k) {
     a.first[lo + k] = at;
-    int c[SORT_WARPS];
 #pragma unroll
-    for (int w = 0; w < SORT_WARPS; ++w) c[w] = count[w * a.width + k];
+    for (int w0 = 0; w0 < SORT_WARPS; w0 += 8) {
+      int c[8];
 #pragma unroll
-    for (int w = 0; w < SORT_WARPS; ++w) {
-      count[w * a.width + k] = at;
-      at += c[w];
+      for (int w = 0; w < 8; ++w) c[w] = count[(w0 + w) * a.width + k];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        count[(w0 + w) * a.width + k] = at;
+        at += c[w];
+      }
     }
   }
   if (k0 < width && k0 + per >= width) {
