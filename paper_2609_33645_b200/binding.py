@@ -747,7 +747,7 @@ def embed(tokens, W, *, scale=1.0, dtype=None, out=None):
 def embed_grad(tokens, grad, vocab=None, *, dW=None, scale=1.0, accumulate=False, dtype=None, workspace=None):
     """The gradient of embed with respect to W: dW[v] = scale * the sum of grad[i] over all i with tokens[i] == v.
 
-    grad [*tokens.shape, D] bf16 or fp32.  dW [V,D] is written whole (rows without a token: zeros), or, with
+    grad [*tokens.shape, D] bf16 or fp32, its rows one stride apart (an expanded view is refused: make it contiguous).  dW [V,D] is written whole (rows without a token: zeros), or, with
     accumulate=True, added to: a tied head's gradient as pruned_ctc_fwd_bwd has left it.  Without dW one is made for `vocab`
     rows, of type `dtype` (default grad's).  Sums are fp32 in a fixed order: repeated calls agree bit for bit.  Returns a
     dict: dW and the workspace (the given one, or a new one where that was too small), which later calls on the same stream may
@@ -763,7 +763,7 @@ def dropout(x, p, seed, *, offset=0, step=None, residual=None, out=None):
 
     The mask is a function of seed, offset (integers, taken modulo 2^64) and a value's index alone (prunedctc.h has the
     formula); it is never stored.  p counts in steps of 1/65536, and the scale is exact for the step taken.  x bf16 or fp32
-    [..., D] whose rows lie one stride apart, residual and out likewise; out may be x or residual.  step: one int64 on the
+    [..., D] whose rows lie one stride apart (an expanded view is refused), residual and out likewise; out may be x or residual.  step: one int64 on the
     device that is added to offset, for calls captured into a CUDA graph.  Not recorded by autograd; a written `out`'s
     version counts up.
     """
@@ -831,7 +831,7 @@ def matmul_i8(a, b, *, bias=None, dtype=None, status=None):
 
 
 def quantized_logits(hidden, head, *, bias=None, dtype=None, workspace=None):
-    """Logits [..., V] of states hidden [..., D] (bf16 or fp32) under a QuantizedHead: the states are quantized row by row
+    """Logits [..., V] of states hidden [..., D] (bf16 or fp32, rows one stride apart) under a QuantizedHead: the states are quantized row by row
     and multiplied in 8-bit integers.  dtype: bf16 or fp32 (default hidden's).  workspace: a uint8 CUDA tensor to use, refused
     if it is too small (its first word is the status word that workspace_status reads).  Not differentiable."""
     return _native().quantized_logits(hidden, head.q, head.scales, bias, dtype, workspace)[0]

@@ -580,15 +580,15 @@ RowView rows_of(const at::Tensor& t, const char* what) {
     return v;
   }
   if (v.cols > 1 && t.stride(-1) != 1) fail(PyExc_ValueError, "%s must be contiguous in its last dimension", what);
-  int64_t next = 0;                       // the stride that the next dimension outwards has to have; 0: any
+  int64_t next = 0;                       // the stride that the next dimension outwards has to have, behind the innermost one
   for (int64_t d = t.dim() - 2; d >= 0; --d) {
     if (t.size(d) == 1) continue;
-    if (next == 0) v.ld = t.stride(d);
+    if (v.rows == 1) v.ld = t.stride(d);
     else if (t.stride(d) != next) fail(PyExc_ValueError, "the rows of %s must lie one stride apart", what);
+    if (v.ld < v.cols) fail(PyExc_ValueError, "rows of %s overlap", what);   // (an expanded dimension has the stride 0)
     next = t.stride(d) * t.size(d);
     v.rows *= t.size(d);
   }
-  if (v.rows > 1 && v.ld < v.cols) fail(PyExc_ValueError, "rows of %s overlap", what);
   return v;
 }
 std::vector<int64_t> with_last(const at::Tensor& t, int64_t last, bool replace) {
@@ -645,10 +645,10 @@ PyObject* embed(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const std::vector<int64_t> shape = with_last(t, W.size(1), false);
   if (given.defined() && (given.device() != dev || given.scalar_type() != type || !is_float(type) || !has_shape(given, shape)))
     fail(PyExc_ValueError, "out must be [*tokens.shape, D] of the asked type (bf16 or fp32) on the tokens' device");
+  const int64_t ld_out = given.defined() ? rows_of(given, "out").ld : W.size(1);
   const c10::cuda::CUDAGuard guard(dev);
   const at::Tensor out = given.defined() ? given : empty(shape, type, dev);
-  const RowView o = rows_of(out, "out");
-  const pctc_embed_t p{t.numel(), W.size(0), W.size(1), w.ld, o.ld, kind_of(W.scalar_type()), kind_of(type), (float)real(a[3]), 0};
+  const pctc_embed_t p{t.numel(), W.size(0), W.size(1), w.ld, ld_out, kind_of(W.scalar_type()), kind_of(type), (float)real(a[3]), 0};
   check(api.embed(&p, (const int32_t*)ptr(t), ptr(W), (const float*)ptr(s), ptr(out), stream_of(dev)), "pctc_embed");
   if (given.defined()) written(given);
   return THPVariable_Wrap(out);
@@ -673,9 +673,9 @@ PyObject* embed_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
                           !is_float(type) || (a[2] != Py_None && integer(a[2]) != V)))
     fail(PyExc_ValueError, "dW must be [V, D], bf16 or fp32, on the tokens' device");
   if (V < 1 || D < 1) fail(PyExc_ValueError, "vocab and D must be at least 1");
-  const c10::cuda::CUDAGuard guard(dev);
   const RowView x = rows_of(g, "grad");
   const int64_t ld_w = given.defined() ? rows_of(given, "dW").ld : D;
+  const c10::cuda::CUDAGuard guard(dev);
   const pctc_embed_t p{t.numel(), V, D, ld_w, x.ld, kind_of(type), kind_of(g.scalar_type()), (float)real(a[4]), accumulate ? 1 : 0};
   size_t need = 0;
   check(api.embed_grad_workspace_bytes(&p, &need), "pctc_embed_grad_workspace_bytes");
@@ -698,12 +698,12 @@ PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
   for (const at::Tensor* t : {&res, &given})
     if (t->defined() && (t->device() != dev || t->scalar_type() != x.scalar_type() || !t->sizes().equals(x.sizes())))
       fail(PyExc_ValueError, "residual and out must be of x's shape, type and device");
+  const RowView v = rows_of(x, "x");
+  const int64_t ld_res = res.defined() ? rows_of(res, "residual").ld : 1;
+  const int64_t ld_out = given.defined() ? rows_of(given, "out").ld : std::max<int64_t>(1, v.cols);
   const c10::cuda::CUDAGuard guard(dev);
   const at::Tensor out = given.defined() ? given : empty(x.sizes(), x.scalar_type(), dev);
-  const RowView v = rows_of(x, "x"), o = rows_of(out, "out");
-  RowView r;
-  if (res.defined()) r = rows_of(res, "residual");
-  pctc_dropout_t p{v.rows, v.cols, v.ld, r.ld, o.ld, kind_of(x.scalar_type()), 0, real(a[1]), word(a[2], "seed"), word(a[3], "offset")};
+  pctc_dropout_t p{v.rows, v.cols, v.ld, ld_res, ld_out, kind_of(x.scalar_type()), 0, real(a[1]), word(a[2], "seed"), word(a[3], "offset")};
   check(api.dropout(&p, ptr(x), ptr(res), (const int64_t*)ptr(step), ptr(out), stream_of(dev)), "pctc_dropout");
   if (given.defined()) written(given);
   return THPVariable_Wrap(out);

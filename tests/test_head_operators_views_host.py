@@ -1,0 +1,46 @@
+"""Views that the binding of the operators around the head's matrix must not hand on, without a GPU: tensors that have a
+device, a shape and strides, but no memory."""
+
+import pytest
+import torch
+from torch._subclasses import FakeTensorMode
+
+from paper_2609_33645_b200 import binding
+
+
+def empty(*shape, dtype=torch.float32):
+    with FakeTensorMode():
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+HEAD = (40, 16)
+VIEWS = [
+    ((3, 1, 16), (3, 5, 16)),            # a middle dimension: what the gradient of x.sum(1) looks like
+    ((1, 5, 16), (3, 5, 16)),            # the outermost one
+    ((1, 1, 16), (3, 5, 16)),            # both
+    ((2, 1, 4, 16), (2, 3, 4, 16)),
+    ((2, 3, 1, 16), (2, 3, 4, 16)),
+    ((3, 1, 1), (3, 5, 1)),              # rows of one value
+]
+CALLS = dict(
+    embed_out=lambda v: binding.embed(empty(*v.shape[:-1], dtype=torch.int32), empty(40, v.shape[-1]), out=v),
+    embed_grad=lambda v: binding.embed_grad(empty(*v.shape[:-1], dtype=torch.int32), v, 40),
+    dropout=lambda v: binding.dropout(v, 0.1, 1),
+    dropout_residual=lambda v: binding.dropout(empty(*v.shape), 0.1, 1, residual=v),
+    dropout_out=lambda v: binding.dropout(empty(*v.shape), 0.1, 1, out=v),
+    quantized_logits=lambda v: binding.quantized_logits(v, binding.QuantizedHead(empty(40, v.shape[-1], dtype=torch.int8), empty(40))),
+)
+
+
+@pytest.mark.parametrize("first,shape", VIEWS)
+@pytest.mark.parametrize("name", CALLS)
+def test_expanded_views_are_refused(lib, name, first, shape):
+    with pytest.raises(ValueError, match="one stride apart|overlap"):
+        CALLS[name](empty(*first).expand(shape))
+
+
+def test_expanded_matrices_are_refused(lib):
+    tokens, row = empty(3, dtype=torch.int32), empty(1, 16).expand(HEAD)
+    for call in (lambda: binding.embed(tokens, row), lambda: binding.embed_grad(tokens, empty(3, 16), dW=row), lambda: binding.quantize_rows(row)):
+        with pytest.raises(ValueError, match="overlap"):
+            call()
