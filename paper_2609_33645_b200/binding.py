@@ -481,7 +481,7 @@ def _pitch(q) -> int:
     return int(q.stride(0)) if q.shape[0] > 1 else (int(q.shape[1]) + 15) // 16 * 16
 
 
-def _checked_head(head: QuantizedHead, hidden) -> QuantizedHead:
+def _checked_head(head: QuantizedHead, hidden, bias) -> QuantizedHead:
     import torch
 
     q, scales = head
@@ -493,6 +493,9 @@ def _checked_head(head: QuantizedHead, hidden) -> QuantizedHead:
         raise ValueError("a quantized head's scales must be contiguous fp32 [V] on the device of hidden")
     if q.shape[1] != hidden.shape[-1]:
         raise ValueError("hidden must be [N, T, D] for a head [V, D]")
+    if bias is not None and (bias.dtype != hidden.dtype or tuple(bias.shape) != (q.shape[0],) or not bias.is_contiguous()
+                             or bias.device != hidden.device):
+        raise ValueError("bias must be contiguous [V], of the type of hidden and on its device")
     return head
 
 
@@ -533,13 +536,13 @@ def topk_decode(hidden, W, bias, input_lengths, k, *, chunk=0, gemm_path=GEMM_AU
     """The k best classes of every frame (k in 1, 2, 4, 8) and their log-probabilities under the
     full-vocabulary softmax: device tensors classes [N,T,k] int32 (-1 on padded frames) and logprobs
     [N,T,k] fp32 (-inf there), plus the reusable workspace.  W may be a QuantizedHead: the frames are then quantized
-    row by row and multiplied in 8-bit integers (gemm_path does not matter)."""
+    row by row and multiplied in 8-bit integers (gemm_path does not matter); bias is of hidden's type."""
     import torch
 
     lib = load()
     head8 = W if isinstance(W, QuantizedHead) else None
     if head8 is not None:
-        W = _checked_head(head8, hidden).q
+        W = _checked_head(head8, hidden, bias).q
     dt = PCTC_BF16 if hidden.dtype == torch.bfloat16 else PCTC_FP32
     N, T, D = hidden.shape
     V = W.shape[0]

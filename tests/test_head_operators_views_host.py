@@ -44,3 +44,26 @@ def test_expanded_matrices_are_refused(lib):
     for call in (lambda: binding.embed(tokens, row), lambda: binding.embed_grad(tokens, empty(3, 16), dW=row), lambda: binding.quantize_rows(row)):
         with pytest.raises(ValueError, match="overlap"):
             call()
+
+
+@pytest.mark.parametrize("bias", [
+    lambda: empty(40),                                             # another type than that of the states
+    lambda: empty(40, dtype=torch.float16),
+    lambda: empty(39, dtype=torch.bfloat16),
+    lambda: empty(40, 1, dtype=torch.bfloat16),
+    lambda: empty(80, dtype=torch.bfloat16)[::2],
+    lambda: empty(1, dtype=torch.bfloat16).expand(40),
+    lambda: torch.zeros(40, dtype=torch.bfloat16),                 # not on the device
+])
+def test_recognition_with_the_head_in_8_bits_checks_its_bias(lib, bias):
+    hidden = empty(2, 3, 16, dtype=torch.bfloat16)
+    head = binding.QuantizedHead(empty(40, 16, dtype=torch.int8), empty(40))
+    for decode in (lambda b: binding.topk_decode(hidden, head, b, [3, 2], 4), lambda b: binding.beam_decode(hidden, head, b, [3, 2], 0, 4)):
+        with pytest.raises(ValueError, match="bias"):
+            decode(bias())
+
+
+def test_recognition_with_the_head_in_8_bits_checks_its_bias_beside_fp32_states(lib):
+    head = binding.QuantizedHead(empty(40, 16, dtype=torch.int8), empty(40))
+    with pytest.raises(ValueError, match="bias"):
+        binding.topk_decode(empty(2, 3, 16), head, empty(40, dtype=torch.bfloat16), [3, 2], 4)
