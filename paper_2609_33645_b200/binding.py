@@ -303,6 +303,8 @@ def pruned_ctc_fwd_bwd(hidden, W, bias, targets, input_lengths, target_lengths, 
     import torch
 
     lib = lib_handle or load()
+    if isinstance(W, QuantizedHead):
+        raise TypeError("the loss and its gradients need the matrix itself, not a QuantizedHead")
     if not (hidden.is_cuda and W.is_cuda and hidden.is_contiguous() and W.is_contiguous()):
         raise ValueError("hidden and W must be contiguous CUDA tensors")
     if hidden.dtype != W.dtype or hidden.dtype not in (torch.bfloat16, torch.float32):
@@ -508,6 +510,8 @@ def greedy_decode(hidden, W, bias, input_lengths, blank_id, *, gemm_path=GEMM_AU
     import torch
 
     lib = load()
+    if isinstance(W, QuantizedHead):
+        raise TypeError("greedy_decode takes no QuantizedHead: topk_decode with k=1 gives the best class of every frame")
     dt = PCTC_BF16 if hidden.dtype == torch.bfloat16 else PCTC_FP32
     N, T, D = hidden.shape
     V = W.shape[0]

@@ -67,3 +67,14 @@ def test_recognition_with_the_head_in_8_bits_checks_its_bias_beside_fp32_states(
     head = binding.QuantizedHead(empty(40, 16, dtype=torch.int8), empty(40))
     with pytest.raises(ValueError, match="bias"):
         binding.topk_decode(empty(2, 3, 16), head, empty(40, dtype=torch.bfloat16), [3, 2], 4)
+
+
+def test_calls_that_need_the_whole_matrix_refuse_one_in_8_bits(lib):
+    hidden, targets = empty(2, 3, 16), empty(2, 4, dtype=torch.int32)
+    head = binding.QuantizedHead(empty(40, 16, dtype=torch.int8), empty(40))
+    with pytest.raises(TypeError, match="topk_decode"):
+        binding.greedy_decode(hidden, head, None, [3, 2], 0)
+    with pytest.raises(TypeError, match="QuantizedHead"):
+        binding.pruned_ctc_fwd_bwd(hidden, head, None, targets, [3, 2], [1, 1], 0)
+    with pytest.raises(TypeError, match="QuantizedHead"):
+        binding.ctc_policy_fwd_bwd(hidden, head, None, targets, [3, 2], [1, 1], 0, empty(2), empty(2))
