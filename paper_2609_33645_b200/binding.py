@@ -501,6 +501,14 @@ def _checked_head(head: QuantizedHead, hidden, bias) -> QuantizedHead:
     return head
 
 
+def _check_types(hidden, W, bias) -> None:
+    """What a recognition call reads is of the states' type; another one would be read as that."""
+    import torch
+
+    if hidden.dtype not in (torch.bfloat16, torch.float32) or any(t is not None and t.dtype != hidden.dtype for t in (W, bias)):
+        raise ValueError("hidden, W and bias must be of one type, bf16 or fp32")
+
+
 def greedy_decode(hidden, W, bias, input_lengths, blank_id, *, gemm_path=GEMM_AUTO, workspace=None):
     """Greedy CTC recognition: frame arg-max of the head, repeats merged, blanks dropped.
 
@@ -512,6 +520,7 @@ def greedy_decode(hidden, W, bias, input_lengths, blank_id, *, gemm_path=GEMM_AU
     lib = load()
     if isinstance(W, QuantizedHead):
         raise TypeError("greedy_decode takes no QuantizedHead: topk_decode with k=1 gives the best class of every frame")
+    _check_types(hidden, W, bias)
     dt = PCTC_BF16 if hidden.dtype == torch.bfloat16 else PCTC_FP32
     N, T, D = hidden.shape
     V = W.shape[0]
@@ -547,6 +556,8 @@ def topk_decode(hidden, W, bias, input_lengths, k, *, chunk=0, gemm_path=GEMM_AU
     head8 = W if isinstance(W, QuantizedHead) else None
     if head8 is not None:
         W = _checked_head(head8, hidden, bias).q
+    else:
+        _check_types(hidden, W, bias)
     dt = PCTC_BF16 if hidden.dtype == torch.bfloat16 else PCTC_FP32
     N, T, D = hidden.shape
     V = W.shape[0]

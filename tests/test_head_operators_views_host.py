@@ -78,3 +78,14 @@ def test_calls_that_need_the_whole_matrix_refuse_one_in_8_bits(lib):
         binding.pruned_ctc_fwd_bwd(hidden, head, None, targets, [3, 2], [1, 1], 0)
     with pytest.raises(TypeError, match="QuantizedHead"):
         binding.ctc_policy_fwd_bwd(hidden, head, None, targets, [3, 2], [1, 1], 0, empty(2), empty(2))
+
+
+def test_recognition_checks_the_types_of_the_head(lib):
+    half = dict(dtype=torch.bfloat16)
+    for hidden, W, bias in ((empty(2, 3, 16, **half), empty(40, 16), None), (empty(2, 3, 16), empty(40, 16, **half), None),
+                            (empty(2, 3, 16, **half), empty(40, 16, **half), empty(40)), (empty(2, 3, 16), empty(40, 16), empty(40, **half)),
+                            (empty(2, 3, 16, dtype=torch.float16), empty(40, 16, dtype=torch.float16), None)):
+        for call in (lambda: binding.topk_decode(hidden, W, bias, [3, 2], 4), lambda: binding.greedy_decode(hidden, W, bias, [3, 2], 0),
+                     lambda: binding.beam_decode(hidden, W, bias, [3, 2], 0, 4)):
+            with pytest.raises(ValueError, match="one type"):
+                call()
