@@ -824,7 +824,7 @@ def ctc_policy_fwd_bwd(hidden, W, bias, targets, input_lengths, target_lengths, 
     """
     if kw.get("utt_weights") is not None or kw.get("forward_only"):
         raise ValueError("utt_weights are the policy loss's, and both passes are run")
-    given = {k: v for k, v in kw.items() if k not in ("accumulate_dW", "trace", "out")}
+    given = {k: v for k, v in kw.items() if k not in ("accumulate_dW", "trace", "out", "forward_only")}
     first = pruned_ctc_fwd_bwd(hidden, W, bias, targets, input_lengths, target_lengths, blank_id, forward_only=True, **given)
     policy = policy_loss(first["loss"], old_losses, advantages, ref_logp=ref_losses, mask=first["flags"] == 0, clip=clip,
                          kl_weight=kl_weight, reduction=reduction, negated=True)

@@ -273,3 +273,14 @@ def test_gains_that_cancel(N, T):
         got = float(call(k, reduction=reduction)["loss"])
         assert abs(want["loss"]) < 1e-3 * float(want["size"].sum())
         assert abs(got - want["loss"]) <= EPS * abs(want["loss"]) + 4 * EPS * part
+
+
+def test_a_policy_step_with_the_defaults_spelt_out():
+    batch = wl.make_batch(wl.reduced(wl.CONFIGS["c2"], name="policy", V=512, D=64, N=4, T_div=8, U_div=2), permute_ids=True)
+    dev = torch.device(DEV)
+    hidden, W = (torch.from_numpy(x).to(dev).to(torch.bfloat16) for x in (batch.hidden, batch.W))
+    args = (hidden, W, None, torch.from_numpy(batch.targets).to(dev), batch.input_lengths, batch.target_lengths, batch.blank,
+            torch.full((4,), 100.0, device=dev), torch.ones(4, device=dev))
+    a, b = binding.ctc_policy_fwd_bwd(*args), binding.ctc_policy_fwd_bwd(*args, forward_only=False, utt_weights=None, skip_dW=False)
+    for name in ("loss", "dH", "dW"):
+        assert torch.equal(a[name], b[name])

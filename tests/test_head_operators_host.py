@@ -220,3 +220,19 @@ def test_binding_refuses_what_it_cannot_hand_on(lib):
 def test_the_tests_own_generator_gives_the_published_words(counter, key, words):
     block, offset = counter[0] | counter[1] << 32, counter[2] | counter[3] << 32
     assert philox(block, offset, key[0] | key[1] << 32) == words
+
+
+def test_a_policy_step_takes_the_defaults_of_the_calls_it_is_made_of(monkeypatch):
+    import inspect
+
+    calls = []
+
+    def both(*args, forward_only=False, utt_weights=None, **kw):
+        calls.append((forward_only, utt_weights is None))
+        return dict(loss=torch.ones(2), flags=torch.zeros(2, dtype=torch.int32))
+    defaults = {k: p.default for k, p in inspect.signature(binding.pruned_ctc_fwd_bwd).parameters.items() if p.kind is p.KEYWORD_ONLY}
+    monkeypatch.setattr(binding, "pruned_ctc_fwd_bwd", both)
+    monkeypatch.setattr(binding, "policy_loss", lambda *args, **kw: dict(grad=torch.ones(2)))
+    assert defaults["forward_only"] is False and "utt_weights" in defaults
+    res = binding.ctc_policy_fwd_bwd(None, None, None, None, None, None, 0, None, None, **defaults)
+    assert calls == [(True, True), (False, False)] and "policy" in res
