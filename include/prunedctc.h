@@ -527,8 +527,10 @@ pctc_status_t pctc_dropout(const pctc_dropout_t* problem, const void* x, const v
  *   w = 1                                                               PCTC_POLICY_SUM.
  * At r = 1 + clip_high (1 - clip_low) exactly the gradient is that of the ratio.  What lies in uncounted places is not
  * looked at, and its gradient is 0; with nothing counted the loss is 0.  Counted values that are not finite give what the
- * formula gives (A = 0 times the ratio of a d that fp32 holds is 0, however large).  Differences are exact, ratios, gains A r and sums
- * 64 bits, KL terms and gradients fp32; repeated calls agree bit for bit.
+ * formula gives (A = 0 times the ratio, and kl_weight = 0 times the KL term, of finite values is 0, however large that is).
+ * Differences d are exact.  Gains A r and sums are 64 bits, and so are ratios but for what goes beyond 1 + d where |d| < 1, which is
+ * an fp32 series.  KL terms and gradients are fp32, and 64 bits from 2^100 on, so that a weight brings back what fp32 does not
+ * hold; repeated calls agree bit for bit.
  */
 typedef enum { PCTC_POLICY_TOKENS = 0, PCTC_POLICY_SEQUENCES = 1, PCTC_POLICY_SUM = 2 } pctc_policy_reduction_t;
 typedef struct {

@@ -8,7 +8,8 @@
 // The weights need the counts before the first gradient can be written: where a mask or lengths are given,
 // k_policy_count goes over them first (a quarter of a byte and less for a byte that the second pass moves).  k_policy then
 // reads every value once.  Few values are done by one cluster in one launch (k_policy_small).  Differences are exact (two
-// fp32 numbers), gains and sums 64 bits, in a fixed order; KL terms, which never cancel one another, 32 bits.  Large calls are
+// fp32 numbers), gains and sums 64 bits, in a fixed order; KL terms, which never cancel one another, and gradients 32 bits, or 64
+// where fp32 does not hold them before they have their weight (far_values).  Large calls are
 // bound by the arithmetic of a token and its loads, about alike (1M tokens with a mask: 14.5 us, of which 2.6 us are bytes at
 // HBM's rate), small ones by the launches (128 x 501: 7.8 us) and the length of one token's chain (64 values: 3.9 us).
 #include "../../include/prunedctc.h"
@@ -81,6 +82,7 @@ __device__ __forceinline__ int length_of(const PolicyArgs& a, long long n) {
 struct TokenSums {
   double gain = 0.0;
   float kl_loss = 0.f, kl = 0.f;                 // loss = kl_loss - gain
+  float size = 0.f;                              // magnitudes of the gradients without their weights
   int clipped = 0, count = 0;
 };
 
@@ -122,7 +124,7 @@ __device__ __forceinline__ float policy_token(const PolicyArgs& a, float x, floa
                                               TokenSums& s) {
   const float2 d = difference(x, x_old);         // exact: whether a ratio is clipped does not depend on a rounding
   const bool over = A > 0.f && above(d, a.log_high), under = A < 0.f && above(a.log_low, d), clipped = over || under;
-  // near 1 the ratio is 1 + d in 64 bits and what is left, a hundredth and less, in 32
+  // below e the ratio is 1 + d in 64 bits and what is left, up to 0.72 (a hundredth where |d| < 0.14), in 32
   const double dd = (double)d.x + (double)d.y;
   const double r = fabsf(d.x) < 1.f ? (1.0 + dd) + (double)exp_tail(d.x) : exp(dd);
   const float r32 = (float)r;
@@ -137,7 +139,14 @@ __device__ __forceinline__ float policy_token(const PolicyArgs& a, float x, floa
   }
   if (!none) s.gain = fma(wd, (double)A * (over ? a.high : under ? a.low : r), s.gain);
   s.clipped += clipped ? 1 : 0;
+  s.size += fabsf(g);
   return g;
+}
+// Whether fp32 held the gradients and KL terms of a thread's tokens without their weights with room to spare (not if one is NaN).
+// Where it did not, far_values does them over; ratios, gains and what they add up to are 64 bits in either case.
+constexpr float POLICY_FAR = 1.2676506e30f;      // 2^100
+__device__ __forceinline__ bool held(const PolicyArgs& a, const TokenSums& s) {
+  return s.size + (fabsf(a.kl_weight) + 1.f) * s.kl < POLICY_FAR;
 }
 
 // The weight of the tokens of a row with `count` of them, in 64 bits: 1 / n for a whole number n.
@@ -314,6 +323,43 @@ struct Values {
   }
 };
 
+// A thread's values first, first + step, ... (POLICY_EACH of each of `groups` groups that lie `group` apart) once more where fp32
+// was too short for one of them, in 64 bits: gradients, and what the KL terms add to the loss and to their sum.
+struct FarSums {
+  double loss, kl;
+};
+__device__ __noinline__ FarSums far_values(const PolicyArgs& a, long long first, int groups, int group, int step, double part) {
+  FarSums s{0.0, 0.0};
+  for (int j = 0; j < groups * POLICY_EACH; ++j) {
+    const long long i = first + (j / POLICY_EACH) * group + (j % POLICY_EACH) * step, n = i / a.T, c = i - n * a.T;
+    if (i >= a.total || c >= length_of(a, n) || (a.mask && a.mask[n * a.ld_mask + c] == 0)) continue;
+    const double wd = a.reduction == PCTC_POLICY_SEQUENCES ? weight_of(a, part, a.mask ? a.row_count[n] : length_of(a, n)) : part;
+    const float x = a.sign * a.logp[n * a.ld_logp + c], A = a.ld_adv ? a.adv[n * a.ld_adv + c] : a.adv[n];
+    const float2 d = difference(x, a.sign * a.old_logp[n * a.ld_old + c]);
+    const bool none = (A > 0.f && above(d, a.log_high)) || (A < 0.f && above(a.log_low, d)) || (A == 0.f && fabsf(d.x) < CUDART_INF_F);
+    double g = none ? 0.0 : -(double)A * exp((double)d.x + (double)d.y);
+    if (a.ref) {
+      const float x_ref = a.sign * a.ref[n * a.ld_ref + c];
+      float kl32, e32;
+      kl_terms(x, x_ref, kl32, e32);
+      double kl = kl32, e = e32;
+      if (!(fabsf(e32) < POLICY_FAR)) {
+        const double f = (double)x_ref - (double)x;
+        e = expm1(f);
+        kl = isinf(e) ? e : e - f;
+      }
+      // (no 0 * inf where exp(f) overflows for a finite f)
+      if (a.kl_weight != 0.f || !(fabsf(x) < CUDART_INF_F && fabsf(x_ref) < CUDART_INF_F)) {
+        g -= a.kl_weight * e;
+        s.loss += wd * (a.kl_weight * kl);
+      }
+      s.kl += kl;
+    }
+    if (a.grad) a.grad[n * a.ld_grad + c] = (float)(a.sign * wd * g);
+  }
+  return s;
+}
+
 __device__ __forceinline__ void write_stats(const PolicyArgs& a, const BlockSums& s) {
   const double n = (double)max(s.count, 1);
   a.stats[0] = (float)s.loss;
@@ -323,7 +369,7 @@ __device__ __forceinline__ void write_stats(const PolicyArgs& a, const BlockSums
 }
 
 template <bool VEC, int GROUPS>
-__global__ void __launch_bounds__(POLICY_THREADS) k_policy(const PolicyArgs a) {
+__global__ void __launch_bounds__(POLICY_THREADS) k_policy(const __grid_constant__ PolicyArgs a) {
   __shared__ double shared_part;
   __shared__ bool last;
   const long long tile = (long long)blockIdx.x * (POLICY_THREADS * POLICY_EACH * GROUPS);
@@ -355,7 +401,10 @@ __global__ void __launch_bounds__(POLICY_THREADS) k_policy(const PolicyArgs a) {
   TokenSums s;
 #pragma unroll
   for (int i = 0; i < GROUPS; ++i) v[i].finish(a, part, s);
-  BlockSums sums = block_sum<POLICY_THREADS>((double)s.kl_loss - s.gain, (double)s.kl, s.count, s.clipped);
+  FarSums k{(double)s.kl_loss, (double)s.kl};
+  if (!held(a, s))
+    k = far_values(a, tile + threadIdx.x * (VEC ? POLICY_EACH : 1), GROUPS, POLICY_THREADS * POLICY_EACH, VEC ? 1 : POLICY_THREADS, part);
+  BlockSums sums = block_sum<POLICY_THREADS>(k.loss - s.gain, k.kl, s.count, s.clipped);
   if (threadIdx.x == 0) {
     BlockSums* p = a.partial + blockIdx.x;
     __stcg(reinterpret_cast<double2*>(p), make_double2(sums.loss, sums.kl));
@@ -383,7 +432,7 @@ __global__ void __launch_bounds__(POLICY_THREADS) k_policy(const PolicyArgs a) {
 
 // All of it by one cluster (of one block or more): the counts and the sums cross shared memory.
 template <bool VEC>
-__global__ void __launch_bounds__(POLICY_SMALL_THREADS) k_policy_small(const PolicyArgs a) {
+__global__ void __launch_bounds__(POLICY_SMALL_THREADS) k_policy_small(const __grid_constant__ PolicyArgs a) {
   __shared__ Totals counts;
   __shared__ double shared_part;
   __shared__ BlockSums block_sums;
@@ -404,8 +453,11 @@ __global__ void __launch_bounds__(POLICY_SMALL_THREADS) k_policy_small(const Pol
     __syncthreads();
   }
   TokenSums s;
-  v.finish(a, a.counting ? shared_part : weight_part(a, t), s);
-  BlockSums sums = block_sum<POLICY_SMALL_THREADS>((double)s.kl_loss - s.gain, (double)s.kl, s.count, s.clipped);
+  const double part = a.counting ? shared_part : weight_part(a, t);
+  v.finish(a, part, s);
+  FarSums k{(double)s.kl_loss, (double)s.kl};
+  if (!held(a, s)) k = far_values(a, VEC ? thread * POLICY_EACH : thread, 1, 0, VEC ? 1 : (int)threads, part);
+  BlockSums sums = block_sum<POLICY_SMALL_THREADS>(k.loss - s.gain, k.kl, s.count, s.clipped);
   if (blocks == 1) {
     if (threadIdx.x == 0) write_stats(a, sums);
     return;

@@ -284,3 +284,40 @@ def test_a_policy_step_with_the_defaults_spelt_out():
     a, b = binding.ctc_policy_fwd_bwd(*args), binding.ctc_policy_fwd_bwd(*args, forward_only=False, utt_weights=None, skip_dW=False)
     for name in ("loss", "dH", "dW"):
         assert torch.equal(a[name], b[name])
+
+
+@pytest.mark.parametrize("N,T", [(1, 40), (7, 33), (40, 100), (5, 4001), (300, 300)])
+@pytest.mark.parametrize("reduction", binding.POLICY_REDUCTIONS)
+def test_exponentials_beyond_fp32(N, T, reduction):
+    """Ratios and KL terms that fp32 does not hold, with weights that bring them back; kl_weight = 0 takes nothing of a KL term."""
+    for mask, kl_weight, small in ((False, 0.0, 1.0), (True, 0.0, 1.0), (False, 1e-6, 1e-3), (True, -1e-30, 1e-30)):
+        k = inputs(N, T, N + T, each=True, mask=mask, garbage=False)
+        g = torch.Generator(device=DEV).manual_seed(3)
+        far = torch.rand(N, T, generator=g, device=DEV) < 4 / (N * T)
+        far[N // 2 - 1 if mask else 0, :2] = True
+        if mask:
+            k["mask"][N // 2 - 1, :2] = True
+        k["logp"] = torch.where(far, k["old"] + 89.0, k["logp"])         # e^89 = 4.5e38
+        k["adv"] = torch.where(far, -small * 1e-3 * k["adv"].abs(), k["adv"])
+        up = torch.rand(N, T, generator=g, device=DEV) < 4 / (N * T)
+        up[N // 2 - 1 if mask else 0, 1:4] = True
+        k["ref"] = torch.where(up, k["logp"] + (88.9 if kl_weight == 0 else 95.0), k["ref"])
+        kw = dict(kl_weight=kl_weight, reduction=reduction, clip=(0.2, 0.2))
+        want = reference(**k, **kw)
+        r = call(k, **kw)
+        if want["kl"] > 3e38:                                            # the mean of the KL terms is beyond fp32 itself
+            assert math.isinf(float(r["kl"]))
+            want["kl"], want["kl_size"] = 0.0, 0.0
+            r["kl"] = torch.zeros(1)
+        assert want["grad"].abs().max() < 3e38 and abs(want["loss"]) < 3e38
+        check(r, want)
+
+
+def test_a_reference_that_is_only_watched_leaves_the_loss_alone():
+    """kl_weight = 0: the loss and its gradient are those without a reference, however far that is."""
+    for N, T in ((3, 5), (300, 300)):
+        k = inputs(N, T, 1, garbage=False)
+        far = k["logp"] + torch.linspace(-3000.0, 3000.0, N, device=DEV)[:, None]
+        r = call({**k, "ref": far}, kl_weight=0.0)
+        assert math.isinf(float(r["kl"]))
+        check({**r, "kl": torch.zeros(1)}, reference(**{**k, "ref": None}))
