@@ -803,7 +803,8 @@ def policy_loss(logp, old_logp, advantages, *, ref_logp=None, mask=None, lengths
     ("tokens"), over each row's and then over the rows that have any ("sequences"), or added up ("sum").
     negated: logp, old_logp, ref_logp are losses (-log p), as pruned_ctc_fwd_bwd returns them, and so is the gradient taken.
     Returns a dict of device tensors: loss, kl (mean of exp(f) - 1 - f), clipped (share of clipped tokens), each [1] fp32,
-    count [1] int32, grad (logp's shape, 0 where nothing is counted; not with want_grad=False), and the workspace.
+    count [1] int32, grad (logp's shape, 0 where nothing is counted; not with want_grad=False), and the workspace.  The
+    four scalars share one small allocation, the gradient and a workspace that is made here another.
     """
     kind = _REDUCTION.get(reduction)
     if kind is None:

@@ -321,3 +321,12 @@ def test_a_reference_that_is_only_watched_leaves_the_loss_alone():
         r = call({**k, "ref": far}, kl_weight=0.0)
         assert math.isinf(float(r["kl"]))
         check({**r, "kl": torch.zeros(1)}, reference(**{**k, "ref": None}))
+
+
+@pytest.mark.parametrize("N,T", [(64, 1), (8, 30), (3, 1600), (256, 4096)])
+def test_the_loss_does_not_hold_on_to_the_gradient_and_the_workspace(N, T):
+    k = inputs(N, T, 1, mask=True)
+    for r in (call(k), call(k, want_grad=False), call(k, workspace=call(k)["workspace"])):
+        for name in ("loss", "kl", "clipped", "count"):
+            assert r[name].untyped_storage().nbytes() <= 64 and r[name].shape == (1,)
+            assert all(r[name].untyped_storage().data_ptr() != r[o].untyped_storage().data_ptr() for o in ("grad", "workspace") if o in r)
