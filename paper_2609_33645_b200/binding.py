@@ -842,15 +842,34 @@ def quantize_rows(x):
     return QuantizedHead(*_native().quantize_rows(x))
 
 
-def matmul_i8(a, b, *, bias=None, dtype=None, status=None):
+def _raise_status(word) -> None:
+    code = workspace_status(word)
+    if code != 0:
+        raise PctcError(6 if code < 0x100 else 1, f"device status word {code:#x}")
+
+
+def matmul_i8(a, b, *, bias=None, dtype=None, status=None, check_status=False):
     """C[i,j] = sum_k a.q[i,k] b.q[j,k] * a.scales[i] * b.scales[j] + bias[j] for two QuantizedHeads (rows of tokens and of
     channels), fp32 or bf16 by `dtype`.  status: zeroed int32 CUDA tensor that receives a code if a bounded device wait
-    gives up."""
-    return _native().matmul_i8(a.q, a.scales, b.q, b.scales, bias, dtype, status)
+    gives up; check_status=True waits for the stream and raises then.  With neither, results that are incomplete for that reason go unnoticed.
+    """
+    if check_status and status is None:
+        import torch
+
+        status = torch.zeros(1, dtype=torch.int32, device=a.q.device)
+    out = _native().matmul_i8(a.q, a.scales, b.q, b.scales, bias, dtype, status)
+    if check_status:
+        _raise_status(status)
+    return out
 
 
-def quantized_logits(hidden, head, *, bias=None, dtype=None, workspace=None):
-    """Logits [..., V] of states hidden [..., D] (bf16 or fp32, rows one stride apart) under a QuantizedHead: the states are quantized row by row
-    and multiplied in 8-bit integers.  dtype: bf16 or fp32 (default hidden's).  workspace: a uint8 CUDA tensor to use, refused
-    if it is too small (its first word is the status word that workspace_status reads).  Not differentiable."""
-    return _native().quantized_logits(hidden, head.q, head.scales, bias, dtype, workspace)[0]
+def quantized_logits(hidden, head, *, bias=None, dtype=None, workspace=None, check_status=False):
+    """Logits [..., V] of states hidden [..., D] (bf16 or fp32, rows one stride apart) under a QuantizedHead: the states are
+    quantized row by row and multiplied in 8-bit integers.  dtype: bf16 or fp32 (default hidden's).  workspace: a uint8 CUDA
+    tensor to use, refused if it is too small; its first word is the status word that workspace_status reads.
+    check_status=True waits for the stream and raises if a bounded device wait gave up; with neither, logits that are incomplete
+    for that reason go unnoticed.  Not differentiable."""
+    out, workspace = _native().quantized_logits(hidden, head.q, head.scales, bias, dtype, workspace)
+    if check_status and out.numel() > 0:       # (a call without states writes no status)
+        _raise_status(workspace)
+    return out

@@ -299,3 +299,17 @@ def test_a_wait_that_runs_out_is_reported_and_the_kernel_returns(lib):
         assert short.pctc_workspace_status(vp(word), stream, ctypes.byref(host)) == 6 and host.value in (1, 2, 3, 4)
         torch.cuda.synchronize()                                  # the kernel has returned and the context is intact
         check(binding.matmul_i8(a, b), *product(a, b))
+
+
+def test_a_checked_product_is_the_product():
+    x, head = torch.randn(3, 64, generator=gen(1), device=DEV), binding.quantize_rows(torch.randn(300, 64, generator=gen(2), device=DEV))
+    for states in (x, x.repeat(100, 1), x[:0]):
+        assert torch.equal(binding.quantized_logits(states, head, check_status=True), binding.quantized_logits(states, head))
+    a, b = pair(30, 300, 64)
+    word = torch.zeros(1, dtype=torch.int32, device=DEV)
+    assert torch.equal(binding.matmul_i8(a, b, check_status=True), binding.matmul_i8(a, b))
+    assert torch.equal(binding.matmul_i8(a, b, status=word, check_status=True), binding.matmul_i8(a, b))
+    word.fill_(3)                                                 # as a wait that gave up leaves it
+    with pytest.raises(binding.PctcError) as e:
+        binding.matmul_i8(a, b, status=word, check_status=True)
+    assert e.value.status == 6

@@ -236,3 +236,37 @@ def test_a_policy_step_takes_the_defaults_of_the_calls_it_is_made_of(monkeypatch
     assert defaults["forward_only"] is False and "utt_weights" in defaults
     res = binding.ctc_policy_fwd_bwd(None, None, None, None, None, None, 0, None, None, **defaults)
     assert calls == [(True, True), (False, False)] and "policy" in res
+
+
+def test_products_report_a_wait_that_gave_up_if_they_are_asked(monkeypatch):
+    class Native:
+        def quantized_logits(self, x, q, scales, bias, dtype, workspace):
+            return torch.zeros(x.shape[0], 5), "the workspace" if workspace is None else workspace
+
+        def matmul_i8(self, a, sa, b, sb, bias, dtype, status):
+            words.append(status)
+            return torch.zeros(a.shape[0], 5)
+    read, words, code = [], [], [0]
+    monkeypatch.setattr(binding, "_native", Native)
+    monkeypatch.setattr(binding, "workspace_status", lambda w: (read.append(w), code[0])[1])
+    head = binding.QuantizedHead(torch.zeros(5, 16, dtype=torch.int8), torch.ones(5))
+    x = torch.zeros(3, 16)
+    binding.quantized_logits(x, head)
+    binding.matmul_i8(head, head)
+    assert read == [] and words == [None]
+    for code[0] in (0, 3):
+        for call, what in ((lambda **kw: binding.quantized_logits(x, head, **kw), "the workspace"),
+                           (lambda **kw: binding.quantized_logits(x, head, workspace="mine", **kw), "mine"),
+                           (lambda **kw: binding.matmul_i8(head, head, status="my word", **kw), "my word")):
+            if code[0]:
+                with pytest.raises(binding.PctcError) as e:
+                    call(check_status=True)
+                assert e.value.status == 6
+            else:
+                assert call(check_status=True).shape[1] == 5
+            assert read.pop() == what
+    with pytest.raises(binding.PctcError):                          # a word of its own where none is given
+        binding.matmul_i8(head, head, check_status=True)
+    assert words[-1].dtype == torch.int32 and int(words[-1].sum()) == 0
+    read.clear()
+    assert binding.quantized_logits(x[:0], head, check_status=True).shape == (0, 5) and read == []    # nothing ran, nothing was written
