@@ -61,12 +61,18 @@ __device__ __forceinline__ int quantize_one(float x, float f) {
   return max(-127, min(127, __float2int_rn(x * f)));
 }
 
+// The kernel behind this one reports to the status word when one of its waits has run out, 3,000 cycles (test build) or two seconds
+// after it has started: long after this.  (Zeroing it ahead of launch_next() costs a call of 37 tokens 0.6 of 12.6 us.)
+__device__ __forceinline__ void launch_next_and_clear(int* status) {
+  launch_next();
+  if (status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
+}
+
 // GROUP threads hold a row: NV pieces of N values each, loaded once.
 template <typename T, int N, int GROUP, int NV>
 __global__ void __launch_bounds__(QUANT_THREADS) k_quantize(const QuantArgs a) {
   __shared__ unsigned tops[QUANT_THREADS / 32];
-  launch_next();
-  if (a.clear && blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
+  launch_next_and_clear(a.clear);
   const long long row = (long long)blockIdx.x * (QUANT_THREADS / GROUP) + threadIdx.x / GROUP;
   const int at = threadIdx.x % GROUP, per_row = row < a.rows ? (int)(a.cols / N) : 0;
   VecN<T, N> v[NV];
@@ -108,8 +114,7 @@ __global__ void __launch_bounds__(QUANT_THREADS) k_quantize(const QuantArgs a) {
 template <typename T>
 __global__ void __launch_bounds__(QUANT_THREADS) k_quantize_any(const QuantArgs a) {
   __shared__ unsigned tops[QUANT_THREADS / 32];
-  launch_next();
-  if (a.clear && blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
+  launch_next_and_clear(a.clear);
   const long long row = blockIdx.x;
   const T* x = (const T*)a.x + row * a.ld_x;
   unsigned top = 0;
@@ -433,7 +438,8 @@ k_i8_gemm(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUten
     __syncwarp();
   }
   if constexpr (OWN) {
-    // nobody gives up a wait within two seconds, so that this comes before whatever is reported
+    // Blocks are started together and nobody gives up a wait within two seconds (PCTC_WAIT_LIMIT_CYCLES), so that this comes before
+    // whatever another block reports; this one waits for nothing before it.
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = 0;
     own.store(a, tokens, st->tops, (float*)extra);
     fence_async_smem();                  // the tensor core reads what was stored here

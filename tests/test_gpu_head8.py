@@ -313,3 +313,26 @@ def test_a_checked_product_is_the_product():
     with pytest.raises(binding.PctcError) as e:
         binding.matmul_i8(a, b, status=word, check_status=True)
     assert e.value.status == 6
+
+
+@pytest.mark.parametrize("m,n,k,dtype", [
+    (16, 256, 32_768, FP), (256, 256, 32_768, BF),                # behind their quantization, one CTA and a pair
+    (1, 128, 6016, FP), (1, 128, 6016, BF)])                      # one CTA that quantizes its token itself
+def test_logits_report_a_wait_that_runs_out_whatever_the_status_word_held(lib, m, n, k, dtype):
+    """As above: 47 blocks of k take an SM some 12,000 cycles at 64 bytes a cycle, 256 take more, and the limit is 3,000."""
+    from paper_2609_33645_b200 import build
+    short = lib.load_variant(build.build_variant("shortwait"))
+    vp = lambda t: ctypes.c_void_p(t.data_ptr())                  # noqa: E731
+    x = torch.randn(m, k, generator=gen(1), device=DEV).to(dtype)
+    head = binding.quantize_rows(torch.randn(n, k, generator=gen(2), device=DEV))
+    C = torch.zeros(m, n, device=DEV)
+    p = binding.I8Problem(m, n, k, 1, k, head.q.stride(0), n, 0, 0)
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    ws = torch.full((2 * m * (k + 128) + 8192,), 255, dtype=torch.uint8, device=DEV)
+    for _ in range(5):
+        assert short.pctc_i8_logits(ctypes.byref(p), vp(x), int(dtype == FP), vp(head.q), vp(head.scales), None, vp(C), vp(ws),
+                                    ctypes.c_size_t(ws.numel()), stream) == 0
+        host = ctypes.c_int32(0)
+        assert short.pctc_workspace_status(vp(ws), stream, ctypes.byref(host)) == 6 and host.value in (1, 2, 3, 4)
+        torch.cuda.synchronize()                                  # the kernel has returned and the context is intact
+    check(binding.quantized_logits(x, head, dtype=FP, check_status=True), *product(binding.QuantizedHead(*quantized(x)), head))
