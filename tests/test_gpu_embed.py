@@ -268,3 +268,66 @@ def test_the_gradient_of_a_tied_head():
     binding.embed_grad(t, g, dW=r["dW"], scale=8.0, accumulate=True)
     check_grad(r["dW"], t, g, 2048, 8.0, before)
     assert H.rel_fro(before.double().cpu().numpy(), H.run_oracle(batch)["dW"]) < 1e-2
+
+
+def around(V, D, dtype, left, right, value):
+    """A [V, D] view in the middle of a buffer of `value`, and a mask of what lies around it."""
+    whole = torch.full((V + 2, D + left + right), value, device=DEV, dtype=dtype)
+    outside = torch.ones(whole.shape, dtype=torch.bool, device=DEV)
+    outside[1:-1, left:left + D] = False
+    return whole, whole[1:-1, left:left + D], outside
+
+
+@pytest.mark.parametrize("M", [1, 37, 255, 256, 257])
+@pytest.mark.parametrize("D", [1023, 1024, 1025, 1026, 2050, 2056])
+@pytest.mark.parametrize("dtype,to", [(BF, BF), (FP, FP), (BF, FP), (FP, BF)])
+def test_gradient_of_few_tokens_in_one_and_several_slices(M, D, dtype, to):
+    """Up to 256 tokens are one launch of blocks that have up to 1,024 columns each; 257 are sorted."""
+    for V, hot in ((90, 0.0), (5003, 0.5), (1, 0.0)):
+        t, g = ids((M,), V, 3, 0.2, hot), rows(M, D, dtype, 4)
+        dW = binding.embed_grad(t, g, V, scale=0.7, dtype=to)["dW"]
+        check_grad(dW, t, g, V, 0.7)
+        given = torch.full((V, D), float("nan"), device=DEV, dtype=to)
+        assert torch.equal(binding.embed_grad(t, g, dW=given, scale=0.7)["dW"], dW)
+
+
+@pytest.mark.parametrize("M", [1, 37, 255, 256, 257])
+@pytest.mark.parametrize("D,left,right", [(64, 8, 8), (61, 3, 2), (1025, 8, 7), (2050, 1, 1), (2056, 0, 8), (2048, 8, 0)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_gradient_of_few_tokens_with_strides(M, D, left, right, dtype):
+    V = 301
+    t, g = ids((M,), V, 5, 0.1), rows(M, D, dtype, 6, pad=left + right, shift=left)
+    whole, dW, outside = around(V, D, dtype, left, right, 3.0)
+    binding.embed_grad(t, g, dW=dW)
+    check_grad(dW, t, g, V, 1.0)
+    assert bool((whole[outside] == 3).all())
+
+
+@pytest.mark.parametrize("M", [1, 37, 255, 256, 257])
+@pytest.mark.parametrize("D,left,right", [(64, 0, 0), (63, 0, 0), (1025, 4, 3), (2050, 0, 0), (2056, 8, 8)])
+@pytest.mark.parametrize("dtype,to", [(BF, BF), (FP, FP), (BF, FP)])
+def test_gradient_of_few_tokens_adds_to_what_is_there(M, D, left, right, dtype, to):
+    V = 301
+    t, g = ids((M,), V, 7, 0.1, 0.3), rows(M, D, dtype, 8)
+    there = torch.zeros(V, dtype=torch.bool, device=DEV)
+    there[t[t >= 0].long()] = True
+    whole, dW, outside = around(V, D, to, left, right, 3.0)
+    dW.copy_(torch.randn(V, D, generator=gen(9), device=DEV))
+    dW[~there] = float("nan")                                     # rows without a token are not even read
+    base = dW.clone()
+    binding.embed_grad(t, g, dW=dW, scale=0.5, accumulate=True)
+    assert bool(dW[~there].isnan().all()) and bool((whole[outside] == 3).all())
+    check_grad(torch.where(there[:, None], dW, 0.0), t, g, V, 0.5, torch.where(there[:, None], base, 0.0))
+
+
+@pytest.mark.parametrize("M", [200, 3000])
+def test_gradient_is_the_one_that_autograd_takes(M):
+    """In 64 bits, through torch's own lookup."""
+    V, D = 301, 72
+    t, g = ids((M,), V, 10, 0.0), rows(M, D, FP, 11)
+    W = torch.randn(V, D, generator=gen(12), device=DEV, dtype=torch.float64, requires_grad=True)
+    (torch.nn.functional.embedding(t.long(), W) * 1.5).backward(g.double())
+    dW = binding.embed_grad(t, g, V, scale=1.5)["dW"]
+    mags = want_grad(t, g, V, 1.5)[1]
+    count = torch.bincount(t.long(), minlength=V)[:, None]
+    assert bool(((dW.double() - W.grad).abs() <= (count + 1) * EPS * mags + TINY).all())
