@@ -336,3 +336,33 @@ def test_logits_report_a_wait_that_runs_out_whatever_the_status_word_held(lib, m
         assert short.pctc_workspace_status(vp(ws), stream, ctypes.byref(host)) == 6 and host.value in (1, 2, 3, 4)
         torch.cuda.synchronize()                                  # the kernel has returned and the context is intact
     check(binding.quantized_logits(x, head, dtype=FP, check_status=True), *product(binding.QuantizedHead(*quantized(x)), head))
+
+
+@pytest.mark.parametrize("dtype,V,beams", [(FP, 1000, 4), (BF, 3001, 6)])
+def test_recognition_in_8_bits_against_64_bits_and_the_oracles_search(dtype, V, beams):
+    """The best classes of the product in 64 bits and a search on the host.  A log-probability is within 1e-5 + 16 EPS of the
+    largest logit (as above), a score within that for each of its frames.  A frame's log-sum-exp shifts all its classes, and all
+    hypotheses, alike; what may change an order are the logits' four roundings and that of the subtraction, on both sides: 10 EPS."""
+    from oracle import pruned_ctc_oracle as O
+    lengths, D, blank = [25, 9, 1], 64, 0
+    hidden = torch.randn(3, 25, D, generator=gen(3), device=DEV).to(dtype)
+    head = binding.quantize_rows((torch.randn(V, D, generator=gen(4), device=DEV) / 4).to(dtype))
+    bias = torch.randn(V, generator=gen(5), device=DEV).to(dtype)
+    bias[blank] += 6.0
+    got = binding.beam_decode(hidden, head, bias, lengths, blank, beams, k=8)
+    assert binding.workspace_status(got["workspace"]) == 0
+    _, z = product(binding.QuantizedHead(*quantized(hidden.view(-1, D))), head, bias)
+    best = torch.log_softmax(z, -1).view(3, 25, V).topk(9)
+    near, apart = 1e-5 + 16 * EPS * float(z.abs().max()), 10 * EPS * float(z.abs().max())
+    for n, T in enumerate(lengths):
+        val = best.values[n, :T]
+        assert bool((val[:, :-1] - val[:, 1:] > apart).all())     # the eight are in no doubt, nor is their order
+        classes, logprobs = best.indices[n, :T, :8].int().cpu().numpy(), val[:, :8].float().cpu().numpy()
+        want, bad = O.prefix_beam_search(classes, logprobs, T, blank, beams + 1)
+        want = want[:beams + 1]
+        assert not bad and len(want) > 1 and all(a[1] - b[1] > T * apart for a, b in zip(want, want[1:]))
+        exact, _ = O.prefix_beam_search(classes, logprobs, T, blank, beams)
+        for b in range(min(beams, len(exact))):
+            labels, score = exact[b]
+            assert got["tokens"][n, b, : len(labels)].tolist() == labels and int(got["token_lengths"][n, b]) == len(labels)
+            assert abs(float(got["scores"][n, b]) - score) <= T * near + 2.0 ** -22 * abs(score)
