@@ -765,11 +765,12 @@ def embed(tokens, W, *, scale=1.0, dtype=None, out=None):
 def embed_grad(tokens, grad, vocab=None, *, dW=None, scale=1.0, accumulate=False, dtype=None, workspace=None):
     """The gradient of embed with respect to W: dW[v] = scale * the sum of grad[i] over all i with tokens[i] == v.
 
-    grad [*tokens.shape, D] bf16 or fp32, its rows one stride apart (an expanded view is refused: make it contiguous).  dW [V,D] is written whole (rows without a token: zeros), or, with
-    accumulate=True, added to: a tied head's gradient as pruned_ctc_fwd_bwd has left it.  Without dW one is made for `vocab`
-    rows, of type `dtype` (default grad's).  Sums are fp32 in a fixed order: repeated calls agree bit for bit.  Returns a
-    dict: dW and the workspace (the given one, or a new one where that was too small), which later calls on the same stream may
-    take.  A written dW's version counts up.
+    grad [*tokens.shape, D] bf16 or fp32, its rows one stride apart (an expanded view, as autograd hands back from a sum, is
+    refused: make it contiguous).  dW [V,D] is written whole (rows without a token: zeros), or, with accumulate=True, added
+    to: a tied head's gradient as pruned_ctc_fwd_bwd has left it.  Without dW one is made for `vocab` rows, of type `dtype`
+    (default grad's).  Sums are fp32 in a fixed order: repeated calls agree bit for bit.  Returns a dict: dW and the
+    workspace (the given one, or a new one where that was too small), which later calls on the same stream may take.  A
+    written dW's version counts up.
     """
     dW, workspace = _native().embed_grad(tokens, grad, vocab, dW, scale, accumulate, dtype, workspace)
     return dict(dW=dW, workspace=workspace)

@@ -13,8 +13,8 @@
 //                  order (in two steps where they are many).
 //   k_embed_grad_few  few tokens: all of it in one launch.  A CTA fills its rows with zeros, finds its own among all
 //                  tokens meanwhile and writes their sums behind the zeros.
-// Both directions are bound by HBM where they are large (32,768 tokens of 151,936 x 2,560 bf16: 51.5 us, 5.9 TB/s; the
-// gradient of as many into 151,936 x 1,024: 70 us, 5.2 TB/s), by their launches where they are small (64 tokens: 2.7 us; 1,999 into
+// Both directions are bound by HBM where they are large (32,768 tokens of 151,936 x 2,560 bf16: 48.5 us, 6.2 TB/s; the
+// gradient of as many into 151,936 x 1,024: 69 us, 5.4 TB/s), by their launches where they are small (64 tokens: 1.8 us; 1,999 into
 // 5,003 x 510: 12 us, two launches and the chain from a token to its last partial sum).
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"

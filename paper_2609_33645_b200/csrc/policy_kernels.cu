@@ -10,8 +10,8 @@
 // reads every value once.  Few values are done by one cluster in one launch (k_policy_small).  Differences are exact (two
 // fp32 numbers), gains and sums 64 bits, in a fixed order; KL terms, which never cancel one another, and gradients 32 bits, or 64
 // where fp32 does not hold them before they have their weight (far_values).  Large calls are
-// bound by the arithmetic of a token and its loads, about alike (1M tokens with a mask: 14.5 us, of which 2.6 us are bytes at
-// HBM's rate), small ones by the launches (128 x 501: 7.8 us) and the length of one token's chain (64 values: 3.9 us).
+// bound by the arithmetic of a token and its loads, about alike (1M tokens with everything: 14.5 us, of which 2.6 us are bytes at
+// HBM's rate), small ones by the launches (128 x 501: 7.3 us) and the length of one token's chain (64 values: 3.8 us).
 #include "../../include/prunedctc.h"
 #include "pctc_internal.h"
 
