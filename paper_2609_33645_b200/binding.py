@@ -782,8 +782,8 @@ def dropout(x, p, seed, *, offset=0, step=None, residual=None, out=None):
 
     The mask is a function of seed, offset (integers, taken modulo 2^64) and a value's index alone (prunedctc.h has the
     formula); it is never stored.  p counts in steps of 1/65536, and the scale is exact for the step taken.  x bf16 or fp32
-    [..., D] whose rows lie one stride apart (an expanded view is refused), residual and out likewise; out may be x or residual.  step: one int64 on the
-    device that is added to offset, for calls captured into a CUDA graph.  Not recorded by autograd; a written `out`'s
+    [..., D] whose rows lie one stride apart (an expanded view is refused), residual and out likewise; out may be x or
+    residual.  step: one int64 on the device that is added to offset, for calls captured into a CUDA graph.  Not recorded by autograd; a written `out`'s
     version counts up.
     """
     return _native().dropout(x, p, seed, offset, step, residual, out)
@@ -852,7 +852,8 @@ def _raise_status(word) -> None:
 def matmul_i8(a, b, *, bias=None, dtype=None, status=None, check_status=False):
     """C[i,j] = sum_k a.q[i,k] b.q[j,k] * a.scales[i] * b.scales[j] + bias[j] for two QuantizedHeads (rows of tokens and of
     channels), fp32 or bf16 by `dtype`.  status: zeroed int32 CUDA tensor that receives a code if a bounded device wait
-    gives up; check_status=True waits for the stream and raises then.  With neither, results that are incomplete for that reason go unnoticed.
+    gives up; check_status=True waits for the stream and raises then.  With neither, results that are incomplete for that
+    reason go unnoticed.
     """
     if check_status and status is None:
         import torch
